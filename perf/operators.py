@@ -11,6 +11,7 @@ the calls of `paper_2501_13986_amd.binding`.
 """
 from __future__ import annotations
 
+from functools import lru_cache
 from math import log, pi, sqrt
 
 import torch
@@ -96,15 +97,20 @@ def _seconds(case):
 # ---- the rows' description ----------------------------------------------------------------------------------------------
 
 def _segments(case):
-    """(mul, 2l+1, whether invariant, first column) of every segment, the gates as a last one of scalars where there are any."""
+    """(mul, 2l+1, whether invariant, first column) of every segment; behind them the gates, scalars, one segment for each of the
+    segments that are not invariant."""
     out, at = [], 0
     for t in IRREPS[case["irreps"]].split("+"):
         mul, ir = t.split("x")
         n = 2 * int(ir[:-1]) + 1
         out.append((int(mul), n, ir == "0e", at))
         at += int(mul) * n
-    gates = sum(s[0] for s in out if not s[2]) if case["gated"] else 0
-    return out + ([(gates, 1, True, at)] if gates else []), at, at + gates
+    gates, dim_y = [], at
+    for s in out:
+        if case["gated"] and not s[2]:
+            gates.append((s[0], 1, True, at))
+            at += s[0]
+    return out + gates, dim_y, at
 
 
 # ---- inputs -------------------------------------------------------------------------------------------------------------
@@ -144,6 +150,14 @@ def _inputs(case, seed):
     return s
 
 
+@lru_cache(None)
+def _handle(irreps, groups, act, gated, dtype, layout):
+    """A program makes its normalisation when the model is defined and keeps it."""
+    from paper_2501_13986_amd import binding as b
+    return b.Norm(IRREPS[irreps], groups=groups, act=act, gated=gated, eps=EPS, dtype=b.CGTP_F64 if dtype == "f64" else b.CGTP_F32,
+                  device=0, flags=b.CGTP_IR_MUL if layout == "ir_mul" else b.CGTP_MUL_IR)
+
+
 def prepare(case, seed):
     s = _inputs(case, seed)
     s["case"] = case
@@ -162,9 +176,7 @@ def prepare(case, seed):
         s["gWg"], s["gWu"] = like(s["Wg"]), like(s["Wu"])
         s["gbg"], s["gbu"] = (like(s["bg"]), like(s["bu"])) if case["bias"] else (None, None)
         return s
-    s["norm"] = b.Norm(IRREPS[case["irreps"]], groups=case["groups"], act=s["act"], gated=case["gated"], eps=EPS,
-                       dtype=b.CGTP_F64 if case["dtype"] == "f64" else b.CGTP_F32, device=0,
-                       flags=b.CGTP_IR_MUL if case["layout"] == "ir_mul" else b.CGTP_MUL_IR)
+    s["norm"] = _handle(case["irreps"], case["groups"], s["act"], case["gated"], case["dtype"], case["layout"])
     dim_y = _segments(case)[1]
     s["y"] = torch.zeros((s["x"].shape[0], dim_y), dtype=s["x"].dtype, device="cuda")
     s["gx"], s["gweight"], s["gbias"] = zeros(s["x"]), like(s["weight"]), like(s["bias"])
@@ -274,8 +286,7 @@ def _norm(s):
     op, G, out = case["op"], case["groups"], ()
     graph, S = _rows(case, s["ptr"])
     stats = _statistics(case, x, s["ptr"]) if op != "bwd" else s["stats"]
-    hat, lin, w_at, b_at = [], [], 0, 0      # normalised values, the same with weight and bias
-    weights = []
+    hat, lin, weights, w_at, b_at = [], [], [], 0, 0      # normalised values, the same with weight and bias
     for k, seg in enumerate(segs):
         mul, _, inv, _ = seg
         t = _of_rows(stats[:, k], graph)
@@ -284,10 +295,10 @@ def _norm(s):
         v = hat[-1] * weights[-1]
         lin.append(v + s["bias"][b_at:b_at + mul].reshape(1, G, -1, 1) if inv else v)
         w_at, b_at = w_at + mul, b_at + (mul if inv else 0)
-    gates = case["gated"] and len(segs) > 0 and segs[-1][3] == dim_y and dim_x > dim_y
-    sig = 1 / (1 + torch.exp(-lin[-1].reshape(N, -1))) if gates else None
-    real = segs[:-1] if gates else segs
-    y, gx, glin, gate_at, ggate = x.new_zeros((x.shape[0], dim_y)), torch.zeros_like(x), [], 0, []
+    gates = dim_x > dim_y
+    real = [t for t in segs if t[3] < dim_y]
+    y, gx, glin, ggate = x.new_zeros((x.shape[0], dim_y)), torch.zeros_like(x), [], []
+    gate_at = 0
     for k, seg in enumerate(real):
         mul, n, inv, at = seg
         gy = _columns(case, s["gy"], seg) if op != "fwd" else None
@@ -295,12 +306,12 @@ def _norm(s):
             a, d = _act(lin[k], case["act"])
             glin.append(gy * d if op != "fwd" else None)
         elif gates:
-            q = sig[:, gate_at:gate_at + mul].reshape(N, G, -1, 1)
+            q = 1 / (1 + torch.exp(-lin[len(real) + gate_at]))
+            gate_at += 1
             a = lin[k] * q
             if op != "fwd":
                 glin.append(gy * q)
-                ggate.append(((gy * lin[k]).sum(3, keepdim=True) * q * (1 - q)).reshape(N, mul))
-            gate_at += mul
+                ggate.append((gy * lin[k]).sum(3, keepdim=True) * q * (1 - q))
         else:
             a = lin[k]
             glin.append(gy)
@@ -310,8 +321,7 @@ def _norm(s):
         out += (y, stats)
     if op == "fwd":
         return out
-    if gates:
-        glin.append(torch.cat(ggate, 1).reshape(N, G, -1, 1))
+    glin += ggate
     rows = _per_graph(torch.ones(N, 1, dtype=torch.float64, device=x.device), graph, S).clamp(min=1)
     gw, gb = [], []
     for k, seg in enumerate(segs):
@@ -409,16 +419,15 @@ def _exact_norm(case, s):
             t = t + bias[nb:nb + mul][channel]
         pieces.append((t, channel))
         nw, nb = nw + mul, nb + (mul if inv else 0)
-    y, at = [], 0
-    gate = pieces[-1][0] if dim_x > dim_y else None
-    for (mul, n, inv, _), (t, channel) in zip(segs, pieces):
-        if gate is not None and t is gate:
+    y = []
+    gates = [t for (_, _, _, at), (t, _) in zip(segs, pieces) if at >= dim_y]
+    for (_, _, inv, at), (t, channel) in zip(segs, pieces):
+        if at >= dim_y:
             break
         if inv:
             t = _act64(t, case["act"])
-        elif gate is not None:
-            t = t * torch.sigmoid(gate[:, at:at + mul])[:, channel]
-            at += mul
+        elif gates:
+            t = t * torch.sigmoid(gates.pop(0))[:, channel]
         y.append(t)
     y = torch.cat(y, 1)
     out = ()
