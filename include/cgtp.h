@@ -306,6 +306,71 @@ cgtp_status cgtp_csr_from_coo_async(const int64_t* recv, const int64_t* send, in
                                     int64_t* t_perm, void* workspace, size_t workspace_bytes, int32_t* bad_flag,
                                     void* hip_stream);
 
+/* ---- layer operators around the convolution --------------------------------------------------- */
+
+/* Activations.  GELU is t Phi(t) with the normal distribution function itself. */
+typedef enum { CGTP_ACT_NONE = 0, CGTP_ACT_SILU = 1, CGTP_ACT_GELU = 2, CGTP_ACT_SIGMOID = 3, CGTP_ACT_TANH = 4 } cgtp_act;
+
+/* Gated feed-forward block, both projections, the activation and the product in one kernel:
+ *     out = act(x Wg + bg) * (x Wu + bu)
+ * x [rows, d_in], Wg, Wu [d_in, d_out], bg, bu [d_out] (both or neither; NULL: no bias), out [rows, d_out].  With d_out = n_w of a
+ * plan it forms the per-edge weights that a convolution reads from the edges' scalars.  ld_x and ld_out are the elements from one
+ * row of x (out) to the next, at least d_in (d_out): rows may be columns of wider ones; what lies between them is not touched.
+ * dtype: cgtp_dtype; act: cgtp_act.  fp32 products run on the matrix cores with each factor as the sum of three
+ * bf16 numbers, which hold its 24 bits, and 32-bit sums: the result is as far from the exact one as that of fp32 products.
+ * Allocates nothing; no workspace.  rows, d_in, d_out < 2^31, and d_in, d_out > 0. */
+cgtp_status gated_forward(const void* x, const void* Wg, const void* Wu, const void* bg, const void* bu, void* out,
+                          int64_t rows, int64_t d_in, int64_t d_out, int64_t ld_x, int64_t ld_out, int32_t act,
+                          int32_t dtype, void* hip_stream);
+
+/* Gradients of gated_forward given gout = dE/dout [rows, d_out]: gx [rows, d_in], gWg, gWu [d_in, d_out] and, where the biases are
+ * given, gbg, gbu [d_out] (NULL otherwise).  The projections are formed again from x, nothing is kept from the forward call.
+ * ld_gout and ld_gx as above.  Sums over rows are formed in a fixed order (bit-identical from run to run) through `workspace`:
+ * caller-owned device memory of at least cgtp_gated_workspace_bytes(rows, d_in, d_out, dtype) bytes, 256-byte aligned (CGTP_EINVAL
+ * if it is smaller), free again for other work on hip_stream after the call.  rows == 0: the weights' gradients are zero. */
+size_t cgtp_gated_workspace_bytes(int64_t rows, int64_t d_in, int64_t d_out, int32_t dtype);
+cgtp_status gated_backward(const void* x, const void* Wg, const void* Wu, const void* bg, const void* bu, const void* gout,
+                           void* gx, void* gWg, void* gWu, void* gbg, void* gbu, int64_t rows, int64_t d_in, int64_t d_out,
+                           int64_t ld_x, int64_t ld_gout, int64_t ld_gx, int32_t act, int32_t dtype, void* workspace,
+                           size_t workspace_bytes, void* hip_stream);
+
+/* Group normalisation of irreps rows with the activation and the gates of an equivariant layer.
+ *
+ * The channels of every segment are split into `groups` equal groups of neighbours.  Over the rows of one sample, the channels of
+ * one group and the components m, a 0e segment has mean mu and variance var; every other segment, which may not be shifted, has
+ * mu = 0 and var = the mean square.  With r = 1 / sqrt(var + eps) and u the channel:
+ *     0e segments:   y = act(weight[u] (x - mu) r + bias[u])
+ *     the others:    y = weight[u] x r, times sigmoid(weight[g] (x_g - mu_g) r_g + bias[g]) with the flag CGTP_NORM_GATED, where x_g
+ *                    is the channel's gate
+ * With CGTP_NORM_GATED a row of x continues behind its irreps with one 0e segment of gates for every segment that is not 0e, of
+ * its multiplicity, in the same order; they are normalised like the 0e segments.  y has the irreps alone.
+ * weight has one number per channel, bias one per 0e channel, gates behind the others in both.  stats [samples, segments, groups, 2]
+ * holds mu and r, the segments of gates behind the others.
+ * The layout flags (CGTP_MUL_IR, CGTP_IR_MUL) are those of plans and mean the same. */
+typedef struct cgtp_norm cgtp_norm; /* opaque; owned by the library until cgtp_norm_destroy */
+enum { CGTP_NORM_GATED = 2u };      /* flag of cgtp_norm_create, beside the layout */
+
+/* `groups` has to divide every multiplicity (CGTP_EINVAL); l <= 8, at most 64 segments, multiplicities up to 65536
+ * (CGTP_EUNSUPPORTED).  eps > 0.  `device` as in cgtp_plan_create. */
+cgtp_status cgtp_norm_create(const char* irreps, int32_t groups, int32_t act, double eps, int32_t dtype, int32_t device,
+                             uint32_t flags, cgtp_norm** out);
+cgtp_status cgtp_norm_destroy(cgtp_norm* norm);
+/* which: 0 = columns of x, 1 = columns of y, 2 = number of weights, 3 = number of biases, 4 = numbers in stats per sample. */
+int64_t cgtp_norm_dim(const cgtp_norm* norm, int32_t which);
+/* Workspace of norm_forward (backward == 0) or norm_backward for N rows in S samples; ptr: whether ptr is given. */
+size_t cgtp_norm_workspace_bytes(const cgtp_norm* norm, int64_t N, int64_t S, int32_t ptr, int32_t backward);
+/* x [N, dim 0], y [N, dim 1], stats [S, dim 4].  ptr (int64 device array [S+1], not decreasing): sample s is the rows
+ * ptr[s] .. ptr[s+1] - 1; rows in front of ptr[0] and from ptr[S] on belong to none and keep what y holds there.  A sample without
+ * rows has mu = 0 and r = 1 / sqrt(eps).  NULL: every row is a sample (S has to be N).  Indices outside [0, N] are taken for the
+ * nearest one inside; where ptr decreases the results are unspecified, within the arrays.  Allocates nothing; deterministic. */
+cgtp_status norm_forward(const cgtp_norm* norm, const void* x, const void* weight, const void* bias, void* y, void* stats,
+                         int64_t N, int64_t S, const int64_t* ptr, void* workspace, size_t workspace_bytes, void* hip_stream);
+/* Gradients of norm_forward given gy = dE/dy [N, dim 1] and the stats that it wrote: gx [N, dim 0] (rows of no sample keep what it
+ * holds), gweight [dim 2], gbias [dim 3].  Deterministic. */
+cgtp_status norm_backward(const cgtp_norm* norm, const void* x, const void* weight, const void* bias, const void* gy,
+                          const void* stats, void* gx, void* gweight, void* gbias, int64_t N, int64_t S, const int64_t* ptr,
+                          void* workspace, size_t workspace_bytes, void* hip_stream);
+
 /* Message of the last error on this thread (valid until the next failing call on it). */
 const char* cgtp_last_error(void);
 

@@ -12,6 +12,7 @@ Everything here is the plain definition evaluated in fp64 with numpy:
   so3.py     real spherical harmonics, Wigner D matrices              (paper Sec. 2.1)
   tp.py      TP(P, x, y, W) of Eq. 1, its gradients (Sec. 3.3)        (paper Eq. 1, Sec. 3.3)
   conv.py    CSR construction, graph convolution of Eq. 4, gradients  (paper Sec. 3.5)
+  layer.py   gated feed-forward block, group normalisation of irreps rows (around the convolution)
 
 Parity pins (what each function is checked against, apart from itself) live in
 tests/test_oracle_*.py.  Functions whose output cannot be pinned to anything but a

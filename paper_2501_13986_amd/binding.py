@@ -18,6 +18,8 @@ CGTP_UVU, CGTP_UVW = 0, 1
 CGTP_MUL_IR, CGTP_IR_MUL = 0, 1
 K_TP_FWD, K_TP_BWD, K_CONV_FWD, K_CONV_BWD, K_CONV_FWD_ATOMIC, K_CONV_BWD_ATOMIC, K_TP_DBL_BWD = 0, 1, 2, 3, 4, 5, 6
 K_CONV_DBL_FWD, K_CONV_DBL_BWD = 7, 8
+ACT_NONE, ACT_SILU, ACT_GELU, ACT_SIGMOID, ACT_TANH = 0, 1, 2, 3, 4
+CGTP_NORM_GATED = 2
 STATUS = {0: "CGTP_OK", 1: "CGTP_EINVAL", 2: "CGTP_EUNSUPPORTED", 3: "CGTP_ECOMPILE", 4: "CGTP_ERUNTIME", 5: "CGTP_ENOMEM"}
 
 EXPORTS = [
@@ -26,6 +28,8 @@ EXPORTS = [
     "tp_forward", "tp_backward", "tp_double_backward", "conv_forward", "conv_forward_static", "conv_backward", "conv_forward_perm", "conv_backward_perm", "conv_double_backward", "conv_double_backward_ws",
     "cgtp_conv_double_workspace_bytes", "conv_forward_atomic", "conv_backward_atomic",
     "cgtp_csr_from_coo", "cgtp_csr_from_coo_async", "cgtp_csr_workspace_bytes", "cgtp_last_error", "cgtp_check_code_object",
+    "gated_forward", "gated_backward", "cgtp_gated_workspace_bytes",
+    "cgtp_norm_create", "cgtp_norm_destroy", "cgtp_norm_dim", "cgtp_norm_workspace_bytes", "norm_forward", "norm_backward",
 ]
 
 
@@ -92,6 +96,18 @@ def lib() -> C.CDLL:
     L.cgtp_csr_workspace_bytes.argtypes = [i64, i64]
     L.cgtp_csr_workspace_bytes.restype = C.c_size_t
     L.cgtp_csr_from_coo_async.argtypes = [vp, vp, i64, i64, vp, vp, vp, vp, vp, vp, C.c_size_t, vp, vp]
+    L.gated_forward.argtypes = [vp] * 6 + [i64] * 5 + [i32, i32, vp]
+    L.gated_backward.argtypes = [vp] * 11 + [i64] * 6 + [i32, i32, vp, C.c_size_t, vp]
+    L.cgtp_gated_workspace_bytes.argtypes = [i64, i64, i64, i32]
+    L.cgtp_gated_workspace_bytes.restype = C.c_size_t
+    L.cgtp_norm_create.argtypes = [C.c_char_p, i32, i32, C.c_double, i32, i32, C.c_uint32, C.POINTER(vp)]
+    L.cgtp_norm_destroy.argtypes = [vp]
+    L.cgtp_norm_dim.argtypes = [vp, i32]
+    L.cgtp_norm_dim.restype = i64
+    L.cgtp_norm_workspace_bytes.argtypes = [vp, i64, i64, i32, i32]
+    L.cgtp_norm_workspace_bytes.restype = C.c_size_t
+    L.norm_forward.argtypes = [vp] * 6 + [i64, i64, vp, vp, C.c_size_t, vp]
+    L.norm_backward.argtypes = [vp] * 9 + [i64, i64, vp, vp, C.c_size_t, vp]
     _lib = L
     return L
 
@@ -314,3 +330,160 @@ def cgtp_csr_from_coo_async(recv, send, V: int, out, workspace, bad_flag=None, t
                                          _ptr(t_row_ptr) if transpose else 0, _ptr(t_perm) if transpose else 0,
                                          _ptr(workspace), workspace.numel() * workspace.element_size(), _ptr(bad_flag), _stream()))
     return out
+
+
+# ---- layer operators around the convolution ---------------------------------------------------------------------------
+
+def _bad(msg: str):
+    raise CgtpError(1, msg)
+
+
+def _operand(t, name: str, shape: Tuple, like=None, optional: bool = False) -> int:
+    """Checks a contiguous operand (like: the tensor whose type and device it shares) and returns its address."""
+    if t is None:
+        return 0 if optional else _bad(f"{name} is missing")
+    if tuple(t.shape) != tuple(shape):
+        _bad(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if not t.is_contiguous():
+        _bad(f"{name} must be contiguous")
+    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+        _bad(f"{name}: {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
+    return t.data_ptr()
+
+
+def _row_operand(t, name: str, shape: Tuple, like=None) -> Tuple[int, int]:
+    """The same for rows that may be columns of wider rows: address and elements from one row to the next."""
+    if t is None:
+        _bad(f"{name} is missing")
+    if tuple(t.shape) != tuple(shape):
+        _bad(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if like is not None and (t.dtype != like.dtype or t.device != like.device):
+        _bad(f"{name}: {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
+    if shape[1] > 1 and t.stride(1) != 1 and t.numel() > 0:
+        _bad(f"{name}: the elements of a row must be neighbours")
+    return t.data_ptr(), t.stride(0) if shape[0] > 1 else shape[1]
+
+
+def _on_current_device(t):
+    """The kernels go to the current stream of the current device: data elsewhere is refused."""
+    import torch
+    if t.device.type != "cuda" or t.device.index != torch._C._cuda_getDevice():
+        _bad(f"tensors are on {t.device}, the current device is cuda:{torch._C._cuda_getDevice() if torch.cuda.is_available() else '(none)'}")
+
+
+def _dtype_of(t) -> int:
+    import torch
+    if t.dtype not in (torch.float32, torch.float64):
+        _bad(f"float32 or float64 expected, got {t.dtype}")
+    return CGTP_F64 if t.dtype == torch.float64 else CGTP_F32
+
+
+def _scratch(n: int, like):
+    """Workspace of a call: torch's, given back to its allocator on the current stream, part of the graph's pool under
+    torch.cuda.graph."""
+    import torch
+    return torch.empty(n, dtype=torch.uint8, device=like.device) if n else None
+
+
+def gated_forward(x, Wg, Wu, out, bg=None, bu=None, act: int = ACT_SILU):
+    """out = act(x Wg + bg) * (x Wu + bu).  x [rows, d_in], Wg, Wu [d_in, d_out], bg, bu [d_out] or None, out [rows, d_out]; x and
+    out may be columns of wider rows.  out must not overlap an input."""
+    dt = _dtype_of(x)
+    if x.dim() != 2 or Wg.dim() != 2:
+        _bad("x and Wg must have two dimensions")
+    (rows, k), n = x.shape, Wg.shape[1]
+    px, ldx = _row_operand(x, "x", (rows, k))
+    po, ldo = _row_operand(out, "out", (rows, n), x)
+    w = [_operand(Wg, "Wg", (k, n), x), _operand(Wu, "Wu", (k, n), x), _operand(bg, "bg", (n,), x, True), _operand(bu, "bu", (n,), x, True)]
+    _on_current_device(x)
+    _check(lib().gated_forward(px, *w, po, rows, k, n, ldx, ldo, act, dt, _stream()))
+    return out
+
+
+def gated_backward(x, Wg, Wu, gout, gx, gWg, gWu, bg=None, bu=None, gbg=None, gbu=None, act: int = ACT_SILU):
+    """Gradients of gated_forward given gout [rows, d_out]; gbg, gbu are given where bg, bu are.  x, gout and gx may be columns of
+    wider rows.  No output may overlap an input."""
+    dt = _dtype_of(x)
+    if x.dim() != 2 or Wg.dim() != 2:
+        _bad("x and Wg must have two dimensions")
+    (rows, k), n = x.shape, Wg.shape[1]
+    px, ldx = _row_operand(x, "x", (rows, k))
+    pg, ldg = _row_operand(gout, "gout", (rows, n), x)
+    pgx, ldgx = _row_operand(gx, "gx", (rows, k), x)
+    w = [_operand(Wg, "Wg", (k, n), x), _operand(Wu, "Wu", (k, n), x), _operand(bg, "bg", (n,), x, True), _operand(bu, "bu", (n,), x, True)]
+    g = [_operand(gWg, "gWg", (k, n), x), _operand(gWu, "gWu", (k, n), x), _operand(gbg, "gbg", (n,), x, True), _operand(gbu, "gbu", (n,), x, True)]
+    _on_current_device(x)
+    L = lib()
+    nb = L.cgtp_gated_workspace_bytes(rows, k, n, dt)
+    ws = _scratch(nb, x)
+    _check(L.gated_backward(px, *w, pg, pgx, *g, rows, k, n, ldx, ldg, ldgx, act, dt, _ptr(ws), nb, _stream()))
+    return gx, gWg, gWu, gbg, gbu
+
+
+class Norm:
+    """Owns a cgtp_norm: the group normalisation of rows of `irreps` with activation and gates (include/cgtp.h).  device as for
+    Plan; flags: the layout."""
+
+    def __init__(self, irreps: str, groups: int = 1, act: int = ACT_SILU, gated: bool = True, eps: float = 1e-5, dtype: int = CGTP_F32,
+                 device: int = 0, flags: int = CGTP_MUL_IR):
+        L, h = lib(), C.c_void_p()
+        _check(L.cgtp_norm_create(irreps.encode(), groups, act, eps, dtype, device, flags | (CGTP_NORM_GATED if gated else 0), C.byref(h)))
+        self._h, self.dtype, self.groups = h, dtype, groups
+        self.dim_x, self.dim_y, self.n_w, self.n_b, self.n_stat = (L.cgtp_norm_dim(h, t) for t in range(5))
+
+    def close(self):
+        if getattr(self, "_h", None):
+            lib().cgtp_norm_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:      # interpreter shutdown: module globals may already be gone
+            pass
+
+
+def _norm_operands(norm: Norm, x, weight, bias, stats, ptr):
+    if _dtype_of(x) != norm.dtype:
+        _bad(f"x is {x.dtype}, the normalisation was made for {'float64' if norm.dtype == CGTP_F64 else 'float32'}")
+    if x.dim() != 2:
+        _bad("x must have two dimensions")
+    N = x.shape[0]
+    S, pp = N, 0
+    if ptr is not None:
+        import torch
+        if ptr.dtype != torch.int64 or ptr.dim() != 1 or ptr.shape[0] < 1 or not ptr.is_contiguous() or ptr.device != x.device:
+            _bad("ptr: a contiguous int64 tensor [samples + 1] on the device of x")
+        S, pp = ptr.shape[0] - 1, ptr.data_ptr()
+    if stats is not None and stats.numel() != S * norm.n_stat:
+        _bad(f"stats: {stats.numel()} numbers, expected {S} * {norm.n_stat}")
+    ops = [_operand(x, "x", (N, norm.dim_x)), _operand(weight, "weight", (norm.n_w,), x),
+           _operand(bias, "bias", (norm.n_b,), x, norm.n_b == 0)]
+    return N, S, pp, ops, 0 if stats is None else _operand(stats, "stats", tuple(stats.shape), x)
+
+
+def norm_forward(norm: Norm, x, weight, bias, y, stats=None, ptr=None):
+    """x [N, dim_x], weight [n_w], bias [n_b], y [N, dim_y], stats: samples * n_stat numbers, or None where no backward pass follows;
+    ptr: int64 [S + 1] or None (every row a sample).  Returns (y, stats)."""
+    N, S, pp, ops, ps = _norm_operands(norm, x, weight, bias, stats, ptr)
+    py = _operand(y, "y", (N, norm.dim_y), x)
+    _on_current_device(x)
+    L = lib()
+    nb = L.cgtp_norm_workspace_bytes(norm._h, N, S, int(ptr is not None), 0)
+    ws = _scratch(nb, x)
+    _check(L.norm_forward(norm._h, *ops, py, ps, N, S, pp, _ptr(ws), nb, _stream()))
+    return y, stats
+
+
+def norm_backward(norm: Norm, x, weight, bias, gy, stats, gx, gweight, gbias, ptr=None):
+    """Gradients of norm_forward given gy [N, dim_y] and the stats that it wrote.  Returns (gx, gweight, gbias)."""
+    N, S, pp, ops, ps = _norm_operands(norm, x, weight, bias, stats, ptr)
+    out = [_operand(gx, "gx", (N, norm.dim_x), x), _operand(gweight, "gweight", (norm.n_w,), x),
+           _operand(gbias, "gbias", (norm.n_b,), x, norm.n_b == 0)]
+    pg = _operand(gy, "gy", (N, norm.dim_y), x)
+    _on_current_device(x)
+    L = lib()
+    nb = L.cgtp_norm_workspace_bytes(norm._h, N, S, int(ptr is not None), 1)
+    ws = _scratch(nb, x)
+    _check(L.norm_backward(norm._h, *ops, pg, ps, *out, N, S, pp, _ptr(ws), nb, _stream()))
+    return gx, gweight, gbias

@@ -25,10 +25,16 @@ namespace {
 
 thread_local std::string g_err;
 
-cgtp_status fail(cgtp_status s, const std::string& msg) {
+}  // namespace
+
+cgtp_status cgtp::fail(cgtp_status s, const std::string& msg) {
   g_err = msg;
   return s;
 }
+
+namespace {
+
+using cgtp::fail;
 
 #define HIP_TRY(expr)                                                                                   \
   do {                                                                                                  \

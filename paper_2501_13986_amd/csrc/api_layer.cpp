@@ -1,0 +1,282 @@
+// Entry points of the layer operators: the gated feed-forward block and the group normalisation.
+#include <algorithm>
+#include <climits>
+#include <cmath>
+#include <memory>
+#include <new>
+#include <string>
+
+#include "csr.hpp"
+#include "layer.hpp"
+#include "norm.hpp"
+
+struct cgtp_norm {
+  cgtp::Norm N;
+};
+
+namespace {
+
+using cgtp::fail;
+
+#define HIP_TRY(expr)                                                                                   \
+  do {                                                                                                  \
+    hipError_t e_ = (expr);                                                                             \
+    if (e_ != hipSuccess) return fail(CGTP_ERUNTIME, std::string(#expr) + ": " + hipGetErrorString(e_)); \
+  } while (0)
+
+bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+
+bool workspace_serves(const void* p, size_t have, size_t need) { return need == 0 || (p && have >= need && aligned(p, 256)); }
+
+cgtp_status bad_workspace(const char* query, size_t need) {
+  return fail(CGTP_EINVAL, "workspace: " + std::to_string(need) + " bytes needed (" + query + "), 256-byte aligned");
+}
+
+cgtp_status check_gated(const cgtp::GatedArgs& a, int32_t dtype) {
+  if (dtype != CGTP_F32 && dtype != CGTP_F64) return fail(CGTP_EINVAL, "dtype must be CGTP_F32 or CGTP_F64");
+  if (a.act < CGTP_ACT_NONE || a.act > CGTP_ACT_TANH) return fail(CGTP_EINVAL, "unknown activation");
+  if (a.rows < 0 || a.d_in <= 0 || a.d_out <= 0) return fail(CGTP_EINVAL, "rows must not be negative, d_in and d_out must be positive");
+  if (a.rows > INT32_MAX || a.d_in > INT32_MAX || a.d_out > INT32_MAX) return fail(CGTP_EUNSUPPORTED, "rows, d_in and d_out must be below 2^31");
+  if (a.d_in > INT32_MAX / a.d_out) return fail(CGTP_EUNSUPPORTED, "d_in * d_out must be below 2^31");
+  if ((a.bg == nullptr) != (a.bu == nullptr)) return fail(CGTP_EINVAL, "bg and bu must both be given or both be NULL");
+  // a row stride beyond this leaves no row inside the address space
+  for (int64_t ld : {a.ld_x, a.ld_out, a.ld_gout, a.ld_gx})
+    if (ld > ((int64_t)1 << 31)) return fail(CGTP_EUNSUPPORTED, "row strides must be at most 2^31");
+  return CGTP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+cgtp_status gated_forward(const void* x, const void* Wg, const void* Wu, const void* bg, const void* bu, void* out,
+                          int64_t rows, int64_t d_in, int64_t d_out, int64_t ld_x, int64_t ld_out, int32_t act,
+                          int32_t dtype, void* hip_stream) {
+  cgtp::GatedArgs a = {};
+  a.x = x; a.Wg = Wg; a.Wu = Wu; a.bg = bg; a.bu = bu; a.out = out;
+  a.rows = rows; a.d_in = d_in; a.d_out = d_out; a.ld_x = ld_x; a.ld_out = ld_out; a.act = act; a.f64 = dtype == CGTP_F64;
+  cgtp_status s = check_gated(a, dtype);
+  if (s != CGTP_OK) return s;
+  if (ld_x < d_in || ld_out < d_out) return fail(CGTP_EINVAL, "a row stride is smaller than its row");
+  if (rows == 0) return CGTP_OK;
+  if (!x || !Wg || !Wu || !out) return fail(CGTP_EINVAL, "NULL data pointer");
+  for (const void* p : {x, Wg, Wu, bg, bu, (const void*)out})
+    if (!aligned(p, 16)) return fail(CGTP_EINVAL, "data pointers must be 16-byte aligned");
+  HIP_TRY(cgtp::gated_forward(a, (hipStream_t)hip_stream));
+  return CGTP_OK;
+}
+
+size_t cgtp_gated_workspace_bytes(int64_t rows, int64_t d_in, int64_t d_out, int32_t dtype) {
+  cgtp::GatedArgs a = {};
+  a.rows = rows; a.d_in = d_in; a.d_out = d_out;
+  if (check_gated(a, dtype) != CGTP_OK || rows == 0) return 0;
+  return cgtp::gated_workspace_bytes(rows, d_in, d_out, dtype == CGTP_F64);
+}
+
+cgtp_status gated_backward(const void* x, const void* Wg, const void* Wu, const void* bg, const void* bu, const void* gout,
+                           void* gx, void* gWg, void* gWu, void* gbg, void* gbu, int64_t rows, int64_t d_in, int64_t d_out,
+                           int64_t ld_x, int64_t ld_gout, int64_t ld_gx, int32_t act, int32_t dtype, void* workspace,
+                           size_t workspace_bytes, void* hip_stream) {
+  cgtp::GatedArgs a = {};
+  a.x = x; a.Wg = Wg; a.Wu = Wu; a.bg = bg; a.bu = bu; a.gout = gout; a.gx = gx; a.gWg = gWg; a.gWu = gWu; a.gbg = gbg; a.gbu = gbu;
+  a.rows = rows; a.d_in = d_in; a.d_out = d_out; a.ld_x = ld_x; a.ld_gout = ld_gout; a.ld_gx = ld_gx; a.act = act; a.f64 = dtype == CGTP_F64;
+  cgtp_status s = check_gated(a, dtype);
+  if (s != CGTP_OK) return s;
+  if (ld_x < d_in || ld_gout < d_out || ld_gx < d_in) return fail(CGTP_EINVAL, "a row stride is smaller than its row");
+  if (!gWg || !gWu) return fail(CGTP_EINVAL, "NULL data pointer");
+  if ((bg != nullptr) != (gbg != nullptr) || (bu != nullptr) != (gbu != nullptr))
+    return fail(CGTP_EINVAL, "gbg and gbu must be given where bg and bu are, and be NULL where they are not");
+  for (const void* p : {x, Wg, Wu, bg, bu, gout, (const void*)gx, (const void*)gWg, (const void*)gWu, (const void*)gbg, (const void*)gbu})
+    if (!aligned(p, 16)) return fail(CGTP_EINVAL, "data pointers must be 16-byte aligned");
+  hipStream_t st = (hipStream_t)hip_stream;
+  if (rows == 0) {   // empty sums
+    const size_t e = a.f64 ? 8 : 4;
+    HIP_TRY(cgtp::launch_fill_zero(gWg, (size_t)(d_in * d_out) * e, st));
+    HIP_TRY(cgtp::launch_fill_zero(gWu, (size_t)(d_in * d_out) * e, st));
+    if (gbg) {
+      HIP_TRY(cgtp::launch_fill_zero(gbg, (size_t)d_out * e, st));
+      HIP_TRY(cgtp::launch_fill_zero(gbu, (size_t)d_out * e, st));
+    }
+    return CGTP_OK;
+  }
+  if (!x || !Wg || !Wu || !gout || !gx) return fail(CGTP_EINVAL, "NULL data pointer");
+  const size_t need = cgtp_gated_workspace_bytes(rows, d_in, d_out, dtype);
+  if (!workspace_serves(workspace, workspace_bytes, need)) return bad_workspace("cgtp_gated_workspace_bytes", need);
+  HIP_TRY(cgtp::gated_backward(a, workspace, st));
+  return CGTP_OK;
+}
+
+cgtp_status cgtp_norm_create(const char* irreps, int32_t groups, int32_t act, double eps, int32_t dtype, int32_t device,
+                             uint32_t flags, cgtp_norm** out) {
+  if (!out) return fail(CGTP_EINVAL, "out is NULL");
+  *out = nullptr;
+  if (!irreps) return fail(CGTP_EINVAL, "irreps string is NULL");
+  if (flags & ~(uint32_t)(CGTP_IR_MUL | CGTP_NORM_GATED)) return fail(CGTP_EINVAL, "unknown bit in flags");
+  if (dtype != CGTP_F32 && dtype != CGTP_F64) return fail(CGTP_EINVAL, "dtype must be CGTP_F32 or CGTP_F64");
+  if (act < CGTP_ACT_NONE || act > CGTP_ACT_TANH) return fail(CGTP_EINVAL, "unknown activation");
+  if (groups <= 0) return fail(CGTP_EINVAL, "the number of groups must be positive");
+  if (!(eps > 0) || !std::isfinite(eps)) return fail(CGTP_EINVAL, "eps must be positive and finite");
+  try {
+    std::unique_ptr<cgtp_norm> H(new cgtp_norm());
+    cgtp::Norm& N = H->N;
+    std::vector<cgtp::Irrep> irs;
+    try {
+      irs = cgtp::parse_irreps(irreps);
+    } catch (const std::invalid_argument& e) {
+      return fail(CGTP_EINVAL, e.what());
+    }
+    if (irs.size() > 64) return fail(CGTP_EUNSUPPORTED, "more than 64 segments");
+    N.groups = groups; N.act = act; N.eps = eps; N.dtype = dtype; N.device = device; N.ir_mul = flags & CGTP_IR_MUL;
+    for (const cgtp::Irrep& ir : irs) {
+      if (ir.l > cgtp::kMaxL) return fail(CGTP_EUNSUPPORTED, "l > 8");
+      if (ir.mul > 65536) return fail(CGTP_EUNSUPPORTED, "multiplicity above 65536");
+      if (ir.mul % groups != 0) return fail(CGTP_EINVAL, "the number of groups has to divide every multiplicity");
+      cgtp::NormSeg s = {};
+      s.mul = ir.mul;
+      s.n = 2 * ir.l + 1;
+      s.inv = ir.l == 0 && ir.p > 0;
+      s.col = s.ycol = (int)N.dim_x;
+      s.gate = s.gst = -1;
+      s.st = (int)N.seg.size();
+      s.w = (int)N.n_w;
+      s.b = (int)N.n_b;
+      N.dim_x += ir.dim();
+      N.n_w += ir.mul;
+      if (s.inv) N.n_b += ir.mul;
+      N.seg.push_back(s);
+    }
+    N.dim_y = N.dim_x;
+    int places = (int)N.seg.size();
+    if (flags & CGTP_NORM_GATED)
+      for (cgtp::NormSeg& s : N.seg)
+        if (!s.inv) {
+          s.gate = (int)N.dim_x;
+          s.gst = places++;
+          s.gw = (int)N.n_w;
+          s.gb = (int)N.n_b;
+          N.dim_x += s.mul;
+          N.n_w += s.mul;
+          N.n_b += s.mul;
+        }
+    N.n_stat = (int64_t)places * groups * 2;
+    cgtp::emit_norm(N, N.fwd, N.bwd, N.sums);
+    // the kernels are loaded on `device`; the caller's current device is restored on return
+    struct Restore {
+      int device = -1;
+      ~Restore() {
+        if (device >= 0) (void)hipSetDevice(device);
+      }
+    } restore;
+    if (device >= 0) {
+      HIP_TRY(hipGetDevice(&restore.device));
+      HIP_TRY(hipSetDevice(device));
+      hipDeviceProp_t prop;
+      HIP_TRY(hipGetDeviceProperties(&prop, device));
+      N.num_cu = prop.multiProcessorCount;
+      if (std::string(prop.gcnArchName).rfind("gfx950", 0) != 0)
+        return fail(CGTP_EUNSUPPORTED, std::string("this library targets gfx950, device is ") + prop.gcnArchName);
+    }
+    try {
+      for (cgtp::Kernel* k : {&N.fwd, &N.bwd, &N.sums}) cgtp::jit_compile(*k, device);
+    } catch (const std::exception& e) {
+      for (cgtp::Kernel* k : {&N.fwd, &N.bwd, &N.sums}) cgtp::jit_unload(*k);
+      return fail(CGTP_ECOMPILE, e.what());
+    }
+    *out = H.release();
+    return CGTP_OK;
+  } catch (const std::bad_alloc&) {
+    return fail(CGTP_ENOMEM, "out of host memory");
+  } catch (const std::exception& e) {
+    return fail(CGTP_ERUNTIME, e.what());
+  }
+}
+
+cgtp_status cgtp_norm_destroy(cgtp_norm* norm) {
+  if (!norm) return CGTP_OK;
+  for (cgtp::Kernel* k : {&norm->N.fwd, &norm->N.bwd, &norm->N.sums}) cgtp::jit_unload(*k);
+  delete norm;
+  return CGTP_OK;
+}
+
+int64_t cgtp_norm_dim(const cgtp_norm* norm, int32_t which) {
+  if (!norm) return -1;
+  const cgtp::Norm& N = norm->N;
+  switch (which) {
+    case 0: return N.dim_x;
+    case 1: return N.dim_y;
+    case 2: return N.n_w;
+    case 3: return N.n_b;
+    case 4: return N.n_stat;
+    default: return -1;
+  }
+}
+
+size_t cgtp_norm_workspace_bytes(const cgtp_norm* norm, int64_t N, int64_t S, int32_t ptr, int32_t backward) {
+  if (!norm || N < 0 || S < 0 || (!ptr && N != S)) return 0;
+  return backward ? (size_t)S * (size_t)(norm->N.n_w + norm->N.n_b) * 8 : 0;
+}
+
+}  // extern "C"
+
+namespace {
+
+cgtp_status check_norm(const cgtp_norm* norm, int64_t N, int64_t S, const int64_t* ptr, std::initializer_list<const void*> data) {
+  if (!norm) return fail(CGTP_EINVAL, "norm is NULL");
+  if (N < 0 || S < 0) return fail(CGTP_EINVAL, "negative size");
+  if (!ptr && S != N) return fail(CGTP_EINVAL, "without ptr every row is a sample: S has to be N");
+  if (N > INT32_MAX || S > INT32_MAX) return fail(CGTP_EUNSUPPORTED, "N and S must be below 2^31");
+  for (const void* p : data)
+    if (!aligned(p, 16)) return fail(CGTP_EINVAL, "data pointers must be 16-byte aligned");
+  if (!norm->N.fwd.fn) return fail(CGTP_EUNSUPPORTED, "kernel " + norm->N.fwd.name + " is not loaded (created without a device?)");
+  return CGTP_OK;
+}
+
+cgtp_status launch(const cgtp::Kernel& k, unsigned grid, void** args, hipStream_t st) {
+  HIP_TRY(hipModuleLaunchKernel(k.fn, grid, 1, 1, (unsigned)k.wg, 1, 1, 0, st, args, nullptr));
+  return CGTP_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+cgtp_status norm_forward(const cgtp_norm* norm, const void* x, const void* weight, const void* bias, void* y, void* stats,
+                         int64_t N, int64_t S, const int64_t* ptr, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  cgtp_status s = check_norm(norm, N, S, ptr, {x, weight, bias, y, stats});
+  if (s != CGTP_OK) return s;
+  if (S == 0) return CGTP_OK;
+  const cgtp::Norm& P = norm->N;
+  if ((N > 0 && (!x || !y)) || !weight || (P.n_b && !bias)) return fail(CGTP_EINVAL, "NULL data pointer");
+  const size_t need = cgtp_norm_workspace_bytes(norm, N, S, ptr != nullptr, 0);
+  if (!workspace_serves(workspace, workspace_bytes, need)) return bad_workspace("cgtp_norm_workspace_bytes", need);
+  const int64_t units = S * (int64_t)P.seg.size() * P.groups;
+  void* args[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&y, (void*)&stats, (void*)&N, (void*)&S, (void*)&ptr};
+  return launch(P.fwd, (unsigned)std::min<int64_t>(units, 1 << 20), args, (hipStream_t)hip_stream);
+}
+
+cgtp_status norm_backward(const cgtp_norm* norm, const void* x, const void* weight, const void* bias, const void* gy,
+                          const void* stats, void* gx, void* gweight, void* gbias, int64_t N, int64_t S, const int64_t* ptr,
+                          void* workspace, size_t workspace_bytes, void* hip_stream) {
+  cgtp_status s = check_norm(norm, N, S, ptr, {x, weight, bias, gy, stats, gx, gweight, gbias});
+  if (s != CGTP_OK) return s;
+  const cgtp::Norm& P = norm->N;
+  if (!gweight || (P.n_b && !gbias)) return fail(CGTP_EINVAL, "NULL data pointer");
+  hipStream_t st = (hipStream_t)hip_stream;
+  if (S == 0) {
+    HIP_TRY(cgtp::launch_fill_zero(gweight, (size_t)P.n_w * P.elt(), st));
+    if (P.n_b) HIP_TRY(cgtp::launch_fill_zero(gbias, (size_t)P.n_b * P.elt(), st));
+    return CGTP_OK;
+  }
+  if ((N > 0 && (!x || !gy || !gx)) || !weight || (P.n_b && !bias) || !stats) return fail(CGTP_EINVAL, "NULL data pointer");
+  const size_t need = cgtp_norm_workspace_bytes(norm, N, S, ptr != nullptr, 1);
+  if (!workspace_serves(workspace, workspace_bytes, need)) return bad_workspace("cgtp_norm_workspace_bytes", need);
+  const int64_t units = S * (int64_t)P.seg.size() * P.groups;
+  double* part = (double*)workspace;
+  void* args[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&gy, (void*)&stats, (void*)&gx, (void*)&part, (void*)&N, (void*)&S, (void*)&ptr};
+  s = launch(P.bwd, (unsigned)std::min<int64_t>(units, 1 << 20), args, st);
+  if (s != CGTP_OK) return s;
+  void* sargs[] = {(void*)&part, (void*)&S, (void*)&gweight, (void*)&gbias};
+  return launch(P.sums, (unsigned)((P.n_w + P.n_b + 15) / 16), sargs, st);
+}
+
+}  // extern "C"

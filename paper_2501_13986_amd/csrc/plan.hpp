@@ -13,6 +13,9 @@
 
 namespace cgtp {
 
+// Records the message that cgtp_last_error() gives on this thread and hands the status back.
+cgtp_status fail(cgtp_status s, const std::string& msg);
+
 struct Irrep {
   int mul = 0;
   int l = 0;

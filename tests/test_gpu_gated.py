@@ -1,0 +1,221 @@
+"""The gated feed-forward block against the fp64 oracle."""
+import numpy as np
+import pytest
+
+from oracle import layer
+from tests._layer import EPS, check, gated_tolerance
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+DT = {"f32": torch.float32, "f64": torch.float64}
+NAMES = ("gx", "gWg", "gWu", "gbg", "gbu")
+
+
+def inputs(rows, k, n, prec, bias, seed=0, spread=0.0):
+    rng = np.random.default_rng(seed)
+    draw = lambda *s: rng.normal(size=s) * np.exp(spread * rng.normal(size=s))  # noqa: E731
+    p = [draw(rows, k), draw(k, n) / np.sqrt(k), draw(k, n) / np.sqrt(k)] + ([draw(n), draw(n)] if bias else [None, None]) + [draw(rows, n)]
+    return [None if a is None else a.astype(np.float32 if prec == "f32" else np.float64) for a in p]
+
+
+def dev(a, wide=0, fill=7.0):
+    """On the GPU; wide: as the first columns of rows that are so much wider."""
+    if a is None:
+        return None
+    t = torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    if not wide:
+        return t
+    w = torch.full((t.shape[0], t.shape[1] + wide), fill, dtype=t.dtype, device="cuda")
+    w[:, :t.shape[1]] = t
+    return w[:, :t.shape[1]]
+
+
+def outputs(rows, k, n, prec, bias, wide=0):
+    new = lambda *s: torch.full(s, float("nan"), dtype=DT[prec], device="cuda")  # noqa: E731
+    return (new(rows, n + wide)[:, :n], new(rows, k + wide)[:, :k], new(k, n), new(k, n)) + ((new(n), new(n)) if bias else (None, None))
+
+
+def run(p, prec, act, bias, wide=0):
+    from paper_2501_13986_amd import binding as b
+    x, Wg, Wu, bg, bu, gout = p
+    rows, (k, n) = x.shape[0], Wg.shape
+    t = [dev(x, wide), dev(Wg), dev(Wu), dev(bg), dev(bu)]
+    o = outputs(rows, k, n, prec, bias, wide)
+    b.gated_forward(t[0], t[1], t[2], o[0], bg=t[3], bu=t[4], act=act)
+    b.gated_backward(t[0], t[1], t[2], dev(gout, wide), o[1], o[2], o[3], bg=t[3], bu=t[4], gbg=o[4], gbu=o[5], act=act)
+    torch.cuda.synchronize()
+    return o
+
+
+def compare(o, p, prec, act, what):
+    x, Wg, Wu, bg, bu, gout = p
+    ref = layer.gated(x, Wg, Wu, bg, bu, act, gout)
+    for name, got in zip(("out",) + NAMES, o):
+        if got is not None:
+            check(got.cpu().numpy(), ref[name], gated_tolerance(ref[name], prec, Wg.shape[0], Wg.shape[1], x.shape[0]), f"{what} {name}")
+
+
+# one of everything, around the tiles' edges, and the widths of this library's plans
+SIZES = [(1, 1, 1), (2, 64, 544), (1, 8, 24), (5, 3, 2), (31, 16, 33), (33, 8, 17), (64, 64, 64), (65, 37, 301), (243, 8, 160), (300, 64, 96),
+         (129, 130, 65), (64, 256, 33), (1000, 16, 130), (31, 128, 127), (257, 5, 64), (128, 200, 7), (97, 129, 40), (1030, 64, 31)]
+
+
+@pytest.mark.parametrize("prec", ["f32", "f64"])
+@pytest.mark.parametrize("rows,k,n", SIZES)
+def test_against_the_oracle(rows, k, n, prec):
+    bias = (rows + n) % 2 == 0
+    p = inputs(rows, k, n, prec, bias)
+    compare(run(p, prec, layer.SILU, bias), p, prec, layer.SILU, f"{rows}x{k}x{n}")
+
+
+@pytest.mark.parametrize("prec", ["f32", "f64"])
+@pytest.mark.parametrize("act", [layer.NONE, layer.GELU, layer.SIGMOID, layer.TANH])
+def test_activations(act, prec):
+    p = inputs(70, 40, 50, prec, True, seed=act)
+    compare(run(p, prec, act, True), p, prec, act, f"act {act}")
+
+
+@pytest.mark.parametrize("prec", ["f32", "f64"])
+@pytest.mark.parametrize("rows,k,n,wide", [(40, 24, 36, 4), (33, 7, 19, 1), (100, 64, 64, 3), (1, 64, 64, 64)])
+def test_columns_of_wider_rows(rows, k, n, wide, prec):
+    """What lies between the rows is not touched."""
+    p = inputs(rows, k, n, prec, False, seed=2)
+    o = run(p, prec, layer.SILU, False, wide)
+    compare(o, p, prec, layer.SILU, "strided")
+    for t, w in ((o[0], n), (o[1], k)):
+        whole = t.as_strided((rows, w + wide), (w + wide, 1))
+        assert torch.isnan(whole[:, w:]).all()
+
+
+@pytest.mark.parametrize("prec", ["f32", "f64"])
+def test_numbers_far_apart(prec):
+    """Factors over many powers of two: each product keeps the precision of its type."""
+    p = inputs(50, 48, 40, prec, True, seed=9, spread=4.0)
+    compare(run(p, prec, layer.NONE, True), p, prec, layer.NONE, "spread")
+
+
+def test_infinities_and_nan_stay_in_their_rows():
+    p = inputs(70, 20, 40, "f32", False, seed=4)
+    ref = run(p, "f32", layer.SILU, False)
+    x = p[0].copy()
+    x[3, 5], x[40, 0], x[69, 19] = np.inf, np.nan, -np.inf
+    o = run([x] + p[1:], "f32", layer.SILU, False)
+    clean = [r for r in range(70) if r not in (3, 40, 69)]
+    assert torch.equal(o[0][clean], ref[0][clean]) and torch.equal(o[1][clean], ref[1][clean])
+    for r in (3, 40, 69):
+        assert not torch.isfinite(o[0][r]).any()
+
+
+def test_saturated_activations():
+    from paper_2501_13986_amd import binding as b
+    x = torch.tensor([[1000.0], [-1000.0], [200.0], [-90.0], [0.0]], device="cuda")
+    one = torch.ones((1, 1), device="cuda")
+    out = torch.empty((5, 1), device="cuda")
+    b.gated_forward(x, one, one, out, act=b.ACT_SILU)
+    assert torch.allclose(out.double(), x.double() ** 2 * torch.sigmoid(x.double()), rtol=1e-6, atol=1e-30)
+    b.gated_forward(x, one, one, out, act=b.ACT_SIGMOID)
+    assert torch.allclose(out.double(), x.double() * torch.sigmoid(x.double()), rtol=1e-6, atol=1e-30)
+
+
+def test_no_rows():
+    p = inputs(0, 8, 16, "f32", True)
+    o = run(p, "f32", layer.SILU, True)
+    for t in o[2:]:
+        assert (t == 0).all()
+
+
+@pytest.mark.parametrize("prec", ["f32", "f64"])
+def test_differences(prec):
+    """Gradients of a random direction against differences of the forward pass itself."""
+    from paper_2501_13986_amd import binding as b
+    p = inputs(64, 24, 40, "f64", True, seed=6)
+    o = run([a.astype(np.float32) if prec == "f32" else a for a in p], prec, layer.SILU, True)
+    rng = np.random.default_rng(1)
+    d = [rng.normal(size=a.shape) for a in p[:5]]
+    out = torch.empty((64, 40), dtype=torch.float64, device="cuda")
+
+    def loss(h):
+        t = [dev(a + h * v) for a, v in zip(p[:5], d)]
+        b.gated_forward(t[0], t[1], t[2], out, bg=t[3], bu=t[4])
+        return float((out * dev(p[5])).sum())
+
+    h = 1e-4
+    num = (loss(h) - loss(-h)) / (2 * h)
+    ana = sum(float((g.double() * dev(v)).sum()) for g, v in zip(o[1:], d))
+    size = sum(float((g.double() * dev(v)).abs().sum()) for g, v in zip(o[1:], d))
+    # the differences' own error is h^2 times third derivatives of the terms, fewer than 100 of them per number
+    assert abs(num - ana) <= (100 * h * h + 400 * EPS[prec]) * size
+
+
+def test_runs_are_bit_identical():
+    p = inputs(5000, 64, 160, "f32", True, seed=8)
+    a, c = run(p, "f32", layer.SILU, True), run(p, "f32", layer.SILU, True)
+    for s, t in zip(a, c):
+        assert torch.equal(s, t)
+
+
+def test_another_stream_and_two_at_once():
+    from paper_2501_13986_amd import binding as b
+    ps = [inputs(3000, 64, 96, "f32", False, seed=s) for s in (1, 2)]
+    ref = [run(p, "f32", layer.SILU, False) for p in ps]
+    streams = [torch.cuda.Stream() for _ in ps]
+    ts = [[dev(a) for a in p] for p in ps]
+    os_ = [outputs(3000, 64, 96, "f32", False) for _ in ps]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for s, t, o in zip(streams, ts, os_):
+            with torch.cuda.stream(s):
+                b.gated_forward(t[0], t[1], t[2], o[0])
+                b.gated_backward(t[0], t[1], t[2], t[5], o[1], o[2], o[3])
+    torch.cuda.synchronize()
+    for r, o in zip(ref, os_):
+        for s, t in zip(r[:4], o[:4]):
+            assert torch.equal(s, t)
+
+
+def test_captured_and_replayed():
+    from paper_2501_13986_amd import binding as b
+    p = inputs(700, 32, 96, "f32", True, seed=3)
+    t = [dev(a) for a in p]
+    o = outputs(700, 32, 96, "f32", True)
+
+    def step():
+        b.gated_forward(t[0], t[1], t[2], o[0], bg=t[3], bu=t[4])
+        b.gated_backward(t[0], t[1], t[2], t[5], o[1], o[2], o[3], bg=t[3], bu=t[4], gbg=o[4], gbu=o[5])
+
+    step()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        step()
+    for seed in (11, 12, 13):
+        q = inputs(700, 32, 96, "f32", True, seed=seed)
+        for dst, src in zip(t, q):
+            dst.copy_(dev(src))
+        for v in o:
+            v.fill_(float("nan"))
+        g.replay()
+        torch.cuda.synchronize()
+        for s, v in zip(run(q, "f32", layer.SILU, True), o):
+            assert torch.equal(s, v)
+
+
+def test_offsets_beyond_32_bits():
+    """More than 2^31 elements between the first and the last row, and more than 4 GiB of results."""
+    from paper_2501_13986_amd import binding as b
+    rows, k, n = 1_050_000, 8, 2080
+    g = torch.Generator(device="cuda").manual_seed(0)
+    x = torch.randn((rows, k), generator=g, device="cuda")
+    W = [torch.randn((k, n), generator=g, device="cuda") for _ in range(2)]
+    out = torch.full((rows, n), float("nan"), device="cuda")
+    b.gated_forward(x, *W, out)
+    gout = torch.zeros((rows, n), device="cuda")
+    at = [0, 1, 524_287, 1_032_444, 1_032_445, rows - 2, rows - 1]
+    gout[at] = torch.randn((len(at), n), generator=g, device="cuda")
+    gx, gW = torch.full_like(x, float("nan")), [torch.empty_like(w) for w in W]
+    b.gated_backward(x, *W, gout, gx, *gW)
+    ref = layer.gated(x[at].cpu().numpy(), *[w.cpu().numpy() for w in W], None, None, layer.SILU, gout[at].cpu().numpy())
+    for name, got in (("out", out[at]), ("gx", gx[at]), ("gWg", gW[0]), ("gWu", gW[1])):
+        check(got.cpu().numpy(), ref[name], gated_tolerance(ref[name], "f32", k, n, len(at)), name)
+    assert not torch.isnan(out[::4099]).any() and not torch.isnan(out[-1]).any() and not torch.isnan(gx).any()
