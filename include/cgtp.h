@@ -317,8 +317,10 @@ typedef enum { CGTP_ACT_NONE = 0, CGTP_ACT_SILU = 1, CGTP_ACT_GELU = 2, CGTP_ACT
  * plan it forms the per-edge weights that a convolution reads from the edges' scalars.  ld_x and ld_out are the elements from one
  * row of x (out) to the next, at least d_in (d_out): rows may be columns of wider ones; what lies between them is not touched.
  * dtype: cgtp_dtype; act: cgtp_act.  fp32 products run on the matrix cores with each factor as the sum of three
- * bf16 numbers, which hold its 24 bits, and 32-bit sums: the result is as far from the exact one as that of fp32 products.
- * Allocates nothing; no workspace.  rows, d_in, d_out < 2^31, and d_in, d_out > 0. */
+ * bf16 numbers, which hold its 24 bits, and 32-bit sums: the result is as far from the exact one as that of fp32 products
+ * (magnitudes above 2^128 (1 - 2^-9) count as infinite, and a row with an infinite number gives NaN).
+ * Allocates nothing; no workspace.  rows < 2^31; d_in and d_out from 1 to 2^20, their product below 2^31.
+ * out must not overlap an input. */
 cgtp_status gated_forward(const void* x, const void* Wg, const void* Wu, const void* bg, const void* bu, void* out,
                           int64_t rows, int64_t d_in, int64_t d_out, int64_t ld_x, int64_t ld_out, int32_t act,
                           int32_t dtype, void* hip_stream);

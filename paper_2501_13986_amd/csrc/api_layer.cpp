@@ -36,8 +36,9 @@ cgtp_status check_gated(const cgtp::GatedArgs& a, int32_t dtype) {
   if (dtype != CGTP_F32 && dtype != CGTP_F64) return fail(CGTP_EINVAL, "dtype must be CGTP_F32 or CGTP_F64");
   if (a.act < CGTP_ACT_NONE || a.act > CGTP_ACT_TANH) return fail(CGTP_EINVAL, "unknown activation");
   if (a.rows < 0 || a.d_in <= 0 || a.d_out <= 0) return fail(CGTP_EINVAL, "rows must not be negative, d_in and d_out must be positive");
-  if (a.rows > INT32_MAX || a.d_in > INT32_MAX || a.d_out > INT32_MAX) return fail(CGTP_EUNSUPPORTED, "rows, d_in and d_out must be below 2^31");
-  if (a.d_in > INT32_MAX / a.d_out) return fail(CGTP_EUNSUPPORTED, "d_in * d_out must be below 2^31");
+  if (a.rows > INT32_MAX) return fail(CGTP_EUNSUPPORTED, "rows must be below 2^31");
+  if (a.d_in > 1 << 20 || a.d_out > 1 << 20 || a.d_in > INT32_MAX / a.d_out)
+    return fail(CGTP_EUNSUPPORTED, "d_in and d_out must be at most 2^20, their product below 2^31");
   if ((a.bg == nullptr) != (a.bu == nullptr)) return fail(CGTP_EINVAL, "bg and bu must both be given or both be NULL");
   // a row stride beyond this leaves no row inside the address space
   for (int64_t ld : {a.ld_x, a.ld_out, a.ld_gout, a.ld_gx})

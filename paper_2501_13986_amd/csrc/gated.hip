@@ -5,6 +5,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 
 #include "act.hpp"
 #include "layer.hpp"
@@ -124,6 +125,229 @@ __global__ void __launch_bounds__(kThreads) k_gated_gw(GatedArgs a, int64_t row0
   }
 }
 
+// ---- fp32, up to 128 columns of x ----------------------------------------------------------------------------------------
+//
+// Products on the matrix cores in bf16, 16 x 16 results from 32 terms an instruction: sixteen times the rate of the fp32 ones.  A
+// factor is the sum of three bf16 numbers, which hold its 24 bits; of the nine products of parts the six largest are formed, the
+// others are below 2^-25 of the product.  Sums are held in fp32.
+//
+// A wave keeps the parts of its columns of Wg and Wu in registers for the whole call and walks over rows, whose parts the workgroup
+// puts into LDS once for its four waves.
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+struct Parts {
+  bf16x8 p[3];
+};
+
+// two numbers as three pairs of bf16
+__device__ inline void split(float a, float b, unsigned* p) {
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    const unsigned h = __builtin_bit_cast(unsigned, __builtin_convertvector(f32x2{a, b}, bf16x2));
+    p[i] = h;
+    if (i == 2) break;
+    a -= __builtin_bit_cast(float, h << 16);
+    b -= __builtin_bit_cast(float, h & 0xffff0000u);
+  }
+}
+
+__device__ inline Parts split8(const float* v) {
+  unsigned w[4][3];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) split(v[2 * i], v[2 * i + 1], w[i]);
+  Parts r;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) r.p[i] = __builtin_bit_cast(bf16x8, u32x4{w[0][i], w[1][i], w[2][i], w[3][i]});
+  return r;
+}
+
+__device__ inline f32x4 mfma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+// which parts meet: the smallest products first
+constexpr int kPairA[6] = {2, 0, 1, 1, 0, 0}, kPairB[6] = {0, 2, 1, 0, 1, 0};
+
+constexpr int kRows = 64;        // rows in LDS at a time
+constexpr int kMaxIn = 128;      // columns of x that the kernels below take
+
+// Four neighbouring numbers of a row, zero beyond its end.  vec: rows and widths are multiples of four.
+__device__ inline f32x4 load4(const float* row, int k, int K, bool vec) {
+  if (vec) {
+    const f32x4 v = *(const f32x4*)(row + (k < K ? k : 0));
+    return k < K ? v : f32x4{0, 0, 0, 0};
+  }
+  f32x4 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float e = row[k + i < K ? k + i : 0];
+    v[i] = k + i < K ? e : 0.f;
+  }
+  return v;
+}
+
+// The parts of a column of W, terms 32 s + 8 q + (0..7), as the right operand
+__device__ inline Parts column_parts(const float* W, int64_t n, int64_t c, int k0, int K) {
+  float v[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const bool in = k0 + j < K && c < n;
+    const float e = W[in ? (int64_t)(k0 + j) * n + c : 0];
+    v[j] = in ? e : 0.f;
+  }
+  return split8(v);
+}
+
+template <int KS>
+struct RowParts {   // 64 rows of x in parts; a row is padded by 16 bytes so that eight rows fill all banks once
+  static constexpr int kPitch = KS * 32 + 8;
+  __bf16 v[3][kRows][kPitch];
+};
+
+// One column of 16 x NT results a lane; results of a row tile: rows 4 q + i, columns NT (lane % 16) + t of the wave's 16 NT.
+template <int KS, int NT, int kAct>
+__global__ void __launch_bounds__(kThreads, 2) k_gated_fwd(GatedArgs a, int col_tiles, int splits, int vec_x, int vec_out) {
+  __shared__ RowParts<KS> X;
+  constexpr int KP = KS * 32, kQuads = KP / 4, kPer = kRows * kQuads / kThreads;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, l16 = lane & 15, q = lane >> 4;
+  const int K = (int)a.d_in;
+  const int64_t n = a.d_out, c = ((int64_t)(blockIdx.x % col_tiles) * 4 + wave) * (16 * NT) + l16 * NT;
+  const float* x = (const float*)a.x;
+  float* out = (float*)a.out;
+  Parts wg[KS][NT], wu[KS][NT];
+  float bg[NT], bu[NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      wg[s][j] = column_parts((const float*)a.Wg, n, c + j, s * 32 + q * 8, K);
+      wu[s][j] = column_parts((const float*)a.Wu, n, c + j, s * 32 + q * 8, K);
+    }
+    bg[j] = a.bg && c + j < n ? ((const float*)a.bg)[c + j] : 0.f;
+    bu[j] = a.bu && c + j < n ? ((const float*)a.bu)[c + j] : 0.f;
+  }
+  const int64_t blocks = (a.rows + kRows - 1) / kRows;
+  f32x4 next[kPer];
+  auto fetch = [&](int64_t b) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int e = t + i * kThreads;
+      const int64_t r = b * kRows + e / kQuads;
+      next[i] = load4(x + (r < a.rows ? r : a.rows - 1) * a.ld_x, e % kQuads * 4, K, vec_x);
+    }
+  };
+  int64_t b = blockIdx.x / col_tiles;
+  if (b < blocks) fetch(b);
+  for (; b < blocks; b += splits) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int e = t + i * kThreads;
+      unsigned lo[3], hi[3];
+      split(next[i][0], next[i][1], lo);
+      split(next[i][2], next[i][3], hi);
+#pragma unroll
+      for (int p = 0; p < 3; ++p) *(uint2*)&X.v[p][e / kQuads][e % kQuads * 4] = make_uint2(lo[p], hi[p]);
+    }
+    __syncthreads();
+    if (b + splits < blocks) fetch(b + splits);
+#pragma unroll
+    for (int rt = 0; rt < kRows / 16; ++rt) {
+      f32x4 g[NT], u[NT];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        g[j] = f32x4{bg[j], bg[j], bg[j], bg[j]};
+        u[j] = f32x4{bu[j], bu[j], bu[j], bu[j]};
+      }
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        Parts xa;
+#pragma unroll
+        for (int p = 0; p < 3; ++p) xa.p[p] = *(const bf16x8*)&X.v[p][rt * 16 + l16][s * 32 + q * 8];
+#pragma unroll
+        for (int m = 0; m < 6; ++m)
+#pragma unroll
+          for (int j = 0; j < NT; ++j) {
+            g[j] = mfma(xa.p[kPairA[m]], wg[s][j].p[kPairB[m]], g[j]);
+            u[j] = mfma(xa.p[kPairA[m]], wu[s][j].p[kPairB[m]], u[j]);
+          }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int64_t r = b * kRows + rt * 16 + q * 4 + i;
+        float v[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) v[j] = act_only<kAct>(g[j][i]) * u[j][i];
+        float* to = out + r * a.ld_out + c;
+        if (r < a.rows) {
+          if constexpr (NT == 2) {
+            if (vec_out && c < n) {
+              __builtin_nontemporal_store(f32x2{v[0], v[1]}, (f32x2*)to);
+              continue;
+            }
+          }
+#pragma unroll
+          for (int j = 0; j < NT; ++j)
+            if (c + j < n) __builtin_nontemporal_store(v[j], to + j);
+        }
+      }
+    }
+  }
+}
+
+// compute units of the current device, asked for once
+hipError_t compute_units(int& cus) {
+  constexpr int kMaxDevices = 64;
+  static std::atomic<int> known[kMaxDevices];
+  int dev = -1;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  if (dev < 0 || dev >= kMaxDevices) return hipErrorInvalidDevice;
+  cus = known[dev].load(std::memory_order_relaxed);
+  if (cus) return hipSuccess;
+  e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
+  if (e == hipSuccess) known[dev].store(cus, std::memory_order_relaxed);
+  return e;
+}
+
+template <int KS, int NT, int kAct>
+hipError_t launch_fwd(const GatedArgs& a, int cus, hipStream_t st) {
+  const int64_t cols = (a.d_out + 64 * NT - 1) / (64 * NT), blocks = (a.rows + kRows - 1) / kRows;
+  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(blocks, 2 * cus / cols));
+  const int vec_x = a.ld_x % 4 == 0 && a.d_in % 4 == 0, vec_out = a.ld_out % 2 == 0 && a.d_out % 2 == 0;
+  k_gated_fwd<KS, NT, kAct><<<dim3((unsigned)(cols * splits)), kThreads, 0, st>>>(a, (int)cols, (int)splits, vec_x, vec_out);
+  return hipGetLastError();
+}
+
+template <int kAct>
+hipError_t launch_fwd_act(const GatedArgs& a, hipStream_t st) {
+  int cus = 0;
+  hipError_t e = compute_units(cus);
+  if (e != hipSuccess) return e;
+  // 32 columns a wave where that leaves every compute unit two workgroups, else 16
+  const bool wide = (a.d_out + 127) / 128 * ((a.rows + kRows - 1) / kRows) >= 2 * cus;
+  switch ((a.d_in + 31) / 32) {
+    case 1: return wide ? launch_fwd<1, 2, kAct>(a, cus, st) : launch_fwd<1, 1, kAct>(a, cus, st);
+    case 2: return wide ? launch_fwd<2, 2, kAct>(a, cus, st) : launch_fwd<2, 1, kAct>(a, cus, st);
+    case 3: return launch_fwd<3, 1, kAct>(a, cus, st);
+    default: return launch_fwd<4, 1, kAct>(a, cus, st);
+  }
+}
+
+hipError_t forward_parts(const GatedArgs& a, hipStream_t st) {
+  switch (a.act) {
+    case CGTP_ACT_NONE: return launch_fwd_act<CGTP_ACT_NONE>(a, st);
+    case CGTP_ACT_SILU: return launch_fwd_act<CGTP_ACT_SILU>(a, st);
+    case CGTP_ACT_GELU: return launch_fwd_act<CGTP_ACT_GELU>(a, st);
+    case CGTP_ACT_SIGMOID: return launch_fwd_act<CGTP_ACT_SIGMOID>(a, st);
+    default: return launch_fwd_act<CGTP_ACT_TANH>(a, st);
+  }
+}
+
 constexpr int64_t kPiece = 8192;   // rows whose dg and du stand in the workspace at a time
 
 int64_t tiles(int64_t n) { return (n + kTile - 1) / kTile; }
@@ -163,6 +387,7 @@ hipError_t backward(const GatedArgs& a, void* ws, hipStream_t st) {
 }  // namespace
 
 hipError_t gated_forward(const GatedArgs& a, hipStream_t st) {
+  if (!a.f64 && a.d_in <= kMaxIn) return forward_parts(a, st);
   const int64_t most = (int64_t)65536 * kTile / std::max<int64_t>(1, tiles(a.d_out)) / kTile * kTile;   // rows of a launch
   for (int64_t row0 = 0; row0 < a.rows; row0 += std::max<int64_t>(kTile, most)) {
     const int64_t rows = std::min(a.rows - row0, std::max<int64_t>(kTile, most));
