@@ -315,7 +315,7 @@ typedef enum { CGTP_ACT_NONE = 0, CGTP_ACT_SILU = 1, CGTP_ACT_GELU = 2, CGTP_ACT
  *     out = act(x Wg + bg) * (x Wu + bu)
  * x [rows, d_in], Wg, Wu [d_in, d_out], bg, bu [d_out] (both or neither; NULL: no bias), out [rows, d_out].  With d_out = n_w of a
  * plan it forms the per-edge weights that a convolution reads from the edges' scalars.  ld_x and ld_out are the elements from one
- * row of x (out) to the next, at least d_in (d_out): rows may be columns of wider ones; what lies between them is not touched.
+ * row of x (out) to the next, at least d_in (d_out) and below 2^22: rows may be columns of wider ones; what lies between them is not touched.
  * dtype: cgtp_dtype; act: cgtp_act.  fp32 products run on the matrix cores with each factor as the sum of three
  * bf16 numbers, which hold its 24 bits, and 32-bit sums: the result is as far from the exact one as that of fp32 products
  * (magnitudes above 2^128 (1 - 2^-9) count as infinite, and a row with an infinite number gives NaN).

@@ -8,17 +8,10 @@
 
 namespace cgtp {
 
-// 1 / (1 + exp(-t)).  fp32: exp by the hardware's power of two, whose argument t log2(e) is corrected by its rounding error
-// (without it the result is off by |t| roundings), and the hardware's reciprocal, 1 unit in the last place each.  Above 128 the
-// result is 1; below -88, where it leaves the normal numbers, it is 0.  The selects keep a NaN, a clamp would not.
-__device__ inline float act_sigmoid(float t) {
-  const float s = t > 128.f ? 128.f : t;
-  const float p = s * -1.44269502f;
-  const float e = __builtin_fmaf(s, -1.44269502f, -p) + s * -1.92596299e-8f;
-  const float x = __builtin_amdgcn_exp2f(p);
-  const float q = __builtin_amdgcn_rcpf(1.f + __builtin_fmaf(x, 0.693147181f * e, x));
-  return t < -88.f ? 0.f : q;
-}
+// 1 / (1 + exp(-t)).  fp32: the hardware's power of two and reciprocal.  The rounding of t log2(e) makes the result off by |t| half
+// steps where t is negative, which is at most 0.3 half steps of 1, and t times it at most 0.6; a correction costs three of seven
+// instructions.  No input leaves the range: 2^x gives infinity or zero, and the reciprocal zero or one.
+__device__ inline float act_sigmoid(float t) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(t * -1.44269502f)); }
 __device__ inline double act_sigmoid(double t) { return 1.0 / (1.0 + exp(-t)); }
 
 // a = act(t) and d = act'(t)

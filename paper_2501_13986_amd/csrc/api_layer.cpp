@@ -40,9 +40,8 @@ cgtp_status check_gated(const cgtp::GatedArgs& a, int32_t dtype) {
   if (a.d_in > 1 << 20 || a.d_out > 1 << 20 || a.d_in > INT32_MAX / a.d_out)
     return fail(CGTP_EUNSUPPORTED, "d_in and d_out must be at most 2^20, their product below 2^31");
   if ((a.bg == nullptr) != (a.bu == nullptr)) return fail(CGTP_EINVAL, "bg and bu must both be given or both be NULL");
-  // a row stride beyond this leaves no row inside the address space
-  for (int64_t ld : {a.ld_x, a.ld_out, a.ld_gout, a.ld_gx})
-    if (ld > ((int64_t)1 << 31)) return fail(CGTP_EUNSUPPORTED, "row strides must be at most 2^31");
+  for (int64_t ld : {a.ld_x, a.ld_out, a.ld_gout, a.ld_gx})   // 64 rows are addressed with 31 bits
+    if (ld >= 1 << 22) return fail(CGTP_EUNSUPPORTED, "row strides must be below 2^22");
   return CGTP_OK;
 }
 

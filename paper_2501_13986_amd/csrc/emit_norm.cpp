@@ -14,14 +14,8 @@ namespace {
 
 const char kShared[] = R"HIP(
 typedef long long i64;
-__device__ inline float sigmoid_(float t) {
-  const float s = t > 128.f ? 128.f : t;
-  const float p = s * -1.44269502f;
-  const float e = __builtin_fmaf(s, -1.44269502f, -p) + s * -1.92596299e-8f;
-  const float x = __builtin_amdgcn_exp2f(p);
-  const float q = __builtin_amdgcn_rcpf(1.f + __builtin_fmaf(x, 0.693147181f * e, x));
-  return t < -88.f ? 0.f : q;
-}
+// off by |t| half steps where t is negative: at most 0.3 half steps of 1
+__device__ inline float sigmoid_(float t) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(t * -1.44269502f)); }
 __device__ inline double sigmoid_(double t) { return 1.0 / (1.0 + exp(-t)); }
 __device__ inline float erfc_(float t) { return erfcf(t); }
 __device__ inline double erfc_(double t) { return erfc(t); }

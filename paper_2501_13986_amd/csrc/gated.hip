@@ -139,6 +139,7 @@ typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 struct Parts {
@@ -175,18 +176,25 @@ constexpr int kPairA[6] = {2, 0, 1, 1, 0, 0}, kPairB[6] = {0, 2, 1, 0, 1, 0};
 constexpr int kRows = 64;        // rows in LDS at a time
 constexpr int kMaxIn = 128;      // columns of x that the kernels below take
 
-// Four neighbouring numbers of a row, zero beyond its end.  vec: rows and widths are multiples of four.
-__device__ inline f32x4 load4(const float* row, int k, int K, bool vec) {
-  if (vec) {
-    const f32x4 v = *(const f32x4*)(row + (k < K ? k : 0));
-    return k < K ? v : f32x4{0, 0, 0, 0};
-  }
+// Rows go through buffer descriptors of at most 64 rows: what lies outside reads as zero and is not written, without a branch.  A
+// place that is not wanted inside the descriptor's range gets the offset kNowhere, behind every range (64 rows of 2^22 numbers of
+// 8 bytes at most).
+constexpr unsigned kNowhere = 0x80000000u;
+constexpr int kNonTemporal = 2;
+using Buffer = __amdgpu_buffer_rsrc_t;
+
+__device__ inline Buffer rows_of(const void* base, int64_t first, int64_t rows, int64_t ld, int64_t width, int element) {
+  const int64_t have = rows - first < kRows ? rows - first : kRows;
+  const char* p = (const char*)base + (have > 0 ? first * ld * element : 0);
+  return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, have > 0 ? (int)(((have - 1) * ld + width) * element) : 0, 0x00020000);
+}
+
+// Four neighbouring numbers of a row from column k, zero beyond its end.  vec: rows and widths are multiples of four.
+__device__ inline f32x4 load4(Buffer B, unsigned row, int k, int K, bool vec) {
+  if (vec) return __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(B, k < K ? row + k * 4 : kNowhere, 0, 0));
   f32x4 v;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const float e = row[k + i < K ? k + i : 0];
-    v[i] = k + i < K ? e : 0.f;
-  }
+  for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(float, __builtin_amdgcn_raw_buffer_load_b32(B, k + i < K ? row + (k + i) * 4 : kNowhere, 0, 0));
   return v;
 }
 
@@ -216,8 +224,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_gated_fwd(GatedArgs a, int col_
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, l16 = lane & 15, q = lane >> 4;
   const int K = (int)a.d_in;
   const int64_t n = a.d_out, c = ((int64_t)(blockIdx.x % col_tiles) * 4 + wave) * (16 * NT) + l16 * NT;
-  const float* x = (const float*)a.x;
-  float* out = (float*)a.out;
+  const unsigned ldx = (unsigned)a.ld_x * 4, ldo = (unsigned)a.ld_out * 4;
   Parts wg[KS][NT], wu[KS][NT];
   float bg[NT], bu[NT];
 #pragma unroll
@@ -233,13 +240,16 @@ __global__ void __launch_bounds__(kThreads, 2) k_gated_fwd(GatedArgs a, int col_
   const int64_t blocks = (a.rows + kRows - 1) / kRows;
   f32x4 next[kPer];
   auto fetch = [&](int64_t b) {
+    const Buffer in = rows_of(a.x, b * kRows, a.rows, a.ld_x, K, 4);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int e = t + i * kThreads;
-      const int64_t r = b * kRows + e / kQuads;
-      next[i] = load4(x + (r < a.rows ? r : a.rows - 1) * a.ld_x, e % kQuads * 4, K, vec_x);
+      next[i] = load4(in, e / kQuads * ldx, e % kQuads * 4, K, vec_x);
     }
   };
+  unsigned at[NT];      // a lane's columns
+#pragma unroll
+  for (int j = 0; j < NT; ++j) at[j] = c + j < n ? (unsigned)(c + j) * 4 + q * 4 * ldo : kNowhere;
   int64_t b = blockIdx.x / col_tiles;
   if (b < blocks) fetch(b);
   for (; b < blocks; b += splits) {
@@ -255,6 +265,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_gated_fwd(GatedArgs a, int col_
     }
     __syncthreads();
     if (b + splits < blocks) fetch(b + splits);
+    const Buffer to = rows_of(a.out, b * kRows, a.rows, a.ld_out, n, 4);
 #pragma unroll
     for (int rt = 0; rt < kRows / 16; ++rt) {
       f32x4 g[NT], u[NT];
@@ -278,21 +289,16 @@ __global__ void __launch_bounds__(kThreads, 2) k_gated_fwd(GatedArgs a, int col_
       }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int64_t r = b * kRows + rt * 16 + q * 4 + i;
+        const unsigned row = (rt * 16 + i) * ldo;
         float v[NT];
 #pragma unroll
         for (int j = 0; j < NT; ++j) v[j] = act_only<kAct>(g[j][i]) * u[j][i];
-        float* to = out + r * a.ld_out + c;
-        if (r < a.rows) {
-          if constexpr (NT == 2) {
-            if (vec_out && c < n) {
-              __builtin_nontemporal_store(f32x2{v[0], v[1]}, (f32x2*)to);
-              continue;
-            }
-          }
+        // kNowhere + row stays below 2^32: 64 rows are less than 2^31 bytes
+        if (NT == 2 && vec_out) {
+          __builtin_amdgcn_raw_buffer_store_b64(u32x2{__builtin_bit_cast(unsigned, v[0]), __builtin_bit_cast(unsigned, v[NT - 1])}, to, at[0] + row, 0, kNonTemporal);
+        } else {
 #pragma unroll
-          for (int j = 0; j < NT; ++j)
-            if (c + j < n) __builtin_nontemporal_store(v[j], to + j);
+          for (int j = 0; j < NT; ++j) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, v[j]), to, at[j] + row, 0, kNonTemporal);
         }
       }
     }

@@ -24,7 +24,7 @@ def forward(x=P, Wg=P, Wu=P, bg=0, bu=0, out=P, rows=4, k=8, n=16, ldx=8, ldo=16
     (dict(x=0), 1), (dict(Wg=0), 1), (dict(Wu=0), 1), (dict(out=0), 1), (dict(x=P + 4), 1), (dict(out=P + 8), 1), (dict(Wu=P + 4), 1),
     (dict(bg=P), 1), (dict(bu=P), 1), (dict(rows=-1), 1), (dict(k=0), 1), (dict(n=0), 1), (dict(n=-3), 1), (dict(ldx=7), 1), (dict(ldo=15), 1),
     (dict(act=5), 1), (dict(act=-1), 1), (dict(dtype=2), 1), (dict(rows=1 << 31), 2), (dict(n=(1 << 20) + 1, ldo=1 << 21), 2), (dict(k=(1 << 20) + 1, ldx=1 << 21), 2),
-    (dict(k=1 << 16, ldx=1 << 16, n=1 << 16, ldo=1 << 16), 2), (dict(ldx=(1 << 31) + 1), 2)])
+    (dict(k=1 << 16, ldx=1 << 16, n=1 << 16, ldo=1 << 16), 2), (dict(ldx=1 << 22), 2), (dict(ldo=1 << 40), 2)])
 def test_gated_forward_refuses(change, want):
     assert forward(**change) == want
     assert b.lib().cgtp_last_error()
