@@ -217,8 +217,8 @@ struct RowParts {   // 64 rows of x in parts; a row is padded by 16 bytes so tha
 };
 
 // One column of 16 x NT results a lane; results of a row tile: rows 4 q + i, columns NT (lane % 16) + t of the wave's 16 NT.
-template <int KS, int NT, int kAct>
-__global__ void __launch_bounds__(kThreads, 2) k_gated_fwd(GatedArgs a, int col_tiles, int splits, int vec_x, int vec_out) {
+template <int KS, int NT, int kAct, bool kVec>
+__global__ void __launch_bounds__(kThreads, 2) k_gated_fwd(GatedArgs a, int col_tiles, int splits) {
   __shared__ RowParts<KS> X;
   constexpr int KP = KS * 32, kQuads = KP / 4, kPer = kRows * kQuads / kThreads;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, l16 = lane & 15, q = lane >> 4;
@@ -244,7 +244,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_gated_fwd(GatedArgs a, int col_
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int e = t + i * kThreads;
-      next[i] = load4(in, e / kQuads * ldx, e % kQuads * 4, K, vec_x);
+      next[i] = load4(in, e / kQuads * ldx, e % kQuads * 4, K, kVec);
     }
   };
   unsigned at[NT];      // a lane's columns
@@ -266,13 +266,13 @@ __global__ void __launch_bounds__(kThreads, 2) k_gated_fwd(GatedArgs a, int col_
     __syncthreads();
     if (b + splits < blocks) fetch(b + splits);
     const Buffer to = rows_of(a.out, b * kRows, a.rows, a.ld_out, n, 4);
-#pragma unroll
-    for (int rt = 0; rt < kRows / 16; ++rt) {
-      f32x4 g[NT], u[NT];
+    // the results of a row tile are finished while the products of the next one run
+    f32x4 g[2][NT], u[2][NT];
+    auto products = [&](int rt, f32x4* gt, f32x4* ut) {
 #pragma unroll
       for (int j = 0; j < NT; ++j) {
-        g[j] = f32x4{bg[j], bg[j], bg[j], bg[j]};
-        u[j] = f32x4{bu[j], bu[j], bu[j], bu[j]};
+        gt[j] = f32x4{bg[j], bg[j], bg[j], bg[j]};
+        ut[j] = f32x4{bu[j], bu[j], bu[j], bu[j]};
       }
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
@@ -283,25 +283,32 @@ __global__ void __launch_bounds__(kThreads, 2) k_gated_fwd(GatedArgs a, int col_
         for (int m = 0; m < 6; ++m)
 #pragma unroll
           for (int j = 0; j < NT; ++j) {
-            g[j] = mfma(xa.p[kPairA[m]], wg[s][j].p[kPairB[m]], g[j]);
-            u[j] = mfma(xa.p[kPairA[m]], wu[s][j].p[kPairB[m]], u[j]);
+            gt[j] = mfma(xa.p[kPairA[m]], wg[s][j].p[kPairB[m]], gt[j]);
+            ut[j] = mfma(xa.p[kPairA[m]], wu[s][j].p[kPairB[m]], ut[j]);
           }
       }
+    };
+    auto finish = [&](int rt, const f32x4* gt, const f32x4* ut) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const unsigned row = (rt * 16 + i) * ldo;
+        const unsigned row = (rt * 16 + i) * ldo;   // kNowhere + row stays below 2^32: 64 rows are less than 2^31 bytes
         float v[NT];
 #pragma unroll
-        for (int j = 0; j < NT; ++j) v[j] = act_only<kAct>(g[j][i]) * u[j][i];
-        // kNowhere + row stays below 2^32: 64 rows are less than 2^31 bytes
-        if (NT == 2 && vec_out) {
-          __builtin_amdgcn_raw_buffer_store_b64(u32x2{__builtin_bit_cast(unsigned, v[0]), __builtin_bit_cast(unsigned, v[NT - 1])}, to, at[0] + row, 0, kNonTemporal);
+        for (int j = 0; j < NT; ++j) v[j] = act_only<kAct>(gt[j][i]) * ut[j][i];
+        if constexpr (NT == 2 && kVec) {
+          __builtin_amdgcn_raw_buffer_store_b64(u32x2{__builtin_bit_cast(unsigned, v[0]), __builtin_bit_cast(unsigned, v[1])}, to, at[0] + row, 0, kNonTemporal);
         } else {
 #pragma unroll
           for (int j = 0; j < NT; ++j) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, v[j]), to, at[j] + row, 0, kNonTemporal);
         }
       }
+    };
+#pragma unroll
+    for (int rt = 0; rt < kRows / 16; ++rt) {
+      products(rt, g[rt & 1], u[rt & 1]);
+      if (rt > 0) finish(rt - 1, g[~rt & 1], u[~rt & 1]);
     }
+    finish(kRows / 16 - 1, g[1], u[1]);
   }
 }
 
@@ -324,8 +331,10 @@ template <int KS, int NT, int kAct>
 hipError_t launch_fwd(const GatedArgs& a, int cus, hipStream_t st) {
   const int64_t cols = (a.d_out + 64 * NT - 1) / (64 * NT), blocks = (a.rows + kRows - 1) / kRows;
   const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(blocks, 2 * cus / cols));
-  const int vec_x = a.ld_x % 4 == 0 && a.d_in % 4 == 0, vec_out = a.ld_out % 2 == 0 && a.d_out % 2 == 0;
-  k_gated_fwd<KS, NT, kAct><<<dim3((unsigned)(cols * splits)), kThreads, 0, st>>>(a, (int)cols, (int)splits, vec_x, vec_out);
+  const dim3 grid((unsigned)(cols * splits));
+  const bool vec = a.ld_x % 4 == 0 && a.d_in % 4 == 0 && a.ld_out % 2 == 0 && a.d_out % 2 == 0;
+  if (vec) k_gated_fwd<KS, NT, kAct, true><<<grid, kThreads, 0, st>>>(a, (int)cols, (int)splits);
+  else k_gated_fwd<KS, NT, kAct, false><<<grid, kThreads, 0, st>>>(a, (int)cols, (int)splits);
   return hipGetLastError();
 }
 
