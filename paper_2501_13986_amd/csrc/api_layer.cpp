@@ -1,5 +1,6 @@
 // Entry points of the layer operators: the gated feed-forward block and the group normalisation.
 #include <algorithm>
+#include <atomic>
 #include <climits>
 #include <cmath>
 #include <memory>
@@ -32,6 +33,22 @@ cgtp_status bad_workspace(const char* query, size_t need) {
   return fail(CGTP_EINVAL, "workspace: " + std::to_string(need) + " bytes needed (" + query + "), 256-byte aligned");
 }
 
+// compute units of the current device, asked for once
+hipError_t compute_units(int& cus) {
+  constexpr int kMaxDevices = 64;
+  static std::atomic<int> known[kMaxDevices];
+  int dev = -1;
+  hipError_t e = hipGetDevice(&dev);
+  if (e != hipSuccess) return e;
+  if (dev < 0 || dev >= kMaxDevices) return hipErrorInvalidDevice;
+  cus = known[dev].load(std::memory_order_relaxed);
+  if (cus) return hipSuccess;
+  e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
+  cus = std::min(cus, 256);
+  if (e == hipSuccess) known[dev].store(cus, std::memory_order_relaxed);
+  return e;
+}
+
 cgtp_status check_gated(const cgtp::GatedArgs& a, int32_t dtype) {
   if (dtype != CGTP_F32 && dtype != CGTP_F64) return fail(CGTP_EINVAL, "dtype must be CGTP_F32 or CGTP_F64");
   if (a.act < CGTP_ACT_NONE || a.act > CGTP_ACT_TANH) return fail(CGTP_EINVAL, "unknown activation");
@@ -54,7 +71,7 @@ cgtp_status gated_forward(const void* x, const void* Wg, const void* Wu, const v
                           int32_t dtype, void* hip_stream) {
   cgtp::GatedArgs a = {};
   a.x = x; a.Wg = Wg; a.Wu = Wu; a.bg = bg; a.bu = bu; a.out = out;
-  a.rows = rows; a.d_in = d_in; a.d_out = d_out; a.ld_x = ld_x; a.ld_out = ld_out; a.act = act; a.f64 = dtype == CGTP_F64;
+  a.rows = rows; a.d_in = d_in; a.d_out = d_out; a.ld_x = ld_x; a.ld_out = ld_out; a.act = act;
   cgtp_status s = check_gated(a, dtype);
   if (s != CGTP_OK) return s;
   if (ld_x < d_in || ld_out < d_out) return fail(CGTP_EINVAL, "a row stride is smaller than its row");
@@ -62,7 +79,9 @@ cgtp_status gated_forward(const void* x, const void* Wg, const void* Wu, const v
   if (!x || !Wg || !Wu || !out) return fail(CGTP_EINVAL, "NULL data pointer");
   for (const void* p : {x, Wg, Wu, bg, bu, (const void*)out})
     if (!aligned(p, 16)) return fail(CGTP_EINVAL, "data pointers must be 16-byte aligned");
-  HIP_TRY(cgtp::gated_forward(a, (hipStream_t)hip_stream));
+  int cus = 0;
+  HIP_TRY(compute_units(cus));
+  HIP_TRY((dtype == CGTP_F64 ? cgtp::gated_forward_f64 : cgtp::gated_forward_f32)(a, cus, (hipStream_t)hip_stream));
   return CGTP_OK;
 }
 
@@ -70,7 +89,7 @@ size_t cgtp_gated_workspace_bytes(int64_t rows, int64_t d_in, int64_t d_out, int
   cgtp::GatedArgs a = {};
   a.rows = rows; a.d_in = d_in; a.d_out = d_out;
   if (check_gated(a, dtype) != CGTP_OK || rows == 0) return 0;
-  return cgtp::gated_workspace_bytes(rows, d_in, d_out, dtype == CGTP_F64);
+  return (dtype == CGTP_F64 ? cgtp::gated_workspace_bytes_f64 : cgtp::gated_workspace_bytes_f32)(rows, d_in, d_out);
 }
 
 cgtp_status gated_backward(const void* x, const void* Wg, const void* Wu, const void* bg, const void* bu, const void* gout,
@@ -79,7 +98,7 @@ cgtp_status gated_backward(const void* x, const void* Wg, const void* Wu, const 
                            size_t workspace_bytes, void* hip_stream) {
   cgtp::GatedArgs a = {};
   a.x = x; a.Wg = Wg; a.Wu = Wu; a.bg = bg; a.bu = bu; a.gout = gout; a.gx = gx; a.gWg = gWg; a.gWu = gWu; a.gbg = gbg; a.gbu = gbu;
-  a.rows = rows; a.d_in = d_in; a.d_out = d_out; a.ld_x = ld_x; a.ld_gout = ld_gout; a.ld_gx = ld_gx; a.act = act; a.f64 = dtype == CGTP_F64;
+  a.rows = rows; a.d_in = d_in; a.d_out = d_out; a.ld_x = ld_x; a.ld_gout = ld_gout; a.ld_gx = ld_gx; a.act = act;
   cgtp_status s = check_gated(a, dtype);
   if (s != CGTP_OK) return s;
   if (ld_x < d_in || ld_gout < d_out || ld_gx < d_in) return fail(CGTP_EINVAL, "a row stride is smaller than its row");
@@ -90,7 +109,7 @@ cgtp_status gated_backward(const void* x, const void* Wg, const void* Wu, const 
     if (!aligned(p, 16)) return fail(CGTP_EINVAL, "data pointers must be 16-byte aligned");
   hipStream_t st = (hipStream_t)hip_stream;
   if (rows == 0) {   // empty sums
-    const size_t e = a.f64 ? 8 : 4;
+    const size_t e = dtype == CGTP_F64 ? 8 : 4;
     HIP_TRY(cgtp::launch_fill_zero(gWg, (size_t)(d_in * d_out) * e, st));
     HIP_TRY(cgtp::launch_fill_zero(gWu, (size_t)(d_in * d_out) * e, st));
     if (gbg) {
@@ -102,7 +121,9 @@ cgtp_status gated_backward(const void* x, const void* Wg, const void* Wu, const 
   if (!x || !Wg || !Wu || !gout || !gx) return fail(CGTP_EINVAL, "NULL data pointer");
   const size_t need = cgtp_gated_workspace_bytes(rows, d_in, d_out, dtype);
   if (!workspace_serves(workspace, workspace_bytes, need)) return bad_workspace("cgtp_gated_workspace_bytes", need);
-  HIP_TRY(cgtp::gated_backward(a, workspace, st));
+  int cus = 0;
+  HIP_TRY(compute_units(cus));
+  HIP_TRY((dtype == CGTP_F64 ? cgtp::gated_backward_f64 : cgtp::gated_backward_f32)(a, cus, workspace, st));
   return CGTP_OK;
 }
 

@@ -1,0 +1,1028 @@
+// Kernels of the gated feed-forward block, for the translation units of its two types (gated_f32.hip, gated_f64.hip).
+//
+// With g = x Wg + bg, u = x Wu + bu, out = act(g) u and t = dE/dout:   dg = t u act'(g),  du = t act(g),
+//     gx = dg Wg^T + du Wu^T,   gWg = x^T dg,   gWu = x^T du,   gbg = sum dg,   gbu = sum du.
+//
+// All products run on the matrix cores, 16 x 16 results from 32 terms at a time.  An operand of them is held in parts: lane l has
+// the terms 8 q + (0..7) of row (left operand) or column (right operand) l16, where l16 = l % 16 and q = l / 16.
+//   fp32   three bf16 numbers whose sum has the 24 bits of the factor; of the nine products of parts the six largest are formed,
+//          the others are below 2^-25 of the product.  Sixteen times the rate of the fp32 matrix instruction, so 2.7 times faster
+//          than it with six products.  Sums are held in fp32.
+//   fp64   the numbers themselves, eight instructions of four terms.
+// A lane's four results are rows Num::row(q, 0..3) of column l16.  Two tiles of them are the parts of another operand with 32 terms,
+// in the order Num::term of the tiles' rows, so that dg and du go into their products from the registers that they are formed in;
+// the other operand stands in the same order.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "act.hpp"
+#include "layer.hpp"
+
+namespace cgtp {
+namespace {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef double f64x2 __attribute__((ext_vector_type(2)));
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kThreads = 256;
+constexpr int kRows = 64;      // rows of x in LDS at a time
+constexpr int kMaxIn = 128;    // columns of x that a wave's registers have room for
+constexpr int kNonTemporal = 2;
+using Buffer = __amdgpu_buffer_rsrc_t;
+
+template <int kUnits>
+struct PartsOf {
+  u32x4 w[kUnits];
+};
+
+template <class T>
+struct Num;
+
+// which parts meet: the smallest products first
+constexpr int kPairA[6] = {2, 0, 1, 1, 0, 0}, kPairB[6] = {0, 2, 1, 0, 1, 0};
+
+template <>
+struct Num<float> {
+  static constexpr int kUnits = 3;
+  using Parts = PartsOf<3>;
+  using Vec = f32x4;
+  static __device__ int row(int q, int i) { return 4 * q + i; }
+  // two numbers as three pairs of bf16
+  static __device__ void split(float a, float b, unsigned* p) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      const unsigned h = __builtin_bit_cast(unsigned, __builtin_convertvector(f32x2{a, b}, bf16x2));
+      p[i] = h;
+      if (i == 2) break;
+      a -= __builtin_bit_cast(float, h << 16);
+      b -= __builtin_bit_cast(float, h & 0xffff0000u);
+    }
+  }
+  static __device__ Parts parts(const float* v) {
+    unsigned w[4][3];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) split(v[2 * i], v[2 * i + 1], w[i]);
+    Parts r;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) r.w[i] = u32x4{w[0][i], w[1][i], w[2][i], w[3][i]};
+    return r;
+  }
+  // c[i] += a[i] b[i], the chains of sums in turn
+  template <int N>
+  static __device__ void mma(const Parts* const (&a)[N], const Parts* const (&b)[N], Vec* const (&c)[N]) {
+#pragma unroll
+    for (int m = 0; m < 6; ++m)
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        *c[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[i]->w[kPairA[m]]), __builtin_bit_cast(bf16x8, b[i]->w[kPairB[m]]), *c[i], 0, 0, 0);
+  }
+};
+
+template <>
+struct Num<double> {
+  static constexpr int kUnits = 4;
+  using Parts = PartsOf<4>;
+  using Vec = f64x4;
+  static __device__ int row(int q, int i) { return 4 * i + q; }
+  static __device__ Parts parts(const double* v) {
+    Parts r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.w[i] = __builtin_bit_cast(u32x4, f64x2{v[2 * i], v[2 * i + 1]});
+    return r;
+  }
+  template <int N>
+  static __device__ void mma(const Parts* const (&a)[N], const Parts* const (&b)[N], Vec* const (&c)[N]) {
+#pragma unroll
+    for (int m = 0; m < 8; ++m)
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const f64x2 u = __builtin_bit_cast(f64x2, a[i]->w[m / 2]), v = __builtin_bit_cast(f64x2, b[i]->w[m / 2]);
+        *c[i] = __builtin_amdgcn_mfma_f64_16x16x4f64(u[m % 2], v[m % 2], *c[i], 0, 0, 0);
+      }
+  }
+};
+
+// the place among 32 terms of row r (< 32) of two tiles of results: lane quarter q, number 4 (r / 16) + i
+template <class T>
+__device__ inline int term(int r) {
+  const int t = r / 16, h = r % 16;
+  return std::is_same<T, float>::value ? h / 4 * 8 + t * 4 + h % 4 : h % 4 * 8 + t * 4 + h / 4;
+}
+
+// ---- rows in memory ---------------------------------------------------------------------------------------------------------
+//
+// Rows go through buffer descriptors of at most kSpan rows: what lies outside reads as zero and is not written, without a branch.  A
+// place inside the descriptor's range that is not wanted gets the offset kNowhere, which is behind every range (row strides are
+// below 2^22 numbers, rows at most 2^20: 63 * 2^22 * 8 + 2^20 * 8 < 2^31), and with a row's offset added still below 2^32.
+
+constexpr unsigned kNowhere = 0x80000000u;
+constexpr int kSpan = 64;
+
+template <class T>
+__device__ inline Buffer rows_of(const void* base, int64_t first, int64_t rows, int64_t ld, int64_t width) {
+  const int64_t have = rows - first < kSpan ? rows - first : kSpan;
+  const T* p = (const T*)base + (have > 0 ? first * ld : 0);
+  return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, have > 0 ? (int)(((have - 1) * ld + width) * sizeof(T)) : 0, 0x00020000);
+}
+
+template <class T>
+__device__ inline T load1(Buffer B, unsigned at) {
+  if constexpr (sizeof(T) == 4) return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(B, at, 0, 0));
+  else return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b64(B, at, 0, 0));
+}
+
+template <class T>
+__device__ inline void store1(T v, Buffer B, unsigned at) {
+  if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, v), B, at, 0, kNonTemporal);
+  else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), B, at, 0, kNonTemporal);
+}
+
+// Four neighbouring numbers of the row that begins at offset `row`, from column k, zero beyond its end.  kVec: base, rows and widths are
+// multiples of four numbers.
+template <bool kVec, class T>
+__device__ inline void load4(Buffer B, unsigned row, int k, int K, T* v) {
+  constexpr int e = sizeof(T);
+  if constexpr (kVec) {
+    const unsigned at = k < K ? row + k * e : kNowhere;
+    if constexpr (e == 4) {
+      const f32x4 w = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(B, at, 0, 0));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = w[i];
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const f64x2 w = __builtin_bit_cast(f64x2, __builtin_amdgcn_raw_buffer_load_b128(B, at + h * 16, 0, 0));
+        v[2 * h] = w[0];
+        v[2 * h + 1] = w[1];
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = load1<T>(B, k + i < K ? row + (k + i) * e : kNowhere);
+  }
+}
+
+// `rows` rows of W [.., n] from row k on, at most 128 of them (2^30 bytes); an element's offset in it
+template <class T>
+__device__ inline Buffer matrix_of(const void* W, int64_t k, int64_t rows, int64_t n) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)((const T*)W + k * n), 0, rows > 0 ? (int)(rows * n * sizeof(T)) : 0, 0x00020000);
+}
+
+// The parts of column c of the rows of W that a descriptor holds, terms k + (0..7).  Rows behind the last are out of its range.
+template <class T>
+__device__ inline typename Num<T>::Parts column_parts(Buffer W, int64_t n, int64_t c, int k) {
+  T v[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = load1<T>(W, c < n ? ((unsigned)(k + j) * (unsigned)n + (unsigned)c) * (unsigned)sizeof(T) : kNowhere);
+  return Num<T>::parts(v);
+}
+
+template <class T>
+__device__ inline T bias_of(const void* b, int64_t c, int64_t n) { return b ? ((const T*)b)[c < n ? c : n - 1] : T(0); }
+
+// kR rows of kC columns in LDS, as operands with the columns as terms.  A row is padded by 16 bytes, so that 16 rows' 16 bytes fill
+// all banks once.
+template <class T, int kR, int kC>
+struct Tile;
+template <int kR, int kC>
+struct Tile<float, kR, kC> {
+  __bf16 v[3][kR][kC + 8];
+  __device__ PartsOf<3> read(int r, int c) const {
+    PartsOf<3> p;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) p.w[i] = *(const u32x4*)&v[i][r][c];
+    return p;
+  }
+  __device__ void write4(int r, int c, const float* x) {
+    unsigned lo[3], hi[3];
+    Num<float>::split(x[0], x[1], lo);
+    Num<float>::split(x[2], x[3], hi);
+#pragma unroll
+    for (int p = 0; p < 3; ++p) *(u32x2*)&v[p][r][c] = u32x2{lo[p], hi[p]};
+  }
+};
+template <int kR, int kC>
+struct Tile<double, kR, kC> {
+  double v[kR][kC + 2];
+  __device__ PartsOf<4> read(int r, int c) const {
+    PartsOf<4> p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p.w[i] = *(const u32x4*)&v[r][c + 2 * i];
+    return p;
+  }
+  __device__ void write4(int r, int c, const double* x) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) *(u32x4*)&v[r][c + 2 * h] = __builtin_bit_cast(u32x4, f64x2{x[2 * h], x[2 * h + 1]});
+  }
+};
+
+// four rows 4 r4 .. of four columns k4 .. of x into X as they are, and into XT by columns, rows in the order of `term`
+template <int KC>
+__device__ inline void write_both(Tile<float, kRows, KC>& X, Tile<float, KC, kRows>& XT, int r4, int k4, float (*x)[4]) {
+  unsigned row[4][2][3];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    Num<float>::split(x[j][0], x[j][1], row[j][0]);
+    Num<float>::split(x[j][2], x[j][3], row[j][1]);
+  }
+  const int at = r4 / 8 * 32 + term<float>(r4 % 8 * 4);   // four neighbours
+#pragma unroll
+  for (int p = 0; p < 3; ++p) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) *(u32x2*)&X.v[p][r4 * 4 + j][k4] = u32x2{row[j][0][p], row[j][1][p]};
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {   // halves of the words of two rows
+      const unsigned a = row[0][w][p], b = row[1][w][p], c = row[2][w][p], d = row[3][w][p];
+      *(u32x2*)&XT.v[p][k4 + 2 * w][at] = u32x2{__builtin_amdgcn_perm(b, a, 0x05040100), __builtin_amdgcn_perm(d, c, 0x05040100)};
+      *(u32x2*)&XT.v[p][k4 + 2 * w + 1][at] = u32x2{__builtin_amdgcn_perm(b, a, 0x07060302), __builtin_amdgcn_perm(d, c, 0x07060302)};
+    }
+  }
+}
+template <int KC>
+__device__ inline void write_both(Tile<double, kRows, KC>& X, Tile<double, KC, kRows>& XT, int r4, int k4, double (*x)[4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    X.write4(r4 * 4 + j, k4, x[j]);
+    const int at = r4 / 8 * 32 + term<double>(r4 % 8 * 4 + j);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) XT.v[k4 + w][at] = x[j][w];
+  }
+}
+
+// ---- up to 128 columns of x -------------------------------------------------------------------------------------------------
+
+// A wave keeps the parts of its 16 NT columns of Wg and Wu in registers for the whole call and walks over rows, whose parts the
+// workgroup puts into LDS once for its four waves.  Lane: columns NT l16 + j.
+template <class T, int KS, int NT, int kAct, bool kVec>
+__global__ void __launch_bounds__(kThreads, (sizeof(T) == 8 && KS > 2 ? 1 : 2)) k_gated_fwd(GatedArgs a, int col_tiles, int splits) {
+  using N = Num<T>;
+  __shared__ Tile<T, kRows, KS * 32> X;
+  constexpr int kQuads = KS * 8, kPer = kRows * kQuads / kThreads, e = sizeof(T);
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, l16 = lane & 15, q = lane >> 4;
+  const int K = (int)a.d_in;
+  const int64_t n = a.d_out, c = ((int64_t)(blockIdx.x % col_tiles) * 4 + wave) * (16 * NT) + l16 * NT;
+  const unsigned ldx = (unsigned)a.ld_x * e, ldo = (unsigned)a.ld_out * e;
+  const Buffer Wg = matrix_of<T>(a.Wg, 0, K, n), Wu = matrix_of<T>(a.Wu, 0, K, n);
+  typename N::Parts wg[KS][NT], wu[KS][NT];
+  T bg[NT], bu[NT];
+#pragma unroll
+  for (int j = 0; j < NT; ++j) {
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      wg[s][j] = column_parts<T>(Wg, n, c + j, s * 32 + q * 8);
+      wu[s][j] = column_parts<T>(Wu, n, c + j, s * 32 + q * 8);
+    }
+    bg[j] = bias_of<T>(a.bg, c + j, n);
+    bu[j] = bias_of<T>(a.bu, c + j, n);
+  }
+  const int64_t blocks = (a.rows + kRows - 1) / kRows;
+  T next[kPer][4];
+  auto fetch = [&](int64_t b) {
+    const Buffer in = rows_of<T>(a.x, b * kRows, a.rows, a.ld_x, K);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int at = t + i * kThreads;
+      load4<kVec>(in, at / kQuads * ldx, at % kQuads * 4, K, next[i]);
+    }
+  };
+  unsigned at[NT];      // a lane's columns
+#pragma unroll
+  for (int j = 0; j < NT; ++j) at[j] = c + j < n ? (unsigned)(c + j) * e + N::row(q, 0) * ldo : kNowhere;
+  int64_t b = blockIdx.x / col_tiles;
+  if (b < blocks) fetch(b);
+  for (; b < blocks; b += splits) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int p = t + i * kThreads;
+      X.write4(p / kQuads, p % kQuads * 4, next[i]);
+    }
+    __syncthreads();
+    if (b + splits < blocks) fetch(b + splits);
+    const Buffer to = rows_of<T>(a.out, b * kRows, a.rows, a.ld_out, n);
+    // the results of a row tile are finished while the products of the next one run
+    typename N::Vec g[2][NT], u[2][NT];
+    auto products = [&](int rt, typename N::Vec* gt, typename N::Vec* ut) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          gt[j][i] = bg[j];
+          ut[j][i] = bu[j];
+        }
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const typename N::Parts xa = X.read(rt * 16 + l16, s * 32 + q * 8);
+        if constexpr (NT == 2) N::template mma<4>({&xa, &xa, &xa, &xa}, {&wg[s][0], &wu[s][0], &wg[s][1], &wu[s][1]}, {&gt[0], &ut[0], &gt[1], &ut[1]});
+        else N::template mma<2>({&xa, &xa}, {&wg[s][0], &wu[s][0]}, {&gt[0], &ut[0]});
+      }
+    };
+    auto finish = [&](int rt, const typename N::Vec* gt, const typename N::Vec* ut) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const unsigned row = (rt * 16 + N::row(0, i)) * ldo;
+        T v[NT];
+#pragma unroll
+        for (int j = 0; j < NT; ++j) v[j] = act_only<kAct>(T(gt[j][i])) * T(ut[j][i]);
+        if constexpr (NT == 2 && kVec && e == 4) {
+          __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, f32x2{v[0], v[1]}), to, at[0] + row, 0, kNonTemporal);
+        } else {
+#pragma unroll
+          for (int j = 0; j < NT; ++j) store1(v[j], to, at[j] + row);
+        }
+      }
+    };
+#pragma unroll
+    for (int rt = 0; rt < kRows / 16; ++rt) {
+      products(rt, g[rt & 1], u[rt & 1]);
+      if (rt > 0) finish(rt - 1, g[~rt & 1], u[~rt & 1]);
+    }
+    finish(kRows / 16 - 1, g[1], u[1]);
+  }
+}
+
+// The gradients: two kernels, each of which forms g and u again.  That is a third more products than with dg and du kept in memory,
+// but those are twice the size of gout, written once and read twice.
+
+// gWg, gWu, gbg, gbu of 16 columns a wave, over the row blocks of a split; partial sums [split][Wg; bg; Wu; bu]
+template <class T, int KS>
+constexpr int kGwWaves = KS > 2 && sizeof(T) == 4 ? 8 : 4;   // eight where the rows in LDS leave room for one workgroup only
+
+template <class T, int KS, int kAct, bool kVec>
+__global__ void __launch_bounds__((kGwWaves<T, KS> * 64), (sizeof(T) == 8 && KS > 1 ? 1 : 2)) k_gated_gw(GatedArgs a, int col_tiles, int splits, T* part) {
+  using N = Num<T>;
+  constexpr int KC = KS * 32, e = sizeof(T);
+  __shared__ Tile<T, kRows, KC> X;
+  __shared__ Tile<T, KC, kRows> XT;
+  // blocks of 4 rows x 4 columns of x; threads without one of their own repeat the last (no lane-conditional code)
+  constexpr int kQuads = KS * 8, kBlocks = kRows / 4 * kQuads, kThr = kGwWaves<T, KS> * 64, kPer = (kBlocks + kThr - 1) / kThr;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, l16 = lane & 15, q = lane >> 4;
+  const int K = (int)a.d_in;
+  const int64_t n = a.d_out, c = ((int64_t)(blockIdx.x % col_tiles) * kGwWaves<T, KS> + wave) * 16 + l16;
+  const unsigned ldx = (unsigned)a.ld_x * e, ldo = (unsigned)a.ld_gout * e;
+  const Buffer Wg = matrix_of<T>(a.Wg, 0, K, n), Wu = matrix_of<T>(a.Wu, 0, K, n);
+  typename N::Parts wg[KS], wu[KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) {
+    wg[s] = column_parts<T>(Wg, n, c, s * 32 + q * 8);
+    wu[s] = column_parts<T>(Wu, n, c, s * 32 + q * 8);
+  }
+  const T bg = bias_of<T>(a.bg, c, n), bu = bias_of<T>(a.bu, c, n);
+  const int64_t blocks = (a.rows + kRows - 1) / kRows;
+  // four by four blocks to 16 neighbouring threads: their 8 bytes fall on different banks in X and in XT
+  auto block = [&](int i, int& r4, int& k4) {
+    const int p = t + i * kThr < kBlocks ? t + i * kThr : kBlocks - 1;
+    r4 = p % 4 + p / 16 % 4 * 4;
+    k4 = (p / 4 % 4 + p / 64 * 4) * 4;
+  };
+  T next[kPer][4][4];
+  auto fetch = [&](int64_t b) {
+    const Buffer in = rows_of<T>(a.x, b * kRows, a.rows, a.ld_x, K);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      int r4, k4;
+      block(i, r4, k4);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) load4<kVec>(in, (r4 * 4 + j) * ldx, k4, K, next[i][j]);
+    }
+  };
+  const unsigned at = c < n ? (unsigned)c * e + N::row(q, 0) * ldo : kNowhere;
+  typename N::Vec sg[KS * 2] = {}, su[KS * 2] = {};
+  T sbg = 0, sbu = 0;
+  int64_t b = blockIdx.x / col_tiles;
+  if (b < blocks) fetch(b);
+  for (; b < blocks; b += splits) {
+    const Buffer go = rows_of<T>(a.gout, b * kRows, a.rows, a.ld_gout, n);
+    T tg[8];   // of gout, 32 rows at a time
+    auto fetch_gout = [&](int half) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) tg[i] = load1<T>(go, at + (half * 32 + i / 4 * 16 + N::row(0, i % 4)) * ldo);
+    };
+    fetch_gout(0);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      int r4, k4;
+      block(i, r4, k4);
+      write_both(X, XT, r4, k4, next[i]);
+    }
+    __syncthreads();
+    if (b + splits < blocks) fetch(b + splits);
+#pragma unroll
+    for (int half = 0; half < kRows / 32; ++half) {
+      T dg[8], du[8];
+#pragma unroll
+      for (int rt = 0; rt < 2; ++rt) {
+        typename N::Vec g, u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          g[i] = bg;
+          u[i] = bu;
+        }
+#pragma unroll
+        for (int s = 0; s < KS; ++s) {
+          const typename N::Parts xa = X.read(half * 32 + rt * 16 + l16, s * 32 + q * 8);
+          N::template mma<2>({&xa, &xa}, {&wg[s], &wu[s]}, {&g, &u});
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const T o = tg[rt * 4 + i];   // zero behind the last row
+          T v, d;
+          act_both<kAct>(T(g[i]), v, d);
+          dg[rt * 4 + i] = o * T(u[i]) * d;
+          du[rt * 4 + i] = o * v;
+          sbg += dg[rt * 4 + i];
+          sbu += du[rt * 4 + i];
+        }
+      }
+      if (half + 1 < kRows / 32) fetch_gout(half + 1);
+      const typename N::Parts pg = N::parts(dg), pu = N::parts(du);
+#pragma unroll
+      for (int d = 0; d < KS * 2; ++d) {
+        const typename N::Parts xt = XT.read(d * 16 + l16, half * 32 + q * 8);
+        N::template mma<2>({&xt, &xt}, {&pg, &pu}, {&sg[d], &su[d]});
+      }
+    }
+  }
+  // the biases' sums of the four quarters of the rows
+  sbg += __shfl_xor(sbg, 16);
+  sbg += __shfl_xor(sbg, 32);
+  sbu += __shfl_xor(sbu, 16);
+  sbu += __shfl_xor(sbu, 32);
+  if (c >= n) return;
+  T* to = part + (int64_t)(blockIdx.x / col_tiles) * 2 * (K + 1) * n + c;
+#pragma unroll
+  for (int d = 0; d < KS * 2; ++d)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int k = d * 16 + N::row(q, i);
+      if (k < K) {
+        to[(int64_t)k * n] = sg[d][i];
+        to[(int64_t)(K + 1 + k) * n] = su[d][i];
+      }
+    }
+  if (q == 0) {
+    to[(int64_t)K * n] = sbg;
+    to[(int64_t)(2 * K + 1) * n] = sbu;
+  }
+}
+
+// adds up the splits, in their order
+template <class T>
+__global__ void __launch_bounds__(kThreads) k_gated_sums(const T* __restrict__ part, int splits, int64_t K, int64_t n, T* __restrict__ gWg,
+                                                     T* __restrict__ gWu, T* __restrict__ gbg, T* __restrict__ gbu) {
+  const int64_t size = 2 * (K + 1) * n, i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (i >= size) return;
+  T v = part[i];
+  for (int s = 1; s < splits; ++s) v += part[s * size + i];
+  const int64_t row = i / n, c = i % n;
+  if (row < K) gWg[i] = v;
+  else if (row == K) { if (gbg) gbg[c] = v; }
+  else if (row <= 2 * K) gWu[i - (K + 1) * n] = v;
+  else if (gbu) gbu[c] = v;
+}
+
+// The operands of W that gx needs, kUnits x 16 bytes a lane: [32 columns of W][operand][unit][lane].  First 4 KS for g and u: (g, u) x tile x s,
+// lane: column 16 tile + l16, terms 32 s + 8 q + (0..7) of d_in; then 4 KS for gx: (g, u) x d, lane: column 16 d + l16 of x, the 32 columns
+// of W in the order of Num::term.
+template <int KS>
+constexpr int kOperands = 8 * KS;
+
+template <class T, int KS>
+__global__ void __launch_bounds__(kThreads) k_gated_operands(GatedArgs a, u32x4* to) {
+  constexpr int kUnits = Num<T>::kUnits;
+  const int K = (int)a.d_in;
+  const int64_t n = a.d_out, steps = (n + 31) / 32, e = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  if (e >= steps * kOperands<KS>) return;
+  const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
+  const int64_t step = e / kOperands<KS>;
+  const int op = (int)(e % kOperands<KS>);
+  T v[8];
+  const Buffer W = matrix_of<T>(op / (2 * KS) % 2 ? a.Wu : a.Wg, 0, K, n);   // `op` is the wave's
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    int k;
+    int64_t c;
+    if (op < 4 * KS) {
+      k = op % KS * 32 + q * 8 + j;
+      c = step * 32 + op / KS % 2 * 16 + l16;
+    } else {
+      k = op % (2 * KS) * 16 + l16;
+      c = step * 32 + j / 4 * 16 + Num<T>::row(q, j % 4);
+    }
+    v[j] = load1<T>(W, k < K && c < n ? ((unsigned)k * (unsigned)n + (unsigned)c) * (unsigned)sizeof(T) : kNowhere);
+  }
+  const typename Num<T>::Parts p = Num<T>::parts(v);
+#pragma unroll
+  for (int i = 0; i < kUnits; ++i) to[(e * kUnits + i) * 64 + lane] = p.w[i];
+}
+
+// gx of 16 R rows a wave: the operands of 32 columns of W at a time in LDS for the eight (fp64 of more than 64 columns of x: four) waves
+// of a workgroup, the columns of a split one after another.  More than one split: partial sums [split][rows][d_in] in part.
+template <class T, int KS>
+constexpr int kGxWaves = KS > 2 && sizeof(T) == 8 ? 4 : 8;
+template <class T, int KS>
+constexpr int kGxTiles = KS > 2 || sizeof(T) == 8 ? 1 : 2;   // 2 would not fit the registers
+
+template <class T, int KS, int kAct, bool kVec>
+__global__ void __launch_bounds__((kGxWaves<T, KS> * 64), (KS > 2 && sizeof(T) == 8 ? 1 : 2)) k_gated_gx(GatedArgs a, const u32x4* __restrict__ ops, int splits, T* part) {
+  using N = Num<T>;
+  constexpr int R = kGxTiles<T, KS>, kUnits = N::kUnits, kOps = kOperands<KS> * kUnits, kThr = kGxWaves<T, KS> * 64, kPer = kOps * 64 / kThr, e = sizeof(T);
+  static_assert(kOps * 64 % kThr == 0, "every thread copies as much");
+  __shared__ u32x4 W[kOps][64];
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, l16 = lane & 15, q = lane >> 4;
+  const int K = (int)a.d_in;
+  const int64_t n = a.d_out, steps = (n + 31) / 32, first = (int64_t)(blockIdx.x / splits) * (kGxWaves<T, KS> * R * 16) + wave * R * 16;
+  const int64_t from = steps * (blockIdx.x % splits) / splits, end = steps * (blockIdx.x % splits + 1) / splits;
+  const unsigned ldx = (unsigned)a.ld_x * e, ldo = (unsigned)a.ld_gout * e;
+  auto operand = [&](int op) {
+    typename N::Parts p;
+#pragma unroll
+    for (int i = 0; i < kUnits; ++i) p.w[i] = W[op * kUnits + i][lane];
+    return p;
+  };
+  // x of rows 16 r + l16, terms 32 s + 8 q + (0..7)
+  typename N::Parts xb[R][KS];
+  {
+    const Buffer in = rows_of<T>(a.x, first, a.rows, a.ld_x, K);
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        T v[8];
+        load4<kVec>(in, (r * 16 + l16) * ldx, s * 32 + q * 8, K, v);
+        load4<kVec>(in, (r * 16 + l16) * ldx, s * 32 + q * 8 + 4, K, v + 4);
+        xb[r][s] = N::parts(v);
+      }
+  }
+  const Buffer go = rows_of<T>(a.gout, first, a.rows, a.ld_gout, n);
+  u32x4 next[kPer];
+  auto fetch = [&](int64_t step) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) next[i] = ops[step * kOps * 64 + t + i * kThr];
+  };
+  typename N::Vec acc[R][KS * 2] = {};
+  fetch(from);
+  for (int64_t step = from; step < end; ++step) {
+    T tg[R][8];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+      for (int tile = 0; tile < 2; ++tile) {
+        const int c = (int)(step * 32 + tile * 16);
+        const unsigned row = (r * 16 + l16) * ldo;
+        if constexpr (e == 4) {
+          load4<kVec>(go, row, c + q * 4, (int)n, tg[r] + tile * 4);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) tg[r][tile * 4 + i] = load1<T>(go, c + N::row(q, i) < n ? row + (c + N::row(q, i)) * e : kNowhere);
+        }
+      }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) (&W[0][0])[t + i * kThr] = next[i];
+    __syncthreads();
+    if (step + 1 < end) fetch(step + 1);
+    T dg[R][8], du[R][8];
+#pragma unroll
+    for (int tile = 0; tile < 2; ++tile) {
+      typename N::Vec g[R], u[R], bg = {0, 0, 0, 0}, bu = {0, 0, 0, 0};
+      if (a.bg) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          bg[i] = bias_of<T>(a.bg, step * 32 + tile * 16 + N::row(q, i), n);
+          bu[i] = bias_of<T>(a.bu, step * 32 + tile * 16 + N::row(q, i), n);
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        g[r] = bg;
+        u[r] = bu;
+      }
+#pragma unroll
+      for (int s = 0; s < KS; ++s) {
+        const typename N::Parts wg = operand(tile * KS + s), wu = operand((2 + tile) * KS + s);
+        if constexpr (R == 2) N::template mma<4>({&wg, &wu, &wg, &wu}, {&xb[0][s], &xb[0][s], &xb[1][s], &xb[1][s]}, {&g[0], &u[0], &g[1], &u[1]});
+        else N::template mma<2>({&wg, &wu}, {&xb[0][s], &xb[0][s]}, {&g[0], &u[0]});
+      }
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const T o = tg[r][tile * 4 + i];     // zero outside
+          T v, d;
+          act_both<kAct>(T(g[r][i]), v, d);
+          dg[r][tile * 4 + i] = o * T(u[r][i]) * d;
+          du[r][tile * 4 + i] = o * v;
+        }
+    }
+    typename N::Parts pg[R], pu[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      pg[r] = N::parts(dg[r]);
+      pu[r] = N::parts(du[r]);
+    }
+#pragma unroll
+    for (int d = 0; d < KS * 2; d += 2) {   // two column tiles in turn
+      const typename N::Parts w0 = operand(4 * KS + d), w1 = operand(4 * KS + d + 1);
+      if constexpr (R == 2) N::template mma<4>({&w0, &w1, &w0, &w1}, {&pg[0], &pg[0], &pg[1], &pg[1]}, {&acc[0][d], &acc[0][d + 1], &acc[1][d], &acc[1][d + 1]});
+      else N::template mma<2>({&w0, &w1}, {&pg[0], &pg[0]}, {&acc[0][d], &acc[0][d + 1]});
+      const typename N::Parts v0 = operand(6 * KS + d), v1 = operand(6 * KS + d + 1);
+      if constexpr (R == 2) N::template mma<4>({&v0, &v1, &v0, &v1}, {&pu[0], &pu[0], &pu[1], &pu[1]}, {&acc[0][d], &acc[0][d + 1], &acc[1][d], &acc[1][d + 1]});
+      else N::template mma<2>({&v0, &v1}, {&pu[0], &pu[0]}, {&acc[0][d], &acc[0][d + 1]});
+    }
+  }
+  const unsigned ldg = (unsigned)(splits > 1 ? K : a.ld_gx) * e;
+  const Buffer to = splits > 1 ? rows_of<T>(part + (int64_t)(blockIdx.x % splits) * a.rows * K, first, a.rows, K, K) : rows_of<T>(a.gx, first, a.rows, a.ld_gx, K);
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+#pragma unroll
+    for (int d = 0; d < KS * 2; ++d) {
+      const unsigned row = (r * 16 + l16) * ldg;
+      if constexpr (kVec && e == 4) {
+        const int k = d * 16 + q * 4;
+        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[r][d]), to, k < K ? row + k * 4 : kNowhere, 0, 0);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int k = d * 16 + N::row(q, i);
+          const T v = acc[r][d][i];   // (a bit cast of the element itself takes the first one)
+          store1(v, to, k < K ? row + k * e : kNowhere);
+        }
+      }
+    }
+}
+
+template <class T>
+__global__ void __launch_bounds__(kThreads) k_gated_gx_sums(const T* __restrict__ part, int splits, int64_t rows, int64_t K, T* __restrict__ gx, int64_t ld) {
+  const int64_t size = rows * K, i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  if (i >= size) return;
+  T v = part[i];
+  for (int s = 1; s < splits; ++s) v += part[s * size + i];
+  gx[i / K * ld + i % K] = v;
+}
+
+// ---- more columns of x ----------------------------------------------------------------------------------------------------------
+//
+// 128 rows x 64 columns of results a workgroup, 16 columns a wave, the terms 32 at a time: the rows' parts in LDS, the columns' parts formed
+// by each wave from memory.  The gradients go through dg and du in the workspace, a piece of the rows at a time.
+
+template <class T>
+constexpr int kManyRows = sizeof(T) == 4 ? 128 : 64;   // rows of a workgroup, for the registers of their sums
+constexpr int64_t kPiece = 8192;   // rows whose dg and du stand in the workspace at a time
+
+// rows first .. of A (ld numbers apart, `width` of them terms), 32 terms from k0 on; each thread copies four at a time
+template <class T>
+struct ManyRows {
+  static constexpr int kPer = kManyRows<T> / 32;
+  Tile<T, kManyRows<T>, 32> X;
+  __device__ void fetch(const T* A, int64_t first, int64_t rows, int64_t ld, int64_t width, int64_t k0, T (*v)[4]) const {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const Buffer in = rows_of<T>(A, first + i * 32, rows, ld, width);
+      load4<false>(in, threadIdx.x / 8 * (unsigned)(ld * sizeof(T)), (int)k0 + threadIdx.x % 8 * 4, (int)width, v[i]);
+    }
+  }
+  __device__ void put(T (*v)[4]) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) X.write4(i * 32 + threadIdx.x / 8, threadIdx.x % 8 * 4, v[i]);
+  }
+};
+
+// out (kBack: dg and du, [rows][d_out] each) of `rows` rows from row0 on
+template <class T, int kAct, bool kBack>
+__global__ void __launch_bounds__(kThreads, 2) k_gated_many(GatedArgs a, int64_t row0, int64_t rows, T* dg, T* du) {
+  using N = Num<T>;
+  constexpr int kTiles = kManyRows<T> / 16, e = sizeof(T);
+  __shared__ ManyRows<T> S;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, q = lane >> 4;
+  const int64_t n = a.d_out, K = a.d_in, tiles = (n + 63) / 64, first = blockIdx.x / tiles * kManyRows<T>, c = blockIdx.x % tiles * 64 + wave * 16 + l16;
+  const T* x = (const T*)a.x + row0 * a.ld_x;
+  typename N::Vec g[kTiles] = {}, u[kTiles] = {};
+  T next[ManyRows<T>::kPer][4];
+  S.fetch(x, first, rows, a.ld_x, K, 0, next);
+  for (int64_t k0 = 0; k0 < K; k0 += 32) {
+    const int64_t have = K - k0 < 32 ? K - k0 : 32;
+    const typename N::Parts wg = column_parts<T>(matrix_of<T>(a.Wg, k0, have, n), n, c, q * 8), wu = column_parts<T>(matrix_of<T>(a.Wu, k0, have, n), n, c, q * 8);
+    __syncthreads();
+    S.put(next);
+    __syncthreads();
+    if (k0 + 32 < K) S.fetch(x, first, rows, a.ld_x, K, k0 + 32, next);
+#pragma unroll
+    for (int rt = 0; rt < kTiles; ++rt) {
+      const typename N::Parts xa = S.X.read(rt * 16 + l16, q * 8);
+      N::template mma<2>({&xa, &xa}, {&wg, &wu}, {&g[rt], &u[rt]});
+    }
+  }
+  const T bg = bias_of<T>(a.bg, c, n), bu = bias_of<T>(a.bu, c, n);
+#pragma unroll
+  for (int h = 0; h < kTiles; h += 4) {   // 64 rows
+    const int64_t at = first + h * 16;
+    const Buffer go = rows_of<T>(kBack ? (const T*)a.gout + row0 * a.ld_gout : nullptr, at, kBack ? rows : 0, a.ld_gout, n);
+    const Buffer to = kBack ? rows_of<T>(dg, at, rows, n, n) : rows_of<T>((T*)a.out + row0 * a.ld_out, at, rows, a.ld_out, n);
+    const Buffer to_u = rows_of<T>(du, at, kBack ? rows : 0, n, n);
+#pragma unroll
+    for (int rt = 0; rt < 4; ++rt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const unsigned row = rt * 16 + N::row(q, i), out = (unsigned)(kBack ? n : a.ld_out) * e;
+        const T gv = g[h + rt][i] + bg, uv = u[h + rt][i] + bu;
+        T v, d;
+        act_both<kAct>(gv, v, d);
+        if constexpr (kBack) {
+          const T o = load1<T>(go, c < n ? row * (unsigned)(a.ld_gout * e) + (unsigned)c * e : kNowhere);
+          store1(o * uv * d, to, c < n ? row * out + (unsigned)c * e : kNowhere);
+          store1(o * v, to_u, c < n ? row * out + (unsigned)c * e : kNowhere);
+        } else {
+          store1(v * uv, to, c < n ? row * out + (unsigned)c * e : kNowhere);
+        }
+      }
+  }
+}
+
+// gx = dg Wg^T + du Wu^T of a piece of rows: 64 columns of x a workgroup
+template <class T>
+__global__ void __launch_bounds__(kThreads, 2) k_gated_many_gx(GatedArgs a, int64_t row0, int64_t rows, const T* dg, const T* du) {
+  using N = Num<T>;
+  constexpr int kTiles = kManyRows<T> / 16, e = sizeof(T);
+  __shared__ ManyRows<T> S;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, q = lane >> 4;
+  const int64_t n = a.d_out, K = a.d_in, tiles = (K + 63) / 64, first = blockIdx.x / tiles * kManyRows<T>, k0 = blockIdx.x % tiles * 64;
+  const int k = wave * 16 + l16;      // behind k0; rows of W beyond the last are out of the descriptors' range
+  const Buffer Wg = matrix_of<T>(a.Wg, k0, K - k0 < 64 ? K - k0 : 64, n), Wu = matrix_of<T>(a.Wu, k0, K - k0 < 64 ? K - k0 : 64, n);
+  const int64_t steps = (n + 31) / 32;
+  typename N::Vec acc[kTiles] = {};
+  T next[ManyRows<T>::kPer][4];
+  S.fetch(dg, first, rows, n, n, 0, next);
+  for (int64_t s = 0; s < 2 * steps; ++s) {
+    T v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const unsigned c = (unsigned)(s % steps * 32) + q * 8 + j, at = c < n ? ((unsigned)k * (unsigned)n + c) * e : kNowhere;
+      v[j] = s < steps ? load1<T>(Wg, at) : load1<T>(Wu, at);
+    }
+    const typename N::Parts w = N::parts(v);
+    __syncthreads();
+    S.put(next);
+    __syncthreads();
+    if (s + 1 < 2 * steps) S.fetch(s + 1 < steps ? dg : du, first, rows, n, n, (s + 1) % steps * 32, next);
+#pragma unroll
+    for (int rt = 0; rt < kTiles; rt += 2) {
+      const typename N::Parts x0 = S.X.read(rt * 16 + l16, q * 8), x1 = S.X.read(rt * 16 + 16 + l16, q * 8);
+      N::template mma<2>({&x0, &x1}, {&w, &w}, {&acc[rt], &acc[rt + 1]});
+    }
+  }
+#pragma unroll
+  for (int h = 0; h < kTiles; h += 4) {
+    const Buffer to = rows_of<T>((T*)a.gx + row0 * a.ld_gx, first + h * 16, rows, a.ld_gx, K);
+#pragma unroll
+    for (int rt = 0; rt < 4; ++rt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const T v = acc[h + rt][i];
+        store1(v, to, k0 + k < K ? (rt * 16 + N::row(q, i)) * (unsigned)(a.ld_gx * e) + (unsigned)(k0 + k) * e : kNowhere);
+      }
+  }
+}
+
+// the weights' gradients of a piece of rows: 64 columns of x by 32 C of W a workgroup, 32 by 16 C a wave, over the 32-row steps of a split;
+// partial sums as k_gated_gw leaves them, to which the pieces after the first add
+template <class T>
+constexpr int kManyCols = sizeof(T) == 4 ? 2 : 1;   // C
+
+template <class T>
+__global__ void __launch_bounds__(kThreads, 2) k_gated_many_gw(GatedArgs a, int64_t row0, int64_t rows, const T* dg, const T* du, int splits, T* part, int add) {
+  using N = Num<T>;
+  constexpr int C = kManyCols<T>, e = sizeof(T);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, q = lane >> 4;
+  const int64_t n = a.d_out, K = a.d_in, ct = (n + 32 * C - 1) / (32 * C), kt = (K + 63) / 64;
+  const int64_t c0 = blockIdx.x % ct * (32 * C) + wave % 2 * (16 * C), k0 = blockIdx.x / ct % kt * 64 + wave / 2 * 32, split = blockIdx.x / (ct * kt);
+  const T* x = (const T*)a.x + row0 * a.ld_x;
+  typename N::Vec sg[2][C] = {}, su[2][C] = {};
+  T bg[C] = {}, bu[C] = {};
+  const int64_t steps = (rows + 31) / 32;
+  for (int64_t s = split; s < steps; s += splits) {
+    const Buffer in = rows_of<T>(x, s * 32, rows, a.ld_x, K), in_g = rows_of<T>(dg, s * 32, rows, n, n), in_u = rows_of<T>(du, s * 32, rows, n, n);
+    typename N::Parts xt[2], pg[C], pu[C];
+    T v[8];
+#pragma unroll
+    for (int d = 0; d < 2; ++d) {
+      const int64_t k = k0 + d * 16 + l16;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = load1<T>(in, k < K ? (q * 8 + j) * (unsigned)(a.ld_x * e) + (unsigned)k * e : kNowhere);
+      xt[d] = N::parts(v);
+    }
+#pragma unroll
+    for (int h = 0; h < C; ++h) {
+      const int64_t c = c0 + h * 16 + l16;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        v[j] = load1<T>(in_g, c < n ? (q * 8 + j) * (unsigned)(n * e) + (unsigned)c * e : kNowhere);
+        bg[h] += v[j];
+      }
+      pg[h] = N::parts(v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        v[j] = load1<T>(in_u, c < n ? (q * 8 + j) * (unsigned)(n * e) + (unsigned)c * e : kNowhere);
+        bu[h] += v[j];
+      }
+      pu[h] = N::parts(v);
+    }
+#pragma unroll
+    for (int h = 0; h < C; ++h)
+      N::template mma<4>({&xt[0], &xt[0], &xt[1], &xt[1]}, {&pg[h], &pu[h], &pg[h], &pu[h]}, {&sg[0][h], &su[0][h], &sg[1][h], &su[1][h]});
+  }
+  T* to = part + split * 2 * (K + 1) * n;
+#pragma unroll
+  for (int h = 0; h < C; ++h) {
+    const int64_t c = c0 + h * 16 + l16;
+    bg[h] += __shfl_xor(bg[h], 16);
+    bg[h] += __shfl_xor(bg[h], 32);
+    bu[h] += __shfl_xor(bu[h], 16);
+    bu[h] += __shfl_xor(bu[h], 32);
+    if (c >= n) continue;
+#pragma unroll
+    for (int d = 0; d < 2; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int64_t k = k0 + d * 16 + N::row(q, i);
+        if (k >= K) continue;
+        T *g = to + k * n + c, *u = to + (K + 1 + k) * n + c;
+        *g = add ? *g + sg[d][h][i] : sg[d][h][i];
+        *u = add ? *u + su[d][h][i] : su[d][h][i];
+      }
+    if (k0 == 0 && q == 0) {
+      T *g = to + K * n + c, *u = to + (2 * K + 1) * n + c;
+      *g = add ? *g + bg[h] : bg[h];
+      *u = add ? *u + bu[h] : bu[h];
+    }
+  }
+}
+
+// ---- launches -----------------------------------------------------------------------------------------------------------------------
+
+constexpr int kMostUnits = 256;   // compute units that the workspace is sized for
+
+template <class T>
+int gw_waves(int64_t K) { return K > 64 ? kGwWaves<T, 4> : kGwWaves<T, 1>; }
+
+// How the rows are split for the weights' gradients: eight waves (fp64 with its registers: four) for each compute unit, but partial
+// sums of at most 64 MiB.
+template <class T>
+int64_t gw_splits(int64_t rows, int64_t K, int64_t n, int cus) {
+  const int64_t wide = 16 * gw_waves<T>(K), cols = (n + wide - 1) / wide, blocks = (rows + kRows - 1) / kRows;
+  const int64_t most = std::max<int64_t>(1, ((int64_t)64 << 20) / (2 * (K + 1) * n * (int64_t)sizeof(T)));
+  return std::max<int64_t>(1, std::min({blocks, 8 / gw_waves<T>(K) * cus / cols, most}));
+}
+
+// How the columns of W are split for gx: where the rows alone leave compute units without work
+template <class T>
+int64_t gx_splits(int64_t rows, int64_t K, int64_t n, int cus) {
+  const int64_t wide = 16 * (K > 64 ? kGxWaves<T, 4> * kGxTiles<T, 4> : kGxWaves<T, 1> * kGxTiles<T, 1>), blocks = (rows + wide - 1) / wide;
+  return std::max<int64_t>(1, std::min((n + 31) / 32, cus / blocks));
+}
+
+template <class T>
+size_t operand_bytes(int64_t K, int64_t n) { return (size_t)((n + 31) / 32 * ((K + 31) / 32) * 8 * Num<T>::kUnits * 64 * 16); }
+
+size_t up(size_t v) { return (v + 255) / 256 * 256; }
+
+// splits of the rows of a piece for k_gated_many_gw
+template <class T>
+int64_t many_splits(int64_t rows, int64_t K, int64_t n, int cus) {
+  constexpr int64_t wide = 32 * kManyCols<T>, element = sizeof(T);
+  const int64_t tiles = (n + wide - 1) / wide * ((K + 63) / 64), steps = (std::min(rows, kPiece) + 31) / 32;
+  const int64_t most = std::max<int64_t>(1, ((int64_t)64 << 20) / (2 * (K + 1) * n * element));
+  return std::max<int64_t>(1, std::min({(steps + 7) / 8, 2 * cus / tiles, most}));
+}
+
+template <class T>
+size_t workspace_bytes(int64_t rows, int64_t K, int64_t n) {
+  const size_t e = sizeof(T), part = 2 * (K + 1) * n * e;
+  if (K <= kMaxIn) {
+    const int64_t gx = gx_splits<T>(rows, K, n, kMostUnits);
+    return up(operand_bytes<T>(K, n)) + up(gw_splits<T>(rows, K, n, kMostUnits) * part) + (gx > 1 ? up(gx * rows * K * e) : 0);
+  }
+  return 2 * up(std::min(rows, kPiece) * n * e) + up(many_splits<T>(rows, K, n, kMostUnits) * part);
+}
+
+template <class T, int KS, int NT, int kAct>
+hipError_t launch_fwd(const GatedArgs& a, int cus, hipStream_t st) {
+  const int64_t cols = (a.d_out + 64 * NT - 1) / (64 * NT), blocks = (a.rows + kRows - 1) / kRows;
+  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(blocks, 2 * cus / cols));
+  const dim3 grid((unsigned)(cols * splits));
+  const bool vec = a.ld_x % 4 == 0 && a.d_in % 4 == 0 && a.ld_out % 2 == 0 && a.d_out % 2 == 0;
+  if (vec) k_gated_fwd<T, KS, NT, kAct, true><<<grid, kThreads, 0, st>>>(a, (int)cols, (int)splits);
+  else k_gated_fwd<T, KS, NT, kAct, false><<<grid, kThreads, 0, st>>>(a, (int)cols, (int)splits);
+  return hipGetLastError();
+}
+
+template <class T, int kAct>
+hipError_t forward_act(const GatedArgs& a, int cus, hipStream_t st) {
+  if (a.d_in > kMaxIn) {
+    const int64_t tiles = (a.d_out + 63) / 64, most = std::max<int64_t>(1, ((int64_t)1 << 22) / tiles) * kManyRows<T>;   // rows of a launch
+    for (int64_t r = 0; r < a.rows; r += most) {
+      const int64_t rows = std::min(a.rows - r, most);
+      k_gated_many<T, kAct, false><<<dim3((unsigned)((rows + kManyRows<T> - 1) / kManyRows<T> * tiles)), kThreads, 0, st>>>(a, r, rows, (T*)nullptr, (T*)nullptr);
+    }
+    return hipGetLastError();
+  }
+  // 32 columns a wave where that leaves every compute unit two workgroups, else 16 (fp64 and more columns of x: 16, for the registers)
+  const bool wide = sizeof(T) == 4 && (a.d_out + 127) / 128 * ((a.rows + kRows - 1) / kRows) >= 2 * cus;
+  switch ((a.d_in + 31) / 32) {
+    case 1:
+      if constexpr (sizeof(T) == 4)
+        if (wide) return launch_fwd<T, 1, 2, kAct>(a, cus, st);
+      return launch_fwd<T, 1, 1, kAct>(a, cus, st);
+    case 2:
+      if constexpr (sizeof(T) == 4)
+        if (wide) return launch_fwd<T, 2, 2, kAct>(a, cus, st);
+      return launch_fwd<T, 2, 1, kAct>(a, cus, st);
+    case 3: return launch_fwd<T, 3, 1, kAct>(a, cus, st);
+    default: return launch_fwd<T, 4, 1, kAct>(a, cus, st);
+  }
+}
+
+template <class T>
+hipError_t sum_splits(const GatedArgs& a, const T* part, int64_t splits, hipStream_t st) {
+  k_gated_sums<T><<<dim3((unsigned)((2 * (a.d_in + 1) * a.d_out + kThreads - 1) / kThreads)), kThreads, 0, st>>>(
+      part, (int)splits, a.d_in, a.d_out, (T*)a.gWg, (T*)a.gWu, (T*)a.gbg, (T*)a.gbu);
+  return hipGetLastError();
+}
+
+template <class T, int KS, int kAct>
+hipError_t launch_bwd(const GatedArgs& a, int cus, char* ws, hipStream_t st) {
+  const int64_t K = a.d_in, n = a.d_out, wide = 16 * kGwWaves<T, KS>, cols = (n + wide - 1) / wide;
+  const int64_t gws = gw_splits<T>(a.rows, K, n, cus), gxs = gx_splits<T>(a.rows, K, n, cus);
+  u32x4* ops = (u32x4*)ws;
+  T* part = (T*)(ws + up(operand_bytes<T>(K, n)));
+  T* gx_part = (T*)((char*)part + up(gw_splits<T>(a.rows, K, n, kMostUnits) * 2 * (K + 1) * n * sizeof(T)));
+  k_gated_operands<T, KS><<<dim3((unsigned)(((n + 31) / 32 * kOperands<KS> + 3) / 4)), kThreads, 0, st>>>(a, ops);
+  constexpr int kGxRows = kGxWaves<T, KS> * kGxTiles<T, KS> * 16, kGxThreads = kGxWaves<T, KS> * 64, kGwThreads = kGwWaves<T, KS> * 64;
+  const dim3 gw((unsigned)(cols * gws)), gx((unsigned)((a.rows + kGxRows - 1) / kGxRows * gxs));
+  const bool vec_x = a.ld_x % 4 == 0 && K % 4 == 0, vec = vec_x && a.ld_gout % 4 == 0 && n % 4 == 0 && a.ld_gx % 4 == 0;
+  if (vec) k_gated_gx<T, KS, kAct, true><<<gx, kGxThreads, 0, st>>>(a, ops, (int)gxs, gx_part);
+  else k_gated_gx<T, KS, kAct, false><<<gx, kGxThreads, 0, st>>>(a, ops, (int)gxs, gx_part);
+  if (gxs > 1) k_gated_gx_sums<T><<<dim3((unsigned)((a.rows * K + kThreads - 1) / kThreads)), kThreads, 0, st>>>(gx_part, (int)gxs, a.rows, K, (T*)a.gx, a.ld_gx);
+  if (vec_x) k_gated_gw<T, KS, kAct, true><<<gw, kGwThreads, 0, st>>>(a, (int)cols, (int)gws, part);
+  else k_gated_gw<T, KS, kAct, false><<<gw, kGwThreads, 0, st>>>(a, (int)cols, (int)gws, part);
+  return sum_splits<T>(a, part, gws, st);
+}
+
+template <class T, int kAct>
+hipError_t backward_act(const GatedArgs& a, int cus, char* ws, hipStream_t st) {
+  switch ((a.d_in + 31) / 32) {
+    case 1: return launch_bwd<T, 1, kAct>(a, cus, ws, st);
+    case 2: return launch_bwd<T, 2, kAct>(a, cus, ws, st);
+    case 3: return launch_bwd<T, 3, kAct>(a, cus, ws, st);
+    case 4: return launch_bwd<T, 4, kAct>(a, cus, ws, st);
+    default: break;
+  }
+  const int64_t K = a.d_in, n = a.d_out, splits = many_splits<T>(a.rows, K, n, cus);
+  const int64_t ct = (n + 63) / 64, kt = (K + 63) / 64, gt = (n + 32 * kManyCols<T> - 1) / (32 * kManyCols<T>);
+  T* dg = (T*)ws;
+  T* du = (T*)(ws + up(std::min(a.rows, kPiece) * n * sizeof(T)));
+  T* part = (T*)((char*)du + up(std::min(a.rows, kPiece) * n * sizeof(T)));
+  for (int64_t r = 0; r < a.rows; r += kPiece) {
+    const int64_t rows = std::min(kPiece, a.rows - r), rb = (rows + kManyRows<T> - 1) / kManyRows<T>;
+    k_gated_many<T, kAct, true><<<dim3((unsigned)(rb * ct)), kThreads, 0, st>>>(a, r, rows, dg, du);
+    k_gated_many_gx<T><<<dim3((unsigned)(rb * kt)), kThreads, 0, st>>>(a, r, rows, dg, du);
+    k_gated_many_gw<T><<<dim3((unsigned)(gt * kt * splits)), kThreads, 0, st>>>(a, r, rows, dg, du, (int)splits, part, r > 0);
+  }
+  return sum_splits<T>(a, part, splits, st);
+}
+
+template <class T>
+hipError_t forward(const GatedArgs& a, int cus, hipStream_t st) {
+  switch (a.act) {
+    case CGTP_ACT_NONE: return forward_act<T, CGTP_ACT_NONE>(a, cus, st);
+    case CGTP_ACT_SILU: return forward_act<T, CGTP_ACT_SILU>(a, cus, st);
+    case CGTP_ACT_GELU: return forward_act<T, CGTP_ACT_GELU>(a, cus, st);
+    case CGTP_ACT_SIGMOID: return forward_act<T, CGTP_ACT_SIGMOID>(a, cus, st);
+    default: return forward_act<T, CGTP_ACT_TANH>(a, cus, st);
+  }
+}
+
+template <class T>
+hipError_t backward(const GatedArgs& a, int cus, char* ws, hipStream_t st) {
+  switch (a.act) {
+    case CGTP_ACT_NONE: return backward_act<T, CGTP_ACT_NONE>(a, cus, ws, st);
+    case CGTP_ACT_SILU: return backward_act<T, CGTP_ACT_SILU>(a, cus, ws, st);
+    case CGTP_ACT_GELU: return backward_act<T, CGTP_ACT_GELU>(a, cus, ws, st);
+    case CGTP_ACT_SIGMOID: return backward_act<T, CGTP_ACT_SIGMOID>(a, cus, ws, st);
+    default: return backward_act<T, CGTP_ACT_TANH>(a, cus, ws, st);
+  }
+}
+
+}  // namespace
+}  // namespace cgtp
