@@ -6,6 +6,7 @@
 #include <memory>
 #include <new>
 #include <string>
+#include <vector>
 
 #include "csr.hpp"
 #include "layer.hpp"
@@ -60,6 +61,56 @@ cgtp_status check_gated(const cgtp::GatedArgs& a, int32_t dtype) {
   for (int64_t ld : {a.ld_x, a.ld_out, a.ld_gout, a.ld_gx})   // 64 rows are addressed with 31 bits
     if (ld >= 1 << 22) return fail(CGTP_EUNSUPPORTED, "row strides must be below 2^22");
   return CGTP_OK;
+}
+
+// How a call of the normalisation is cut up, and its workspace: shares and totals of long samples, partial sums of the parameters' gradients.
+struct NormWork {
+  int64_t R = 0;            // rows of a chunk
+  int64_t blocks = 1;       // workgroups (of each sub-unit)
+  int64_t sum_rows = 1;     // partial sums
+  bool longer = false;      // samples of more than R rows are possible
+  size_t part = 0, total = 0, bytes = 0;
+  NormWork(const cgtp::Norm& P, int64_t N, int64_t S, bool ptr, bool backward) {
+    auto up = [](size_t v) { return (v + 255) / 256 * 256; };
+    const size_t units = P.seg.size() * (size_t)P.groups;
+    const int64_t most = 1 << 23;   // workgroups of a launch: 2^32 threads are too many (a normalisation has at most 2^14 sub-units)
+    if (!P.covered) {
+      blocks = std::min<int64_t>(S * (int64_t)units, 1 << 20);
+      sum_rows = S;
+    } else if (!ptr) {
+      // Forward: a wave takes a few steps of rows; backward, where each workgroup leaves sums: as many workgroups as stay on the chip
+      int rows = 1;
+      for (const cgtp::NormSeg& s : P.seg) rows = std::max(rows, s.rows);
+      const int64_t steps = (N + 4 * rows - 1) / (4 * rows);
+      blocks = std::max<int64_t>(1, backward ? std::min<int64_t>(steps, std::max(1, 2048 / P.subs)) : std::min<int64_t>(steps, std::max<int64_t>(1, most / P.subs)));
+      sum_rows = blocks;
+    } else {
+      R = 64;
+      while (R < 256 && N > R * 512) R *= 2;
+      while ((N + R - 1) / R > most / P.subs) R *= 2;
+      blocks = std::max<int64_t>(1, (N + R - 1) / R);
+      sum_rows = blocks;
+      longer = N > R;
+      if (longer) {
+        part = up((size_t)blocks * 2 * units * 4 * sizeof(double));
+        total = up((size_t)blocks * units * 4 * P.elt());
+      }
+    }
+    bytes = part + total + (backward ? up((size_t)sum_rows * (size_t)(P.n_w + P.n_b) * sizeof(double)) : 0);
+  }
+};
+
+struct Function {
+  hipFunction_t* fn;
+  const char* name;
+};
+
+// the functions of a normalisation's module
+std::vector<Function> functions(cgtp::Norm& N) {
+  if (!N.covered) return {{&N.unit_fwd, "cgtp_norm_unit_fwd"}, {&N.unit_bwd, "cgtp_norm_unit_bwd"}, {&N.sums, "cgtp_norm_sums"}};
+  return {{&N.row_fwd, "cgtp_norm_row_fwd"},   {&N.row_bwd, "cgtp_norm_row_bwd"},     {&N.part_fwd, "cgtp_norm_part_fwd"}, {&N.mean_fwd, "cgtp_norm_mean_fwd"},
+          {&N.graph_fwd, "cgtp_norm_graph_fwd"}, {&N.part_bwd, "cgtp_norm_part_bwd"}, {&N.mean_bwd, "cgtp_norm_mean_bwd"}, {&N.graph_bwd, "cgtp_norm_graph_bwd"},
+          {&N.sums, "cgtp_norm_sums"}};
 }
 
 }  // namespace
@@ -180,7 +231,7 @@ cgtp_status cgtp_norm_create(const char* irreps, int32_t groups, int32_t act, do
           N.n_b += s.mul;
         }
     N.n_stat = (int64_t)places * groups * 2;
-    cgtp::emit_norm(N, N.fwd, N.bwd, N.sums);
+    cgtp::emit_norm(N);
     // the kernels are loaded on `device`; the caller's current device is restored on return
     struct Restore {
       int device = -1;
@@ -198,9 +249,14 @@ cgtp_status cgtp_norm_create(const char* irreps, int32_t groups, int32_t act, do
         return fail(CGTP_EUNSUPPORTED, std::string("this library targets gfx950, device is ") + prop.gcnArchName);
     }
     try {
-      for (cgtp::Kernel* k : {&N.fwd, &N.bwd, &N.sums}) cgtp::jit_compile(*k, device);
+      cgtp::jit_compile(N.code, device);
+      if (device >= 0)
+        for (const Function& f : functions(N)) {
+          hipError_t e = hipModuleGetFunction(f.fn, N.code.module, f.name);
+          if (e != hipSuccess) throw std::runtime_error(std::string("hipModuleGetFunction failed for ") + f.name + ": " + hipGetErrorString(e));
+        }
     } catch (const std::exception& e) {
-      for (cgtp::Kernel* k : {&N.fwd, &N.bwd, &N.sums}) cgtp::jit_unload(*k);
+      cgtp::jit_unload(N.code);
       return fail(CGTP_ECOMPILE, e.what());
     }
     *out = H.release();
@@ -214,7 +270,7 @@ cgtp_status cgtp_norm_create(const char* irreps, int32_t groups, int32_t act, do
 
 cgtp_status cgtp_norm_destroy(cgtp_norm* norm) {
   if (!norm) return CGTP_OK;
-  for (cgtp::Kernel* k : {&norm->N.fwd, &norm->N.bwd, &norm->N.sums}) cgtp::jit_unload(*k);
+  cgtp::jit_unload(norm->N.code);
   delete norm;
   return CGTP_OK;
 }
@@ -233,8 +289,8 @@ int64_t cgtp_norm_dim(const cgtp_norm* norm, int32_t which) {
 }
 
 size_t cgtp_norm_workspace_bytes(const cgtp_norm* norm, int64_t N, int64_t S, int32_t ptr, int32_t backward) {
-  if (!norm || N < 0 || S < 0 || (!ptr && N != S)) return 0;
-  return backward ? (size_t)S * (size_t)(norm->N.n_w + norm->N.n_b) * 8 : 0;
+  if (!norm || N < 0 || S < 0 || N > INT32_MAX || S > INT32_MAX || (!ptr && N != S) || S == 0) return 0;
+  return NormWork(norm->N, N, S, ptr != 0, backward != 0).bytes;
 }
 
 }  // extern "C"
@@ -248,13 +304,18 @@ cgtp_status check_norm(const cgtp_norm* norm, int64_t N, int64_t S, const int64_
   if (N > INT32_MAX || S > INT32_MAX) return fail(CGTP_EUNSUPPORTED, "N and S must be below 2^31");
   for (const void* p : data)
     if (!aligned(p, 16)) return fail(CGTP_EINVAL, "data pointers must be 16-byte aligned");
-  if (!norm->N.fwd.fn) return fail(CGTP_EUNSUPPORTED, "kernel " + norm->N.fwd.name + " is not loaded (created without a device?)");
+  if (!norm->N.sums) return fail(CGTP_EUNSUPPORTED, "kernel " + norm->N.code.name + " is not loaded (created without a device?)");
   return CGTP_OK;
 }
 
-cgtp_status launch(const cgtp::Kernel& k, unsigned grid, void** args, hipStream_t st) {
-  HIP_TRY(hipModuleLaunchKernel(k.fn, grid, 1, 1, (unsigned)k.wg, 1, 1, 0, st, args, nullptr));
+cgtp_status launch(hipFunction_t fn, int64_t grid, void** args, hipStream_t st) {
+  HIP_TRY(hipModuleLaunchKernel(fn, (unsigned)grid, 1, 1, 256, 1, 1, 0, st, args, nullptr));
   return CGTP_OK;
+}
+
+cgtp_status launch_sums(const cgtp::Norm& P, const double* sums, int64_t rows, void* gweight, void* gbias, hipStream_t st) {
+  void* args[] = {(void*)&sums, (void*)&rows, (void*)&gweight, (void*)&gbias};
+  return launch(P.sums, (P.n_w + P.n_b + 15) / 16, args, st);
 }
 
 }  // namespace
@@ -268,11 +329,28 @@ cgtp_status norm_forward(const cgtp_norm* norm, const void* x, const void* weigh
   if (S == 0) return CGTP_OK;
   const cgtp::Norm& P = norm->N;
   if ((N > 0 && (!x || !y)) || !weight || (P.n_b && !bias)) return fail(CGTP_EINVAL, "NULL data pointer");
-  const size_t need = cgtp_norm_workspace_bytes(norm, N, S, ptr != nullptr, 0);
-  if (!workspace_serves(workspace, workspace_bytes, need)) return bad_workspace("cgtp_norm_workspace_bytes", need);
-  const int64_t units = S * (int64_t)P.seg.size() * P.groups;
-  void* args[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&y, (void*)&stats, (void*)&N, (void*)&S, (void*)&ptr};
-  return launch(P.fwd, (unsigned)std::min<int64_t>(units, 1 << 20), args, (hipStream_t)hip_stream);
+  const NormWork w(P, N, S, ptr != nullptr, false);
+  if (!workspace_serves(workspace, workspace_bytes, w.bytes)) return bad_workspace("cgtp_norm_workspace_bytes", w.bytes);
+  hipStream_t st = (hipStream_t)hip_stream;
+  int64_t R = w.R;
+  double* part = (double*)workspace;
+  void* total = (char*)workspace + w.part;
+  if (!P.covered) {
+    void* args[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&y, (void*)&stats, (void*)&N, (void*)&S, (void*)&ptr};
+    return launch(P.unit_fwd, w.blocks, args, st);
+  }
+  if (!ptr) {
+    void* args[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&y, (void*)&stats, (void*)&N};
+    return launch(P.row_fwd, w.blocks * P.subs, args, st);
+  }
+  if (w.longer) {
+    void* pargs[] = {(void*)&x, (void*)&part, (void*)&ptr, (void*)&N, (void*)&S, (void*)&R};
+    if ((s = launch(P.part_fwd, w.blocks * P.subs, pargs, st)) != CGTP_OK) return s;
+    void* margs[] = {(void*)&x, (void*)&part, (void*)&total, (void*)&stats, (void*)&ptr, (void*)&N, (void*)&S, (void*)&R};
+    if ((s = launch(P.mean_fwd, w.blocks, margs, st)) != CGTP_OK) return s;
+  }
+  void* args[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&y, (void*)&stats, (void*)&total, (void*)&ptr, (void*)&N, (void*)&S, (void*)&R};
+  return launch(P.graph_fwd, w.blocks * P.subs, args, st);
 }
 
 cgtp_status norm_backward(const cgtp_norm* norm, const void* x, const void* weight, const void* bias, const void* gy,
@@ -289,15 +367,30 @@ cgtp_status norm_backward(const cgtp_norm* norm, const void* x, const void* weig
     return CGTP_OK;
   }
   if ((N > 0 && (!x || !gy || !gx)) || !weight || (P.n_b && !bias) || !stats) return fail(CGTP_EINVAL, "NULL data pointer");
-  const size_t need = cgtp_norm_workspace_bytes(norm, N, S, ptr != nullptr, 1);
-  if (!workspace_serves(workspace, workspace_bytes, need)) return bad_workspace("cgtp_norm_workspace_bytes", need);
-  const int64_t units = S * (int64_t)P.seg.size() * P.groups;
+  const NormWork w(P, N, S, ptr != nullptr, true);
+  if (!workspace_serves(workspace, workspace_bytes, w.bytes)) return bad_workspace("cgtp_norm_workspace_bytes", w.bytes);
+  int64_t R = w.R;
   double* part = (double*)workspace;
-  void* args[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&gy, (void*)&stats, (void*)&gx, (void*)&part, (void*)&N, (void*)&S, (void*)&ptr};
-  s = launch(P.bwd, (unsigned)std::min<int64_t>(units, 1 << 20), args, st);
+  void* total = (char*)workspace + w.part;
+  double* sums = (double*)((char*)workspace + w.part + w.total);
+  if (!P.covered) {
+    void* args[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&gy, (void*)&stats, (void*)&gx, (void*)&sums, (void*)&N, (void*)&S, (void*)&ptr};
+    s = launch(P.unit_bwd, w.blocks, args, st);
+  } else if (!ptr) {
+    void* args[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&gy, (void*)&stats, (void*)&gx, (void*)&sums, (void*)&N};
+    s = launch(P.row_bwd, w.blocks * P.subs, args, st);
+  } else {
+    if (w.longer) {
+      void* pargs[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&gy, (void*)&stats, (void*)&part, (void*)&ptr, (void*)&N, (void*)&S, (void*)&R};
+      if ((s = launch(P.part_bwd, w.blocks * P.subs, pargs, st)) != CGTP_OK) return s;
+      void* margs[] = {(void*)&part, (void*)&total, (void*)&ptr, (void*)&N, (void*)&S, (void*)&R};
+      if ((s = launch(P.mean_bwd, w.blocks, margs, st)) != CGTP_OK) return s;
+    }
+    void* args[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&gy, (void*)&stats, (void*)&gx, (void*)&sums, (void*)&total, (void*)&ptr, (void*)&N, (void*)&S, (void*)&R};
+    s = launch(P.graph_bwd, w.blocks * P.subs, args, st);
+  }
   if (s != CGTP_OK) return s;
-  void* sargs[] = {(void*)&part, (void*)&S, (void*)&gweight, (void*)&gbias};
-  return launch(P.sums, (unsigned)((P.n_w + P.n_b + 15) / 16), sargs, st);
+  return launch_sums(P, sums, w.sum_rows, gweight, gbias, st);
 }
 
 }  // extern "C"

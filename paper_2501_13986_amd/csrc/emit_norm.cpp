@@ -5,6 +5,7 @@
 //   0e:      y = act(w xh + b)         l = dE/d(w xh + b) = gy act'
 //   others:  y = w xh q                l = gy q;  gates: l_g = q (1 - q) sum_m gy w xh
 //   gw = sum l xh, gb = sum l, h = w l,  gx = r (h - [0e, gates: mean(h)] - xh mean(h xh))
+#include <algorithm>
 #include <sstream>
 
 #include "norm.hpp"
@@ -23,6 +24,8 @@ __device__ inline float exp_(float t) { return expf(t); }
 __device__ inline double exp_(double t) { return exp(t); }
 __device__ inline float tanh_(float t) { return tanhf(t); }
 __device__ inline double tanh_(double t) { return tanh(t); }
+__device__ inline float sqrt_(float t) { return sqrtf(t); }
+__device__ inline double sqrt_(double t) { return sqrt(t); }
 __device__ inline float fma_(float a, float b, float c) { return __builtin_fmaf(a, b, c); }
 __device__ inline double fma_(double a, double b, double c) { return __builtin_fma(a, b, c); }
 
@@ -156,8 +159,663 @@ __device__ inline double block_sum_(double v, double* lds) {
 }
 )HIP";
 
-// One workgroup for each unit of a sample, whatever its length: the rows are read once for each of mean, variance and result.
-const char kForward[] = R"HIP(
+// ---- a wave's lanes over a segment ----
+//
+// A lane has V J channels of one group: (j L + li) V + k, li < L its place among the group's L lanes.  A wave takes GP groups and RP rows a step; the
+// groups of a segment take PH phases of GP.  All of a segment's words of a step stay in registers.
+const char kLanes[] = R"HIP(
+// sum over the L lanes of a group, the same in each of them; the order is fixed
+template <int ctrl> __device__ inline float dpp_(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), ctrl, 0xf, 0xf, false)); }
+template <int ctrl> __device__ inline double dpp_(double v) {
+  const long long b = __builtin_bit_cast(long long, v);
+  const int lo = __builtin_amdgcn_update_dpp(0, (int)b, ctrl, 0xf, 0xf, false), hi = __builtin_amdgcn_update_dpp(0, (int)(b >> 32), ctrl, 0xf, 0xf, false);
+  return __builtin_bit_cast(double, (long long)(((unsigned long long)(unsigned)hi << 32) | (unsigned)lo));
+}
+template <int L, class X> __device__ inline X lanes_sum_(X v) {
+  if constexpr (L > 1) v += dpp_<0xB1>(v);     // neighbour
+  if constexpr (L > 2) v += dpp_<0x4E>(v);     // other pair
+  if constexpr (L > 4) v += dpp_<0x141>(v);    // the other four, mirrored (within four all are alike by now)
+  if constexpr (L > 8) v += dpp_<0x140>(v);
+  if constexpr (L > 16) v += __shfl_xor(v, 16);
+  if constexpr (L > 32) v += __shfl_xor(v, 32);
+  return v;
+}
+
+template <int w> struct Wide_ { typedef T type __attribute__((ext_vector_type(w))); };
+// w words that are neighbours in memory
+template <int w, bool vec> __device__ inline void get_(const T* p, T* v) {
+  if constexpr (vec && w % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < w; i += 4) {
+      const typename Wide_<4>::type q = *(const typename Wide_<4>::type*)(p + i);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[i + k] = q[k];
+    }
+  } else if constexpr (vec && w % 2 == 0) {
+#pragma unroll
+    for (int i = 0; i < w; i += 2) {
+      const typename Wide_<2>::type q = *(const typename Wide_<2>::type*)(p + i);
+      v[i] = q[0];
+      v[i + 1] = q[1];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < w; ++i) v[i] = p[i];
+  }
+}
+template <int w, bool vec> __device__ inline void put_(T* p, const T* v) {
+  if constexpr (vec && w % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < w; i += 4) *(typename Wide_<4>::type*)(p + i) = typename Wide_<4>::type{v[i], v[i + 1], v[i + 2], v[i + 3]};
+  } else if constexpr (vec && w % 2 == 0) {
+#pragma unroll
+    for (int i = 0; i < w; i += 2) *(typename Wide_<2>::type*)(p + i) = typename Wide_<2>::type{v[i], v[i + 1]};
+  } else {
+#pragma unroll
+    for (int i = 0; i < w; ++i) p[i] = v[i];
+  }
+}
+
+template <int s> struct Lane {
+  static constexpr int n = SEG[s].n, V = SEG[s].V, J = SEG[s].J, L = SEG[s].lanes, GP = SEG[s].at_once, RP = SEG[s].rows, cg = SEG[s].mul / G, C = V * J;
+  static constexpr bool gated = SEG[s].gate >= 0, inv = SEG[s].inv, vec = SEG[s].vec, full = L * C == cg;
+  int li, gq, rho, g;       // place in the group, group of the step, row of the step, group
+  bool on;                  // lanes that are left over repeat the first row's
+  __device__ Lane(int phase) {
+    const int lane = threadIdx.x & 63, at = lane / L;
+    on = at < GP * RP;
+    li = lane % L;
+    gq = at % GP;
+    rho = on ? at / GP : 0;
+    g = phase * GP + gq;
+  }
+  __device__ bool has(int j) const { return full || (j * L + li) * V < cg; }
+  __device__ int channel(int j) const { return g * cg + (full || (j * L + li) * V < cg ? (j * L + li) * V : 0); }
+  // words of channels channel(j) + k, component m at v[(j V + k) n + m]; base: the row's first word of the segment
+  __device__ void read(const T* base, T* v) const {
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      if constexpr (IR_MUL) {
+#pragma unroll
+        for (int m = 0; m < n; ++m) {
+          T w[V];
+          get_<V, vec>(base + m * SEG[s].mul + channel(j), w);
+#pragma unroll
+          for (int k = 0; k < V; ++k) v[(j * V + k) * n + m] = w[k];
+        }
+      } else {
+        get_<V * n, vec>(base + channel(j) * n, v + j * V * n);
+      }
+    }
+  }
+  __device__ void write(T* base, const T* v) const {
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      if (!has(j)) continue;
+      if constexpr (IR_MUL) {
+#pragma unroll
+        for (int m = 0; m < n; ++m) {
+          T w[V];
+#pragma unroll
+          for (int k = 0; k < V; ++k) w[k] = v[(j * V + k) * n + m];
+          put_<V, vec>(base + m * SEG[s].mul + channel(j), w);
+        }
+      } else {
+        put_<V * n, vec>(base + channel(j) * n, v + j * V * n);
+      }
+    }
+  }
+  __device__ void read_gates(const T* row, T* g_) const {
+    if constexpr (gated) {
+#pragma unroll
+      for (int j = 0; j < J; ++j) get_<V, vec>(row + SEG[s].gate + channel(j), g_ + j * V);
+    }
+  }
+  __device__ void write_gates(T* row, const T* g_) const {
+    if constexpr (gated) {
+#pragma unroll
+      for (int j = 0; j < J; ++j)
+        if (has(j)) put_<V, vec>(row + SEG[s].gate + channel(j), g_ + j * V);
+    }
+  }
+  __device__ void params(const T* __restrict__ weight, const T* __restrict__ bias, Param* p) const {
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int k = 0; k < V; ++k) p[j * V + k] = param_<s>(weight, bias, channel(j) + k);
+  }
+  __device__ Stat stat(const T* __restrict__ st) const {
+    Stat S = {st[(SEG[s].st * G + g) * 2], st[(SEG[s].st * G + g) * 2 + 1], T(0), T(0)};
+    if constexpr (gated) {
+      S.gmu = st[(SEG[s].gst * G + g) * 2];
+      S.gr = st[(SEG[s].gst * G + g) * 2 + 1];
+    }
+    return S;
+  }
+  __device__ void put_stat(T* st, const Stat& S) const {
+    st[(SEG[s].st * G + g) * 2] = S.mu;
+    st[(SEG[s].st * G + g) * 2 + 1] = S.r;
+    if constexpr (gated) {
+      st[(SEG[s].gst * G + g) * 2] = S.gmu;
+      st[(SEG[s].gst * G + g) * 2 + 1] = S.gr;
+    }
+  }
+  // y of the words in v, in their place
+  __device__ void forward(T* v, const T* g_, const Stat& S, const Param* p) const {
+#pragma unroll
+    for (int c = 0; c < C; ++c) forward_<s>(v + c * n, gated ? g_[c] : T(0), S, p[c]);
+  }
+  // v, g_: of x, then xh; q: of gy, then h; qg: h of the gates.  Adds to the sums of the channels (a) and of the group (o)
+  struct Sum { double w[C], b[C], gw[C], gb[C]; };
+  __device__ Sums backward(T* v, T* g_, T* q, T* qg, const Stat& S, const Param* p, bool in, Sum* a) const {
+    Sums o = {};
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      T none = T(0), none_q = T(0);
+      const Sums t = backward_<s>(v + c * n, gated ? g_[c] : none, q + c * n, gated ? qg[c] : none_q, S, p[c]);
+      const bool count = in && has(c / V);
+      o.h += count ? t.h : T(0);
+      o.hx += count ? t.hx : T(0);
+      o.gh += count ? t.gh : T(0);
+      o.ghx += count ? t.ghx : T(0);
+      if (a) {
+        a->w[c] += count ? (double)t.w : 0.0;
+        if (inv) a->b[c] += count ? (double)t.b : 0.0;
+        if (gated) {
+          a->gw[c] += count ? (double)t.gw : 0.0;
+          a->gb[c] += count ? (double)t.gb : 0.0;
+        }
+      }
+    }
+    return o;
+  }
+  __device__ void finish(const T* v, const T* g_, T* q, T* qg, const Stat& S, const Means& e) const {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      T none = T(0);
+      finish_<s>(v + c * n, gated ? g_[c] : none, q + c * n, gated ? qg[c] : none, S, e);
+    }
+  }
+  // whether the rows of a step are added by shuffles: they are 64 / RP lanes apart
+  static constexpr bool even = (GP * L & (GP * L - 1)) == 0;
+  static __device__ double rows_sum(double v) {
+    if constexpr (even)
+#pragma unroll
+      for (int o = GP * L; o < 64; o *= 2) v += __shfl_xor(v, o);
+    return v;
+  }
+  // the workgroup's sums of the channels' gradients: to + place of the weight or bias.  Four at a time, one for each wave to add up
+  __device__ void put_sums(const Sum& a, double* to, double* lds) const {
+    constexpr int kinds = 1 + (inv ? 1 : 0) + (gated ? 2 : 0);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
+#pragma unroll
+    for (int first = 0; first < C * kinds; first += 4) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (first + i >= C * kinds) break;
+        const int c = (first + i) / kinds, k = (first + i) % kinds;
+        const double v = k == 0 ? a.w[c] : inv ? a.b[c] : k == 1 ? a.gw[c] : a.gb[c];
+        lds[i * 256 + threadIdx.x] = rows_sum(on ? v : 0.0);
+      }
+      __syncthreads();
+      const int c = (first + wave) / kinds, k = (first + wave) % kinds;
+      if (c < C && lane < GP * L && has(c / V)) {     // a lane of the step's first row
+        double t = 0;
+        for (int w = 0; w < 4; ++w)
+          for (int r = 0; r < (even ? 1 : RP); ++r) t += lds[wave * 256 + w * 64 + r * GP * L + lane];
+        const int base = k == 0 ? SEG[s].w : inv ? NW + SEG[s].b : k == 1 ? SEG[s].gw : NW + SEG[s].gb;
+        to[base + channel(c / V) + c % V] = t;
+      }
+    }
+  }
+};
+
+// what a sub-unit (a phase of a segment) is: SUB in the order of their size, the largest first
+template <class F> __device__ inline void with_sub_(int u, F f) { with_segment_<0>(SUB[u].s, f); }
+__device__ inline int sub_() { return blockIdx.x % NSUB; }
+__device__ inline i64 part_() { return blockIdx.x / NSUB; }
+)HIP";
+
+// Every row is a sample: a group's numbers of a row are in the registers of its lanes, read once.  Sums in T: trees of at most 64 words a lane
+// and six levels.
+const char kRowsText[] = R"HIP(
+struct RowFwd {
+  const T* __restrict__ x; const T* __restrict__ weight; const T* __restrict__ bias; T* __restrict__ y; T* __restrict__ stats; i64 N; int phase;
+  template <int s> __device__ void operator()() const {
+    typedef Lane<s> A;
+    const A a(phase);
+    const i64 waves = (gridDim.x / NSUB) * 4;
+    Param p[A::C];
+    a.params(weight, bias, p);
+    for (i64 base = (part_() * 4 + threadIdx.x / 64) * A::RP; base < N; base += waves * A::RP) {
+      const bool in = a.on && base + a.rho < N;
+      const i64 r = base + a.rho < N ? base + a.rho : N - 1;
+      T v[A::C * A::n], g[A::C];
+      a.read(x + r * DX + SEG[s].col, v);
+      a.read_gates(x + r * DX, g);
+      Stat S = {T(0), T(0), T(0), T(0)};
+      auto moments = [&](const T* w, int words, bool centre, T inv_m, T& mu, T& rs) {
+        if (centre) {
+          T t = T(0);
+#pragma unroll
+          for (int i = 0; i < words; ++i) t += A::full || a.has(i / (words / A::J)) ? w[i] : T(0);
+          mu = lanes_sum_<A::L>(t) * inv_m;
+        }
+        T t = T(0);
+#pragma unroll
+        for (int i = 0; i < words; ++i) {
+          const T d = w[i] - mu;
+          t = fma_(A::full || a.has(i / (words / A::J)) ? d : T(0), d, t);
+        }
+        rs = T(1) / sqrt_(fma_(lanes_sum_<A::L>(t), inv_m, T(EPS)));
+      };
+      moments(v, A::C * A::n, A::inv, T(1.0 / (A::cg * A::n)), S.mu, S.r);
+      if constexpr (A::gated) moments(g, A::C, true, T(1.0 / A::cg), S.gmu, S.gr);
+      a.forward(v, g, S, p);
+      if (in) {
+        a.write(y + r * DY + SEG[s].ycol, v);
+        if (stats && a.li == 0) a.put_stat(stats + r * NST, S);
+      }
+    }
+  }
+};
+extern "C" __global__ void __launch_bounds__(256) cgtp_norm_row_fwd(const T* __restrict__ x, const T* __restrict__ weight, const T* __restrict__ bias,
+                                                                T* __restrict__ y, T* __restrict__ stats, i64 N) {
+  with_sub_(sub_(), RowFwd{x, weight, bias, y, stats, N, SUB[sub_()].phase});
+}
+
+struct RowBwd {
+  const T* __restrict__ x; const T* __restrict__ weight; const T* __restrict__ bias; const T* __restrict__ gy; const T* __restrict__ stats;
+  T* __restrict__ gx; double* __restrict__ part; i64 N; int phase; double* lds;
+  template <int s> __device__ void operator()() const {
+    typedef Lane<s> A;
+    const A a(phase);
+    const i64 waves = (gridDim.x / NSUB) * 4;
+    Param p[A::C];
+    a.params(weight, bias, p);
+    typename A::Sum sum = {};
+    for (i64 base = (part_() * 4 + threadIdx.x / 64) * A::RP; base < N; base += waves * A::RP) {
+      const bool in = a.on && base + a.rho < N;
+      const i64 r = base + a.rho < N ? base + a.rho : N - 1;
+      T v[A::C * A::n], q[A::C * A::n], g[A::C], qg[A::C];
+      a.read(x + r * DX + SEG[s].col, v);
+      a.read(gy + r * DY + SEG[s].ycol, q);
+      a.read_gates(x + r * DX, g);
+      const Stat S = a.stat(stats + r * NST);
+      const Sums o = a.backward(v, g, q, qg, S, p, in, &sum);
+      Means e = {T(0), lanes_sum_<A::L>(o.hx) * T(1.0 / (A::cg * A::n)), T(0), T(0)};
+      if constexpr (A::inv) e.h = lanes_sum_<A::L>(o.h) * T(1.0 / A::cg);
+      if constexpr (A::gated) {
+        e.gh = lanes_sum_<A::L>(o.gh) * T(1.0 / A::cg);
+        e.ghx = lanes_sum_<A::L>(o.ghx) * T(1.0 / A::cg);
+      }
+      a.finish(v, g, q, qg, S, e);
+      if (in) {
+        a.write(gx + r * DX + SEG[s].col, q);
+        a.write_gates(gx + r * DX, qg);
+      }
+    }
+    a.put_sums(sum, part + part_() * (NW + NB), lds);
+  }
+};
+extern "C" __global__ void __launch_bounds__(256) cgtp_norm_row_bwd(const T* __restrict__ x, const T* __restrict__ weight, const T* __restrict__ bias,
+                                                                const T* __restrict__ gy, const T* __restrict__ stats, T* __restrict__ gx,
+                                                                double* __restrict__ part, i64 N) {
+  __shared__ double lds[1024];
+  with_sub_(sub_(), RowBwd{x, weight, bias, gy, stats, gx, part, N, SUB[sub_()].phase, lds});
+}
+)HIP";
+
+// Samples of any number of rows.  The rows are cut into chunks of R; a workgroup has a sub-unit of a chunk.  A sample of at most R rows belongs to the chunk of its
+// first row: its sums are formed and its results written by one workgroup, from registers if it fits one step.  Longer samples take three kernels: sums of
+// each chunk's share (a chunk has at most two: one that goes on, slot 0, one that begins, slot 1), their total (place: the chunk of the sample's first row),
+// and the results.  The first two are launched only if N > R.  Sums over rows are held in 64 bits; fp64 ones are of the distance from the group's first
+// number of the sample, for their variance.
+const char kGraphs[] = R"HIP(
+__device__ inline i64 inside_(i64 p, i64 N) { return p < 0 ? 0 : p > N ? N : p; }
+
+// number of i < S with ptr[i] < row (ptr not decreasing), by all 64 lanes of every wave: 64 probes a step
+__device__ inline i64 first_from_(const i64* __restrict__ ptr, i64 S, i64 N, i64 row) {
+  const int lane = threadIdx.x & 63;
+  i64 lo = 0, hi = S;     // the answer is in [lo, hi]
+  while (lo < hi) {
+    const i64 step = (hi - lo + 63) / 64, at = lo + lane * step;
+    const bool less = at < hi && inside_(ptr[at], N) < row;
+    const int c = __popcll(__ballot(less));     // probes 0 .. c - 1 are below
+    if (c == 0) return lo;
+    const i64 l = lo + (i64)(c - 1) * step + 1, h = lo + (i64)c * step;
+    hi = h < hi ? h : hi;
+    lo = l;
+  }
+  return lo;
+}
+
+// the samples of a chunk: f(sample, first row, end, from, to, slot): the whole of a short one, or a long one's rows in this chunk
+template <class F> __device__ inline void each_piece_(const i64* __restrict__ ptr, i64 S, i64 N, i64 R, i64 chunk, F f) {
+  const i64 a = chunk * R, b = a + R < N ? a + R : N;
+  const bool last = a + R >= N;
+  i64 s = first_from_(ptr, S, N, a);
+  if (s > 0) {
+    const i64 r0 = inside_(ptr[s - 1], N), r1 = inside_(ptr[s], N);
+    if (r1 > a && r1 - r0 > R) f(s - 1, r0, r1, a, r1 < b ? r1 : b, 0);
+  }
+  for (; s < S; ++s) {
+    const i64 r0 = inside_(ptr[s], N);
+    if (r0 < a || (r0 >= b && !(last && r0 == N))) break;
+    const i64 e = inside_(ptr[s + 1], N), r1 = e < r0 ? r0 : e;
+    const bool is_long = r1 - r0 > R;
+    f(s, r0, r1, r0, is_long ? b : r1, is_long ? 1 : -1);
+  }
+}
+
+// sums of the lanes, rows and waves for each group of the step: four numbers
+template <class A> __device__ inline void group_sums_(const A& a, double (&t)[4], double* lds) {
+  constexpr int rows = A::even ? 1 : A::RP;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) t[i] = A::rows_sum(lanes_sum_<A::L>(t[i]));
+  __syncthreads();
+  if (a.on && a.li == 0 && a.rho < rows)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) lds[(((threadIdx.x / 64) * rows + a.rho) * A::GP + a.gq) * 4 + i] = t[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    t[i] = 0;
+    for (int k = 0; k < 4 * rows; ++k) t[i] += lds[(k * A::GP + a.gq) * 4 + i];
+  }
+}
+
+// what the moments are taken about: fp64: the group's first numbers of the sample; fp32: zero, a square has 48 of the 53 bits that its sum is held in
+template <int s> struct Shift { double x, g; };
+template <int s> __device__ inline Shift<s> shift_(const Lane<s>& a, const T* __restrict__ x, i64 r0, i64 rows) {
+  Shift<s> h = {0, 0};
+  if (sizeof(T) == 8 && rows > 0) {
+    if (Lane<s>::inv) h.x = x[r0 * DX + SEG[s].col + a.g * Lane<s>::cg];
+    if (Lane<s>::gated) h.g = x[r0 * DX + SEG[s].gate + a.g * Lane<s>::cg];
+  }
+  return h;
+}
+template <int s> __device__ inline void moments_(const Lane<s>& a, const T* v, const T* g, const Shift<s>& h, bool in, double (&t)[4]) {
+  typedef Lane<s> A;
+#pragma unroll
+  for (int c = 0; c < A::C; ++c) {
+    if (!A::full && !a.has(c / A::V)) continue;
+#pragma unroll
+    for (int m = 0; m < A::n; ++m) {
+      const double d = in ? (double)v[c * A::n + m] - h.x : 0.0;
+      if (A::inv) t[0] += d;
+      t[1] = __builtin_fma(d, d, t[1]);
+    }
+    if constexpr (A::gated) {
+      const double d = in ? (double)g[c] - h.g : 0.0;
+      t[2] += d;
+      t[3] = __builtin_fma(d, d, t[3]);
+    }
+  }
+}
+template <int s> __device__ inline Stat stat_of_(const double (&t)[4], const Shift<s>& h, i64 rows) {
+  typedef Lane<s> A;
+  const double m = rows > 0 ? (double)rows * A::cg : 1.0, M = m * A::n;
+  const double d = t[0] / M, var = t[1] / M - d * d;
+  Stat S = {A::inv ? (T)(rows > 0 ? h.x + d : 0.0) : T(0), (T)(1.0 / sqrt((var > 0 || var != var ? var : 0.0) + EPS)), T(0), T(0)};
+  if constexpr (A::gated) {
+    const double e = t[2] / m, gvar = t[3] / m - e * e;
+    S.gmu = (T)(rows > 0 ? h.g + e : 0.0);
+    S.gr = (T)(1.0 / sqrt((gvar > 0 || gvar != gvar ? gvar : 0.0) + EPS));
+  }
+  return S;
+}
+
+// sums of the shares of long samples: part[chunk][slot][segment][group][4]
+struct PartFwd {
+  const T* __restrict__ x; double* __restrict__ part; const i64* __restrict__ ptr; i64 N, S, R, chunk; int phase; double* lds;
+  template <int s> __device__ void operator()() const {
+    typedef Lane<s> A;
+    const A a(phase);
+    each_piece_(ptr, S, N, R, chunk, [&](i64, i64 r0, i64 r1, i64 from, i64 to, int slot) {
+      if (slot < 0) return;
+      const Shift<s> h = shift_<s>(a, x, r0, r1 - r0);
+      double t[4] = {};
+      for (i64 base = from + (threadIdx.x / 64) * A::RP; base < to; base += 4 * A::RP) {
+        const bool in = a.on && base + a.rho < to;
+        const i64 r = base + a.rho < to ? base + a.rho : to - 1;
+        T v[A::C * A::n], g[A::C];
+        a.read(x + r * DX + SEG[s].col, v);
+        a.read_gates(x + r * DX, g);
+        moments_<s>(a, v, g, h, in, t);
+      }
+      group_sums_(a, t, lds);
+      if (threadIdx.x < 64 && a.on && a.rho == 0 && a.li == 0)
+        for (int i = 0; i < 4; ++i) part[(((chunk * 2 + slot) * NS + s) * G + a.g) * 4 + i] = t[i];
+    });
+  }
+};
+extern "C" __global__ void __launch_bounds__(256) cgtp_norm_part_fwd(const T* __restrict__ x, double* __restrict__ part, const i64* __restrict__ ptr, i64 N, i64 S, i64 R) {
+  __shared__ double lds[1024];
+  with_sub_(sub_(), PartFwd{x, part, ptr, N, S, R, part_(), SUB[sub_()].phase, lds});
+}
+
+// the long sample that begins in a chunk: f(sample, first row, end)
+template <class F> __device__ inline void long_sample_(const i64* __restrict__ ptr, i64 S, i64 N, i64 R, i64 chunk, F f) {
+  each_piece_(ptr, S, N, R, chunk, [&](i64 s, i64 r0, i64 r1, i64, i64, int slot) {
+    if (slot == 1) f(s, r0, r1);
+  });
+}
+// total of a unit's shares, by 16 neighbouring lanes
+__device__ inline void total_(const double* __restrict__ part, i64 R, i64 chunk, i64 r1, int unit, double (&t)[4]) {
+  const i64 end = (r1 - 1) / R;
+  for (int i = 0; i < 4; ++i) t[i] = 0;
+  for (i64 c = chunk + threadIdx.x % 16; c <= end; c += 16)
+    for (int i = 0; i < 4; ++i) t[i] += part[((c * 2 + (c == chunk)) * NS * G + unit) * 4 + i];
+  for (int i = 0; i < 4; ++i) t[i] = lanes_sum_<16>(t[i]);
+}
+struct MeanFwd {
+  const T* __restrict__ x; const double* t; T* __restrict__ total; T* __restrict__ stats; i64 r0, r1, sample, chunk; int g;
+  template <int s> __device__ void operator()() const {
+    Lane<s> a(0);
+    a.g = g;
+    const double v[4] = {t[0], t[1], t[2], t[3]};
+    const Stat S = stat_of_<s>(v, shift_<s>(a, x, r0, r1 - r0), r1 - r0);
+    T* to = total + ((chunk * NS + s) * G + g) * 4;
+    to[0] = S.mu; to[1] = S.r; to[2] = S.gmu; to[3] = S.gr;
+    if (stats) a.put_stat(stats + sample * NST, S);
+  }
+};
+extern "C" __global__ void __launch_bounds__(256) cgtp_norm_mean_fwd(const T* __restrict__ x, const double* __restrict__ part, T* __restrict__ total, T* __restrict__ stats,
+                                                                 const i64* __restrict__ ptr, i64 N, i64 S, i64 R) {
+  const i64 chunk = blockIdx.x;
+  long_sample_(ptr, S, N, R, chunk, [&](i64 sample, i64 r0, i64 r1) {
+    for (int u0 = 0; u0 < NS * G; u0 += 16) {
+      const int u = u0 + threadIdx.x / 16 < NS * G ? u0 + threadIdx.x / 16 : NS * G - 1;
+      double t[4];
+      total_(part, R, chunk, r1, u, t);
+      if (threadIdx.x % 16 == 0) with_segment_<0>(u / G, MeanFwd{x, t, total, stats, r0, r1, sample, chunk, u % G});
+    }
+  });
+}
+
+struct GraphFwd {
+  const T* __restrict__ x; const T* __restrict__ weight; const T* __restrict__ bias; T* __restrict__ y; T* __restrict__ stats; const T* __restrict__ total;
+  const i64* __restrict__ ptr; i64 N, S, R, chunk; int phase; double* lds;
+  template <int s> __device__ void operator()() const {
+    typedef Lane<s> A;
+    const A a(phase);
+    Param p[A::C];
+    a.params(weight, bias, p);
+    each_piece_(ptr, S, N, R, chunk, [&](i64 sample, i64 r0, i64 r1, i64 from, i64 to, int slot) {
+      const i64 first = from + (threadIdx.x / 64) * A::RP;
+      i64 base = first;
+      T v[A::C * A::n], g[A::C];
+      Stat st;
+      auto fetch = [&] {
+        const i64 r = base + a.rho < to ? base + a.rho : to - 1;
+        a.read(x + r * DX + SEG[s].col, v);
+        a.read_gates(x + r * DX, g);
+      };
+      bool held = false;      // the last step's rows are in v, g
+      if (slot < 0) {
+        const Shift<s> h = shift_<s>(a, x, r0, r1 - r0);
+        double t[4] = {};
+        for (; base < to; base += 4 * A::RP) {
+          fetch();
+          moments_<s>(a, v, g, h, a.on && base + a.rho < to, t);
+        }
+        group_sums_(a, t, lds);
+        st = stat_of_<s>(t, h, r1 - r0);
+        if (stats && threadIdx.x < 64 && a.on && a.rho == 0 && a.li == 0) a.put_stat(stats + sample * NST, st);
+        base -= 4 * A::RP;
+        held = true;
+      } else {
+        const T* tt = total + ((r0 / R * NS + s) * G + a.g) * 4;
+        st = Stat{tt[0], tt[1], tt[2], tt[3]};
+        if (base < to) base += (to - 1 - base) / (4 * A::RP) * (4 * A::RP);
+        else base -= 4 * A::RP;
+      }
+      for (; base >= first; base -= 4 * A::RP) {
+        if (!held) fetch();
+        held = false;
+        a.forward(v, g, st, p);
+        if (a.on && base + a.rho < to) a.write(y + (base + a.rho) * DY + SEG[s].ycol, v);
+      }
+    });
+  }
+};
+extern "C" __global__ void __launch_bounds__(256) cgtp_norm_graph_fwd(const T* __restrict__ x, const T* __restrict__ weight, const T* __restrict__ bias,
+                                                                  T* __restrict__ y, T* __restrict__ stats, const T* __restrict__ total,
+                                                                  const i64* __restrict__ ptr, i64 N, i64 S, i64 R) {
+  __shared__ double lds[1024];
+  with_sub_(sub_(), GraphFwd{x, weight, bias, y, stats, total, ptr, N, S, R, part_(), SUB[sub_()].phase, lds});
+}
+
+template <int s> struct BwdRow {
+  typedef Lane<s> A;
+  T v[A::C * A::n], q[A::C * A::n], g[A::C], qg[A::C];
+  __device__ void fetch(const A& a, const T* __restrict__ x, const T* __restrict__ gy, i64 r) {
+    a.read(x + r * DX + SEG[s].col, v);
+    a.read(gy + r * DY + SEG[s].ycol, q);
+    a.read_gates(x + r * DX, g);
+  }
+};
+__device__ inline void add_(double (&t)[4], const Sums& o) {
+  t[0] += o.h;
+  t[1] += o.hx;
+  t[2] += o.gh;
+  t[3] += o.ghx;
+}
+template <int s> __device__ inline Means means_of_(const double (&t)[4], i64 rows) {
+  const double m = rows > 0 ? (double)rows * Lane<s>::cg : 1.0;
+  return Means{(T)(t[0] / m), (T)(t[1] / (m * Lane<s>::n)), (T)(t[2] / m), (T)(t[3] / m)};
+}
+
+struct PartBwd {
+  const T* __restrict__ x; const T* __restrict__ weight; const T* __restrict__ bias; const T* __restrict__ gy; const T* __restrict__ stats; double* __restrict__ part;
+  const i64* __restrict__ ptr; i64 N, S, R, chunk; int phase; double* lds;
+  template <int s> __device__ void operator()() const {
+    typedef Lane<s> A;
+    const A a(phase);
+    Param p[A::C];
+    a.params(weight, bias, p);
+    each_piece_(ptr, S, N, R, chunk, [&](i64 sample, i64, i64, i64 from, i64 to, int slot) {
+      if (slot < 0) return;
+      const Stat st = a.stat(stats + sample * NST);
+      double t[4] = {};
+      for (i64 base = from + (threadIdx.x / 64) * A::RP; base < to; base += 4 * A::RP) {
+        const bool in = a.on && base + a.rho < to;
+        BwdRow<s> w;
+        w.fetch(a, x, gy, base + a.rho < to ? base + a.rho : to - 1);
+        add_(t, a.backward(w.v, w.g, w.q, w.qg, st, p, in, nullptr));
+      }
+      group_sums_(a, t, lds);
+      if (threadIdx.x < 64 && a.on && a.rho == 0 && a.li == 0)
+        for (int i = 0; i < 4; ++i) part[(((chunk * 2 + slot) * NS + s) * G + a.g) * 4 + i] = t[i];
+    });
+  }
+};
+extern "C" __global__ void __launch_bounds__(256) cgtp_norm_part_bwd(const T* __restrict__ x, const T* __restrict__ weight, const T* __restrict__ bias,
+                                                                 const T* __restrict__ gy, const T* __restrict__ stats, double* __restrict__ part,
+                                                                 const i64* __restrict__ ptr, i64 N, i64 S, i64 R) {
+  __shared__ double lds[1024];
+  with_sub_(sub_(), PartBwd{x, weight, bias, gy, stats, part, ptr, N, S, R, part_(), SUB[sub_()].phase, lds});
+}
+struct MeanBwd {
+  const double* t; T* __restrict__ total; i64 rows, chunk; int g;
+  template <int s> __device__ void operator()() const {
+    const double v[4] = {t[0], t[1], t[2], t[3]};
+    const Means e = means_of_<s>(v, rows);
+    T* to = total + ((chunk * NS + s) * G + g) * 4;
+    to[0] = e.h; to[1] = e.hx; to[2] = e.gh; to[3] = e.ghx;
+  }
+};
+extern "C" __global__ void __launch_bounds__(256) cgtp_norm_mean_bwd(const double* __restrict__ part, T* __restrict__ total, const i64* __restrict__ ptr, i64 N, i64 S, i64 R) {
+  const i64 chunk = blockIdx.x;
+  long_sample_(ptr, S, N, R, chunk, [&](i64, i64 r0, i64 r1) {
+    for (int u0 = 0; u0 < NS * G; u0 += 16) {
+      const int u = u0 + threadIdx.x / 16 < NS * G ? u0 + threadIdx.x / 16 : NS * G - 1;
+      double t[4];
+      total_(part, R, chunk, r1, u, t);
+      if (threadIdx.x % 16 == 0) with_segment_<0>(u / G, MeanBwd{t, total, r1 - r0, chunk, u % G});
+    }
+  });
+}
+struct GraphBwd {
+  const T* __restrict__ x; const T* __restrict__ weight; const T* __restrict__ bias; const T* __restrict__ gy; const T* __restrict__ stats; T* __restrict__ gx;
+  double* __restrict__ sums; const T* __restrict__ total; const i64* __restrict__ ptr; i64 N, S, R, chunk; int phase; double* lds;
+  template <int s> __device__ void operator()() const {
+    typedef Lane<s> A;
+    const A a(phase);
+    Param p[A::C];
+    a.params(weight, bias, p);
+    typename A::Sum sum = {};
+    each_piece_(ptr, S, N, R, chunk, [&](i64 sample, i64 r0, i64 r1, i64 from, i64 to, int slot) {
+      const i64 first = from + (threadIdx.x / 64) * A::RP;
+      i64 base = first;
+      const Stat st = a.stat(stats + sample * NST);
+      BwdRow<s> w;
+      Means e;
+      auto products = [&](typename A::Sum* add) {
+        w.fetch(a, x, gy, base + a.rho < to ? base + a.rho : to - 1);
+        return a.backward(w.v, w.g, w.q, w.qg, st, p, a.on && base + a.rho < to, add);
+      };
+      bool held = false, count = true;      // the channels' sums are still to be added to
+      if (slot < 0) {
+        double t[4] = {};
+        for (; base < to; base += 4 * A::RP) add_(t, products(&sum));
+        group_sums_(a, t, lds);
+        e = means_of_<s>(t, r1 - r0);
+        base -= 4 * A::RP;
+        held = true;
+        count = false;
+      } else {
+        const T* tt = total + ((r0 / R * NS + s) * G + a.g) * 4;
+        e = Means{tt[0], tt[1], tt[2], tt[3]};
+        if (base < to) base += (to - 1 - base) / (4 * A::RP) * (4 * A::RP);
+        else base -= 4 * A::RP;
+      }
+      for (; base >= first; base -= 4 * A::RP) {
+        if (!held) products(count ? &sum : nullptr);
+        held = false;
+        a.finish(w.v, w.g, w.q, w.qg, st, e);
+        if (a.on && base + a.rho < to) {
+          a.write(gx + (base + a.rho) * DX + SEG[s].col, w.q);
+          a.write_gates(gx + (base + a.rho) * DX, w.qg);
+        }
+      }
+    });
+    a.put_sums(sum, sums + chunk * (NW + NB), lds);
+  }
+};
+extern "C" __global__ void __launch_bounds__(256) cgtp_norm_graph_bwd(const T* __restrict__ x, const T* __restrict__ weight, const T* __restrict__ bias,
+                                                                  const T* __restrict__ gy, const T* __restrict__ stats, T* __restrict__ gx,
+                                                                  double* __restrict__ sums, const T* __restrict__ total, const i64* __restrict__ ptr, i64 N, i64 S, i64 R) {
+  __shared__ double lds[1024];
+  with_sub_(sub_(), GraphBwd{x, weight, bias, gy, stats, gx, sums, total, ptr, N, S, R, part_(), SUB[sub_()].phase, lds});
+}
+)HIP";
+
+// Groups too large for the registers of a wave (more than 64 words a lane, fp64 32): one workgroup for each unit of a sample, whatever its
+// length; the rows are read once for each of mean, variance and result.
+const char kUnits[] = R"HIP(
 struct UnitFwd {
   const T* __restrict__ x; const T* __restrict__ weight; const T* __restrict__ bias; T* __restrict__ y; T* __restrict__ stats;
   i64 r0, r1, sample; int g; double* lds;
@@ -219,7 +877,7 @@ struct UnitFwd {
       }
   }
 };
-extern "C" __global__ void __launch_bounds__(256) cgtp_norm_fwd(const T* __restrict__ x, const T* __restrict__ weight, const T* __restrict__ bias,
+extern "C" __global__ void __launch_bounds__(256) cgtp_norm_unit_fwd(const T* __restrict__ x, const T* __restrict__ weight, const T* __restrict__ bias,
                                                             T* __restrict__ y, T* __restrict__ stats, i64 N, i64 S, const i64* __restrict__ ptr) {
   __shared__ double lds[4];
   for (i64 u = blockIdx.x; u < S * NS * G; u += gridDim.x) {
@@ -230,9 +888,7 @@ extern "C" __global__ void __launch_bounds__(256) cgtp_norm_fwd(const T* __restr
     with_segment_<0>(unit / G, UnitFwd{x, weight, bias, y, stats, r0, r1, sample, unit % G, lds});
   }
 }
-)HIP";
 
-const char kBackward[] = R"HIP(
 struct UnitBwd {
   const T* __restrict__ x; const T* __restrict__ weight; const T* __restrict__ bias; const T* __restrict__ gy; const T* __restrict__ stats;
   T* __restrict__ gx; double* __restrict__ part; i64 r0, r1, sample; int g; double* lds; double* cols;
@@ -307,7 +963,7 @@ struct UnitBwd {
       }
   }
 };
-extern "C" __global__ void __launch_bounds__(256) cgtp_norm_bwd(const T* __restrict__ x, const T* __restrict__ weight, const T* __restrict__ bias,
+extern "C" __global__ void __launch_bounds__(256) cgtp_norm_unit_bwd(const T* __restrict__ x, const T* __restrict__ weight, const T* __restrict__ bias,
                                                             const T* __restrict__ gy, const T* __restrict__ stats, T* __restrict__ gx,
                                                             double* __restrict__ part, i64 N, i64 S, const i64* __restrict__ ptr) {
   __shared__ double lds[4], cols[256];
@@ -340,28 +996,63 @@ extern "C" __global__ void __launch_bounds__(256) cgtp_norm_sums(const double* _
 
 }  // namespace
 
-void emit_norm(const Norm& N, Kernel& fwd, Kernel& bwd, Kernel& sums) {
+void emit_norm(Norm& N) {
+  const bool f64 = N.dtype == CGTP_F64;
+  const int most = f64 ? 32 : 64;          // words a lane holds of a row
+  N.covered = true;
+  struct Sub {
+    int s, phase, size;
+  };
+  std::vector<Sub> subs;
+  for (size_t i = 0; i < N.seg.size(); ++i) {
+    NormSeg& s = N.seg[i];
+    const int cg = s.mul / N.groups;
+    // V channels in one piece: everything that is added to a row's start is a multiple of V words
+    auto fits = [&](int V) {
+      const bool cols = s.col % V == 0 && s.ycol % V == 0 && N.dim_x % V == 0 && N.dim_y % V == 0 && (s.gate < 0 || s.gate % V == 0);
+      return cols && cg % V == 0 && V * s.n <= most / 2;
+    };
+    s.V = fits(4) ? 4 : fits(2) ? 2 : 1;
+    s.vec = s.V > 1;
+    s.lanes = 1;
+    while (s.lanes < 64 && s.lanes * s.V < cg) s.lanes *= 2;
+    s.J = (cg + s.lanes * s.V - 1) / (s.lanes * s.V);
+    s.at_once = 1;
+    for (int g = 1; g <= N.groups; ++g)
+      if (N.groups % g == 0 && g * s.lanes <= 64) s.at_once = g;
+    s.rows = 64 / (s.at_once * s.lanes);
+    s.phases = N.groups / s.at_once;
+    if (s.V * s.J * s.n > most || s.phases > 256) N.covered = false;
+    for (int p = 0; N.covered && p < s.phases; ++p) subs.push_back({(int)i, p, s.at_once * cg * (s.n + (s.gate >= 0))});
+  }
+  std::stable_sort(subs.begin(), subs.end(), [](const Sub& a, const Sub& b) { return a.size > b.size; });
+  N.subs = (int)subs.size();
   std::ostringstream o;
   o.precision(17);
-  o << "// group normalisation of irreps rows\ntypedef " << (N.dtype == CGTP_F64 ? "double" : "float") << " T;\n"
-    << "struct Seg { int mul, n, col, ycol; bool inv; int gate, w, b, gw, gb, st, gst; };\n"
+  o << "// group normalisation of irreps rows\ntypedef " << (f64 ? "double" : "float") << " T;\n"
+    << "struct Seg { int mul, n, col, ycol; bool inv; int gate, w, b, gw, gb, st, gst, V, J, lanes, at_once, rows; bool vec; };\n"
     << "constexpr int NS = " << N.seg.size() << ", G = " << N.groups << ", ACT = " << N.act << ", DX = " << N.dim_x << ", DY = " << N.dim_y
-    << ", NW = " << N.n_w << ", NB = " << N.n_b << ", NST = " << N.n_stat << ";\n"
+    << ", NW = " << N.n_w << ", NB = " << N.n_b << ", NST = " << N.n_stat << ", NSUB = " << subs.size() << ";\n"
     << "constexpr bool IR_MUL = " << (N.ir_mul ? "true" : "false") << ";\nconstexpr double EPS = " << N.eps << ";\n"
     << "constexpr Seg SEG[NS] = {\n";
   for (const NormSeg& s : N.seg)
     o << "  {" << s.mul << ", " << s.n << ", " << s.col << ", " << s.ycol << ", " << (s.inv ? "true" : "false") << ", " << s.gate << ", " << s.w
-      << ", " << s.b << ", " << s.gw << ", " << s.gb << ", " << s.st << ", " << s.gst << "},\n";
-  o << "};\n" << kShared;
-  const std::string head = o.str();
-  auto make = [&](Kernel& k, const char* name, const char* text) {
-    k.name = name;
-    k.wg = 256;
-    k.source = head + text;
-  };
-  make(fwd, "cgtp_norm_fwd", kForward);
-  make(bwd, "cgtp_norm_bwd", kBackward);
-  make(sums, "cgtp_norm_sums", kSums);
+      << ", " << s.b << ", " << s.gw << ", " << s.gb << ", " << s.st << ", " << s.gst << ", " << s.V << ", " << s.J << ", " << s.lanes << ", " << s.at_once
+      << ", " << s.rows << ", " << (s.vec ? "true" : "false") << "},\n";
+  o << "};\n";
+  if (N.covered) {
+    o << "struct Sub { int s, phase; };\n__constant__ constexpr Sub SUB[NSUB] = {";
+    for (const Sub& s : subs) o << "{" << s.s << ", " << s.phase << "}, ";
+    o << "};\n";
+  }
+  o << kShared;
+  if (N.covered) o << kLanes << kRowsText << kGraphs;
+  else o << kUnits;
+  o << kSums;
+  N.code = Kernel();
+  N.code.name = "cgtp_norm_sums";
+  N.code.wg = 256;
+  N.code.source = o.str();
 }
 
 }  // namespace cgtp

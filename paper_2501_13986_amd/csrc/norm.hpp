@@ -12,6 +12,10 @@ struct NormSeg {
   int gate;          // first column of its gates, -1: none
   int w, b, gw, gb;  // first weight and bias (b: 0e segments), of the gates as well
   int st, gst;       // its place among the segments of stats, of its gates
+  // how a wave goes over it: V neighbouring channels a lane, J times, `lanes` lanes a group, `at_once` groups and `rows` rows a step,
+  // in phases of groups / at_once; V channels are read and written in one piece where `vec`.  V = 0: not by these kernels
+  int V, J, lanes, at_once, rows, phases;
+  bool vec;
 };
 
 struct Norm {
@@ -20,10 +24,15 @@ struct Norm {
   bool ir_mul = false;
   double eps = 0;
   int64_t dim_x = 0, dim_y = 0, n_w = 0, n_b = 0, n_stat = 0;   // n_stat: numbers per sample
-  Kernel fwd, bwd, sums;
+  int subs = 0;        // segments times their phases
+  bool covered = false;
+  Kernel code;         // holds the module; the functions in it:
+  hipFunction_t row_fwd = nullptr, row_bwd = nullptr, part_fwd = nullptr, mean_fwd = nullptr, graph_fwd = nullptr, part_bwd = nullptr, mean_bwd = nullptr,
+                graph_bwd = nullptr, sums = nullptr, unit_fwd = nullptr, unit_bwd = nullptr;
   size_t elt() const { return dtype == CGTP_F64 ? 8 : 4; }
 };
 
-void emit_norm(const Norm& N, Kernel& fwd, Kernel& bwd, Kernel& sums);
+// Fills in how the segments are gone over, and the source.
+void emit_norm(Norm& N);
 
 }  // namespace cgtp
