@@ -63,13 +63,13 @@ cgtp_status check_gated(const cgtp::GatedArgs& a, int32_t dtype) {
   return CGTP_OK;
 }
 
-// How a call of the normalisation is cut up, and its workspace: shares and totals of long samples, partial sums of the parameters' gradients.
+// How a call of the normalisation is cut up, and its workspace: the shares of long samples, partial sums of the parameters' gradients.
 struct NormWork {
-  int64_t R = 0;            // rows of a chunk
+  int64_t R = 128, D = 0;   // rows of a short sample at most, of a chunk
   int64_t blocks = 1;       // workgroups (of each sub-unit)
-  int64_t sum_rows = 1;     // partial sums
+  int64_t sum_rows = 1;     // partial sums of the parameters' gradients (one: written where they belong at once)
   bool longer = false;      // samples of more than R rows are possible
-  size_t part = 0, total = 0, bytes = 0;
+  size_t part = 0, bytes = 0;
   NormWork(const cgtp::Norm& P, int64_t N, int64_t S, bool ptr, bool backward) {
     auto up = [](size_t v) { return (v + 255) / 256 * 256; };
     const size_t units = P.seg.size() * (size_t)P.groups;
@@ -78,25 +78,24 @@ struct NormWork {
       blocks = std::min<int64_t>(S * (int64_t)units, 1 << 20);
       sum_rows = S;
     } else if (!ptr) {
-      // Forward: a wave takes a few steps of rows; backward, where each workgroup leaves sums: as many workgroups as stay on the chip
+      // Forward: a wave takes a step of rows; backward, where each workgroup leaves sums: as many workgroups as stay on the chip
       int rows = 1;
       for (const cgtp::NormSeg& s : P.seg) rows = std::max(rows, s.rows);
       const int64_t steps = (N + 4 * rows - 1) / (4 * rows);
-      blocks = std::max<int64_t>(1, backward ? std::min<int64_t>(steps, std::max(1, 2048 / P.subs)) : std::min<int64_t>(steps, std::max<int64_t>(1, most / P.subs)));
+      blocks = std::max<int64_t>(1, std::min<int64_t>(steps, std::max<int64_t>(1, (backward ? 2048 : most) / P.subs)));
       sum_rows = blocks;
     } else {
-      R = 64;
-      while (R < 256 && N > R * 512) R *= 2;
-      while ((N + R - 1) / R > most / P.subs) R *= 2;
-      blocks = std::max<int64_t>(1, (N + R - 1) / R);
-      sum_rows = blocks;
+      // Chunks of 16 rows leave many workgroups where samples are short; with long ones, whose shares each workgroup adds up, 128
+      D = 16;
+      while (D < 128 && (N / D * P.subs > 8192 || N / D > 4 * S)) D *= 2;
+      while ((N + D - 1) / D > most / P.subs) D *= 2;
+      R = std::max(R, D);
+      blocks = std::max<int64_t>(1, (N + D - 1) / D);
       longer = N > R;
-      if (longer) {
-        part = up((size_t)blocks * 2 * units * 4 * sizeof(double));
-        total = up((size_t)blocks * units * 4 * P.elt());
-      }
+      sum_rows = longer ? 2 * blocks : blocks;
+      if (longer) part = up((size_t)blocks * 2 * units * 4 * sizeof(double));
     }
-    bytes = part + total + (backward ? up((size_t)sum_rows * (size_t)(P.n_w + P.n_b) * sizeof(double)) : 0);
+    bytes = part + (backward && (sum_rows > 1 || !P.covered) ? up((size_t)sum_rows * (size_t)(P.n_w + P.n_b) * sizeof(double)) : 0);
   }
 };
 
@@ -108,8 +107,8 @@ struct Function {
 // the functions of a normalisation's module
 std::vector<Function> functions(cgtp::Norm& N) {
   if (!N.covered) return {{&N.unit_fwd, "cgtp_norm_unit_fwd"}, {&N.unit_bwd, "cgtp_norm_unit_bwd"}, {&N.sums, "cgtp_norm_sums"}};
-  return {{&N.row_fwd, "cgtp_norm_row_fwd"},   {&N.row_bwd, "cgtp_norm_row_bwd"},     {&N.part_fwd, "cgtp_norm_part_fwd"}, {&N.mean_fwd, "cgtp_norm_mean_fwd"},
-          {&N.graph_fwd, "cgtp_norm_graph_fwd"}, {&N.part_bwd, "cgtp_norm_part_bwd"}, {&N.mean_bwd, "cgtp_norm_mean_bwd"}, {&N.graph_bwd, "cgtp_norm_graph_bwd"},
+  return {{&N.row_fwd, "cgtp_norm_row_fwd"},     {&N.row_bwd, "cgtp_norm_row_bwd"},     {&N.graph_fwd, "cgtp_norm_graph_fwd"},
+          {&N.long_fwd, "cgtp_norm_long_fwd"},   {&N.graph_bwd, "cgtp_norm_graph_bwd"}, {&N.long_bwd, "cgtp_norm_long_bwd"},
           {&N.sums, "cgtp_norm_sums"}};
 }
 
@@ -249,6 +248,11 @@ cgtp_status cgtp_norm_create(const char* irreps, int32_t groups, int32_t act, do
         return fail(CGTP_EUNSUPPORTED, std::string("this library targets gfx950, device is ") + prop.gcnArchName);
     }
     try {
+      if (device != -1) cgtp::jit_compile(N.code, -2);
+      if (N.covered && (N.code.scratch > 0 || N.code.agprs > 0)) {   // rows that do not fit the registers after all
+        cgtp::emit_norm(N, false);
+        cgtp::jit_compile(N.code, -2);
+      }
       cgtp::jit_compile(N.code, device);
       if (device >= 0)
         for (const Function& f : functions(N)) {
@@ -308,14 +312,9 @@ cgtp_status check_norm(const cgtp_norm* norm, int64_t N, int64_t S, const int64_
   return CGTP_OK;
 }
 
-cgtp_status launch(hipFunction_t fn, int64_t grid, void** args, hipStream_t st) {
-  HIP_TRY(hipModuleLaunchKernel(fn, (unsigned)grid, 1, 1, 256, 1, 1, 0, st, args, nullptr));
+cgtp_status launch(hipFunction_t fn, int64_t grid, void** args, hipStream_t st, unsigned threads = 256) {
+  HIP_TRY(hipModuleLaunchKernel(fn, (unsigned)grid, 1, 1, threads, 1, 1, 0, st, args, nullptr));
   return CGTP_OK;
-}
-
-cgtp_status launch_sums(const cgtp::Norm& P, const double* sums, int64_t rows, void* gweight, void* gbias, hipStream_t st) {
-  void* args[] = {(void*)&sums, (void*)&rows, (void*)&gweight, (void*)&gbias};
-  return launch(P.sums, (P.n_w + P.n_b + 15) / 16, args, st);
 }
 
 }  // namespace
@@ -332,9 +331,7 @@ cgtp_status norm_forward(const cgtp_norm* norm, const void* x, const void* weigh
   const NormWork w(P, N, S, ptr != nullptr, false);
   if (!workspace_serves(workspace, workspace_bytes, w.bytes)) return bad_workspace("cgtp_norm_workspace_bytes", w.bytes);
   hipStream_t st = (hipStream_t)hip_stream;
-  int64_t R = w.R;
   double* part = (double*)workspace;
-  void* total = (char*)workspace + w.part;
   if (!P.covered) {
     void* args[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&y, (void*)&stats, (void*)&N, (void*)&S, (void*)&ptr};
     return launch(P.unit_fwd, w.blocks, args, st);
@@ -343,14 +340,9 @@ cgtp_status norm_forward(const cgtp_norm* norm, const void* x, const void* weigh
     void* args[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&y, (void*)&stats, (void*)&N};
     return launch(P.row_fwd, w.blocks * P.subs, args, st);
   }
-  if (w.longer) {
-    void* pargs[] = {(void*)&x, (void*)&part, (void*)&ptr, (void*)&N, (void*)&S, (void*)&R};
-    if ((s = launch(P.part_fwd, w.blocks * P.subs, pargs, st)) != CGTP_OK) return s;
-    void* margs[] = {(void*)&x, (void*)&part, (void*)&total, (void*)&stats, (void*)&ptr, (void*)&N, (void*)&S, (void*)&R};
-    if ((s = launch(P.mean_fwd, w.blocks, margs, st)) != CGTP_OK) return s;
-  }
-  void* args[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&y, (void*)&stats, (void*)&total, (void*)&ptr, (void*)&N, (void*)&S, (void*)&R};
-  return launch(P.graph_fwd, w.blocks * P.subs, args, st);
+  void* args[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&y, (void*)&stats, (void*)&part, (void*)&ptr, (void*)&N, (void*)&S, (void*)&w.R, (void*)&w.D};
+  s = launch(P.graph_fwd, w.blocks * P.subs, args, st);
+  return s != CGTP_OK || !w.longer ? s : launch(P.long_fwd, w.blocks * P.subs, args, st);
 }
 
 cgtp_status norm_backward(const cgtp_norm* norm, const void* x, const void* weight, const void* bias, const void* gy,
@@ -369,28 +361,25 @@ cgtp_status norm_backward(const cgtp_norm* norm, const void* x, const void* weig
   if ((N > 0 && (!x || !gy || !gx)) || !weight || (P.n_b && !bias) || !stats) return fail(CGTP_EINVAL, "NULL data pointer");
   const NormWork w(P, N, S, ptr != nullptr, true);
   if (!workspace_serves(workspace, workspace_bytes, w.bytes)) return bad_workspace("cgtp_norm_workspace_bytes", w.bytes);
-  int64_t R = w.R;
   double* part = (double*)workspace;
-  void* total = (char*)workspace + w.part;
-  double* sums = (double*)((char*)workspace + w.part + w.total);
+  double* sums = w.sum_rows > 1 || !P.covered ? (double*)((char*)workspace + w.part) : nullptr;
   if (!P.covered) {
     void* args[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&gy, (void*)&stats, (void*)&gx, (void*)&sums, (void*)&N, (void*)&S, (void*)&ptr};
     s = launch(P.unit_bwd, w.blocks, args, st);
   } else if (!ptr) {
-    void* args[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&gy, (void*)&stats, (void*)&gx, (void*)&sums, (void*)&N};
+    void* args[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&gy, (void*)&stats, (void*)&gx, (void*)&sums, (void*)&gweight, (void*)&gbias, (void*)&N};
     s = launch(P.row_bwd, w.blocks * P.subs, args, st);
   } else {
-    if (w.longer) {
-      void* pargs[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&gy, (void*)&stats, (void*)&part, (void*)&ptr, (void*)&N, (void*)&S, (void*)&R};
-      if ((s = launch(P.part_bwd, w.blocks * P.subs, pargs, st)) != CGTP_OK) return s;
-      void* margs[] = {(void*)&part, (void*)&total, (void*)&ptr, (void*)&N, (void*)&S, (void*)&R};
-      if ((s = launch(P.mean_bwd, w.blocks, margs, st)) != CGTP_OK) return s;
-    }
-    void* args[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&gy, (void*)&stats, (void*)&gx, (void*)&sums, (void*)&total, (void*)&ptr, (void*)&N, (void*)&S, (void*)&R};
+    double* more = sums ? sums + w.blocks * (P.n_w + P.n_b) : nullptr;
+    void* args[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&gy, (void*)&stats, (void*)&gx, (void*)&part, (void*)&sums, (void*)&gweight, (void*)&gbias,
+                    (void*)&ptr, (void*)&N, (void*)&S, (void*)&w.R, (void*)&w.D};
     s = launch(P.graph_bwd, w.blocks * P.subs, args, st);
+    args[7] = (void*)&more;
+    if (s == CGTP_OK && w.longer) s = launch(P.long_bwd, w.blocks * P.subs, args, st);
   }
-  if (s != CGTP_OK) return s;
-  return launch_sums(P, sums, w.sum_rows, gweight, gbias, st);
+  if (s != CGTP_OK || !sums) return s;
+  void* args[] = {(void*)&sums, (void*)&w.sum_rows, (void*)&gweight, (void*)&gbias};
+  return launch(P.sums, (P.n_w + P.n_b + 15) / 16, args, st, 1024);
 }
 
 }  // extern "C"

@@ -307,7 +307,7 @@ template <int s> struct Lane {
   }
   // v, g_: of x, then xh; q: of gy, then h; qg: h of the gates.  Adds to the sums of the channels (a) and of the group (o)
   struct Sum { double w[C], b[C], gw[C], gb[C]; };
-  __device__ Sums backward(T* v, T* g_, T* q, T* qg, const Stat& S, const Param* p, bool in, Sum* a) const {
+  __device__ Sums backward(T* v, T* g_, T* q, T* qg, const Stat& S, const Param* p, bool in, bool add, Sum& a) const {
     Sums o = {};
 #pragma unroll
     for (int c = 0; c < C; ++c) {
@@ -318,12 +318,12 @@ template <int s> struct Lane {
       o.hx += count ? t.hx : T(0);
       o.gh += count ? t.gh : T(0);
       o.ghx += count ? t.ghx : T(0);
-      if (a) {
-        a->w[c] += count ? (double)t.w : 0.0;
-        if (inv) a->b[c] += count ? (double)t.b : 0.0;
+      if (add) {
+        a.w[c] += count ? (double)t.w : 0.0;
+        if (inv) a.b[c] += count ? (double)t.b : 0.0;
         if (gated) {
-          a->gw[c] += count ? (double)t.gw : 0.0;
-          a->gb[c] += count ? (double)t.gb : 0.0;
+          a.gw[c] += count ? (double)t.gw : 0.0;
+          a.gb[c] += count ? (double)t.gb : 0.0;
         }
       }
     }
@@ -344,8 +344,9 @@ template <int s> struct Lane {
       for (int o = GP * L; o < 64; o *= 2) v += __shfl_xor(v, o);
     return v;
   }
-  // the workgroup's sums of the channels' gradients: to + place of the weight or bias.  Four at a time, one for each wave to add up
-  __device__ void put_sums(const Sum& a, double* to, double* lds) const {
+  // the workgroup's sums of the channels' gradients, four at a time, one for each wave to add up: into a row of partial sums, or, of the only
+  // workgroup of its channels, into gweight and gbias
+  __device__ void put_sums(const Sum& a, double* to, T* gweight, T* gbias, double* lds) const {
     constexpr int kinds = 1 + (inv ? 1 : 0) + (gated ? 2 : 0);
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
 #pragma unroll
@@ -364,8 +365,10 @@ template <int s> struct Lane {
         double t = 0;
         for (int w = 0; w < 4; ++w)
           for (int r = 0; r < (even ? 1 : RP); ++r) t += lds[wave * 256 + w * 64 + r * GP * L + lane];
-        const int base = k == 0 ? SEG[s].w : inv ? NW + SEG[s].b : k == 1 ? SEG[s].gw : NW + SEG[s].gb;
-        to[base + channel(c / V) + c % V] = t;
+        const bool b = inv ? k == 1 : k == 2;
+        const int at = (k == 0 ? SEG[s].w : inv ? SEG[s].b : k == 1 ? SEG[s].gw : SEG[s].gb) + channel(c / V) + c % V;
+        if (to) to[b ? NW + at : at] = t;
+        else (b ? gbias : gweight)[at] = (T)t;
       }
     }
   }
@@ -427,7 +430,7 @@ extern "C" __global__ void __launch_bounds__(256) cgtp_norm_row_fwd(const T* __r
 
 struct RowBwd {
   const T* __restrict__ x; const T* __restrict__ weight; const T* __restrict__ bias; const T* __restrict__ gy; const T* __restrict__ stats;
-  T* __restrict__ gx; double* __restrict__ part; i64 N; int phase; double* lds;
+  T* __restrict__ gx; double* __restrict__ sums; T* __restrict__ gweight; T* __restrict__ gbias; i64 N; int phase; double* lds;
   template <int s> __device__ void operator()() const {
     typedef Lane<s> A;
     const A a(phase);
@@ -443,7 +446,7 @@ struct RowBwd {
       a.read(gy + r * DY + SEG[s].ycol, q);
       a.read_gates(x + r * DX, g);
       const Stat S = a.stat(stats + r * NST);
-      const Sums o = a.backward(v, g, q, qg, S, p, in, &sum);
+      const Sums o = a.backward(v, g, q, qg, S, p, in, true, sum);
       Means e = {T(0), lanes_sum_<A::L>(o.hx) * T(1.0 / (A::cg * A::n)), T(0), T(0)};
       if constexpr (A::inv) e.h = lanes_sum_<A::L>(o.h) * T(1.0 / A::cg);
       if constexpr (A::gated) {
@@ -456,22 +459,22 @@ struct RowBwd {
         a.write_gates(gx + r * DX, qg);
       }
     }
-    a.put_sums(sum, part + part_() * (NW + NB), lds);
+    a.put_sums(sum, sums ? sums + part_() * (NW + NB) : nullptr, gweight, gbias, lds);
   }
 };
 extern "C" __global__ void __launch_bounds__(256) cgtp_norm_row_bwd(const T* __restrict__ x, const T* __restrict__ weight, const T* __restrict__ bias,
                                                                 const T* __restrict__ gy, const T* __restrict__ stats, T* __restrict__ gx,
-                                                                double* __restrict__ part, i64 N) {
+                                                                double* __restrict__ sums, T* __restrict__ gweight, T* __restrict__ gbias, i64 N) {
   __shared__ double lds[1024];
-  with_sub_(sub_(), RowBwd{x, weight, bias, gy, stats, gx, part, N, SUB[sub_()].phase, lds});
+  with_sub_(sub_(), RowBwd{x, weight, bias, gy, stats, gx, sums, gweight, gbias, N, SUB[sub_()].phase, lds});
 }
 )HIP";
 
-// Samples of any number of rows.  The rows are cut into chunks of R; a workgroup has a sub-unit of a chunk.  A sample of at most R rows belongs to the chunk of its
-// first row: its sums are formed and its results written by one workgroup, from registers if it fits one step.  Longer samples take three kernels: sums of
-// each chunk's share (a chunk has at most two: one that goes on, slot 0, one that begins, slot 1), their total (place: the chunk of the sample's first row),
-// and the results.  The first two are launched only if N > R.  Sums over rows are held in 64 bits; fp64 ones are of the distance from the group's first
-// number of the sample, for their variance.
+// Samples of any number of rows.  The rows are cut into chunks of D; a workgroup has a sub-unit of a chunk.  A sample of at most R rows (R >= D) belongs to the
+// chunk of its first row: its sums are formed and its results written by one workgroup, from registers if it fits one step.  Longer samples take a second
+// kernel, which is launched only if N > R: the first leaves the sums of each chunk's share (a chunk has at most two: one that goes on, slot 0, one
+// that begins, slot 1), the second adds up the shares of a sample, each workgroup for its groups, and writes the results.  Sums over rows are held
+// in 64 bits; those of fp64 are of the distance from the group's first number of the sample, for their variance.
 const char kGraphs[] = R"HIP(
 __device__ inline i64 inside_(i64 p, i64 N) { return p < 0 ? 0 : p > N ? N : p; }
 
@@ -491,23 +494,59 @@ __device__ inline i64 first_from_(const i64* __restrict__ ptr, i64 S, i64 N, i64
   return lo;
 }
 
-// the samples of a chunk: f(sample, first row, end, from, to, slot): the whole of a short one, or a long one's rows in this chunk
-template <class F> __device__ inline void each_piece_(const i64* __restrict__ ptr, i64 S, i64 N, i64 R, i64 chunk, F f) {
-  const i64 a = chunk * R, b = a + R < N ? a + R : N;
-  const bool last = a + R >= N;
-  i64 s = first_from_(ptr, S, N, a);
-  if (s > 0) {
-    const i64 r0 = inside_(ptr[s - 1], N), r1 = inside_(ptr[s], N);
-    if (r1 > a && r1 - r0 > R) f(s - 1, r0, r1, a, r1 < b ? r1 : b, 0);
+struct Chunks {
+  const i64* __restrict__ ptr;
+  i64 N, S, R, D, chunk;
+  // the samples of the chunk: f(sample, first row, end, from, to, slot): the whole of a short one (slot -1), or a long one's rows in this chunk
+  template <class F> __device__ void each(F f) const {
+    const i64 a = chunk * D, b = a + D < N ? a + D : N;
+    const bool last = a + D >= N;
+    i64 s = first_from_(ptr, S, N, a);
+    if (s > 0) {
+      const i64 r0 = inside_(ptr[s - 1], N), r1 = inside_(ptr[s], N);
+      if (r1 > a && r1 - r0 > R) f(s - 1, r0, r1, a, r1 < b ? r1 : b, 0);
+    }
+    for (; s < S; ++s) {
+      const i64 r0 = inside_(ptr[s], N);
+      if (r0 < a || (r0 >= b && !(last && r0 == N))) break;
+      const i64 e = inside_(ptr[s + 1], N), r1 = e < r0 ? r0 : e;
+      const bool is_long = r1 - r0 > R;
+      f(s, r0, r1, r0, is_long ? b : r1, is_long ? 1 : -1);
+    }
   }
-  for (; s < S; ++s) {
-    const i64 r0 = inside_(ptr[s], N);
-    if (r0 < a || (r0 >= b && !(last && r0 == N))) break;
-    const i64 e = inside_(ptr[s + 1], N), r1 = e < r0 ? r0 : e;
-    const bool is_long = r1 - r0 > R;
-    f(s, r0, r1, r0, is_long ? b : r1, is_long ? 1 : -1);
+  // place of a share of a unit's sums
+  __device__ i64 share(i64 c, int slot, int s, int g) const { return (((c * 2 + slot) * NS + s) * G + g) * 4; }
+  // the sums of all shares of a long sample for the lane's group, by the workgroup: 256 / GP threads a group
+  template <class A, int s> __device__ void total(const A& a, const double* __restrict__ part, i64 r0, i64 r1, double (&t)[4], double* lds) const {
+    constexpr int per = A::GP < 256 ? 256 / A::GP : 1;      // threads a group
+    const i64 c0 = r0 / D, end = (r1 - 1) / D;
+    __syncthreads();
+    if ((int)threadIdx.x < per * A::GP) {
+      const int gq = threadIdx.x % A::GP, g = a.g - a.gq + gq;
+      double v[4] = {};
+      for (i64 c = c0 + threadIdx.x / A::GP; c <= end; c += per) {
+        const double* p = part + share(c, c == c0, s, g);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] += p[i];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) lds[threadIdx.x * 4 + i] = v[i];
+    }
+    __syncthreads();
+    // a tree over the threads of a group, in a fixed order
+    for (int m = per; m > 1;) {
+      const int h = (m + 1) / 2;
+      if ((int)threadIdx.x < (m - h) * A::GP)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) lds[threadIdx.x * 4 + i] += lds[(threadIdx.x + h * A::GP) * 4 + i];
+      __syncthreads();
+      m = h;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] = lds[a.gq * 4 + i];
+    __syncthreads();
   }
-}
+};
 
 // sums of the lanes, rows and waves for each group of the step: four numbers
 template <class A> __device__ inline void group_sums_(const A& a, double (&t)[4], double* lds) {
@@ -527,34 +566,34 @@ template <class A> __device__ inline void group_sums_(const A& a, double (&t)[4]
 }
 
 // what the moments are taken about: fp64: the group's first numbers of the sample; fp32: zero, a square has 48 of the 53 bits that its sum is held in
-template <int s> struct Shift { double x, g; };
-template <int s> __device__ inline Shift<s> shift_(const Lane<s>& a, const T* __restrict__ x, i64 r0, i64 rows) {
-  Shift<s> h = {0, 0};
+struct Shift { double x, g; };
+template <int s> __device__ inline Shift shift_(const Lane<s>& a, const T* __restrict__ x, i64 r0, i64 rows) {
+  Shift h = {0, 0};
   if (sizeof(T) == 8 && rows > 0) {
     if (Lane<s>::inv) h.x = x[r0 * DX + SEG[s].col + a.g * Lane<s>::cg];
     if (Lane<s>::gated) h.g = x[r0 * DX + SEG[s].gate + a.g * Lane<s>::cg];
   }
   return h;
 }
-template <int s> __device__ inline void moments_(const Lane<s>& a, const T* v, const T* g, const Shift<s>& h, bool in, double (&t)[4]) {
+template <int s> __device__ inline void moments_(const Lane<s>& a, const T* v, const T* g, const Shift& h, bool in, double (&t)[4]) {
   typedef Lane<s> A;
 #pragma unroll
   for (int c = 0; c < A::C; ++c) {
-    if (!A::full && !a.has(c / A::V)) continue;
+    const bool count = in && a.has(c / A::V);
 #pragma unroll
     for (int m = 0; m < A::n; ++m) {
-      const double d = in ? (double)v[c * A::n + m] - h.x : 0.0;
+      const double d = count ? (double)v[c * A::n + m] - h.x : 0.0;
       if (A::inv) t[0] += d;
       t[1] = __builtin_fma(d, d, t[1]);
     }
     if constexpr (A::gated) {
-      const double d = in ? (double)g[c] - h.g : 0.0;
+      const double d = count ? (double)g[c] - h.g : 0.0;
       t[2] += d;
       t[3] = __builtin_fma(d, d, t[3]);
     }
   }
 }
-template <int s> __device__ inline Stat stat_of_(const double (&t)[4], const Shift<s>& h, i64 rows) {
+template <int s> __device__ inline Stat stat_of_(const double (&t)[4], const Shift& h, i64 rows) {
   typedef Lane<s> A;
   const double m = rows > 0 ? (double)rows * A::cg : 1.0, M = m * A::n;
   const double d = t[0] / M, var = t[1] / M - d * d;
@@ -567,111 +606,48 @@ template <int s> __device__ inline Stat stat_of_(const double (&t)[4], const Shi
   return S;
 }
 
-// sums of the shares of long samples: part[chunk][slot][segment][group][4]
-struct PartFwd {
-  const T* __restrict__ x; double* __restrict__ part; const i64* __restrict__ ptr; i64 N, S, R, chunk; int phase; double* lds;
-  template <int s> __device__ void operator()() const {
-    typedef Lane<s> A;
-    const A a(phase);
-    each_piece_(ptr, S, N, R, chunk, [&](i64, i64 r0, i64 r1, i64 from, i64 to, int slot) {
-      if (slot < 0) return;
-      const Shift<s> h = shift_<s>(a, x, r0, r1 - r0);
-      double t[4] = {};
-      for (i64 base = from + (threadIdx.x / 64) * A::RP; base < to; base += 4 * A::RP) {
-        const bool in = a.on && base + a.rho < to;
-        const i64 r = base + a.rho < to ? base + a.rho : to - 1;
-        T v[A::C * A::n], g[A::C];
-        a.read(x + r * DX + SEG[s].col, v);
-        a.read_gates(x + r * DX, g);
-        moments_<s>(a, v, g, h, in, t);
-      }
-      group_sums_(a, t, lds);
-      if (threadIdx.x < 64 && a.on && a.rho == 0 && a.li == 0)
-        for (int i = 0; i < 4; ++i) part[(((chunk * 2 + slot) * NS + s) * G + a.g) * 4 + i] = t[i];
-    });
-  }
-};
-extern "C" __global__ void __launch_bounds__(256) cgtp_norm_part_fwd(const T* __restrict__ x, double* __restrict__ part, const i64* __restrict__ ptr, i64 N, i64 S, i64 R) {
-  __shared__ double lds[1024];
-  with_sub_(sub_(), PartFwd{x, part, ptr, N, S, R, part_(), SUB[sub_()].phase, lds});
-}
-
-// the long sample that begins in a chunk: f(sample, first row, end)
-template <class F> __device__ inline void long_sample_(const i64* __restrict__ ptr, i64 S, i64 N, i64 R, i64 chunk, F f) {
-  each_piece_(ptr, S, N, R, chunk, [&](i64 s, i64 r0, i64 r1, i64, i64, int slot) {
-    if (slot == 1) f(s, r0, r1);
-  });
-}
-// total of a unit's shares, by 16 neighbouring lanes
-__device__ inline void total_(const double* __restrict__ part, i64 R, i64 chunk, i64 r1, int unit, double (&t)[4]) {
-  const i64 end = (r1 - 1) / R;
-  for (int i = 0; i < 4; ++i) t[i] = 0;
-  for (i64 c = chunk + threadIdx.x % 16; c <= end; c += 16)
-    for (int i = 0; i < 4; ++i) t[i] += part[((c * 2 + (c == chunk)) * NS * G + unit) * 4 + i];
-  for (int i = 0; i < 4; ++i) t[i] = lanes_sum_<16>(t[i]);
-}
-struct MeanFwd {
-  const T* __restrict__ x; const double* t; T* __restrict__ total; T* __restrict__ stats; i64 r0, r1, sample, chunk; int g;
-  template <int s> __device__ void operator()() const {
-    Lane<s> a(0);
-    a.g = g;
-    const double v[4] = {t[0], t[1], t[2], t[3]};
-    const Stat S = stat_of_<s>(v, shift_<s>(a, x, r0, r1 - r0), r1 - r0);
-    T* to = total + ((chunk * NS + s) * G + g) * 4;
-    to[0] = S.mu; to[1] = S.r; to[2] = S.gmu; to[3] = S.gr;
-    if (stats) a.put_stat(stats + sample * NST, S);
-  }
-};
-extern "C" __global__ void __launch_bounds__(256) cgtp_norm_mean_fwd(const T* __restrict__ x, const double* __restrict__ part, T* __restrict__ total, T* __restrict__ stats,
-                                                                 const i64* __restrict__ ptr, i64 N, i64 S, i64 R) {
-  const i64 chunk = blockIdx.x;
-  long_sample_(ptr, S, N, R, chunk, [&](i64 sample, i64 r0, i64 r1) {
-    for (int u0 = 0; u0 < NS * G; u0 += 16) {
-      const int u = u0 + threadIdx.x / 16 < NS * G ? u0 + threadIdx.x / 16 : NS * G - 1;
-      double t[4];
-      total_(part, R, chunk, r1, u, t);
-      if (threadIdx.x % 16 == 0) with_segment_<0>(u / G, MeanFwd{x, t, total, stats, r0, r1, sample, chunk, u % G});
-    }
-  });
-}
-
-struct GraphFwd {
-  const T* __restrict__ x; const T* __restrict__ weight; const T* __restrict__ bias; T* __restrict__ y; T* __restrict__ stats; const T* __restrict__ total;
-  const i64* __restrict__ ptr; i64 N, S, R, chunk; int phase; double* lds;
+// kLong: the second kernel
+template <bool kLong> struct GraphFwd {
+  const T* __restrict__ x; const T* __restrict__ weight; const T* __restrict__ bias; T* __restrict__ y; T* __restrict__ stats; double* __restrict__ part;
+  Chunks of; int phase; double* lds;
   template <int s> __device__ void operator()() const {
     typedef Lane<s> A;
     const A a(phase);
     Param p[A::C];
     a.params(weight, bias, p);
-    each_piece_(ptr, S, N, R, chunk, [&](i64 sample, i64 r0, i64 r1, i64 from, i64 to, int slot) {
+    of.each([&](i64 sample, i64 r0, i64 r1, i64 from, i64 to, int slot) {
+      if (kLong && slot < 0) return;
       const i64 first = from + (threadIdx.x / 64) * A::RP;
       i64 base = first;
       T v[A::C * A::n], g[A::C];
-      Stat st;
       auto fetch = [&] {
         const i64 r = base + a.rho < to ? base + a.rho : to - 1;
         a.read(x + r * DX + SEG[s].col, v);
         a.read_gates(x + r * DX, g);
       };
+      const Shift h = shift_<s>(a, x, r0, r1 - r0);
+      double t[4] = {};
       bool held = false;      // the last step's rows are in v, g
-      if (slot < 0) {
-        const Shift<s> h = shift_<s>(a, x, r0, r1 - r0);
-        double t[4] = {};
+      if (kLong) {
+        of.template total<A, s>(a, part, r0, r1, t, lds);
+        if (base < to) base += (to - 1 - base) / (4 * A::RP) * (4 * A::RP);
+        else base -= 4 * A::RP;
+      } else {
         for (; base < to; base += 4 * A::RP) {
           fetch();
           moments_<s>(a, v, g, h, a.on && base + a.rho < to, t);
         }
         group_sums_(a, t, lds);
-        st = stat_of_<s>(t, h, r1 - r0);
-        if (stats && threadIdx.x < 64 && a.on && a.rho == 0 && a.li == 0) a.put_stat(stats + sample * NST, st);
+        if (slot >= 0) {
+          if (threadIdx.x < 64 && a.on && a.rho == 0 && a.li == 0)
+            for (int i = 0; i < 4; ++i) part[of.share(of.chunk, slot, s, a.g) + i] = t[i];
+          return;
+        }
         base -= 4 * A::RP;
         held = true;
-      } else {
-        const T* tt = total + ((r0 / R * NS + s) * G + a.g) * 4;
-        st = Stat{tt[0], tt[1], tt[2], tt[3]};
-        if (base < to) base += (to - 1 - base) / (4 * A::RP) * (4 * A::RP);
-        else base -= 4 * A::RP;
       }
+      const Stat st = stat_of_<s>(t, h, r1 - r0);
+      if (stats && slot != 0 && threadIdx.x < 64 && a.on && a.rho == 0 && a.li == 0) a.put_stat(stats + sample * NST, st);
       for (; base >= first; base -= 4 * A::RP) {
         if (!held) fetch();
         held = false;
@@ -681,136 +657,90 @@ struct GraphFwd {
     });
   }
 };
-extern "C" __global__ void __launch_bounds__(256) cgtp_norm_graph_fwd(const T* __restrict__ x, const T* __restrict__ weight, const T* __restrict__ bias,
-                                                                  T* __restrict__ y, T* __restrict__ stats, const T* __restrict__ total,
-                                                                  const i64* __restrict__ ptr, i64 N, i64 S, i64 R) {
-  __shared__ double lds[1024];
-  with_sub_(sub_(), GraphFwd{x, weight, bias, y, stats, total, ptr, N, S, R, part_(), SUB[sub_()].phase, lds});
-}
-
-template <int s> struct BwdRow {
-  typedef Lane<s> A;
-  T v[A::C * A::n], q[A::C * A::n], g[A::C], qg[A::C];
-  __device__ void fetch(const A& a, const T* __restrict__ x, const T* __restrict__ gy, i64 r) {
-    a.read(x + r * DX + SEG[s].col, v);
-    a.read(gy + r * DY + SEG[s].ycol, q);
-    a.read_gates(x + r * DX, g);
+#define GRAPH_FWD(name, kLong) \
+  extern "C" __global__ void __launch_bounds__(256) name(const T* __restrict__ x, const T* __restrict__ weight, const T* __restrict__ bias, T* __restrict__ y, \
+                                                         T* __restrict__ stats, double* __restrict__ part, const i64* __restrict__ ptr, i64 N, i64 S, i64 R, i64 D) { \
+    __shared__ double lds[1024]; \
+    const i64 chunk = kLong ? gridDim.x / NSUB - 1 - part_() : part_();     /* what the first kernel read last is still near */ \
+    with_sub_(sub_(), GraphFwd<kLong>{x, weight, bias, y, stats, part, Chunks{ptr, N, S, R, D, chunk}, SUB[sub_()].phase, lds}); \
   }
-};
-__device__ inline void add_(double (&t)[4], const Sums& o) {
-  t[0] += o.h;
-  t[1] += o.hx;
-  t[2] += o.gh;
-  t[3] += o.ghx;
-}
+GRAPH_FWD(cgtp_norm_graph_fwd, false)
+GRAPH_FWD(cgtp_norm_long_fwd, true)
+
 template <int s> __device__ inline Means means_of_(const double (&t)[4], i64 rows) {
   const double m = rows > 0 ? (double)rows * Lane<s>::cg : 1.0;
   return Means{(T)(t[0] / m), (T)(t[1] / (m * Lane<s>::n)), (T)(t[2] / m), (T)(t[3] / m)};
 }
-
-struct PartBwd {
-  const T* __restrict__ x; const T* __restrict__ weight; const T* __restrict__ bias; const T* __restrict__ gy; const T* __restrict__ stats; double* __restrict__ part;
-  const i64* __restrict__ ptr; i64 N, S, R, chunk; int phase; double* lds;
-  template <int s> __device__ void operator()() const {
-    typedef Lane<s> A;
-    const A a(phase);
-    Param p[A::C];
-    a.params(weight, bias, p);
-    each_piece_(ptr, S, N, R, chunk, [&](i64 sample, i64, i64, i64 from, i64 to, int slot) {
-      if (slot < 0) return;
-      const Stat st = a.stat(stats + sample * NST);
-      double t[4] = {};
-      for (i64 base = from + (threadIdx.x / 64) * A::RP; base < to; base += 4 * A::RP) {
-        const bool in = a.on && base + a.rho < to;
-        BwdRow<s> w;
-        w.fetch(a, x, gy, base + a.rho < to ? base + a.rho : to - 1);
-        add_(t, a.backward(w.v, w.g, w.q, w.qg, st, p, in, nullptr));
-      }
-      group_sums_(a, t, lds);
-      if (threadIdx.x < 64 && a.on && a.rho == 0 && a.li == 0)
-        for (int i = 0; i < 4; ++i) part[(((chunk * 2 + slot) * NS + s) * G + a.g) * 4 + i] = t[i];
-    });
-  }
-};
-extern "C" __global__ void __launch_bounds__(256) cgtp_norm_part_bwd(const T* __restrict__ x, const T* __restrict__ weight, const T* __restrict__ bias,
-                                                                 const T* __restrict__ gy, const T* __restrict__ stats, double* __restrict__ part,
-                                                                 const i64* __restrict__ ptr, i64 N, i64 S, i64 R) {
-  __shared__ double lds[1024];
-  with_sub_(sub_(), PartBwd{x, weight, bias, gy, stats, part, ptr, N, S, R, part_(), SUB[sub_()].phase, lds});
-}
-struct MeanBwd {
-  const double* t; T* __restrict__ total; i64 rows, chunk; int g;
-  template <int s> __device__ void operator()() const {
-    const double v[4] = {t[0], t[1], t[2], t[3]};
-    const Means e = means_of_<s>(v, rows);
-    T* to = total + ((chunk * NS + s) * G + g) * 4;
-    to[0] = e.h; to[1] = e.hx; to[2] = e.gh; to[3] = e.ghx;
-  }
-};
-extern "C" __global__ void __launch_bounds__(256) cgtp_norm_mean_bwd(const double* __restrict__ part, T* __restrict__ total, const i64* __restrict__ ptr, i64 N, i64 S, i64 R) {
-  const i64 chunk = blockIdx.x;
-  long_sample_(ptr, S, N, R, chunk, [&](i64, i64 r0, i64 r1) {
-    for (int u0 = 0; u0 < NS * G; u0 += 16) {
-      const int u = u0 + threadIdx.x / 16 < NS * G ? u0 + threadIdx.x / 16 : NS * G - 1;
-      double t[4];
-      total_(part, R, chunk, r1, u, t);
-      if (threadIdx.x % 16 == 0) with_segment_<0>(u / G, MeanBwd{t, total, r1 - r0, chunk, u % G});
-    }
-  });
-}
-struct GraphBwd {
+// the parameters' gradients are summed where a row's results are written
+template <bool kLong> struct GraphBwd {
   const T* __restrict__ x; const T* __restrict__ weight; const T* __restrict__ bias; const T* __restrict__ gy; const T* __restrict__ stats; T* __restrict__ gx;
-  double* __restrict__ sums; const T* __restrict__ total; const i64* __restrict__ ptr; i64 N, S, R, chunk; int phase; double* lds;
+  double* __restrict__ part; double* __restrict__ sums; T* __restrict__ gweight; T* __restrict__ gbias; Chunks of; int phase; double* lds;
   template <int s> __device__ void operator()() const {
     typedef Lane<s> A;
     const A a(phase);
     Param p[A::C];
     a.params(weight, bias, p);
     typename A::Sum sum = {};
-    each_piece_(ptr, S, N, R, chunk, [&](i64 sample, i64 r0, i64 r1, i64 from, i64 to, int slot) {
+    of.each([&](i64 sample, i64 r0, i64 r1, i64 from, i64 to, int slot) {
+      if (kLong && slot < 0) return;
       const i64 first = from + (threadIdx.x / 64) * A::RP;
       i64 base = first;
       const Stat st = a.stat(stats + sample * NST);
-      BwdRow<s> w;
-      Means e;
-      auto products = [&](typename A::Sum* add) {
-        w.fetch(a, x, gy, base + a.rho < to ? base + a.rho : to - 1);
-        return a.backward(w.v, w.g, w.q, w.qg, st, p, a.on && base + a.rho < to, add);
+      T v[A::C * A::n], q[A::C * A::n], g[A::C], qg[A::C];
+      auto products = [&](bool add) {
+        const i64 r = base + a.rho < to ? base + a.rho : to - 1;
+        a.read(x + r * DX + SEG[s].col, v);
+        a.read(gy + r * DY + SEG[s].ycol, q);
+        a.read_gates(x + r * DX, g);
+        return a.backward(v, g, q, qg, st, p, a.on && base + a.rho < to, add, sum);
       };
-      bool held = false, count = true;      // the channels' sums are still to be added to
-      if (slot < 0) {
-        double t[4] = {};
-        for (; base < to; base += 4 * A::RP) add_(t, products(&sum));
-        group_sums_(a, t, lds);
-        e = means_of_<s>(t, r1 - r0);
-        base -= 4 * A::RP;
-        held = true;
-        count = false;
-      } else {
-        const T* tt = total + ((r0 / R * NS + s) * G + a.g) * 4;
-        e = Means{tt[0], tt[1], tt[2], tt[3]};
+      double t[4] = {};
+      bool held = false;
+      if (kLong) {
+        of.template total<A, s>(a, part, r0, r1, t, lds);
         if (base < to) base += (to - 1 - base) / (4 * A::RP) * (4 * A::RP);
         else base -= 4 * A::RP;
+      } else {
+        for (; base < to; base += 4 * A::RP) {
+          const Sums o = products(slot < 0);
+          t[0] += o.h;
+          t[1] += o.hx;
+          t[2] += o.gh;
+          t[3] += o.ghx;
+        }
+        group_sums_(a, t, lds);
+        if (slot >= 0) {
+          if (threadIdx.x < 64 && a.on && a.rho == 0 && a.li == 0)
+            for (int i = 0; i < 4; ++i) part[of.share(of.chunk, slot, s, a.g) + i] = t[i];
+          return;
+        }
+        base -= 4 * A::RP;
+        held = true;
       }
+      const Means e = means_of_<s>(t, r1 - r0);
       for (; base >= first; base -= 4 * A::RP) {
-        if (!held) products(count ? &sum : nullptr);
+        if (!held) products(kLong);
         held = false;
-        a.finish(w.v, w.g, w.q, w.qg, st, e);
+        a.finish(v, g, q, qg, st, e);
         if (a.on && base + a.rho < to) {
-          a.write(gx + (base + a.rho) * DX + SEG[s].col, w.q);
-          a.write_gates(gx + (base + a.rho) * DX, w.qg);
+          a.write(gx + (base + a.rho) * DX + SEG[s].col, q);
+          a.write_gates(gx + (base + a.rho) * DX, qg);
         }
       }
     });
-    a.put_sums(sum, sums + chunk * (NW + NB), lds);
+    a.put_sums(sum, sums ? sums + part_() * (NW + NB) : nullptr, gweight, gbias, lds);
   }
 };
-extern "C" __global__ void __launch_bounds__(256) cgtp_norm_graph_bwd(const T* __restrict__ x, const T* __restrict__ weight, const T* __restrict__ bias,
-                                                                  const T* __restrict__ gy, const T* __restrict__ stats, T* __restrict__ gx,
-                                                                  double* __restrict__ sums, const T* __restrict__ total, const i64* __restrict__ ptr, i64 N, i64 S, i64 R) {
-  __shared__ double lds[1024];
-  with_sub_(sub_(), GraphBwd{x, weight, bias, gy, stats, gx, sums, total, ptr, N, S, R, part_(), SUB[sub_()].phase, lds});
-}
+#define GRAPH_BWD(name, kLong) \
+  extern "C" __global__ void __launch_bounds__(256) name(const T* __restrict__ x, const T* __restrict__ weight, const T* __restrict__ bias, const T* __restrict__ gy, \
+                                                         const T* __restrict__ stats, T* __restrict__ gx, double* __restrict__ part, double* __restrict__ sums, \
+                                                         T* __restrict__ gweight, T* __restrict__ gbias, const i64* __restrict__ ptr, i64 N, i64 S, i64 R, i64 D) { \
+    __shared__ double lds[1024]; \
+    const i64 chunk = kLong ? gridDim.x / NSUB - 1 - part_() : part_(); \
+    with_sub_(sub_(), GraphBwd<kLong>{x, weight, bias, gy, stats, gx, part, sums, gweight, gbias, Chunks{ptr, N, S, R, D, chunk}, SUB[sub_()].phase, lds}); \
+  }
+GRAPH_BWD(cgtp_norm_graph_bwd, false)
+GRAPH_BWD(cgtp_norm_long_bwd, true)
 )HIP";
 
 // Groups too large for the registers of a wave (more than 64 words a lane, fp64 32): one workgroup for each unit of a sample, whatever its
@@ -977,29 +907,34 @@ extern "C" __global__ void __launch_bounds__(256) cgtp_norm_unit_bwd(const T* __
 }
 )HIP";
 
-// gweight and gbias from `rows` rows of partial sums
+// gweight and gbias from `rows` rows of partial sums: 16 columns a workgroup, 64 threads a column
 const char kSums[] = R"HIP(
-extern "C" __global__ void __launch_bounds__(256) cgtp_norm_sums(const double* __restrict__ part, i64 rows, T* __restrict__ gweight, T* __restrict__ gbias) {
-  __shared__ double lds[256];
-  const int c = blockIdx.x * 16 + threadIdx.x % 16, t = threadIdx.x / 16;
-  double v = 0;
-  if (c < NW + NB)
-    for (i64 r = t; r < rows; r += 16) v += part[r * (NW + NB) + c];
-  lds[threadIdx.x] = v;
+extern "C" __global__ void __launch_bounds__(1024) cgtp_norm_sums(const double* __restrict__ part, i64 rows, T* __restrict__ gweight, T* __restrict__ gbias) {
+  __shared__ double lds[1024];
+  const int c = blockIdx.x * 16 + threadIdx.x % 16, t = threadIdx.x / 16, cc = c < NW + NB ? c : 0;
+  double v[4] = {};
+  for (i64 r = t; r < rows; r += 256)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] += r + 64 * i < rows ? part[(r + 64 * i) * (NW + NB) + cc] : 0.0;
+  lds[threadIdx.x] = (v[0] + v[1]) + (v[2] + v[3]);
   __syncthreads();
+#pragma unroll
+  for (int h = 512; h >= 16; h /= 2) {
+    if ((int)threadIdx.x < h) lds[threadIdx.x] += lds[threadIdx.x + h];
+    __syncthreads();
+  }
   if (t != 0 || c >= NW + NB) return;
-  for (int i = 1; i < 16; ++i) v += lds[threadIdx.x + 16 * i];
-  if (c < NW) gweight[c] = (T)v;
-  else gbias[c - NW] = (T)v;
+  if (c < NW) gweight[c] = (T)lds[threadIdx.x];
+  else gbias[c - NW] = (T)lds[threadIdx.x];
 }
 )HIP";
 
 }  // namespace
 
-void emit_norm(Norm& N) {
+void emit_norm(Norm& N, bool covered) {
   const bool f64 = N.dtype == CGTP_F64;
   const int most = f64 ? 32 : 64;          // words a lane holds of a row
-  N.covered = true;
+  N.covered = covered;
   struct Sub {
     int s, phase, size;
   };

@@ -8,6 +8,7 @@
 #include <sys/stat.h>
 #include <unistd.h>
 
+#include <algorithm>
 #include <climits>
 #include <cstdio>
 #include <cstdlib>
@@ -125,24 +126,27 @@ std::vector<char> compile(const Kernel& k) {
 }
 
 // Value of an integer entry of the code object's kernel metadata (a MessagePack map inside the ELF note;
-// the key is a short string, the value follows it as a MessagePack unsigned integer).  One kernel per
-// code object, so the first occurrence of the key is the one.  Returns -1 when absent.
+// the key is a short string, the value follows it as a MessagePack unsigned integer): the largest one, where a
+// code object holds several kernels (those of the normalisation; all others hold one).  Returns -1 when absent.
 long metadata_int(const std::vector<char>& code, const char* key) {
   const size_t n = std::strlen(key);
   if (n == 0 || n > 31 || code.size() < n + 2) return -1;
   const unsigned char tag = (unsigned char)(0xa0 | n);  // fixstr header
+  long most = -1;
   for (size_t i = 0; i + n + 1 < code.size(); ++i) {
     if ((unsigned char)code[i] != tag || std::memcmp(&code[i + 1], key, n) != 0) continue;
     size_t at = i + 1 + n;
     unsigned char t = (unsigned char)code[at];
-    if (t < 0x80) return t;
-    size_t w = t == 0xcc ? 1 : t == 0xcd ? 2 : t == 0xce ? 4 : t == 0xcf ? 8 : 0;
-    if (!w || at + w >= code.size()) return -1;
-    unsigned long long v = 0;
-    for (size_t b = 0; b < w; ++b) v = (v << 8) | (unsigned char)code[at + 1 + b];
-    return (long)v;
+    unsigned long long v = t;
+    if (t >= 0x80) {
+      size_t w = t == 0xcc ? 1 : t == 0xcd ? 2 : t == 0xce ? 4 : t == 0xcf ? 8 : 0;
+      if (!w || at + w >= code.size()) continue;
+      v = 0;
+      for (size_t b = 0; b < w; ++b) v = (v << 8) | (unsigned char)code[at + 1 + b];
+    }
+    most = std::max(most, (long)v);
   }
-  return -1;
+  return most;
 }
 
 // ---- a check of what the compiler produced -------------------------------------------------------------------

@@ -27,12 +27,12 @@ struct Norm {
   int subs = 0;        // segments times their phases
   bool covered = false;
   Kernel code;         // holds the module; the functions in it:
-  hipFunction_t row_fwd = nullptr, row_bwd = nullptr, part_fwd = nullptr, mean_fwd = nullptr, graph_fwd = nullptr, part_bwd = nullptr, mean_bwd = nullptr,
-                graph_bwd = nullptr, sums = nullptr, unit_fwd = nullptr, unit_bwd = nullptr;
+  hipFunction_t row_fwd = nullptr, row_bwd = nullptr, graph_fwd = nullptr, long_fwd = nullptr, graph_bwd = nullptr, long_bwd = nullptr, sums = nullptr,
+                unit_fwd = nullptr, unit_bwd = nullptr;
   size_t elt() const { return dtype == CGTP_F64 ? 8 : 4; }
 };
 
-// Fills in how the segments are gone over, and the source.
-void emit_norm(Norm& N);
+// Fills in how the segments are gone over, and the source.  covered == false: with the kernels for any size.
+void emit_norm(Norm& N, bool covered = true);
 
 }  // namespace cgtp

@@ -50,6 +50,8 @@ def compare(got, irreps, groups, act, gated, ir_mul, p, prec, ptr, eps=1e-5):
 
 IRREPS = [("32x0e+32x1o+32x2e+32x3o", 4), ("7x0e+5x1o+3x2e+9x0e", 1), ("48x0e+10x1o+10x1e+48x0o", 2), ("4x0e+4x1o+4x1e+4x2e", 4), ("1x0e", 1),
           ("1x1o", 1), ("128x0e+128x1o", 8), ("96x0e+96x1o+96x2e", 3), ("2x4e+2x0e+2x8e", 1), ("130x0e+65x1o", 1), ("300x0e+20x0o", 20), ("16x0e+32x1o+16x2e", 16)]
+# groups that a wave's registers do not hold, and many groups
+LARGE = [("5000x0e+300x8e", 1), ("700x0e+512x3o", 1), ("512x0e+512x1o", 256), ("96x0e+192x1o", 48)]
 GRAPHS = [None, [0, 27], [0, 1, 1, 3, 40, 41], [2, 2, 9, 35], [0, 0]]
 
 
@@ -63,6 +65,15 @@ def test_against_the_oracle(irreps, groups, ir_mul, prec):
             N = 41 if ptr is not None else 37
             p = inputs(n, N, prec, seed=i)
             compare(run(n, p, ptr), irreps, groups, layer.SILU, gated, ir_mul, p, prec, ptr)
+
+
+@pytest.mark.parametrize("prec", ["f32", "f64"])
+@pytest.mark.parametrize("irreps,groups", LARGE)
+def test_large_groups(irreps, groups, prec):
+    n = handle(irreps, groups, layer.SILU, True, prec, groups == 256)
+    for ptr in (None, [0, 5, 5, 11], [0, 12]):
+        p = inputs(n, 12, prec, seed=3)
+        compare(run(n, p, ptr), irreps, groups, layer.SILU, True, groups == 256, p, prec, ptr)
 
 
 @pytest.mark.parametrize("prec", ["f32", "f64"])
