@@ -338,85 +338,106 @@ def _bad(msg: str):
     raise CgtpError(1, msg)
 
 
-def _operand(t, name: str, shape: Tuple, like=None, optional: bool = False) -> int:
-    """Checks a contiguous operand (like: the tensor whose type and device it shares) and returns its address."""
+_torch = None
+
+
+def _torch_module():
+    """torch, without the cost of an import statement in every call (0.3 of the 8 us that the host needs for a small one)."""
+    global _torch
+    if _torch is None:
+        import torch
+        _torch = torch
+    return _torch
+
+
+def _operand(t, name: str, shape: Tuple, dtype, device: int, optional: bool = False) -> int:
+    """Checks a contiguous operand and returns its address."""
     if t is None:
         return 0 if optional else _bad(f"{name} is missing")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         _bad(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.dtype != dtype or t.get_device() != device:
+        _bad(f"{name}: {t.dtype} on {t.device}, expected {dtype} where x is")
     if not t.is_contiguous():
         _bad(f"{name} must be contiguous")
-    if like is not None and (t.dtype != like.dtype or t.device != like.device):
-        _bad(f"{name}: {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
     return t.data_ptr()
 
 
-def _row_operand(t, name: str, shape: Tuple, like=None) -> Tuple[int, int]:
+def _row_operand(t, name: str, shape: Tuple, dtype, device: int) -> Tuple[int, int]:
     """The same for rows that may be columns of wider rows: address and elements from one row to the next."""
     if t is None:
         _bad(f"{name} is missing")
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         _bad(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
-    if like is not None and (t.dtype != like.dtype or t.device != like.device):
-        _bad(f"{name}: {t.dtype} on {t.device}, expected {like.dtype} on {like.device}")
-    if shape[1] > 1 and t.stride(1) != 1 and t.numel() > 0:
+    if t.dtype != dtype or t.get_device() != device:
+        _bad(f"{name}: {t.dtype} on {t.device}, expected {dtype} where x is")
+    ld, step = t.stride()
+    if step != 1 and shape[1] > 1 and shape[0] > 0:
         _bad(f"{name}: the elements of a row must be neighbours")
-    return t.data_ptr(), t.stride(0) if shape[0] > 1 else shape[1]
+    return t.data_ptr(), ld if shape[0] > 1 else shape[1]
 
 
-def _on_current_device(t):
-    """The kernels go to the current stream of the current device: data elsewhere is refused."""
-    import torch
-    if t.device.type != "cuda" or t.device.index != torch._C._cuda_getDevice():
-        _bad(f"tensors are on {t.device}, the current device is cuda:{torch._C._cuda_getDevice() if torch.cuda.is_available() else '(none)'}")
+def _type_and_device(x) -> Tuple[int, int]:
+    """The kernels go to the current stream of the current device: data elsewhere is refused, after the other checks (device -1: not
+    on a GPU)."""
+    torch = _torch_module()
+    if x is None:
+        _bad("x is missing")
+    if x.dtype == torch.float32:
+        return CGTP_F32, x.get_device()
+    if x.dtype == torch.float64:
+        return CGTP_F64, x.get_device()
+    _bad(f"float32 or float64 expected, got {x.dtype}")
 
 
-def _dtype_of(t) -> int:
-    import torch
-    if t.dtype not in (torch.float32, torch.float64):
-        _bad(f"float32 or float64 expected, got {t.dtype}")
-    return CGTP_F64 if t.dtype == torch.float64 else CGTP_F32
+def _stream_of(x, device: int) -> int:
+    if device < 0 or _torch._C._cuda_getDevice() != device:
+        current = f"cuda:{_torch._C._cuda_getDevice()}" if _torch.cuda.is_available() else "none"
+        _bad(f"tensors are on {x.device}, the current device is {current}")
+    return _stream()
 
 
 def _scratch(n: int, like):
     """Workspace of a call: torch's, given back to its allocator on the current stream, part of the graph's pool under
     torch.cuda.graph."""
-    import torch
-    return torch.empty(n, dtype=torch.uint8, device=like.device) if n else None
+    return _torch.empty(n, dtype=_torch.uint8, device=like.device) if n else None
 
 
 def gated_forward(x, Wg, Wu, out, bg=None, bu=None, act: int = ACT_SILU):
     """out = act(x Wg + bg) * (x Wu + bu).  x [rows, d_in], Wg, Wu [d_in, d_out], bg, bu [d_out] or None, out [rows, d_out]; x and
     out may be columns of wider rows.  out must not overlap an input."""
-    dt = _dtype_of(x)
-    if x.dim() != 2 or Wg.dim() != 2:
+    dt, dev = _type_and_device(x)
+    if x.dim() != 2 or Wg is None or Wg.dim() != 2:
         _bad("x and Wg must have two dimensions")
-    (rows, k), n = x.shape, Wg.shape[1]
-    px, ldx = _row_operand(x, "x", (rows, k))
-    po, ldo = _row_operand(out, "out", (rows, n), x)
-    w = [_operand(Wg, "Wg", (k, n), x), _operand(Wu, "Wu", (k, n), x), _operand(bg, "bg", (n,), x, True), _operand(bu, "bu", (n,), x, True)]
-    _on_current_device(x)
-    _check(lib().gated_forward(px, *w, po, rows, k, n, ldx, ldo, act, dt, _stream()))
+    (rows, k), n, ty = x.shape, Wg.shape[1], x.dtype
+    px, ldx = _row_operand(x, "x", (rows, k), ty, dev)
+    po, ldo = _row_operand(out, "out", (rows, n), ty, dev)
+    w = (_operand(Wg, "Wg", (k, n), ty, dev), _operand(Wu, "Wu", (k, n), ty, dev), _operand(bg, "bg", (n,), ty, dev, True),
+         _operand(bu, "bu", (n,), ty, dev, True))
+    st = _stream_of(x, dev)
+    _check(lib().gated_forward(px, *w, po, rows, k, n, ldx, ldo, act, dt, st))
     return out
 
 
 def gated_backward(x, Wg, Wu, gout, gx, gWg, gWu, bg=None, bu=None, gbg=None, gbu=None, act: int = ACT_SILU):
     """Gradients of gated_forward given gout [rows, d_out]; gbg, gbu are given where bg, bu are.  x, gout and gx may be columns of
     wider rows.  No output may overlap an input."""
-    dt = _dtype_of(x)
-    if x.dim() != 2 or Wg.dim() != 2:
+    dt, dev = _type_and_device(x)
+    if x.dim() != 2 or Wg is None or Wg.dim() != 2:
         _bad("x and Wg must have two dimensions")
-    (rows, k), n = x.shape, Wg.shape[1]
-    px, ldx = _row_operand(x, "x", (rows, k))
-    pg, ldg = _row_operand(gout, "gout", (rows, n), x)
-    pgx, ldgx = _row_operand(gx, "gx", (rows, k), x)
-    w = [_operand(Wg, "Wg", (k, n), x), _operand(Wu, "Wu", (k, n), x), _operand(bg, "bg", (n,), x, True), _operand(bu, "bu", (n,), x, True)]
-    g = [_operand(gWg, "gWg", (k, n), x), _operand(gWu, "gWu", (k, n), x), _operand(gbg, "gbg", (n,), x, True), _operand(gbu, "gbu", (n,), x, True)]
-    _on_current_device(x)
+    (rows, k), n, ty = x.shape, Wg.shape[1], x.dtype
+    px, ldx = _row_operand(x, "x", (rows, k), ty, dev)
+    pg, ldg = _row_operand(gout, "gout", (rows, n), ty, dev)
+    pgx, ldgx = _row_operand(gx, "gx", (rows, k), ty, dev)
+    w = (_operand(Wg, "Wg", (k, n), ty, dev), _operand(Wu, "Wu", (k, n), ty, dev), _operand(bg, "bg", (n,), ty, dev, True),
+         _operand(bu, "bu", (n,), ty, dev, True))
+    g = (_operand(gWg, "gWg", (k, n), ty, dev), _operand(gWu, "gWu", (k, n), ty, dev), _operand(gbg, "gbg", (n,), ty, dev, True),
+         _operand(gbu, "gbu", (n,), ty, dev, True))
+    st = _stream_of(x, dev)
     L = lib()
     nb = L.cgtp_gated_workspace_bytes(rows, k, n, dt)
     ws = _scratch(nb, x)
-    _check(L.gated_backward(px, *w, pg, pgx, *g, rows, k, n, ldx, ldg, ldgx, act, dt, _ptr(ws), nb, _stream()))
+    _check(L.gated_backward(px, *w, pg, pgx, *g, rows, k, n, ldx, ldg, ldgx, act, dt, _ptr(ws), nb, st))
     return gx, gWg, gWu, gbg, gbu
 
 
@@ -444,46 +465,49 @@ class Norm:
 
 
 def _norm_operands(norm: Norm, x, weight, bias, stats, ptr):
-    if _dtype_of(x) != norm.dtype:
+    dt, dev = _type_and_device(x)
+    if dt != norm.dtype:
         _bad(f"x is {x.dtype}, the normalisation was made for {'float64' if norm.dtype == CGTP_F64 else 'float32'}")
     if x.dim() != 2:
         _bad("x must have two dimensions")
-    N = x.shape[0]
-    S, pp = N, 0
+    N, ty = x.shape[0], x.dtype
+    S, pp, ps = N, 0, 0
     if ptr is not None:
-        import torch
-        if ptr.dtype != torch.int64 or ptr.dim() != 1 or ptr.shape[0] < 1 or not ptr.is_contiguous() or ptr.device != x.device:
+        if ptr.dtype != _torch.int64 or ptr.dim() != 1 or ptr.shape[0] < 1 or not ptr.is_contiguous() or ptr.get_device() != dev:
             _bad("ptr: a contiguous int64 tensor [samples + 1] on the device of x")
         S, pp = ptr.shape[0] - 1, ptr.data_ptr()
-    if stats is not None and stats.numel() != S * norm.n_stat:
-        _bad(f"stats: {stats.numel()} numbers, expected {S} * {norm.n_stat}")
-    ops = [_operand(x, "x", (N, norm.dim_x)), _operand(weight, "weight", (norm.n_w,), x),
-           _operand(bias, "bias", (norm.n_b,), x, norm.n_b == 0)]
-    return N, S, pp, ops, 0 if stats is None else _operand(stats, "stats", tuple(stats.shape), x)
+    if stats is not None:
+        if stats.numel() != S * norm.n_stat:
+            _bad(f"stats: {stats.numel()} numbers, expected {S} * {norm.n_stat}")
+        ps = _operand(stats, "stats", stats.shape, ty, dev)
+    ops = (_operand(x, "x", (N, norm.dim_x), ty, dev), _operand(weight, "weight", (norm.n_w,), ty, dev),
+           _operand(bias, "bias", (norm.n_b,), ty, dev, norm.n_b == 0))
+    return N, S, pp, ops, ps, ty, dev
 
 
 def norm_forward(norm: Norm, x, weight, bias, y, stats=None, ptr=None):
     """x [N, dim_x], weight [n_w], bias [n_b], y [N, dim_y], stats: samples * n_stat numbers, or None where no backward pass follows;
-    ptr: int64 [S + 1] or None (every row a sample).  Returns (y, stats)."""
-    N, S, pp, ops, ps = _norm_operands(norm, x, weight, bias, stats, ptr)
-    py = _operand(y, "y", (N, norm.dim_y), x)
-    _on_current_device(x)
+    ptr: int64 [S + 1] or None (every row a sample).  Returns (y, stats).  No output may overlap an input."""
+    N, S, pp, ops, ps, ty, dev = _norm_operands(norm, x, weight, bias, stats, ptr)
+    py = _operand(y, "y", (N, norm.dim_y), ty, dev)
+    st = _stream_of(x, dev)
     L = lib()
-    nb = L.cgtp_norm_workspace_bytes(norm._h, N, S, int(ptr is not None), 0)
+    nb = L.cgtp_norm_workspace_bytes(norm._h, N, S, ptr is not None, 0)
     ws = _scratch(nb, x)
-    _check(L.norm_forward(norm._h, *ops, py, ps, N, S, pp, _ptr(ws), nb, _stream()))
+    _check(L.norm_forward(norm._h, *ops, py, ps, N, S, pp, _ptr(ws), nb, st))
     return y, stats
 
 
 def norm_backward(norm: Norm, x, weight, bias, gy, stats, gx, gweight, gbias, ptr=None):
-    """Gradients of norm_forward given gy [N, dim_y] and the stats that it wrote.  Returns (gx, gweight, gbias)."""
-    N, S, pp, ops, ps = _norm_operands(norm, x, weight, bias, stats, ptr)
-    out = [_operand(gx, "gx", (N, norm.dim_x), x), _operand(gweight, "gweight", (norm.n_w,), x),
-           _operand(gbias, "gbias", (norm.n_b,), x, norm.n_b == 0)]
-    pg = _operand(gy, "gy", (N, norm.dim_y), x)
-    _on_current_device(x)
+    """Gradients of norm_forward given gy [N, dim_y] and the stats that it wrote.  Returns (gx, gweight, gbias).  No output may overlap
+    an input."""
+    N, S, pp, ops, ps, ty, dev = _norm_operands(norm, x, weight, bias, stats, ptr)
+    out = (_operand(gx, "gx", (N, norm.dim_x), ty, dev), _operand(gweight, "gweight", (norm.n_w,), ty, dev),
+           _operand(gbias, "gbias", (norm.n_b,), ty, dev, norm.n_b == 0))
+    pg = _operand(gy, "gy", (N, norm.dim_y), ty, dev)
+    st = _stream_of(x, dev)
     L = lib()
-    nb = L.cgtp_norm_workspace_bytes(norm._h, N, S, int(ptr is not None), 1)
+    nb = L.cgtp_norm_workspace_bytes(norm._h, N, S, ptr is not None, 1)
     ws = _scratch(nb, x)
-    _check(L.norm_backward(norm._h, *ops, pg, ps, *out, N, S, pp, _ptr(ws), nb, _stream()))
+    _check(L.norm_backward(norm._h, *ops, pg, ps, *out, N, S, pp, _ptr(ws), nb, st))
     return gx, gweight, gbias

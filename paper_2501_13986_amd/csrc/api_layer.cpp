@@ -67,6 +67,7 @@ cgtp_status check_gated(const cgtp::GatedArgs& a, int32_t dtype) {
 struct NormWork {
   int64_t R = 128, D = 0;   // rows of a short sample at most, of a chunk
   int64_t blocks = 1;       // workgroups (of each sub-unit)
+  int64_t long_blocks = 1;  // of the second kernel
   int64_t sum_rows = 1;     // partial sums of the parameters' gradients (one: written where they belong at once)
   bool longer = false;      // samples of more than R rows are possible
   size_t part = 0, bytes = 0;
@@ -85,15 +86,18 @@ struct NormWork {
       blocks = std::max<int64_t>(1, std::min<int64_t>(steps, std::max<int64_t>(1, (backward ? 2048 : most) / P.subs)));
       sum_rows = blocks;
     } else {
-      // Chunks of 16 rows leave many workgroups where samples are short; with long ones, whose shares each workgroup adds up, 128
-      D = 16;
-      while (D < 128 && (N / D * P.subs > 8192 || N / D > 4 * S)) D *= 2;
+      // Chunks of 32 rows where samples are short (500 molecules in 12 000 rows of 32 channels, l <= 3: 79 us forward and backward, with 16
+      // rows 94); up to 128 with many workgroups of them or long samples, whose shares each workgroup adds up, as long as that leaves enough
+      D = 32;
+      while (D < 128 && N / (2 * D) * P.subs >= 512 && (N / D * P.subs > 8192 || N / D > 4 * S)) D *= 2;
       while ((N + D - 1) / D > most / P.subs) D *= 2;
       R = std::max(R, D);
-      blocks = std::max<int64_t>(1, (N + D - 1) / D);
+      const int64_t chunks = std::max<int64_t>(1, (N + D - 1) / D);
       longer = N > R;
-      sum_rows = longer ? 2 * blocks : blocks;
-      if (longer) part = up((size_t)blocks * 2 * units * 4 * sizeof(double));
+      long_blocks = std::min<int64_t>(chunks, std::max(1, 2048 / P.subs));
+      blocks = backward ? long_blocks : chunks;
+      sum_rows = longer ? blocks + long_blocks : blocks;
+      if (longer) part = up((size_t)chunks * 2 * units * 4 * sizeof(double));
     }
     bytes = part + (backward && (sum_rows > 1 || !P.covered) ? up((size_t)sum_rows * (size_t)(P.n_w + P.n_b) * sizeof(double)) : 0);
   }
@@ -342,7 +346,7 @@ cgtp_status norm_forward(const cgtp_norm* norm, const void* x, const void* weigh
   }
   void* args[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&y, (void*)&stats, (void*)&part, (void*)&ptr, (void*)&N, (void*)&S, (void*)&w.R, (void*)&w.D};
   s = launch(P.graph_fwd, w.blocks * P.subs, args, st);
-  return s != CGTP_OK || !w.longer ? s : launch(P.long_fwd, w.blocks * P.subs, args, st);
+  return s != CGTP_OK || !w.longer ? s : launch(P.long_fwd, w.long_blocks * P.subs, args, st);
 }
 
 cgtp_status norm_backward(const cgtp_norm* norm, const void* x, const void* weight, const void* bias, const void* gy,
@@ -375,7 +379,7 @@ cgtp_status norm_backward(const cgtp_norm* norm, const void* x, const void* weig
                     (void*)&ptr, (void*)&N, (void*)&S, (void*)&w.R, (void*)&w.D};
     s = launch(P.graph_bwd, w.blocks * P.subs, args, st);
     args[7] = (void*)&more;
-    if (s == CGTP_OK && w.longer) s = launch(P.long_bwd, w.blocks * P.subs, args, st);
+    if (s == CGTP_OK && w.longer) s = launch(P.long_bwd, w.long_blocks * P.subs, args, st);
   }
   if (s != CGTP_OK || !sums) return s;
   void* args[] = {(void*)&sums, (void*)&w.sum_rows, (void*)&gweight, (void*)&gbias};
