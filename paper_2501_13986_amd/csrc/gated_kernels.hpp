@@ -226,9 +226,94 @@ struct Tile<double, kR, kC> {
   }
 };
 
+// Operands with the columns of x as terms, kIn (8, 16 or a multiple of 32) of them.  With 8 or 16 the 32 terms of an fp32 instruction hold four or
+// two of the six products of parts side by side (a lane's parts are those of the products that its quarter of the terms is for), so
+// that two or three instructions do; fp64 leaves out the empty ones.
+template <class T, int kIn>
+struct In {
+  using N = Num<T>;
+  static constexpr bool f32 = sizeof(T) == 4, few = kIn < 32;
+  static constexpr int KS = few ? 1 : kIn / 32;                                   // operands a row
+  static constexpr int kUnits = !few ? N::kUnits : f32 ? (kIn == 8 ? 2 : 3) : kIn / 8;
+  static constexpr int kTerms = few && !f32 ? kIn / 4 : 8;                        // a lane's terms
+  static constexpr int kGroup = few && f32 ? kIn / 8 : 4;                         // quarters that hold one product's terms
+  static constexpr int DT = (kIn + 15) / 16;                                      // tiles of 16 columns of x
+  using Parts = PartsOf<kUnits>;
+  static __device__ int first(int s, int q) { return few ? q % kGroup * kTerms : s * 32 + q * 8; }
+  // number of the product of parts that unit m of quarter q is for
+  static __device__ int pair(int m, int q) { return m * (4 / kGroup) + q / kGroup; }
+  // of a lane's terms, for the left or right operand
+  static __device__ Parts parts(const T* v, int q, bool left) {
+    if constexpr (few && f32) {
+      const typename N::Parts w = N::parts(v);
+      Parts r;
+#pragma unroll
+      for (int m = 0; m < kUnits; ++m) {
+        const int p = pair(m, q);
+        // parts of the six products, two bits each, for the left and the right operand; 3: none
+        const int part = (left ? 0xff052 : 0xff118) >> (2 * p) & 3;
+        r.w[m] = part == 0 ? w.w[0] : part == 1 ? w.w[1] : part == 2 ? w.w[2] : u32x4{0, 0, 0, 0};
+      }
+      return r;
+    } else if constexpr (few) {
+      Parts r;
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i) r.w[i] = __builtin_bit_cast(u32x4, f64x2{v[2 * i], v[2 * i + 1]});
+      return r;
+    } else {
+      return N::parts(v);
+    }
+  }
+  // of a row in LDS, for the left operand
+  template <int kR>
+  static __device__ Parts read(const Tile<T, kR, kIn>& X, int row, int s, int q) {
+    if constexpr (few && f32) {
+      Parts r;
+#pragma unroll
+      for (int m = 0; m < kUnits; ++m) {
+        const int part = 0xff052 >> (2 * pair(m, q)) & 3;    // 3: any, the right operand has zeros
+        r.w[m] = *(const u32x4*)&X.v[part == 3 ? 0 : part][row][first(0, q)];
+      }
+      return r;
+    } else if constexpr (few) {
+      Parts r;
+#pragma unroll
+      for (int i = 0; i < kUnits; ++i) r.w[i] = *(const u32x4*)&X.v[row][first(0, q) + 2 * i];
+      return r;
+    } else {
+      return X.read(row, first(s, q));
+    }
+  }
+  // of column c of W (all its rows in the descriptor), for the right operand
+  static __device__ Parts column(Buffer W, int64_t n, int64_t c, int s, int q) {
+    T v[8] = {};
+#pragma unroll
+    for (int j = 0; j < kTerms; ++j) v[j] = load1<T>(W, c < n ? ((unsigned)(first(s, q) + j) * (unsigned)n + (unsigned)c) * (unsigned)sizeof(T) : kNowhere);
+    return parts(v, q, false);
+  }
+  template <int M>
+  static __device__ void mma(const Parts* const (&a)[M], const Parts* const (&b)[M], typename N::Vec* const (&c)[M]) {
+    if constexpr (!few) {
+      N::template mma<M>(a, b, c);
+    } else if constexpr (f32) {
+#pragma unroll
+      for (int m = 0; m < kUnits; ++m)
+#pragma unroll
+        for (int i = 0; i < M; ++i)
+          *c[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[i]->w[m]), __builtin_bit_cast(bf16x8, b[i]->w[m]), *c[i], 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int m = 0; m < kTerms; ++m)
+#pragma unroll
+        for (int i = 0; i < M; ++i)
+          *c[i] = __builtin_amdgcn_mfma_f64_16x16x4f64(__builtin_bit_cast(f64x2, a[i]->w[m / 2])[m % 2], __builtin_bit_cast(f64x2, b[i]->w[m / 2])[m % 2], *c[i], 0, 0, 0);
+    }
+  }
+};
+
 // four rows 4 r4 .. of four columns k4 .. of x into X as they are, and into XT by columns, rows in the order of `term`
-template <int KC>
-__device__ inline void write_both(Tile<float, kRows, KC>& X, Tile<float, KC, kRows>& XT, int r4, int k4, float (*x)[4]) {
+template <int KC, int KD>
+__device__ inline void write_both(Tile<float, kRows, KC>& X, Tile<float, KD, kRows>& XT, int r4, int k4, float (*x)[4]) {
   unsigned row[4][2][3];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
@@ -248,8 +333,8 @@ __device__ inline void write_both(Tile<float, kRows, KC>& X, Tile<float, KC, kRo
     }
   }
 }
-template <int KC>
-__device__ inline void write_both(Tile<double, kRows, KC>& X, Tile<double, KC, kRows>& XT, int r4, int k4, double (*x)[4]) {
+template <int KC, int KD>
+__device__ inline void write_both(Tile<double, kRows, KC>& X, Tile<double, KD, kRows>& XT, int r4, int k4, double (*x)[4]) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     X.write4(r4 * 4 + j, k4, x[j]);
@@ -263,24 +348,25 @@ __device__ inline void write_both(Tile<double, kRows, KC>& X, Tile<double, KC, k
 
 // A wave keeps the parts of its 16 NT columns of Wg and Wu in registers for the whole call and walks over rows, whose parts the
 // workgroup puts into LDS once for its four waves.  Lane: columns NT l16 + j.
-template <class T, int KS, int NT, int kAct, bool kVec>
-__global__ void __launch_bounds__(kThreads, (sizeof(T) == 8 && KS > 2 ? 1 : 2)) k_gated_fwd(GatedArgs a, int col_tiles, int splits) {
+template <class T, int kIn, int NT, int kAct, bool kVec>
+__global__ void __launch_bounds__(kThreads, (sizeof(T) == 8 && kIn > 64 ? 1 : 2)) k_gated_fwd(GatedArgs a, int col_tiles, int splits) {
   using N = Num<T>;
-  __shared__ Tile<T, kRows, KS * 32> X;
-  constexpr int kQuads = KS * 8, kPer = kRows * kQuads / kThreads, e = sizeof(T);
+  using I = In<T, kIn>;
+  __shared__ Tile<T, kRows, kIn> X;
+  constexpr int KS = I::KS, kQuads = kIn / 4, kAll = kRows * kQuads, kPer = (kAll + kThreads - 1) / kThreads, e = sizeof(T);
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, l16 = lane & 15, q = lane >> 4;
   const int K = (int)a.d_in;
   const int64_t n = a.d_out, c = ((int64_t)(blockIdx.x % col_tiles) * 4 + wave) * (16 * NT) + l16 * NT;
   const unsigned ldx = (unsigned)a.ld_x * e, ldo = (unsigned)a.ld_out * e;
   const Buffer Wg = matrix_of<T>(a.Wg, 0, K, n), Wu = matrix_of<T>(a.Wu, 0, K, n);
-  typename N::Parts wg[KS][NT], wu[KS][NT];
+  typename I::Parts wg[KS][NT], wu[KS][NT];
   T bg[NT], bu[NT];
 #pragma unroll
   for (int j = 0; j < NT; ++j) {
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      wg[s][j] = column_parts<T>(Wg, n, c + j, s * 32 + q * 8);
-      wu[s][j] = column_parts<T>(Wu, n, c + j, s * 32 + q * 8);
+      wg[s][j] = I::column(Wg, n, c + j, s, q);
+      wu[s][j] = I::column(Wu, n, c + j, s, q);
     }
     bg[j] = bias_of<T>(a.bg, c + j, n);
     bu[j] = bias_of<T>(a.bu, c + j, n);
@@ -291,7 +377,7 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 8 && KS > 2 ? 1 : 2)) 
     const Buffer in = rows_of<T>(a.x, b * kRows, a.rows, a.ld_x, K);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const int at = t + i * kThreads;
+      const int at = t + i * kThreads < kAll ? t + i * kThreads : kAll - 1;
       load4<kVec>(in, at / kQuads * ldx, at % kQuads * 4, K, next[i]);
     }
   };
@@ -305,7 +391,7 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 8 && KS > 2 ? 1 : 2)) 
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int p = t + i * kThreads;
-      X.write4(p / kQuads, p % kQuads * 4, next[i]);
+      if (kAll % kThreads == 0 || __builtin_amdgcn_readfirstlane(p) < kAll) X.write4(p / kQuads, p % kQuads * 4, next[i]);   // whole waves
     }
     __syncthreads();
     if (b + splits < blocks) fetch(b + splits);
@@ -322,9 +408,9 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 8 && KS > 2 ? 1 : 2)) 
         }
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
-        const typename N::Parts xa = X.read(rt * 16 + l16, s * 32 + q * 8);
-        if constexpr (NT == 2) N::template mma<4>({&xa, &xa, &xa, &xa}, {&wg[s][0], &wu[s][0], &wg[s][1], &wu[s][1]}, {&gt[0], &ut[0], &gt[1], &ut[1]});
-        else N::template mma<2>({&xa, &xa}, {&wg[s][0], &wu[s][0]}, {&gt[0], &ut[0]});
+        const typename I::Parts xa = I::read(X, rt * 16 + l16, s, q);
+        if constexpr (NT == 2) I::template mma<4>({&xa, &xa, &xa, &xa}, {&wg[s][0], &wu[s][0], &wg[s][1], &wu[s][1]}, {&gt[0], &ut[0], &gt[1], &ut[1]});
+        else I::template mma<2>({&xa, &xa}, {&wg[s][0], &wu[s][0]}, {&gt[0], &ut[0]});
       }
     };
     auto finish = [&](int rt, const typename N::Vec* gt, const typename N::Vec* ut) {
@@ -355,35 +441,37 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 8 && KS > 2 ? 1 : 2)) 
 // but those are twice the size of gout, written once and read twice.
 
 // gWg, gWu, gbg, gbu of 16 columns a wave, over the row blocks of a split; partial sums [split][Wg; bg; Wu; bu]
-template <class T, int KS>
-constexpr int kGwWaves = KS > 2 && sizeof(T) == 4 ? 8 : 4;   // eight where the rows in LDS leave room for one workgroup only
+template <class T, int kIn>
+constexpr int kGwWaves = kIn > 64 && sizeof(T) == 4 ? 8 : 4;   // eight where the rows in LDS leave room for one workgroup only
 
-template <class T, int KS, int kAct, bool kVec>
-__global__ void __launch_bounds__((kGwWaves<T, KS> * 64), (sizeof(T) == 8 && KS > 1 ? 1 : 2)) k_gated_gw(GatedArgs a, int col_tiles, int splits, T* part) {
+template <class T, int kIn, int kAct, bool kVec>
+__global__ void __launch_bounds__((kGwWaves<T, kIn> * 64), (sizeof(T) == 8 && kIn > 32 ? 1 : 2)) k_gated_gw(GatedArgs a, int col_tiles, int splits, T* part) {
   using N = Num<T>;
-  constexpr int KC = KS * 32, e = sizeof(T);
-  __shared__ Tile<T, kRows, KC> X;
-  __shared__ Tile<T, KC, kRows> XT;
-  // blocks of 4 rows x 4 columns of x; threads without one of their own repeat the last (no lane-conditional code)
-  constexpr int kQuads = KS * 8, kBlocks = kRows / 4 * kQuads, kThr = kGwWaves<T, KS> * 64, kPer = (kBlocks + kThr - 1) / kThr;
+  using I = In<T, kIn>;
+  constexpr int KS = I::KS, DT = I::DT, e = sizeof(T);
+  __shared__ Tile<T, kRows, kIn> X;
+  __shared__ Tile<T, DT * 16, kRows> XT;      // with 8 columns of x the other half holds anything: sums that are not kept
+  // blocks of 4 rows x 4 columns of x; lanes without one of their own repeat the last, waves without any do nothing
+  constexpr int kQuads = kIn / 4, kBlocks = kRows / 4 * kQuads, kThr = kGwWaves<T, kIn> * 64, kPer = (kBlocks + kThr - 1) / kThr;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, l16 = lane & 15, q = lane >> 4;
   const int K = (int)a.d_in;
-  const int64_t n = a.d_out, c = ((int64_t)(blockIdx.x % col_tiles) * kGwWaves<T, KS> + wave) * 16 + l16;
+  const int64_t n = a.d_out, c = ((int64_t)(blockIdx.x % col_tiles) * kGwWaves<T, kIn> + wave) * 16 + l16;
   const unsigned ldx = (unsigned)a.ld_x * e, ldo = (unsigned)a.ld_gout * e;
   const Buffer Wg = matrix_of<T>(a.Wg, 0, K, n), Wu = matrix_of<T>(a.Wu, 0, K, n);
-  typename N::Parts wg[KS], wu[KS];
+  typename I::Parts wg[KS], wu[KS];
 #pragma unroll
   for (int s = 0; s < KS; ++s) {
-    wg[s] = column_parts<T>(Wg, n, c, s * 32 + q * 8);
-    wu[s] = column_parts<T>(Wu, n, c, s * 32 + q * 8);
+    wg[s] = I::column(Wg, n, c, s, q);
+    wu[s] = I::column(Wu, n, c, s, q);
   }
   const T bg = bias_of<T>(a.bg, c, n), bu = bias_of<T>(a.bu, c, n);
   const int64_t blocks = (a.rows + kRows - 1) / kRows;
   // four by four blocks to 16 neighbouring threads: their 8 bytes fall on different banks in X and in XT
   auto block = [&](int i, int& r4, int& k4) {
     const int p = t + i * kThr < kBlocks ? t + i * kThr : kBlocks - 1;
-    r4 = p % 4 + p / 16 % 4 * 4;
-    k4 = (p / 4 % 4 + p / 64 * 4) * 4;
+    constexpr int kSide = kQuads < 4 ? kQuads : 4;      // quads side by side
+    r4 = p % 4 + p / (4 * kSide) % 4 * 4;
+    k4 = (p / 4 % kSide + p / (16 * kSide) * 4) * 4;
   };
   T next[kPer][4][4];
   auto fetch = [&](int64_t b) {
@@ -397,7 +485,7 @@ __global__ void __launch_bounds__((kGwWaves<T, KS> * 64), (sizeof(T) == 8 && KS 
     }
   };
   const unsigned at = c < n ? (unsigned)c * e + N::row(q, 0) * ldo : kNowhere;
-  typename N::Vec sg[KS * 2] = {}, su[KS * 2] = {};
+  typename N::Vec sg[DT] = {}, su[DT] = {};
   T sbg = 0, sbu = 0;
   int64_t b = blockIdx.x / col_tiles;
   if (b < blocks) fetch(b);
@@ -412,6 +500,7 @@ __global__ void __launch_bounds__((kGwWaves<T, KS> * 64), (sizeof(T) == 8 && KS 
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
+      if (kBlocks % kThr != 0 && __builtin_amdgcn_readfirstlane(t + i * kThr) >= kBlocks) break;
       int r4, k4;
       block(i, r4, k4);
       write_both(X, XT, r4, k4, next[i]);
@@ -431,8 +520,8 @@ __global__ void __launch_bounds__((kGwWaves<T, KS> * 64), (sizeof(T) == 8 && KS 
         }
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
-          const typename N::Parts xa = X.read(half * 32 + rt * 16 + l16, s * 32 + q * 8);
-          N::template mma<2>({&xa, &xa}, {&wg[s], &wu[s]}, {&g, &u});
+          const typename I::Parts xa = I::read(X, half * 32 + rt * 16 + l16, s, q);
+          I::template mma<2>({&xa, &xa}, {&wg[s], &wu[s]}, {&g, &u});
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -448,7 +537,7 @@ __global__ void __launch_bounds__((kGwWaves<T, KS> * 64), (sizeof(T) == 8 && KS 
       if (half + 1 < kRows / 32) fetch_gout(half + 1);
       const typename N::Parts pg = N::parts(dg), pu = N::parts(du);
 #pragma unroll
-      for (int d = 0; d < KS * 2; ++d) {
+      for (int d = 0; d < DT; ++d) {
         const typename N::Parts xt = XT.read(d * 16 + l16, half * 32 + q * 8);
         N::template mma<2>({&xt, &xt}, {&pg, &pu}, {&sg[d], &su[d]});
       }
@@ -462,7 +551,7 @@ __global__ void __launch_bounds__((kGwWaves<T, KS> * 64), (sizeof(T) == 8 && KS 
   if (c >= n) return;
   T* to = part + (int64_t)(blockIdx.x / col_tiles) * 2 * (K + 1) * n + c;
 #pragma unroll
-  for (int d = 0; d < KS * 2; ++d)
+  for (int d = 0; d < DT; ++d)
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int k = d * 16 + N::row(q, i);
@@ -477,102 +566,136 @@ __global__ void __launch_bounds__((kGwWaves<T, KS> * 64), (sizeof(T) == 8 && KS 
   }
 }
 
-// adds up the splits, in their order
+// adds up the splits, in their order: the weights' and biases' gradients, and gx where its sums are split (gx_splits > 1)
 template <class T>
-__global__ void __launch_bounds__(kThreads) k_gated_sums(const T* __restrict__ part, int splits, int64_t K, int64_t n, T* __restrict__ gWg,
-                                                     T* __restrict__ gWu, T* __restrict__ gbg, T* __restrict__ gbu) {
-  const int64_t size = 2 * (K + 1) * n, i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (i >= size) return;
-  T v = part[i];
-  for (int s = 1; s < splits; ++s) v += part[s * size + i];
-  const int64_t row = i / n, c = i % n;
-  if (row < K) gWg[i] = v;
-  else if (row == K) { if (gbg) gbg[c] = v; }
-  else if (row <= 2 * K) gWu[i - (K + 1) * n] = v;
-  else if (gbu) gbu[c] = v;
+__global__ void __launch_bounds__(kThreads) k_gated_sums(GatedArgs a, const T* __restrict__ part, int splits, const T* __restrict__ gx_part, int gx_splits) {
+  const int64_t K = a.d_in, n = a.d_out, size = 2 * (K + 1) * n, gx_size = gx_splits > 1 ? a.rows * K : 0;
+  int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
+  auto total = [&](const T* p, int m, int64_t of) {
+    T v = p[i];
+    for (int s = 1; s < m; ++s) v += p[s * of + i];
+    return v;
+  };
+  if (i < size) {
+    const T v = total(part, splits, size);
+    const int64_t row = i / n, c = i % n;
+    if (row < K) ((T*)a.gWg)[i] = v;
+    else if (row == K) { if (a.gbg) ((T*)a.gbg)[c] = v; }
+    else if (row <= 2 * K) ((T*)a.gWu)[i - (K + 1) * n] = v;
+    else if (a.gbu) ((T*)a.gbu)[c] = v;
+    return;
+  }
+  i -= size;
+  if (i < gx_size) ((T*)a.gx)[i / K * a.ld_gx + i % K] = total(gx_part, gx_splits, gx_size);
 }
 
-// The operands of W that gx needs, kUnits x 16 bytes a lane: [32 columns of W][operand][unit][lane].  First 4 KS for g and u: (g, u) x tile x s,
-// lane: column 16 tile + l16, terms 32 s + 8 q + (0..7) of d_in; then 4 KS for gx: (g, u) x d, lane: column 16 d + l16 of x, the 32 columns
-// of W in the order of Num::term.
-template <int KS>
-constexpr int kOperands = 8 * KS;
-
-template <class T, int KS>
-__global__ void __launch_bounds__(kThreads) k_gated_operands(GatedArgs a, u32x4* to) {
-  constexpr int kUnits = Num<T>::kUnits;
-  const int K = (int)a.d_in;
-  const int64_t n = a.d_out, steps = (n + 31) / 32, e = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
-  if (e >= steps * kOperands<KS>) return;
-  const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4;
-  const int64_t step = e / kOperands<KS>;
-  const int op = (int)(e % kOperands<KS>);
-  T v[8];
-  const Buffer W = matrix_of<T>(op / (2 * KS) % 2 ? a.Wu : a.Wg, 0, K, n);   // `op` is the wave's
+// The operands of W that gx needs for 32 of its columns, in units of 16 bytes a lane.  First 4 KS for g and u: (g, u) x tile x s, lane:
+// column 16 tile + l16, its terms of d_in; then 2 DT for gx: (g, u) x d, lane: column 16 d + l16 of x, the 32 columns of W in the order of Num::term.
+template <class T, int kIn>
+struct Operands {
+  using N = Num<T>;
+  using I = In<T, kIn>;
+  static constexpr int kIns = 4 * I::KS, kOuts = 2 * I::DT, kOps = kIns + kOuts, kUnits = kIns * I::kUnits + kOuts * N::kUnits;
+  // operand `op` (the wave's) of columns 32 step .., put(unit, value)
+  template <class F>
+  static __device__ void make(const GatedArgs& a, int64_t step, int op, F put) {
+    const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4, K = (int)a.d_in;
+    const int64_t n = a.d_out;
+    const bool in = op < kIns;
+    const Buffer W = matrix_of<T>((in ? op / (2 * I::KS) : (op - kIns) / I::DT) ? a.Wu : a.Wg, 0, K, n);
+    T v[8] = {};
+    if (in) {
+      const int64_t c = step * 32 + op / I::KS % 2 * 16 + l16;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    int k;
-    int64_t c;
-    if (op < 4 * KS) {
-      k = op % KS * 32 + q * 8 + j;
-      c = step * 32 + op / KS % 2 * 16 + l16;
+      for (int j = 0; j < I::kTerms; ++j) v[j] = load1<T>(W, c < n ? ((unsigned)(I::first(op % I::KS, q) + j) * (unsigned)n + (unsigned)c) * (unsigned)sizeof(T) : kNowhere);
+      const typename I::Parts p = I::parts(v, q, true);
+#pragma unroll
+      for (int i = 0; i < I::kUnits; ++i) put(op * I::kUnits + i, p.w[i]);
     } else {
-      k = op % (2 * KS) * 16 + l16;
-      c = step * 32 + j / 4 * 16 + Num<T>::row(q, j % 4);
-    }
-    v[j] = load1<T>(W, k < K && c < n ? ((unsigned)k * (unsigned)n + (unsigned)c) * (unsigned)sizeof(T) : kNowhere);
-  }
-  const typename Num<T>::Parts p = Num<T>::parts(v);
+      const int k = (op - kIns) % I::DT * 16 + l16;
 #pragma unroll
-  for (int i = 0; i < kUnits; ++i) to[(e * kUnits + i) * 64 + lane] = p.w[i];
+      for (int j = 0; j < 8; ++j) {
+        const int64_t c = step * 32 + j / 4 * 16 + N::row(q, j % 4);
+        v[j] = load1<T>(W, k < K && c < n ? ((unsigned)k * (unsigned)n + (unsigned)c) * (unsigned)sizeof(T) : kNowhere);
+      }
+      const typename N::Parts p = N::parts(v);
+#pragma unroll
+      for (int i = 0; i < N::kUnits; ++i) put(kIns * I::kUnits + (op - kIns) * N::kUnits + i, p.w[i]);
+    }
+  }
+};
+
+// all of them, [32 columns of W][unit][lane]
+template <class T, int kIn>
+__global__ void __launch_bounds__(kThreads) k_gated_operands(GatedArgs a, u32x4* to) {
+  using O = Operands<T, kIn>;
+  const int64_t steps = (a.d_out + 31) / 32, e = (int64_t)blockIdx.x * (kThreads / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+  if (e >= steps * O::kOps) return;
+  const int64_t step = e / O::kOps;
+  O::make(a, step, (int)(e % O::kOps), [&](int unit, u32x4 v) { to[(step * O::kUnits + unit) * 64 + (threadIdx.x & 63)] = v; });
 }
 
 // gx of 16 R rows a wave: the operands of 32 columns of W at a time in LDS for the eight (fp64 of more than 64 columns of x: four) waves
-// of a workgroup, the columns of a split one after another.  More than one split: partial sums [split][rows][d_in] in part.
-template <class T, int KS>
-constexpr int kGxWaves = KS > 2 && sizeof(T) == 8 ? 4 : 8;
-template <class T, int KS>
-constexpr int kGxTiles = KS > 2 || sizeof(T) == 8 ? 1 : 2;   // 2 would not fit the registers
+// of a workgroup, the columns of a split one after another.  More than one split: partial sums [split][rows][d_in] in part.  ops NULL: the
+// workgroups form the operands themselves, which saves a launch where the rows are few.
+template <class T, int kIn>
+constexpr int kGxWaves = kIn > 64 && sizeof(T) == 8 ? 4 : 8;
+template <class T, int kIn>
+constexpr int kGxTiles = kIn > 64 || sizeof(T) == 8 ? 1 : 2;   // 2 would not fit the registers
 
-template <class T, int KS, int kAct, bool kVec>
-__global__ void __launch_bounds__((kGxWaves<T, KS> * 64), (KS > 2 && sizeof(T) == 8 ? 1 : 2)) k_gated_gx(GatedArgs a, const u32x4* __restrict__ ops, int splits, T* part) {
+template <class T, int kIn, int kAct, bool kVec>
+__global__ void __launch_bounds__((kGxWaves<T, kIn> * 64), (kIn > 64 && sizeof(T) == 8 ? 1 : 2)) k_gated_gx(GatedArgs a, const u32x4* __restrict__ ops, int splits, T* part) {
   using N = Num<T>;
-  constexpr int R = kGxTiles<T, KS>, kUnits = N::kUnits, kOps = kOperands<KS> * kUnits, kThr = kGxWaves<T, KS> * 64, kPer = kOps * 64 / kThr, e = sizeof(T);
-  static_assert(kOps * 64 % kThr == 0, "every thread copies as much");
-  __shared__ u32x4 W[kOps][64];
-  const int t = threadIdx.x, lane = t & 63, wave = t >> 6, l16 = lane & 15, q = lane >> 4;
+  using I = In<T, kIn>;
+  using O = Operands<T, kIn>;
+  constexpr int R = kGxTiles<T, kIn>, KS = I::KS, DT = I::DT, kWaves = kGxWaves<T, kIn>, kPer = (O::kUnits + kWaves - 1) / kWaves, e = sizeof(T);
+  __shared__ u32x4 W[O::kUnits][64];
+  const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), l16 = lane & 15, q = lane >> 4;
   const int K = (int)a.d_in;
-  const int64_t n = a.d_out, steps = (n + 31) / 32, first = (int64_t)(blockIdx.x / splits) * (kGxWaves<T, KS> * R * 16) + wave * R * 16;
+  const int64_t n = a.d_out, steps = (n + 31) / 32, first = (int64_t)(blockIdx.x / splits) * (kWaves * R * 16) + wave * R * 16;
   const int64_t from = steps * (blockIdx.x % splits) / splits, end = steps * (blockIdx.x % splits + 1) / splits;
   const unsigned ldx = (unsigned)a.ld_x * e, ldo = (unsigned)a.ld_gout * e;
-  auto operand = [&](int op) {
-    typename N::Parts p;
+  auto operand_in = [&](int op) {
+    typename I::Parts p;
 #pragma unroll
-    for (int i = 0; i < kUnits; ++i) p.w[i] = W[op * kUnits + i][lane];
+    for (int i = 0; i < I::kUnits; ++i) p.w[i] = W[op * I::kUnits + i][lane];
     return p;
   };
-  // x of rows 16 r + l16, terms 32 s + 8 q + (0..7)
-  typename N::Parts xb[R][KS];
+  auto operand_out = [&](int op) {
+    typename N::Parts p;
+#pragma unroll
+    for (int i = 0; i < N::kUnits; ++i) p.w[i] = W[O::kIns * I::kUnits + op * N::kUnits + i][lane];
+    return p;
+  };
+  // x of rows 16 r + l16
+  typename I::Parts xb[R][KS];
   {
     const Buffer in = rows_of<T>(a.x, first, a.rows, a.ld_x, K);
 #pragma unroll
     for (int r = 0; r < R; ++r)
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
-        T v[8];
-        load4<kVec>(in, (r * 16 + l16) * ldx, s * 32 + q * 8, K, v);
-        load4<kVec>(in, (r * 16 + l16) * ldx, s * 32 + q * 8 + 4, K, v + 4);
-        xb[r][s] = N::parts(v);
+        T v[8] = {};
+        const int k = I::first(s, q);
+        if constexpr (I::kTerms >= 4) {
+#pragma unroll
+          for (int i = 0; i < I::kTerms; i += 4) load4<kVec>(in, (r * 16 + l16) * ldx, k + i, K, v + i);
+        } else {
+#pragma unroll
+          for (int i = 0; i < I::kTerms; ++i) v[i] = load1<T>(in, k + i < K ? (r * 16 + l16) * ldx + (k + i) * e : kNowhere);
+        }
+        xb[r][s] = I::parts(v, q, false);
       }
   }
   const Buffer go = rows_of<T>(a.gout, first, a.rows, a.ld_gout, n);
   u32x4 next[kPer];
   auto fetch = [&](int64_t step) {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) next[i] = ops[step * kOps * 64 + t + i * kThr];
+    for (int i = 0; i < kPer; ++i)
+      if (O::kUnits % kWaves == 0 || wave + i * kWaves < O::kUnits) next[i] = ops[(step * O::kUnits + wave + i * kWaves) * 64 + lane];
   };
-  typename N::Vec acc[R][KS * 2] = {};
-  fetch(from);
+  typename N::Vec acc[R][DT] = {};
+  if (ops) fetch(from);
   for (int64_t step = from; step < end; ++step) {
     T tg[R][8];
 #pragma unroll
@@ -589,10 +712,15 @@ __global__ void __launch_bounds__((kGxWaves<T, KS> * 64), (KS > 2 && sizeof(T) =
         }
       }
     __syncthreads();
+    if (ops) {
 #pragma unroll
-    for (int i = 0; i < kPer; ++i) (&W[0][0])[t + i * kThr] = next[i];
+      for (int i = 0; i < kPer; ++i)
+        if (O::kUnits % kWaves == 0 || wave + i * kWaves < O::kUnits) W[wave + i * kWaves][lane] = next[i];
+    } else {
+      for (int op = wave; op < O::kOps; op += kWaves) O::make(a, step, op, [&](int unit, u32x4 v) { W[unit][lane] = v; });
+    }
     __syncthreads();
-    if (step + 1 < end) fetch(step + 1);
+    if (ops && step + 1 < end) fetch(step + 1);
     T dg[R][8], du[R][8];
 #pragma unroll
     for (int tile = 0; tile < 2; ++tile) {
@@ -611,9 +739,9 @@ __global__ void __launch_bounds__((kGxWaves<T, KS> * 64), (KS > 2 && sizeof(T) =
       }
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
-        const typename N::Parts wg = operand(tile * KS + s), wu = operand((2 + tile) * KS + s);
-        if constexpr (R == 2) N::template mma<4>({&wg, &wu, &wg, &wu}, {&xb[0][s], &xb[0][s], &xb[1][s], &xb[1][s]}, {&g[0], &u[0], &g[1], &u[1]});
-        else N::template mma<2>({&wg, &wu}, {&xb[0][s], &xb[0][s]}, {&g[0], &u[0]});
+        const typename I::Parts wg = operand_in(tile * KS + s), wu = operand_in((2 + tile) * KS + s);
+        if constexpr (R == 2) I::template mma<4>({&wg, &wu, &wg, &wu}, {&xb[0][s], &xb[0][s], &xb[1][s], &xb[1][s]}, {&g[0], &u[0], &g[1], &u[1]});
+        else I::template mma<2>({&wg, &wu}, {&xb[0][s], &xb[0][s]}, {&g[0], &u[0]});
       }
 #pragma unroll
       for (int r = 0; r < R; ++r)
@@ -632,14 +760,25 @@ __global__ void __launch_bounds__((kGxWaves<T, KS> * 64), (KS > 2 && sizeof(T) =
       pg[r] = N::parts(dg[r]);
       pu[r] = N::parts(du[r]);
     }
+    if constexpr (DT == 1) {
+      const typename N::Parts w = operand_out(0), v = operand_out(1);
+      if constexpr (R == 2) {
+        N::template mma<2>({&w, &w}, {&pg[0], &pg[1]}, {&acc[0][0], &acc[1][0]});
+        N::template mma<2>({&v, &v}, {&pu[0], &pu[1]}, {&acc[0][0], &acc[1][0]});
+      } else {
+        N::template mma<1>({&w}, {&pg[0]}, {&acc[0][0]});
+        N::template mma<1>({&v}, {&pu[0]}, {&acc[0][0]});
+      }
+    } else {
 #pragma unroll
-    for (int d = 0; d < KS * 2; d += 2) {   // two column tiles in turn
-      const typename N::Parts w0 = operand(4 * KS + d), w1 = operand(4 * KS + d + 1);
-      if constexpr (R == 2) N::template mma<4>({&w0, &w1, &w0, &w1}, {&pg[0], &pg[0], &pg[1], &pg[1]}, {&acc[0][d], &acc[0][d + 1], &acc[1][d], &acc[1][d + 1]});
-      else N::template mma<2>({&w0, &w1}, {&pg[0], &pg[0]}, {&acc[0][d], &acc[0][d + 1]});
-      const typename N::Parts v0 = operand(6 * KS + d), v1 = operand(6 * KS + d + 1);
-      if constexpr (R == 2) N::template mma<4>({&v0, &v1, &v0, &v1}, {&pu[0], &pu[0], &pu[1], &pu[1]}, {&acc[0][d], &acc[0][d + 1], &acc[1][d], &acc[1][d + 1]});
-      else N::template mma<2>({&v0, &v1}, {&pu[0], &pu[0]}, {&acc[0][d], &acc[0][d + 1]});
+      for (int d = 0; d + 1 < DT; d += 2) {   // two column tiles in turn
+        const typename N::Parts w0 = operand_out(d), w1 = operand_out(d + 1);
+        if constexpr (R == 2) N::template mma<4>({&w0, &w1, &w0, &w1}, {&pg[0], &pg[0], &pg[1], &pg[1]}, {&acc[0][d], &acc[0][d + 1], &acc[1][d], &acc[1][d + 1]});
+        else N::template mma<2>({&w0, &w1}, {&pg[0], &pg[0]}, {&acc[0][d], &acc[0][d + 1]});
+        const typename N::Parts v0 = operand_out(DT + d), v1 = operand_out(DT + d + 1);
+        if constexpr (R == 2) N::template mma<4>({&v0, &v1, &v0, &v1}, {&pu[0], &pu[0], &pu[1], &pu[1]}, {&acc[0][d], &acc[0][d + 1], &acc[1][d], &acc[1][d + 1]});
+        else N::template mma<2>({&v0, &v1}, {&pu[0], &pu[0]}, {&acc[0][d], &acc[0][d + 1]});
+      }
     }
   }
   const unsigned ldg = (unsigned)(splits > 1 ? K : a.ld_gx) * e;
@@ -647,7 +786,7 @@ __global__ void __launch_bounds__((kGxWaves<T, KS> * 64), (KS > 2 && sizeof(T) =
 #pragma unroll
   for (int r = 0; r < R; ++r)
 #pragma unroll
-    for (int d = 0; d < KS * 2; ++d) {
+    for (int d = 0; d < DT; ++d) {
       const unsigned row = (r * 16 + l16) * ldg;
       if constexpr (kVec && e == 4) {
         const int k = d * 16 + q * 4;
@@ -661,15 +800,6 @@ __global__ void __launch_bounds__((kGxWaves<T, KS> * 64), (KS > 2 && sizeof(T) =
         }
       }
     }
-}
-
-template <class T>
-__global__ void __launch_bounds__(kThreads) k_gated_gx_sums(const T* __restrict__ part, int splits, int64_t rows, int64_t K, T* __restrict__ gx, int64_t ld) {
-  const int64_t size = rows * K, i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  if (i >= size) return;
-  T v = part[i];
-  for (int s = 1; s < splits; ++s) v += part[s * size + i];
-  gx[i / K * ld + i % K] = v;
 }
 
 // ---- more columns of x ----------------------------------------------------------------------------------------------------------
@@ -873,27 +1003,45 @@ __global__ void __launch_bounds__(kThreads, 2) k_gated_many_gw(GatedArgs a, int6
 
 constexpr int kMostUnits = 256;   // compute units that the workspace is sized for
 
-template <class T>
-int gw_waves(int64_t K) { return K > 64 ? kGwWaves<T, 4> : kGwWaves<T, 1>; }
+// f(kIn) for the least of 8, 16, 32, 64, 96, 128 columns that holds K
+template <class F>
+auto with_columns(int64_t K, F f) {
+  if (K <= 8) return f(std::integral_constant<int, 8>());
+  if (K <= 16) return f(std::integral_constant<int, 16>());
+  if (K <= 32) return f(std::integral_constant<int, 32>());
+  if (K <= 64) return f(std::integral_constant<int, 64>());
+  if (K <= 96) return f(std::integral_constant<int, 96>());
+  return f(std::integral_constant<int, 128>());
+}
 
-// How the rows are split for the weights' gradients: eight waves (fp64 with its registers: four) for each compute unit, but partial
-// sums of at most 64 MiB.
+// workgroups of four waves that a compute unit has registers for
+template <class T, int kIn>
+constexpr int kGroups = kIn <= 32 && sizeof(T) == 4 ? 3 : 2;
+
+// How the rows are split for the weights' gradients: as many workgroups as stay on the chip, but partial sums of at most 64 MiB.
 template <class T>
 int64_t gw_splits(int64_t rows, int64_t K, int64_t n, int cus) {
-  const int64_t wide = 16 * gw_waves<T>(K), cols = (n + wide - 1) / wide, blocks = (rows + kRows - 1) / kRows;
+  const int waves = with_columns(K, [](auto in) { return kGwWaves<T, decltype(in)::value>; });
+  const int groups = with_columns(K, [](auto in) { return kGroups<T, decltype(in)::value>; }) * 4 / waves;
+  const int64_t wide = 16 * waves, cols = (n + wide - 1) / wide, blocks = (rows + kRows - 1) / kRows;
   const int64_t most = std::max<int64_t>(1, ((int64_t)64 << 20) / (2 * (K + 1) * n * (int64_t)sizeof(T)));
-  return std::max<int64_t>(1, std::min({blocks, 8 / gw_waves<T>(K) * cus / cols, most}));
+  return std::max<int64_t>(1, std::min({blocks, groups * cus / cols, most}));
 }
 
-// How the columns of W are split for gx: where the rows alone leave compute units without work
+// Rows of a workgroup of k_gated_gx, and how the columns of W are split where the rows alone leave compute units without work
+template <class T>
+int64_t gx_rows(int64_t K) { return with_columns(K, [](auto in) { return kGxWaves<T, decltype(in)::value> * kGxTiles<T, decltype(in)::value> * 16; }); }
 template <class T>
 int64_t gx_splits(int64_t rows, int64_t K, int64_t n, int cus) {
-  const int64_t wide = 16 * (K > 64 ? kGxWaves<T, 4> * kGxTiles<T, 4> : kGxWaves<T, 1> * kGxTiles<T, 1>), blocks = (rows + wide - 1) / wide;
+  const int64_t blocks = (rows + gx_rows<T>(K) - 1) / gx_rows<T>(K);
   return std::max<int64_t>(1, std::min((n + 31) / 32, cus / blocks));
 }
+constexpr int64_t kFewBlocks = 4;   // up to this many blocks of rows form the operands of W themselves
 
 template <class T>
-size_t operand_bytes(int64_t K, int64_t n) { return (size_t)((n + 31) / 32 * ((K + 31) / 32) * 8 * Num<T>::kUnits * 64 * 16); }
+size_t operand_bytes(int64_t K, int64_t n) {
+  return (size_t)((n + 31) / 32) * with_columns(K, [](auto in) { return Operands<T, decltype(in)::value>::kUnits; }) * 64 * 16;
+}
 
 size_t up(size_t v) { return (v + 255) / 256 * 256; }
 
@@ -916,14 +1064,14 @@ size_t workspace_bytes(int64_t rows, int64_t K, int64_t n) {
   return 2 * up(std::min(rows, kPiece) * n * e) + up(many_splits<T>(rows, K, n, kMostUnits) * part);
 }
 
-template <class T, int KS, int NT, int kAct>
+template <class T, int kIn, int NT, int kAct>
 hipError_t launch_fwd(const GatedArgs& a, int cus, hipStream_t st) {
   const int64_t cols = (a.d_out + 64 * NT - 1) / (64 * NT), blocks = (a.rows + kRows - 1) / kRows;
-  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(blocks, 2 * cus / cols));
+  const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(blocks, kGroups<T, kIn> * cus / cols));
   const dim3 grid((unsigned)(cols * splits));
   const bool vec = a.ld_x % 4 == 0 && a.d_in % 4 == 0 && a.ld_out % 2 == 0 && a.d_out % 2 == 0;
-  if (vec) k_gated_fwd<T, KS, NT, kAct, true><<<grid, kThreads, 0, st>>>(a, (int)cols, (int)splits);
-  else k_gated_fwd<T, KS, NT, kAct, false><<<grid, kThreads, 0, st>>>(a, (int)cols, (int)splits);
+  if (vec) k_gated_fwd<T, kIn, NT, kAct, true><<<grid, kThreads, 0, st>>>(a, (int)cols, (int)splits);
+  else k_gated_fwd<T, kIn, NT, kAct, false><<<grid, kThreads, 0, st>>>(a, (int)cols, (int)splits);
   return hipGetLastError();
 }
 
@@ -939,55 +1087,42 @@ hipError_t forward_act(const GatedArgs& a, int cus, hipStream_t st) {
   }
   // 32 columns a wave where that leaves every compute unit two workgroups, else 16 (fp64 and more columns of x: 16, for the registers)
   const bool wide = sizeof(T) == 4 && (a.d_out + 127) / 128 * ((a.rows + kRows - 1) / kRows) >= 2 * cus;
-  switch ((a.d_in + 31) / 32) {
-    case 1:
-      if constexpr (sizeof(T) == 4)
-        if (wide) return launch_fwd<T, 1, 2, kAct>(a, cus, st);
-      return launch_fwd<T, 1, 1, kAct>(a, cus, st);
-    case 2:
-      if constexpr (sizeof(T) == 4)
-        if (wide) return launch_fwd<T, 2, 2, kAct>(a, cus, st);
-      return launch_fwd<T, 2, 1, kAct>(a, cus, st);
-    case 3: return launch_fwd<T, 3, 1, kAct>(a, cus, st);
-    default: return launch_fwd<T, 4, 1, kAct>(a, cus, st);
-  }
+  return with_columns(a.d_in, [&](auto in) {
+    constexpr int kIn = decltype(in)::value;
+    if constexpr (sizeof(T) == 4 && kIn <= 64)
+      if (wide) return launch_fwd<T, kIn, 2, kAct>(a, cus, st);
+    return launch_fwd<T, kIn, 1, kAct>(a, cus, st);
+  });
 }
 
 template <class T>
-hipError_t sum_splits(const GatedArgs& a, const T* part, int64_t splits, hipStream_t st) {
-  k_gated_sums<T><<<dim3((unsigned)((2 * (a.d_in + 1) * a.d_out + kThreads - 1) / kThreads)), kThreads, 0, st>>>(
-      part, (int)splits, a.d_in, a.d_out, (T*)a.gWg, (T*)a.gWu, (T*)a.gbg, (T*)a.gbu);
+hipError_t sum_splits(const GatedArgs& a, const T* part, int64_t splits, const T* gx_part, int64_t gx_splits, hipStream_t st) {
+  const int64_t size = 2 * (a.d_in + 1) * a.d_out + (gx_splits > 1 ? a.rows * a.d_in : 0);
+  k_gated_sums<T><<<dim3((unsigned)((size + kThreads - 1) / kThreads)), kThreads, 0, st>>>(a, part, (int)splits, gx_part, (int)gx_splits);
   return hipGetLastError();
 }
 
-template <class T, int KS, int kAct>
+template <class T, int kIn, int kAct>
 hipError_t launch_bwd(const GatedArgs& a, int cus, char* ws, hipStream_t st) {
-  const int64_t K = a.d_in, n = a.d_out, wide = 16 * kGwWaves<T, KS>, cols = (n + wide - 1) / wide;
-  const int64_t gws = gw_splits<T>(a.rows, K, n, cus), gxs = gx_splits<T>(a.rows, K, n, cus);
-  u32x4* ops = (u32x4*)ws;
+  const int64_t K = a.d_in, n = a.d_out, wide = 16 * kGwWaves<T, kIn>, cols = (n + wide - 1) / wide;
+  const int64_t gws = gw_splits<T>(a.rows, K, n, cus), gxs = gx_splits<T>(a.rows, K, n, cus), blocks = (a.rows + gx_rows<T>(K) - 1) / gx_rows<T>(K);
+  u32x4* ops = blocks > kFewBlocks ? (u32x4*)ws : nullptr;
   T* part = (T*)(ws + up(operand_bytes<T>(K, n)));
   T* gx_part = (T*)((char*)part + up(gw_splits<T>(a.rows, K, n, kMostUnits) * 2 * (K + 1) * n * sizeof(T)));
-  k_gated_operands<T, KS><<<dim3((unsigned)(((n + 31) / 32 * kOperands<KS> + 3) / 4)), kThreads, 0, st>>>(a, ops);
-  constexpr int kGxRows = kGxWaves<T, KS> * kGxTiles<T, KS> * 16, kGxThreads = kGxWaves<T, KS> * 64, kGwThreads = kGwWaves<T, KS> * 64;
-  const dim3 gw((unsigned)(cols * gws)), gx((unsigned)((a.rows + kGxRows - 1) / kGxRows * gxs));
+  if (ops) k_gated_operands<T, kIn><<<dim3((unsigned)(((n + 31) / 32 * Operands<T, kIn>::kOps + 3) / 4)), kThreads, 0, st>>>(a, ops);
+  constexpr int kGxThreads = kGxWaves<T, kIn> * 64, kGwThreads = kGwWaves<T, kIn> * 64;
+  const dim3 gw((unsigned)(cols * gws)), gx((unsigned)(blocks * gxs));
   const bool vec_x = a.ld_x % 4 == 0 && K % 4 == 0, vec = vec_x && a.ld_gout % 4 == 0 && n % 4 == 0 && a.ld_gx % 4 == 0;
-  if (vec) k_gated_gx<T, KS, kAct, true><<<gx, kGxThreads, 0, st>>>(a, ops, (int)gxs, gx_part);
-  else k_gated_gx<T, KS, kAct, false><<<gx, kGxThreads, 0, st>>>(a, ops, (int)gxs, gx_part);
-  if (gxs > 1) k_gated_gx_sums<T><<<dim3((unsigned)((a.rows * K + kThreads - 1) / kThreads)), kThreads, 0, st>>>(gx_part, (int)gxs, a.rows, K, (T*)a.gx, a.ld_gx);
-  if (vec_x) k_gated_gw<T, KS, kAct, true><<<gw, kGwThreads, 0, st>>>(a, (int)cols, (int)gws, part);
-  else k_gated_gw<T, KS, kAct, false><<<gw, kGwThreads, 0, st>>>(a, (int)cols, (int)gws, part);
-  return sum_splits<T>(a, part, gws, st);
+  if (vec) k_gated_gx<T, kIn, kAct, true><<<gx, kGxThreads, 0, st>>>(a, ops, (int)gxs, gx_part);
+  else k_gated_gx<T, kIn, kAct, false><<<gx, kGxThreads, 0, st>>>(a, ops, (int)gxs, gx_part);
+  if (vec_x) k_gated_gw<T, kIn, kAct, true><<<gw, kGwThreads, 0, st>>>(a, (int)cols, (int)gws, part);
+  else k_gated_gw<T, kIn, kAct, false><<<gw, kGwThreads, 0, st>>>(a, (int)cols, (int)gws, part);
+  return sum_splits<T>(a, part, gws, gx_part, gxs, st);
 }
 
 template <class T, int kAct>
 hipError_t backward_act(const GatedArgs& a, int cus, char* ws, hipStream_t st) {
-  switch ((a.d_in + 31) / 32) {
-    case 1: return launch_bwd<T, 1, kAct>(a, cus, ws, st);
-    case 2: return launch_bwd<T, 2, kAct>(a, cus, ws, st);
-    case 3: return launch_bwd<T, 3, kAct>(a, cus, ws, st);
-    case 4: return launch_bwd<T, 4, kAct>(a, cus, ws, st);
-    default: break;
-  }
+  if (a.d_in <= kMaxIn) return with_columns(a.d_in, [&](auto in) { return launch_bwd<T, decltype(in)::value, kAct>(a, cus, ws, st); });
   const int64_t K = a.d_in, n = a.d_out, splits = many_splits<T>(a.rows, K, n, cus);
   const int64_t ct = (n + 63) / 64, kt = (K + 63) / 64, gt = (n + 32 * kManyCols<T> - 1) / (32 * kManyCols<T>);
   T* dg = (T*)ws;
@@ -999,7 +1134,7 @@ hipError_t backward_act(const GatedArgs& a, int cus, char* ws, hipStream_t st) {
     k_gated_many_gx<T><<<dim3((unsigned)(rb * kt)), kThreads, 0, st>>>(a, r, rows, dg, du);
     k_gated_many_gw<T><<<dim3((unsigned)(gt * kt * splits)), kThreads, 0, st>>>(a, r, rows, dg, du, (int)splits, part, r > 0);
   }
-  return sum_splits<T>(a, part, splits, st);
+  return sum_splits<T>(a, part, splits, nullptr, 1, st);
 }
 
 template <class T>

@@ -58,7 +58,7 @@ def compare(o, p, prec, act, what):
 
 # one of everything, around the tiles' edges, and the widths of this library's plans
 SIZES = [(1, 1, 1), (2, 64, 544), (1, 8, 24), (5, 3, 2), (31, 16, 33), (33, 8, 17), (64, 64, 64), (65, 37, 301), (243, 8, 160), (300, 64, 96),
-         (129, 130, 65), (64, 256, 33), (1000, 16, 130), (31, 128, 127), (257, 5, 64), (128, 200, 7), (97, 129, 40), (1030, 64, 31), (8300, 136, 40), (300, 96, 100), (2100, 70, 129), (700, 33, 270)]
+         (129, 130, 65), (64, 256, 33), (1000, 16, 130), (31, 128, 127), (257, 5, 64), (128, 200, 7), (97, 129, 40), (1030, 64, 31), (8300, 136, 40), (300, 96, 100), (2100, 70, 129), (700, 33, 270), (2000, 8, 70), (1500, 5, 33), (90, 16, 48), (5000, 12, 20), (33, 10, 100), (1300, 20, 64)]
 
 
 @pytest.mark.parametrize("prec", ["f32", "f64"])
@@ -71,7 +71,7 @@ def test_against_the_oracle(rows, k, n, prec):
 
 @pytest.mark.parametrize("prec", ["f32", "f64"])
 @pytest.mark.parametrize("act", [layer.NONE, layer.GELU, layer.SIGMOID, layer.TANH])
-@pytest.mark.parametrize("k", [20, 40, 80, 110, 140])
+@pytest.mark.parametrize("k", [7, 14, 20, 40, 80, 110, 140])
 def test_activations(k, act, prec):
     p = inputs(70, k, 50, prec, True, seed=act)
     compare(run(p, prec, act, True), p, prec, act, f"act {act}")
