@@ -635,11 +635,12 @@ __global__ void __launch_bounds__(kThreads) k_gated_operands(GatedArgs a, u32x4*
   O::make(a, step, (int)(e % O::kOps), [&](int unit, u32x4 v) { to[(step * O::kUnits + unit) * 64 + (threadIdx.x & 63)] = v; });
 }
 
-// gx of 16 R rows a wave: the operands of 32 columns of W at a time in LDS for the eight (fp64 of more than 64 columns of x: four) waves
-// of a workgroup, the columns of a split one after another.  More than one split: partial sums [split][rows][d_in] in part.  ops NULL: the
+// gx of 16 R rows a wave: the operands of 32 columns of W at a time in LDS for the waves of a workgroup, the columns of a split one after
+// another.  Four waves, so that two workgroups of a compute unit are in different phases (160 710 x 64 x 2176, all of backward 2.01 ms, with
+// eight 2.12); eight in fp32 of more than 64 columns of x, whose operands fill the LDS for one workgroup (50 000 x 128 x 2176 1.46 ms, with four 1.91).  More than one split: partial sums [split][rows][d_in] in part.  ops NULL: the
 // workgroups form the operands themselves, which saves a launch where the rows are few.
 template <class T, int kIn>
-constexpr int kGxWaves = kIn > 64 && sizeof(T) == 8 ? 4 : 8;
+constexpr int kGxWaves = kIn > 64 && sizeof(T) == 4 ? 8 : 4;
 template <class T, int kIn>
 constexpr int kGxTiles = kIn > 64 || sizeof(T) == 8 ? 1 : 2;   // 2 would not fit the registers
 
