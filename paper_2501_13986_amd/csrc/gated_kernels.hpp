@@ -190,17 +190,23 @@ __device__ inline typename Num<T>::Parts column_parts(Buffer W, int64_t n, int64
 template <class T>
 __device__ inline T bias_of(const void* b, int64_t c, int64_t n) { return b ? ((const T*)b)[c < n ? c : n - 1] : T(0); }
 
-// kR rows of kC columns in LDS, as operands with the columns as terms.  A row is padded by 16 bytes, so that 16 rows' 16 bytes fill
-// all banks once.
+// kR rows of kC columns in LDS, as operands with the columns as terms.  A wave reads 16 bytes of each of 16 rows: they have to lie on different banks
+// (256 bytes in all).  fp32 of 64 columns: the 16 bytes of a row change places by an exclusive or with the row's number, in
+// which also the lanes that write 4 x 4 blocks (write_both) find different ones; others: rows are padded by 16 bytes.
 template <class T, int kR, int kC>
 struct Tile;
 template <int kR, int kC>
 struct Tile<float, kR, kC> {
-  __bf16 v[3][kR][kC + 8];
+  static constexpr bool turned = kC == 64;
+  __bf16 v[3][kR][turned ? kC : kC + 8];
+  static __device__ int at(int r, int c) {
+    if constexpr (kC == 64) return c ^ ((r >> 1 ^ r >> 4 << 2) & 7) * 8;
+    else return c;
+  }
   __device__ PartsOf<3> read(int r, int c) const {
     PartsOf<3> p;
 #pragma unroll
-    for (int i = 0; i < 3; ++i) p.w[i] = *(const u32x4*)&v[i][r][c];
+    for (int i = 0; i < 3; ++i) p.w[i] = *(const u32x4*)&v[i][r][at(r, c)];
     return p;
   }
   __device__ void write4(int r, int c, const float* x) {
@@ -208,7 +214,7 @@ struct Tile<float, kR, kC> {
     Num<float>::split(x[0], x[1], lo);
     Num<float>::split(x[2], x[3], hi);
 #pragma unroll
-    for (int p = 0; p < 3; ++p) *(u32x2*)&v[p][r][c] = u32x2{lo[p], hi[p]};
+    for (int p = 0; p < 3; ++p) *(u32x2*)&v[p][r][at(r, c)] = u32x2{lo[p], hi[p]};
   }
 };
 template <int kR, int kC>
@@ -324,12 +330,12 @@ __device__ inline void write_both(Tile<float, kRows, KC>& X, Tile<float, KD, kRo
 #pragma unroll
   for (int p = 0; p < 3; ++p) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) *(u32x2*)&X.v[p][r4 * 4 + j][k4] = u32x2{row[j][0][p], row[j][1][p]};
+    for (int j = 0; j < 4; ++j) *(u32x2*)&X.v[p][r4 * 4 + j][X.at(r4 * 4 + j, k4)] = u32x2{row[j][0][p], row[j][1][p]};
 #pragma unroll
     for (int w = 0; w < 2; ++w) {   // halves of the words of two rows
       const unsigned a = row[0][w][p], b = row[1][w][p], c = row[2][w][p], d = row[3][w][p];
-      *(u32x2*)&XT.v[p][k4 + 2 * w][at] = u32x2{__builtin_amdgcn_perm(b, a, 0x05040100), __builtin_amdgcn_perm(d, c, 0x05040100)};
-      *(u32x2*)&XT.v[p][k4 + 2 * w + 1][at] = u32x2{__builtin_amdgcn_perm(b, a, 0x07060302), __builtin_amdgcn_perm(d, c, 0x07060302)};
+      *(u32x2*)&XT.v[p][k4 + 2 * w][XT.at(k4 + 2 * w, at)] = u32x2{__builtin_amdgcn_perm(b, a, 0x05040100), __builtin_amdgcn_perm(d, c, 0x05040100)};
+      *(u32x2*)&XT.v[p][k4 + 2 * w + 1][XT.at(k4 + 2 * w + 1, at)] = u32x2{__builtin_amdgcn_perm(b, a, 0x07060302), __builtin_amdgcn_perm(d, c, 0x07060302)};
     }
   }
 }
@@ -470,8 +476,9 @@ __global__ void __launch_bounds__((kGwWaves<T, kIn> * 64), (sizeof(T) == 8 && kI
   auto block = [&](int i, int& r4, int& k4) {
     const int p = t + i * kThr < kBlocks ? t + i * kThr : kBlocks - 1;
     constexpr int kSide = kQuads < 4 ? kQuads : 4;      // quads side by side
-    r4 = p % 4 + p / (4 * kSide) % 4 * 4;
-    k4 = (p / 4 % kSide + p / (16 * kSide) * 4) * 4;
+    const int u = p / (4 * kSide);
+    r4 = (p & 1) | (u & 1) << 1 | (p >> 1 & 1) << 2 | (u >> 1 & 1) << 3;
+    k4 = (p / 4 % kSide + u / 4 * 4) * 4;
   };
   T next[kPer][4][4];
   auto fetch = [&](int64_t b) {
