@@ -888,21 +888,22 @@ __global__ void __launch_bounds__(kThreads, 2) k_gated_many(GatedArgs a, int64_t
   }
 }
 
-// gx = dg Wg^T + du Wu^T of a piece of rows: 64 columns of x a workgroup
+// gx = dg Wg^T + du Wu^T of a piece of rows: 64 columns of x a workgroup.  More than one split (of the columns of Wg, then Wu): partial sums
+// [split][rows][d_in] in part.
 template <class T>
-__global__ void __launch_bounds__(kThreads, 2) k_gated_many_gx(GatedArgs a, int64_t row0, int64_t rows, const T* dg, const T* du) {
+__global__ void __launch_bounds__(kThreads, 2) k_gated_many_gx(GatedArgs a, int64_t row0, int64_t rows, const T* dg, const T* du, int splits, T* part) {
   using N = Num<T>;
   constexpr int kTiles = kManyRows<T> / 16, e = sizeof(T);
   __shared__ ManyRows<T> S;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, q = lane >> 4;
-  const int64_t n = a.d_out, K = a.d_in, tiles = (K + 63) / 64, first = blockIdx.x / tiles * kManyRows<T>, k0 = blockIdx.x % tiles * 64;
+  const int64_t n = a.d_out, K = a.d_in, tiles = (K + 63) / 64, block = blockIdx.x / splits, first = block / tiles * kManyRows<T>, k0 = block % tiles * 64;
   const int k = wave * 16 + l16;      // behind k0; rows of W beyond the last are out of the descriptors' range
   const Buffer Wg = matrix_of<T>(a.Wg, k0, K - k0 < 64 ? K - k0 : 64, n), Wu = matrix_of<T>(a.Wu, k0, K - k0 < 64 ? K - k0 : 64, n);
-  const int64_t steps = (n + 31) / 32;
+  const int64_t steps = (n + 31) / 32, split = blockIdx.x % splits, from = 2 * steps * split / splits, end = 2 * steps * (split + 1) / splits;
   typename N::Vec acc[kTiles] = {};
   T next[ManyRows<T>::kPer][4];
-  S.fetch(dg, first, rows, n, n, 0, next);
-  for (int64_t s = 0; s < 2 * steps; ++s) {
+  S.fetch(from < steps ? dg : du, first, rows, n, n, from % steps * 32, next);
+  for (int64_t s = from; s < end; ++s) {
     T v[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
@@ -913,7 +914,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_gated_many_gx(GatedArgs a, int6
     __syncthreads();
     S.put(next);
     __syncthreads();
-    if (s + 1 < 2 * steps) S.fetch(s + 1 < steps ? dg : du, first, rows, n, n, (s + 1) % steps * 32, next);
+    if (s + 1 < end) S.fetch(s + 1 < steps ? dg : du, first, rows, n, n, (s + 1) % steps * 32, next);
 #pragma unroll
     for (int rt = 0; rt < kTiles; rt += 2) {
       const typename N::Parts x0 = S.X.read(rt * 16 + l16, q * 8), x1 = S.X.read(rt * 16 + 16 + l16, q * 8);
@@ -922,13 +923,14 @@ __global__ void __launch_bounds__(kThreads, 2) k_gated_many_gx(GatedArgs a, int6
   }
 #pragma unroll
   for (int h = 0; h < kTiles; h += 4) {
-    const Buffer to = rows_of<T>((T*)a.gx + row0 * a.ld_gx, first + h * 16, rows, a.ld_gx, K);
+    const int64_t ld = splits > 1 ? K : a.ld_gx;
+    const Buffer to = rows_of<T>(splits > 1 ? part + split * rows * K : (T*)a.gx + row0 * a.ld_gx, first + h * 16, rows, ld, K);
 #pragma unroll
     for (int rt = 0; rt < 4; ++rt)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const T v = acc[h + rt][i];
-        store1(v, to, k0 + k < K ? (rt * 16 + N::row(q, i)) * (unsigned)(a.ld_gx * e) + (unsigned)(k0 + k) * e : kNowhere);
+        store1(v, to, k0 + k < K ? (rt * 16 + N::row(q, i)) * (unsigned)(ld * e) + (unsigned)(k0 + k) * e : kNowhere);
       }
   }
 }
@@ -1062,6 +1064,13 @@ int64_t many_splits(int64_t rows, int64_t K, int64_t n, int cus) {
   return std::max<int64_t>(1, std::min({(steps + 7) / 8, 2 * cus / tiles, most}));
 }
 
+// splits of k_gated_many_gx: where one piece of rows leaves compute units without work
+template <class T>
+int64_t many_gx_splits(int64_t rows, int64_t K, int64_t n, int cus) {
+  const int64_t blocks = (rows + kManyRows<T> - 1) / kManyRows<T> * ((K + 63) / 64);
+  return rows > kPiece ? 1 : std::max<int64_t>(1, std::min(2 * ((n + 31) / 32), cus / blocks));
+}
+
 template <class T>
 size_t workspace_bytes(int64_t rows, int64_t K, int64_t n) {
   const size_t e = sizeof(T), part = 2 * (K + 1) * n * e;
@@ -1069,7 +1078,8 @@ size_t workspace_bytes(int64_t rows, int64_t K, int64_t n) {
     const int64_t gx = gx_splits<T>(rows, K, n, kMostUnits);
     return up(operand_bytes<T>(K, n)) + up(gw_splits<T>(rows, K, n, kMostUnits) * part) + (gx > 1 ? up(gx * rows * K * e) : 0);
   }
-  return 2 * up(std::min(rows, kPiece) * n * e) + up(many_splits<T>(rows, K, n, kMostUnits) * part);
+  const int64_t gx = many_gx_splits<T>(rows, K, n, kMostUnits);
+  return 2 * up(std::min(rows, kPiece) * n * e) + up(many_splits<T>(rows, K, n, kMostUnits) * part) + (gx > 1 ? up(gx * rows * K * e) : 0);
 }
 
 template <class T, int kIn, int NT, int kAct>
@@ -1136,13 +1146,15 @@ hipError_t backward_act(const GatedArgs& a, int cus, char* ws, hipStream_t st) {
   T* dg = (T*)ws;
   T* du = (T*)(ws + up(std::min(a.rows, kPiece) * n * sizeof(T)));
   T* part = (T*)((char*)du + up(std::min(a.rows, kPiece) * n * sizeof(T)));
+  T* gx_part = (T*)((char*)part + up(many_splits<T>(a.rows, K, n, kMostUnits) * 2 * (K + 1) * n * sizeof(T)));
+  const int64_t gxs = many_gx_splits<T>(a.rows, K, n, cus);
   for (int64_t r = 0; r < a.rows; r += kPiece) {
     const int64_t rows = std::min(kPiece, a.rows - r), rb = (rows + kManyRows<T> - 1) / kManyRows<T>;
     k_gated_many<T, kAct, true><<<dim3((unsigned)(rb * ct)), kThreads, 0, st>>>(a, r, rows, dg, du);
-    k_gated_many_gx<T><<<dim3((unsigned)(rb * kt)), kThreads, 0, st>>>(a, r, rows, dg, du);
+    k_gated_many_gx<T><<<dim3((unsigned)(rb * kt * gxs)), kThreads, 0, st>>>(a, r, rows, dg, du, (int)gxs, gx_part);
     k_gated_many_gw<T><<<dim3((unsigned)(gt * kt * splits)), kThreads, 0, st>>>(a, r, rows, dg, du, (int)splits, part, r > 0);
   }
-  return sum_splits<T>(a, part, splits, nullptr, 1, st);
+  return sum_splits<T>(a, part, splits, gx_part, gxs, st);
 }
 
 template <class T>
