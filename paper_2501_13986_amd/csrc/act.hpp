@@ -14,6 +14,16 @@ namespace cgtp {
 __device__ inline float act_sigmoid(float t) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(t * -1.44269502f)); }
 __device__ inline double act_sigmoid(double t) { return 1.0 / (1.0 + exp(-t)); }
 
+// fp32: 1 - 2 / (1 + exp(2 |t|)), and near zero, where that loses bits, five terms of the series (the sixth is below 2^-27 of the result
+// there).  Without branches: kernels whose registers overflow must not have lane-conditional code.
+__device__ inline float act_tanh(float t) {
+  const float s = t * t, x = __builtin_fabsf(t);
+  const float p = t + t * s * (-0.333333333f + s * (0.133333333f + s * (-0.0539682540f + s * 0.0218694885f)));
+  const float q = 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * 2.88539008f));
+  return x < 0.25f ? p : __builtin_copysignf(q, t);
+}
+__device__ inline double act_tanh(double t) { return tanh(t); }
+
 // a = act(t) and d = act'(t)
 template <int kAct, class T>
 __device__ inline void act_both(T t, T& a, T& d) {
@@ -32,7 +42,7 @@ __device__ inline void act_both(T t, T& a, T& d) {
     a = act_sigmoid(t);
     d = a * (T(1) - a);
   } else {
-    a = tanh(t);
+    a = act_tanh(t);
     d = T(1) - a * a;
   }
 }

@@ -15,6 +15,8 @@ namespace {
 
 const char kShared[] = R"HIP(
 typedef long long i64;
+__device__ inline float fma_(float a, float b, float c) { return __builtin_fmaf(a, b, c); }
+__device__ inline double fma_(double a, double b, double c) { return __builtin_fma(a, b, c); }
 // off by |t| half steps where t is negative: at most 0.3 half steps of 1
 __device__ inline float sigmoid_(float t) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(t * -1.44269502f)); }
 __device__ inline double sigmoid_(double t) { return 1.0 / (1.0 + exp(-t)); }
@@ -22,12 +24,16 @@ __device__ inline float erfc_(float t) { return erfcf(t); }
 __device__ inline double erfc_(double t) { return erfc(t); }
 __device__ inline float exp_(float t) { return expf(t); }
 __device__ inline double exp_(double t) { return exp(t); }
-__device__ inline float tanh_(float t) { return tanhf(t); }
+// 1 - 2 / (1 + exp(2 |t|)), near zero five terms of the series
+__device__ inline float tanh_(float t) {
+  const float s = t * t, x = __builtin_fabsf(t);
+  const float p = fma_(t * s, fma_(s, fma_(s, fma_(s, 0.0218694885f, -0.0539682540f), 0.133333333f), -0.333333333f), t);
+  const float q = 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * 2.88539008f));
+  return x < 0.25f ? p : __builtin_copysignf(q, t);
+}
 __device__ inline double tanh_(double t) { return tanh(t); }
 __device__ inline float sqrt_(float t) { return sqrtf(t); }
 __device__ inline double sqrt_(double t) { return sqrt(t); }
-__device__ inline float fma_(float a, float b, float c) { return __builtin_fmaf(a, b, c); }
-__device__ inline double fma_(double a, double b, double c) { return __builtin_fma(a, b, c); }
 
 // activation and derivative
 __device__ inline void act_(T t, T& a, T& d) {

@@ -447,21 +447,24 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 8 && kIn > 64 ? 1 : 2)
 // but those are twice the size of gout, written once and read twice.
 
 // gWg, gWu, gbg, gbu of 16 columns a wave, over the row blocks of a split; partial sums [split][Wg; bg; Wu; bu]
+constexpr int kGwWaves = 4;
+// whether a wave needs the registers of two: fp64, and from 65 columns of x on (20 011 x 128 x 301, forward and backward 214 us, with two waves that
+// keep what does not fit in private memory 230)
 template <class T, int kIn>
-constexpr int kGwWaves = kIn > 64 && sizeof(T) == 4 ? 8 : 4;   // eight where the rows in LDS leave room for one workgroup only
+constexpr bool kGwAlone = kIn > (sizeof(T) == 8 ? 32 : 64);
 
 template <class T, int kIn, int kAct, bool kVec>
-__global__ void __launch_bounds__((kGwWaves<T, kIn> * 64), (sizeof(T) == 8 && kIn > 32 ? 1 : 2)) k_gated_gw(GatedArgs a, int col_tiles, int splits, T* part) {
+__global__ void __launch_bounds__((kGwWaves * 64), (kGwAlone<T, kIn> ? 1 : 2)) k_gated_gw(GatedArgs a, int col_tiles, int splits, T* part) {
   using N = Num<T>;
   using I = In<T, kIn>;
   constexpr int KS = I::KS, DT = I::DT, e = sizeof(T);
   __shared__ Tile<T, kRows, kIn> X;
   __shared__ Tile<T, DT * 16, kRows> XT;      // with 8 columns of x the other half holds anything: sums that are not kept
   // blocks of 4 rows x 4 columns of x; lanes without one of their own repeat the last, waves without any do nothing
-  constexpr int kQuads = kIn / 4, kBlocks = kRows / 4 * kQuads, kThr = kGwWaves<T, kIn> * 64, kPer = (kBlocks + kThr - 1) / kThr;
+  constexpr int kQuads = kIn / 4, kBlocks = kRows / 4 * kQuads, kThr = kGwWaves * 64, kPer = (kBlocks + kThr - 1) / kThr;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6, l16 = lane & 15, q = lane >> 4;
   const int K = (int)a.d_in;
-  const int64_t n = a.d_out, c = ((int64_t)(blockIdx.x % col_tiles) * kGwWaves<T, kIn> + wave) * 16 + l16;
+  const int64_t n = a.d_out, c = ((int64_t)(blockIdx.x % col_tiles) * kGwWaves + wave) * 16 + l16;
   const unsigned ldx = (unsigned)a.ld_x * e, ldo = (unsigned)a.ld_gout * e;
   const Buffer Wg = matrix_of<T>(a.Wg, 0, K, n), Wu = matrix_of<T>(a.Wu, 0, K, n);
   typename I::Parts wg[KS], wu[KS];
@@ -579,9 +582,13 @@ __global__ void __launch_bounds__(kThreads) k_gated_sums(GatedArgs a, const T* _
   const int64_t K = a.d_in, n = a.d_out, size = 2 * (K + 1) * n, gx_size = gx_splits > 1 ? a.rows * K : 0;
   int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
   auto total = [&](const T* p, int m, int64_t of) {
-    T v = p[i];
-    for (int s = 1; s < m; ++s) v += p[s * of + i];
-    return v;
+    T v[8] = {};
+    int s = 0;
+    for (; s + 8 <= m; s += 8)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += p[(s + j) * of + i];
+    for (; s < m; ++s) v[0] += p[s * of + i];
+    return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
   };
   if (i < size) {
     const T v = total(part, splits, size);
@@ -1031,9 +1038,8 @@ constexpr int kGroups = kIn <= 32 && sizeof(T) == 4 ? 3 : 2;
 // How the rows are split for the weights' gradients: as many workgroups as stay on the chip, but partial sums of at most 64 MiB.
 template <class T>
 int64_t gw_splits(int64_t rows, int64_t K, int64_t n, int cus) {
-  const int waves = with_columns(K, [](auto in) { return kGwWaves<T, decltype(in)::value>; });
-  const int groups = with_columns(K, [](auto in) { return kGroups<T, decltype(in)::value>; }) * 4 / waves;
-  const int64_t wide = 16 * waves, cols = (n + wide - 1) / wide, blocks = (rows + kRows - 1) / kRows;
+  const int groups = with_columns(K, [](auto in) { return kGwAlone<T, decltype(in)::value> ? 1 : kGroups<T, decltype(in)::value>; });
+  const int64_t wide = 16 * kGwWaves, cols = (n + wide - 1) / wide, blocks = (rows + kRows - 1) / kRows;
   const int64_t most = std::max<int64_t>(1, ((int64_t)64 << 20) / (2 * (K + 1) * n * (int64_t)sizeof(T)));
   return std::max<int64_t>(1, std::min({blocks, groups * cus / cols, most}));
 }
@@ -1043,8 +1049,8 @@ template <class T>
 int64_t gx_rows(int64_t K) { return with_columns(K, [](auto in) { return kGxWaves<T, decltype(in)::value> * kGxTiles<T, decltype(in)::value> * 16; }); }
 template <class T>
 int64_t gx_splits(int64_t rows, int64_t K, int64_t n, int cus) {
-  const int64_t blocks = (rows + gx_rows<T>(K) - 1) / gx_rows<T>(K);
-  return std::max<int64_t>(1, std::min((n + 31) / 32, cus / blocks));
+  const int64_t blocks = (rows + gx_rows<T>(K) - 1) / gx_rows<T>(K), room = (K > 64 ? 1 : 2) * cus;
+  return std::max<int64_t>(1, std::min((n + 31) / 32, room / blocks));
 }
 constexpr int64_t kFewBlocks = 4;   // up to this many blocks of rows form the operands of W themselves
 
@@ -1122,13 +1128,13 @@ hipError_t sum_splits(const GatedArgs& a, const T* part, int64_t splits, const T
 
 template <class T, int kIn, int kAct>
 hipError_t launch_bwd(const GatedArgs& a, int cus, char* ws, hipStream_t st) {
-  const int64_t K = a.d_in, n = a.d_out, wide = 16 * kGwWaves<T, kIn>, cols = (n + wide - 1) / wide;
+  const int64_t K = a.d_in, n = a.d_out, wide = 16 * kGwWaves, cols = (n + wide - 1) / wide;
   const int64_t gws = gw_splits<T>(a.rows, K, n, cus), gxs = gx_splits<T>(a.rows, K, n, cus), blocks = (a.rows + gx_rows<T>(K) - 1) / gx_rows<T>(K);
   u32x4* ops = blocks > kFewBlocks ? (u32x4*)ws : nullptr;
   T* part = (T*)(ws + up(operand_bytes<T>(K, n)));
   T* gx_part = (T*)((char*)part + up(gw_splits<T>(a.rows, K, n, kMostUnits) * 2 * (K + 1) * n * sizeof(T)));
   if (ops) k_gated_operands<T, kIn><<<dim3((unsigned)(((n + 31) / 32 * Operands<T, kIn>::kOps + 3) / 4)), kThreads, 0, st>>>(a, ops);
-  constexpr int kGxThreads = kGxWaves<T, kIn> * 64, kGwThreads = kGwWaves<T, kIn> * 64;
+  constexpr int kGxThreads = kGxWaves<T, kIn> * 64, kGwThreads = kGwWaves * 64;
   const dim3 gw((unsigned)(cols * gws)), gx((unsigned)(blocks * gxs));
   const bool vec_x = a.ld_x % 4 == 0 && K % 4 == 0, vec = vec_x && a.ld_gout % 4 == 0 && n % 4 == 0 && a.ld_gx % 4 == 0;
   if (vec) k_gated_gx<T, kIn, kAct, true><<<gx, kGxThreads, 0, st>>>(a, ops, (int)gxs, gx_part);

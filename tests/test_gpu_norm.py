@@ -59,7 +59,8 @@ GRAPHS = [None, [0, 27], [0, 1, 1, 3, 40, 41], [2, 2, 9, 35], [0, 0]]
 @pytest.mark.parametrize("ir_mul", [False, True])
 @pytest.mark.parametrize("irreps,groups", IRREPS)
 def test_against_the_oracle(irreps, groups, ir_mul, prec):
-    for gated in (True, False):
+    # without gates in one layout each (a normalisation takes seconds to compile where its code is not cached)
+    for gated in (True, False) if (IRREPS.index((irreps, groups)) % 2 == 0) == ir_mul and prec == "f32" else (True,):
         n = handle(irreps, groups, layer.SILU, gated, prec, ir_mul)
         for i, ptr in enumerate(GRAPHS):
             N = 41 if ptr is not None else 37
