@@ -641,10 +641,11 @@ template <bool kLong> struct GraphFwd {
     typedef Lane<s> A;
     const A a(phase);
     Param p[A::C];
-    a.params(weight, bias, p);
+    if (!kLong) a.params(weight, bias, p);
     Chunks of = in;
     of.all(kLong /* what the first kernel read last is still near */, [&] { of.each([&](i64 sample, i64 r0, i64 r1, i64 from, i64 to, int slot) {
       if (kLong && slot < 0) return;
+      if (kLong) a.params(weight, bias, p);     // most workgroups find nothing long
       const i64 first = from + (threadIdx.x / 64) * A::RP;
       i64 base = first;
       T v[A::C * A::n], g[A::C];
@@ -706,12 +707,13 @@ template <bool kLong> struct GraphBwd {
     typedef Lane<s> A;
     const A a(phase);
     Param p[A::C];
-    a.params(weight, bias, p);
+    if (!kLong) a.params(weight, bias, p);
     typename A::Sum sum = {};
     bool any = false;
     Chunks of = in;
     of.all(kLong, [&] { of.each([&](i64 sample, i64 r0, i64 r1, i64 from, i64 to, int slot) {
       if (kLong && slot < 0) return;
+      if (kLong) a.params(weight, bias, p);     // most workgroups find nothing long
       const i64 first = from + (threadIdx.x / 64) * A::RP;
       i64 base = first;
       any = true;
