@@ -580,8 +580,7 @@ __global__ void __launch_bounds__((kGwWaves * 64), (kGwAlone<T, kIn> ? 1 : 2)) k
 template <class T>
 __global__ void __launch_bounds__(kThreads) k_gated_sums(GatedArgs a, const T* __restrict__ part, int splits, const T* __restrict__ gx_part, int gx_splits) {
   const int64_t K = a.d_in, n = a.d_out, size = 2 * (K + 1) * n, gx_size = gx_splits > 1 ? a.rows * K : 0;
-  int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  auto total = [&](const T* p, int m, int64_t of) {
+  auto total = [](const T* p, int m, int64_t of, int64_t i) {
     T v[8] = {};
     int s = 0;
     for (; s + 8 <= m; s += 8)
@@ -590,17 +589,19 @@ __global__ void __launch_bounds__(kThreads) k_gated_sums(GatedArgs a, const T* _
     for (; s < m; ++s) v[0] += p[s * of + i];
     return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
   };
-  if (i < size) {
-    const T v = total(part, splits, size);
-    const int64_t row = i / n, c = i % n;
-    if (row < K) ((T*)a.gWg)[i] = v;
-    else if (row == K) { if (a.gbg) ((T*)a.gbg)[c] = v; }
-    else if (row <= 2 * K) ((T*)a.gWu)[i - (K + 1) * n] = v;
-    else if (a.gbu) ((T*)a.gbu)[c] = v;
-    return;
+  for (int64_t at = (int64_t)blockIdx.x * kThreads + threadIdx.x; at < size + gx_size; at += (int64_t)gridDim.x * kThreads) {
+    if (at < size) {
+      const T v = total(part, splits, size, at);
+      const int64_t row = at / n, c = at % n;
+      if (row < K) ((T*)a.gWg)[at] = v;
+      else if (row == K) { if (a.gbg) ((T*)a.gbg)[c] = v; }
+      else if (row <= 2 * K) ((T*)a.gWu)[at - (K + 1) * n] = v;
+      else if (a.gbu) ((T*)a.gbu)[c] = v;
+    } else {
+      const int64_t i = at - size;
+      ((T*)a.gx)[i / K * a.ld_gx + i % K] = total(gx_part, gx_splits, gx_size, i);
+    }
   }
-  i -= size;
-  if (i < gx_size) ((T*)a.gx)[i / K * a.ld_gx + i % K] = total(gx_part, gx_splits, gx_size);
 }
 
 // The operands of W that gx needs for 32 of its columns, in units of 16 bytes a lane.  First 4 KS for g and u: (g, u) x tile x s, lane:
@@ -1019,6 +1020,7 @@ __global__ void __launch_bounds__(kThreads, 2) k_gated_many_gw(GatedArgs a, int6
 // ---- launches -----------------------------------------------------------------------------------------------------------------------
 
 constexpr int kMostUnits = 256;   // compute units that the workspace is sized for
+constexpr int64_t kMostGroups = (int64_t)1 << 22;   // workgroups of a launch: 2^32 threads are too many
 
 // f(kIn) for the least of 8, 16, 32, 64, 96, 128 columns that holds K
 template <class F>
@@ -1102,7 +1104,7 @@ hipError_t launch_fwd(const GatedArgs& a, int cus, hipStream_t st) {
 template <class T, int kAct>
 hipError_t forward_act(const GatedArgs& a, int cus, hipStream_t st) {
   if (a.d_in > kMaxIn) {
-    const int64_t tiles = (a.d_out + 63) / 64, most = std::max<int64_t>(1, ((int64_t)1 << 22) / tiles) * kManyRows<T>;   // rows of a launch
+    const int64_t tiles = (a.d_out + 63) / 64, most = std::max<int64_t>(1, kMostGroups / tiles) * kManyRows<T>;   // rows of a launch
     for (int64_t r = 0; r < a.rows; r += most) {
       const int64_t rows = std::min(a.rows - r, most);
       k_gated_many<T, kAct, false><<<dim3((unsigned)((rows + kManyRows<T> - 1) / kManyRows<T> * tiles)), kThreads, 0, st>>>(a, r, rows, (T*)nullptr, (T*)nullptr);
@@ -1122,7 +1124,7 @@ hipError_t forward_act(const GatedArgs& a, int cus, hipStream_t st) {
 template <class T>
 hipError_t sum_splits(const GatedArgs& a, const T* part, int64_t splits, const T* gx_part, int64_t gx_splits, hipStream_t st) {
   const int64_t size = 2 * (a.d_in + 1) * a.d_out + (gx_splits > 1 ? a.rows * a.d_in : 0);
-  k_gated_sums<T><<<dim3((unsigned)((size + kThreads - 1) / kThreads)), kThreads, 0, st>>>(a, part, (int)splits, gx_part, (int)gx_splits);
+  k_gated_sums<T><<<dim3((unsigned)std::min((size + kThreads - 1) / kThreads, kMostGroups)), kThreads, 0, st>>>(a, part, (int)splits, gx_part, (int)gx_splits);
   return hipGetLastError();
 }
 
@@ -1135,10 +1137,19 @@ hipError_t launch_bwd(const GatedArgs& a, int cus, char* ws, hipStream_t st) {
   T* gx_part = (T*)((char*)part + up(gw_splits<T>(a.rows, K, n, kMostUnits) * 2 * (K + 1) * n * sizeof(T)));
   if (ops) k_gated_operands<T, kIn><<<dim3((unsigned)(((n + 31) / 32 * Operands<T, kIn>::kOps + 3) / 4)), kThreads, 0, st>>>(a, ops);
   constexpr int kGxThreads = kGxWaves<T, kIn> * 64, kGwThreads = kGwWaves * 64;
-  const dim3 gw((unsigned)(cols * gws)), gx((unsigned)(blocks * gxs));
+  const dim3 gw((unsigned)(cols * gws));
   const bool vec_x = a.ld_x % 4 == 0 && K % 4 == 0, vec = vec_x && a.ld_gout % 4 == 0 && n % 4 == 0 && a.ld_gx % 4 == 0;
-  if (vec) k_gated_gx<T, kIn, kAct, true><<<gx, kGxThreads, 0, st>>>(a, ops, (int)gxs, gx_part);
-  else k_gated_gx<T, kIn, kAct, false><<<gx, kGxThreads, 0, st>>>(a, ops, (int)gxs, gx_part);
+  for (int64_t b = 0; b < blocks; b += kMostGroups) {   // one launch where gxs > 1
+    const int64_t r = b * gx_rows<T>(K);
+    GatedArgs p = a;
+    p.rows = std::min(a.rows - r, kMostGroups * gx_rows<T>(K));
+    p.x = (const T*)a.x + r * a.ld_x;
+    p.gout = (const T*)a.gout + r * a.ld_gout;
+    p.gx = (T*)a.gx + r * a.ld_gx;
+    const dim3 gx((unsigned)(std::min(blocks - b, kMostGroups) * gxs));
+    if (vec) k_gated_gx<T, kIn, kAct, true><<<gx, kGxThreads, 0, st>>>(p, ops, (int)gxs, gx_part);
+    else k_gated_gx<T, kIn, kAct, false><<<gx, kGxThreads, 0, st>>>(p, ops, (int)gxs, gx_part);
+  }
   if (vec_x) k_gated_gw<T, kIn, kAct, true><<<gw, kGwThreads, 0, st>>>(a, (int)cols, (int)gws, part);
   else k_gated_gw<T, kIn, kAct, false><<<gw, kGwThreads, 0, st>>>(a, (int)cols, (int)gws, part);
   return sum_splits<T>(a, part, gws, gx_part, gxs, st);

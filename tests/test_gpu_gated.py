@@ -220,3 +220,50 @@ def test_offsets_beyond_32_bits():
     for name, got in (("out", out[at]), ("gx", gx[at]), ("gWg", gW[0]), ("gWu", gW[1])):
         check(got.cpu().numpy(), ref[name], gated_tolerance(ref[name], "f32", k, n, len(at)), name)
     assert not torch.isnan(out[::4099]).any() and not torch.isnan(out[-1]).any() and not torch.isnan(gx).any()
+
+
+def sparse_gout(rows, n, at, dtype, gen):
+    gout = torch.zeros((rows, n), dtype=dtype, device="cuda")
+    gout[at] = torch.randn((len(at), n), generator=gen, dtype=dtype, device="cuda")
+    return gout
+
+
+def test_more_rows_than_one_launch_has_threads_for():
+    """2^30 rows and some: 64 to a workgroup of 256 threads."""
+    from paper_2501_13986_amd import binding as b
+    rows = (1 << 30) + 70
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn((rows, 1), generator=g, dtype=torch.float64, device="cuda")
+    W = [torch.randn((1, 1), generator=g, dtype=torch.float64, device="cuda") for _ in range(2)]
+    at = [0, 63, (1 << 28) - 1, 1 << 28, (1 << 29) + 5, (1 << 30) - 1, 1 << 30, rows - 1]
+    gout = sparse_gout(rows, 1, at, torch.float64, g)
+    gx, gW = torch.full_like(x, float("nan")), [torch.empty_like(w) for w in W]
+    b.gated_backward(x, *W, gout, gx, *gW)
+    ref = layer.gated(x[at].cpu().numpy(), *[w.cpu().numpy() for w in W], None, None, layer.SILU, gout[at].cpu().numpy())
+    for name, got in (("gx", gx[at]), ("gWg", gW[0]), ("gWu", gW[1])):
+        check(got.cpu().numpy(), ref[name], gated_tolerance(ref[name], "f64", 1, 1, len(at)), name)
+    assert not torch.isnan(gx).any()
+    del gout, gx
+    out = torch.full_like(x, float("nan"))
+    b.gated_forward(x, *W, out)
+    check(out[at].cpu().numpy(), ref["out"], gated_tolerance(ref["out"], "f64", 1, 1, len(at)), "out")
+    assert not torch.isnan(out).any()
+
+
+def test_more_weights_than_one_launch_has_threads_for():
+    """2 * 2048 * 2^20 sums: a row of 2047 numbers, 2^20 columns."""
+    from paper_2501_13986_amd import binding as b
+    k, n = 2047, 1 << 20
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randn((1, k), generator=g, device="cuda")
+    W = [torch.randn((k, n), generator=g, device="cuda") for _ in range(2)]
+    at = [0, 1, 255, 256, 524_287, n - 2, n - 1]     # columns of gout that are not zero
+    gout = torch.zeros((1, n), device="cuda")
+    gout[:, at] = torch.randn((1, len(at)), generator=g, device="cuda")
+    gx, gW = torch.full_like(x, float("nan")), [torch.full_like(w, float("nan")) for w in W]
+    b.gated_backward(x, *W, gout, gx, *gW)
+    ref = layer.gated(x.cpu().numpy(), *[w[:, at].cpu().numpy() for w in W], None, None, layer.SILU, gout[:, at].cpu().numpy())
+    for name, got in (("gx", gx), ("gWg", gW[0][:, at]), ("gWu", gW[1][:, at])):
+        check(got.cpu().numpy(), ref[name], gated_tolerance(ref[name], "f32", k, len(at), 1), name)
+    for t in gW:
+        assert not torch.isnan(t[::97]).any() and not torch.isnan(t[-1]).any() and (t[:, 2] == 0).all()
