@@ -318,7 +318,8 @@ typedef enum { CGTP_ACT_NONE = 0, CGTP_ACT_SILU = 1, CGTP_ACT_GELU = 2, CGTP_ACT
  * row of x (out) to the next, at least d_in (d_out) and below 2^22: rows may be columns of wider ones; what lies between them is not touched.
  * dtype: cgtp_dtype; act: cgtp_act.  fp32 products run on the matrix cores with each factor as the sum of three
  * bf16 numbers, which hold its 24 bits, and 32-bit sums: the result is as far from the exact one as that of fp32 products
- * (magnitudes above 2^128 (1 - 2^-9) count as infinite, and a row with an infinite number gives NaN).
+ * (magnitudes above 2^128 (1 - 2^-9) count as infinite, and a row with an infinite number gives NaN; a factor is off by up to
+ * 2^-125, where parts of it are below the normal numbers, so factors below 2^-101 have fewer bits).
  * Allocates nothing; no workspace.  rows < 2^31; d_in and d_out from 1 to 2^20, their product below 2^31.
  * out must not overlap an input. */
 cgtp_status gated_forward(const void* x, const void* Wg, const void* Wu, const void* bg, const void* bu, void* out,
@@ -329,7 +330,8 @@ cgtp_status gated_forward(const void* x, const void* Wg, const void* Wu, const v
  * given, gbg, gbu [d_out] (NULL otherwise).  The projections are formed again from x, nothing is kept from the forward call.
  * ld_gout and ld_gx as above.  Sums over rows are formed in a fixed order (bit-identical from run to run) through `workspace`:
  * caller-owned device memory of at least cgtp_gated_workspace_bytes(rows, d_in, d_out, dtype) bytes, 256-byte aligned (CGTP_EINVAL
- * if it is smaller), free again for other work on hip_stream after the call.  rows == 0: the weights' gradients are zero. */
+ * if it is smaller), free again for other work on hip_stream after the call.  rows == 0: the weights' gradients are zero.
+ * No output may overlap an input or another output. */
 size_t cgtp_gated_workspace_bytes(int64_t rows, int64_t d_in, int64_t d_out, int32_t dtype);
 cgtp_status gated_backward(const void* x, const void* Wg, const void* Wu, const void* bg, const void* bu, const void* gout,
                            void* gx, void* gWg, void* gWu, void* gbg, void* gbu, int64_t rows, int64_t d_in, int64_t d_out,
@@ -353,7 +355,8 @@ typedef struct cgtp_norm cgtp_norm; /* opaque; owned by the library until cgtp_n
 enum { CGTP_NORM_GATED = 2u };      /* flag of cgtp_norm_create, beside the layout */
 
 /* `groups` has to divide every multiplicity (CGTP_EINVAL); l <= 8, at most 64 segments, multiplicities up to 65536
- * (CGTP_EUNSUPPORTED).  eps > 0.  `device` as in cgtp_plan_create. */
+ * (CGTP_EUNSUPPORTED).  eps has to be a positive normal number of the type.  `device` as in cgtp_plan_create; it has to be the current
+ * device of the calls (CGTP_EINVAL). */
 cgtp_status cgtp_norm_create(const char* irreps, int32_t groups, int32_t act, double eps, int32_t dtype, int32_t device,
                              uint32_t flags, cgtp_norm** out);
 cgtp_status cgtp_norm_destroy(cgtp_norm* norm);
@@ -364,11 +367,13 @@ size_t cgtp_norm_workspace_bytes(const cgtp_norm* norm, int64_t N, int64_t S, in
 /* x [N, dim 0], y [N, dim 1], stats [S, dim 4].  ptr (int64 device array [S+1], not decreasing): sample s is the rows
  * ptr[s] .. ptr[s+1] - 1; rows in front of ptr[0] and from ptr[S] on belong to none and keep what y holds there.  A sample without
  * rows has mu = 0 and r = 1 / sqrt(eps).  NULL: every row is a sample (S has to be N).  Indices outside [0, N] are taken for the
- * nearest one inside; where ptr decreases the results are unspecified, within the arrays.  Allocates nothing; deterministic. */
+ * nearest one inside; where ptr decreases the results are unspecified, within the arrays.  fp32 rows that are samples by themselves are
+ * summed in fp32: deviations from the mean whose squares overflow (above 1e19) give r = 0; all other sums are held in fp64.
+ * Allocates nothing; deterministic; no output may overlap an input or another output. */
 cgtp_status norm_forward(const cgtp_norm* norm, const void* x, const void* weight, const void* bias, void* y, void* stats,
                          int64_t N, int64_t S, const int64_t* ptr, void* workspace, size_t workspace_bytes, void* hip_stream);
 /* Gradients of norm_forward given gy = dE/dy [N, dim 1] and the stats that it wrote: gx [N, dim 0] (rows of no sample keep what it
- * holds), gweight [dim 2], gbias [dim 3].  Deterministic. */
+ * holds), gweight [dim 2], gbias [dim 3].  Deterministic; no output may overlap an input or another output. */
 cgtp_status norm_backward(const cgtp_norm* norm, const void* x, const void* weight, const void* bias, const void* gy,
                           const void* stats, void* gx, void* gweight, void* gbias, int64_t N, int64_t S, const int64_t* ptr,
                           void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -1,8 +1,8 @@
 // Entry points of the layer operators: the gated feed-forward block and the group normalisation.
 #include <algorithm>
 #include <atomic>
+#include <cfloat>
 #include <climits>
-#include <cmath>
 #include <memory>
 #include <new>
 #include <string>
@@ -190,7 +190,8 @@ cgtp_status cgtp_norm_create(const char* irreps, int32_t groups, int32_t act, do
   if (dtype != CGTP_F32 && dtype != CGTP_F64) return fail(CGTP_EINVAL, "dtype must be CGTP_F32 or CGTP_F64");
   if (act < CGTP_ACT_NONE || act > CGTP_ACT_TANH) return fail(CGTP_EINVAL, "unknown activation");
   if (groups <= 0) return fail(CGTP_EINVAL, "the number of groups must be positive");
-  if (!(eps > 0) || !std::isfinite(eps)) return fail(CGTP_EINVAL, "eps must be positive and finite");
+  const double least = dtype == CGTP_F64 ? DBL_MIN : FLT_MIN, greatest = dtype == CGTP_F64 ? DBL_MAX : FLT_MAX;
+  if (!(eps >= least && eps <= greatest)) return fail(CGTP_EINVAL, "eps must be a positive normal number of the type");
   try {
     std::unique_ptr<cgtp_norm> H(new cgtp_norm());
     cgtp::Norm& N = H->N;
@@ -313,6 +314,9 @@ cgtp_status check_norm(const cgtp_norm* norm, int64_t N, int64_t S, const int64_
   for (const void* p : data)
     if (!aligned(p, 16)) return fail(CGTP_EINVAL, "data pointers must be 16-byte aligned");
   if (!norm->N.sums) return fail(CGTP_EUNSUPPORTED, "kernel " + norm->N.code.name + " is not loaded (created without a device?)");
+  int current = -1;      // its kernels are on one device
+  HIP_TRY(hipGetDevice(&current));
+  if (current != norm->N.device) return fail(CGTP_EINVAL, "the normalisation's device is not the current device");
   return CGTP_OK;
 }
 

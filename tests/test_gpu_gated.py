@@ -96,6 +96,18 @@ def test_numbers_far_apart(prec):
     compare(run(p, prec, layer.NONE, True), p, prec, layer.NONE, "spread")
 
 
+@pytest.mark.parametrize("k", [8, 16, 64, 200])
+@pytest.mark.parametrize("power", [100, 115, 126, 140])
+def test_smallest_numbers(k, power):
+    """A part of a factor below 2^-126 counts as zero: two parts of it at most, so a factor is off by 2^-125 at most."""
+    p = inputs(64, k, 64, "f32", True, seed=power)
+    p[0] = (p[0].astype(np.float64) * 2.0 ** -power).astype(np.float32)
+    p[2][:], p[3][:], p[4][:] = 0, 0, 1        # out = x Wg
+    out = run(p, "f32", layer.NONE, True)[0].cpu().numpy()
+    ref = layer.gated(*p[:5], layer.NONE, p[5])["out"]
+    check(out, ref, gated_tolerance(ref, "f32", k, 64, 64) + 2.0 ** -125 * np.abs(p[1].astype(np.float64)).sum(0), "out")
+
+
 def test_infinities_and_nan_stay_in_their_rows():
     p = inputs(70, 20, 40, "f32", False, seed=4)
     ref = run(p, "f32", layer.SILU, False)

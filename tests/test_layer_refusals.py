@@ -75,6 +75,12 @@ def test_norm_create_refuses(change, want):
     assert b.lib().cgtp_last_error()
 
 
+def test_norm_eps_is_a_normal_number_of_its_type():
+    """1e-40 would be zero for some fp32 arithmetic, 1 / sqrt(eps) infinite and a constant row NaN."""
+    assert make(eps=1e-40) == 1 and make(eps=1e39) == 1 and make(eps=5e-324, dtype=b.CGTP_F64) == 1
+    assert make(eps=2.0 ** -126) == 0 and make(eps=1e-40, dtype=b.CGTP_F64) == 0
+
+
 def test_norm_dims():
     n = b.Norm("4x0e+3x1o+2x0o", groups=1, gated=True, device=-1)
     assert (n.dim_x, n.dim_y, n.n_w, n.n_b, n.n_stat) == (4 + 9 + 2 + 5, 15, 14, 9, 10)
