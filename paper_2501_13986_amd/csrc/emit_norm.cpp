@@ -522,8 +522,9 @@ struct Chunks {
       f();
     }
   }
-  // the samples of the chunk: f(sample, first row, end, from, to, slot): the whole of a short one (slot -1), or a long one's rows in this chunk
-  template <class F> __device__ void each(F f) const {
+  // the samples of the chunk: f(sample, first row, end, from, to, slot): the whole of a short one (slot -1), or a long one's rows in this chunk;
+  // none(sample, end): neighbours without rows
+  template <class F, class E> __device__ void each(F f, E none) const {
     const i64 a = chunk * D, b = a + D < N ? a + D : N;
     const bool last = a + D >= N;
     i64 s = first_from_(ptr, S, N, a);
@@ -533,6 +534,12 @@ struct Chunks {
       const bool is_long = r1 - r0 > R;
       if (goes_on && (!is_long || r1 <= a)) continue;
       if (!goes_on && (r0 < a || (r0 >= b && !(last && r0 == N)))) break;
+      if (r1 == r0) {     // those behind it that begin at its row, but for the last, have no rows either
+        const i64 next = first_from_(ptr, S, N, r0 + 1) - 1, until = next > s ? next : s + 1;
+        none(s, until);
+        s = until - 1;
+        continue;
+      }
       f(s, r0, r1, goes_on ? a : r0, is_long && r1 > b ? b : r1, is_long ? !goes_on : -1);
     }
   }
@@ -683,6 +690,15 @@ template <bool kLong> struct GraphFwd {
         a.forward(v, g, st, p);
         if (a.on && base + a.rho < to) a.write(y + (base + a.rho) * DY + SEG[s].ycol, v);
       }
+    }, [&](i64 sample, i64 end) {
+      if (kLong || !stats) return;
+      const double none[4] = {};
+      const Stat st = stat_of_<s>(none, Shift{0, 0}, 0);
+      A b = a;
+      for (i64 i = threadIdx.x; i < (end - sample) * A::GP; i += 256) {
+        b.g = phase * A::GP + (int)(i % A::GP);
+        b.put_stat(stats + (sample + i / A::GP) * NST, st);
+      }
     }); });
   }
 };
@@ -759,7 +775,7 @@ template <bool kLong> struct GraphBwd {
           a.write_gates(gx + (base + a.rho) * DX, qg);
         }
       }
-    }); });
+    }, [](i64, i64) {}); });
     a.put_sums(sum, any, sums ? sums + part_() * (NW + NB) : nullptr, gweight, gbias, lds);
   }
 };

@@ -97,6 +97,26 @@ def test_lengths(N, ptr, prec):
     compare(run(n, p, ptr), irreps, 2, layer.SILU, True, True, p, prec, ptr)
 
 
+@pytest.mark.parametrize("prec", ["f32", "f64"])
+def test_many_samples_without_rows(prec):
+    """In front of the rows, between them, inside a chunk and behind the last; and no rows at all."""
+    irreps = "16x0e+8x1o+8x2e"
+    n = handle(irreps, 2, layer.SILU, True, prec, True)
+    p = inputs(n, 400, prec, seed=5)
+    own = [3, 7, 300, 400]       # ends of the samples with rows; rows 0 .. 2 belong to none
+    ptr = sum(([v] * m for v, m in zip(own, (30_000, 70, 40_000, 25_000))), [])
+    got, few = run(n, p, ptr), run(n, p, own)
+    for name in ("y", "gx", "gweight", "gbias"):
+        assert torch.equal(torch.nan_to_num(got[name]), torch.nan_to_num(few[name])), name
+    have = torch.tensor([e > s for s, e in zip(ptr, ptr[1:])], device="cuda")
+    assert torch.equal(got["stats"][have], few["stats"])
+    none = got["stats"][~have].view(-1, n.n_stat // 2, 2)
+    r = torch.tensor(1 / np.sqrt(1e-5), dtype=none.dtype, device="cuda")
+    assert (none[..., 0] == 0).all() and torch.allclose(none[..., 1], r, rtol=1e-6, atol=0)
+    got = run(n, [p[0][:0], p[1], p[2], p[3][:0]], [0] * 50_001)
+    assert torch.allclose(got["stats"].view(50_000, -1, 2)[..., 1], r, rtol=1e-6, atol=0) and (got["gweight"] == 0).all() and (got["gbias"] == 0).all()
+
+
 @pytest.mark.parametrize("prec,shift", [("f32", 1000.0), ("f64", 1e6)])
 def test_far_from_zero(prec, shift):
     """Scalars whose mean is far larger than their spread: the variance is not the difference of two large numbers."""
