@@ -1046,13 +1046,23 @@ int64_t gw_splits(int64_t rows, int64_t K, int64_t n, int cus) {
   return std::max<int64_t>(1, std::min({blocks, groups * cus / cols, most}));
 }
 
-// Rows of a workgroup of k_gated_gx, and how the columns of W are split where the rows alone leave compute units without work
+// rows of a workgroup of k_gated_gx
 template <class T>
 int64_t gx_rows(int64_t K) { return with_columns(K, [](auto in) { return kGxWaves<T, decltype(in)::value> * kGxTiles<T, decltype(in)::value> * 16; }); }
+
+// How the columns of W are split for gx.  Few rows: so that every compute unit has work.  More: where the units' shares are uneven, a workgroup more on some
+// than on others (40 000 x 128 x 2176, 313 workgroups on 256 units, gradients 1260 us, in three splits 1064; fp64, 20 000 x 64 x 544, 324 and 281).
+// That has to save a quarter of the time, or the partial sums cost more than it gives (20 011 x 128 x 301, forward and backward 194 us, in three
+// splits, which save a fifth, 214).
 template <class T>
-int64_t gx_splits(int64_t rows, int64_t K, int64_t n, int cus) {
-  const int64_t blocks = (rows + gx_rows<T>(K) - 1) / gx_rows<T>(K), room = (K > 64 ? 1 : 2) * cus;
-  return std::max<int64_t>(1, std::min((n + 31) / 32, room / blocks));
+int64_t gx_splits(int64_t rows, int64_t K, int64_t n) {
+  const int64_t blocks = (rows + gx_rows<T>(K) - 1) / gx_rows<T>(K), room = (K > 64 ? 1 : 2) * kMostUnits, steps = (n + 31) / 32;
+  if (blocks <= room / 2) return std::min(steps, room / blocks);
+  auto time = [&](int64_t s) { return (blocks * s + kMostUnits - 1) / kMostUnits * ((steps + s - 1) / s); };
+  int64_t best = 1;
+  for (int64_t s = 2; s <= std::min<int64_t>(steps, 4); ++s)
+    if (time(s) < time(best) && 4 * time(s) <= 3 * time(1)) best = s;
+  return best;
 }
 constexpr int64_t kFewBlocks = 4;   // up to this many blocks of rows form the operands of W themselves
 
@@ -1083,7 +1093,7 @@ template <class T>
 size_t workspace_bytes(int64_t rows, int64_t K, int64_t n) {
   const size_t e = sizeof(T), part = 2 * (K + 1) * n * e;
   if (K <= kMaxIn) {
-    const int64_t gx = gx_splits<T>(rows, K, n, kMostUnits);
+    const int64_t gx = gx_splits<T>(rows, K, n);
     return up(operand_bytes<T>(K, n)) + up(gw_splits<T>(rows, K, n, kMostUnits) * part) + (gx > 1 ? up(gx * rows * K * e) : 0);
   }
   const int64_t gx = many_gx_splits<T>(rows, K, n, kMostUnits);
@@ -1131,7 +1141,7 @@ hipError_t sum_splits(const GatedArgs& a, const T* part, int64_t splits, const T
 template <class T, int kIn, int kAct>
 hipError_t launch_bwd(const GatedArgs& a, int cus, char* ws, hipStream_t st) {
   const int64_t K = a.d_in, n = a.d_out, wide = 16 * kGwWaves, cols = (n + wide - 1) / wide;
-  const int64_t gws = gw_splits<T>(a.rows, K, n, cus), gxs = gx_splits<T>(a.rows, K, n, cus), blocks = (a.rows + gx_rows<T>(K) - 1) / gx_rows<T>(K);
+  const int64_t gws = gw_splits<T>(a.rows, K, n, cus), gxs = gx_splits<T>(a.rows, K, n), blocks = (a.rows + gx_rows<T>(K) - 1) / gx_rows<T>(K);
   u32x4* ops = blocks > kFewBlocks ? (u32x4*)ws : nullptr;
   T* part = (T*)(ws + up(operand_bytes<T>(K, n)));
   T* gx_part = (T*)((char*)part + up(gw_splits<T>(a.rows, K, n, kMostUnits) * 2 * (K + 1) * n * sizeof(T)));

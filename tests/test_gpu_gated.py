@@ -69,6 +69,13 @@ def test_against_the_oracle(rows, k, n, prec):
     compare(run(p, prec, layer.SILU, bias), p, prec, layer.SILU, f"{rows}x{k}x{n}")
 
 
+@pytest.mark.parametrize("rows,k,n,prec", [(40_000, 16, 70, "f32"), (20_000, 14, 70, "f64"), (33_000, 100, 97, "f32"), (16_500, 128, 65, "f64")])
+def test_uneven_shares_are_split(rows, k, n, prec):
+    """A few workgroups more than compute units: the columns of W are split for gx."""
+    p = inputs(rows, k, n, prec, True, seed=rows)
+    compare(run(p, prec, layer.SILU, True), p, prec, layer.SILU, (rows, k, n))
+
+
 @pytest.mark.parametrize("prec", ["f32", "f64"])
 @pytest.mark.parametrize("act", [layer.NONE, layer.GELU, layer.SIGMOID, layer.TANH])
 @pytest.mark.parametrize("k", [7, 14, 20, 40, 80, 110, 140])
