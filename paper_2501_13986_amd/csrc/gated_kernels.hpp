@@ -354,6 +354,11 @@ __device__ inline void write_both(Tile<double, kRows, KC>& X, Tile<double, KD, k
 
 // A wave keeps the parts of its 16 NT columns of Wg and Wu in registers for the whole call and walks over rows, whose parts the
 // workgroup puts into LDS once for its four waves.  Lane: columns NT l16 + j.
+// Bound by the matrix pipe at the clock that its load leaves: 160 710 x 64 x 2176 fp32 450 us, 1.19 PFLOP/s of bf16 products (library 1.13) beside
+// 3.1 TB/s of writes; the pipe is busy 59 % of the cycles at 1.9 GHz; without the stores 376 us, with half of the products 327.  With 8 columns of x
+// bound by the writes: 270 us, 5.2 TB/s.  fp64, 30 011 x 64 x 544: 107 us, 39 TFLOP/s (library 72; an instruction of the matrix pipe and one of the vector
+// pipe in fp64 do not run at once).  Two waves per SIMD, for the registers; four with half the columns were no faster.  With the
+// instruction of 32 x 32 results 482 us for 457; 16 columns a wave 546 for 472.
 template <class T, int kIn, int NT, int kAct, bool kVec>
 __global__ void __launch_bounds__(kThreads, (sizeof(T) == 8 && kIn > 64 ? 1 : 2)) k_gated_fwd(GatedArgs a, int col_tiles, int splits) {
   using N = Num<T>;
@@ -447,6 +452,9 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 8 && kIn > 64 ? 1 : 2)
 // but those are twice the size of gout, written once and read twice.
 
 // gWg, gWu, gbg, gbu of 16 columns a wave, over the row blocks of a split; partial sums [split][Wg; bg; Wu; bu]
+// Bound by the matrix pipe and the vector instructions between its products (activation, cuts into parts), at 1.8 GHz: 160 710 x 64 x 2176 fp32 0.95 ms
+// (with gx 1.90 ms, of which 0.3 would do for the bytes), pipe busy 51 % of the cycles.  Activations of one tile beside the products of another: within
+// 1 %.  fp64, 30 011 x 64 x 544: 200 us.
 constexpr int kGwWaves = 4;
 // whether a wave needs the registers of two: fp64, and from 65 columns of x on (20 011 x 128 x 301, forward and backward 214 us, with two waves that
 // keep what does not fit in private memory 230)
@@ -576,7 +584,8 @@ __global__ void __launch_bounds__((kGwWaves * 64), (kGwAlone<T, kIn> ? 1 : 2)) k
   }
 }
 
-// adds up the splits, in their order: the weights' and biases' gradients, and gx where its sums are split (gx_splits > 1)
+// adds up the splits, in their order: the weights' and biases' gradients, and gx where its sums are split (gx_splits > 1).  4 to 6 us, eight loads in
+// flight a thread for the latency of few rows.
 template <class T>
 __global__ void __launch_bounds__(kThreads) k_gated_sums(GatedArgs a, const T* __restrict__ part, int splits, const T* __restrict__ gx_part, int gx_splits) {
   const int64_t K = a.d_in, n = a.d_out, size = 2 * (K + 1) * n, gx_size = gx_splits > 1 ? a.rows * K : 0;
@@ -651,8 +660,9 @@ __global__ void __launch_bounds__(kThreads) k_gated_operands(GatedArgs a, u32x4*
 }
 
 // gx of 16 R rows a wave: the operands of 32 columns of W at a time in LDS for the waves of a workgroup, the columns of a split one after
-// another.  Four waves, so that two workgroups of a compute unit are in different phases (160 710 x 64 x 2176, all of backward 2.01 ms, with
-// eight 2.12); eight in fp32 of more than 64 columns of x, whose operands fill the LDS for one workgroup (50 000 x 128 x 2176 1.46 ms, with four 1.91).  More than one split: partial sums [split][rows][d_in] in part.  ops NULL: the
+// another.  Bound like k_gated_gw: 160 710 x 64 x 2176 fp32 0.95 ms, matrix pipe busy 51 % of the cycles at 1.8 GHz; fp64, 30 011 x 64 x 544, 223 us.
+// Four waves, so that two workgroups of a compute unit are in different phases (160 710 x 64 x 2176, all of backward 2.01 ms before the
+// tiles were without bank conflicts, with eight 2.12); eight in fp32 of more than 64 columns of x, whose operands fill the LDS for one workgroup (50 000 x 128 x 2176 backward 1.40 ms; 1.46 when four took 1.91).  More than one split: partial sums [split][rows][d_in] in part.  ops NULL: the
 // workgroups form the operands themselves, which saves a launch where the rows are few.
 template <class T, int kIn>
 constexpr int kGxWaves = kIn > 64 && sizeof(T) == 4 ? 8 : 4;
@@ -821,7 +831,10 @@ __global__ void __launch_bounds__((kGxWaves<T, kIn> * 64), (kIn > 64 && sizeof(T
 // ---- more columns of x ----------------------------------------------------------------------------------------------------------
 //
 // 128 rows x 64 columns of results a workgroup, 16 columns a wave, the terms 32 at a time: the rows' parts in LDS, the columns' parts formed
-// by each wave from memory.  The gradients go through dg and du in the workspace, a piece of the rows at a time.
+// by each wave from memory.  The gradients go through dg and du in the workspace, a piece of the rows at a time, since W
+// no longer stays in registers for products that would form g and u again.  Bound by the matrix pipe and the loads of W that each wave makes: forward and backward of
+// 30 000 x 200 x 1000 fp32 1.27 ms (75 TFLOP/s of fp32 products; six bf16 products each at the library's rate would take 0.51), 20 000 x 200 x 500 fp64
+// 0.90 ms (35 TFLOP/s, library 72).  One row of 256 to 2176 numbers: 66 us, five launches of few workgroups.
 
 template <class T>
 constexpr int kManyRows = sizeof(T) == 4 ? 128 : 64;   // rows of a workgroup, for the registers of their sums
