@@ -141,35 +141,45 @@ __device__ inline T load1(Buffer B, unsigned at) {
   else return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b64(B, at, 0, 0));
 }
 
-template <class T>
+template <int kHow = kNonTemporal, class T>
 __device__ inline void store1(T v, Buffer B, unsigned at) {
-  if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, v), B, at, 0, kNonTemporal);
-  else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), B, at, 0, kNonTemporal);
+  if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, v), B, at, 0, kHow);
+  else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), B, at, 0, kHow);
 }
 
-// Four neighbouring numbers of the row that begins at offset `row`, from column k, zero beyond its end.  kVec: base, rows and widths are
-// multiples of four numbers.
-template <bool kVec, class T>
+// Four neighbouring numbers of the row that begins at offset `row`, from column k, zero beyond its end (kWhole: the row's width is a multiple of four).
+// Buffer accesses of several words need the alignment of one, and are held against the range word by word.
+template <bool kWhole, class T>
 __device__ inline void load4(Buffer B, unsigned row, int k, int K, T* v) {
   constexpr int e = sizeof(T);
-  if constexpr (kVec) {
-    const unsigned at = k < K ? row + k * e : kNowhere;
-    if constexpr (e == 4) {
-      const f32x4 w = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(B, at, 0, 0));
+  const unsigned at = k < K ? row + k * e : kNowhere;
+  if constexpr (e == 4) {
+    const f32x4 w = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(B, at, 0, 0));
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = w[i];
-    } else {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const f64x2 w = __builtin_bit_cast(f64x2, __builtin_amdgcn_raw_buffer_load_b128(B, at + h * 16, 0, 0));
-        v[2 * h] = w[0];
-        v[2 * h + 1] = w[1];
-      }
-    }
+    for (int i = 0; i < 4; ++i) v[i] = w[i];
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = load1<T>(B, k + i < K ? row + (k + i) * e : kNowhere);
+    for (int h = 0; h < 2; ++h) {
+      const f64x2 w = __builtin_bit_cast(f64x2, __builtin_amdgcn_raw_buffer_load_b128(B, at + h * 16, 0, 0));
+      v[2 * h] = w[0];
+      v[2 * h + 1] = w[1];
+    }
   }
+  if constexpr (!kWhole)
+#pragma unroll
+    for (int i = 1; i < 4; ++i) v[i] = k + i < K ? v[i] : T(0);     // else of the next row, or what lies between rows
+}
+
+// the same for writing, fp32
+template <bool kWhole>
+__device__ inline void store4(f32x4 v, Buffer B, unsigned row, int k, int K) {
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), B, k + 4 <= K ? row + k * 4 : kNowhere, 0, 0);
+  if constexpr (!kWhole)
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+      const float w = v[i];
+      __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, w), B, k + 4 > K && k + i < K ? row + (k + i) * 4 : kNowhere, 0, 0);
+    }
 }
 
 // `rows` rows of W [.., n] from row k on, at most 128 of them (2^30 bytes); an element's offset in it
@@ -359,7 +369,7 @@ __device__ inline void write_both(Tile<double, kRows, KC>& X, Tile<double, KD, k
 // bound by the writes: 270 us, 5.2 TB/s.  fp64, 30 011 x 64 x 544: 107 us, 39 TFLOP/s (library 72; an instruction of the matrix pipe and one of the vector
 // pipe in fp64 do not run at once).  Two waves per SIMD, for the registers; four with half the columns were no faster.  With the
 // instruction of 32 x 32 results 482 us for 457; 16 columns a wave 546 for 472.
-template <class T, int kIn, int NT, int kAct, bool kVec>
+template <class T, int kIn, int NT, int kAct, bool kWhole>
 __global__ void __launch_bounds__(kThreads, (sizeof(T) == 8 && kIn > 64 ? 1 : 2)) k_gated_fwd(GatedArgs a, int col_tiles, int splits) {
   using N = Num<T>;
   using I = In<T, kIn>;
@@ -389,12 +399,14 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 8 && kIn > 64 ? 1 : 2)
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int at = t + i * kThreads < kAll ? t + i * kThreads : kAll - 1;
-      load4<kVec>(in, at / kQuads * ldx, at % kQuads * 4, K, next[i]);
+      load4<kWhole>(in, at / kQuads * ldx, at % kQuads * 4, K, next[i]);
     }
   };
-  unsigned at[NT];      // a lane's columns
-#pragma unroll
-  for (int j = 0; j < NT; ++j) at[j] = c + j < n ? (unsigned)(c + j) * e + N::row(q, 0) * ldo : kNowhere;
+  // a lane's columns: of all, or of the first alone where the row ends behind it
+  const unsigned at = c + NT <= n ? (unsigned)c * e + N::row(q, 0) * ldo : kNowhere, at_last = c + 1 == n ? (unsigned)c * e + N::row(q, 0) * ldo : kNowhere;
+  // Whole lines are written past the caches, parts of lines are left to them (160 710 x 64 x 2176, a number between the rows 877 and 522 us, none
+  // 482 and 495; fp64, 60 000 x 8 x 544, a number between them 146 and 76 us)
+  const bool past = ldo % 64 == 0;
   int64_t b = blockIdx.x / col_tiles;
   if (b < blocks) fetch(b);
   for (; b < blocks; b += splits) {
@@ -425,19 +437,26 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 8 && kIn > 64 ? 1 : 2)
       }
     };
     auto finish = [&](int rt, const typename N::Vec* gt, const typename N::Vec* ut) {
+      T v[4][NT];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const unsigned row = (rt * 16 + N::row(0, i)) * ldo;
-        T v[NT];
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) v[j] = act_only<kAct>(T(gt[j][i])) * T(ut[j][i]);
-        if constexpr (NT == 2 && kVec && e == 4) {
-          __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, f32x2{v[0], v[1]}), to, at[0] + row, 0, kNonTemporal);
-        } else {
+        for (int j = 0; j < NT; ++j) v[i][j] = act_only<kAct>(T(gt[j][i])) * T(ut[j][i]);
+      auto write = [&](auto how) {
+        constexpr int kHow = decltype(how)::value;
 #pragma unroll
-          for (int j = 0; j < NT; ++j) store1(v[j], to, at[j] + row);
+        for (int i = 0; i < 4; ++i) {
+          const unsigned row = (rt * 16 + N::row(0, i)) * ldo;
+          if constexpr (NT == 2) {
+            __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, f32x2{v[i][0], v[i][1]}), to, at + row, 0, kHow);
+            if constexpr (!kWhole) store1<kHow>(v[i][0], to, at_last + row);
+          } else {
+            store1<kHow>(v[i][0], to, at + row);
+          }
         }
-      }
+      };
+      if (past) write(std::integral_constant<int, kNonTemporal>());
+      else write(std::integral_constant<int, 0>());
     };
 #pragma unroll
     for (int rt = 0; rt < kRows / 16; ++rt) {
@@ -461,7 +480,7 @@ constexpr int kGwWaves = 4;
 template <class T, int kIn>
 constexpr bool kGwAlone = kIn > (sizeof(T) == 8 ? 32 : 64);
 
-template <class T, int kIn, int kAct, bool kVec>
+template <class T, int kIn, int kAct, bool kWhole>
 __global__ void __launch_bounds__((kGwWaves * 64), (kGwAlone<T, kIn> ? 1 : 2)) k_gated_gw(GatedArgs a, int col_tiles, int splits, T* part) {
   using N = Num<T>;
   using I = In<T, kIn>;
@@ -499,7 +518,7 @@ __global__ void __launch_bounds__((kGwWaves * 64), (kGwAlone<T, kIn> ? 1 : 2)) k
       int r4, k4;
       block(i, r4, k4);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) load4<kVec>(in, (r4 * 4 + j) * ldx, k4, K, next[i][j]);
+      for (int j = 0; j < 4; ++j) load4<kWhole>(in, (r4 * 4 + j) * ldx, k4, K, next[i][j]);
     }
   };
   const unsigned at = c < n ? (unsigned)c * e + N::row(q, 0) * ldo : kNowhere;
@@ -669,7 +688,7 @@ constexpr int kGxWaves = kIn > 64 && sizeof(T) == 4 ? 8 : 4;
 template <class T, int kIn>
 constexpr int kGxTiles = kIn > 64 || sizeof(T) == 8 ? 1 : 2;   // 2 would not fit the registers
 
-template <class T, int kIn, int kAct, bool kVec>
+template <class T, int kIn, int kAct, bool kWhole>
 __global__ void __launch_bounds__((kGxWaves<T, kIn> * 64), (kIn > 64 && sizeof(T) == 8 ? 1 : 2)) k_gated_gx(GatedArgs a, const u32x4* __restrict__ ops, int splits, T* part) {
   using N = Num<T>;
   using I = In<T, kIn>;
@@ -705,7 +724,7 @@ __global__ void __launch_bounds__((kGxWaves<T, kIn> * 64), (kIn > 64 && sizeof(T
         const int k = I::first(s, q);
         if constexpr (I::kTerms >= 4) {
 #pragma unroll
-          for (int i = 0; i < I::kTerms; i += 4) load4<kVec>(in, (r * 16 + l16) * ldx, k + i, K, v + i);
+          for (int i = 0; i < I::kTerms; i += 4) load4<kWhole>(in, (r * 16 + l16) * ldx, k + i, K, v + i);
         } else {
 #pragma unroll
           for (int i = 0; i < I::kTerms; ++i) v[i] = load1<T>(in, k + i < K ? (r * 16 + l16) * ldx + (k + i) * e : kNowhere);
@@ -731,7 +750,7 @@ __global__ void __launch_bounds__((kGxWaves<T, kIn> * 64), (kIn > 64 && sizeof(T
         const int c = (int)(step * 32 + tile * 16);
         const unsigned row = (r * 16 + l16) * ldo;
         if constexpr (e == 4) {
-          load4<kVec>(go, row, c + q * 4, (int)n, tg[r] + tile * 4);
+          load4<kWhole>(go, row, c + q * 4, (int)n, tg[r] + tile * 4);
         } else {
 #pragma unroll
           for (int i = 0; i < 4; ++i) tg[r][tile * 4 + i] = load1<T>(go, c + N::row(q, i) < n ? row + (c + N::row(q, i)) * e : kNowhere);
@@ -814,9 +833,8 @@ __global__ void __launch_bounds__((kGxWaves<T, kIn> * 64), (kIn > 64 && sizeof(T
 #pragma unroll
     for (int d = 0; d < DT; ++d) {
       const unsigned row = (r * 16 + l16) * ldg;
-      if constexpr (kVec && e == 4) {
-        const int k = d * 16 + q * 4;
-        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, acc[r][d]), to, k < K ? row + k * 4 : kNowhere, 0, 0);
+      if constexpr (e == 4) {
+        store4<kWhole>(acc[r][d], to, row, d * 16 + q * 4, K);
       } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -1118,8 +1136,7 @@ hipError_t launch_fwd(const GatedArgs& a, int cus, hipStream_t st) {
   const int64_t cols = (a.d_out + 64 * NT - 1) / (64 * NT), blocks = (a.rows + kRows - 1) / kRows;
   const int64_t splits = std::max<int64_t>(1, std::min<int64_t>(blocks, kGroups<T, kIn> * cus / cols));
   const dim3 grid((unsigned)(cols * splits));
-  const bool vec = a.ld_x % 4 == 0 && a.d_in % 4 == 0 && a.ld_out % 2 == 0 && a.d_out % 2 == 0;
-  if (vec) k_gated_fwd<T, kIn, NT, kAct, true><<<grid, kThreads, 0, st>>>(a, (int)cols, (int)splits);
+  if (a.d_in % 4 == 0 && a.d_out % 2 == 0) k_gated_fwd<T, kIn, NT, kAct, true><<<grid, kThreads, 0, st>>>(a, (int)cols, (int)splits);
   else k_gated_fwd<T, kIn, NT, kAct, false><<<grid, kThreads, 0, st>>>(a, (int)cols, (int)splits);
   return hipGetLastError();
 }
@@ -1161,7 +1178,7 @@ hipError_t launch_bwd(const GatedArgs& a, int cus, char* ws, hipStream_t st) {
   if (ops) k_gated_operands<T, kIn><<<dim3((unsigned)(((n + 31) / 32 * Operands<T, kIn>::kOps + 3) / 4)), kThreads, 0, st>>>(a, ops);
   constexpr int kGxThreads = kGxWaves<T, kIn> * 64, kGwThreads = kGwWaves * 64;
   const dim3 gw((unsigned)(cols * gws));
-  const bool vec_x = a.ld_x % 4 == 0 && K % 4 == 0, vec = vec_x && a.ld_gout % 4 == 0 && n % 4 == 0 && a.ld_gx % 4 == 0;
+  const bool whole = K % 4 == 0;
   for (int64_t b = 0; b < blocks; b += kMostGroups) {   // one launch where gxs > 1
     const int64_t r = b * gx_rows<T>(K);
     GatedArgs p = a;
@@ -1170,10 +1187,10 @@ hipError_t launch_bwd(const GatedArgs& a, int cus, char* ws, hipStream_t st) {
     p.gout = (const T*)a.gout + r * a.ld_gout;
     p.gx = (T*)a.gx + r * a.ld_gx;
     const dim3 gx((unsigned)(std::min(blocks - b, kMostGroups) * gxs));
-    if (vec) k_gated_gx<T, kIn, kAct, true><<<gx, kGxThreads, 0, st>>>(p, ops, (int)gxs, gx_part);
+    if (whole && n % 4 == 0) k_gated_gx<T, kIn, kAct, true><<<gx, kGxThreads, 0, st>>>(p, ops, (int)gxs, gx_part);
     else k_gated_gx<T, kIn, kAct, false><<<gx, kGxThreads, 0, st>>>(p, ops, (int)gxs, gx_part);
   }
-  if (vec_x) k_gated_gw<T, kIn, kAct, true><<<gw, kGwThreads, 0, st>>>(a, (int)cols, (int)gws, part);
+  if (whole) k_gated_gw<T, kIn, kAct, true><<<gw, kGwThreads, 0, st>>>(a, (int)cols, (int)gws, part);
   else k_gated_gw<T, kIn, kAct, false><<<gw, kGwThreads, 0, st>>>(a, (int)cols, (int)gws, part);
   return sum_splits<T>(a, part, gws, gx_part, gxs, st);
 }

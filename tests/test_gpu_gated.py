@@ -97,6 +97,22 @@ def test_columns_of_wider_rows(rows, k, n, wide, prec):
 
 
 @pytest.mark.parametrize("prec", ["f32", "f64"])
+@pytest.mark.parametrize("rows,k,n,wide", [(70, 7, 19, 3), (65, 30, 33, 2), (130, 61, 66, 1), (20, 101, 30, 5), (140, 131, 35, 3), (64, 10, 9, 7), (64, 15, 18, 1)])
+def test_what_lies_between_rows_is_not_used(rows, k, n, wide, prec):
+    """NaN behind every row, whose widths end inside a load of four numbers."""
+    p = inputs(rows, k, n, prec, True, seed=k)
+    from paper_2501_13986_amd import binding as b
+    x, gout = dev(p[0], wide, float("nan")), dev(p[5], wide, float("nan"))
+    t = [dev(a) for a in p[1:5]]
+    o = outputs(rows, k, n, prec, True, wide)
+    b.gated_forward(x, *t[:2], o[0], bg=t[2], bu=t[3])
+    b.gated_backward(x, *t[:2], gout, o[1], o[2], o[3], bg=t[2], bu=t[3], gbg=o[4], gbu=o[5])
+    compare(o, p, prec, layer.SILU, (rows, k, n, wide))
+    for out, w in ((o[0], n), (o[1], k)):
+        assert torch.isnan(out.as_strided((rows - 1, wide), (w + wide, 1), w)).all()
+
+
+@pytest.mark.parametrize("prec", ["f32", "f64"])
 def test_numbers_far_apart(prec):
     """Factors over many powers of two: each product keeps the precision of its type."""
     p = inputs(50, 48, 40, prec, True, seed=9, spread=4.0)
