@@ -86,10 +86,11 @@ struct NormWork {
       blocks = std::max<int64_t>(1, std::min<int64_t>(steps, std::max<int64_t>(1, (backward ? 2048 : most) / P.subs)));
       sum_rows = blocks;
     } else {
-      // Chunks of 32 rows where samples are short (500 molecules in 12 000 rows of 32 channels, l <= 3: 79 us forward and backward, with 16
-      // rows 94); up to 128 with many workgroups of them or long samples, whose shares each workgroup adds up, as long as that leaves enough
-      D = 32;
-      while (D < 128 && N / (2 * D) * P.subs >= 512 && (N / D * P.subs > 8192 || N / D > 4 * S)) D *= 2;
+      // Chunks of 32 rows, of 64 where that leaves two workgroups a compute unit: a chunk's samples are found once (samples of 25 rows, l <= 3, 12 000 rows
+      // of 32 channels forward and backward 67 us with 32 rows, 59 with 64, 58 with 128; l <= 2, 80 000 rows 165, 130 and 125; with 128 channels
+      // 30 000 rows 407, 408 and 425); of 128 for long samples, whose shares each workgroup adds up
+      D = N / 64 * P.subs >= 512 ? 64 : 32;
+      if (N / 128 * P.subs >= 512 && N / 64 > 4 * S) D = 128;
       while ((N + D - 1) / D > most / P.subs) D *= 2;
       R = std::max(R, D);
       const int64_t chunks = std::max<int64_t>(1, (N + D - 1) / D);

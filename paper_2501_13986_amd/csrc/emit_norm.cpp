@@ -517,6 +517,12 @@ __device__ inline i64 first_from_(const i64* __restrict__ ptr, i64 S, i64 N, i64
   return lo;
 }
 
+// lane i's number; i is the same in all lanes
+__device__ inline i64 lane_of_(i64 v, int i) {
+  const unsigned lo = __builtin_amdgcn_readlane((int)v, i), hi = __builtin_amdgcn_readlane((int)(v >> 32), i);
+  return (i64)((unsigned long long)hi << 32 | lo);
+}
+
 struct Chunks {
   const i64* __restrict__ ptr;
   i64 N, S, R, D, chunk;
@@ -533,10 +539,15 @@ struct Chunks {
   template <class F, class E> __device__ void each(F f, E none) const {
     const i64 a = chunk * D, b = a + D < N ? a + D : N;
     const bool last = a + D >= N;
-    i64 s = first_from_(ptr, S, N, a);
+    i64 s = first_from_(ptr, S, N, a), from = -64, p = 0;      // p: a lane's number of ptr, from `from` on
     bool goes_on = s > 0;       // the one before may reach into the chunk
     for (s -= goes_on; s < S; ++s, goes_on = false) {
-      const i64 r0 = inside_(ptr[s], N), e = inside_(ptr[s + 1], N), r1 = e < r0 ? r0 : e;
+      if (s - from > 62) {
+        const i64 i = s + (threadIdx.x & 63);
+        from = s;
+        p = inside_(ptr[i < S ? i : S], N);
+      }
+      const i64 r0 = lane_of_(p, (int)(s - from)), e = lane_of_(p, (int)(s - from) + 1), r1 = e < r0 ? r0 : e;
       const bool is_long = r1 - r0 > R;
       if (goes_on && (!is_long || r1 <= a)) continue;
       if (!goes_on && (r0 < a || (r0 >= b && !(last && r0 == N)))) break;
