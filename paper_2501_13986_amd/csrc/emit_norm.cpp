@@ -495,7 +495,7 @@ extern "C" __global__ void __launch_bounds__(256) cgtp_norm_row_bwd(const T* __r
 // that begins, slot 1), the second adds up the shares of a sample, each workgroup for its groups, and writes the results.  Sums over rows are held
 // in 64 bits; those of fp64 are of the distance from the group's first number of the sample, for their variance.
 // Bound, with short samples, by the chain of a sample's steps (ptr, rows, sums through LDS, results), which the other workgroups of a unit hide in part: 500
-// samples in 12 000 rows of 32 channels, l <= 3, forward 21 us (2.6 TB/s), backward 38 (2.2); with a sample a wave instead of a workgroup no faster.
+// samples in 12 000 rows of 32 channels, l <= 3, forward 20 to 29 us (2.7 to 1.9 TB/s), backward 36 (2.3); with a sample a wave instead of a workgroup no faster.
 // Long ones: by memory, which is read twice (no chip-wide barrier): one sample of 20 000 rows of 128 channels 118 and 199 us, the second kernel going through
 // the chunks from the last on, which are still in the caches.
 const char kGraphs[] = R"HIP(

@@ -364,7 +364,7 @@ __device__ inline void write_both(Tile<double, kRows, KC>& X, Tile<double, KD, k
 
 // A wave keeps the parts of its 16 NT columns of Wg and Wu in registers for the whole call and walks over rows, whose parts the
 // workgroup puts into LDS once for its four waves.  Lane: columns NT l16 + j.
-// Bound by the matrix pipe at the clock that its load leaves: 160 710 x 64 x 2176 fp32 450 us, 1.19 PFLOP/s of bf16 products (library 1.13) beside
+// Bound by the matrix pipe at the clock that its load leaves: 160 710 x 64 x 2176 fp32 450 to 470 us, 1.14 to 1.19 PFLOP/s of bf16 products (library 1.13) beside
 // 3.1 TB/s of writes; the pipe is busy 59 % of the cycles at 1.9 GHz; without the stores 376 us, with half of the products 327.  With 8 columns of x
 // bound by the writes: 270 us, 5.2 TB/s.  fp64, 30 011 x 64 x 544: 107 us, 39 TFLOP/s (library 72; an instruction of the matrix pipe and one of the vector
 // pipe in fp64 do not run at once).  Two waves per SIMD, for the registers; four with half the columns were no faster.  With the
@@ -851,8 +851,8 @@ __global__ void __launch_bounds__((kGxWaves<T, kIn> * 64), (kIn > 64 && sizeof(T
 // 128 rows x 64 columns of results a workgroup, 16 columns a wave, the terms 32 at a time: the rows' parts in LDS, the columns' parts formed
 // by each wave from memory.  The gradients go through dg and du in the workspace, a piece of the rows at a time, since W
 // no longer stays in registers for products that would form g and u again.  Bound by the matrix pipe and the loads of W that each wave makes: forward and backward of
-// 30 000 x 200 x 1000 fp32 1.27 ms (75 TFLOP/s of fp32 products; six bf16 products each at the library's rate would take 0.51), 20 000 x 200 x 500 fp64
-// 0.90 ms (35 TFLOP/s, library 72).  One row of 256 to 2176 numbers: 66 us, five launches of few workgroups.
+// 30 000 x 200 x 1000 fp32 1.17 ms (82 TFLOP/s of fp32 products; six bf16 products each at the library's rate would take 0.51), 20 000 x 200 x 500 fp64
+// 0.90 ms (35 TFLOP/s, library 72).  One row of 256 to 2176 numbers: 60 us, five launches of few workgroups.
 
 template <class T>
 constexpr int kManyRows = sizeof(T) == 4 ? 128 : 64;   // rows of a workgroup, for the registers of their sums
@@ -1083,8 +1083,8 @@ int64_t gx_rows(int64_t K) { return with_columns(K, [](auto in) { return kGxWave
 
 // How the columns of W are split for gx.  Few rows: so that every compute unit has work.  More: where the units' shares are uneven, a workgroup more on some
 // than on others (40 000 x 128 x 2176, 313 workgroups on 256 units, gradients 1260 us, in three splits 1064; fp64, 20 000 x 64 x 544, 324 and 281).
-// That has to save a quarter of the time, or the partial sums cost more than it gives (20 011 x 128 x 301, forward and backward 194 us, in three
-// splits, which save a fifth, 214).
+// That has to save a quarter of the time, or the partial sums cost more than it gives (20 011 x 128 x 301, forward and backward 194 us with loads of
+// single words, in three splits, which save a fifth, 214).
 template <class T>
 int64_t gx_splits(int64_t rows, int64_t K, int64_t n) {
   const int64_t blocks = (rows + gx_rows<T>(K) - 1) / gx_rows<T>(K), room = (K > 64 ? 1 : 2) * kMostUnits, steps = (n + 31) / 32;
