@@ -254,8 +254,15 @@ cgtp_status cgtp_norm_create(const char* irreps, int32_t groups, int32_t act, do
         return fail(CGTP_EUNSUPPORTED, std::string("this library targets gfx950, device is ") + prop.gcnArchName);
     }
     try {
-      if (device != -1) cgtp::jit_compile(N.code, -2);
-      if (N.covered && (N.code.scratch > 0 || N.code.agprs > 0)) {   // rows that do not fit the registers after all
+      bool fits = true;     // whether the rows fit the registers, and the code passes the checks
+      try {
+        if (device != -1) cgtp::jit_compile(N.code, -2);
+        fits = N.code.scratch == 0 && N.code.agprs == 0;
+      } catch (const cgtp::RefusedCode&) {
+        if (!N.covered) throw;
+        fits = false;
+      }
+      if (N.covered && !fits) {
         cgtp::emit_norm(N, false);
         cgtp::jit_compile(N.code, -2);
       }

@@ -808,7 +808,9 @@ GRAPH_BWD(cgtp_norm_long_bwd, true)
 )HIP";
 
 // Groups too large for the registers of a wave (more than 64 words a lane, fp64 32): one workgroup for each unit of a sample, whatever its
-// length; the rows are read once for each of mean, variance and result.  A way for rare shapes: bound by the loops of one workgroup a unit.
+// length; the rows are read once for each of mean, variance and result.  A way for rare shapes: bound by the loops of one workgroup a unit.  All
+// lanes make the same steps, those without a row or channel of their own with another's numbers, which do not count: behind a loop that lanes leave at
+// different times the compiler has been seen to place vector instructions that none of them executes.
 const char kUnits[] = R"HIP(
 struct UnitFwd {
   const T* __restrict__ x; const T* __restrict__ weight; const T* __restrict__ bias; T* __restrict__ y; T* __restrict__ stats;
@@ -820,26 +822,35 @@ struct UnitFwd {
     const i64 count = (r1 - r0) * cg;
     double mu = 0, gmu = 0, sq = 0, gsq = 0;
     auto each = [&](auto f) {
-      for (i64 r = r0 + tr; r < r1; r += TR)
-        for (int c = tc; c < cg; c += TC) f(x + r * DX, g * cg + c);
+#pragma unroll cg <= TC && n <= 3 ? 4 : 1
+      for (i64 first = r0; first < r1; first += TR) {
+        const i64 r = TR == 1 || first + tr < r1 ? first + tr : r1 - 1;
+#pragma unroll 4
+        for (int c0 = 0; c0 < cg; c0 += TC) {
+          const bool own = cg % TC == 0 || c0 + tc < cg;
+          f(r, g * cg + (own ? c0 + tc : cg - 1), own && (TR == 1 || first + tr < r1));
+        }
+      }
     };
     if (inv || gated) {
-      each([&](const T* row, int c) {
-        if (inv) mu += row[SEG[s].col + c];
-        if (gated) gmu += row[SEG[s].gate + c];
+      each([&](i64 r, int c, bool in) {
+        const T* row = x + r * DX;
+        if (inv) mu += in ? (double)row[SEG[s].col + c] : 0.0;
+        if (gated) gmu += in ? (double)row[SEG[s].gate + c] : 0.0;
       });
       const double M = count > 0 ? (double)count : 1.0;
       if (inv) mu = block_sum_(mu, lds) / M;
       if (gated) gmu = block_sum_(gmu, lds) / M;
     }
-    each([&](const T* row, int c) {
+    each([&](i64 r, int c, bool in) {
+      const T* row = x + r * DX;
 #pragma unroll
       for (int m = 0; m < n; ++m) {
-        const double d = (double)row[SEG[s].col + at_<s>(c, m)] - mu;
+        const double d = in ? (double)row[SEG[s].col + at_<s>(c, m)] - mu : 0.0;
         sq += d * d;
       }
       if (gated) {
-        const double d = (double)row[SEG[s].gate + c] - gmu;
+        const double d = in ? (double)row[SEG[s].gate + c] - gmu : 0.0;
         gsq += d * d;
       }
     });
@@ -858,17 +869,16 @@ struct UnitFwd {
         st[(SEG[s].gst * G + g) * 2 + 1] = S.gr;
       }
     }
-    for (i64 r = r0 + tr; r < r1; r += TR)
-      for (int c = tc; c < cg; c += TC) {
-        const T* row = x + r * DX;
-        const int ch = g * cg + c;
-        T v[n], gt = gated ? row[SEG[s].gate + ch] : T(0);
+    each([&](i64 r, int ch, bool in) {
+      const T* row = x + r * DX;
+      T v[n], gt = gated ? row[SEG[s].gate + ch] : T(0);
 #pragma unroll
-        for (int m = 0; m < n; ++m) v[m] = row[SEG[s].col + at_<s>(ch, m)];
-        forward_<s>(v, gt, S, param_<s>(weight, bias, ch));
+      for (int m = 0; m < n; ++m) v[m] = row[SEG[s].col + at_<s>(ch, m)];
+      forward_<s>(v, gt, S, param_<s>(weight, bias, ch));
+      if (!in) return;
 #pragma unroll
-        for (int m = 0; m < n; ++m) y[r * DY + SEG[s].ycol + at_<s>(ch, m)] = v[m];
-      }
+      for (int m = 0; m < n; ++m) y[r * DY + SEG[s].ycol + at_<s>(ch, m)] = v[m];
+    });
   }
 };
 extern "C" __global__ void __launch_bounds__(256) cgtp_norm_unit_fwd(const T* __restrict__ x, const T* __restrict__ weight, const T* __restrict__ bias,
@@ -918,17 +928,18 @@ struct UnitBwd {
     };
     double h = 0, hx = 0, gh = 0, ghx = 0;
     for (int c0 = 0; c0 < cg; c0 += TC) {
-      const int ch = g * cg + c0 + tc;
       const bool in = c0 + tc < cg;
+      const int ch = g * cg + (in ? c0 + tc : cg - 1);
       double w = 0, b = 0, gw = 0, gb = 0;
-      if (in) {
-        const Param p = param_<s>(weight, bias, ch);
-        for (i64 r = r0 + tr; r < r1; r += TR) {
-          load(r, ch);
-          const Sums o = backward_<s>(v, gt, q, qg, S, p);
-          w += o.w; b += o.b; gw += o.gw; gb += o.gb;
-          h += o.h; hx += o.hx; gh += o.gh; ghx += o.ghx;
-        }
+      const Param p = param_<s>(weight, bias, ch);
+#pragma unroll n <= 3 ? 4 : 1
+      for (i64 first = r0; first < r1; first += TR) {
+        const bool count = in && first + tr < r1;
+        load(first + tr < r1 ? first + tr : r1 - 1, ch);
+        const Sums o = backward_<s>(v, gt, q, qg, S, p);
+        auto add = [count](double& to, T v) { to += count ? (double)v : 0.0; };
+        add(w, o.w), add(b, o.b), add(gw, o.gw), add(gb, o.gb);
+        add(h, o.h), add(hx, o.hx), add(gh, o.gh), add(ghx, o.ghx);
       }
       double* row = part + sample * (NW + NB);
       column<TC>(w, row + SEG[s].w + ch, in);
@@ -945,16 +956,21 @@ struct UnitBwd {
       e.gh = (T)(block_sum_(gh, lds) / M);
       e.ghx = (T)(block_sum_(ghx, lds) / M);
     }
-    for (i64 r = r0 + tr; r < r1; r += TR)
-      for (int c = tc; c < cg; c += TC) {
-        const int ch = g * cg + c;
+    for (i64 first = r0; first < r1; first += TR) {
+      const i64 r = first + tr < r1 ? first + tr : r1 - 1;
+#pragma unroll n <= 3 ? 4 : 1
+      for (int c0 = 0; c0 < cg; c0 += TC) {
+        const bool in = first + tr < r1 && c0 + tc < cg;
+        const int ch = g * cg + (c0 + tc < cg ? c0 + tc : cg - 1);
         load(r, ch);
         backward_<s>(v, gt, q, qg, S, param_<s>(weight, bias, ch));
         finish_<s>(v, gt, q, qg, S, e);
+        if (!in) continue;
 #pragma unroll
         for (int m = 0; m < n; ++m) gx[r * DX + SEG[s].col + at_<s>(ch, m)] = q[m];
         if (gated) gx[r * DX + SEG[s].gate + ch] = qg;
       }
+    }
   }
 };
 extern "C" __global__ void __launch_bounds__(256) cgtp_norm_unit_bwd(const T* __restrict__ x, const T* __restrict__ weight, const T* __restrict__ bias,
