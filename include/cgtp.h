@@ -362,6 +362,11 @@ cgtp_status cgtp_norm_create(const char* irreps, int32_t groups, int32_t act, do
 cgtp_status cgtp_norm_destroy(cgtp_norm* norm);
 /* which: 0 = columns of x, 1 = columns of y, 2 = number of weights, 3 = number of biases, 4 = numbers in stats per sample. */
 int64_t cgtp_norm_dim(const cgtp_norm* norm, int32_t which);
+/* Name of the (first) kernel that norm_forward (backward == 0) or norm_backward runs; ptr: whether ptr is given.  cgtp_norm_row_* and
+ * cgtp_norm_graph_* hold a row's numbers of a group in registers.  Where a wave's do not hold them (more than 64 words a lane, fp64 32, or
+ * code that the compiler could not fit), cgtp_norm_unit_* serve the call: one workgroup for a group of a segment of a sample, whatever its
+ * length, so that few long samples leave most of the GPU without work.  NULL: norm is NULL. */
+const char* cgtp_norm_kernel(const cgtp_norm* norm, int32_t ptr, int32_t backward);
 /* Workspace of norm_forward (backward == 0) or norm_backward for N rows in S samples; ptr: whether ptr is given. */
 size_t cgtp_norm_workspace_bytes(const cgtp_norm* norm, int64_t N, int64_t S, int32_t ptr, int32_t backward);
 /* x [N, dim 0], y [N, dim 1], stats [S, dim 4].  ptr (int64 device array [S+1], not decreasing): sample s is the rows

@@ -29,7 +29,7 @@ EXPORTS = [
     "cgtp_conv_double_workspace_bytes", "conv_forward_atomic", "conv_backward_atomic",
     "cgtp_csr_from_coo", "cgtp_csr_from_coo_async", "cgtp_csr_workspace_bytes", "cgtp_last_error", "cgtp_check_code_object",
     "gated_forward", "gated_backward", "cgtp_gated_workspace_bytes",
-    "cgtp_norm_create", "cgtp_norm_destroy", "cgtp_norm_dim", "cgtp_norm_workspace_bytes", "norm_forward", "norm_backward",
+    "cgtp_norm_create", "cgtp_norm_destroy", "cgtp_norm_dim", "cgtp_norm_kernel", "cgtp_norm_workspace_bytes", "norm_forward", "norm_backward",
 ]
 
 
@@ -104,6 +104,8 @@ def lib() -> C.CDLL:
     L.cgtp_norm_destroy.argtypes = [vp]
     L.cgtp_norm_dim.argtypes = [vp, i32]
     L.cgtp_norm_dim.restype = i64
+    L.cgtp_norm_kernel.argtypes = [vp, i32, i32]
+    L.cgtp_norm_kernel.restype = C.c_char_p
     L.cgtp_norm_workspace_bytes.argtypes = [vp, i64, i64, i32, i32]
     L.cgtp_norm_workspace_bytes.restype = C.c_size_t
     L.norm_forward.argtypes = [vp] * 6 + [i64, i64, vp, vp, C.c_size_t, vp]
@@ -451,6 +453,10 @@ class Norm:
         _check(L.cgtp_norm_create(irreps.encode(), groups, act, eps, dtype, device, flags | (CGTP_NORM_GATED if gated else 0), C.byref(h)))
         self._h, self.dtype, self.groups = h, dtype, groups
         self.dim_x, self.dim_y, self.n_w, self.n_b, self.n_stat = (L.cgtp_norm_dim(h, t) for t in range(5))
+
+    def kernel(self, ptr: bool, backward: bool) -> str:
+        """Name of the (first) kernel that a call runs; ptr: whether ptr is given."""
+        return lib().cgtp_norm_kernel(self._h, ptr, backward).decode()
 
     def close(self):
         if getattr(self, "_h", None):

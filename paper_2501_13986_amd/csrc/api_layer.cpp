@@ -75,7 +75,8 @@ struct NormWork {
     auto up = [](size_t v) { return (v + 255) / 256 * 256; };
     const size_t units = P.seg.size() * (size_t)P.groups;
     const int64_t most = 1 << 23;   // workgroups of a launch: 2^32 threads are too many (a normalisation has at most 2^14 sub-units)
-    if (!P.covered) {
+    const bool any = P.call[(ptr ? cgtp::kGraphsForward : cgtp::kRowsForward) + backward].any;
+    if (any) {
       blocks = std::min<int64_t>(S * (int64_t)units, 1 << 20);
       sum_rows = S;
     } else if (!ptr) {
@@ -100,21 +101,57 @@ struct NormWork {
       sum_rows = longer ? blocks + long_blocks : blocks;
       if (longer) part = up((size_t)chunks * 2 * units * 4 * sizeof(double));
     }
-    bytes = part + (backward && (sum_rows > 1 || !P.covered) ? up((size_t)sum_rows * (size_t)(P.n_w + P.n_b) * sizeof(double)) : 0);
+    bytes = part + (backward && (sum_rows > 1 || any) ? up((size_t)sum_rows * (size_t)(P.n_w + P.n_b) * sizeof(double)) : 0);
   }
 };
 
-struct Function {
-  hipFunction_t* fn;
-  const char* name;
-};
+// Compiles the kernels of the four calls, each with what fits it.  Registers that the code moves about are no place for a row's words (lanes of a
+// wave are masked off in these kernels, and the compiler has been seen to move under a mask what all lanes need), and refused code is
+// no code: such a call takes the kernels for any size.
+void compile(cgtp::Norm& N) {
+  bool any[2] = {};
+  for (int i = 0; i < cgtp::kNormCalls; ++i) {
+    cgtp::NormCall& c = N.call[i];
+    try {
+      cgtp::jit_compile(c.code, -2);
+      c.any = c.any || c.code.relocates;
+    } catch (const cgtp::RefusedCode&) {
+      c.any = true;
+    }
+    if (c.any) c.code = cgtp::Kernel();
+    any[i % 2] |= c.any;
+  }
+  for (int i = 0; i < 2; ++i) {
+    if (!any[i]) N.any[i] = cgtp::Kernel();
+    cgtp::jit_compile(N.any[i], -2);
+    if (N.any[i].relocates) throw cgtp::RefusedCode(N.any[i].name + ": the compiled code relocates registers; the kernel is not used");
+  }
+}
 
-// the functions of a normalisation's module
-std::vector<Function> functions(cgtp::Norm& N) {
-  if (!N.covered) return {{&N.unit_fwd, "cgtp_norm_unit_fwd"}, {&N.unit_bwd, "cgtp_norm_unit_bwd"}, {&N.sums, "cgtp_norm_sums"}};
-  return {{&N.row_fwd, "cgtp_norm_row_fwd"},     {&N.row_bwd, "cgtp_norm_row_bwd"},     {&N.graph_fwd, "cgtp_norm_graph_fwd"},
-          {&N.long_fwd, "cgtp_norm_long_fwd"},   {&N.graph_bwd, "cgtp_norm_graph_bwd"}, {&N.long_bwd, "cgtp_norm_long_bwd"},
-          {&N.sums, "cgtp_norm_sums"}};
+hipFunction_t function(const cgtp::Kernel& k, const char* name) {
+  hipFunction_t f = nullptr;
+  const hipError_t e = hipModuleGetFunction(&f, k.module, name);
+  if (e != hipSuccess) throw std::runtime_error(std::string("hipModuleGetFunction failed for ") + name + ": " + hipGetErrorString(e));
+  return f;
+}
+
+void load(cgtp::Norm& N, int device) {
+  for (int i = 0; i < cgtp::kNormCalls; ++i) {
+    cgtp::NormCall& c = N.call[i];
+    if (c.any) continue;
+    cgtp::jit_compile(c.code, device);
+    if (i == cgtp::kGraphsForward) c.longer = function(c.code, "cgtp_norm_long_fwd");
+    if (i == cgtp::kGraphsBackward) c.longer = function(c.code, "cgtp_norm_long_bwd");
+    if (i % 2) c.sums = function(c.code, "cgtp_norm_sums");
+  }
+  for (cgtp::Kernel& k : N.any) cgtp::jit_compile(k, device);
+  if (N.any[1].module) N.any_sums = function(N.any[1], "cgtp_norm_sums");
+  N.loaded = true;
+}
+
+void unload(cgtp::Norm& N) {
+  for (cgtp::NormCall& c : N.call) cgtp::jit_unload(c.code);
+  for (cgtp::Kernel& k : N.any) cgtp::jit_unload(k);
 }
 
 }  // namespace
@@ -254,26 +291,10 @@ cgtp_status cgtp_norm_create(const char* irreps, int32_t groups, int32_t act, do
         return fail(CGTP_EUNSUPPORTED, std::string("this library targets gfx950, device is ") + prop.gcnArchName);
     }
     try {
-      bool fits = true;     // whether the rows fit the registers, and the code passes the checks
-      try {
-        if (device != -1) cgtp::jit_compile(N.code, -2);
-        fits = N.code.scratch == 0 && N.code.agprs == 0;
-      } catch (const cgtp::RefusedCode&) {
-        if (!N.covered) throw;
-        fits = false;
-      }
-      if (N.covered && !fits) {
-        cgtp::emit_norm(N, false);
-        cgtp::jit_compile(N.code, -2);
-      }
-      cgtp::jit_compile(N.code, device);
-      if (device >= 0)
-        for (const Function& f : functions(N)) {
-          hipError_t e = hipModuleGetFunction(f.fn, N.code.module, f.name);
-          if (e != hipSuccess) throw std::runtime_error(std::string("hipModuleGetFunction failed for ") + f.name + ": " + hipGetErrorString(e));
-        }
+      if (device != -1) compile(N);
+      if (device >= 0) load(N, device);
     } catch (const std::exception& e) {
-      cgtp::jit_unload(N.code);
+      unload(N);
       return fail(CGTP_ECOMPILE, e.what());
     }
     *out = H.release();
@@ -287,7 +308,7 @@ cgtp_status cgtp_norm_create(const char* irreps, int32_t groups, int32_t act, do
 
 cgtp_status cgtp_norm_destroy(cgtp_norm* norm) {
   if (!norm) return CGTP_OK;
-  cgtp::jit_unload(norm->N.code);
+  unload(norm->N);
   delete norm;
   return CGTP_OK;
 }
@@ -303,6 +324,13 @@ int64_t cgtp_norm_dim(const cgtp_norm* norm, int32_t which) {
     case 4: return N.n_stat;
     default: return -1;
   }
+}
+
+const char* cgtp_norm_kernel(const cgtp_norm* norm, int32_t ptr, int32_t backward) {
+  if (!norm) return nullptr;
+  const int direction = backward != 0;
+  const cgtp::NormCall& c = norm->N.call[(ptr ? cgtp::kGraphsForward : cgtp::kRowsForward) + direction];
+  return (c.any ? norm->N.any[direction] : c.code).name.c_str();
 }
 
 size_t cgtp_norm_workspace_bytes(const cgtp_norm* norm, int64_t N, int64_t S, int32_t ptr, int32_t backward) {
@@ -321,7 +349,7 @@ cgtp_status check_norm(const cgtp_norm* norm, int64_t N, int64_t S, const int64_
   if (N > INT32_MAX || S > INT32_MAX) return fail(CGTP_EUNSUPPORTED, "N and S must be below 2^31");
   for (const void* p : data)
     if (!aligned(p, 16)) return fail(CGTP_EINVAL, "data pointers must be 16-byte aligned");
-  if (!norm->N.sums) return fail(CGTP_EUNSUPPORTED, "kernel " + norm->N.code.name + " is not loaded (created without a device?)");
+  if (!norm->N.loaded) return fail(CGTP_EUNSUPPORTED, "the normalisation's kernels are not loaded (created without a device?)");
   int current = -1;      // its kernels are on one device
   HIP_TRY(hipGetDevice(&current));
   if (current != norm->N.device) return fail(CGTP_EINVAL, "the normalisation's device is not the current device");
@@ -348,17 +376,18 @@ cgtp_status norm_forward(const cgtp_norm* norm, const void* x, const void* weigh
   if (!workspace_serves(workspace, workspace_bytes, w.bytes)) return bad_workspace("cgtp_norm_workspace_bytes", w.bytes);
   hipStream_t st = (hipStream_t)hip_stream;
   double* part = (double*)workspace;
-  if (!P.covered) {
+  const cgtp::NormCall& c = P.call[ptr ? cgtp::kGraphsForward : cgtp::kRowsForward];
+  if (c.any) {
     void* args[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&y, (void*)&stats, (void*)&N, (void*)&S, (void*)&ptr};
-    return launch(P.unit_fwd, w.blocks, args, st);
+    return launch(P.any[0].fn, w.blocks, args, st);
   }
   if (!ptr) {
     void* args[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&y, (void*)&stats, (void*)&N};
-    return launch(P.row_fwd, w.blocks * P.subs, args, st);
+    return launch(c.code.fn, w.blocks * P.subs, args, st);
   }
   void* args[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&y, (void*)&stats, (void*)&part, (void*)&ptr, (void*)&N, (void*)&S, (void*)&w.R, (void*)&w.D};
-  s = launch(P.graph_fwd, w.blocks * P.subs, args, st);
-  return s != CGTP_OK || !w.longer ? s : launch(P.long_fwd, w.long_blocks * P.subs, args, st);
+  s = launch(c.code.fn, w.blocks * P.subs, args, st);
+  return s != CGTP_OK || !w.longer ? s : launch(c.longer, w.long_blocks * P.subs, args, st);
 }
 
 cgtp_status norm_backward(const cgtp_norm* norm, const void* x, const void* weight, const void* bias, const void* gy,
@@ -378,24 +407,25 @@ cgtp_status norm_backward(const cgtp_norm* norm, const void* x, const void* weig
   const NormWork w(P, N, S, ptr != nullptr, true);
   if (!workspace_serves(workspace, workspace_bytes, w.bytes)) return bad_workspace("cgtp_norm_workspace_bytes", w.bytes);
   double* part = (double*)workspace;
-  double* sums = w.sum_rows > 1 || !P.covered ? (double*)((char*)workspace + w.part) : nullptr;
-  if (!P.covered) {
+  const cgtp::NormCall& c = P.call[ptr ? cgtp::kGraphsBackward : cgtp::kRowsBackward];
+  double* sums = w.sum_rows > 1 || c.any ? (double*)((char*)workspace + w.part) : nullptr;
+  if (c.any) {
     void* args[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&gy, (void*)&stats, (void*)&gx, (void*)&sums, (void*)&N, (void*)&S, (void*)&ptr};
-    s = launch(P.unit_bwd, w.blocks, args, st);
+    s = launch(P.any[1].fn, w.blocks, args, st);
   } else if (!ptr) {
     void* args[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&gy, (void*)&stats, (void*)&gx, (void*)&sums, (void*)&gweight, (void*)&gbias, (void*)&N};
-    s = launch(P.row_bwd, w.blocks * P.subs, args, st);
+    s = launch(c.code.fn, w.blocks * P.subs, args, st);
   } else {
     double* more = sums ? sums + w.blocks * (P.n_w + P.n_b) : nullptr;
     void* args[] = {(void*)&x, (void*)&weight, (void*)&bias, (void*)&gy, (void*)&stats, (void*)&gx, (void*)&part, (void*)&sums, (void*)&gweight, (void*)&gbias,
                     (void*)&ptr, (void*)&N, (void*)&S, (void*)&w.R, (void*)&w.D};
-    s = launch(P.graph_bwd, w.blocks * P.subs, args, st);
+    s = launch(c.code.fn, w.blocks * P.subs, args, st);
     args[7] = (void*)&more;
-    if (s == CGTP_OK && w.longer) s = launch(P.long_bwd, w.long_blocks * P.subs, args, st);
+    if (s == CGTP_OK && w.longer) s = launch(c.longer, w.long_blocks * P.subs, args, st);
   }
   if (s != CGTP_OK || !sums) return s;
   void* args[] = {(void*)&sums, (void*)&w.sum_rows, (void*)&gweight, (void*)&gbias};
-  return launch(P.sums, (P.n_w + P.n_b + 15) / 16, args, st, 1024);
+  return launch(c.any ? P.any_sums : c.sums, (P.n_w + P.n_b + 15) / 16, args, st, 1024);
 }
 
 }  // extern "C"

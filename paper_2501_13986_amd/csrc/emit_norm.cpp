@@ -401,7 +401,7 @@ __device__ inline i64 part_() { return blockIdx.x / NSUB; }
 // and six levels.  Bound by memory: 20 000 rows of 128 channels, l <= 3 with gates (359 MB forward, 554 MB backward), IR_MUL forward 65 to 75 us (4.8 to
 // 5.5 TB/s, a copy 4.95), MUL_IR forward and backward 207 to 223 us (4.1 to 4.4 TB/s).  Backward keeps the sums of its channels over all its rows in
 // registers: as many workgroups as stay on the chip, one row of partial sums each.
-const char kRowsText[] = R"HIP(
+const char kRowFwd[] = R"HIP(
 struct RowFwd {
   const T* __restrict__ x; const T* __restrict__ weight; const T* __restrict__ bias; T* __restrict__ y; T* __restrict__ stats; i64 N; int phase;
   template <int s> __device__ void operator()() const {
@@ -446,7 +446,9 @@ extern "C" __global__ void __launch_bounds__(256) cgtp_norm_row_fwd(const T* __r
                                                                 T* __restrict__ y, T* __restrict__ stats, i64 N) {
   with_sub_(sub_(), RowFwd{x, weight, bias, y, stats, N, SUB[sub_()].phase});
 }
+)HIP";
 
+const char kRowBwd[] = R"HIP(
 struct RowBwd {
   const T* __restrict__ x; const T* __restrict__ weight; const T* __restrict__ bias; const T* __restrict__ gy; const T* __restrict__ stats;
   T* __restrict__ gx; double* __restrict__ sums; T* __restrict__ gweight; T* __restrict__ gbias; i64 N; int phase; double* lds;
@@ -657,6 +659,9 @@ template <int s> __device__ inline Stat stat_of_(const double (&t)[4], const Shi
   return S;
 }
 
+)HIP";
+
+const char kGraphFwd[] = R"HIP(
 // kLong: the second kernel
 template <bool kLong> struct GraphFwd {
   const T* __restrict__ x; const T* __restrict__ weight; const T* __restrict__ bias; T* __restrict__ y; T* __restrict__ stats; double* __restrict__ part;
@@ -727,7 +732,9 @@ template <bool kLong> struct GraphFwd {
   }
 GRAPH_FWD(cgtp_norm_graph_fwd, false)
 GRAPH_FWD(cgtp_norm_long_fwd, true)
+)HIP";
 
+const char kGraphBwd[] = R"HIP(
 template <int s> __device__ inline Means means_of_(const double (&t)[4], i64 rows) {
   const double inv = rows > 0 ? 1.0 / ((double)rows * Lane<s>::cg) : 1.0;
   return Means{(T)(t[0] * inv), (T)(t[1] * inv * (1.0 / Lane<s>::n)), (T)(t[2] * inv), (T)(t[3] * inv)};
@@ -807,11 +814,14 @@ GRAPH_BWD(cgtp_norm_graph_bwd, false)
 GRAPH_BWD(cgtp_norm_long_bwd, true)
 )HIP";
 
-// Groups too large for the registers of a wave (more than 64 words a lane, fp64 32): one workgroup for each unit of a sample, whatever its
-// length; the rows are read once for each of mean, variance and result.  A way for rare shapes: bound by the loops of one workgroup a unit.  All
+// Calls whose kernels above do not fit the registers of a wave: more than 64 words a lane (fp64 32), or code that relocates registers or is refused.  Backward
+// holds twice the words of forward and the channels' sums: of one group in fp32 forward fits up to about 2048 channels x components of a segment, backward up
+// to about 1024, in fp64 half of that.  One workgroup for each unit of a sample, whatever its length; the rows are read once for each of mean, variance
+// and result.  Rows as samples, 20 000 x 8192x0e fp32: forward 376 us (3.5 TB/s; 49 us and 6.7 for 2048x0e in registers); bound by the loops of one workgroup
+// where samples are long: one of 20 000 rows of 512x0e+512x1o backward 32 ms (forward in registers 106 us).  All
 // lanes make the same steps, those without a row or channel of their own with another's numbers, which do not count: behind a loop that lanes leave at
 // different times the compiler has been seen to place vector instructions that none of them executes.
-const char kUnits[] = R"HIP(
+const char kUnitFwd[] = R"HIP(
 struct UnitFwd {
   const T* __restrict__ x; const T* __restrict__ weight; const T* __restrict__ bias; T* __restrict__ y; T* __restrict__ stats;
   i64 r0, r1, sample; int g; double* lds;
@@ -892,7 +902,9 @@ extern "C" __global__ void __launch_bounds__(256) cgtp_norm_unit_fwd(const T* __
     with_segment_<0>(unit / G, UnitFwd{x, weight, bias, y, stats, r0, r1, sample, unit % G, lds});
   }
 }
+)HIP";
 
+const char kUnitBwd[] = R"HIP(
 struct UnitBwd {
   const T* __restrict__ x; const T* __restrict__ weight; const T* __restrict__ bias; const T* __restrict__ gy; const T* __restrict__ stats;
   T* __restrict__ gx; double* __restrict__ part; i64 r0, r1, sample; int g; double* lds; double* cols;
@@ -1011,10 +1023,10 @@ extern "C" __global__ void __launch_bounds__(1024) cgtp_norm_sums(const double* 
 
 }  // namespace
 
-void emit_norm(Norm& N, bool covered) {
+void emit_norm(Norm& N) {
   const bool f64 = N.dtype == CGTP_F64;
   const int most = f64 ? 32 : 64;          // words a lane holds of a row
-  N.covered = covered;
+  bool covered = true;
   struct Sub {
     int s, phase, size;
   };
@@ -1039,8 +1051,8 @@ void emit_norm(Norm& N, bool covered) {
       if (N.groups % g == 0 && g * s.lanes <= 64) s.at_once = g;
     s.rows = 64 / (s.at_once * s.lanes);
     s.phases = N.groups / s.at_once;
-    if (s.V * s.J * s.n > most || s.phases > 256) N.covered = false;
-    for (int p = 0; N.covered && p < s.phases; ++p) subs.push_back({(int)i, p, s.at_once * cg * (s.n + (s.gate >= 0))});
+    if (s.V * s.J * s.n > most || s.phases > 256) covered = false;
+    for (int p = 0; covered && p < s.phases; ++p) subs.push_back({(int)i, p, s.at_once * cg * (s.n + (s.gate >= 0))});
   }
   std::stable_sort(subs.begin(), subs.end(), [](const Sub& a, const Sub& b) { return a.size > b.size; });
   N.subs = (int)subs.size();
@@ -1057,19 +1069,27 @@ void emit_norm(Norm& N, bool covered) {
       << ", " << s.b << ", " << s.gw << ", " << s.gb << ", " << s.st << ", " << s.gst << ", " << s.V << ", " << s.J << ", " << s.lanes << ", " << s.at_once
       << ", " << s.rows << ", " << (s.vec ? "true" : "false") << "},\n";
   o << "};\n";
-  if (N.covered) {
+  if (covered) {
     o << "struct Sub { int s, phase; };\n__constant__ constexpr Sub SUB[NSUB] = {";
     for (const Sub& s : subs) o << "{" << s.s << ", " << s.phase << "}, ";
     o << "};\n";
   }
   o << kShared;
-  if (N.covered) o << kLanes << kRowsText << kGraphs;
-  else o << kUnits;
-  o << kSums;
-  N.code = Kernel();
-  N.code.name = "cgtp_norm_sums";
-  N.code.wg = 256;
-  N.code.source = o.str();
+  auto kernel = [&o](const char* name, std::initializer_list<const char*> text) {
+    Kernel k;
+    k.name = name;
+    k.source = o.str();
+    for (const char* t : text) k.source += t;
+    return k;
+  };
+  N.any[0] = kernel("cgtp_norm_unit_fwd", {kUnitFwd});
+  N.any[1] = kernel("cgtp_norm_unit_bwd", {kUnitBwd, kSums});
+  for (NormCall& c : N.call) c.any = !covered;
+  if (!covered) return;
+  N.call[kRowsForward].code = kernel("cgtp_norm_row_fwd", {kLanes, kRowFwd});
+  N.call[kRowsBackward].code = kernel("cgtp_norm_row_bwd", {kLanes, kRowBwd, kSums});
+  N.call[kGraphsForward].code = kernel("cgtp_norm_graph_fwd", {kLanes, kGraphs, kGraphFwd});
+  N.call[kGraphsBackward].code = kernel("cgtp_norm_graph_bwd", {kLanes, kGraphs, kGraphBwd, kSums});
 }
 
 }  // namespace cgtp

@@ -319,6 +319,7 @@ static void compile_and_check(Kernel& k) {
   if (v_ >= 0) k.scratch = (int)v_;
   v_ = metadata_int(code, ".group_segment_fixed_size");
   if (v_ >= 0) k.lds = (int)v_;
+  k.relocates = k.agprs > 0 || std::any_of(ins.begin(), ins.end(), [](const std::string& t) { return starts_with(t, "scratch_"); });
   k.code = std::move(code);
 }
 

@@ -81,6 +81,8 @@ struct Kernel {
   hipModule_t module = nullptr;
   hipFunction_t fn = nullptr;
   int vgprs = 0, agprs = 0, sgprs = 0, lds = 0, scratch = 0;  // vgprs counts both register kinds
+  bool relocates = false;   // the code keeps values in accumulation registers or in private memory (scratch > 0 alone may be room that no
+                            // instruction uses: scalar registers that went to the lanes of a vector register)
   Schedule sched;
   // uvu kernels: refuse compiled code that both changes the execution mask (a lane-conditional region or loop) and
   // relocates registers (accumulation registers or private memory in use); see jit_compile

@@ -17,3 +17,30 @@ def test_wide_groups(irreps, ir_mul, prec):
         for ptr in (None, [0, 5, 5, 11], [2, 12]):
             p = inputs(n, 12, prec, seed=3)
             compare(run(n, p, ptr), irreps, 1, act, gated, ir_mul, p, prec, ptr)
+
+
+# one of the four calls at least is served by the kernels for any size, the others by registers
+MIXED = [("512x0e+512x1o", 1), ("2048x0e", 1), ("1536x0e", 1), ("256x0e+256x1o+256x2e+256x3o", 1), ("1024x0e", 1)]
+
+
+@pytest.mark.parametrize("prec", ["f32", "f64"])
+@pytest.mark.parametrize("irreps,groups", MIXED)
+def test_calls_with_kernels_of_both_kinds(irreps, groups, prec):
+    """Forward and backward exchange statistics and nothing else; samples longer than a chunk among them."""
+    n = handle(irreps, groups, layer.SILU, True, prec, False)
+    for N, ptr in ((5, None), (300, [0, 300]), (290, [0, 3, 3, 40, 200, 287])):
+        p = inputs(n, N, prec, seed=N)
+        compare(run(n, p, ptr), irreps, groups, layer.SILU, True, False, p, prec, ptr)
+
+
+# scalar registers that went to a vector register's lanes leave room for private memory that nothing uses
+ROOM = [("48x0e+10x1o+10x1e+48x0o", 1), ("7x0e+5x1o+3x2e+9x0e", 1), ("32x0e+32x1o+32x2e+32x3o", 1), ("4x0e+4x1o+4x1e+4x2e", 4)]
+
+
+@pytest.mark.parametrize("prec", ["f32", "f64"])
+@pytest.mark.parametrize("irreps,groups", ROOM)
+def test_code_with_unused_private_room(irreps, groups, prec):
+    n = handle(irreps, groups, layer.NONE, True, prec, True)
+    for N, ptr in ((7, None), (1000, [0, 1000]), (900, [0, 2, 2, 60, 500, 899])):
+        p = inputs(n, N, prec, seed=N)
+        compare(run(n, p, ptr), irreps, groups, layer.NONE, True, True, p, prec, ptr)
