@@ -815,17 +815,31 @@ GRAPH_BWD(cgtp_norm_long_bwd, true)
 )HIP";
 
 // Calls whose kernels above do not fit the registers of a wave: more than 64 words a lane (fp64 32), or code that relocates registers or is refused.  Backward
-// holds twice the words of forward and the channels' sums: of one group in fp32 forward fits up to about 2048 channels x components of a segment, backward up
-// to about 1024, in fp64 half of that.  One workgroup for each unit of a sample, whatever its length; the rows are read once for each of mean, variance
+// holds twice the words of forward and the channels' sums: groups of 512 x 0e + 512 x 1o fit forward and, as rows, backward in fp32, 2048 x 0e forward alone, 512 x 3o
+// in fp64 neither.  One workgroup for each unit of a sample, whatever its length; the rows are read once for each of mean, variance
 // and result.  Rows as samples, 20 000 x 8192x0e fp32: forward 376 us (3.5 TB/s; 49 us and 6.7 for 2048x0e in registers); bound by the loops of one workgroup
 // where samples are long: one of 20 000 rows of 512x0e+512x1o backward 32 ms (forward in registers 106 us).  All
 // lanes make the same steps, those without a row or channel of their own with another's numbers, which do not count: behind a loop that lanes leave at
 // different times the compiler has been seen to place vector instructions that none of them executes.
+const char kUnits[] = R"HIP(
+// a workgroup has one unit of every so many samples (and backward a row of partial sums for all of them)
+__device__ inline int unit_() { return (int)(blockIdx.x % (NS * G)); }
+__device__ inline i64 first_() { return blockIdx.x / (NS * G); }
+__device__ inline i64 apart_() { return gridDim.x / (NS * G); }
+)HIP";
+
 const char kUnitFwd[] = R"HIP(
 struct UnitFwd {
   const T* __restrict__ x; const T* __restrict__ weight; const T* __restrict__ bias; T* __restrict__ y; T* __restrict__ stats;
-  i64 r0, r1, sample; int g; double* lds;
+  i64 N, S; const i64* __restrict__ ptr; int g; double* lds;
   template <int s> __device__ void operator()() const {
+    for (i64 sample = first_(); sample < S; sample += apart_()) {
+      i64 r0, r1;
+      range_(ptr, sample, N, r0, r1);
+      one<s>(sample, r0, r1);
+    }
+  }
+  template <int s> __device__ void one(i64 sample, i64 r0, i64 r1) const {
     constexpr int n = SEG[s].n, cg = SEG[s].mul / G, TC = pow2_(cg) < 256 ? pow2_(cg) : 256, TR = 256 / TC;
     constexpr bool gated = SEG[s].gate >= 0, inv = SEG[s].inv;
     const int tc = threadIdx.x % TC, tr = threadIdx.x / TC;
@@ -894,32 +908,33 @@ struct UnitFwd {
 extern "C" __global__ void __launch_bounds__(256) cgtp_norm_unit_fwd(const T* __restrict__ x, const T* __restrict__ weight, const T* __restrict__ bias,
                                                             T* __restrict__ y, T* __restrict__ stats, i64 N, i64 S, const i64* __restrict__ ptr) {
   __shared__ double lds[4];
-  for (i64 u = blockIdx.x; u < S * NS * G; u += gridDim.x) {
-    const i64 sample = u / (NS * G);
-    const int unit = (int)(u % (NS * G));
-    i64 r0, r1;
-    range_(ptr, sample, N, r0, r1);
-    with_segment_<0>(unit / G, UnitFwd{x, weight, bias, y, stats, r0, r1, sample, unit % G, lds});
-  }
+  with_segment_<0>(unit_() / G, UnitFwd{x, weight, bias, y, stats, N, S, ptr, unit_() % G, lds});
 }
 )HIP";
 
 const char kUnitBwd[] = R"HIP(
 struct UnitBwd {
   const T* __restrict__ x; const T* __restrict__ weight; const T* __restrict__ bias; const T* __restrict__ gy; const T* __restrict__ stats;
-  T* __restrict__ gx; double* __restrict__ part; i64 r0, r1, sample; int g; double* lds; double* cols;
-  // sum over the rows' threads of a channel, into to[] for channel c < cg
-  template <int TC> __device__ void column(double v, double* to, bool in) const {
-    __syncthreads();
-    cols[threadIdx.x] = v;
-    __syncthreads();
-    if ((int)threadIdx.x < TC && in) {
-      double t = 0;
-      for (int i = 0; i < 256; i += TC) t += cols[threadIdx.x + i];
-      *to = t;
+  T* __restrict__ gx; double* __restrict__ row; i64 N, S; const i64* __restrict__ ptr; int g; double* lds; double* cols;
+  // sum over the rows' threads of a channel, for channel c < cg: written or added to what the same thread left of the samples before
+  template <int TC> __device__ void column(double v, double* to, bool in, bool more) const {
+    if constexpr (TC < 256) {
+      __syncthreads();
+      cols[threadIdx.x] = v;
+      __syncthreads();
+      v = 0;
+      for (int i = 0; i < 256; i += TC) v += cols[threadIdx.x % TC + i];
     }
+    if ((int)threadIdx.x < TC && in) *to = more ? *to + v : v;
   }
   template <int s> __device__ void operator()() const {
+    for (i64 sample = first_(); sample < S; sample += apart_()) {
+      i64 r0, r1;
+      range_(ptr, sample, N, r0, r1);
+      if (r0 < r1 || sample == first_()) one<s>(sample, r0, r1, sample != first_());
+    }
+  }
+  template <int s> __device__ void one(i64 sample, i64 r0, i64 r1, bool more) const {
     constexpr int n = SEG[s].n, cg = SEG[s].mul / G, TC = pow2_(cg) < 256 ? pow2_(cg) : 256, TR = 256 / TC;
     constexpr bool gated = SEG[s].gate >= 0, inv = SEG[s].inv;
     const int tc = threadIdx.x % TC, tr = threadIdx.x / TC;
@@ -953,12 +968,11 @@ struct UnitBwd {
         add(w, o.w), add(b, o.b), add(gw, o.gw), add(gb, o.gb);
         add(h, o.h), add(hx, o.hx), add(gh, o.gh), add(ghx, o.ghx);
       }
-      double* row = part + sample * (NW + NB);
-      column<TC>(w, row + SEG[s].w + ch, in);
-      if (inv) column<TC>(b, row + NW + SEG[s].b + ch, in);
+      column<TC>(w, row + SEG[s].w + ch, in, more);
+      if (inv) column<TC>(b, row + NW + SEG[s].b + ch, in, more);
       if (gated) {
-        column<TC>(gw, row + SEG[s].gw + ch, in);
-        column<TC>(gb, row + NW + SEG[s].gb + ch, in);
+        column<TC>(gw, row + SEG[s].gw + ch, in, more);
+        column<TC>(gb, row + NW + SEG[s].gb + ch, in, more);
       }
     }
     const double M = r1 > r0 ? (double)(r1 - r0) * cg : 1.0;
@@ -989,13 +1003,7 @@ extern "C" __global__ void __launch_bounds__(256) cgtp_norm_unit_bwd(const T* __
                                                             const T* __restrict__ gy, const T* __restrict__ stats, T* __restrict__ gx,
                                                             double* __restrict__ part, i64 N, i64 S, const i64* __restrict__ ptr) {
   __shared__ double lds[4], cols[256];
-  for (i64 u = blockIdx.x; u < S * NS * G; u += gridDim.x) {
-    const i64 sample = u / (NS * G);
-    const int unit = (int)(u % (NS * G));
-    i64 r0, r1;
-    range_(ptr, sample, N, r0, r1);
-    with_segment_<0>(unit / G, UnitBwd{x, weight, bias, gy, stats, gx, part, r0, r1, sample, unit % G, lds, cols});
-  }
+  with_segment_<0>(unit_() / G, UnitBwd{x, weight, bias, gy, stats, gx, part + first_() * (NW + NB), N, S, ptr, unit_() % G, lds, cols});
 }
 )HIP";
 
@@ -1082,8 +1090,8 @@ void emit_norm(Norm& N) {
     for (const char* t : text) k.source += t;
     return k;
   };
-  N.any[0] = kernel("cgtp_norm_unit_fwd", {kUnitFwd});
-  N.any[1] = kernel("cgtp_norm_unit_bwd", {kUnitBwd, kSums});
+  N.any[0] = kernel("cgtp_norm_unit_fwd", {kUnits, kUnitFwd});
+  N.any[1] = kernel("cgtp_norm_unit_bwd", {kUnits, kUnitBwd, kSums});
   for (NormCall& c : N.call) c.any = !covered;
   if (!covered) return;
   N.call[kRowsForward].code = kernel("cgtp_norm_row_fwd", {kLanes, kRowFwd});

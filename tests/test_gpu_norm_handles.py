@@ -2,7 +2,7 @@
 import pytest
 
 from oracle import layer
-from tests.test_gpu_norm import compare, handle, inputs, run
+from tests.test_gpu_norm import compare, handle, inputs, run, torch
 from tests.test_layer_handles import WIDE
 
 pytestmark = pytest.mark.gpu
@@ -44,3 +44,20 @@ def test_code_with_unused_private_room(irreps, groups, prec):
     for N, ptr in ((7, None), (1000, [0, 1000]), (900, [0, 2, 2, 60, 500, 899])):
         p = inputs(n, N, prec, seed=N)
         compare(run(n, p, ptr), irreps, groups, layer.NONE, True, True, p, prec, ptr)
+
+
+@pytest.mark.parametrize("prec", ["f32", "f64"])
+@pytest.mark.parametrize("irreps,groups,N", [("300x8e", 1, 2600), ("700x0e+512x3o", 1, 2300), ("96x7o", 1, 2500), ("260x6e", 2, 1300)])
+def test_more_samples_than_rows_of_partial_sums(irreps, groups, N, prec):
+    """A workgroup has several samples, some without rows, also the first."""
+    n = handle(irreps, groups, layer.SILU, True, prec, False)
+    if irreps != "96x7o":      # which is held in registers
+        assert "cgtp_norm_unit_bwd" in (n.kernel(True, True), n.kernel(False, True))
+    p = inputs(n, N, prec, seed=N)
+    ends = sorted([0, 0, 0, 1, 1, N] + [min(N, 2 * i // 3) for i in range(N)])
+    for ptr in (None, ends):
+        got = run(n, p, ptr)
+        compare(got, irreps, groups, layer.SILU, True, False, p, prec, ptr)
+        again = run(n, p, ptr)
+        for k in got:
+            assert torch.equal(torch.nan_to_num(got[k]), torch.nan_to_num(again[k])), k

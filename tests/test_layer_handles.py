@@ -67,3 +67,15 @@ def test_kernel_names_without_compiling():
     n = b.Norm("4x0e+4x1o", device=-1)
     assert [n.kernel(ptr, backward) for ptr in (False, True) for backward in (False, True)] == REGISTERS
     assert b.lib().cgtp_norm_kernel(None, 0, 0) is None
+
+
+@pytest.mark.parametrize("irreps", ["8192x0e", "2048x0e", "65536x0e+65536x1o", "5000x0e+300x8e"])
+def test_workspace_does_not_grow_with_the_samples(irreps):
+    """Partial sums of the parameters' gradients are one row a workgroup, as many as fill the chip, not one a sample."""
+    n = b.Norm(irreps, device=-2)
+    assert n.kernel(False, True) == "cgtp_norm_unit_bwd"
+    of = lambda N, S, ptr: b.lib().cgtp_norm_workspace_bytes(n._h, N, S, ptr, 1)  # noqa: E731
+    row = 8 * (n.n_w + n.n_b)
+    few = (256 << 20) + 256 * row + 256
+    assert of(1_000_000, 1_000_000, 0) == of(50_000_000, 50_000_000, 0) <= few
+    assert of(1_000_000, 40_000, 1) <= few and of(1000, 1, 1) <= row + 255 and of(3, 3, 0) <= 3 * row + 255
