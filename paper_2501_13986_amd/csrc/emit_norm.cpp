@@ -14,29 +14,32 @@ namespace cgtp {
 namespace {
 
 const char kShared[] = R"HIP(
+// All of it is one function: from some size on (32 segments) the compiler would leave calls, whose arguments lie in private memory.
+#define ALWAYS __attribute__((always_inline))
+#define INLINE __device__ ALWAYS inline
 typedef long long i64;
-__device__ inline float fma_(float a, float b, float c) { return __builtin_fmaf(a, b, c); }
-__device__ inline double fma_(double a, double b, double c) { return __builtin_fma(a, b, c); }
+INLINE float fma_(float a, float b, float c) { return __builtin_fmaf(a, b, c); }
+INLINE double fma_(double a, double b, double c) { return __builtin_fma(a, b, c); }
 // off by |t| half steps where t is negative: at most 0.3 half steps of 1
-__device__ inline float sigmoid_(float t) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(t * -1.44269502f)); }
-__device__ inline double sigmoid_(double t) { return 1.0 / (1.0 + exp(-t)); }
-__device__ inline float erfc_(float t) { return erfcf(t); }
-__device__ inline double erfc_(double t) { return erfc(t); }
-__device__ inline float exp_(float t) { return expf(t); }
-__device__ inline double exp_(double t) { return exp(t); }
+INLINE float sigmoid_(float t) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(t * -1.44269502f)); }
+INLINE double sigmoid_(double t) { return 1.0 / (1.0 + exp(-t)); }
+INLINE float erfc_(float t) { return erfcf(t); }
+INLINE double erfc_(double t) { return erfc(t); }
+INLINE float exp_(float t) { return expf(t); }
+INLINE double exp_(double t) { return exp(t); }
 // 1 - 2 / (1 + exp(2 |t|)), near zero five terms of the series
-__device__ inline float tanh_(float t) {
+INLINE float tanh_(float t) {
   const float s = t * t, x = __builtin_fabsf(t);
   const float p = fma_(t * s, fma_(s, fma_(s, fma_(s, 0.0218694885f, -0.0539682540f), 0.133333333f), -0.333333333f), t);
   const float q = 1.f - 2.f * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x * 2.88539008f));
   return x < 0.25f ? p : __builtin_copysignf(q, t);
 }
-__device__ inline double tanh_(double t) { return tanh(t); }
-__device__ inline float sqrt_(float t) { return sqrtf(t); }
-__device__ inline double sqrt_(double t) { return sqrt(t); }
+INLINE double tanh_(double t) { return tanh(t); }
+INLINE float sqrt_(float t) { return sqrtf(t); }
+INLINE double sqrt_(double t) { return sqrt(t); }
 
 // activation and derivative
-__device__ inline void act_(T t, T& a, T& d) {
+INLINE void act_(T t, T& a, T& d) {
   if constexpr (ACT == 0) {
     a = t;
     d = T(1);
@@ -58,12 +61,12 @@ __device__ inline void act_(T t, T& a, T& d) {
 }
 
 // column of component m of channel c, counted from the segment's first
-template <int s> __device__ inline int at_(int c, int m) { return IR_MUL ? m * SEG[s].mul + c : c * SEG[s].n + m; }
+template <int s> INLINE int at_(int c, int m) { return IR_MUL ? m * SEG[s].mul + c : c * SEG[s].n + m; }
 
 struct Stat { T mu, r, gmu, gr; };       // of a unit and of its gates
 struct Param { T w, b, gw, gb; };        // of a channel and of its gate
 
-template <int s> __device__ inline Param param_(const T* __restrict__ weight, const T* __restrict__ bias, int c) {
+template <int s> INLINE Param param_(const T* __restrict__ weight, const T* __restrict__ bias, int c) {
   Param p = {weight[SEG[s].w + c], T(0), T(0), T(0)};
   if constexpr (SEG[s].inv) p.b = bias[SEG[s].b + c];
   if constexpr (SEG[s].gate >= 0) {
@@ -74,7 +77,7 @@ template <int s> __device__ inline Param param_(const T* __restrict__ weight, co
 }
 
 // one channel of one row, its n components in v and its gate in g, normalised: y in place of v
-template <int s> __device__ inline void forward_(T* v, T g, const Stat& S, const Param& p) {
+template <int s> INLINE void forward_(T* v, T g, const Stat& S, const Param& p) {
   if constexpr (SEG[s].inv) {
     T d;
     act_(fma_(p.w, (v[0] - S.mu) * S.r, p.b), v[0], d);
@@ -90,7 +93,7 @@ template <int s> __device__ inline void forward_(T* v, T g, const Stat& S, const
 struct Sums { T w, b, gw, gb, h, hx, gh, ghx; };
 
 // v, g in: the channel's numbers of x; q: of gy.  Out: v, g as xh, and q, qg as h
-template <int s> __device__ inline Sums backward_(T* v, T& g, T* q, T& qg, const Stat& S, const Param& p) {
+template <int s> INLINE Sums backward_(T* v, T& g, T* q, T& qg, const Stat& S, const Param& p) {
   Sums o = {};
   if constexpr (SEG[s].inv) {
     T a, d;
@@ -130,14 +133,14 @@ template <int s> __device__ inline Sums backward_(T* v, T& g, T* q, T& qg, const
 struct Means { T h, hx, gh, ghx; };   // of a unit of a sample
 
 // gx of a channel, from what backward_ left, in place of q and qg
-template <int s> __device__ inline void finish_(const T* v, T g, T* q, T& qg, const Stat& S, const Means& e) {
+template <int s> INLINE void finish_(const T* v, T g, T* q, T& qg, const Stat& S, const Means& e) {
 #pragma unroll
   for (int m = 0; m < SEG[s].n; ++m) q[m] = S.r * (q[m] - (SEG[s].inv ? e.h : T(0)) - v[m] * e.hx);
   if constexpr (SEG[s].gate >= 0) qg = S.gr * (qg - e.gh - g * e.ghx);
 }
 
 // rows of sample s, within [0, N]
-__device__ inline void range_(const i64* __restrict__ ptr, i64 s, i64 N, i64& r0, i64& r1) {
+INLINE void range_(const i64* __restrict__ ptr, i64 s, i64 N, i64& r0, i64& r1) {
   r0 = ptr ? ptr[s] : s;
   r1 = ptr ? ptr[s + 1] : s + 1;
   r0 = r0 < 0 ? 0 : r0 > N ? N : r0;
@@ -147,7 +150,7 @@ __device__ inline void range_(const i64* __restrict__ ptr, i64 s, i64 N, i64& r0
 constexpr int pow2_(int v) { int p = 1; while (p < v) p *= 2; return p; }
 
 // f<s>() for a number s that all lanes share
-template <int s, class F> __device__ inline void with_segment_(int k, F f) {
+template <int s, class F> INLINE void with_segment_(int k, F f) {
   if constexpr (s + 1 < NS) {
     if (k != s) return with_segment_<s + 1>(k, f);
   }
@@ -155,7 +158,7 @@ template <int s, class F> __device__ inline void with_segment_(int k, F f) {
 }
 
 // sum over the workgroup, the same in every thread; the order is fixed
-__device__ inline double block_sum_(double v, double* lds) {
+INLINE double block_sum_(double v, double* lds) {
 #pragma unroll
   for (int o = 1; o < 64; o *= 2) v += __shfl_xor(v, o);
   __syncthreads();
@@ -171,13 +174,13 @@ __device__ inline double block_sum_(double v, double* lds) {
 // groups of a segment take PH phases of GP.  All of a segment's words of a step stay in registers.
 const char kLanes[] = R"HIP(
 // sum over the L lanes of a group, the same in each of them; the order is fixed
-template <int ctrl> __device__ inline float dpp_(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), ctrl, 0xf, 0xf, false)); }
-template <int ctrl> __device__ inline double dpp_(double v) {
+template <int ctrl> INLINE float dpp_(float v) { return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), ctrl, 0xf, 0xf, false)); }
+template <int ctrl> INLINE double dpp_(double v) {
   const long long b = __builtin_bit_cast(long long, v);
   const int lo = __builtin_amdgcn_update_dpp(0, (int)b, ctrl, 0xf, 0xf, false), hi = __builtin_amdgcn_update_dpp(0, (int)(b >> 32), ctrl, 0xf, 0xf, false);
   return __builtin_bit_cast(double, (long long)(((unsigned long long)(unsigned)hi << 32) | (unsigned)lo));
 }
-template <int L, class X> __device__ inline X lanes_sum_(X v) {
+template <int L, class X> INLINE X lanes_sum_(X v) {
   if constexpr (L > 1) v += dpp_<0xB1>(v);     // neighbour
   if constexpr (L > 2) v += dpp_<0x4E>(v);     // other pair
   if constexpr (L > 4) v += dpp_<0x141>(v);    // the other four, mirrored (within four all are alike by now)
@@ -189,7 +192,7 @@ template <int L, class X> __device__ inline X lanes_sum_(X v) {
 
 template <int w> struct Wide_ { typedef T type __attribute__((ext_vector_type(w))); };
 // w words that are neighbours in memory
-template <int w, bool vec> __device__ inline void get_(const T* p, T* v) {
+template <int w, bool vec> INLINE void get_(const T* p, T* v) {
   if constexpr (vec && w % 4 == 0) {
 #pragma unroll
     for (int i = 0; i < w; i += 4) {
@@ -211,7 +214,7 @@ template <int w, bool vec> __device__ inline void get_(const T* p, T* v) {
 }
 // Results are written past the caches: nothing here reads them again (20 000 rows as above, forward 80 -> 65 us; one graph of them 341 -> 308).
 #define ST(a, b) __builtin_nontemporal_store(b, &(a))
-template <int w, bool vec> __device__ inline void put_(T* p, const T* v) {
+template <int w, bool vec> INLINE void put_(T* p, const T* v) {
   if constexpr (vec && w % 4 == 0) {
 #pragma unroll
     for (int i = 0; i < w; i += 4) { typename Wide_<4>::type q = {v[i], v[i + 1], v[i + 2], v[i + 3]}; ST(*(typename Wide_<4>::type*)(p + i), q); }
@@ -229,7 +232,7 @@ template <int s> struct Lane {
   static constexpr bool gated = SEG[s].gate >= 0, inv = SEG[s].inv, vec = SEG[s].vec, full = L * C == cg;
   int li, gq, rho, g;       // place in the group, group of the step, row of the step, group
   bool on;                  // lanes that are left over repeat the first row's
-  __device__ Lane(int phase) {
+  INLINE Lane(int phase) {
     const int lane = threadIdx.x & 63, at = lane / L;
     on = at < GP * RP;
     li = lane % L;
@@ -237,10 +240,10 @@ template <int s> struct Lane {
     rho = on ? at / GP : 0;
     g = phase * GP + gq;
   }
-  __device__ bool has(int j) const { return full || (j * L + li) * V < cg; }
-  __device__ int channel(int j) const { return g * cg + (full || (j * L + li) * V < cg ? (j * L + li) * V : 0); }
+  INLINE bool has(int j) const { return full || (j * L + li) * V < cg; }
+  INLINE int channel(int j) const { return g * cg + (full || (j * L + li) * V < cg ? (j * L + li) * V : 0); }
   // words of channels channel(j) + k, component m at v[(j V + k) n + m]; base: the row's first word of the segment
-  __device__ void read(const T* base, T* v) const {
+  INLINE void read(const T* base, T* v) const {
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       if constexpr (IR_MUL) {
@@ -256,7 +259,7 @@ template <int s> struct Lane {
       }
     }
   }
-  __device__ void write(T* base, const T* v) const {
+  INLINE void write(T* base, const T* v) const {
 #pragma unroll
     for (int j = 0; j < J; ++j) {
       if (!has(j)) continue;
@@ -273,26 +276,26 @@ template <int s> struct Lane {
       }
     }
   }
-  __device__ void read_gates(const T* row, T* g_) const {
+  INLINE void read_gates(const T* row, T* g_) const {
     if constexpr (gated) {
 #pragma unroll
       for (int j = 0; j < J; ++j) get_<V, vec>(row + SEG[s].gate + channel(j), g_ + j * V);
     }
   }
-  __device__ void write_gates(T* row, const T* g_) const {
+  INLINE void write_gates(T* row, const T* g_) const {
     if constexpr (gated) {
 #pragma unroll
       for (int j = 0; j < J; ++j)
         if (has(j)) put_<V, vec>(row + SEG[s].gate + channel(j), g_ + j * V);
     }
   }
-  __device__ void params(const T* __restrict__ weight, const T* __restrict__ bias, Param* p) const {
+  INLINE void params(const T* __restrict__ weight, const T* __restrict__ bias, Param* p) const {
 #pragma unroll
     for (int j = 0; j < J; ++j)
 #pragma unroll
       for (int k = 0; k < V; ++k) p[j * V + k] = param_<s>(weight, bias, channel(j) + k);
   }
-  __device__ Stat stat(const T* __restrict__ st) const {
+  INLINE Stat stat(const T* __restrict__ st) const {
     Stat S = {st[(SEG[s].st * G + g) * 2], st[(SEG[s].st * G + g) * 2 + 1], T(0), T(0)};
     if constexpr (gated) {
       S.gmu = st[(SEG[s].gst * G + g) * 2];
@@ -300,7 +303,7 @@ template <int s> struct Lane {
     }
     return S;
   }
-  __device__ void put_stat(T* st, const Stat& S) const {
+  INLINE void put_stat(T* st, const Stat& S) const {
     st[(SEG[s].st * G + g) * 2] = S.mu;
     st[(SEG[s].st * G + g) * 2 + 1] = S.r;
     if constexpr (gated) {
@@ -309,13 +312,13 @@ template <int s> struct Lane {
     }
   }
   // y of the words in v, in their place
-  __device__ void forward(T* v, const T* g_, const Stat& S, const Param* p) const {
+  INLINE void forward(T* v, const T* g_, const Stat& S, const Param* p) const {
 #pragma unroll
     for (int c = 0; c < C; ++c) forward_<s>(v + c * n, gated ? g_[c] : T(0), S, p[c]);
   }
   // v, g_: of x, then xh; q: of gy, then h; qg: h of the gates.  Adds to the sums of the channels (a) and of the group (o)
   struct Sum { double w[C], b[C], gw[C], gb[C]; };
-  __device__ Sums backward(T* v, T* g_, T* q, T* qg, const Stat& S, const Param* p, bool in, bool add, Sum& a) const {
+  INLINE Sums backward(T* v, T* g_, T* q, T* qg, const Stat& S, const Param* p, bool in, bool add, Sum& a) const {
     Sums o = {};
 #pragma unroll
     for (int c = 0; c < C; ++c) {
@@ -337,7 +340,7 @@ template <int s> struct Lane {
     }
     return o;
   }
-  __device__ void finish(const T* v, const T* g_, T* q, T* qg, const Stat& S, const Means& e) const {
+  INLINE void finish(const T* v, const T* g_, T* q, T* qg, const Stat& S, const Means& e) const {
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       T none = T(0);
@@ -346,7 +349,7 @@ template <int s> struct Lane {
   }
   // whether the rows of a step are added by shuffles: they are 64 / RP lanes apart
   static constexpr bool even = (GP * L & (GP * L - 1)) == 0;
-  static __device__ double rows_sum(double v) {
+  static INLINE double rows_sum(double v) {
     if constexpr (even)
 #pragma unroll
       for (int o = GP * L; o < 64; o *= 2) v += __shfl_xor(v, o);
@@ -355,10 +358,10 @@ template <int s> struct Lane {
   // the workgroup's sums of the channels' gradients, four at a time, one for each wave to add up: into a row of partial sums, or, of the only
   // workgroup of its channels, into gweight and gbias
   // any: whether there is anything in them (the workgroup's)
-  __device__ void put_sums(const Sum& a, bool any, double* to, T* gweight, T* gbias, double* lds) const {
+  INLINE void put_sums(const Sum& a, bool any, double* to, T* gweight, T* gbias, double* lds) const {
     constexpr int kinds = 1 + (inv ? 1 : 0) + (gated ? 2 : 0);
     const int lane = threadIdx.x & 63, wave = threadIdx.x / 64;
-    auto put = [&](int i, double t) {
+    auto put = [&](int i, double t) ALWAYS {
       const int c = i / kinds, k = i % kinds;
       const bool b = inv ? k == 1 : k == 2;
       const int at = (k == 0 ? SEG[s].w : inv ? SEG[s].b : k == 1 ? SEG[s].gw : SEG[s].gb) + channel(c / V) + c % V;
@@ -392,9 +395,9 @@ template <int s> struct Lane {
 };
 
 // what a sub-unit (a phase of a segment) is: SUB in the order of their size, the largest first
-template <class F> __device__ inline void with_sub_(int u, F f) { with_segment_<0>(SUB[u].s, f); }
-__device__ inline int sub_() { return blockIdx.x % NSUB; }
-__device__ inline i64 part_() { return blockIdx.x / NSUB; }
+template <class F> INLINE void with_sub_(int u, F f) { with_segment_<0>(SUB[u].s, f); }
+INLINE int sub_() { return blockIdx.x % NSUB; }
+INLINE i64 part_() { return blockIdx.x / NSUB; }
 )HIP";
 
 // Every row is a sample: a group's numbers of a row are in the registers of its lanes, read once.  Sums in T: trees of at most 64 words a lane
@@ -404,7 +407,7 @@ __device__ inline i64 part_() { return blockIdx.x / NSUB; }
 const char kRowFwd[] = R"HIP(
 struct RowFwd {
   const T* __restrict__ x; const T* __restrict__ weight; const T* __restrict__ bias; T* __restrict__ y; T* __restrict__ stats; i64 N; int phase;
-  template <int s> __device__ void operator()() const {
+  template <int s> INLINE void operator()() const {
     typedef Lane<s> A;
     const A a(phase);
     const i64 waves = (gridDim.x / NSUB) * 4;
@@ -417,7 +420,7 @@ struct RowFwd {
       a.read(x + r * DX + SEG[s].col, v);
       a.read_gates(x + r * DX, g);
       Stat S = {T(0), T(0), T(0), T(0)};
-      auto moments = [&](const T* w, int words, bool centre, T inv_m, T& mu, T& rs) {
+      auto moments = [&](const T* w, int words, bool centre, T inv_m, T& mu, T& rs) ALWAYS {
         if (centre) {
           T t = T(0);
 #pragma unroll
@@ -452,7 +455,7 @@ const char kRowBwd[] = R"HIP(
 struct RowBwd {
   const T* __restrict__ x; const T* __restrict__ weight; const T* __restrict__ bias; const T* __restrict__ gy; const T* __restrict__ stats;
   T* __restrict__ gx; double* __restrict__ sums; T* __restrict__ gweight; T* __restrict__ gbias; i64 N; int phase; double* lds;
-  template <int s> __device__ void operator()() const {
+  template <int s> INLINE void operator()() const {
     typedef Lane<s> A;
     const A a(phase);
     const i64 waves = (gridDim.x / NSUB) * 4;
@@ -501,10 +504,10 @@ extern "C" __global__ void __launch_bounds__(256) cgtp_norm_row_bwd(const T* __r
 // Long ones: by memory, which is read twice (no chip-wide barrier): one sample of 20 000 rows of 128 channels 118 and 199 us, the second kernel going through
 // the chunks from the last on, which are still in the caches.
 const char kGraphs[] = R"HIP(
-__device__ inline i64 inside_(i64 p, i64 N) { return p < 0 ? 0 : p > N ? N : p; }
+INLINE i64 inside_(i64 p, i64 N) { return p < 0 ? 0 : p > N ? N : p; }
 
 // number of i < S with ptr[i] < row (ptr not decreasing), by all 64 lanes of every wave: 64 probes a step
-__device__ inline i64 first_from_(const i64* __restrict__ ptr, i64 S, i64 N, i64 row) {
+INLINE i64 first_from_(const i64* __restrict__ ptr, i64 S, i64 N, i64 row) {
   const int lane = threadIdx.x & 63;
   i64 lo = 0, hi = S;     // the answer is in [lo, hi]
   while (lo < hi) {
@@ -520,7 +523,7 @@ __device__ inline i64 first_from_(const i64* __restrict__ ptr, i64 S, i64 N, i64
 }
 
 // lane i's number; i is the same in all lanes
-__device__ inline i64 lane_of_(i64 v, int i) {
+INLINE i64 lane_of_(i64 v, int i) {
   const unsigned lo = __builtin_amdgcn_readlane((int)v, i), hi = __builtin_amdgcn_readlane((int)(v >> 32), i);
   return (i64)((unsigned long long)hi << 32 | lo);
 }
@@ -529,7 +532,7 @@ struct Chunks {
   const i64* __restrict__ ptr;
   i64 N, S, R, D, chunk;
   // f() for each chunk of the workgroup; back: from the last one on
-  template <class F> __device__ void all(bool back, F f) {
+  template <class F> INLINE void all(bool back, F f) {
     const i64 n = N > 0 ? (N + D - 1) / D : 1;
     for (i64 c = part_(); c < n; c += gridDim.x / NSUB) {
       chunk = back ? n - 1 - c : c;
@@ -538,7 +541,7 @@ struct Chunks {
   }
   // the samples of the chunk: f(sample, first row, end, from, to, slot): the whole of a short one (slot -1), or a long one's rows in this chunk;
   // none(sample, end): neighbours without rows
-  template <class F, class E> __device__ void each(F f, E none) const {
+  template <class F, class E> INLINE void each(F f, E none) const {
     const i64 a = chunk * D, b = a + D < N ? a + D : N;
     const bool last = a + D >= N;
     i64 s = first_from_(ptr, S, N, a), from = -64, p = 0;      // p: a lane's number of ptr, from `from` on
@@ -563,9 +566,9 @@ struct Chunks {
     }
   }
   // place of a share of a unit's sums
-  __device__ i64 share(i64 c, int slot, int s, int g) const { return (((c * 2 + slot) * NS + s) * G + g) * 4; }
+  INLINE i64 share(i64 c, int slot, int s, int g) const { return (((c * 2 + slot) * NS + s) * G + g) * 4; }
   // the sums of all shares of a long sample for the lane's group, by the workgroup: 256 / GP threads a group
-  template <class A, int s> __device__ void total(const A& a, const double* __restrict__ part, i64 r0, i64 r1, double (&t)[4], double* lds) const {
+  template <class A, int s> INLINE void total(const A& a, const double* __restrict__ part, i64 r0, i64 r1, double (&t)[4], double* lds) const {
     constexpr int per = A::GP < 256 ? 256 / A::GP : 1;      // threads a group
     const i64 c0 = r0 / D, end = (r1 - 1) / D;
     __syncthreads();
@@ -597,7 +600,7 @@ struct Chunks {
 };
 
 // sums of the lanes, rows and waves for each group of the step: four numbers
-template <class A> __device__ inline void group_sums_(const A& a, double (&t)[4], double* lds) {
+template <class A> INLINE void group_sums_(const A& a, double (&t)[4], double* lds) {
   constexpr int rows = A::even ? 1 : A::RP;
 #pragma unroll
   for (int i = 0; i < 4; ++i) t[i] = A::rows_sum(lanes_sum_<A::L>(t[i]));
@@ -615,7 +618,7 @@ template <class A> __device__ inline void group_sums_(const A& a, double (&t)[4]
 
 // what the moments are taken about: fp64: the group's first numbers of the sample; fp32: zero, a square has 48 of the 53 bits that its sum is held in
 struct Shift { double x, g; };
-template <int s> __device__ inline Shift shift_(const Lane<s>& a, const T* __restrict__ x, i64 r0, i64 rows) {
+template <int s> INLINE Shift shift_(const Lane<s>& a, const T* __restrict__ x, i64 r0, i64 rows) {
   Shift h = {0, 0};
   if (sizeof(T) == 8 && rows > 0) {
     if (Lane<s>::inv) h.x = x[r0 * DX + SEG[s].col + a.g * Lane<s>::cg];
@@ -623,7 +626,7 @@ template <int s> __device__ inline Shift shift_(const Lane<s>& a, const T* __res
   }
   return h;
 }
-template <int s> __device__ inline void moments_(const Lane<s>& a, const T* v, const T* g, const Shift& h, bool in, double (&t)[4]) {
+template <int s> INLINE void moments_(const Lane<s>& a, const T* v, const T* g, const Shift& h, bool in, double (&t)[4]) {
   typedef Lane<s> A;
 #pragma unroll
   for (int c = 0; c < A::C; ++c) {
@@ -642,11 +645,11 @@ template <int s> __device__ inline void moments_(const Lane<s>& a, const T* v, c
   }
 }
 // 1 / sqrt(var + eps); a variance below zero by rounding is zero, a NaN stays one
-__device__ inline T root_(double var) {
+INLINE T root_(double var) {
   const T v = (T)((var > 0 || var != var ? var : 0.0) + EPS);
   return T(1) / sqrt_(v);
 }
-template <int s> __device__ inline Stat stat_of_(const double (&t)[4], const Shift& h, i64 rows) {
+template <int s> INLINE Stat stat_of_(const double (&t)[4], const Shift& h, i64 rows) {
   typedef Lane<s> A;
   const double inv = rows > 0 ? 1.0 / ((double)rows * A::cg) : 1.0, inv_n = inv * (1.0 / A::n);
   const double d = t[0] * inv_n, var = t[1] * inv_n - d * d;
@@ -666,19 +669,19 @@ const char kGraphFwd[] = R"HIP(
 template <bool kLong> struct GraphFwd {
   const T* __restrict__ x; const T* __restrict__ weight; const T* __restrict__ bias; T* __restrict__ y; T* __restrict__ stats; double* __restrict__ part;
   Chunks in; int phase; double* lds;
-  template <int s> __device__ void operator()() const {
+  template <int s> INLINE void operator()() const {
     typedef Lane<s> A;
     const A a(phase);
     Param p[A::C];
     if (!kLong) a.params(weight, bias, p);
     Chunks of = in;
-    of.all(kLong /* what the first kernel read last is still near */, [&] { of.each([&](i64 sample, i64 r0, i64 r1, i64 from, i64 to, int slot) {
+    of.all(kLong /* what the first kernel read last is still near */, [&]() ALWAYS { of.each([&](i64 sample, i64 r0, i64 r1, i64 from, i64 to, int slot) ALWAYS {
       if (kLong && slot < 0) return;
       if (kLong) a.params(weight, bias, p);     // most workgroups find nothing long
       const i64 first = from + (threadIdx.x / 64) * A::RP;
       i64 base = first;
       T v[A::C * A::n], g[A::C];
-      auto fetch = [&] {
+      auto fetch = [&]() ALWAYS {
         const i64 r = base + a.rho < to ? base + a.rho : to - 1;
         a.read(x + r * DX + SEG[s].col, v);
         a.read_gates(x + r * DX, g);
@@ -712,7 +715,7 @@ template <bool kLong> struct GraphFwd {
         a.forward(v, g, st, p);
         if (a.on && base + a.rho < to) a.write(y + (base + a.rho) * DY + SEG[s].ycol, v);
       }
-    }, [&](i64 sample, i64 end) {
+    }, [&](i64 sample, i64 end) ALWAYS {
       if (kLong || !stats) return;
       const double none[4] = {};
       const Stat st = stat_of_<s>(none, Shift{0, 0}, 0);
@@ -735,7 +738,7 @@ GRAPH_FWD(cgtp_norm_long_fwd, true)
 )HIP";
 
 const char kGraphBwd[] = R"HIP(
-template <int s> __device__ inline Means means_of_(const double (&t)[4], i64 rows) {
+template <int s> INLINE Means means_of_(const double (&t)[4], i64 rows) {
   const double inv = rows > 0 ? 1.0 / ((double)rows * Lane<s>::cg) : 1.0;
   return Means{(T)(t[0] * inv), (T)(t[1] * inv * (1.0 / Lane<s>::n)), (T)(t[2] * inv), (T)(t[3] * inv)};
 }
@@ -743,7 +746,7 @@ template <int s> __device__ inline Means means_of_(const double (&t)[4], i64 row
 template <bool kLong> struct GraphBwd {
   const T* __restrict__ x; const T* __restrict__ weight; const T* __restrict__ bias; const T* __restrict__ gy; const T* __restrict__ stats; T* __restrict__ gx;
   double* __restrict__ part; double* __restrict__ sums; T* __restrict__ gweight; T* __restrict__ gbias; Chunks in; int phase; double* lds;
-  template <int s> __device__ void operator()() const {
+  template <int s> INLINE void operator()() const {
     typedef Lane<s> A;
     const A a(phase);
     Param p[A::C];
@@ -751,7 +754,7 @@ template <bool kLong> struct GraphBwd {
     typename A::Sum sum = {};
     bool any = false;
     Chunks of = in;
-    of.all(kLong, [&] { of.each([&](i64 sample, i64 r0, i64 r1, i64 from, i64 to, int slot) {
+    of.all(kLong, [&]() ALWAYS { of.each([&](i64 sample, i64 r0, i64 r1, i64 from, i64 to, int slot) ALWAYS {
       if (kLong && slot < 0) return;
       if (kLong) a.params(weight, bias, p);     // most workgroups find nothing long
       const i64 first = from + (threadIdx.x / 64) * A::RP;
@@ -759,7 +762,7 @@ template <bool kLong> struct GraphBwd {
       any = true;
       const Stat st = a.stat(stats + sample * NST);
       T v[A::C * A::n], q[A::C * A::n], g[A::C], qg[A::C];
-      auto products = [&](bool add) {
+      auto products = [&](bool add) ALWAYS {
         const i64 r = base + a.rho < to ? base + a.rho : to - 1;
         a.read(x + r * DX + SEG[s].col, v);
         a.read(gy + r * DY + SEG[s].ycol, q);
@@ -799,7 +802,7 @@ template <bool kLong> struct GraphBwd {
           a.write_gates(gx + (base + a.rho) * DX, qg);
         }
       }
-    }, [](i64, i64) {}); });
+    }, [](i64, i64) ALWAYS {}); });
     a.put_sums(sum, any, sums ? sums + part_() * (NW + NB) : nullptr, gweight, gbias, lds);
   }
 };
@@ -823,29 +826,29 @@ GRAPH_BWD(cgtp_norm_long_bwd, true)
 // different times the compiler has been seen to place vector instructions that none of them executes.
 const char kUnits[] = R"HIP(
 // a workgroup has one unit of every so many samples (and backward a row of partial sums for all of them)
-__device__ inline int unit_() { return (int)(blockIdx.x % (NS * G)); }
-__device__ inline i64 first_() { return blockIdx.x / (NS * G); }
-__device__ inline i64 apart_() { return gridDim.x / (NS * G); }
+INLINE int unit_() { return (int)(blockIdx.x % (NS * G)); }
+INLINE i64 first_() { return blockIdx.x / (NS * G); }
+INLINE i64 apart_() { return gridDim.x / (NS * G); }
 )HIP";
 
 const char kUnitFwd[] = R"HIP(
 struct UnitFwd {
   const T* __restrict__ x; const T* __restrict__ weight; const T* __restrict__ bias; T* __restrict__ y; T* __restrict__ stats;
   i64 N, S; const i64* __restrict__ ptr; int g; double* lds;
-  template <int s> __device__ void operator()() const {
+  template <int s> INLINE void operator()() const {
     for (i64 sample = first_(); sample < S; sample += apart_()) {
       i64 r0, r1;
       range_(ptr, sample, N, r0, r1);
       one<s>(sample, r0, r1);
     }
   }
-  template <int s> __device__ void one(i64 sample, i64 r0, i64 r1) const {
+  template <int s> INLINE void one(i64 sample, i64 r0, i64 r1) const {
     constexpr int n = SEG[s].n, cg = SEG[s].mul / G, TC = pow2_(cg) < 256 ? pow2_(cg) : 256, TR = 256 / TC;
     constexpr bool gated = SEG[s].gate >= 0, inv = SEG[s].inv;
     const int tc = threadIdx.x % TC, tr = threadIdx.x / TC;
     const i64 count = (r1 - r0) * cg;
     double mu = 0, gmu = 0, sq = 0, gsq = 0;
-    auto each = [&](auto f) {
+    auto each = [&](auto f) ALWAYS {
 #pragma unroll cg <= TC && n <= 3 ? 4 : 1
       for (i64 first = r0; first < r1; first += TR) {
         const i64 r = TR == 1 || first + tr < r1 ? first + tr : r1 - 1;
@@ -857,7 +860,7 @@ struct UnitFwd {
       }
     };
     if (inv || gated) {
-      each([&](i64 r, int c, bool in) {
+      each([&](i64 r, int c, bool in) ALWAYS {
         const T* row = x + r * DX;
         if (inv) mu += in ? (double)row[SEG[s].col + c] : 0.0;
         if (gated) gmu += in ? (double)row[SEG[s].gate + c] : 0.0;
@@ -866,7 +869,7 @@ struct UnitFwd {
       if (inv) mu = block_sum_(mu, lds) / M;
       if (gated) gmu = block_sum_(gmu, lds) / M;
     }
-    each([&](i64 r, int c, bool in) {
+    each([&](i64 r, int c, bool in) ALWAYS {
       const T* row = x + r * DX;
 #pragma unroll
       for (int m = 0; m < n; ++m) {
@@ -893,7 +896,7 @@ struct UnitFwd {
         st[(SEG[s].gst * G + g) * 2 + 1] = S.gr;
       }
     }
-    each([&](i64 r, int ch, bool in) {
+    each([&](i64 r, int ch, bool in) ALWAYS {
       const T* row = x + r * DX;
       T v[n], gt = gated ? row[SEG[s].gate + ch] : T(0);
 #pragma unroll
@@ -917,7 +920,7 @@ struct UnitBwd {
   const T* __restrict__ x; const T* __restrict__ weight; const T* __restrict__ bias; const T* __restrict__ gy; const T* __restrict__ stats;
   T* __restrict__ gx; double* __restrict__ row; i64 N, S; const i64* __restrict__ ptr; int g; double* lds; double* cols;
   // sum over the rows' threads of a channel, for channel c < cg: written or added to what the same thread left of the samples before
-  template <int TC> __device__ void column(double v, double* to, bool in, bool more) const {
+  template <int TC> INLINE void column(double v, double* to, bool in, bool more) const {
     if constexpr (TC < 256) {
       __syncthreads();
       cols[threadIdx.x] = v;
@@ -927,14 +930,14 @@ struct UnitBwd {
     }
     if ((int)threadIdx.x < TC && in) *to = more ? *to + v : v;
   }
-  template <int s> __device__ void operator()() const {
+  template <int s> INLINE void operator()() const {
     for (i64 sample = first_(); sample < S; sample += apart_()) {
       i64 r0, r1;
       range_(ptr, sample, N, r0, r1);
       if (r0 < r1 || sample == first_()) one<s>(sample, r0, r1, sample != first_());
     }
   }
-  template <int s> __device__ void one(i64 sample, i64 r0, i64 r1, bool more) const {
+  template <int s> INLINE void one(i64 sample, i64 r0, i64 r1, bool more) const {
     constexpr int n = SEG[s].n, cg = SEG[s].mul / G, TC = pow2_(cg) < 256 ? pow2_(cg) : 256, TR = 256 / TC;
     constexpr bool gated = SEG[s].gate >= 0, inv = SEG[s].inv;
     const int tc = threadIdx.x % TC, tr = threadIdx.x / TC;
@@ -945,7 +948,7 @@ struct UnitBwd {
       S.gr = st[(SEG[s].gst * G + g) * 2 + 1];
     }
     T v[n], q[n], gt = T(0), qg = T(0);
-    auto load = [&](i64 r, int ch) {
+    auto load = [&](i64 r, int ch) ALWAYS {
 #pragma unroll
       for (int m = 0; m < n; ++m) {
         v[m] = x[r * DX + SEG[s].col + at_<s>(ch, m)];
@@ -964,7 +967,7 @@ struct UnitBwd {
         const bool count = in && first + tr < r1;
         load(first + tr < r1 ? first + tr : r1 - 1, ch);
         const Sums o = backward_<s>(v, gt, q, qg, S, p);
-        auto add = [count](double& to, T v) { to += count ? (double)v : 0.0; };
+        auto add = [count](double& to, T v) ALWAYS { to += count ? (double)v : 0.0; };
         add(w, o.w), add(b, o.b), add(gw, o.gw), add(gb, o.gb);
         add(h, o.h), add(hx, o.hx), add(gh, o.gh), add(ghx, o.ghx);
       }

@@ -12,6 +12,14 @@ from perf.operators import IRREPS
 WIDE = ["256x0e+256x1o+256x2e+256x3o+256x4e", "512x0e+512x1o+512x2e", "300x8e+300x7o+300x6e+300x5o+5000x0e"]
 
 
+# so many segments that the compiler would leave calls in the kernels, with private memory for their arguments
+MANY = "5000x0e+" + "+".join(["1x0e"] * 35)
+
+
+def test_many_segments_have_kernels():
+    b.Norm(MANY, act=b.ACT_NONE, device=-2).close()
+
+
 @pytest.mark.parametrize("flags", [b.CGTP_MUL_IR, b.CGTP_IR_MUL])
 @pytest.mark.parametrize("dtype", [b.CGTP_F32, b.CGTP_F64])
 @pytest.mark.parametrize("irreps", WIDE)
