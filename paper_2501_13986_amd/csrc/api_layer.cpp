@@ -95,7 +95,13 @@ struct NormWork {
       // of 32 channels forward and backward 67 us with 32 rows, 59 with 64, 58 with 128; l <= 2, 80 000 rows 165, 130 and 125; with 128 channels
       // 30 000 rows 407, 408 and 425); of 128 for long samples, whose shares each workgroup adds up
       D = N / 64 * P.subs >= 512 ? 64 : 32;
-      if (N / 128 * P.subs >= 512 && N / 64 > 4 * S) D = 128;
+      if (N / 128 * P.subs >= 512 && N / 64 > 4 * S) {
+        D = 128;
+        // Longer ones where a sample has many: more workgroups than stay on the chip only add shares that each of them reads (one sample of 1 000 000 rows
+        // of 128x0e in 32 groups, forward 1066 us with 128 rows, 489 with 512; 160 000 rows of 128 channels, l <= 3, 1014 and with 256 921; 16 samples in as
+        // many rows 892 with 128, 927 with 256)
+        while (N / D * P.subs > 2048 && N / D >= 256 * S) D *= 2;
+      }
       while ((N + D - 1) / D > most / P.subs) D *= 2;
       R = std::max(R, D);
       const int64_t chunks = std::max<int64_t>(1, (N + D - 1) / D);

@@ -567,8 +567,15 @@ struct Chunks {
   }
   // place of a share of a unit's sums
   INLINE i64 share(i64 c, int slot, int s, int g) const { return (((c * 2 + slot) * NS + s) * G + g) * 4; }
-  // the sums of all shares of a long sample for the lane's group, by the workgroup: 256 / GP threads a group
-  template <class A, int s> INLINE void total(const A& a, const double* __restrict__ part, i64 r0, i64 r1, double (&t)[4], double* lds) const {
+  // the sums of all shares of a long sample for the lane's group, by the workgroup: 256 / GP threads a group.  They stay in LDS for the sample's other chunks
+  // (`known`): formed for each chunk they are work that grows with the square of the sample's length
+  template <class A, int s> INLINE void total(const A& a, const double* __restrict__ part, i64 sample, i64 r0, i64 r1, i64& known, double (&t)[4], double* lds) const {
+    if (sample != known) form<A, s>(a, part, r0, r1, lds);
+    known = sample;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] = lds[a.gq * 4 + i];
+  }
+  template <class A, int s> INLINE void form(const A& a, const double* __restrict__ part, i64 r0, i64 r1, double* lds) const {
     constexpr int per = A::GP < 256 ? 256 / A::GP : 1;      // threads a group
     const i64 c0 = r0 / D, end = (r1 - 1) / D;
     __syncthreads();
@@ -593,9 +600,6 @@ struct Chunks {
       __syncthreads();
       m = h;
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) t[i] = lds[a.gq * 4 + i];
-    __syncthreads();
   }
 };
 
@@ -675,6 +679,7 @@ template <bool kLong> struct GraphFwd {
     Param p[A::C];
     if (!kLong) a.params(weight, bias, p);
     Chunks of = in;
+    i64 known = -1;
     of.all(kLong /* what the first kernel read last is still near */, [&]() ALWAYS { of.each([&](i64 sample, i64 r0, i64 r1, i64 from, i64 to, int slot) ALWAYS {
       if (kLong && slot < 0) return;
       if (kLong) a.params(weight, bias, p);     // most workgroups find nothing long
@@ -690,7 +695,7 @@ template <bool kLong> struct GraphFwd {
       double t[4] = {};
       bool held = false;      // the last step's rows are in v, g
       if (kLong) {
-        of.template total<A, s>(a, part, r0, r1, t, lds);
+        of.template total<A, s>(a, part, sample, r0, r1, known, t, lds);
         if (base < to) base += (to - 1 - base) / (4 * A::RP) * (4 * A::RP);
         else base -= 4 * A::RP;
       } else {
@@ -754,6 +759,7 @@ template <bool kLong> struct GraphBwd {
     typename A::Sum sum = {};
     bool any = false;
     Chunks of = in;
+    i64 known = -1;
     of.all(kLong, [&]() ALWAYS { of.each([&](i64 sample, i64 r0, i64 r1, i64 from, i64 to, int slot) ALWAYS {
       if (kLong && slot < 0) return;
       if (kLong) a.params(weight, bias, p);     // most workgroups find nothing long
@@ -772,7 +778,7 @@ template <bool kLong> struct GraphBwd {
       double t[4] = {};
       bool held = false;
       if (kLong) {
-        of.template total<A, s>(a, part, r0, r1, t, lds);
+        of.template total<A, s>(a, part, sample, r0, r1, known, t, lds);
         if (base < to) base += (to - 1 - base) / (4 * A::RP) * (4 * A::RP);
         else base -= 4 * A::RP;
       } else {

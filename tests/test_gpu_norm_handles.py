@@ -69,3 +69,35 @@ def test_more_samples_than_rows_of_partial_sums(irreps, groups, N, prec):
         again = run(n, p, ptr)
         for k in got:
             assert torch.equal(torch.nan_to_num(got[k]), torch.nan_to_num(again[k])), k
+
+
+def test_cost_of_a_long_sample_grows_with_its_rows():
+    """Eight times the rows of one sample in 32 groups take eight times as long; when every chunk summed up all the others it was 33 times."""
+    from paper_2501_13986_amd import binding as b
+    n = handle("128x0e", 32, layer.SILU, True, "f32", False)
+
+    def time(N):
+        x, w, bias = torch.randn((N, n.dim_x), device="cuda"), torch.ones(n.n_w, device="cuda"), torch.zeros(n.n_b, device="cuda")
+        y, stats, ptr = torch.empty((N, n.dim_y), device="cuda"), torch.empty(n.n_stat, device="cuda"), torch.tensor([0, N], device="cuda")
+        gx, gw, gb = torch.empty_like(x), torch.empty_like(w), torch.empty_like(bias)
+        best = float("inf")
+        for _ in range(6):
+            start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            start.record()
+            b.norm_forward(n, x, w, bias, y, stats, ptr=ptr)
+            b.norm_backward(n, x, w, bias, x, stats, gx, gw, gb, ptr=ptr)
+            end.record()
+            torch.cuda.synchronize()
+            best = min(best, start.elapsed_time(end))
+        return best
+
+    assert time(1_000_000) < 16 * time(125_000)
+
+
+@pytest.mark.parametrize("ends", [[0, 150_000], [5, 90_000, 90_001, 90_040, 149_990]])
+def test_samples_of_many_chunks(ends):
+    """Chunks of more than 128 rows, several of them and several samples a workgroup."""
+    irreps = "8x0e+4x1o"
+    n = handle(irreps, 2, layer.SILU, True, "f32", False)
+    p = inputs(n, 150_000, "f32", seed=3)
+    compare(run(n, p, ends), irreps, 2, layer.SILU, True, False, [a.astype("float64") for a in p], "f32", ends)
