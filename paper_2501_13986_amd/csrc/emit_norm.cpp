@@ -498,7 +498,7 @@ extern "C" __global__ void __launch_bounds__(256) cgtp_norm_row_bwd(const T* __r
 // chunk of its first row: its sums are formed and its results written by one workgroup, from registers if it fits one step.  Longer samples take a second
 // kernel, which is launched only if N > R: the first leaves the sums of each chunk's share (a chunk has at most two: one that goes on, slot 0, one
 // that begins, slot 1), the second adds up the shares of a sample, each workgroup for its groups, and writes the results.  Sums over rows are held
-// in 64 bits; those of fp64 are of the distance from the group's first number of the sample, for their variance.
+// in 64 bits; those of fp64 are of the distance from one of the group's numbers (shift_), for their variance.
 // Bound, with short samples, by the chain of a sample's steps (ptr, rows, sums through LDS, results), which the other workgroups of a unit hide in part: 500
 // samples in 12 000 rows of 32 channels, l <= 3, forward 20 to 29 us (2.7 to 1.9 TB/s), backward 36 (2.3); with a sample a wave instead of a workgroup no faster.
 // Long ones: by memory, which is read twice (no chip-wide barrier): one sample of 20 000 rows of 128 channels 118 and 199 us, the second kernel going through
@@ -620,13 +620,17 @@ template <class A> INLINE void group_sums_(const A& a, double (&t)[4], double* l
   }
 }
 
-// what the moments are taken about: fp64: the group's first numbers of the sample; fp32: zero, a square has 48 of the 53 bits that its sum is held in
+// What the moments are taken about.  fp64: the middle one of three numbers of the group, of the sample's first, middle and last row (about the first one alone, a
+// number far from all others loses as many digits of the variance as the sample's size has).  fp32: zero, a square has 48 of the 53 bits that its sum is
+// held in.
+INLINE double middle_(double a, double b, double c) { return __builtin_fmax(__builtin_fmin(a, b), __builtin_fmin(__builtin_fmax(a, b), c)); }
 struct Shift { double x, g; };
 template <int s> INLINE Shift shift_(const Lane<s>& a, const T* __restrict__ x, i64 r0, i64 rows) {
   Shift h = {0, 0};
   if (sizeof(T) == 8 && rows > 0) {
-    if (Lane<s>::inv) h.x = x[r0 * DX + SEG[s].col + a.g * Lane<s>::cg];
-    if (Lane<s>::gated) h.g = x[r0 * DX + SEG[s].gate + a.g * Lane<s>::cg];
+    const T *first = x + r0 * DX + a.g * Lane<s>::cg, *mid = first + rows / 2 * DX, *last = first + (rows - 1) * DX;
+    if (Lane<s>::inv) h.x = middle_(first[SEG[s].col], mid[SEG[s].col], last[SEG[s].col]);
+    if (Lane<s>::gated) h.g = middle_(first[SEG[s].gate], mid[SEG[s].gate], last[SEG[s].gate]);
   }
   return h;
 }

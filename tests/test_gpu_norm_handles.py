@@ -2,6 +2,7 @@
 import pytest
 
 from oracle import layer
+from tests._layer import check, norm_tolerance
 from tests.test_gpu_norm import compare, handle, inputs, run, torch
 from tests.test_layer_handles import MANY, WIDE
 
@@ -101,3 +102,17 @@ def test_samples_of_many_chunks(ends):
     n = handle(irreps, 2, layer.SILU, True, "f32", False)
     p = inputs(n, 150_000, "f32", seed=3)
     compare(run(n, p, ends), irreps, 2, layer.SILU, True, False, [a.astype("float64") for a in p], "f32", ends)
+
+
+@pytest.mark.parametrize("row", [0, 10_000, 19_999])
+def test_a_number_far_from_all_others(row):
+    """fp64: wherever it stands, the variance has its digits.  Sums about a number of the sample's bulk have no cancellation beyond that of
+    their terms, of which at most 400 are added one after another (a wave's rows of a chunk, waves, the chunks' shares)."""
+    irreps, N = "8x0e+8x1o", 20_000
+    n = handle(irreps, 1, layer.NONE, True, "f64", False)
+    p = inputs(n, N, "f64", seed=7, shift=3.0, scale=1.0)
+    p[0][row, 0], p[0][row, n.dim_y] = 1e8, -1e9      # of the scalars and of the gates
+    ref = layer.norm(irreps, 1, layer.NONE, True, 1e-5, False, *p[:3], [0, N])
+    got = run(n, p, [0, N])
+    for k in ("stats", "y"):
+        check(got[k].cpu().numpy().reshape(ref[k][0].shape), ref[k], norm_tolerance(ref[k], "f64", 400), k)
