@@ -3,7 +3,7 @@ import pytest
 
 from oracle import layer
 from tests._layer import check, norm_tolerance
-from tests.test_gpu_norm import compare, handle, inputs, run, torch
+from tests.test_gpu_norm import GRAPHS, IRREPS, LARGE, compare, handle, inputs, run, torch
 from tests.test_layer_handles import MANY, WIDE
 
 pytestmark = pytest.mark.gpu
@@ -116,3 +116,35 @@ def test_a_number_far_from_all_others(row):
     got = run(n, p, [0, N])
     for k in ("stats", "y"):
         check(got[k].cpu().numpy().reshape(ref[k][0].shape), ref[k], norm_tolerance(ref[k], "f64", 400), k)
+
+
+@pytest.mark.parametrize("prec", ["f32", "f64"])
+@pytest.mark.parametrize("ir_mul", [False, True])
+@pytest.mark.parametrize("irreps,groups", IRREPS + LARGE)
+def test_without_gates(irreps, groups, ir_mul, prec):
+    n = handle(irreps, groups, layer.SILU, False, prec, ir_mul)
+    for i, ptr in enumerate(GRAPHS):
+        p = inputs(n, 41 if ptr is not None else 37, prec, seed=i)
+        compare(run(n, p, ptr), irreps, groups, layer.SILU, False, ir_mul, p, prec, ptr)
+
+
+@pytest.mark.parametrize("prec", ["f32", "f64"])
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("act", [layer.NONE, layer.GELU, layer.SIGMOID, layer.TANH])
+def test_activations_in_the_other_layout(act, gated, prec):
+    irreps = "12x0e+4x1o"
+    n = handle(irreps, 2, act, gated, prec, True)
+    for ptr in (None, [0, 9, 20]):
+        p = inputs(n, 20, prec, seed=act)
+        compare(run(n, p, ptr), irreps, 2, act, gated, True, p, prec, ptr)
+
+
+@pytest.mark.parametrize("prec", ["f32", "f64"])
+@pytest.mark.parametrize("irreps,groups", [("32x0e+32x1o", 4), ("512x0e+512x1o", 1)])
+def test_runs_are_bit_identical_and_finite(irreps, groups, prec):
+    n = handle(irreps, groups, layer.SILU, True, prec, False)
+    p = inputs(n, 4000, prec)
+    for ptr in (None, [0, 4000], [0, 5, 1200, 4000]):
+        a, c = run(n, p, ptr), run(n, p, ptr)
+        for k in a:
+            assert torch.isfinite(a[k]).all() and torch.equal(a[k], c[k]), k
