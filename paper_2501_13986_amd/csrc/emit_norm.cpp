@@ -212,9 +212,11 @@ template <int w, bool vec> INLINE void get_(const T* p, T* v) {
     for (int i = 0; i < w; ++i) v[i] = p[i];
   }
 }
-// Results are written past the caches: nothing here reads them again (20 000 rows as above, forward 80 -> 65 us; one graph of them 341 -> 308).
+// Results are written past the caches: nothing here reads them again (20 000 rows as above, forward 80 -> 65 us; one graph of them 341 -> 308).  Not where a
+// lane's words are neighbours and so many that each instruction writes little of a line (Lane::past): 10 000 rows of 256x3o fp64 in MUL_IR, forward 168 past
+// the caches, 72 through them, 20 000 rows of 64x8e fp32 80 and 40, of 512x3o 163 and 117; of 128 channels, l <= 3, 71 and 96.
 #define ST(a, b) __builtin_nontemporal_store(b, &(a))
-template <int w, bool vec> INLINE void put_(T* p, const T* v) {
+template <int w, bool vec, bool past> INLINE void put_(T* p, const T* v) {
   if constexpr (vec && w % 4 == 0) {
 #pragma unroll
     for (int i = 0; i < w; i += 4) { typename Wide_<4>::type q = {v[i], v[i + 1], v[i + 2], v[i + 3]}; ST(*(typename Wide_<4>::type*)(p + i), q); }
@@ -223,13 +225,17 @@ template <int w, bool vec> INLINE void put_(T* p, const T* v) {
     for (int i = 0; i < w; i += 2) { typename Wide_<2>::type q = {v[i], v[i + 1]}; ST(*(typename Wide_<2>::type*)(p + i), q); }
   } else {
 #pragma unroll
-    for (int i = 0; i < w; ++i) ST(p[i], v[i]);
+    for (int i = 0; i < w; ++i) {
+      if constexpr (past) ST(p[i], v[i]);
+      else p[i] = v[i];
+    }
   }
 }
 
 template <int s> struct Lane {
   static constexpr int n = SEG[s].n, V = SEG[s].V, J = SEG[s].J, L = SEG[s].lanes, GP = SEG[s].at_once, RP = SEG[s].rows, cg = SEG[s].mul / G, C = V * J;
   static constexpr bool gated = SEG[s].gate >= 0, inv = SEG[s].inv, vec = SEG[s].vec, full = L * C == cg;
+  static constexpr bool past = IR_MUL || n == 1 || (n * sizeof(T) <= 32 && J * n * sizeof(T) <= 192);
   int li, gq, rho, g;       // place in the group, group of the step, row of the step, group
   bool on;                  // lanes that are left over repeat the first row's
   INLINE Lane(int phase) {
@@ -269,10 +275,10 @@ template <int s> struct Lane {
           T w[V];
 #pragma unroll
           for (int k = 0; k < V; ++k) w[k] = v[(j * V + k) * n + m];
-          put_<V, vec>(base + m * SEG[s].mul + channel(j), w);
+          put_<V, vec, true>(base + m * SEG[s].mul + channel(j), w);
         }
       } else {
-        put_<V * n, vec>(base + channel(j) * n, v + j * V * n);
+        put_<V * n, vec, past>(base + channel(j) * n, v + j * V * n);
       }
     }
   }
@@ -286,7 +292,7 @@ template <int s> struct Lane {
     if constexpr (gated) {
 #pragma unroll
       for (int j = 0; j < J; ++j)
-        if (has(j)) put_<V, vec>(row + SEG[s].gate + channel(j), g_ + j * V);
+        if (has(j)) put_<V, vec, true>(row + SEG[s].gate + channel(j), g_ + j * V);
     }
   }
   INLINE void params(const T* __restrict__ weight, const T* __restrict__ bias, Param* p) const {
