@@ -308,7 +308,8 @@ cgtp_status cgtp_csr_from_coo_async(const int64_t* recv, const int64_t* send, in
 
 /* ---- layer operators around the convolution --------------------------------------------------- */
 
-/* Activations.  GELU is t Phi(t) with the normal distribution function itself. */
+/* Activations.  GELU is t Phi(t) with the normal distribution function itself.  fp32: the sigmoid, that of gates too, is off by at most
+ * 2^-22 and by at most (6 + 1.25 |t|) 2^-24 of itself: small values at large negative t have fewer bits. */
 typedef enum { CGTP_ACT_NONE = 0, CGTP_ACT_SILU = 1, CGTP_ACT_GELU = 2, CGTP_ACT_SIGMOID = 3, CGTP_ACT_TANH = 4 } cgtp_act;
 
 /* Gated feed-forward block, both projections, the activation and the product in one kernel:
@@ -328,7 +329,8 @@ cgtp_status gated_forward(const void* x, const void* Wg, const void* Wu, const v
 
 /* Gradients of gated_forward given gout = dE/dout [rows, d_out]: gx [rows, d_in], gWg, gWu [d_in, d_out] and, where the biases are
  * given, gbg, gbu [d_out] (NULL otherwise).  The projections are formed again from x, nothing is kept from the forward call.
- * ld_gout and ld_gx as above.  Sums over rows are formed in a fixed order (bit-identical from run to run) through `workspace`:
+ * ld_gout and ld_gx as above.  Sums over rows, those of the biases among them, are held in the type of the data; they are formed in a fixed order
+ * (bit-identical from run to run) through `workspace`:
  * caller-owned device memory of at least cgtp_gated_workspace_bytes(rows, d_in, d_out, dtype) bytes, 256-byte aligned (CGTP_EINVAL
  * if it is smaller), free again for other work on hip_stream after the call.  rows == 0: the weights' gradients are zero.
  * No output may overlap an input or another output. */
@@ -349,7 +351,7 @@ cgtp_status gated_backward(const void* x, const void* Wg, const void* Wu, const 
  * With CGTP_NORM_GATED a row of x continues behind its irreps with one 0e segment of gates for every segment that is not 0e, of
  * its multiplicity, in the same order; they are normalised like the 0e segments.  y has the irreps alone.
  * weight has one number per channel, bias one per 0e channel, gates behind the others in both.  stats [samples, segments, groups, 2]
- * holds mu and r, the segments of gates behind the others.
+ * holds mu and r, the segments of gates behind the others; norm_forward takes NULL for it where no backward pass follows.
  * The layout flags (CGTP_MUL_IR, CGTP_IR_MUL) are those of plans and mean the same. */
 typedef struct cgtp_norm cgtp_norm; /* opaque; owned by the library until cgtp_norm_destroy */
 enum { CGTP_NORM_GATED = 2u };      /* flag of cgtp_norm_create, beside the layout */
@@ -373,7 +375,8 @@ size_t cgtp_norm_workspace_bytes(const cgtp_norm* norm, int64_t N, int64_t S, in
  * ptr[s] .. ptr[s+1] - 1; rows in front of ptr[0] and from ptr[S] on belong to none and keep what y holds there.  A sample without
  * rows has mu = 0 and r = 1 / sqrt(eps).  NULL: every row is a sample (S has to be N).  Indices outside [0, N] are taken for the
  * nearest one inside; where ptr decreases the results are unspecified, within the arrays.  fp32 rows that are samples by themselves are
- * summed in fp32: deviations from the mean whose squares overflow (above 1e19) give r = 0; all other sums are held in fp64.
+ * summed in fp32: deviations from the mean whose squares overflow (above 1e19) give r = 0; all sums over rows are held in fp64.  The variance of
+ * fp64 samples of several rows is formed in one pass about one of the group's numbers, chosen among three so that one far from all others does no harm.
  * Allocates nothing; deterministic; no output may overlap an input or another output. */
 cgtp_status norm_forward(const cgtp_norm* norm, const void* x, const void* weight, const void* bias, void* y, void* stats,
                          int64_t N, int64_t S, const int64_t* ptr, void* workspace, size_t workspace_bytes, void* hip_stream);

@@ -9,8 +9,9 @@
 namespace cgtp {
 
 // 1 / (1 + exp(-t)).  fp32: the hardware's power of two and reciprocal.  The rounding of t log2(e) makes the result off by |t| half
-// steps where t is negative, which is at most 0.3 half steps of 1, and t times it at most 0.6; a correction costs three of seven
-// instructions.  No input leaves the range: 2^x gives infinity or zero, and the reciprocal zero or one.
+// steps where t is negative, which is at most 0.3 half steps of 1, and t times it at most 0.6: a choice, which the header states.  With the argument
+// corrected (five instructions more) the block of 160 710 x 64 x 2176 takes 497 us forward for 478 and 1992 backward for 1913, with 8 columns of x 281 for 274
+// and 941 for 868.  No input leaves the range: 2^x gives infinity or zero, and the reciprocal zero or one.
 __device__ inline float act_sigmoid(float t) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(t * -1.44269502f)); }
 __device__ inline double act_sigmoid(double t) { return 1.0 / (1.0 + exp(-t)); }
 

@@ -20,7 +20,7 @@ const char kShared[] = R"HIP(
 typedef long long i64;
 INLINE float fma_(float a, float b, float c) { return __builtin_fmaf(a, b, c); }
 INLINE double fma_(double a, double b, double c) { return __builtin_fma(a, b, c); }
-// off by |t| half steps where t is negative: at most 0.3 half steps of 1
+// off by |t| half steps where t is negative: at most 0.3 half steps of 1 (as the gated block's, act.hpp, for the same reason)
 INLINE float sigmoid_(float t) { return __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(t * -1.44269502f)); }
 INLINE double sigmoid_(double t) { return 1.0 / (1.0 + exp(-t)); }
 INLINE float erfc_(float t) { return erfcf(t); }
@@ -834,10 +834,10 @@ GRAPH_BWD(cgtp_norm_long_bwd, true)
 )HIP";
 
 // Calls whose kernels above do not fit the registers of a wave: more than 64 words a lane (fp64 32), or code that relocates registers or is refused.  Backward
-// holds twice the words of forward and the channels' sums: groups of 512 x 0e + 512 x 1o fit forward and, as rows, backward in fp32, 2048 x 0e forward alone, 512 x 3o
-// in fp64 neither.  One workgroup for each unit of a sample, whatever its length; the rows are read once for each of mean, variance
+// holds twice the words of forward and the channels' sums: single groups of 512x0e+512x1o fit both ways in fp32, of 2048x0e forward alone, of 512x3o in
+// fp64 neither.  One workgroup for each unit of a sample, whatever its length; the rows are read once for each of mean, variance
 // and result.  Rows as samples, 20 000 x 8192x0e fp32: forward 376 us (3.5 TB/s; 49 us and 6.7 for 2048x0e in registers); bound by the loops of one workgroup
-// where samples are long: one of 20 000 rows of 512x0e+512x1o backward 32 ms (forward in registers 106 us).  All
+// where samples are long: one of 20 000 rows of 2048x0e backward 105 ms (forward in registers 84 us).  All
 // lanes make the same steps, those without a row or channel of their own with another's numbers, which do not count: behind a loop that lanes leave at
 // different times the compiler has been seen to place vector instructions that none of them executes.
 const char kUnits[] = R"HIP(

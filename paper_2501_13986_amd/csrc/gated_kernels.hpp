@@ -364,10 +364,10 @@ __device__ inline void write_both(Tile<double, kRows, KC>& X, Tile<double, KD, k
 
 // A wave keeps the parts of its 16 NT columns of Wg and Wu in registers for the whole call and walks over rows, whose parts the
 // workgroup puts into LDS once for its four waves.  Lane: columns NT l16 + j.
-// Bound by the matrix pipe at the clock that its load leaves: 160 710 x 64 x 2176 fp32 450 to 470 us, 1.14 to 1.19 PFLOP/s of bf16 products (library 1.13) beside
-// 3.1 TB/s of writes; the pipe is busy 59 % of the cycles at 1.9 GHz; without the stores 376 us, with half of the products 327.  With 8 columns of x
-// bound by the writes: 270 us, 5.2 TB/s.  fp64, 30 011 x 64 x 544: 107 us, 39 TFLOP/s (library 72; an instruction of the matrix pipe and one of the vector
-// pipe in fp64 do not run at once).  Two waves per SIMD, for the registers; four with half the columns were no faster.  With the
+// 160 710 x 64 x 2176 fp32 450 to 480 us, 1.12 to 1.19 PFLOP/s of bf16 products (library 1.13) beside 3.1 TB/s of writes: the matrix pipe is busy 59 % of the
+// cycles, vector instructions issue in 22 %, at the 1.8 GHz that this load leaves (2.5 GHz where memory is the bound); without the stores 376 us, with half of
+// the products 327, so that each has its share and none alone is the bound.  With 8 columns of x bound by the writes: 270 us, 5.2 TB/s.  fp64, 30 011 x 64 x 544:
+// 107 us, 39 TFLOP/s (library 72); pipe busy 56 %, vector instructions 17 %, 2.3 GHz.  Two waves per SIMD, for the registers; four with half the columns were no faster.  With the
 // instruction of 32 x 32 results 482 us for 457; 16 columns a wave 546 for 472.
 template <class T, int kIn, int NT, int kAct, bool kWhole>
 __global__ void __launch_bounds__(kThreads, (sizeof(T) == 8 && kIn > 64 ? 1 : 2)) k_gated_fwd(GatedArgs a, int col_tiles, int splits) {
@@ -468,12 +468,15 @@ __global__ void __launch_bounds__(kThreads, (sizeof(T) == 8 && kIn > 64 ? 1 : 2)
 }
 
 // The gradients: two kernels, each of which forms g and u again.  That is a third more products than with dg and du kept in memory,
-// but those are twice the size of gout, written once and read twice.
+// but those are twice the size of gout, written once and read twice.  (One kernel that forms both gradients of a share of the columns would need
+// neither; its partial sums of gx and what it has to pass through LDS have not been tried.)
 
 // gWg, gWu, gbg, gbu of 16 columns a wave, over the row blocks of a split; partial sums [split][Wg; bg; Wu; bu]
-// Bound by the matrix pipe and the vector instructions between its products (activation, cuts into parts), at 1.8 GHz: 160 710 x 64 x 2176 fp32 0.95 ms
-// (with gx 1.90 ms, of which 0.3 would do for the bytes), pipe busy 51 % of the cycles.  Activations of one tile beside the products of another: within
-// 1 %.  fp64, 30 011 x 64 x 544: 200 us.
+// Products and the vector instructions between them (activation, cuts into parts): 160 710 x 64 x 2176 fp32 1.08 ms under the profiler (with gx 1.89 to 1.94 ms in
+// a run of passes, of which 0.3 would do for the bytes), matrix pipe busy 51 % of the cycles, vector instructions 33 %, 1.86 GHz.  Activations of one tile beside the
+// products of another: within 1 %.  fp64, 30 011 x 64 x 544: 200 us, pipe busy 61 %, vector instructions 13 %.
+// The biases' sums are held like the weights' in the type itself: 16 rows a lane and block one after another, the quarters of the rows, the splits in eight
+// chains.
 constexpr int kGwWaves = 4;
 // whether a wave needs the registers of two: fp64, and from 65 columns of x on (20 011 x 128 x 301, forward and backward 214 us, with two waves that
 // keep what does not fit in private memory 230)
@@ -679,7 +682,8 @@ __global__ void __launch_bounds__(kThreads) k_gated_operands(GatedArgs a, u32x4*
 }
 
 // gx of 16 R rows a wave: the operands of 32 columns of W at a time in LDS for the waves of a workgroup, the columns of a split one after
-// another.  Bound like k_gated_gw: 160 710 x 64 x 2176 fp32 0.95 ms, matrix pipe busy 51 % of the cycles at 1.8 GHz; fp64, 30 011 x 64 x 544, 223 us.
+// another.  160 710 x 64 x 2176 fp32 1.04 ms under the profiler, matrix pipe busy 51 % of the cycles, vector instructions 26 %, 1.84 GHz; fp64, 30 011 x 64 x 544, 223 us,
+// pipe busy 51 %, vector instructions 13 %.  20 011 x 128 x 301 fp32 79 us: 157 workgroups on 256 units, pipe busy 20 %, vector instructions 22 %, the rest waits.
 // Four waves, so that two workgroups of a compute unit are in different phases (160 710 x 64 x 2176, all of backward 2.01 ms before the
 // tiles were without bank conflicts, with eight 2.12); eight in fp32 of more than 64 columns of x, whose operands fill the LDS for one workgroup (50 000 x 128 x 2176 backward 1.40 ms; 1.46 when four took 1.91).  More than one split: partial sums [split][rows][d_in] in part.  ops NULL: the
 // workgroups form the operands themselves, which saves a launch where the rows are few.
@@ -850,9 +854,10 @@ __global__ void __launch_bounds__((kGxWaves<T, kIn> * 64), (kIn > 64 && sizeof(T
 //
 // 128 rows x 64 columns of results a workgroup, 16 columns a wave, the terms 32 at a time: the rows' parts in LDS, the columns' parts formed
 // by each wave from memory.  The gradients go through dg and du in the workspace, a piece of the rows at a time, since W
-// no longer stays in registers for products that would form g and u again.  Bound by the matrix pipe and the loads of W that each wave makes: forward and backward of
+// no longer stays in registers for products that would form g and u again.  Forward and backward of
 // 30 000 x 200 x 1000 fp32 1.17 ms (82 TFLOP/s of fp32 products; six bf16 products each at the library's rate would take 0.51), 20 000 x 200 x 500 fp64
-// 0.90 ms (35 TFLOP/s, library 72).  One row of 256 to 2176 numbers: 60 us, five launches of few workgroups.
+// 0.90 ms (35 TFLOP/s, library 72).  Shares of the cycles, matrix pipe and vector instructions: forward 55 and 40 % (each wave forms the parts of its columns
+// of W), of a piece dg and du 29 and 21 %, gx 13 and 13 % (one workgroup a unit, bound by its loads), the weights' gradients 24 and 40 %.  One row of 256 to 2176 numbers: 60 us, five launches of few workgroups.
 
 template <class T>
 constexpr int kManyRows = sizeof(T) == 4 ? 128 : 64;   // rows of a workgroup, for the registers of their sums

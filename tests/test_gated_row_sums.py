@@ -71,3 +71,18 @@ def test_every_row_counts_once(rows, k, n, prec):
     tol = tolerances(ref, rows, k, n, prec)
     for name, got in zip(("gx", "gWg", "gWu", "gbg", "gbu"), run(p, prec, layer.SILU, True)[1:]):
         check(got.cpu().numpy(), ref[name], tol[name], f"{rows}x{k}x{n} {name}")
+
+
+@pytest.mark.gpu
+def test_accuracy_of_the_sigmoid():
+    """What the header states: hardware exponential and reciprocal, one unit each (2^-23), the sum's rounding, and t log2(e) rounded once with a
+    constant that is off by 0.22 half steps."""
+    import torch
+    from paper_2501_13986_amd import binding as b
+    t = torch.cat([torch.linspace(-86, 90, 200_001), torch.linspace(-2, 2, 20_001), torch.tensor([-200.0, -1000.0, 1000.0])]).cuda()[:, None]
+    one, out = torch.ones((1, 1), device="cuda"), torch.empty_like(t)
+    b.gated_forward(t, one, torch.zeros_like(one), out, bg=torch.zeros(1, device="cuda"), bu=torch.ones(1, device="cuda"), act=b.ACT_SIGMOID)
+    exact = torch.sigmoid(t.double())
+    off = (out.double() - exact).abs()
+    assert (off <= 2.0 ** -22).all()
+    assert (off <= exact * (6 + 1.25 * t.abs().double()) * 2.0 ** -24 + 2.0 ** -125).all()
