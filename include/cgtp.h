@@ -386,6 +386,51 @@ cgtp_status norm_backward(const cgtp_norm* norm, const void* x, const void* weig
                           const void* stats, void* gx, void* gweight, void* gbias, int64_t N, int64_t S, const int64_t* ptr,
                           void* workspace, size_t workspace_bytes, void* hip_stream);
 
+/* ---- products by kind of row, orthogonalised updates ---------------------------------------------- */
+
+/* Rows of one kind (species of nodes, pair types of edges) share a matrix.  Positions ptr[g] .. ptr[g+1] - 1 belong to group g,
+ * 0 <= g < groups; position p is row perm[p] of x and out (perm NULL: row p).  For the components c < comps of a row, which stand one
+ * behind the other in it (a segment of 2l + 1 components in the layout IR_MUL; comps = 1: ordinary rows):
+ *     out[row, c, :] = x[row, c, :] W[g] + b[g]
+ * x [rows, comps, d_in], W [groups, d_in, d_out], b [groups, d_out] (NULL: none; only with comps = 1), out [rows, comps, d_out].  ld_x and ld_out are
+ * the elements from one row of x (out) to the next, at least comps * d_in (comps * d_out): rows may be columns of wider ones; what
+ * lies between them is not touched.  ptr (int64 device array [groups+1], not decreasing) and perm (int64 device array [rows], no
+ * row twice) are what cgtp_csr_from_coo makes of the kinds as receivers (row_ptr and perm).  Rows of positions in front of ptr[0] and from ptr[groups]
+ * on belong to no group and keep what out holds there.  Numbers of ptr outside [0, rows] are taken for the nearest one
+ * inside; where ptr decreases the results are unspecified, within the arrays.  Positions whose perm is outside [0, rows) are left out; of a row that perm has twice out
+ * holds one of the results.
+ * Pointers have to be aligned to their type alone.  Sums over d_in are held in the type; fp32 products as in gated_forward, with its limits at
+ * infinite and smallest numbers.  Allocates nothing; no workspace; deterministic.  rows * comps < 2^31; comps up to 1024, groups up
+ * to 2^24, d_in and d_out from 1 to 2^20, their product below 2^31; strides below 2^31.  out must not overlap an input. */
+cgtp_status grouped_forward(const void* x, const void* W, const void* b, void* out, int64_t rows, int64_t d_in, int64_t d_out,
+                            int64_t comps, int64_t groups, const int64_t* ptr, const int64_t* perm, int64_t ld_x, int64_t ld_out,
+                            int32_t dtype, void* hip_stream);
+
+/* Gradients of grouped_forward given gout = dE/dout [rows, comps, d_out]: gx [rows, comps, d_in] (rows of no group keep what it holds), gW [groups, d_in,
+ * d_out] and, where gb is not NULL (comps = 1), gb [groups, d_out]; zero for groups without rows.  Sums over rows are held in the type
+ * and formed in a fixed order (bit-identical from run to run) through `workspace`: caller-owned device memory of at least
+ * cgtp_grouped_workspace_bytes(rows, d_in, d_out, comps, groups, dtype) bytes, 256-byte aligned (CGTP_EINVAL if it is smaller), free again
+ * for other work on hip_stream after the call.  The product is linear in x and in W, so that gradients of these gradients are the same
+ * calls with other arguments.  No output may overlap an input or another output. */
+size_t cgtp_grouped_workspace_bytes(int64_t rows, int64_t d_in, int64_t d_out, int64_t comps, int64_t groups, int32_t dtype);
+cgtp_status grouped_backward(const void* x, const void* W, const void* gout, void* gx, void* gW, void* gb, int64_t rows, int64_t d_in,
+                             int64_t d_out, int64_t comps, int64_t groups, const int64_t* ptr, const int64_t* perm, int64_t ld_x,
+                             int64_t ld_gout, int64_t ld_gx, int32_t dtype, void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/* Updates of weights with all singular values taken towards one (the step of an optimiser that orthogonalises): for each of `batch` matrices G [m, n],
+ *     X = G / (|G| + eps), |G| the root of the sum of squares;  then for each of `steps` triples a, b, c of `coefficients`
+ *     X <- a X + (b A + c A A) X,  A = X X^T,
+ * and out = X.  coefficients: host array [steps, 3], read before the call returns; steps from 1 to 64.  ld_g and ld_out are the elements
+ * from one row of a matrix to the next, stride_g and stride_out from one matrix to the next; matrices of out must not overlap.  A matrix of zeros gives zeros;
+ * one with a number that is not finite gives NaN in it alone.  The sum of squares is held in fp64 (numbers of fp64 above 1e150 overflow in it), all other
+ * sums in the type; fp32 products as in gated_forward.  The gradients that grouped_backward and gated_backward
+ * write are such batches.  `workspace` as above, of cgtp_orthogonalise_workspace_bytes(batch, m, n, dtype) bytes.  Allocates nothing; deterministic.
+ * m n and batch below 2^31, batch m n at most 2^40.  out must not overlap g. */
+size_t cgtp_orthogonalise_workspace_bytes(int64_t batch, int64_t m, int64_t n, int32_t dtype);
+cgtp_status orthogonalise(const void* g, void* out, int64_t batch, int64_t m, int64_t n, int64_t ld_g, int64_t ld_out, int64_t stride_g,
+                          int64_t stride_out, const double* coefficients, int32_t steps, double eps, int32_t dtype, void* workspace,
+                          size_t workspace_bytes, void* hip_stream);
+
 /* Message of the last error on this thread (valid until the next failing call on it). */
 const char* cgtp_last_error(void);
 

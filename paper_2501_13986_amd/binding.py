@@ -30,6 +30,7 @@ EXPORTS = [
     "cgtp_csr_from_coo", "cgtp_csr_from_coo_async", "cgtp_csr_workspace_bytes", "cgtp_last_error", "cgtp_check_code_object",
     "gated_forward", "gated_backward", "cgtp_gated_workspace_bytes",
     "cgtp_norm_create", "cgtp_norm_destroy", "cgtp_norm_dim", "cgtp_norm_kernel", "cgtp_norm_workspace_bytes", "norm_forward", "norm_backward",
+    "grouped_forward", "grouped_backward", "cgtp_grouped_workspace_bytes", "orthogonalise", "cgtp_orthogonalise_workspace_bytes",
 ]
 
 
@@ -110,6 +111,13 @@ def lib() -> C.CDLL:
     L.cgtp_norm_workspace_bytes.restype = C.c_size_t
     L.norm_forward.argtypes = [vp] * 6 + [i64, i64, vp, vp, C.c_size_t, vp]
     L.norm_backward.argtypes = [vp] * 9 + [i64, i64, vp, vp, C.c_size_t, vp]
+    L.grouped_forward.argtypes = [vp] * 4 + [i64] * 5 + [vp, vp, i64, i64, i32, vp]
+    L.grouped_backward.argtypes = [vp] * 6 + [i64] * 5 + [vp, vp, i64, i64, i64, i32, vp, C.c_size_t, vp]
+    L.cgtp_grouped_workspace_bytes.argtypes = [i64] * 5 + [i32]
+    L.cgtp_grouped_workspace_bytes.restype = C.c_size_t
+    L.orthogonalise.argtypes = [vp, vp] + [i64] * 7 + [C.POINTER(C.c_double), i32, C.c_double, i32, vp, C.c_size_t, vp]
+    L.cgtp_orthogonalise_workspace_bytes.argtypes = [i64] * 3 + [i32]
+    L.cgtp_orthogonalise_workspace_bytes.restype = C.c_size_t
     _lib = L
     return L
 
@@ -517,3 +525,94 @@ def norm_backward(norm: Norm, x, weight, bias, gy, stats, gx, gweight, gbias, pt
     ws = _scratch(nb, x)
     _check(L.norm_backward(norm._h, *ops, pg, ps, *out, N, S, pp, _ptr(ws), nb, st))
     return gx, gweight, gbias
+
+
+# ---- products by kind of row, orthogonalised updates ------------------------------------------------------------------
+
+def _index_operand(t, name: str, size: int, device: int) -> int:
+    if t is None:
+        return 0
+    if t.dtype != _torch.int64 or t.dim() != 1 or t.shape[0] != size or not t.is_contiguous() or t.get_device() != device:
+        _bad(f"{name}: a contiguous int64 tensor [{size}] where x is")
+    return t.data_ptr()
+
+
+def _grouped_operands(x, W, ptr, perm, comps: int):
+    dt, dev = _type_and_device(x)
+    if x.dim() != 2 or W is None or W.dim() != 3:
+        _bad("x must have two dimensions, W three")
+    if comps < 1:
+        _bad("comps must be positive")
+    rows, (groups, k, n), ty = x.shape[0], W.shape, x.dtype
+    if ptr is None:
+        _bad("ptr is missing")
+    index = (_index_operand(ptr, "ptr", groups + 1, dev), _index_operand(perm, "perm", rows, dev))
+    return rows, groups, k, n, ty, dt, dev, index, _row_operand(x, "x", (rows, comps * k), ty, dev), _operand(W, "W", (groups, k, n), ty, dev)
+
+
+def grouped_forward(x, W, out, ptr, b=None, perm=None, comps: int = 1):
+    """out = x W[g] + b[g] for the rows of each group g: positions ptr[g] .. ptr[g+1] - 1, position p being row perm[p] (or p).  x [rows, comps * d_in],
+    W [groups, d_in, d_out], b [groups, d_out] or None, out [rows, comps * d_out]; ptr int64 [groups + 1], perm int64 [rows] or None: row_ptr
+    and perm of cgtp_csr_from_coo with the kinds as receivers.  x and out may be columns of wider rows.  Rows of no group keep
+    what out holds.  out must not overlap an input."""
+    rows, groups, k, n, ty, dt, dev, index, (px, ldx), pw = _grouped_operands(x, W, ptr, perm, comps)
+    po, ldo = _row_operand(out, "out", (rows, comps * n), ty, dev)
+    pb = _operand(b, "b", (groups, n), ty, dev, True)
+    st = _stream_of(x, dev)
+    _check(lib().grouped_forward(px, pw, pb, po, rows, k, n, comps, groups, *index, ldx, ldo, dt, st))
+    return out
+
+
+def grouped_backward(x, W, gout, gx, gW, ptr, gb=None, perm=None, comps: int = 1):
+    """Gradients of grouped_forward given gout [rows, comps * d_out]: gx like x, gW like W, and gb [groups, d_out] where it is given.  x, gout and gx
+    may be columns of wider rows.  Returns (gx, gW, gb).  No output may overlap an input."""
+    rows, groups, k, n, ty, dt, dev, index, (px, ldx), pw = _grouped_operands(x, W, ptr, perm, comps)
+    pg, ldg = _row_operand(gout, "gout", (rows, comps * n), ty, dev)
+    pgx, ldgx = _row_operand(gx, "gx", (rows, comps * k), ty, dev)
+    out = (pgx, _operand(gW, "gW", (groups, k, n), ty, dev), _operand(gb, "gb", (groups, n), ty, dev, True))
+    st = _stream_of(x, dev)
+    L = lib()
+    nb = L.cgtp_grouped_workspace_bytes(rows, k, n, comps, groups, dt)
+    ws = _scratch(nb, x)
+    _check(L.grouped_backward(px, pw, pg, *out, rows, k, n, comps, groups, *index, ldx, ldg, ldgx, dt, _ptr(ws), nb, st))
+    return gx, gW, gb
+
+
+STEPS = ((3.4445, -4.7750, 2.0315),) * 5      # take singular values from 0.002 of the size of a matrix to all of it into 0.68 to 1.21
+
+
+def _matrices(t, name: str, shape: Tuple, dtype, device: int) -> Tuple[int, int, int]:
+    """Address, elements from one row and from one matrix to the next."""
+    if t is None:
+        _bad(f"{name} is missing")
+    if t.shape != shape:
+        _bad(f"{name}: shape {tuple(t.shape)}, expected {tuple(shape)}")
+    if t.dtype != dtype or t.get_device() != device:
+        _bad(f"{name}: {t.dtype} on {t.device}, expected {dtype} where G is")
+    stride, ld, step = t.stride()
+    if step != 1 and shape[2] > 1 and t.numel() > 0:
+        _bad(f"{name}: the elements of a row must be neighbours")
+    return t.data_ptr(), ld if shape[1] > 1 else shape[2], stride if shape[0] > 1 else shape[1] * shape[2]
+
+
+def orthogonalise(G, out, coefficients: Sequence[Sequence[float]] = STEPS, eps: float = 1e-7):
+    """out = G [batch, m, n] (or [m, n]) with the singular values of each matrix taken towards one: X = G / (|G| + eps), then for each triple of
+    coefficients X <- a X + (b A + c A A) X with A = X X^T.  Rows of G and out may be columns of wider ones.  out must not overlap G."""
+    dt, dev = _type_and_device(G)
+    if G.dim() == 2:
+        orthogonalise(G[None], None if out is None else out[None], coefficients, eps)
+        return out
+    if G.dim() != 3:
+        _bad("G must have two or three dimensions")
+    (batch, m, n), ty = G.shape, G.dtype
+    pg, ldg, sg = _matrices(G, "G", G.shape, ty, dev)
+    po, ldo, so = _matrices(out, "out", G.shape, ty, dev)
+    if any(len(t) != 3 for t in coefficients):
+        _bad("coefficients: three numbers for each step")
+    c = (C.c_double * (3 * len(coefficients)))(*(v for t in coefficients for v in t))
+    st = _stream_of(G, dev)
+    L = lib()
+    nb = L.cgtp_orthogonalise_workspace_bytes(batch, m, n, dt)
+    ws = _scratch(nb, G)
+    _check(L.orthogonalise(pg, po, batch, m, n, ldg, ldo, sg, so, c, len(coefficients), eps, dt, _ptr(ws), nb, st))
+    return out

@@ -1,6 +1,5 @@
 // Entry points of the layer operators: the gated feed-forward block and the group normalisation.
 #include <algorithm>
-#include <atomic>
 #include <cfloat>
 #include <climits>
 #include <memory>
@@ -9,6 +8,7 @@
 #include <vector>
 
 #include "csr.hpp"
+#include "entry.hpp"
 #include "layer.hpp"
 #include "norm.hpp"
 
@@ -18,37 +18,11 @@ struct cgtp_norm {
 
 namespace {
 
+using cgtp::aligned;
+using cgtp::bad_workspace;
+using cgtp::compute_units;
 using cgtp::fail;
-
-#define HIP_TRY(expr)                                                                                   \
-  do {                                                                                                  \
-    hipError_t e_ = (expr);                                                                             \
-    if (e_ != hipSuccess) return fail(CGTP_ERUNTIME, std::string(#expr) + ": " + hipGetErrorString(e_)); \
-  } while (0)
-
-bool aligned(const void* p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
-
-bool workspace_serves(const void* p, size_t have, size_t need) { return need == 0 || (p && have >= need && aligned(p, 256)); }
-
-cgtp_status bad_workspace(const char* query, size_t need) {
-  return fail(CGTP_EINVAL, "workspace: " + std::to_string(need) + " bytes needed (" + query + "), 256-byte aligned");
-}
-
-// compute units of the current device, asked for once
-hipError_t compute_units(int& cus) {
-  constexpr int kMaxDevices = 64;
-  static std::atomic<int> known[kMaxDevices];
-  int dev = -1;
-  hipError_t e = hipGetDevice(&dev);
-  if (e != hipSuccess) return e;
-  if (dev < 0 || dev >= kMaxDevices) return hipErrorInvalidDevice;
-  cus = known[dev].load(std::memory_order_relaxed);
-  if (cus) return hipSuccess;
-  e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev);
-  cus = std::min(cus, 256);
-  if (e == hipSuccess) known[dev].store(cus, std::memory_order_relaxed);
-  return e;
-}
+using cgtp::workspace_serves;
 
 cgtp_status check_gated(const cgtp::GatedArgs& a, int32_t dtype) {
   if (dtype != CGTP_F32 && dtype != CGTP_F64) return fail(CGTP_EINVAL, "dtype must be CGTP_F32 or CGTP_F64");

@@ -3,13 +3,7 @@
 // With g = x Wg + bg, u = x Wu + bu, out = act(g) u and t = dE/dout:   dg = t u act'(g),  du = t act(g),
 //     gx = dg Wg^T + du Wu^T,   gWg = x^T dg,   gWu = x^T du,   gbg = sum dg,   gbu = sum du.
 //
-// All products run on the matrix cores, 16 x 16 results from 32 terms at a time.  An operand of them is held in parts: lane l has
-// the terms 8 q + (0..7) of row (left operand) or column (right operand) l16, where l16 = l % 16 and q = l / 16.
-//   fp32   three bf16 numbers whose sum has the 24 bits of the factor; of the nine products of parts the six largest are formed,
-//          the others are below 2^-25 of the product.  Sixteen times the rate of the fp32 matrix instruction, so 2.7 times faster
-//          than it with six products.  Sums are held in fp32.
-//   fp64   the numbers themselves, eight instructions of four terms.
-// A lane's four results are rows Num::row(q, 0..3) of column l16.  Two tiles of them are the parts of another operand with 32 terms,
+// All products run on the matrix cores, operands in parts (mma.hpp).  Two tiles of a lane's results are the parts of another operand with 32 terms,
 // in the order Num::term of the tiles' rows, so that dg and du go into their products from the registers that they are formed in;
 // the other operand stands in the same order.
 #pragma once
@@ -21,96 +15,16 @@
 
 #include "act.hpp"
 #include "layer.hpp"
+#include "mma.hpp"
 
 namespace cgtp {
 namespace {
-
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef double f64x2 __attribute__((ext_vector_type(2)));
-typedef double f64x4 __attribute__((ext_vector_type(4)));
-typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
-typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 256;
 constexpr int kRows = 64;      // rows of x in LDS at a time
 constexpr int kMaxIn = 128;    // columns of x that a wave's registers have room for
 constexpr int kNonTemporal = 2;
 using Buffer = __amdgpu_buffer_rsrc_t;
-
-template <int kUnits>
-struct PartsOf {
-  u32x4 w[kUnits];
-};
-
-template <class T>
-struct Num;
-
-// which parts meet: the smallest products first
-constexpr int kPairA[6] = {2, 0, 1, 1, 0, 0}, kPairB[6] = {0, 2, 1, 0, 1, 0};
-
-template <>
-struct Num<float> {
-  static constexpr int kUnits = 3;
-  using Parts = PartsOf<3>;
-  using Vec = f32x4;
-  static __device__ int row(int q, int i) { return 4 * q + i; }
-  // two numbers as three pairs of bf16
-  static __device__ void split(float a, float b, unsigned* p) {
-#pragma unroll
-    for (int i = 0; i < 3; ++i) {
-      const unsigned h = __builtin_bit_cast(unsigned, __builtin_convertvector(f32x2{a, b}, bf16x2));
-      p[i] = h;
-      if (i == 2) break;
-      a -= __builtin_bit_cast(float, h << 16);
-      b -= __builtin_bit_cast(float, h & 0xffff0000u);
-    }
-  }
-  static __device__ Parts parts(const float* v) {
-    unsigned w[4][3];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) split(v[2 * i], v[2 * i + 1], w[i]);
-    Parts r;
-#pragma unroll
-    for (int i = 0; i < 3; ++i) r.w[i] = u32x4{w[0][i], w[1][i], w[2][i], w[3][i]};
-    return r;
-  }
-  // c[i] += a[i] b[i], the chains of sums in turn
-  template <int N>
-  static __device__ void mma(const Parts* const (&a)[N], const Parts* const (&b)[N], Vec* const (&c)[N]) {
-#pragma unroll
-    for (int m = 0; m < 6; ++m)
-#pragma unroll
-      for (int i = 0; i < N; ++i)
-        *c[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[i]->w[kPairA[m]]), __builtin_bit_cast(bf16x8, b[i]->w[kPairB[m]]), *c[i], 0, 0, 0);
-  }
-};
-
-template <>
-struct Num<double> {
-  static constexpr int kUnits = 4;
-  using Parts = PartsOf<4>;
-  using Vec = f64x4;
-  static __device__ int row(int q, int i) { return 4 * i + q; }
-  static __device__ Parts parts(const double* v) {
-    Parts r;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) r.w[i] = __builtin_bit_cast(u32x4, f64x2{v[2 * i], v[2 * i + 1]});
-    return r;
-  }
-  template <int N>
-  static __device__ void mma(const Parts* const (&a)[N], const Parts* const (&b)[N], Vec* const (&c)[N]) {
-#pragma unroll
-    for (int m = 0; m < 8; ++m)
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        const f64x2 u = __builtin_bit_cast(f64x2, a[i]->w[m / 2]), v = __builtin_bit_cast(f64x2, b[i]->w[m / 2]);
-        *c[i] = __builtin_amdgcn_mfma_f64_16x16x4f64(u[m % 2], v[m % 2], *c[i], 0, 0, 0);
-      }
-  }
-};
 
 // the place among 32 terms of row r (< 32) of two tiles of results: lane quarter q, number 4 (r / 16) + i
 template <class T>

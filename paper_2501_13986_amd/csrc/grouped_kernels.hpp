@@ -1,0 +1,344 @@
+// Kernels of the products by kind of row, for the translation units of their two types (grouped_f32.hip, grouped_f64.hip).
+//
+// Positions ptr[g] .. ptr[g+1] - 1 belong to group g; position p is row perm[p] (or p) of x and out, whose components are neighbours in it:
+//     out = x W[g] + b[g],   gx = gout W[g]^T,   gW[g] = sum x^T gout,   gb[g] = sum gout.
+// "Line" is a component of a position: line = position * comps + component.
+// The host does not know ptr: workgroups find their group (find_group), and there are as many of them as any ptr can need.
+#pragma once
+
+#include <algorithm>
+
+#include "grouped.hpp"
+#include "product.hpp"
+
+namespace cgtp {
+namespace {
+
+// ---- positions and groups -----------------------------------------------------------------------------------------------------
+
+__device__ inline int64_t cut(const GroupedArgs& a, int64_t g) {
+  const int64_t p = a.ptr[g];
+  return p < 0 ? 0 : p > a.rows ? a.rows : p;
+}
+
+// Pieces of `of` lines (a power of two) are numbered so that group g's begin at line(ptr[g]) / of + g: a group never needs more numbers than there
+// are up to the next one's, and the number alone names the group.  The greatest group whose pieces begin at or before `id`: 64 of them at a time.
+__device__ inline int64_t first_piece(const GroupedArgs& a, int64_t g, int64_t comps, int shift) { return (cut(a, g) * comps >> shift) + g; }
+
+__device__ inline int64_t find_group(const GroupedArgs& a, int64_t comps, int shift, int64_t id) {
+  int64_t lo = 0, n = a.groups;
+  while (n > 1) {
+    const int64_t step = (n + 63) / 64, g = lo + (threadIdx.x & 63) * step;
+    const bool in = g < lo + n;
+    const int64_t key = first_piece(a, in ? g : lo, comps, shift);
+    const int found = __popcll(__ballot(in && key <= id));
+    const int64_t skip = found > 0 ? (found - 1) * step : 0;
+    lo += skip;
+    n = n - skip < step ? n - skip : step;
+  }
+  return lo;
+}
+
+// lines -> positions and components, for lines of one workgroup: numbers below 2^16 past a line that is divided once
+struct Lines {
+  int64_t position;      // of line 0
+  unsigned component, comps;
+  float inverse;
+  __device__ Lines(int64_t first, int64_t comps_) : comps((unsigned)comps_) {
+    position = comps == 1 ? first : first / comps_;
+    component = (unsigned)(first - position * comps_);
+    inverse = 1.f / (float)comps;
+  }
+  // position (past the first one) and component of line i
+  __device__ void of(unsigned i, unsigned& p, unsigned& m) const {
+    const unsigned u = component + i;
+    p = (unsigned)((float)u * inverse);      // off by one at most
+    int r = (int)(u - p * comps);
+    p += r < 0 ? -1 : r >= (int)comps ? 1 : 0;
+    m = u - p * comps;
+  }
+};
+
+// the row of a position, -1: none
+__device__ inline int64_t row_of(const GroupedArgs& a, int64_t p) {
+  const int64_t r = a.perm ? a.perm[p] : p;
+  return r >= 0 && r < a.rows ? r : -1;
+}
+
+// ---- rows times a matrix ------------------------------------------------------------------------------------------------------
+
+// kR lines x kC columns of out = x W + b (forward) or of gx = gout W^T (kBack).
+template <class T, int kR, int kC, bool kWhole, bool kBack>
+__global__ void __launch_bounds__(kProductThreads, 2) k_grouped_rows(GroupedArgs a, int64_t first_id, int column_tiles) {
+  using Rows = AlongTerms<T, kR, kWhole>;
+  __shared__ Operand<T, kR> R;
+  __shared__ Operand<T, kC> C;
+  __shared__ int64_t place[kR];      // of the lines in the results, -1: none
+  constexpr int kShift = kR == 128 ? 7 : 6;
+  const int64_t id = first_id + blockIdx.x / column_tiles, g = find_group(a, a.comps, kShift, id);
+  const int64_t lines_end = cut(a, g + 1) * a.comps, begin = cut(a, g) * a.comps + ((id - first_piece(a, g, a.comps, kShift)) << kShift);
+  if (id < first_piece(a, g, a.comps, kShift) || begin >= lines_end) return;
+  const int have = (int)(lines_end - begin < kR ? lines_end - begin : kR);
+  const int K = (int)(kBack ? a.d_out : a.d_in), n = (int)(kBack ? a.d_in : a.d_out), c0 = (int)(blockIdx.x % column_tiles) * kC;
+  const T *x = (const T*)(kBack ? a.gout : a.x), *W = (const T*)a.W + g * a.d_in * a.d_out;
+  const int64_t ld = kBack ? a.ld_gout : a.ld_x, ld_to = kBack ? a.ld_gx : a.ld_out;
+  const Lines lines(begin, a.comps);
+  const T* p[Rows::kPer];
+#pragma unroll
+  for (int i = 0; i < Rows::kPer; ++i) {
+    unsigned at, m;
+    const int line = Rows::row(i);
+    lines.of(line < have ? line : 0, at, m);
+    const int64_t r = row_of(a, lines.position + at);
+    p[i] = x + (r < 0 ? 0 : r) * ld + m * (int64_t)K;
+    if (threadIdx.x % 8 == 0) place[line] = r < 0 || line >= have ? -1 : r * ld_to + m * (int64_t)n;
+  }
+  Rows rows;
+  AcrossTerms<T, kC, kWhole> across;
+  AlongTerms<T, kC, kWhole> along;
+  const T* pw[kC / 32];
+  if constexpr (kBack)
+#pragma unroll
+    for (int i = 0; i < kC / 32; ++i) {
+      const int c = c0 + along.row(i);
+      pw[i] = W + (int64_t)(c < n ? c : 0) * K;
+    }
+  auto fetch = [&](int k0) {
+    rows.fetch(p, k0, K);
+    if constexpr (kBack) {
+      along.fetch(pw, k0, K);
+    } else {
+      const T* q[4];
+      bool ok[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int k = k0 + across.term() + j;
+        ok[j] = k < K;
+        q[j] = W + (int64_t)(ok[j] ? k : 0) * n;
+      }
+      across.fetch(q, ok, c0, n);
+    }
+  };
+  Results<T, kR, kC> out;
+  fetch(0);
+  for (int k0 = 0; k0 < K; k0 += kStep) {
+    __syncthreads();
+    rows.put(R);
+    if constexpr (kBack) along.put(C);
+    else across.put(C);
+    __syncthreads();
+    if (k0 + kStep < K) fetch(k0 + kStep);
+    out.multiply(R, C);
+  }
+  const T* bias = kBack || !a.b ? nullptr : (const T*)a.b + g * n;
+  T* to = (T*)(kBack ? a.gx : a.out);
+#pragma unroll
+  for (int ct = 0; ct < out.CT; ++ct) {
+    const int c = c0 + out.column(ct);
+    T add[4] = {};
+    if (bias)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) add[i] = bias[c + i < n ? c + i : 0];
+#pragma unroll
+    for (int rt = 0; rt < out.RT; ++rt) {
+      const int64_t at = place[out.row(rt)];
+      T v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = out.acc[rt][ct][i] + add[i];
+      if (at >= 0 && c < n) store_some(to + at + c, v, n - c);
+    }
+  }
+}
+
+// ---- the matrices' gradients ----------------------------------------------------------------------------------------------------
+
+constexpr int kMostPositions = 1024;      // of a chunk
+
+// kR x kC numbers of gW[g] (and kC of gb[g]) over the positions of group g in one chunk: chunks are the same for all groups, so that those of a group that has several
+// leave their sums at slot 2 chunk + (0: the group began before the chunk, 1: in it).  A group with one chunk, or without rows, is
+// written at once.
+template <class T, int kR, int kC, bool kWhole>
+__global__ void __launch_bounds__(kProductThreads, 2) k_grouped_weights(GroupedArgs a, int64_t first_id, int shift, int row_tiles, int column_tiles, T* part, T* part_b) {
+  __shared__ Operand<T, kR> R;
+  __shared__ Operand<T, kC> C;
+  __shared__ int64_t row[kMostPositions];
+  const int tiles = row_tiles * column_tiles, tile = blockIdx.x % tiles;
+  const int64_t id = first_id + blockIdx.x / tiles, g = find_group(a, 1, shift, id), chunk = id - g;
+  const int64_t from = cut(a, g), end = cut(a, g + 1), lo = std::max(from, chunk << shift), hi = std::min(end, (chunk + 1) << shift);
+  const bool empty = end <= from && chunk == from >> shift;
+  if (chunk < from >> shift || (hi <= lo && !empty)) return;
+  const int K = (int)a.d_in, n = (int)a.d_out, k0 = tile / column_tiles * kR, c0 = tile % column_tiles * kC;
+  const int positions = hi > lo ? (int)(hi - lo) : 0, count = positions * (int)a.comps;
+  for (int i = threadIdx.x; i < positions; i += kProductThreads) row[i] = row_of(a, lo + i);
+  __syncthreads();
+  AcrossTerms<T, kR, kWhole> x;
+  AcrossTerms<T, kC, kWhole> t;
+  const Lines lines(0, a.comps);
+  auto fetch = [&](int line0) {
+    const T *px[4], *pt[4];
+    bool ok[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int line = line0 + x.term() + j;
+      unsigned at, m;
+      lines.of(line < count ? line : 0, at, m);
+      const int64_t r = row[at];
+      ok[j] = line < count && r >= 0;
+      px[j] = (const T*)a.x + (r < 0 ? 0 : r) * a.ld_x + m * (int64_t)K;
+      pt[j] = (const T*)a.gout + (r < 0 ? 0 : r) * a.ld_gout + m * (int64_t)n;
+    }
+    x.fetch(px, ok, k0, K);
+    t.fetch(pt, ok, c0, n);
+  };
+  Results<T, kR, kC> out;
+  T sum[kC / 32] = {};
+  if (count > 0) fetch(0);
+  for (int l = 0; l < count; l += kStep) {
+    __syncthreads();
+    x.put(R);
+    t.put(C);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kC / 32; ++i) sum[i] += (t.v[0][i] + t.v[1][i]) + (t.v[2][i] + t.v[3][i]);
+    if (l + kStep < count) fetch(l + kStep);
+    out.multiply(R, C);
+  }
+  const bool whole = from >> shift == (end - 1) >> shift || empty;
+  const int64_t slot = 2 * chunk + (from >= chunk << shift);
+  T* to = whole ? (T*)a.gW + g * a.d_in * a.d_out : part + slot * a.d_in * a.d_out;
+#pragma unroll
+  for (int rt = 0; rt < out.RT; ++rt)
+#pragma unroll
+    for (int ct = 0; ct < out.CT; ++ct) {
+      const int k = k0 + out.row(rt), c = c0 + out.column(ct);
+      T v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = out.acc[rt][ct][i];
+      if (k < K && c < n) store_some(to + (int64_t)k * n + c, v, n - c);
+    }
+  if (!a.gb || k0 > 0) return;
+  // the eight threads of a column, one after another
+  __syncthreads();
+  T* sums = (T*)&C;      // [8][kC]
+#pragma unroll
+  for (int i = 0; i < kC / 32; ++i) sums[x.term() / 4 * kC + t.place() + i] = sum[i];
+  __syncthreads();
+  T* to_b = whole ? (T*)a.gb + g * a.d_out : part_b + slot * a.d_out;
+  for (int c = threadIdx.x; c < kC && c0 + c < n; c += kProductThreads) {
+    T v = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v += sums[j * kC + c];
+    to_b[c0 + c] = v;
+  }
+}
+
+// Adds up, in their order, the chunks of the group that begins in chunk blockIdx.x / blocks and goes on behind it, if there is one.
+template <class T>
+__global__ void __launch_bounds__(kProductThreads) k_grouped_sums(GroupedArgs a, int64_t first_chunk, int shift, int blocks, const T* part, const T* part_b) {
+  const int64_t chunk = first_chunk + blockIdx.x / blocks, next = (chunk + 1) << shift;
+  if (next >= a.rows) return;
+  // the last group that begins before the next chunk
+  int64_t lo = 0, n = a.groups;
+  while (n > 1) {
+    const int64_t step = (n + 63) / 64, g = lo + (threadIdx.x & 63) * step;
+    const bool in = g < lo + n;
+    const int found = __popcll(__ballot(in && cut(a, in ? g : lo) < next));
+    const int64_t skip = found > 0 ? (found - 1) * step : 0;
+    lo += skip;
+    n = n - skip < step ? n - skip : step;
+  }
+  const int64_t from = cut(a, lo), end = cut(a, lo + 1);
+  if (from < chunk << shift || from >= next || end <= next) return;
+  const int64_t last = (end - 1) >> shift, size = a.d_in * a.d_out, all = size + (a.gb ? a.d_out : 0);
+  for (int64_t i = (int64_t)(blockIdx.x % blocks) * kProductThreads + threadIdx.x; i < all; i += (int64_t)blocks * kProductThreads) {
+    const bool b = i >= size;
+    const T* p = b ? part_b + (i - size) : part + i;
+    const int64_t of = b ? a.d_out : size;
+    T v[8] = {p[(2 * chunk + 1) * of]};
+    int64_t c = chunk + 1;
+    for (; c + 8 <= last + 1; c += 8)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += p[2 * (c + j) * of];
+    for (; c <= last; ++c) v[0] += p[2 * c * of];
+    const T total = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+    if (b) ((T*)a.gb)[lo * a.d_out + (i - size)] = total;
+    else ((T*)a.gW)[lo * size + i] = total;
+  }
+}
+
+// ---- launches -------------------------------------------------------------------------------------------------------------------
+
+constexpr int64_t kMostBlocks = (int64_t)1 << 23;   // workgroups of a launch: 2^32 threads are too many
+
+size_t up(size_t v) { return (v + 255) / 256 * 256; }
+
+// f(first, blocks) for pieces ids of `tiles` workgroups each, as many a launch as there may be
+template <class F>
+hipError_t in_launches(int64_t ids, int64_t tiles, F f) {
+  const int64_t most = std::max<int64_t>(1, kMostBlocks / tiles);
+  for (int64_t at = 0; at < ids; at += most) {
+    f(at, dim3((unsigned)(std::min(most, ids - at) * tiles)));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+template <class T>
+constexpr int kTile = sizeof(T) == 4 ? 128 : 64;
+
+template <class T, bool kBack>
+hipError_t launch_rows(const GroupedArgs& a, hipStream_t st) {
+  const int64_t n = kBack ? a.d_in : a.d_out;
+  const bool whole = a.d_in % 4 == 0 && a.d_out % 4 == 0;
+  auto go = [&](auto wide) {
+    constexpr int kR = kTile<T>, kC = decltype(wide)::value ? kTile<T> : 64;
+    const int64_t tiles = (n + kC - 1) / kC, ids = a.rows * a.comps / kR + a.groups;
+    return in_launches(ids, tiles, [&](int64_t first, dim3 grid) {
+      if (whole) k_grouped_rows<T, kR, kC, true, kBack><<<grid, kProductThreads, 0, st>>>(a, first, (int)tiles);
+      else k_grouped_rows<T, kR, kC, false, kBack><<<grid, kProductThreads, 0, st>>>(a, first, (int)tiles);
+    });
+  };
+  return n > 64 ? go(std::true_type()) : go(std::false_type());
+}
+
+// positions of a chunk (a power of two), slots of partial sums
+struct Chunks {
+  int shift = 8;
+  int64_t count, slots;
+  Chunks(int64_t rows) {
+    while (shift < 10 && rows >> shift > 512) ++shift;
+    count = (rows + (1 << shift) - 1) >> shift;
+    slots = count > 1 ? 2 * count : 0;
+  }
+};
+
+template <class T>
+size_t workspace_bytes(int64_t rows, int64_t K, int64_t n) {
+  const Chunks c(rows);
+  return up(c.slots * K * n * sizeof(T)) + up(c.slots * n * sizeof(T));
+}
+
+template <class T>
+hipError_t backward(const GroupedArgs& a, char* ws, hipStream_t st) {
+  const int64_t K = a.d_in, n = a.d_out;
+  hipError_t e = a.rows ? launch_rows<T, true>(a, st) : hipSuccess;
+  if (e != hipSuccess) return e;
+  const Chunks c(a.rows);
+  T *part = (T*)ws, *part_b = (T*)(ws + up(c.slots * K * n * sizeof(T)));
+  constexpr int kR = kTile<T>, kC = kTile<T>;
+  const int64_t rt = (K + kR - 1) / kR, ct = (n + kC - 1) / kC;
+  const bool whole = K % 4 == 0 && n % 4 == 0;
+  e = in_launches((a.rows >> c.shift) + a.groups, rt * ct, [&](int64_t first, dim3 grid) {
+    if (whole) k_grouped_weights<T, kR, kC, true><<<grid, kProductThreads, 0, st>>>(a, first, c.shift, (int)rt, (int)ct, part, part_b);
+    else k_grouped_weights<T, kR, kC, false><<<grid, kProductThreads, 0, st>>>(a, first, c.shift, (int)rt, (int)ct, part, part_b);
+  });
+  if (e != hipSuccess || c.slots == 0) return e;
+  const int64_t blocks = std::min<int64_t>((K * n + n + kProductThreads - 1) / kProductThreads, 1024);
+  return in_launches(c.count - 1, blocks, [&](int64_t first, dim3 grid) {
+    k_grouped_sums<T><<<grid, kProductThreads, 0, st>>>(a, first, c.shift, (int)blocks, part, part_b);
+  });
+}
+
+}  // namespace
+}  // namespace cgtp

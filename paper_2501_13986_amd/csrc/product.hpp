@@ -1,0 +1,182 @@
+// Products of matrices in memory, a tile of results a workgroup: the parts of 32 terms of both operands in LDS at a time, the next ones on their way to
+// registers meanwhile.  For the products by kind of row (grouped_kernels.hpp) and the steps of orthogonalise (orth_kernels.hpp).
+//
+// The results are kR rows x kC columns, four waves 2 x 2.  The columns are the left operand of the matrix instructions, so that a lane's results are four neighbours
+// of one row: row l16 of a tile, columns 4 q + (0..3).
+// Nothing here depends on a lane's own condition until results are stored: addresses outside are replaced by ones inside and what they read by zero.
+#pragma once
+
+#include "mma.hpp"
+
+namespace cgtp {
+namespace {
+
+constexpr int kProductThreads = 256;
+constexpr int kStep = 32;      // terms in LDS at a time
+
+// which of 16 columns lane l16 of a left operand holds, for results 4 q + i to be neighbours: a lane's results are rows Num::row(q, i) of the instruction
+template <class T>
+__device__ inline int column_place(int l16) {
+  return sizeof(T) == 4 ? l16 : l16 % 4 * 4 + l16 / 4;
+}
+
+// V neighbours of a row of `width` numbers from column k on, zero behind its end.  kWhole: width is a multiple of V.
+template <class T, int V, bool kWhole>
+__device__ inline void load_some(const T* row, int k, int width, T* v) {
+  typedef T Words __attribute__((ext_vector_type(V), aligned(sizeof(T))));
+  if (kWhole || width >= V) {
+    const int at = k <= width - V ? k : width - V;
+    const Words w = *(const Words*)(row + at);
+    if constexpr (kWhole) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = k < width ? w[i] : T(0);
+    } else {      // the row's last ones, moved down
+      const int s = k - at;
+      T u[V];
+#pragma unroll
+      for (int i = 0; i < V; ++i) u[i] = s & 1 ? (i + 1 < V ? w[i + 1] : T(0)) : w[i];
+#pragma unroll
+      for (int i = 0; i < V; ++i) v[i] = s >= V ? T(0) : V > 2 && (s & 2) ? (i + 2 < V ? u[i + 2] : T(0)) : u[i];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+      const T w = row[k + i < width ? k + i : 0];
+      v[i] = k + i < width ? w : T(0);
+    }
+  }
+}
+
+// kR rows (columns) of 32 terms in LDS.  A wave reads 16 bytes of each of 16 rows, and writes 8 bytes of rows that are one, two or four apart: the rows are 80
+// bytes apart and their 16 bytes change places with the row's number / 16, in which all of these find different banks (256 bytes in all).
+template <class T, int kR>
+struct Operand;
+template <int kR>
+struct Operand<float, kR> {
+  __bf16 v[3][kR][kStep + 8];
+  static __device__ int at(int r, int k) { return k ^ (r >> 4 & 3) * 8; }
+  __device__ PartsOf<3> read(int r, int k) const {
+    PartsOf<3> p;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) p.w[i] = *(const u32x4*)&v[i][r][at(r, k)];
+    return p;
+  }
+  __device__ void write4(int r, int k, const float* x) {
+    unsigned lo[3], hi[3];
+    Num<float>::split(x[0], x[1], lo);
+    Num<float>::split(x[2], x[3], hi);
+#pragma unroll
+    for (int p = 0; p < 3; ++p) *(u32x2*)&v[p][r][at(r, k)] = u32x2{lo[p], hi[p]};
+  }
+};
+template <int kR>
+struct Operand<double, kR> {
+  double v[kR][kStep + 2];
+  __device__ PartsOf<4> read(int r, int k) const {
+    PartsOf<4> p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p.w[i] = *(const u32x4*)&v[r][k + 2 * i];
+    return p;
+  }
+  __device__ void write4(int r, int k, const double* x) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) *(u32x4*)&v[r][k + 2 * h] = __builtin_bit_cast(u32x4, f64x2{x[2 * h], x[2 * h + 1]});
+  }
+};
+
+// An operand whose terms are neighbours in memory: a thread has four of them of each of kPer rows
+template <class T, int kR, bool kWhole>
+struct AlongTerms {
+  static constexpr int kPer = kR / 32;
+  T v[kPer][4];
+  static __device__ int row(int i) { return i * 32 + (int)threadIdx.x / 8; }      // of the thread's i-th
+  static __device__ int term() { return (int)threadIdx.x % 8 * 4; }
+  // p: the rows in memory, any address inside where there is none (their results are not kept)
+  __device__ void fetch(const T* const (&p)[kPer], int k0, int terms) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) load_some<T, 4, kWhole>(p[i], k0 + term(), terms, v[i]);
+  }
+  __device__ void put(Operand<T, kR>& to) const {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) to.write4(row(i), term(), v[i]);
+  }
+};
+
+// An operand whose terms are rows of memory: a thread has kPer neighbours of each of four of them
+template <class T, int kR, bool kWhole>
+struct AcrossTerms {
+  static constexpr int kPer = kR / 32;
+  T v[4][kPer];
+  static __device__ int place() { return ((int)threadIdx.x >> 1 & 31) * kPer; }
+  static __device__ int term() { return ((int)threadIdx.x >> 6) * 8 + ((int)threadIdx.x & 1) * 4; }
+  // p: rows of the thread's four terms, an address inside where there is none (ok false: zero)
+  __device__ void fetch(const T* const (&p)[4], const bool (&ok)[4], int first, int width) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      load_some<T, kPer, kWhole>(p[j], first + place(), width, v[j]);
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) v[j][i] = ok[j] ? v[j][i] : T(0);
+    }
+  }
+  __device__ void put(Operand<T, kR>& to) const {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const T x[4] = {v[0][i], v[1][i], v[2][i], v[3][i]};
+      to.write4(place() + i, term(), x);
+    }
+  }
+};
+
+// The results of a workgroup: a wave's quarter of them
+template <class T, int kR, int kC>
+struct Results {
+  using N = Num<T>;
+  static constexpr int RT = kR / 32, CT = kC / 32;
+  typename N::Vec acc[RT][CT] = {};
+  static __device__ int lane() { return (int)threadIdx.x & 63; }
+  static __device__ int wave() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
+  static __device__ int row(int rt) { return wave() / 2 * (kR / 2) + rt * 16 + lane() % 16; }
+  static __device__ int column(int ct) { return wave() % 2 * (kC / 2) + ct * 16 + lane() / 16 * 4; }      // the first of four
+  __device__ void multiply(const Operand<T, kR>& R, const Operand<T, kC>& C) {
+    const int l16 = lane() % 16, k = lane() / 16 * 8, r0 = wave() / 2 * (kR / 2), c0 = wave() % 2 * (kC / 2) + column_place<T>(l16);
+    typename N::Parts c[CT];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) c[ct] = C.read(c0 + ct * 16, k);
+    constexpr int kSide = CT >= 4 || RT < 2 ? 1 : 2;      // rows of tiles side by side: chains of sums in turn
+#pragma unroll
+    for (int rt = 0; rt < RT; rt += kSide) {
+      typename N::Parts r[kSide];
+#pragma unroll
+      for (int s = 0; s < kSide; ++s) r[s] = R.read(r0 + (rt + s) * 16 + l16, k);
+      constexpr int kUnits = sizeof(T) == 4 ? 6 : 8;
+#pragma unroll
+      for (int m = 0; m < kUnits; ++m)
+#pragma unroll
+        for (int s = 0; s < kSide; ++s)
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) {
+            auto& a = acc[rt + s][ct];
+            if constexpr (sizeof(T) == 4)
+              a = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, c[ct].w[kPairA[m]]), __builtin_bit_cast(bf16x8, r[s].w[kPairB[m]]), a, 0, 0, 0);
+            else
+              a = __builtin_amdgcn_mfma_f64_16x16x4f64(__builtin_bit_cast(f64x2, c[ct].w[m / 2])[m % 2], __builtin_bit_cast(f64x2, r[s].w[m / 2])[m % 2], a, 0, 0, 0);
+          }
+    }
+  }
+};
+
+// the first `have` of four neighbours, at most four
+template <class T>
+__device__ inline void store_some(T* to, const T* v, int have) {
+  typedef T Words __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+  if (have >= 4) {
+    *(Words*)to = Words{v[0], v[1], v[2], v[3]};
+  } else {
+#pragma unroll
+    for (int i = 0; i < 3; ++i)
+      if (i < have) to[i] = v[i];
+  }
+}
+
+}  // namespace
+}  // namespace cgtp

@@ -1,0 +1,160 @@
+"""Orthogonalised updates against the steps in a longer type."""
+import numpy as np
+import pytest
+
+from tests._products import orth_check
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+NP = {"f32": np.float32, "f64": np.float64}
+PRECS = ["f32", "f64"]
+
+
+def gradients(batch, m, n, prec, seed=0):
+    rng = np.random.default_rng(seed)
+    g = rng.normal(size=(batch, m, n)) * np.exp(0.5 * rng.normal(size=(batch, m, 1))) * np.exp(0.5 * rng.normal(size=(batch, 1, n))) * 1e-3
+    return g.astype(NP[prec])
+
+
+def run(G, **k):
+    from paper_2501_13986_amd import binding as b
+    print(f"{G.shape} {G.dtype} {k}", flush=True)
+    t = torch.from_numpy(G).cuda()
+    out = torch.full_like(t, float("nan"))
+    b.orthogonalise(t, out, **k)
+    torch.cuda.synchronize()
+    return out.cpu().numpy()
+
+
+SIZES = [(1, 1, 1), (3, 1, 9), (2, 9, 1), (4, 5, 5), (1, 16, 16), (2, 31, 33), (2, 33, 31), (1, 64, 64), (3, 63, 65), (2, 64, 300), (2, 300, 64), (1, 65, 129), (2, 100, 97), (3, 128, 128),
+         (1, 127, 500), (1, 129, 130), (1, 200, 136), (2, 96, 301), (1, 8, 2176), (1, 257, 300), (40, 20, 24), (150, 3, 2), (1, 130, 520), (5, 48, 40)]
+
+
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("batch,m,n", SIZES)
+def test_against_the_oracle(batch, m, n, prec):
+    if prec == "f64" and batch * m * n > 40_000:
+        batch = 1
+    G = gradients(batch, m, n, prec, seed=m + n)
+    orth_check(run(G), G, prec, (batch, m, n))
+
+
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("m,n", [(20, 20), (30, 50), (140, 150), (70, 20)])
+def test_other_steps(m, n, prec):
+    """One step, cubic ones, a schedule; the coefficients differ from step to step."""
+    G = gradients(2, m, n, prec, seed=5)
+    for c in ([(1.0, 0.0, 0.0)], [(1.5, -0.5, 0.0)] * 8, [(3.0, -3.2, 1.2), (2.0, -1.5, 0.5), (1.875, -1.25, 0.375)], [(0.0, 0.0, 1.0)] * 2):
+        orth_check(run(G, coefficients=c, eps=1e-3), G, prec, (m, n, c), coefficients=c, eps=1e-3)
+
+
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("m,n", [(12, 20), (128, 128), (150, 140), (64, 700)])
+def test_zeros_and_numbers_that_are_not_finite_stay_in_their_matrices(m, n, prec):
+    G = gradients(5, m, n, prec, seed=6)
+    G[1] = 0
+    ref = run(G)
+    assert not ref[1].any()
+    bad = G.copy()
+    bad[0, 3, 4], bad[3, m - 1, n - 1] = np.nan, np.inf
+    got = run(bad)
+    assert np.isnan(got[[0, 3]]).all()
+    assert np.array_equal(got[[1, 2, 4]], ref[[1, 2, 4]])
+
+
+@pytest.mark.parametrize("prec", PRECS)
+def test_few_singular_values(prec):
+    """Gradients of fewer rows than columns have singular values of zero, which stay small."""
+    rng = np.random.default_rng(7)
+    G = (rng.normal(size=(2, 40, 3)) @ rng.normal(size=(2, 3, 50))).astype(NP[prec])
+    got = run(G)
+    orth_check(got, G, prec, "rank 3")
+    s = np.linalg.svd(got.astype(np.float64), compute_uv=False)
+    assert (s[:, :3] > 0.6).all() and (s[:, :3] < 1.25).all() and (s[:, 3:] < (1e-3 if prec == "f32" else 1e-11)).all()
+
+
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("scale", [1e-30, 1e-12, 1e25])
+def test_sizes_of_numbers(scale, prec):
+    G = (gradients(2, 24, 30, "f64", seed=8) * scale).astype(NP[prec])
+    orth_check(run(G, eps=1e-40), G, prec, scale, eps=1e-40)
+
+
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("m,n", [(20, 33), (64, 64), (130, 40), (131, 140)])
+def test_strides(m, n, prec):
+    """Columns of wider rows, and matrices side by side; what lies between is not touched, NaN between those of G not used."""
+    from paper_2501_13986_amd import binding as b
+    G = gradients(3, m, n, prec, seed=9)
+    t = torch.full((3, m + 2, n + 5), float("nan"), dtype=torch.from_numpy(G).dtype, device="cuda")
+    o = torch.full_like(t, float("nan"))
+    t[:, 1:m + 1, 3:n + 3] = torch.from_numpy(G).cuda()
+    b.orthogonalise(t[:, 1:m + 1, 3:n + 3], o[:, 1:m + 1, 3:n + 3])
+    got = o.cpu().numpy()
+    orth_check(got[:, 1:m + 1, 3:n + 3], G, prec, "inside")
+    got[:, 1:m + 1, 3:n + 3] = np.nan
+    assert np.isnan(got).all()
+    side = torch.full((m, 3, n), float("nan"), dtype=t.dtype, device="cuda")
+    b.orthogonalise(t[:, 1:m + 1, 3:n + 3], side.transpose(0, 1))
+    orth_check(side.transpose(0, 1).cpu().numpy(), G, prec, "side by side")
+    same = torch.from_numpy(G[:1]).cuda().expand(3, m, n)      # one matrix three times
+    three = torch.empty_like(same, memory_format=torch.contiguous_format)
+    b.orthogonalise(same, three)
+    assert torch.equal(three[0], three[1]) and torch.equal(three[0], three[2])
+
+
+def test_one_matrix_of_two_dimensions():
+    from paper_2501_13986_amd import binding as b
+    G = gradients(1, 30, 20, "f32")
+    out = torch.empty(30, 20, device="cuda")
+    assert b.orthogonalise(torch.from_numpy(G[0]).cuda(), out) is out
+    orth_check(out.cpu().numpy()[None], G, "f32", "matrix")
+
+
+@pytest.mark.parametrize("batch,m,n", [(3, 64, 500), (9, 128, 128), (1, 300, 320)])
+def test_runs_repeat_bit_for_bit_and_do_not_depend_on_the_batch(batch, m, n):
+    G = gradients(batch, m, n, "f32", seed=3)
+    a = run(G)
+    assert np.array_equal(a, run(G))
+    orth_check(run(G[-1:]), G[-1:], "f32", "alone")
+
+
+@pytest.mark.parametrize("m,n", [(24, 20), (128, 130), (20, 900), (200, 180)])
+def test_captured_and_replayed(m, n):
+    from paper_2501_13986_amd import binding as b
+    t = torch.from_numpy(gradients(3, m, n, "f32")).cuda()
+    out = torch.empty_like(t)
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        b.orthogonalise(t, out)
+    torch.cuda.synchronize()
+    graphs = []
+    for _ in range(2):      # two graphs with workspaces of their own
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            b.orthogonalise(t, out)
+        graphs.append(g)
+    for i in range(4):
+        t.copy_(torch.from_numpy(gradients(3, m, n, "f32", seed=30 + i)))
+        out.fill_(float("nan"))
+        graphs[i % 2].replay()
+        other = torch.empty_like(t)
+        b.orthogonalise(t, other)
+        torch.cuda.synchronize()
+        assert torch.equal(out, other)
+        orth_check(out.cpu().numpy(), t.cpu().numpy(), "f32", f"replay {i}")
+
+
+def test_two_streams():
+    from paper_2501_13986_amd import binding as b
+    t = torch.from_numpy(gradients(4, 100, 120, "f32")).cuda()
+    ref = torch.empty_like(t)
+    b.orthogonalise(t, ref)
+    torch.cuda.synchronize()
+    outs = [torch.empty_like(t) for _ in range(2)]
+    for o in outs:
+        with torch.cuda.stream(torch.cuda.Stream()):
+            b.orthogonalise(t, o)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], ref) and torch.equal(outs[1], ref)
