@@ -68,6 +68,18 @@ struct Operand<float, kR> {
 #pragma unroll
     for (int p = 0; p < 3; ++p) *(u32x2*)&v[p][r][at(r, k)] = u32x2{lo[p], hi[p]};
   }
+  __device__ void write_some(int r, int k, const float (&x)[1]) {
+    unsigned w[3];
+    Num<float>::split(x[0], 0.f, w);
+#pragma unroll
+    for (int p = 0; p < 3; ++p) *(unsigned short*)&v[p][r][at(r, k)] = (unsigned short)w[p];
+  }
+  __device__ void write_some(int r, int k, const float (&x)[2]) {
+    unsigned w[3];
+    Num<float>::split(x[0], x[1], w);
+#pragma unroll
+    for (int p = 0; p < 3; ++p) *(unsigned*)&v[p][r][at(r, k)] = w[p];
+  }
 };
 template <int kR>
 struct Operand<double, kR> {
@@ -82,6 +94,7 @@ struct Operand<double, kR> {
 #pragma unroll
     for (int h = 0; h < 2; ++h) *(u32x4*)&v[r][k + 2 * h] = __builtin_bit_cast(u32x4, f64x2{x[2 * h], x[2 * h + 1]});
   }
+  __device__ void write_some(int r, int k, const double (&x)[1]) { v[r][k] = x[0]; }
 };
 
 // An operand whose terms are neighbours in memory: a thread has four of them of each of kPer rows
@@ -137,6 +150,22 @@ struct Results {
   static __device__ int wave() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
   static __device__ int row(int rt) { return wave() / 2 * (kR / 2) + rt * 16 + lane() % 16; }
   static __device__ int column(int ct) { return wave() % 2 * (kC / 2) + ct * 16 + lane() / 16 * 4; }      // the first of four
+  // in the order of the registers: kR x kC numbers
+  __device__ void keep(T* to) const {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) *(typename N::Vec*)(to + ((rt * CT + ct) * kProductThreads + (int)threadIdx.x) * 4) = acc[rt][ct];
+  }
+  // the sum of `parts` such, in their order
+  __device__ void add_up(const T* from, int parts) {
+#pragma unroll 2
+    for (int p = 0; p < parts; ++p, from += kR * kC)
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) acc[rt][ct] += *(const typename N::Vec*)(from + ((rt * CT + ct) * kProductThreads + (int)threadIdx.x) * 4);
+  }
   __device__ void multiply(const Operand<T, kR>& R, const Operand<T, kC>& C) {
     const int l16 = lane() % 16, k = lane() / 16 * 8, r0 = wave() / 2 * (kR / 2), c0 = wave() % 2 * (kC / 2) + column_place<T>(l16);
     typename N::Parts c[CT];
