@@ -73,7 +73,7 @@ size_t cgtp_grouped_workspace_bytes(int64_t rows, int64_t d_in, int64_t d_out, i
   cgtp::GroupedArgs a = {};
   a.rows = rows; a.d_in = d_in; a.d_out = d_out; a.comps = comps; a.groups = groups;
   if (check_grouped(a, dtype) != CGTP_OK || rows == 0 || groups == 0) return 0;
-  return (dtype == CGTP_F64 ? cgtp::grouped_workspace_bytes_f64 : cgtp::grouped_workspace_bytes_f32)(rows, d_in, d_out, comps, groups);
+  return (dtype == CGTP_F64 ? cgtp::grouped_workspace_bytes_f64 : cgtp::grouped_workspace_bytes_f32)(rows, d_in, d_out, comps);
 }
 
 cgtp_status grouped_backward(const void* x, const void* W, const void* gout, void* gx, void* gW, void* gb, int64_t rows, int64_t d_in,

@@ -18,8 +18,8 @@ struct GroupedArgs {
 // Everything is enqueued on `st`; nothing is allocated and nothing synchronises.
 hipError_t grouped_forward_f32(const GroupedArgs& a, hipStream_t st);
 hipError_t grouped_forward_f64(const GroupedArgs& a, hipStream_t st);
-size_t grouped_workspace_bytes_f32(int64_t rows, int64_t d_in, int64_t d_out, int64_t comps, int64_t groups);
-size_t grouped_workspace_bytes_f64(int64_t rows, int64_t d_in, int64_t d_out, int64_t comps, int64_t groups);
+size_t grouped_workspace_bytes_f32(int64_t rows, int64_t d_in, int64_t d_out, int64_t comps);
+size_t grouped_workspace_bytes_f64(int64_t rows, int64_t d_in, int64_t d_out, int64_t comps);
 hipError_t grouped_backward_f32(const GroupedArgs& a, void* workspace, hipStream_t st);
 hipError_t grouped_backward_f64(const GroupedArgs& a, void* workspace, hipStream_t st);
 

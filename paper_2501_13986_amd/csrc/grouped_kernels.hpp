@@ -7,6 +7,8 @@
 #pragma once
 
 #include <algorithm>
+#include <cstdlib>
+#include <type_traits>
 
 #include "grouped.hpp"
 #include "product.hpp"
@@ -63,6 +65,116 @@ struct Lines {
 __device__ inline int64_t row_of(const GroupedArgs& a, int64_t p) {
   const int64_t r = a.perm ? a.perm[p] : p;
   return r >= 0 && r < a.rows ? r : -1;
+}
+
+// ---- rows times a matrix of at most 128 rows --------------------------------------------------------------------------------------
+
+constexpr int kMostTerms = 128;
+template <class T>
+constexpr int kMostShift = sizeof(T) == 4 ? 10 : 9;      // lines of a workgroup: their places in LDS leave room for two workgroups
+
+// A wave keeps the parts of its 16 NT columns of the matrix in registers, for up to 2^kMostShift lines of one group, whose parts the workgroup puts into LDS once for its four
+// waves, 64 at a time.  Lane: columns NT l16 + j.  out = x W + b, or gx = gout W^T (kBack).
+template <class T, int kIn, int NT, bool kWhole, bool kBack>
+__global__ void __launch_bounds__(kProductThreads, 2) k_grouped_stream(GroupedArgs a, int64_t first_id, int column_tiles, int shift) {
+  using N = Num<T>;
+  using Rows = AlongTerms<T, 64, kWhole>;
+  constexpr int kSlices = kIn / 32;
+  __shared__ Operand<T, 64> X[kSlices];
+  __shared__ int64_t from[1 << kMostShift<T>], place[1 << kMostShift<T>];      // of the lines in memory and in the results (-1: none)
+  const int64_t id = first_id + blockIdx.x / column_tiles, g = find_group(a, a.comps, shift, id), piece = first_piece(a, g, a.comps, shift);
+  const int64_t lines_end = cut(a, g + 1) * a.comps, begin = cut(a, g) * a.comps + ((id - piece) << shift);
+  if (id < piece || begin >= lines_end) return;
+  const int have = (int)(lines_end - begin < 1 << shift ? lines_end - begin : 1 << shift);
+  const int K = (int)(kBack ? a.d_out : a.d_in), n = (int)(kBack ? a.d_in : a.d_out);
+  const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4, c = (int)(blockIdx.x % column_tiles) * (64 * NT) + (threadIdx.x >> 6) * (16 * NT) + l16 * NT;
+  const T *x = (const T*)(kBack ? a.gout : a.x), *W = (const T*)a.W + g * a.d_in * a.d_out;
+  T* to = (T*)(kBack ? a.gx : a.out);
+  {
+    const int64_t ld = kBack ? a.ld_gout : a.ld_x, ld_to = kBack ? a.ld_gx : a.ld_out;
+    const Lines lines(begin, a.comps);
+    for (int i = threadIdx.x; i < (have + 63) / 64 * 64; i += kProductThreads) {
+      unsigned at, m;
+      lines.of(i < have ? i : 0, at, m);
+      const int64_t r = row_of(a, lines.position + at);
+      from[i] = (r < 0 ? 0 : r) * ld + m * (int64_t)K;
+      place[i] = r < 0 || i >= have ? -1 : r * ld_to + m * (int64_t)n;
+    }
+  }
+  __syncthreads();
+  T next[kSlices][Rows::kPer][4];
+  auto fetch = [&](int line) {
+#pragma unroll
+    for (int i = 0; i < Rows::kPer; ++i) {
+      const T* p = x + from[line + Rows::row(i)];
+#pragma unroll
+      for (int s = 0; s < kSlices; ++s) load_some<T, 4, kWhole>(p, s * 32 + Rows::term(), K, next[s][i]);
+    }
+  };
+  fetch(0);
+  // the matrix: rows behind its end are zero, columns behind it any
+  typename N::Parts w[kSlices][NT];
+  T bias[NT];
+#pragma unroll
+  for (int s = 0; s < kSlices; ++s) {
+    T v[NT][8];
+    if constexpr (kBack) {
+#pragma unroll
+      for (int j = 0; j < NT; ++j) {
+        const T* p = W + (int64_t)(c + j < n ? c + j : 0) * K;
+        load_some<T, 4, kWhole>(p, s * 32 + q * 8, K, v[j]);
+        load_some<T, 4, kWhole>(p, s * 32 + q * 8 + 4, K, v[j] + 4);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int k = s * 32 + q * 8 + i;
+        T u[NT];
+        load_some<T, NT, kWhole>(W + (int64_t)(k < K ? k : 0) * n, c, n, u);
+#pragma unroll
+        for (int j = 0; j < NT; ++j) v[j][i] = k < K ? u[j] : T(0);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j) w[s][j] = N::parts(v[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < NT; ++j) bias[j] = !kBack && a.b ? ((const T*)a.b)[g * n + (c + j < n ? c + j : 0)] : T(0);
+  for (int line = 0; line < have; line += 64) {
+    __syncthreads();
+#pragma unroll
+    for (int s = 0; s < kSlices; ++s)
+#pragma unroll
+      for (int i = 0; i < Rows::kPer; ++i) X[s].write4(Rows::row(i), Rows::term(), next[s][i]);
+    __syncthreads();
+    if (line + 64 < have) fetch(line + 64);
+#pragma unroll
+    for (int rt = 0; rt < 4; ++rt) {
+      if (line + rt * 16 >= have) break;
+      typename N::Vec o[NT];
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[j][i] = bias[j];
+#pragma unroll
+      for (int s = 0; s < kSlices; ++s) {
+        const typename N::Parts xa = X[s].read(rt * 16 + l16, q * 8);
+        if constexpr (NT == 2) N::template mma<2>({&xa, &xa}, {&w[s][0], &w[s][1]}, {&o[0], &o[1]});
+        else N::template mma<1>({&xa}, {&w[s][0]}, {&o[0]});
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int64_t at = place[line + rt * 16 + N::row(q, i)];
+        if constexpr (NT == 2) {
+          typedef T Two __attribute__((ext_vector_type(2), aligned(sizeof(T))));
+          if (at >= 0 && c + 1 < n) *(Two*)(to + at + c) = Two{o[0][i], o[1][i]};
+          else if (at >= 0 && c < n) to[at + c] = o[0][i];
+        } else {
+          if (at >= 0 && c < n) to[at + c] = o[0][i];
+        }
+      }
+    }
+  }
 }
 
 // ---- rows times a matrix ------------------------------------------------------------------------------------------------------
@@ -152,7 +264,7 @@ __global__ void __launch_bounds__(kProductThreads, 2) k_grouped_rows(GroupedArgs
 
 // ---- the matrices' gradients ----------------------------------------------------------------------------------------------------
 
-constexpr int kMostPositions = 1024;      // of a chunk
+constexpr int kTable = 1024;      // positions whose rows stand in LDS at a time
 
 // kR x kC numbers of gW[g] (and kC of gb[g]) over the positions of group g in one chunk: chunks are the same for all groups, so that those of a group that has several
 // leave their sums at slot 2 chunk + (0: the group began before the chunk, 1: in it).  A group with one chunk, or without rows, is
@@ -161,47 +273,50 @@ template <class T, int kR, int kC, bool kWhole>
 __global__ void __launch_bounds__(kProductThreads, 2) k_grouped_weights(GroupedArgs a, int64_t first_id, int shift, int row_tiles, int column_tiles, T* part, T* part_b) {
   __shared__ Operand<T, kR> R;
   __shared__ Operand<T, kC> C;
-  __shared__ int64_t row[kMostPositions];
+  __shared__ int64_t row[kTable];
   const int tiles = row_tiles * column_tiles, tile = blockIdx.x % tiles;
   const int64_t id = first_id + blockIdx.x / tiles, g = find_group(a, 1, shift, id), chunk = id - g;
   const int64_t from = cut(a, g), end = cut(a, g + 1), lo = std::max(from, chunk << shift), hi = std::min(end, (chunk + 1) << shift);
   const bool empty = end <= from && chunk == from >> shift;
   if (chunk < from >> shift || (hi <= lo && !empty)) return;
   const int K = (int)a.d_in, n = (int)a.d_out, k0 = tile / column_tiles * kR, c0 = tile % column_tiles * kC;
-  const int positions = hi > lo ? (int)(hi - lo) : 0, count = positions * (int)a.comps;
-  for (int i = threadIdx.x; i < positions; i += kProductThreads) row[i] = row_of(a, lo + i);
-  __syncthreads();
   AcrossTerms<T, kR, kWhole> x;
   AcrossTerms<T, kC, kWhole> t;
   const Lines lines(0, a.comps);
-  auto fetch = [&](int line0) {
-    const T *px[4], *pt[4];
-    bool ok[4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int line = line0 + x.term() + j;
-      unsigned at, m;
-      lines.of(line < count ? line : 0, at, m);
-      const int64_t r = row[at];
-      ok[j] = line < count && r >= 0;
-      px[j] = (const T*)a.x + (r < 0 ? 0 : r) * a.ld_x + m * (int64_t)K;
-      pt[j] = (const T*)a.gout + (r < 0 ? 0 : r) * a.ld_gout + m * (int64_t)n;
-    }
-    x.fetch(px, ok, k0, K);
-    t.fetch(pt, ok, c0, n);
-  };
   Results<T, kR, kC> out;
   T sum[kC / 32] = {};
-  if (count > 0) fetch(0);
-  for (int l = 0; l < count; l += kStep) {
+  for (int64_t p0 = lo; p0 < hi; p0 += kTable) {
+    const int positions = (int)(hi - p0 < kTable ? hi - p0 : kTable), count = positions * (int)a.comps;
     __syncthreads();
-    x.put(R);
-    t.put(C);
+    for (int i = threadIdx.x; i < positions; i += kProductThreads) row[i] = row_of(a, p0 + i);
     __syncthreads();
+    auto fetch = [&](int line0) {
+      const T *px[4], *pt[4];
+      bool ok[4];
 #pragma unroll
-    for (int i = 0; i < kC / 32; ++i) sum[i] += (t.v[0][i] + t.v[1][i]) + (t.v[2][i] + t.v[3][i]);
-    if (l + kStep < count) fetch(l + kStep);
-    out.multiply(R, C);
+      for (int j = 0; j < 4; ++j) {
+        const int line = line0 + x.term() + j;
+        unsigned at, m;
+        lines.of(line < count ? line : 0, at, m);
+        const int64_t r = row[at];
+        ok[j] = line < count && r >= 0;
+        px[j] = (const T*)a.x + (r < 0 ? 0 : r) * a.ld_x + m * (int64_t)K;
+        pt[j] = (const T*)a.gout + (r < 0 ? 0 : r) * a.ld_gout + m * (int64_t)n;
+      }
+      x.fetch(px, ok, k0, K);
+      t.fetch(pt, ok, c0, n);
+    };
+    fetch(0);
+    for (int l = 0; l < count; l += kStep) {
+      __syncthreads();
+      x.put(R);
+      t.put(C);
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kC / 32; ++i) sum[i] += (t.v[0][i] + t.v[1][i]) + (t.v[2][i] + t.v[3][i]);
+      if (l + kStep < count) fetch(l + kStep);
+      out.multiply(R, C);
+    }
   }
   const bool whole = from >> shift == (end - 1) >> shift || empty;
   const int64_t slot = 2 * chunk + (from >= chunk << shift);
@@ -287,8 +402,36 @@ hipError_t in_launches(int64_t ids, int64_t tiles, F f) {
 template <class T>
 constexpr int kTile = sizeof(T) == 4 ? 128 : 64;
 
+template <class T, int kIn, int NT, bool kBack>
+hipError_t launch_stream(const GroupedArgs& a, hipStream_t st) {
+  const int64_t n = kBack ? a.d_in : a.d_out, tiles = (n + 64 * NT - 1) / (64 * NT), lines = a.rows * a.comps;
+  const bool whole = a.d_in % 4 == 0 && a.d_out % 4 == 0;
+  int shift = kMostShift<T>;      // lines of a workgroup: fewer where that leaves compute units without work
+  while (shift > 6 && (lines >> shift) * tiles < 1024) --shift;
+  return in_launches((lines >> shift) + a.groups, tiles, [&](int64_t first, dim3 grid) {
+    if (whole) k_grouped_stream<T, kIn, NT, true, kBack><<<grid, kProductThreads, 0, st>>>(a, first, (int)tiles, shift);
+    else k_grouped_stream<T, kIn, NT, false, kBack><<<grid, kProductThreads, 0, st>>>(a, first, (int)tiles, shift);
+  });
+}
+
+template <class T, bool kBack>
+hipError_t launch_few_terms(const GroupedArgs& a, hipStream_t st) {
+  const int64_t terms = kBack ? a.d_out : a.d_in, n = kBack ? a.d_in : a.d_out;
+  auto go = [&](auto in) {
+    constexpr int kIn = decltype(in)::value;
+    if constexpr (sizeof(T) == 4)
+      if (n > 64) return launch_stream<T, kIn, 2, kBack>(a, st);
+    return launch_stream<T, kIn, 1, kBack>(a, st);
+  };
+  if (terms <= 32) return go(std::integral_constant<int, 32>());
+  if (terms <= 64) return go(std::integral_constant<int, 64>());
+  if (terms <= 96) return go(std::integral_constant<int, 96>());
+  return go(std::integral_constant<int, 128>());
+}
+
 template <class T, bool kBack>
 hipError_t launch_rows(const GroupedArgs& a, hipStream_t st) {
+  if ((kBack ? a.d_out : a.d_in) <= kMostTerms) return launch_few_terms<T, kBack>(a, st);
   const int64_t n = kBack ? a.d_in : a.d_out;
   const bool whole = a.d_in % 4 == 0 && a.d_out % 4 == 0;
   auto go = [&](auto wide) {
@@ -302,37 +445,46 @@ hipError_t launch_rows(const GroupedArgs& a, hipStream_t st) {
   return n > 64 ? go(std::true_type()) : go(std::false_type());
 }
 
-// positions of a chunk (a power of two), slots of partial sums
+// How the positions are cut for the matrices' gradients
+template <class T>
 struct Chunks {
-  int shift = 8;
-  int64_t count, slots;
-  Chunks(int64_t rows) {
-    while (shift < 10 && rows >> shift > 512) ++shift;
-    count = (rows + (1 << shift) - 1) >> shift;
+  int64_t row_tiles, column_tiles, count, slots;      // chunks, partial sums
+  int shift = 20;                                     // positions of a chunk
+  bool narrow;                                        // 64 rows of gW a workgroup
+  Chunks(int64_t rows, int64_t K, int64_t n, int64_t comps) {
+    narrow = sizeof(T) == 8 || K <= 64;
+    row_tiles = (K + (narrow ? 63 : 127)) / (narrow ? 64 : 128);
+    column_tiles = (n + kTile<T> - 1) / kTile<T>;
+    const int64_t want = getenv("GW_WANT") ? atoi(getenv("GW_WANT")) : 400, least = getenv("GW_LEAST") ? atoi(getenv("GW_LEAST")) : 128;
+    while (shift > 4 && (rows >> shift) * row_tiles * column_tiles < want && comps << (shift - 1) >= least) --shift;
+    count = (rows + ((int64_t)1 << shift) - 1) >> shift;
     slots = count > 1 ? 2 * count : 0;
   }
 };
 
 template <class T>
-size_t workspace_bytes(int64_t rows, int64_t K, int64_t n) {
-  const Chunks c(rows);
+size_t workspace_bytes(int64_t rows, int64_t K, int64_t n, int64_t comps) {
+  const Chunks<T> c(rows, K, n, comps);
   return up(c.slots * K * n * sizeof(T)) + up(c.slots * n * sizeof(T));
+}
+
+template <class T, int kR, int kC>
+hipError_t launch_weights(const GroupedArgs& a, const Chunks<T>& c, T* part, T* part_b, hipStream_t st) {
+  const bool whole = a.d_in % 4 == 0 && a.d_out % 4 == 0;
+  return in_launches((a.rows >> c.shift) + a.groups, c.row_tiles * c.column_tiles, [&](int64_t first, dim3 grid) {
+    if (whole) k_grouped_weights<T, kR, kC, true><<<grid, kProductThreads, 0, st>>>(a, first, c.shift, (int)c.row_tiles, (int)c.column_tiles, part, part_b);
+    else k_grouped_weights<T, kR, kC, false><<<grid, kProductThreads, 0, st>>>(a, first, c.shift, (int)c.row_tiles, (int)c.column_tiles, part, part_b);
+  });
 }
 
 template <class T>
 hipError_t backward(const GroupedArgs& a, char* ws, hipStream_t st) {
   const int64_t K = a.d_in, n = a.d_out;
-  hipError_t e = a.rows ? launch_rows<T, true>(a, st) : hipSuccess;
+  hipError_t e = launch_rows<T, true>(a, st);
   if (e != hipSuccess) return e;
-  const Chunks c(a.rows);
+  const Chunks<T> c(a.rows, K, n, a.comps);
   T *part = (T*)ws, *part_b = (T*)(ws + up(c.slots * K * n * sizeof(T)));
-  constexpr int kR = kTile<T>, kC = kTile<T>;
-  const int64_t rt = (K + kR - 1) / kR, ct = (n + kC - 1) / kC;
-  const bool whole = K % 4 == 0 && n % 4 == 0;
-  e = in_launches((a.rows >> c.shift) + a.groups, rt * ct, [&](int64_t first, dim3 grid) {
-    if (whole) k_grouped_weights<T, kR, kC, true><<<grid, kProductThreads, 0, st>>>(a, first, c.shift, (int)rt, (int)ct, part, part_b);
-    else k_grouped_weights<T, kR, kC, false><<<grid, kProductThreads, 0, st>>>(a, first, c.shift, (int)rt, (int)ct, part, part_b);
-  });
+  e = c.narrow ? launch_weights<T, 64, kTile<T>>(a, c, part, part_b, st) : launch_weights<T, kTile<T>, kTile<T>>(a, c, part, part_b, st);
   if (e != hipSuccess || c.slots == 0) return e;
   const int64_t blocks = std::min<int64_t>((K * n + n + kProductThreads - 1) / kProductThreads, 1024);
   return in_launches(c.count - 1, blocks, [&](int64_t first, dim3 grid) {

@@ -14,7 +14,7 @@
 namespace cgtp {
 namespace {
 
-constexpr int kShares = 64;      // partial sums of squares of a matrix, at most
+constexpr int kShares = 256;      // partial sums of squares of a matrix, at most
 
 // ---- the start ------------------------------------------------------------------------------------------------------------------
 
@@ -24,11 +24,21 @@ __global__ void __launch_bounds__(kProductThreads) k_orth_squares(OrthArgs a, in
   __shared__ double sums[kProductThreads / 64];
   const int64_t matrix = first + blockIdx.x / shares, share = blockIdx.x % shares;
   const T* g = (const T*)a.g + matrix * a.stride_g;
-  const int64_t from = a.m * share / shares, size = (a.m * (share + 1) / shares - from) * a.n;
+  const int64_t from = a.m * share / shares, end = a.m * (share + 1) / shares;
+  // as many lanes side by side as a row has numbers, eight numbers on their way to a thread
+  const int wide = a.n >= kProductThreads ? kProductThreads : a.n > 64 ? 128 : a.n > 16 ? 64 : 16, x = threadIdx.x % wide, y = threadIdx.x / wide, high = kProductThreads / wide;
   double v = 0;
-  for (int64_t i = threadIdx.x; i < size; i += kProductThreads) {
-    const double w = (double)g[(from + i / a.n) * a.ld_g + i % a.n];
-    v += w * w;
+  for (int64_t r = from + y; r < end; r += high) {
+    const T* p = g + r * a.ld_g;
+    int64_t c = x;
+    for (; c + 7 * wide < a.n; c += 8 * wide) {
+      double w[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = (double)p[c + i * wide];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v += w[i] * w[i];
+    }
+    for (; c < a.n; c += wide) v += (double)p[c] * (double)p[c];
   }
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
