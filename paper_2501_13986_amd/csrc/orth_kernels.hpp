@@ -2,10 +2,10 @@
 //
 // X = G / (|G| + eps), transposed if G has more rows than columns, so that X is s x l with s <= l; a step is
 //     A = X X^T,  B = b A + c A A,  X <- a X + B X.
-// A and B are symmetric: tiles on and above the diagonal are formed and written twice.
 #pragma once
 
 #include <algorithm>
+#include <cstdlib>
 #include <type_traits>
 
 #include "orth.hpp"
@@ -47,34 +47,130 @@ __global__ void __launch_bounds__(kProductThreads) k_orth_squares(OrthArgs a, in
   if (threadIdx.x == 0) part[matrix * shares + share] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
 }
 
+// 1 / (|G| + eps), by all lanes of a wave
 __device__ inline double scale_of(const double* part, int shares, double eps) {
   double v = 0;
-  for (int i = 0; i < shares; ++i) v += part[i];
+  for (int i = (int)threadIdx.x & 63; i < (shares + 63) / 64 * 64; i += 64) v += i < shares ? part[i < shares ? i : 0] : 0;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
   return 1.0 / (sqrt(v) + eps);
 }
 
-// X, 64 x 64 numbers of G a workgroup; rounded once
+// ---- more rows --------------------------------------------------------------------------------------------------------------------
+//
+// X, its transpose, A and B stand in memory as operands: in parts, cut once by the kernel that writes them, in blocks of 64 rows x 32 terms, padded with
+// zeros.  A product is tiles of kTile x kTile results with the terms in splits, so that there is work for all compute units; sums of splits are left in
+// the order of the registers and added up, in their order, by k_orth_finish, which turns the results into operands both ways.  With one split the product does that itself.
+
+constexpr int kBlock = 64;
+
+// numbers [rows, terms] as an operand of products; sizes are those of the padded matrix
 template <class T>
-__global__ void __launch_bounds__(kProductThreads) k_orth_start(OrthArgs a, int64_t first, int64_t tiles, int shares, const double* part, T* X) {
-  __shared__ T tile[64][65];
-  const int64_t matrix = first + blockIdx.x / tiles, across = (a.n + 63) / 64, r0 = blockIdx.x % tiles / across * 64, c0 = blockIdx.x % tiles % across * 64;
+struct Stored;
+template <>
+struct Stored<float> {
+  static constexpr int kBytes = 6;
+  unsigned short* p;
+  int64_t plane;      // from one part to the next
+  int ld;             // blocks a row of blocks
+  __device__ Stored(void* at, int64_t rows, int64_t terms) : p((unsigned short*)at), plane(rows * terms), ld((int)(terms / kStep)) {}
+  __device__ int64_t at(int r, int k) const { return ((int64_t)(r / kBlock) * ld + k / kStep) * (kBlock * kStep) + r % kBlock * kStep + k % kStep; }
+  __device__ void write4(int r, int k, const float* x) const {
+    unsigned lo[3], hi[3];
+    Num<float>::split(x[0], x[1], lo);
+    Num<float>::split(x[2], x[3], hi);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) *(u32x2*)(p + i * plane + at(r, k)) = u32x2{lo[i], hi[i]};
+  }
+  // the parts' sum is the number itself
+  __device__ void read4(int r, int k, float* x) const {
+    u32x2 w[3];
+#pragma unroll
+    for (int i = 0; i < 3; ++i) w[i] = *(const u32x2*)(p + i * plane + at(r, k));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float v[3];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) v[i] = __builtin_bit_cast(float, j & 1 ? w[i][j / 2] & 0xffff0000u : w[i][j / 2] << 16);
+      x[j] = (v[2] + v[1]) + v[0];
+    }
+  }
+};
+template <>
+struct Stored<double> {
+  static constexpr int kBytes = 8;
+  double* p;
+  int ld;
+  __device__ Stored(void* at, int64_t, int64_t terms) : p((double*)at), ld((int)(terms / kStep)) {}
+  __device__ int64_t at(int r, int k) const { return ((int64_t)(r / kBlock) * ld + k / kStep) * (kBlock * kStep) + r % kBlock * kStep + k % kStep; }
+  __device__ void write4(int r, int k, const double* x) const { *(f64x4*)(p + at(r, k)) = f64x4{x[0], x[1], x[2], x[3]}; }
+  __device__ void read4(int r, int k, double* x) const {
+    const f64x4 w = *(const f64x4*)(p + at(r, k));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = w[j];
+  }
+};
+
+// kR rows of 32 terms on their way to LDS
+template <class T, int kR>
+struct Copy;
+template <int kR>
+struct Copy<float, kR> {
+  static constexpr int kPer = 3 * kR / kBlock;
+  u32x4 v[kPer];
+  __device__ void fetch(const Stored<float>& from, int r0, int k0) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      v[i] = *(const u32x4*)(from.p + i / (kR / kBlock) * from.plane + ((int64_t)(r0 / kBlock + i % (kR / kBlock)) * from.ld + k0 / kStep) * (kBlock * kStep) + threadIdx.x * 8);
+  }
+  __device__ void put(Operand<float, kR>& to) const {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) {
+      const int r = i % (kR / kBlock) * kBlock + (int)threadIdx.x / 4;
+      *(u32x4*)&to.v[i / (kR / kBlock)][r][to.at(r, (int)threadIdx.x % 4 * 8)] = v[i];
+    }
+  }
+};
+template <int kR>
+struct Copy<double, kR> {
+  static constexpr int kPer = 4 * kR / kBlock;
+  u32x4 v[kPer];
+  __device__ void fetch(const Stored<double>& from, int r0, int k0) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+      v[i] = *(const u32x4*)(from.p + ((int64_t)(r0 / kBlock + i / 4) * from.ld + k0 / kStep) * (kBlock * kStep) + (i % 4 * kProductThreads + threadIdx.x) * 2);
+  }
+  __device__ void put(Operand<double, kR>& to) const {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) *(u32x4*)&to.v[i / 4 * kBlock + i % 4 * 16 + (int)threadIdx.x / 16][(int)threadIdx.x % 16 * 2] = v[i];
+  }
+};
+
+// X and its transpose, 64 x 64 numbers of G a workgroup; rounded once.  s, l: padded
+template <class T>
+__global__ void __launch_bounds__(kProductThreads) k_orth_start(OrthArgs a, int64_t first, int tiles, int s, int l, int shares, const double* part, char* X, char* XT) {
+  __shared__ T tile[kBlock][kBlock + 1];
+  const int64_t matrix = first + blockIdx.x / tiles, size = (int64_t)s * l * Stored<T>::kBytes;
+  const bool turned = a.m > a.n;
+  const int across = l / kBlock, r0 = blockIdx.x % tiles / across * kBlock, c0 = blockIdx.x % tiles % across * kBlock;      // of X
   const double scale = scale_of(part + matrix * shares, shares, a.eps);
   const T* g = (const T*)a.g + matrix * a.stride_g;
-  T* to = X + matrix * a.m * a.n;
-  const int x = threadIdx.x % 64;
-  if (a.m <= a.n) {
-    for (int y = threadIdx.x / 64; y < 64; y += 4)
-      if (r0 + y < a.m && c0 + x < a.n) to[(r0 + y) * a.n + c0 + x] = (T)((double)g[(r0 + y) * a.ld_g + c0 + x] * scale);
-    return;
+  const Stored<T> to(X + matrix * size, s, l), to_t(XT + matrix * size, l, s);
+  const int x = threadIdx.x % kBlock;
+  for (int y = threadIdx.x / kBlock; y < kBlock; y += kProductThreads / kBlock) {      // neighbours of G side by side
+    const int64_t r = (turned ? c0 : r0) + y, c = (turned ? r0 : c0) + x;
+    const T v = r < a.m && c < a.n ? (T)((double)g[r * a.ld_g + c] * scale) : T(0);
+    if (turned) tile[x][y] = v;
+    else tile[y][x] = v;
   }
-  for (int y = threadIdx.x / 64; y < 64; y += 4)
-    if (r0 + y < a.m && c0 + x < a.n) tile[y][x] = (T)((double)g[(r0 + y) * a.ld_g + c0 + x] * scale);
   __syncthreads();
-  for (int y = threadIdx.x / 64; y < 64; y += 4)
-    if (c0 + y < a.n && r0 + x < a.m) to[(c0 + y) * a.m + r0 + x] = tile[x][y];
+  for (int i = threadIdx.x; i < kBlock * kBlock / 4; i += kProductThreads) {
+    const int y = i / 16, k = i % 16 * 4;
+    const T v[4] = {tile[y][k], tile[y][k + 1], tile[y][k + 2], tile[y][k + 3]}, u[4] = {tile[k][y], tile[k + 1][y], tile[k + 2][y], tile[k + 3][y]};
+    to.write4(r0 + y, c0 + k, v);
+    to_t.write4(c0 + y, r0 + k, u);
+  }
 }
-
-// ---- the products of a step -----------------------------------------------------------------------------------------------------
 
 // tile number -> row and column of tiles, on and above the diagonal
 __device__ inline void upper_tile(int t, int& r, int& c) {
@@ -84,117 +180,128 @@ __device__ inline void upper_tile(int t, int& r, int& c) {
   r = t - c * (c + 1) / 2;
 }
 
-// to = alpha Y Y^T (+ beta Y where Y is s x s: it is symmetric itself), Y [s, terms]
-template <class T, int kR, bool kWhole>
-__global__ void __launch_bounds__(kProductThreads, 2) k_orth_square(int64_t first, int tiles, int s, int terms, const T* Y, T alpha, T beta, T* to) {
-  __shared__ Operand<T, kR> R, C;
-  const int64_t matrix = first + blockIdx.x / tiles;
-  int tr, tc;
-  upper_tile(blockIdx.x % tiles, tr, tc);
-  const int r0 = tr * kR, c0 = tc * kR;
-  Y += matrix * s * terms;
-  to += matrix * s * s;
-  using Along = AlongTerms<T, kR, kWhole>;
-  Along rows, columns;
-  const T *pr[Along::kPer], *pc[Along::kPer];
-#pragma unroll
-  for (int i = 0; i < Along::kPer; ++i) {
-    const int r = r0 + Along::row(i), c = c0 + Along::row(i);
-    pr[i] = Y + (int64_t)(r < s ? r : 0) * terms;
-    pc[i] = Y + (int64_t)(c < s ? c : 0) * terms;
+// A product R C^T [rows, columns]: alpha Y + beta R C^T of it is kept in to (and its transpose in to_t), or in the caller's output.  Symmetric: the tiles on and above the
+// diagonal alone, whose transposes are the others.
+struct Product {
+  char *rows_at, *columns_at, *y, *to, *to_t;
+  int rows, columns, terms, tiles, splits;      // padded; tiles a matrix
+  double alpha, beta;
+  bool symmetric, last;
+};
+
+constexpr int kStrip = 32;      // rows of a tile that are turned at a time: 16 of each half
+
+template <class T, int kTile>
+union ProductLds {
+  struct {
+    Operand<T, kTile> R, C;
+  } in;
+  T out[kStrip][kTile + 1];
+  __device__ ProductLds() {}
+};
+
+template <class T, int kTile>
+__device__ inline void tile_of(const Product& p, int t, int& tr, int& tc) {
+  if (p.symmetric) {
+    upper_tile(t, tr, tc);
+  } else {
+    tr = t / (p.columns / kTile);
+    tc = t % (p.columns / kTile);
   }
-  Results<T, kR, kR> out;
-  rows.fetch(pr, 0, terms);
-  columns.fetch(pc, 0, terms);
-  for (int k0 = 0; k0 < terms; k0 += kStep) {
-    __syncthreads();
-    rows.put(R);
-    columns.put(C);
-    __syncthreads();
-    if (k0 + kStep < terms) {
-      rows.fetch(pr, k0 + kStep, terms);
-      columns.fetch(pc, k0 + kStep, terms);
-    }
-    out.multiply(R, C);
-  }
-#pragma unroll
-  for (int rt = 0; rt < out.RT; ++rt)
-#pragma unroll
-    for (int ct = 0; ct < out.CT; ++ct) {
-      const int r = r0 + out.row(rt), c = c0 + out.column(ct);
-      if (r >= s || c >= s) continue;
-      T v[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        v[i] = alpha * out.acc[rt][ct][i];
-        if (beta != T(0)) v[i] += beta * Y[(int64_t)r * s + (c + i < s ? c + i : c)];
-      }
-      store_some(to + (int64_t)r * s + c, v, s - c);
-      if (tr != tc)
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (c + i < s) to[(int64_t)(c + i) * s + r] = v[i];
-    }
 }
 
-// to = alpha X + B X, X [s, l]; kLast: to is the caller's output, transposed where X is
-template <class T, int kR, int kC, bool kWhole, bool kLast>
-__global__ void __launch_bounds__(kProductThreads, 2) k_orth_apply(int64_t first, int tiles, int s, int l, const T* X, const T* B, T alpha, T* to, int64_t ld, int64_t stride, bool turned) {
-  __shared__ Operand<T, kR> R;
-  __shared__ Operand<T, kC> C;
-  const int64_t matrix = first + blockIdx.x / tiles;
-  const int across = (l + kC - 1) / kC, r0 = blockIdx.x % tiles / across * kR, c0 = blockIdx.x % tiles % across * kC;
-  X += matrix * s * l;
-  B += matrix * s * s;
-  to += matrix * stride;
-  using Along = AlongTerms<T, kR, kWhole>;
-  Along rows;
-  AcrossTerms<T, kC, kWhole> columns;
-  const T* pr[Along::kPer];
+// the rows of tiles rt of the four waves
+template <class T, int kTile, class Vec>
+__device__ inline void finish(const OrthArgs& a, const Product& p, int64_t matrix, int tr, int tc, int rt, const Vec (&acc)[kTile / 32], T (&tile)[kStrip][kTile + 1]) {
+  using Out = Results<T, kTile, kTile>;
+  const int64_t size = (int64_t)p.rows * p.columns * Stored<T>::kBytes;
+  const int r0 = tr * kTile, c0 = tc * kTile;
+  const T alpha = (T)p.alpha, beta = (T)p.beta;
+  auto row = [&](int y) { return r0 + y / 16 * (kTile / 2) + rt * 16 + y % 16; };
 #pragma unroll
-  for (int i = 0; i < Along::kPer; ++i) {
-    const int r = r0 + Along::row(i);
-    pr[i] = B + (int64_t)(r < s ? r : 0) * s;
-  }
-  auto fetch = [&](int k0) {
-    rows.fetch(pr, k0, s);
-    const T* p[4];
-    bool ok[4];
+  for (int ct = 0; ct < Out::CT; ++ct) {
+    const int r = Out::row(rt), c = Out::column(ct), y16 = Out::wave() / 2 * 16 + Out::lane() % 16;
+    T v[4], y[4] = {};
+    if (p.alpha != 0) Stored<T>(p.y + matrix * size, p.rows, p.columns).read4(r0 + r, c0 + c, y);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int k = k0 + columns.term() + j;
-      ok[j] = k < s;
-      p[j] = X + (int64_t)(ok[j] ? k : 0) * l;
+    for (int i = 0; i < 4; ++i) {
+      v[i] = beta * acc[ct][i] + alpha * y[i];
+      tile[y16][c + i] = v[i];
     }
-    columns.fetch(p, ok, c0, l);
-  };
-  Results<T, kR, kC> out;
-  fetch(0);
-  for (int k0 = 0; k0 < s; k0 += kStep) {
-    __syncthreads();
-    rows.put(R);
-    columns.put(C);
-    __syncthreads();
-    if (k0 + kStep < s) fetch(k0 + kStep);
-    out.multiply(R, C);
+    if (!p.last) Stored<T>(p.to + matrix * size, p.rows, p.columns).write4(r0 + r, c0 + c, v);
   }
-#pragma unroll
-  for (int rt = 0; rt < out.RT; ++rt)
-#pragma unroll
-    for (int ct = 0; ct < out.CT; ++ct) {
-      const int r = r0 + out.row(rt), c = c0 + out.column(ct);
-      if (r >= s || c >= l) continue;
-      T v[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = out.acc[rt][ct][i] + alpha * X[(int64_t)r * l + (c + i < l ? c + i : c)];
-      if (kLast && turned) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (c + i < l) to[(c + i) * ld + r] = v[i];
-      } else {
-        store_some(to + r * ld + c, v, l - c);
+  if (p.symmetric && tr == tc) return;
+  __syncthreads();
+  if (p.last) {
+    T* to = (T*)a.out + matrix * a.stride_out;
+    if (a.m > a.n) {
+      for (int i = threadIdx.x; i < kTile * kStrip; i += kProductThreads) {
+        const int y = i % kStrip, x = i / kStrip;
+        if (c0 + x < a.m && row(y) < a.n) to[(int64_t)(c0 + x) * a.ld_out + row(y)] = tile[y][x];
+      }
+    } else {
+      for (int i = threadIdx.x; i < kTile * kStrip; i += kProductThreads) {
+        const int y = i / kTile, x = i % kTile;
+        if (row(y) < a.m && c0 + x < a.n) to[(int64_t)row(y) * a.ld_out + c0 + x] = tile[y][x];
       }
     }
+    return;
+  }
+  const Stored<T> to((p.symmetric ? p.to : p.to_t) + matrix * size, p.columns, p.rows);
+  for (int i = threadIdx.x; i < kTile * kStrip / 4; i += kProductThreads) {
+    const int c = i % kTile, k = i / kTile * 4;      // neighbours of a row of the tile side by side
+    const T v[4] = {tile[k][c], tile[k + 1][c], tile[k + 2][c], tile[k + 3][c]};
+    to.write4(c0 + c, row(k), v);
+  }
+}
+
+template <class T, int kTile>
+__global__ void __launch_bounds__(kProductThreads, 2) k_orth_product(OrthArgs a, Product p, int64_t first, T* part) {
+  __shared__ ProductLds<T, kTile> S;
+  const unsigned block = on_one_die(blockIdx.x, gridDim.x);
+  const int t = block % p.tiles, split = block / p.tiles % p.splits;
+  const int64_t matrix = first + block / p.tiles / p.splits;
+  int tr, tc;
+  tile_of<T, kTile>(p, t, tr, tc);
+  const Stored<T> left(p.rows_at + matrix * p.rows * p.terms * Stored<T>::kBytes, p.rows, p.terms), right(p.columns_at + matrix * p.columns * p.terms * Stored<T>::kBytes, p.columns, p.terms);
+  const int steps = p.terms / kStep, from = steps * split / p.splits, end = steps * (split + 1) / p.splits;
+  Copy<T, kTile> rows, columns;
+  Results<T, kTile, kTile> out;
+  rows.fetch(left, tr * kTile, from * kStep);
+  columns.fetch(right, tc * kTile, from * kStep);
+  for (int k = from; k < end; ++k) {
+    __syncthreads();
+    rows.put(S.in.R);
+    columns.put(S.in.C);
+    __syncthreads();
+    if (k + 1 < end) {
+      rows.fetch(left, tr * kTile, (k + 1) * kStep);
+      columns.fetch(right, tc * kTile, (k + 1) * kStep);
+    }
+    out.multiply(S.in.R, S.in.C);
+  }
+  if (p.splits > 1) {
+    out.keep(part + ((matrix * p.tiles + t) * p.splits + split) * (kTile * kTile));
+    return;
+  }
+#pragma unroll
+  for (int rt = 0; rt < out.RT; ++rt) {
+    __syncthreads();
+    finish<T, kTile>(a, p, matrix, tr, tc, rt, out.acc[rt], S.out);
+  }
+}
+
+template <class T, int kTile>
+__global__ void __launch_bounds__(kProductThreads) k_orth_finish(OrthArgs a, Product p, int64_t first, const T* part) {
+  using Out = Results<T, kTile, kTile>;
+  __shared__ T tile[kStrip][kTile + 1];
+  const int rt = blockIdx.x % Out::RT, t = blockIdx.x / Out::RT % p.tiles;
+  const int64_t matrix = first + blockIdx.x / Out::RT / p.tiles;
+  int tr, tc;
+  tile_of<T, kTile>(p, t, tr, tc);
+  typename Out::N::Vec acc[Out::CT] = {};
+  Out::add_up(part + (matrix * p.tiles + t) * p.splits * (kTile * kTile), p.splits, rt, acc);
+  finish<T, kTile>(a, p, matrix, tr, tc, rt, acc, tile);
 }
 
 // ---- up to 128 rows of X --------------------------------------------------------------------------------------------------------
@@ -419,7 +526,8 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_orth_step(OrthArgs a, in
   Cols X;
   X.take(X_at + place * (kS * Cols::kWide));
   typename Cols::Gram A;
-  A.add_up(A_from + matrix * parts * (kS * kS), parts);
+#pragma unroll
+  for (int rt = 0; rt < Cols::Gram::RT; ++rt) Cols::Gram::add_up(A_from + matrix * parts * (kS * kS), parts, rt, A.acc[rt]);
   Cols::put(S, A);
   X.step(S, c0, c1, c2);
   if constexpr (kLast) {
@@ -486,49 +594,72 @@ struct Few {
   size_t sum_size() const { return chunks > kMostShares ? rows * rows : 0; }
 };
 
+// The products of a step where X has many rows
+template <class T>
+struct Many {
+  bool large;                        // tiles of 128 x 128
+  int64_t s, l, square, wide;        // padded sizes, tiles of A (on and above the diagonal) and of X
+  int a_splits, b_splits, x_splits;
+  Many(int64_t batch, int64_t m, int64_t n) {
+    const int64_t s0 = std::min(m, n), l0 = std::max(m, n);
+    large = sizeof(T) == 4 && s0 > 384;
+    const int64_t tile = large ? 128 : 64;
+    s = (s0 + tile - 1) / tile * tile;
+    l = (l0 + tile - 1) / tile * tile;
+    square = s / tile * (s / tile + 1) / 2;
+    wide = s / tile * (l / tile);
+    static const int per = getenv("ORTH_WANT") ? atoi(getenv("ORTH_WANT")) : 512;
+    auto splits = [&](int64_t tiles, int64_t terms) { return (int)std::max<int64_t>(1, std::min(terms / kStep / 4, per / (batch * tiles))); };
+    a_splits = splits(square, l);
+    b_splits = splits(square, s);
+    x_splits = splits(wide, s);
+  }
+  int64_t results() const { return (large ? 128 * 128 : 64 * 64) * std::max({square * (a_splits > 1 ? a_splits : 0), square * (b_splits > 1 ? b_splits : 0), wide * (x_splits > 1 ? x_splits : 0)}); }
+  size_t x_size() const { return s * l * Stored<T>::kBytes; }
+  size_t a_size() const { return s * s * Stored<T>::kBytes; }
+};
+
 template <class T>
 size_t workspace_bytes(int64_t batch, int64_t m, int64_t n) {
-  const int64_t s = std::min(m, n);
-  if (s <= kMostRows) {
+  if (std::min(m, n) <= kMostRows) {
     const Few f(m, n, sizeof(T) == 8);
     if (f.chunks == 1) return 0;
     return up(batch * shares_of(m, n) * sizeof(double)) + up(batch * f.x_size() * sizeof(T)) + 2 * up(batch * f.a_size() * sizeof(T)) + up(batch * f.sum_size() * sizeof(T));
   }
-  return up(batch * shares_of(m, n) * sizeof(double)) + 2 * up(batch * m * n * sizeof(T)) + 2 * up(batch * s * s * sizeof(T));
+  const Many<T> f(batch, m, n);
+  return up(batch * shares_of(m, n) * sizeof(double)) + 4 * up(batch * f.x_size()) + 2 * up(batch * f.a_size()) + up(batch * f.results() * sizeof(T));
 }
 
-template <class T, bool kWhole>
-hipError_t steps_of(const OrthArgs& a, const double* coefficients, int steps, char* ws, hipStream_t st) {
-  const int64_t s = std::min(a.m, a.n), l = std::max(a.m, a.n);
-  const int shares = shares_of(a.m, a.n);
+template <class T, int kTile>
+hipError_t product(const OrthArgs& a, const Product& p, T* part, hipStream_t st) {
+  hipError_t e = in_launches(a.batch, (int64_t)p.tiles * p.splits, [&](int64_t first, dim3 grid) { k_orth_product<T, kTile><<<grid, kProductThreads, 0, st>>>(a, p, first, part); });
+  if (e != hipSuccess || p.splits == 1) return e;
+  return in_launches(a.batch, (int64_t)p.tiles * (kTile / 32), [&](int64_t first, dim3 grid) { k_orth_finish<T, kTile><<<grid, kProductThreads, 0, st>>>(a, p, first, part); });
+}
+
+template <class T, int kTile>
+hipError_t many_rows(const OrthArgs& a, const double* coefficients, int steps, char* ws, hipStream_t st) {
+  const Many<T> f(a.batch, a.m, a.n);
+  const int shares = shares_of(a.m, a.n), s = (int)f.s, l = (int)f.l;
   double* part = (double*)ws;
-  T* X = (T*)(ws + up(a.batch * shares * sizeof(double)));
-  T* other = (T*)((char*)X + up(a.batch * a.m * a.n * sizeof(T)));
-  T* A = (T*)((char*)other + up(a.batch * a.m * a.n * sizeof(T)));
-  T* B = (T*)((char*)A + up(a.batch * s * s * sizeof(T)));
+  auto next = [&, at = ws + up(a.batch * shares * sizeof(double))](size_t bytes) mutable {
+    char* p = at;
+    at += up(a.batch * bytes);
+    return p;
+  };
+  char *X = next(f.x_size()), *XT = next(f.x_size()), *other = next(f.x_size()), *other_t = next(f.x_size()), *A = next(f.a_size()), *B = next(f.a_size());
+  T* sums = (T*)next(f.results() * sizeof(T));
   hipError_t e = in_launches(a.batch, shares, [&](int64_t first, dim3 grid) { k_orth_squares<T><<<grid, kProductThreads, 0, st>>>(a, first, shares, part); });
   if (e != hipSuccess) return e;
-  const int64_t squares = ((a.m + 63) / 64) * ((a.n + 63) / 64);
-  e = in_launches(a.batch, squares, [&](int64_t first, dim3 grid) { k_orth_start<T><<<grid, kProductThreads, 0, st>>>(a, first, squares, shares, part, X); });
-  constexpr int kR = 64, kC = 64;
-  const int64_t side = (s + kR - 1) / kR, upper = side * (side + 1) / 2, all = side * ((l + kC - 1) / kC);
+  const int64_t blocks = f.s / kBlock * (f.l / kBlock);
+  e = in_launches(a.batch, blocks, [&](int64_t first, dim3 grid) { k_orth_start<T><<<grid, kProductThreads, 0, st>>>(a, first, (int)blocks, s, l, shares, part, X, XT); });
   for (int i = 0; i < steps && e == hipSuccess; ++i) {
     const double* c = coefficients + 3 * i;
-    e = in_launches(a.batch, upper, [&](int64_t first, dim3 grid) {
-      k_orth_square<T, kR, kWhole><<<grid, kProductThreads, 0, st>>>(first, (int)upper, (int)s, (int)l, X, T(1), T(0), A);
-    });
-    if (e != hipSuccess) break;
-    e = in_launches(a.batch, upper, [&](int64_t first, dim3 grid) {
-      k_orth_square<T, kR, kWhole><<<grid, kProductThreads, 0, st>>>(first, (int)upper, (int)s, (int)s, A, (T)c[2], (T)c[1], B);
-    });
-    if (e != hipSuccess) break;
-    e = in_launches(a.batch, all, [&](int64_t first, dim3 grid) {
-      if (i + 1 < steps)
-        k_orth_apply<T, kR, kC, kWhole, false><<<grid, kProductThreads, 0, st>>>(first, (int)all, (int)s, (int)l, X, B, (T)c[0], other, l, s * l, false);
-      else
-        k_orth_apply<T, kR, kC, kWhole, true><<<grid, kProductThreads, 0, st>>>(first, (int)all, (int)s, (int)l, X, B, (T)c[0], (T*)a.out, a.ld_out, a.stride_out, a.m > a.n);
-    });
+    e = product<T, kTile>(a, {X, X, nullptr, A, nullptr, s, s, l, (int)f.square, f.a_splits, 0, 1, true, false}, sums, st);
+    if (e == hipSuccess) e = product<T, kTile>(a, {A, A, A, B, nullptr, s, s, s, (int)f.square, f.b_splits, c[1], c[2], true, false}, sums, st);
+    if (e == hipSuccess) e = product<T, kTile>(a, {B, XT, X, other, other_t, s, l, s, (int)f.wide, f.x_splits, c[0], 1, false, i + 1 == steps}, sums, st);
     std::swap(X, other);
+    std::swap(XT, other_t);
   }
   return e;
 }
@@ -587,7 +718,9 @@ hipError_t orthogonalise(const OrthArgs& a, const double* coefficients, int step
       default: return go(std::integral_constant<int, 128>());
     }
   }
-  return a.m % 4 == 0 && a.n % 4 == 0 ? steps_of<T, true>(a, coefficients, steps, ws, st) : steps_of<T, false>(a, coefficients, steps, ws, st);
+  if constexpr (sizeof(T) == 4)
+    if (Many<T>(a.batch, a.m, a.n).large) return many_rows<T, 128>(a, coefficients, steps, ws, st);
+  return many_rows<T, 64>(a, coefficients, steps, ws, st);
 }
 
 }  // namespace

@@ -14,6 +14,12 @@ namespace {
 constexpr int kProductThreads = 256;
 constexpr int kStep = 32;      // terms in LDS at a time
 
+// Neighbouring workgroups go to the eight dies in turn: the numbers that make neighbours in work run on one, whose L2 they share.
+__device__ inline unsigned on_one_die(unsigned block, unsigned blocks) {
+  const unsigned die = block % 8, each = blocks / 8, more = blocks % 8;
+  return die * each + (die < more ? die : more) + block / 8;
+}
+
 // which of 16 columns lane l16 of a left operand holds, for results 4 q + i to be neighbours: a lane's results are rows Num::row(q, i) of the instruction
 template <class T>
 __device__ inline int column_place(int l16) {
@@ -50,9 +56,9 @@ __device__ inline void load_some(const T* row, int k, int width, T* v) {
 // kR rows (columns) of 32 terms in LDS.  A wave reads 16 bytes of each of 16 rows, and writes 8 bytes of rows that are one, two or four apart: the rows are 80
 // bytes apart and their 16 bytes change places with the row's number / 16, in which all of these find different banks (256 bytes in all).
 template <class T, int kR>
-struct Operand;
+struct alignas(16) Operand;
 template <int kR>
-struct Operand<float, kR> {
+struct alignas(16) Operand<float, kR> {
   __bf16 v[3][kR][kStep + 8];
   static __device__ int at(int r, int k) { return k ^ (r >> 4 & 3) * 8; }
   __device__ PartsOf<3> read(int r, int k) const {
@@ -82,7 +88,7 @@ struct Operand<float, kR> {
   }
 };
 template <int kR>
-struct Operand<double, kR> {
+struct alignas(16) Operand<double, kR> {
   double v[kR][kStep + 2];
   __device__ PartsOf<4> read(int r, int k) const {
     PartsOf<4> p;
@@ -157,14 +163,13 @@ struct Results {
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) *(typename N::Vec*)(to + ((rt * CT + ct) * kProductThreads + (int)threadIdx.x) * 4) = acc[rt][ct];
   }
-  // the sum of `parts` such, in their order
-  __device__ void add_up(const T* from, int parts) {
-#pragma unroll 2
-    for (int p = 0; p < parts; ++p, from += kR * kC)
+  // the sum of tiles rt of `parts` such, in their order
+  static __device__ void add_up(const T* from, int parts, int rt, typename N::Vec (&to)[CT]) {
+    from += (rt * CT * kProductThreads + (int)threadIdx.x) * 4;
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p)
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) acc[rt][ct] += *(const typename N::Vec*)(from + ((rt * CT + ct) * kProductThreads + (int)threadIdx.x) * 4);
+      for (int ct = 0; ct < CT; ++ct) to[ct] += *(const typename N::Vec*)(from + (int64_t)p * (kR * kC) + ct * kProductThreads * 4);
   }
   __device__ void multiply(const Operand<T, kR>& R, const Operand<T, kC>& C) {
     const int l16 = lane() % 16, k = lane() / 16 * 8, r0 = wave() / 2 * (kR / 2), c0 = wave() % 2 * (kC / 2) + column_place<T>(l16);
