@@ -61,6 +61,40 @@ struct Lines {
   }
 };
 
+// ---- lines through buffer descriptors -------------------------------------------------------------------------------------------
+
+// four numbers from column k on of the line at offset `at`, zero behind its end.  kWhole: its width is a multiple of four.
+template <bool kWhole, class T>
+__device__ inline void load_at(Buffer B, unsigned at, int k, int width, T* v) {
+  constexpr int e = sizeof(T);
+  const unsigned off = plus(at, k < width ? (unsigned)k * e : kNowhere);
+  if constexpr (e == 4) {
+    const f32x4 w = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(B, off, 0, 0));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = w[i];
+  } else {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const f64x2 w = __builtin_bit_cast(f64x2, __builtin_amdgcn_raw_buffer_load_b128(B, plus(off, h * 16), 0, 0));
+      v[2 * h] = w[0];
+      v[2 * h + 1] = w[1];
+    }
+  }
+  if constexpr (!kWhole)
+#pragma unroll
+    for (int i = 1; i < 4; ++i) v[i] = k + i < width ? v[i] : T(0);
+}
+
+template <int kHow, class T>
+__device__ inline void store_at(const T (&v)[1], Buffer B, unsigned at) {
+  if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(unsigned, v[0]), B, at, 0, kHow);
+  else __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v[0]), B, at, 0, kHow);
+}
+template <int kHow>
+__device__ inline void store_at(const float (&v)[2], Buffer B, unsigned at) {
+  __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, f32x2{v[0], v[1]}), B, at, 0, kHow);
+}
+
 // the row of a position, -1: none
 __device__ inline int64_t row_of(const GroupedArgs& a, int64_t p) {
   const int64_t r = a.perm ? a.perm[p] : p;
@@ -69,46 +103,48 @@ __device__ inline int64_t row_of(const GroupedArgs& a, int64_t p) {
 
 // ---- rows times a matrix of at most 128 rows --------------------------------------------------------------------------------------
 
-constexpr int kMostTerms = 128;
-template <class T>
-constexpr int kMostShift = sizeof(T) == 4 ? 10 : 9;      // lines of a workgroup: their places in LDS leave room for two workgroups
+constexpr int kMostTerms = 128, kMostShift = 10;      // lines of a workgroup
 
 // A wave keeps the parts of its 16 NT columns of the matrix in registers, for up to 2^kMostShift lines of one group, whose parts the workgroup puts into LDS once for its four
 // waves, 64 at a time.  Lane: columns NT l16 + j.  out = x W + b, or gx = gout W^T (kBack).
+// Lines are reached through buffer descriptors of less than 2^31 bytes: what is not wanted has the offset kNowhere, which is behind them, reads zero and is not
+// written.
 template <class T, int kIn, int NT, bool kWhole, bool kBack>
 __global__ void __launch_bounds__(kProductThreads, 2) k_grouped_stream(GroupedArgs a, int64_t first_id, int column_tiles, int shift) {
   using N = Num<T>;
-  using Rows = AlongTerms<T, 64, kWhole>;
-  constexpr int kSlices = kIn / 32;
+  constexpr int kSlices = kIn / 32, kPer = 2, e = sizeof(T);
   __shared__ Operand<T, 64> X[kSlices];
-  __shared__ int64_t from[1 << kMostShift<T>], place[1 << kMostShift<T>];      // of the lines in memory and in the results (-1: none)
-  const int64_t id = first_id + blockIdx.x / column_tiles, g = find_group(a, a.comps, shift, id), piece = first_piece(a, g, a.comps, shift);
+  __shared__ unsigned from[1 << kMostShift], place[1 << kMostShift];      // of the lines in memory and in the results, bytes
+  const unsigned block = on_one_die(blockIdx.x, gridDim.x);      // which read the same lines
+  const int64_t id = first_id + block / column_tiles, g = find_group(a, a.comps, shift, id), piece = first_piece(a, g, a.comps, shift);
   const int64_t lines_end = cut(a, g + 1) * a.comps, begin = cut(a, g) * a.comps + ((id - piece) << shift);
   if (id < piece || begin >= lines_end) return;
   const int have = (int)(lines_end - begin < 1 << shift ? lines_end - begin : 1 << shift);
   const int K = (int)(kBack ? a.d_out : a.d_in), n = (int)(kBack ? a.d_in : a.d_out);
-  const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4, c = (int)(blockIdx.x % column_tiles) * (64 * NT) + (threadIdx.x >> 6) * (16 * NT) + l16 * NT;
-  const T *x = (const T*)(kBack ? a.gout : a.x), *W = (const T*)a.W + g * a.d_in * a.d_out;
-  T* to = (T*)(kBack ? a.gx : a.out);
-  {
-    const int64_t ld = kBack ? a.ld_gout : a.ld_x, ld_to = kBack ? a.ld_gx : a.ld_out;
-    const Lines lines(begin, a.comps);
-    for (int i = threadIdx.x; i < (have + 63) / 64 * 64; i += kProductThreads) {
-      unsigned at, m;
-      lines.of(i < have ? i : 0, at, m);
-      const int64_t r = row_of(a, lines.position + at);
-      from[i] = (r < 0 ? 0 : r) * ld + m * (int64_t)K;
-      place[i] = r < 0 || i >= have ? -1 : r * ld_to + m * (int64_t)n;
-    }
+  const int lane = threadIdx.x & 63, l16 = lane & 15, q = lane >> 4, c = (int)(block % column_tiles) * (64 * NT) + (threadIdx.x >> 6) * (16 * NT) + l16 * NT;
+  const T* W = (const T*)a.W + g * a.d_in * a.d_out;
+  const Lines lines(begin, a.comps);
+  const int64_t ld = kBack ? a.ld_gout : a.ld_x, ld_to = kBack ? a.ld_gx : a.ld_out, row0 = a.perm ? 0 : lines.position;
+  const int64_t span = a.perm ? a.rows : (have + lines.component + a.comps - 1) / a.comps;      // rows that lines may be in
+  const Buffer x = buffer_of((const T*)(kBack ? a.gout : a.x) + row0 * ld, ((span - 1) * ld + a.comps * K) * e);
+  const Buffer to = buffer_of((T*)(kBack ? a.gx : a.out) + row0 * ld_to, ((span - 1) * ld_to + a.comps * n) * e);
+  for (int i = threadIdx.x; i < (have + 63) / 64 * 64; i += kProductThreads) {
+    unsigned at, m;
+    lines.of(i < have ? i : 0, at, m);
+    const int64_t r = row_of(a, lines.position + at) - row0;
+    const bool ok = i < have && r >= 0;
+    from[i] = ok ? (unsigned)((r * ld + m * (int64_t)K) * e) : kNowhere;
+    place[i] = ok ? (unsigned)((r * ld_to + m * (int64_t)n) * e) : kNowhere;
   }
   __syncthreads();
-  T next[kSlices][Rows::kPer][4];
+  T next[kSlices][kPer][4];
+  const int row = threadIdx.x / 8, term = threadIdx.x % 8 * 4;      // a thread copies four terms of lines row + 32 i
   auto fetch = [&](int line) {
 #pragma unroll
-    for (int i = 0; i < Rows::kPer; ++i) {
-      const T* p = x + from[line + Rows::row(i)];
+    for (int i = 0; i < kPer; ++i) {
+      const unsigned at = from[line + row + i * 32];
 #pragma unroll
-      for (int s = 0; s < kSlices; ++s) load_some<T, 4, kWhole>(p, s * 32 + Rows::term(), K, next[s][i]);
+      for (int s = 0; s < kSlices; ++s) load_at<kWhole>(x, at, s * 32 + term, K, next[s][i]);
     }
   };
   fetch(0);
@@ -140,39 +176,50 @@ __global__ void __launch_bounds__(kProductThreads, 2) k_grouped_stream(GroupedAr
   }
 #pragma unroll
   for (int j = 0; j < NT; ++j) bias[j] = !kBack && a.b ? ((const T*)a.b)[g * n + (c + j < n ? c + j : 0)] : T(0);
+  // a lane's columns: of all, or of the first alone where the row ends behind it
+  const unsigned at_all = c + NT <= n ? (unsigned)c * e : kNowhere, at_last = c + 1 == n ? (unsigned)c * e : kNowhere;
+  typename N::Vec o[2][NT];
+  auto products = [&](int rt, typename N::Vec* to) {
+#pragma unroll
+    for (int j = 0; j < NT; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) to[j][i] = bias[j];
+#pragma unroll
+    for (int s = 0; s < kSlices; ++s) {
+      const typename N::Parts xa = X[s].read(rt * 16 + l16, q * 8);
+      if constexpr (NT == 2) N::template mma<2>({&xa, &xa}, {&w[s][0], &w[s][1]}, {&to[0], &to[1]});
+      else N::template mma<1>({&xa}, {&w[s][0]}, {&to[0]});
+    }
+  };
+  auto finish = [&](int line, const typename N::Vec* v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const unsigned at = place[line + N::row(q, i)];
+      T u[NT];
+#pragma unroll
+      for (int j = 0; j < NT; ++j) u[j] = v[j][i];
+      store_at<0>(u, to, plus(at, at_all));
+      if constexpr (NT == 2 && !kWhole) store_at<0>({u[0]}, to, plus(at, at_last));
+    }
+  };
   for (int line = 0; line < have; line += 64) {
     __syncthreads();
 #pragma unroll
     for (int s = 0; s < kSlices; ++s)
 #pragma unroll
-      for (int i = 0; i < Rows::kPer; ++i) X[s].write4(Rows::row(i), Rows::term(), next[s][i]);
+      for (int i = 0; i < kPer; ++i) X[s].write4(row + i * 32, term, next[s][i]);
     __syncthreads();
     if (line + 64 < have) fetch(line + 64);
+    if (line + 16 < have) {      // the results of a tile are on their way while the products of the next one run
 #pragma unroll
-    for (int rt = 0; rt < 4; ++rt) {
-      if (line + rt * 16 >= have) break;
-      typename N::Vec o[NT];
-#pragma unroll
-      for (int j = 0; j < NT; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) o[j][i] = bias[j];
-#pragma unroll
-      for (int s = 0; s < kSlices; ++s) {
-        const typename N::Parts xa = X[s].read(rt * 16 + l16, q * 8);
-        if constexpr (NT == 2) N::template mma<2>({&xa, &xa}, {&w[s][0], &w[s][1]}, {&o[0], &o[1]});
-        else N::template mma<1>({&xa}, {&w[s][0]}, {&o[0]});
+      for (int rt = 0; rt < 4; ++rt) {
+        products(rt, o[rt & 1]);
+        if (rt > 0) finish(line + rt * 16 - 16, o[~rt & 1]);
       }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int64_t at = place[line + rt * 16 + N::row(q, i)];
-        if constexpr (NT == 2) {
-          typedef T Two __attribute__((ext_vector_type(2), aligned(sizeof(T))));
-          if (at >= 0 && c + 1 < n) *(Two*)(to + at + c) = Two{o[0][i], o[1][i]};
-          else if (at >= 0 && c < n) to[at + c] = o[0][i];
-        } else {
-          if (at >= 0 && c < n) to[at + c] = o[0][i];
-        }
-      }
+      finish(line + 48, o[1]);
+    } else {
+      products(0, o[0]);
+      finish(line, o[0]);
     }
   }
 }
@@ -187,11 +234,12 @@ __global__ void __launch_bounds__(kProductThreads, 2) k_grouped_rows(GroupedArgs
   __shared__ Operand<T, kC> C;
   __shared__ int64_t place[kR];      // of the lines in the results, -1: none
   constexpr int kShift = kR == 128 ? 7 : 6;
-  const int64_t id = first_id + blockIdx.x / column_tiles, g = find_group(a, a.comps, kShift, id);
+  const unsigned block = on_one_die(blockIdx.x, gridDim.x);
+  const int64_t id = first_id + block / column_tiles, g = find_group(a, a.comps, kShift, id);
   const int64_t lines_end = cut(a, g + 1) * a.comps, begin = cut(a, g) * a.comps + ((id - first_piece(a, g, a.comps, kShift)) << kShift);
   if (id < first_piece(a, g, a.comps, kShift) || begin >= lines_end) return;
   const int have = (int)(lines_end - begin < kR ? lines_end - begin : kR);
-  const int K = (int)(kBack ? a.d_out : a.d_in), n = (int)(kBack ? a.d_in : a.d_out), c0 = (int)(blockIdx.x % column_tiles) * kC;
+  const int K = (int)(kBack ? a.d_out : a.d_in), n = (int)(kBack ? a.d_in : a.d_out), c0 = (int)(block % column_tiles) * kC;
   const T *x = (const T*)(kBack ? a.gout : a.x), *W = (const T*)a.W + g * a.d_in * a.d_out;
   const int64_t ld = kBack ? a.ld_gout : a.ld_x, ld_to = kBack ? a.ld_gx : a.ld_out;
   const Lines lines(begin, a.comps);
@@ -206,7 +254,7 @@ __global__ void __launch_bounds__(kProductThreads, 2) k_grouped_rows(GroupedArgs
     if (threadIdx.x % 8 == 0) place[line] = r < 0 || line >= have ? -1 : r * ld_to + m * (int64_t)n;
   }
   Rows rows;
-  AcrossTerms<T, kC, kWhole> across;
+  AcrossTerms<T, kC, kWhole> across(c0, n);
   AlongTerms<T, kC, kWhole> along;
   const T* pw[kC / 32];
   if constexpr (kBack)
@@ -220,15 +268,15 @@ __global__ void __launch_bounds__(kProductThreads, 2) k_grouped_rows(GroupedArgs
     if constexpr (kBack) {
       along.fetch(pw, k0, K);
     } else {
-      const T* q[4];
-      bool ok[4];
+      const T* q[8];
+      bool ok[8];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < 8; ++j) {
         const int k = k0 + across.term() + j;
         ok[j] = k < K;
         q[j] = W + (int64_t)(ok[j] ? k : 0) * n;
       }
-      across.fetch(q, ok, c0, n);
+      across.fetch(q, ok);
     }
   };
   Results<T, kR, kC> out;
@@ -264,58 +312,111 @@ __global__ void __launch_bounds__(kProductThreads, 2) k_grouped_rows(GroupedArgs
 
 // ---- the matrices' gradients ----------------------------------------------------------------------------------------------------
 
-constexpr int kTable = 1024;      // positions whose rows stand in LDS at a time
-
 // kR x kC numbers of gW[g] (and kC of gb[g]) over the positions of group g in one chunk: chunks are the same for all groups, so that those of a group that has several
 // leave their sums at slot 2 chunk + (0: the group began before the chunk, 1: in it).  A group with one chunk, or without rows, is
 // written at once.
-template <class T, int kR, int kC, bool kWhole>
+constexpr int kTable = 512;      // lines whose offsets stand in LDS at a time
+
+// kFar: rows of x or gout lie 2^31 bytes apart or more, addresses are formed for each.
+template <class T, int kR, int kC, bool kWhole, bool kFar>
 __global__ void __launch_bounds__(kProductThreads, 2) k_grouped_weights(GroupedArgs a, int64_t first_id, int shift, int row_tiles, int column_tiles, T* part, T* part_b) {
   __shared__ Operand<T, kR> R;
   __shared__ Operand<T, kC> C;
-  __shared__ int64_t row[kTable];
-  const int tiles = row_tiles * column_tiles, tile = blockIdx.x % tiles;
-  const int64_t id = first_id + blockIdx.x / tiles, g = find_group(a, 1, shift, id), chunk = id - g;
+  __shared__ alignas(16) unsigned table[kFar ? 1 : kTable][2];
+  const unsigned block = on_one_die(blockIdx.x, gridDim.x);      // which read the same rows
+  const int tiles = row_tiles * column_tiles, tile = block % tiles;
+  const int64_t id = first_id + block / tiles, g = find_group(a, 1, shift, id), chunk = id - g;
   const int64_t from = cut(a, g), end = cut(a, g + 1), lo = std::max(from, chunk << shift), hi = std::min(end, (chunk + 1) << shift);
   const bool empty = end <= from && chunk == from >> shift;
   if (chunk < from >> shift || (hi <= lo && !empty)) return;
-  const int K = (int)a.d_in, n = (int)a.d_out, k0 = tile / column_tiles * kR, c0 = tile % column_tiles * kC;
-  AcrossTerms<T, kR, kWhole> x;
-  AcrossTerms<T, kC, kWhole> t;
-  const Lines lines(0, a.comps);
+  const int K = (int)a.d_in, n = (int)a.d_out, comps = (int)a.comps, k0 = tile / column_tiles * kR, c0 = tile % column_tiles * kC;
+  AcrossTerms<T, kR, kWhole> x(k0, K);
+  AcrossTerms<T, kC, kWhole> t(c0, n);
   Results<T, kR, kC> out;
-  T sum[kC / 32] = {};
-  for (int64_t p0 = lo; p0 < hi; p0 += kTable) {
-    const int positions = (int)(hi - p0 < kTable ? hi - p0 : kTable), count = positions * (int)a.comps;
-    __syncthreads();
-    for (int i = threadIdx.x; i < positions; i += kProductThreads) row[i] = row_of(a, p0 + i);
-    __syncthreads();
-    auto fetch = [&](int line0) {
-      const T *px[4], *pt[4];
-      bool ok[4];
+  T sum[kC / 64] = {};
+  // the position and component of the wave's first term; all of it is the wave's own
+  unsigned position = (unsigned)lo + x.term() / comps;      // below 2^31 but for steps behind the end
+  int component = x.term() % comps;
+  const unsigned last = (unsigned)hi, rows = (unsigned)a.rows;
+  const int skip = kStep / comps, rest = kStep % comps;
+  auto fetch = [&]() {
+    const T *px[8], *pt[8];
+    bool ok[8];
+    unsigned p = position;
+    int m = component;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int line = line0 + x.term() + j;
-        unsigned at, m;
-        lines.of(line < count ? line : 0, at, m);
-        const int64_t r = row[at];
-        ok[j] = line < count && r >= 0;
-        px[j] = (const T*)a.x + (r < 0 ? 0 : r) * a.ld_x + m * (int64_t)K;
-        pt[j] = (const T*)a.gout + (r < 0 ? 0 : r) * a.ld_gout + m * (int64_t)n;
+    for (int j = 0; j < 8; ++j) {
+      const unsigned at = p < last ? p : (unsigned)lo;
+      unsigned r = at, beyond = 0;
+      if (a.perm) {
+        const u32x2 w = *(const u32x2*)(a.perm + at);
+        r = w[0];
+        beyond = w[1];
       }
-      x.fetch(px, ok, k0, K);
-      t.fetch(pt, ok, c0, n);
-    };
-    fetch(0);
-    for (int l = 0; l < count; l += kStep) {
-      __syncthreads();
-      x.put(R);
-      t.put(C);
-      __syncthreads();
+      ok[j] = p < last && beyond == 0 && r < rows;
+      const unsigned row = ok[j] ? r : 0, part_of = ok[j] ? (unsigned)m : 0;      // strides and rows are below 2^31
+      px[j] = (const T*)a.x + ((uint64_t)row * (unsigned)a.ld_x + part_of * (unsigned)K);
+      pt[j] = (const T*)a.gout + ((uint64_t)row * (unsigned)a.ld_gout + part_of * (unsigned)n);
+      const bool next = ++m == comps;
+      p += next ? 1 : 0;
+      m = next ? 0 : m;
+    }
+    x.fetch(px, ok);
+    t.fetch(pt, ok);
+    component += rest;
+    const bool next = component >= comps;
+    position += skip + (next ? 1 : 0);
+    component -= next ? comps : 0;
+  };
+  const int64_t count = hi > lo ? (hi - lo) * comps : 0;
+  auto multiply = [&](bool more, auto fetch_next) {
+    __syncthreads();
+    x.put(R);
+    t.put(C);
+    __syncthreads();
+    if (a.gb)
 #pragma unroll
-      for (int i = 0; i < kC / 32; ++i) sum[i] += (t.v[0][i] + t.v[1][i]) + (t.v[2][i] + t.v[3][i]);
-      if (l + kStep < count) fetch(l + kStep);
-      out.multiply(R, C);
+      for (int i = 0; i < kC / 64; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum[i] += t.v[j][i];
+    if (more) fetch_next();
+    out.multiply(R, C);
+  };
+  if constexpr (kFar) {
+    if (count > 0) fetch();
+    for (int64_t l = 0; l < count; l += kStep) multiply(l + kStep < count, fetch);
+  } else {
+    const int64_t row0 = a.perm ? 0 : lo, span = a.perm ? a.rows : hi - lo;
+    const Buffer bx = buffer_of((const T*)a.x + row0 * a.ld_x, ((span - 1) * a.ld_x + comps * (int64_t)K) * (int)sizeof(T));
+    const Buffer bt = buffer_of((const T*)a.gout + row0 * a.ld_gout, ((span - 1) * a.ld_gout + comps * (int64_t)n) * (int)sizeof(T));
+    for (int64_t l0 = 0; l0 < count; l0 += kTable) {
+      const int lines = (int)(count - l0 < kTable ? count - l0 : kTable);
+      const Lines of(lo * comps + l0, comps);
+      __syncthreads();
+      for (int i = threadIdx.x; i < (lines + kStep - 1) / kStep * kStep; i += kProductThreads) {
+        unsigned at, m;
+        of.of(i < lines ? i : 0, at, m);
+        const int64_t r = row_of(a, of.position + at) - row0;
+        const bool ok = i < lines && r >= 0;
+        table[i][0] = ok ? (unsigned)((r * a.ld_x + m * (int64_t)K) * (int)sizeof(T)) : kNowhere;
+        table[i][1] = ok ? (unsigned)((r * a.ld_gout + m * (int64_t)n) * (int)sizeof(T)) : kNowhere;
+      }
+      __syncthreads();
+      auto fetch_at = [&](int l) {
+        unsigned rx[8], rt[8];
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+          const u32x4 w = *(const u32x4*)&table[l + x.term() + j][0];
+          rx[j] = w[0];
+          rt[j] = w[1];
+          rx[j + 1] = w[2];
+          rt[j + 1] = w[3];
+        }
+        x.fetch(bx, rx);
+        t.fetch(bt, rt);
+      };
+      fetch_at(0);
+      for (int l = 0; l < lines; l += kStep) multiply(l + kStep < lines, [&]() { fetch_at(l + kStep); });
     }
   }
   const bool whole = from >> shift == (end - 1) >> shift || empty;
@@ -332,52 +433,61 @@ __global__ void __launch_bounds__(kProductThreads, 2) k_grouped_weights(GroupedA
       if (k < K && c < n) store_some(to + (int64_t)k * n + c, v, n - c);
     }
   if (!a.gb || k0 > 0) return;
-  // the eight threads of a column, one after another
+  // the waves' terms, one after another
   __syncthreads();
-  T* sums = (T*)&C;      // [8][kC]
+  T* sums = (T*)&C;      // [4][kC]
 #pragma unroll
-  for (int i = 0; i < kC / 32; ++i) sums[x.term() / 4 * kC + t.place() + i] = sum[i];
+  for (int i = 0; i < kC / 64; ++i) sums[x.term() / 8 * kC + t.place() + i] = sum[i];
   __syncthreads();
   T* to_b = whole ? (T*)a.gb + g * a.d_out : part_b + slot * a.d_out;
   for (int c = threadIdx.x; c < kC && c0 + c < n; c += kProductThreads) {
     T v = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v += sums[j * kC + c];
+    for (int j = 0; j < 4; ++j) v += sums[j * kC + c];
     to_b[c0 + c] = v;
   }
 }
 
-// Adds up, in their order, the chunks of the group that begins in chunk blockIdx.x / blocks and goes on behind it, if there is one.
-template <class T>
-__global__ void __launch_bounds__(kProductThreads) k_grouped_sums(GroupedArgs a, int64_t first_chunk, int shift, int blocks, const T* part, const T* part_b) {
-  const int64_t chunk = first_chunk + blockIdx.x / blocks, next = (chunk + 1) << shift;
-  if (next >= a.rows) return;
-  // the last group that begins before the next chunk
-  int64_t lo = 0, n = a.groups;
-  while (n > 1) {
-    const int64_t step = (n + 63) / 64, g = lo + (threadIdx.x & 63) * step;
-    const bool in = g < lo + n;
-    const int found = __popcll(__ballot(in && cut(a, in ? g : lo) < next));
-    const int64_t skip = found > 0 ? (found - 1) * step : 0;
-    lo += skip;
-    n = n - skip < step ? n - skip : step;
+// Adds up, in their order, the chunks of the groups that have several: of group `at` (of_groups), or of the one that begins in chunk `at` and goes on behind it, whichever are
+// fewer.  V numbers a thread.
+template <class T, int V>
+__global__ void __launch_bounds__(kProductThreads) k_grouped_sums(GroupedArgs a, int64_t first, int shift, int blocks, bool of_groups, const T* part, const T* part_b) {
+  typedef T Words __attribute__((ext_vector_type(V)));
+  const int64_t at = first + blockIdx.x / blocks;
+  int64_t lo = at;
+  if (!of_groups) {
+    const int64_t next = (at + 1) << shift;
+    if (next >= a.rows) return;
+    // the last group that begins before the next chunk
+    lo = 0;
+    int64_t n = a.groups;
+    while (n > 1) {
+      const int64_t step = (n + 63) / 64, g = lo + (threadIdx.x & 63) * step;
+      const bool in = g < lo + n;
+      const int found = __popcll(__ballot(in && cut(a, in ? g : lo) < next));
+      const int64_t skip = found > 0 ? (found - 1) * step : 0;
+      lo += skip;
+      n = n - skip < step ? n - skip : step;
+    }
   }
-  const int64_t from = cut(a, lo), end = cut(a, lo + 1);
-  if (from < chunk << shift || from >= next || end <= next) return;
-  const int64_t last = (end - 1) >> shift, size = a.d_in * a.d_out, all = size + (a.gb ? a.d_out : 0);
-  for (int64_t i = (int64_t)(blockIdx.x % blocks) * kProductThreads + threadIdx.x; i < all; i += (int64_t)blocks * kProductThreads) {
+  const int64_t from = cut(a, lo), end = cut(a, lo + 1), chunk = from >> shift, last = (end - 1) >> shift;
+  if (end <= from || last <= chunk || (!of_groups && chunk != at)) return;
+  const int64_t size = a.d_in * a.d_out, all = (size + (a.gb ? a.d_out : 0)) / V;
+  for (int64_t w = (int64_t)(blockIdx.x % blocks) * kProductThreads + threadIdx.x; w < all; w += (int64_t)blocks * kProductThreads) {
+    const int64_t i = w * V;
     const bool b = i >= size;
     const T* p = b ? part_b + (i - size) : part + i;
     const int64_t of = b ? a.d_out : size;
-    T v[8] = {p[(2 * chunk + 1) * of]};
+    Words v[8] = {*(const Words*)(p + (2 * chunk + 1) * of)};
     int64_t c = chunk + 1;
     for (; c + 8 <= last + 1; c += 8)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] += p[2 * (c + j) * of];
-    for (; c <= last; ++c) v[0] += p[2 * c * of];
-    const T total = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
-    if (b) ((T*)a.gb)[lo * a.d_out + (i - size)] = total;
-    else ((T*)a.gW)[lo * size + i] = total;
+      for (int j = 0; j < 8; ++j) v[j] += *(const Words*)(p + 2 * (c + j) * of);
+    for (; c <= last; ++c) v[0] += *(const Words*)(p + 2 * c * of);
+    const Words total = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+    T* to = b ? (T*)a.gb + lo * a.d_out + (i - size) : (T*)a.gW + lo * size + i;
+#pragma unroll
+    for (int j = 0; j < V; ++j) to[j] = total[j];
   }
 }
 
@@ -406,7 +516,7 @@ template <class T, int kIn, int NT, bool kBack>
 hipError_t launch_stream(const GroupedArgs& a, hipStream_t st) {
   const int64_t n = kBack ? a.d_in : a.d_out, tiles = (n + 64 * NT - 1) / (64 * NT), lines = a.rows * a.comps;
   const bool whole = a.d_in % 4 == 0 && a.d_out % 4 == 0;
-  int shift = kMostShift<T>;      // lines of a workgroup: fewer where that leaves compute units without work
+  int shift = kMostShift;      // lines of a workgroup: fewer where that leaves compute units without work
   while (shift > 6 && (lines >> shift) * tiles < 1024) --shift;
   return in_launches((lines >> shift) + a.groups, tiles, [&](int64_t first, dim3 grid) {
     if (whole) k_grouped_stream<T, kIn, NT, true, kBack><<<grid, kProductThreads, 0, st>>>(a, first, (int)tiles, shift);
@@ -429,9 +539,13 @@ hipError_t launch_few_terms(const GroupedArgs& a, hipStream_t st) {
   return go(std::integral_constant<int, 128>());
 }
 
+// bytes from the first of `rows` rows to the end of the last; descriptors hold less than 2^31
+bool in_reach(int64_t rows, int64_t ld, size_t element) { return rows * ld < (int64_t)(((size_t)1 << 31) / element); }
+
 template <class T, bool kBack>
 hipError_t launch_rows(const GroupedArgs& a, hipStream_t st) {
-  if ((kBack ? a.d_out : a.d_in) <= kMostTerms) return launch_few_terms<T, kBack>(a, st);
+  const int64_t rows = a.perm ? a.rows : std::min(a.rows, ((int64_t)1 << kMostShift) / a.comps + 2);
+  if ((kBack ? a.d_out : a.d_in) <= kMostTerms && in_reach(rows, std::max(kBack ? a.ld_gout : a.ld_x, kBack ? a.ld_gx : a.ld_out), sizeof(T))) return launch_few_terms<T, kBack>(a, st);
   const int64_t n = kBack ? a.d_in : a.d_out;
   const bool whole = a.d_in % 4 == 0 && a.d_out % 4 == 0;
   auto go = [&](auto wide) {
@@ -444,6 +558,8 @@ hipError_t launch_rows(const GroupedArgs& a, hipStream_t st) {
   };
   return n > 64 ? go(std::true_type()) : go(std::false_type());
 }
+
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 // How the positions are cut for the matrices' gradients
 template <class T>
@@ -471,10 +587,14 @@ size_t workspace_bytes(int64_t rows, int64_t K, int64_t n, int64_t comps) {
 template <class T, int kR, int kC>
 hipError_t launch_weights(const GroupedArgs& a, const Chunks<T>& c, T* part, T* part_b, hipStream_t st) {
   const bool whole = a.d_in % 4 == 0 && a.d_out % 4 == 0;
-  return in_launches((a.rows >> c.shift) + a.groups, c.row_tiles * c.column_tiles, [&](int64_t first, dim3 grid) {
-    if (whole) k_grouped_weights<T, kR, kC, true><<<grid, kProductThreads, 0, st>>>(a, first, c.shift, (int)c.row_tiles, (int)c.column_tiles, part, part_b);
-    else k_grouped_weights<T, kR, kC, false><<<grid, kProductThreads, 0, st>>>(a, first, c.shift, (int)c.row_tiles, (int)c.column_tiles, part, part_b);
-  });
+  const bool near = in_reach(a.perm ? a.rows : std::min(a.rows, (int64_t)1 << c.shift), std::max(a.ld_x, a.ld_gout), sizeof(T));
+  auto go = [&](auto whole, auto far) {
+    return in_launches((a.rows >> c.shift) + a.groups, c.row_tiles * c.column_tiles, [&](int64_t first, dim3 grid) {
+      k_grouped_weights<T, kR, kC, decltype(whole)::value, decltype(far)::value><<<grid, kProductThreads, 0, st>>>(a, first, c.shift, (int)c.row_tiles, (int)c.column_tiles, part, part_b);
+    });
+  };
+  if (!near) return go(std::false_type(), std::true_type());
+  return whole ? go(std::true_type(), std::false_type()) : go(std::false_type(), std::false_type());
 }
 
 template <class T>
@@ -486,9 +606,13 @@ hipError_t backward(const GroupedArgs& a, char* ws, hipStream_t st) {
   T *part = (T*)ws, *part_b = (T*)(ws + up(c.slots * K * n * sizeof(T)));
   e = c.narrow ? launch_weights<T, 64, kTile<T>>(a, c, part, part_b, st) : launch_weights<T, kTile<T>, kTile<T>>(a, c, part, part_b, st);
   if (e != hipSuccess || c.slots == 0) return e;
-  const int64_t blocks = std::min<int64_t>((K * n + n + kProductThreads - 1) / kProductThreads, 1024);
-  return in_launches(c.count - 1, blocks, [&](int64_t first, dim3 grid) {
-    k_grouped_sums<T><<<grid, kProductThreads, 0, st>>>(a, first, c.shift, (int)blocks, part, part_b);
+  // most chunks have nothing to add up, so that they get few workgroups
+  const bool of_groups = a.groups <= c.count - 1, wide = n % 4 == 0 && aligned16(a.gW) && aligned16(a.gb);
+  const int64_t pieces = of_groups ? a.groups : c.count - 1, numbers = (K * n + n) / (wide ? 4 : 1);
+  const int64_t blocks = std::max<int64_t>(1, std::min((numbers + kProductThreads - 1) / kProductThreads, std::max<int64_t>(16, 16384 / pieces)));
+  return in_launches(pieces, blocks, [&](int64_t first, dim3 grid) {
+    if (wide) k_grouped_sums<T, 4><<<grid, kProductThreads, 0, st>>>(a, first, c.shift, (int)blocks, of_groups, part, part_b);
+    else k_grouped_sums<T, 1><<<grid, kProductThreads, 0, st>>>(a, first, c.shift, (int)blocks, of_groups, part, part_b);
   });
 }
 

@@ -20,6 +20,16 @@ __device__ inline unsigned on_one_die(unsigned block, unsigned blocks) {
   return die * each + (die < more ? die : more) + block / 8;
 }
 
+// ---- buffer descriptors: what is behind their range reads as zero and is not written, without a branch
+
+using Buffer = __amdgpu_buffer_rsrc_t;
+constexpr unsigned kNowhere = 0x80000000u;      // an offset behind every range
+
+// sums of offsets that stay behind the range where one of them is
+__device__ inline unsigned plus(unsigned a, unsigned b) { return __builtin_elementwise_add_sat(a, b); }
+
+__device__ inline Buffer buffer_of(const void* p, int64_t bytes) { return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, (int)bytes, 0x00020000); }
+
 // which of 16 columns lane l16 of a left operand holds, for results 4 q + i to be neighbours: a lane's results are rows Num::row(q, i) of the instruction
 template <class T>
 __device__ inline int column_place(int l16) {
@@ -53,7 +63,7 @@ __device__ inline void load_some(const T* row, int k, int width, T* v) {
   }
 }
 
-// kR rows (columns) of 32 terms in LDS.  A wave reads 16 bytes of each of 16 rows, and writes 8 bytes of rows that are one, two or four apart: the rows are 80
+// kR rows (columns) of 32 terms in LDS.  A wave reads 16 bytes of each of 16 rows, and writes 8 or 16 bytes of rows that are one, two or four apart: the rows are 80
 // bytes apart and their 16 bytes change places with the row's number / 16, in which all of these find different banks (256 bytes in all).
 template <class T, int kR>
 struct alignas(16) Operand;
@@ -73,6 +83,11 @@ struct alignas(16) Operand<float, kR> {
     Num<float>::split(x[2], x[3], hi);
 #pragma unroll
     for (int p = 0; p < 3; ++p) *(u32x2*)&v[p][r][at(r, k)] = u32x2{lo[p], hi[p]};
+  }
+  __device__ void write8(int r, int k, const float* x) {
+    const PartsOf<3> w = Num<float>::parts(x);
+#pragma unroll
+    for (int p = 0; p < 3; ++p) *(u32x4*)&v[p][r][at(r, k)] = w.w[p];
   }
   __device__ void write_some(int r, int k, const float (&x)[1]) {
     unsigned w[3];
@@ -100,6 +115,10 @@ struct alignas(16) Operand<double, kR> {
 #pragma unroll
     for (int h = 0; h < 2; ++h) *(u32x4*)&v[r][k + 2 * h] = __builtin_bit_cast(u32x4, f64x2{x[2 * h], x[2 * h + 1]});
   }
+  __device__ void write8(int r, int k, const double* x) {
+    write4(r, k, x);
+    write4(r, k + 4, x + 4);
+  }
   __device__ void write_some(int r, int k, const double (&x)[1]) { v[r][k] = x[0]; }
 };
 
@@ -121,27 +140,67 @@ struct AlongTerms {
   }
 };
 
-// An operand whose terms are rows of memory: a thread has kPer neighbours of each of four of them
+// An operand whose terms are rows of memory: a wave has eight of them, so that their addresses are the wave's, and a thread kPer neighbours of each
 template <class T, int kR, bool kWhole>
 struct AcrossTerms {
-  static constexpr int kPer = kR / 32;
-  T v[4][kPer];
-  static __device__ int place() { return ((int)threadIdx.x >> 1 & 31) * kPer; }
-  static __device__ int term() { return ((int)threadIdx.x >> 6) * 8 + ((int)threadIdx.x & 1) * 4; }
-  // p: rows of the thread's four terms, an address inside where there is none (ok false: zero)
-  __device__ void fetch(const T* const (&p)[4], const bool (&ok)[4], int first, int width) {
+  static constexpr int kPer = kR / 64;
+  T v[8][kPer];
+  unsigned at[kPer];      // bytes from the start of a row
+  static __device__ int place() { return ((int)threadIdx.x & 63) * kPer; }
+  static __device__ int term() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6) * 8; }
+  // places first .. of rows of `width` numbers; those behind the end hold anything: their results are not kept.  kWhole: width is a multiple of kPer.
+  __device__ AcrossTerms(int first, int width) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      load_some<T, kPer, kWhole>(p[j], first + place(), width, v[j]);
+    for (int i = 0; i < kPer; ++i) {
+      const int c = first + place() + i;
+      at[i] = (unsigned)(c < width ? c : kWhole ? i : width - 1) * (unsigned)sizeof(T);
+    }
+  }
+  // p: rows of the wave's terms, an address inside where there is none (ok false: zero)
+  __device__ void fetch(const T* const (&p)[8], const bool (&ok)[8]) {
+    typedef T Words __attribute__((ext_vector_type(kPer), aligned(sizeof(T))));
+    bool all = true;
 #pragma unroll
-      for (int i = 0; i < kPer; ++i) v[j][i] = ok[j] ? v[j][i] : T(0);
+    for (int j = 0; j < 8; ++j) {
+      if constexpr (kWhole) {
+        const Words w = *(const Words*)((const char*)p[j] + at[0]);
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) v[j][i] = w[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) v[j][i] = *(const T*)((const char*)p[j] + at[i]);
+      }
+      all = all && ok[j];
+    }
+    if (!all) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) v[j][i] = ok[j] ? v[j][i] : T(0);
+    }
+  }
+  // the same through a buffer descriptor, rows at the offsets `row`: what is behind its range is zero
+  __device__ void fetch(Buffer B, const unsigned (&row)[8]) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      if constexpr (kWhole && kPer == 2 && sizeof(T) == 4) {
+        const f32x2 w = __builtin_bit_cast(f32x2, __builtin_amdgcn_raw_buffer_load_b64(B, plus(row[j], at[0]), 0, 0));
+        v[j][0] = w[0];
+        v[j][1] = w[1];
+      } else {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+          if constexpr (sizeof(T) == 4) v[j][i] = __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(B, plus(row[j], at[i]), 0, 0));
+          else v[j][i] = __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b64(B, plus(row[j], at[i]), 0, 0));
+        }
+      }
     }
   }
   __device__ void put(Operand<T, kR>& to) const {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
-      const T x[4] = {v[0][i], v[1][i], v[2][i], v[3][i]};
-      to.write4(place() + i, term(), x);
+      const T x[8] = {v[0][i], v[1][i], v[2][i], v[3][i], v[4][i], v[5][i], v[6][i], v[7][i]};
+      to.write8(place() + i, term(), x);
     }
   }
 };
