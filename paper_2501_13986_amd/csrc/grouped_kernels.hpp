@@ -7,7 +7,6 @@
 #pragma once
 
 #include <algorithm>
-#include <cstdlib>
 #include <type_traits>
 
 #include "grouped.hpp"
@@ -62,28 +61,6 @@ struct Lines {
 };
 
 // ---- lines through buffer descriptors -------------------------------------------------------------------------------------------
-
-// four numbers from column k on of the line at offset `at`, zero behind its end.  kWhole: its width is a multiple of four.
-template <bool kWhole, class T>
-__device__ inline void load_at(Buffer B, unsigned at, int k, int width, T* v) {
-  constexpr int e = sizeof(T);
-  const unsigned off = plus(at, k < width ? (unsigned)k * e : kNowhere);
-  if constexpr (e == 4) {
-    const f32x4 w = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(B, off, 0, 0));
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = w[i];
-  } else {
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const f64x2 w = __builtin_bit_cast(f64x2, __builtin_amdgcn_raw_buffer_load_b128(B, plus(off, h * 16), 0, 0));
-      v[2 * h] = w[0];
-      v[2 * h + 1] = w[1];
-    }
-  }
-  if constexpr (!kWhole)
-#pragma unroll
-    for (int i = 1; i < 4; ++i) v[i] = k + i < width ? v[i] : T(0);
-}
 
 template <int kHow, class T>
 __device__ inline void store_at(const T (&v)[1], Buffer B, unsigned at) {
@@ -226,14 +203,15 @@ __global__ void __launch_bounds__(kProductThreads, 2) k_grouped_stream(GroupedAr
 
 // ---- rows times a matrix ------------------------------------------------------------------------------------------------------
 
-// kR lines x kC columns of out = x W + b (forward) or of gx = gout W^T (kBack).
-template <class T, int kR, int kC, bool kWhole, bool kBack>
+// kR lines x kC columns of out = x W + b (forward) or of gx = gout W^T (kBack).  kFar: rows lie 2^31 bytes apart or more, or the matrix is as large.
+template <class T, int kR, int kC, bool kWhole, bool kBack, bool kFar>
 __global__ void __launch_bounds__(kProductThreads, 2) k_grouped_rows(GroupedArgs a, int64_t first_id, int column_tiles) {
   using Rows = AlongTerms<T, kR, kWhole>;
+  using Along = AlongTerms<T, kC, kWhole>;
   __shared__ Operand<T, kR> R;
   __shared__ Operand<T, kC> C;
   __shared__ int64_t place[kR];      // of the lines in the results, -1: none
-  constexpr int kShift = kR == 128 ? 7 : 6;
+  constexpr int kShift = kR == 128 ? 7 : kR == 64 ? 6 : 5, e = sizeof(T);
   const unsigned block = on_one_die(blockIdx.x, gridDim.x);
   const int64_t id = first_id + block / column_tiles, g = find_group(a, a.comps, kShift, id);
   const int64_t lines_end = cut(a, g + 1) * a.comps, begin = cut(a, g) * a.comps + ((id - first_piece(a, g, a.comps, kShift)) << kShift);
@@ -243,31 +221,37 @@ __global__ void __launch_bounds__(kProductThreads, 2) k_grouped_rows(GroupedArgs
   const T *x = (const T*)(kBack ? a.gout : a.x), *W = (const T*)a.W + g * a.d_in * a.d_out;
   const int64_t ld = kBack ? a.ld_gout : a.ld_x, ld_to = kBack ? a.ld_gx : a.ld_out;
   const Lines lines(begin, a.comps);
-  const T* p[Rows::kPer];
+  const int64_t row0 = kFar || a.perm ? 0 : lines.position, span = a.perm ? a.rows : (have + lines.component + a.comps - 1) / a.comps;
+  const Buffer bx = buffer_of(x + row0 * ld, kFar ? 0 : ((span - 1) * ld + a.comps * K) * e), bw = buffer_of(W, kFar ? 0 : a.d_in * a.d_out * e);
+  const T *p[Rows::kPer], *pw[Along::kPer];
+  unsigned at_x[Rows::kPer], at_w[Along::kPer];
 #pragma unroll
   for (int i = 0; i < Rows::kPer; ++i) {
     unsigned at, m;
     const int line = Rows::row(i);
     lines.of(line < have ? line : 0, at, m);
-    const int64_t r = row_of(a, lines.position + at);
-    p[i] = x + (r < 0 ? 0 : r) * ld + m * (int64_t)K;
+    const int64_t r = row_of(a, lines.position + at), from = (r < 0 ? 0 : r - row0) * ld + m * (int64_t)K;
+    p[i] = x + from;
+    at_x[i] = r < 0 ? kNowhere : (unsigned)(from * e);
     if (threadIdx.x % 8 == 0) place[line] = r < 0 || line >= have ? -1 : r * ld_to + m * (int64_t)n;
   }
   Rows rows;
   AcrossTerms<T, kC, kWhole> across(c0, n);
-  AlongTerms<T, kC, kWhole> along;
-  const T* pw[kC / 32];
+  Along along;
   if constexpr (kBack)
 #pragma unroll
-    for (int i = 0; i < kC / 32; ++i) {
+    for (int i = 0; i < Along::kPer; ++i) {
       const int c = c0 + along.row(i);
       pw[i] = W + (int64_t)(c < n ? c : 0) * K;
+      at_w[i] = c < n ? (unsigned)c * (unsigned)K * e : kNowhere;
     }
   auto fetch = [&](int k0) {
-    rows.fetch(p, k0, K);
+    if constexpr (kFar) rows.fetch(p, k0, K);
+    else rows.fetch(bx, at_x, k0, K);
     if constexpr (kBack) {
-      along.fetch(pw, k0, K);
-    } else {
+      if constexpr (kFar) along.fetch(pw, k0, K);
+      else along.fetch(bw, at_w, k0, K);
+    } else if constexpr (kFar) {
       const T* q[8];
       bool ok[8];
 #pragma unroll
@@ -277,6 +261,14 @@ __global__ void __launch_bounds__(kProductThreads, 2) k_grouped_rows(GroupedArgs
         q[j] = W + (int64_t)(ok[j] ? k : 0) * n;
       }
       across.fetch(q, ok);
+    } else {
+      unsigned q[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int k = k0 + across.term() + j;
+        q[j] = k < K ? (unsigned)k * (unsigned)n * e : kNowhere;
+      }
+      across.fetch(bw, q);
     }
   };
   Results<T, kR, kC> out;
@@ -546,17 +538,28 @@ template <class T, bool kBack>
 hipError_t launch_rows(const GroupedArgs& a, hipStream_t st) {
   const int64_t rows = a.perm ? a.rows : std::min(a.rows, ((int64_t)1 << kMostShift) / a.comps + 2);
   if ((kBack ? a.d_out : a.d_in) <= kMostTerms && in_reach(rows, std::max(kBack ? a.ld_gout : a.ld_x, kBack ? a.ld_gx : a.ld_out), sizeof(T))) return launch_few_terms<T, kBack>(a, st);
-  const int64_t n = kBack ? a.d_in : a.d_out;
-  const bool whole = a.d_in % 4 == 0 && a.d_out % 4 == 0;
-  auto go = [&](auto wide) {
-    constexpr int kR = kTile<T>, kC = decltype(wide)::value ? kTile<T> : 64;
-    const int64_t tiles = (n + kC - 1) / kC, ids = a.rows * a.comps / kR + a.groups;
-    return in_launches(ids, tiles, [&](int64_t first, dim3 grid) {
-      if (whole) k_grouped_rows<T, kR, kC, true, kBack><<<grid, kProductThreads, 0, st>>>(a, first, (int)tiles);
-      else k_grouped_rows<T, kR, kC, false, kBack><<<grid, kProductThreads, 0, st>>>(a, first, (int)tiles);
+  const int64_t n = kBack ? a.d_in : a.d_out, lines = a.rows * a.comps;
+  const bool whole = a.d_in % 4 == 0 && a.d_out % 4 == 0, near = in_reach(rows, kBack ? a.ld_gout : a.ld_x, sizeof(T)) && in_reach(a.d_in, a.d_out, sizeof(T));
+  auto go = [&](auto tall, auto wide, auto whole_, auto far) {
+    constexpr int kR = decltype(tall)::value, kC = decltype(wide)::value;
+    const int64_t tiles = (n + kC - 1) / kC;
+    return in_launches(lines / kR + a.groups, tiles, [&](int64_t first, dim3 grid) {
+      k_grouped_rows<T, kR, kC, decltype(whole_)::value, kBack, decltype(far)::value><<<grid, kProductThreads, 0, st>>>(a, first, (int)tiles);
     });
   };
-  return n > 64 ? go(std::true_type()) : go(std::false_type());
+  auto size = [&](auto whole_, auto far) {
+    constexpr int kAll = kTile<T>;
+    using Tall = std::integral_constant<int, kAll>;
+    using Half = std::integral_constant<int, kAll / 2>;
+    using Narrow = std::integral_constant<int, 64>;
+    // tiles of half the lines where there are fewer than two workgroups a compute unit
+    const bool half = !decltype(far)::value && lines / kAll * ((n + kAll - 1) / kAll) < 512;
+    if constexpr (!decltype(far)::value)
+      if (half) return go(Half(), Narrow(), whole_, far);
+    return n > 64 ? go(Tall(), Tall(), whole_, far) : go(Tall(), Narrow(), whole_, far);
+  };
+  if (!near) return size(std::false_type(), std::true_type());
+  return whole ? size(std::true_type(), std::false_type()) : size(std::false_type(), std::false_type());
 }
 
 bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
@@ -571,8 +574,9 @@ struct Chunks {
     narrow = sizeof(T) == 8 || K <= 64;
     row_tiles = (K + (narrow ? 63 : 127)) / (narrow ? 64 : 128);
     column_tiles = (n + kTile<T> - 1) / kTile<T>;
-    const int64_t want = getenv("GW_WANT") ? atoi(getenv("GW_WANT")) : 400, least = getenv("GW_LEAST") ? atoi(getenv("GW_LEAST")) : 128;
-    while (shift > 4 && (rows >> shift) * row_tiles * column_tiles < want && comps << (shift - 1) >= least) --shift;
+    // 256 lines a chunk are few enough for partial sums to cost little (20 000 x 7 x 128 x 128: 60 us with 256 lines, 68 with 128); fewer where compute units are without work
+    auto workgroups = [&]() { return (rows >> shift) * row_tiles * column_tiles; };
+    while (shift > 4 && ((workgroups() < 1600 && comps << (shift - 1) >= 256) || (workgroups() < 320 && comps << (shift - 1) >= 64))) --shift;
     count = (rows + ((int64_t)1 << shift) - 1) >> shift;
     slots = count > 1 ? 2 * count : 0;
   }

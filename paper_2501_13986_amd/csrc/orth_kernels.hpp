@@ -321,7 +321,7 @@ template <class T, int kS, int NT>
 struct Columns {
   using N = Num<T>;
   static constexpr int kTiles = kS / 16, kWide = 64 * NT, kSlices = (kS > kWide ? kS : kWide) / 32;
-  using Lds = Operand<T, kS>[kSlices];
+  using Lds = Operand<T, kS, true>[kSlices];
   using Gram = Results<T, kS, kS>;
   typename N::Vec x[kTiles][NT];
 

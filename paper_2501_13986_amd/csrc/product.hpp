@@ -30,6 +30,28 @@ __device__ inline unsigned plus(unsigned a, unsigned b) { return __builtin_eleme
 
 __device__ inline Buffer buffer_of(const void* p, int64_t bytes) { return __builtin_amdgcn_make_buffer_rsrc((void*)p, 0, (int)bytes, 0x00020000); }
 
+// four numbers from column k on of the line at offset `at`, zero behind its end.  kWhole: its width is a multiple of four.
+template <bool kWhole, class T>
+__device__ inline void load_at(Buffer B, unsigned at, int k, int width, T* v) {
+  constexpr int e = sizeof(T);
+  const unsigned off = plus(at, k < width ? (unsigned)k * e : kNowhere);
+  if constexpr (e == 4) {
+    const f32x4 w = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(B, off, 0, 0));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = w[i];
+  } else {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const f64x2 w = __builtin_bit_cast(f64x2, __builtin_amdgcn_raw_buffer_load_b128(B, plus(off, h * 16), 0, 0));
+      v[2 * h] = w[0];
+      v[2 * h + 1] = w[1];
+    }
+  }
+  if constexpr (!kWhole)
+#pragma unroll
+    for (int i = 1; i < 4; ++i) v[i] = k + i < width ? v[i] : T(0);
+}
+
 // which of 16 columns lane l16 of a left operand holds, for results 4 q + i to be neighbours: a lane's results are rows Num::row(q, i) of the instruction
 template <class T>
 __device__ inline int column_place(int l16) {
@@ -63,14 +85,14 @@ __device__ inline void load_some(const T* row, int k, int width, T* v) {
   }
 }
 
-// kR rows (columns) of 32 terms in LDS.  A wave reads 16 bytes of each of 16 rows, and writes 8 or 16 bytes of rows that are one, two or four apart: the rows are 80
-// bytes apart and their 16 bytes change places with the row's number / 16, in which all of these find different banks (256 bytes in all).
-template <class T, int kR>
+// kR rows (columns) of 32 terms in LDS.  A wave reads 16 bytes of each of 16 rows and writes rows of 64 bytes one behind the other: the 16 bytes of a row change places with
+// the row's number, so that both find different banks.  kApart: it writes pieces of rows that are four apart; rows are 80 bytes apart then.
+template <class T, int kR, bool kApart = false>
 struct alignas(16) Operand;
-template <int kR>
-struct alignas(16) Operand<float, kR> {
-  __bf16 v[3][kR][kStep + 8];
-  static __device__ int at(int r, int k) { return k ^ (r >> 4 & 3) * 8; }
+template <int kR, bool kApart>
+struct alignas(16) Operand<float, kR, kApart> {
+  __bf16 v[3][kR][kApart ? kStep + 8 : kStep];
+  static __device__ int at(int r, int k) { return k ^ (kApart ? r >> 4 & 3 : (r >> 1 ^ r >> 3) & 3) * 8; }
   __device__ PartsOf<3> read(int r, int k) const {
     PartsOf<3> p;
 #pragma unroll
@@ -102,8 +124,8 @@ struct alignas(16) Operand<float, kR> {
     for (int p = 0; p < 3; ++p) *(unsigned*)&v[p][r][at(r, k)] = w[p];
   }
 };
-template <int kR>
-struct alignas(16) Operand<double, kR> {
+template <int kR, bool kApart>
+struct alignas(16) Operand<double, kR, kApart> {
   double v[kR][kStep + 2];
   __device__ PartsOf<4> read(int r, int k) const {
     PartsOf<4> p;
@@ -133,6 +155,11 @@ struct AlongTerms {
   __device__ void fetch(const T* const (&p)[kPer], int k0, int terms) {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) load_some<T, 4, kWhole>(p[i], k0 + term(), terms, v[i]);
+  }
+  // the same through a buffer descriptor, rows at the offsets `at`
+  __device__ void fetch(Buffer B, const unsigned (&at)[kPer], int k0, int terms) {
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) load_at<kWhole>(B, at[i], k0 + term(), terms, v[i]);
   }
   __device__ void put(Operand<T, kR>& to) const {
 #pragma unroll
@@ -230,7 +257,8 @@ struct Results {
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) to[ct] += *(const typename N::Vec*)(from + (int64_t)p * (kR * kC) + ct * kProductThreads * 4);
   }
-  __device__ void multiply(const Operand<T, kR>& R, const Operand<T, kC>& C) {
+  template <bool kApart>
+  __device__ void multiply(const Operand<T, kR, kApart>& R, const Operand<T, kC, kApart>& C) {
     const int l16 = lane() % 16, k = lane() / 16 * 8, r0 = wave() / 2 * (kR / 2), c0 = wave() % 2 * (kC / 2) + column_place<T>(l16);
     typename N::Parts c[CT];
 #pragma unroll
