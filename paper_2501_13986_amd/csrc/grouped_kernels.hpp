@@ -209,7 +209,7 @@ __global__ void __launch_bounds__(kProductThreads, 2) k_grouped_rows(GroupedArgs
   using Rows = AlongTerms<T, kR, kWhole>;
   using Along = AlongTerms<T, kC, kWhole>;
   __shared__ Operand<T, kR> R;
-  __shared__ Operand<T, kC> C;
+  __shared__ std::conditional_t<kBack, Operand<T, kC>, typename AcrossTerms<T, kC, kWhole>::To> C;
   __shared__ int64_t place[kR];      // of the lines in the results, -1: none
   constexpr int kShift = kR == 128 ? 7 : kR == 64 ? 6 : 5, e = sizeof(T);
   const unsigned block = on_one_die(blockIdx.x, gridDim.x);
@@ -312,8 +312,8 @@ constexpr int kTable = 512;      // lines whose offsets stand in LDS at a time
 // kFar: rows of x or gout lie 2^31 bytes apart or more, addresses are formed for each.
 template <class T, int kR, int kC, bool kWhole, bool kFar>
 __global__ void __launch_bounds__(kProductThreads, 2) k_grouped_weights(GroupedArgs a, int64_t first_id, int shift, int row_tiles, int column_tiles, T* part, T* part_b) {
-  __shared__ Operand<T, kR> R;
-  __shared__ Operand<T, kC> C;
+  __shared__ typename AcrossTerms<T, kR, kWhole>::To R;
+  __shared__ typename AcrossTerms<T, kC, kWhole>::To C;
   __shared__ alignas(16) unsigned table[kFar ? 1 : kTable][2];
   const unsigned block = on_one_die(blockIdx.x, gridDim.x);      // which read the same rows
   const int tiles = row_tiles * column_tiles, tile = block % tiles;

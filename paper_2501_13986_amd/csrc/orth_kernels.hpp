@@ -306,7 +306,7 @@ __global__ void __launch_bounds__(kProductThreads) k_orth_finish(OrthArgs a, Pro
 
 // ---- up to 128 rows of X --------------------------------------------------------------------------------------------------------
 //
-// A workgroup has 64 NT columns of X in its registers, a wave 16 NT of them with all their rows: lane: columns NT l16 + j, rows 16 t + 4 q + (0..3).
+// A workgroup has 16 NT columns of X for each of its kWaves waves in registers, a wave all their rows: lane: columns NT l16 + j, rows 16 t + 4 q + (0..3).
 // A step is X <- a X + A V, V = b X + c A X, so that both products have A (in LDS) on the left and on the right what the wave has: results of the matrix
 // instructions are operands of the next ones as they are, with the terms of 32 rows in the order `place`.  Only for A = X X^T does X go through LDS.
 // Where the workgroup has all columns, the steps run without leaving it.  Where not, a launch is a step: the workgroups leave their shares of A, which all of the next
@@ -317,12 +317,12 @@ constexpr int kMostRows = 128;
 // the place of row r among 32 terms of results
 __device__ inline int place(int r) { return r % 16 / 4 * 8 + r / 16 * 4 + r % 4; }
 
-template <class T, int kS, int NT>
+template <class T, int kS, int NT, int kWaves>
 struct Columns {
   using N = Num<T>;
-  static constexpr int kTiles = kS / 16, kWide = 64 * NT, kSlices = (kS > kWide ? kS : kWide) / 32;
-  using Lds = Operand<T, kS, true>[kSlices];
-  using Gram = Results<T, kS, kS>;
+  static constexpr int kTiles = kS / 16, kWide = 16 * NT * kWaves, kSlices = (kS > kWide ? kS : kWide) / 32, kThreads = 64 * kWaves;
+  using Lds = Operand<T, kS, kApart>[kSlices];
+  using Gram = Results<T, kS, kS, 2, kWaves / 2>;
   typename N::Vec x[kTiles][NT];
 
   static __device__ int lane() { return (int)threadIdx.x & 63; }
@@ -362,13 +362,13 @@ struct Columns {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-      for (int j = 0; j < NT; ++j) *(typename N::Vec*)(to + ((t * NT + j) * kProductThreads + (int)threadIdx.x) * 4) = x[t][j];
+      for (int j = 0; j < NT; ++j) *(typename N::Vec*)(to + ((t * NT + j) * kThreads + (int)threadIdx.x) * 4) = x[t][j];
   }
   __device__ void take(const T* from) {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-      for (int j = 0; j < NT; ++j) x[t][j] = *(const typename N::Vec*)(from + ((t * NT + j) * kProductThreads + (int)threadIdx.x) * 4);
+      for (int j = 0; j < NT; ++j) x[t][j] = *(const typename N::Vec*)(from + ((t * NT + j) * kThreads + (int)threadIdx.x) * 4);
   }
   // the thread's share of the sum of squares
   __device__ double squares() const {
@@ -467,30 +467,34 @@ struct Columns {
 };
 
 // sum over the workgroup, to all its threads
+template <int kWaves>
 __device__ inline double sum_of_all(double v, double* sums) {
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
   sums[threadIdx.x / 64] = v;      // all lanes the same
   __syncthreads();
-  return (sums[0] + sums[1]) + (sums[2] + sums[3]);
+  v = 0;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) v += sums[i];
+  return v;
 }
 
 struct Schedule {
   double c[64][3];
 };
 
-// all steps of a matrix of at most 64 NT columns
-template <class T, int kS, int NT>
-__global__ void __launch_bounds__(kProductThreads, 1) k_orth_whole(OrthArgs a, int64_t first, int steps, Schedule schedule) {
-  using Cols = Columns<T, kS, NT>;
+// all steps of a matrix of at most 16 NT kWaves columns
+template <class T, int kS, int NT, int kWaves>
+__global__ void __launch_bounds__((64 * kWaves), (kWaves / 4)) k_orth_whole(OrthArgs a, int64_t first, int steps, Schedule schedule) {
+  using Cols = Columns<T, kS, NT, kWaves>;
   __shared__ typename Cols::Lds S;
-  __shared__ double sums[kProductThreads / 64];
+  __shared__ double sums[kWaves];
   const int64_t matrix = first + blockIdx.x;
   const bool turned = a.m > a.n;
   const int s = (int)(turned ? a.n : a.m), l = (int)(turned ? a.m : a.n);
   Cols X;
   X.load((const T*)a.g + matrix * a.stride_g, a.ld_g, s, l, 0, turned);
-  X.scale(1.0 / (sqrt(sum_of_all(X.squares(), sums)) + a.eps));
+  X.scale(1.0 / (sqrt(sum_of_all<kWaves>(X.squares(), sums)) + a.eps));
   for (int i = 0; i < steps; ++i) {
     typename Cols::Gram A;
     X.gram(S, A);
@@ -500,10 +504,10 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_orth_whole(OrthArgs a, i
   X.store((T*)a.out + matrix * a.stride_out, a.ld_out, s, l, 0, turned);
 }
 
-// The first share of A [matrix][chunk][kS * kS] and X [matrix][chunk][kS * 64 NT], in the order of the registers
-template <class T, int kS, int NT>
-__global__ void __launch_bounds__(kProductThreads, 1) k_orth_begin(OrthArgs a, int64_t first, int chunks, int shares, const double* part, T* X_to, T* A_to) {
-  using Cols = Columns<T, kS, NT>;
+// The first share of A [matrix][chunk][kS * kS] and X [matrix][chunk][kS * columns], in the order of the registers
+template <class T, int kS, int NT, int kWaves>
+__global__ void __launch_bounds__((64 * kWaves), (kWaves / 4)) k_orth_begin(OrthArgs a, int64_t first, int chunks, int shares, const double* part, T* X_to, T* A_to) {
+  using Cols = Columns<T, kS, NT, kWaves>;
   __shared__ typename Cols::Lds S;
   const int64_t matrix = first + blockIdx.x / chunks, place = matrix * chunks + blockIdx.x % chunks;
   const bool turned = a.m > a.n;
@@ -518,9 +522,9 @@ __global__ void __launch_bounds__(kProductThreads, 1) k_orth_begin(OrthArgs a, i
 }
 
 // A step.  parts: how many shares of A there are a matrix
-template <class T, int kS, int NT, bool kLast>
-__global__ void __launch_bounds__(kProductThreads, 1) k_orth_step(OrthArgs a, int64_t first, int chunks, int parts, T c0, T c1, T c2, T* X_at, const T* A_from, T* A_to) {
-  using Cols = Columns<T, kS, NT>;
+template <class T, int kS, int NT, int kWaves, bool kLast>
+__global__ void __launch_bounds__((64 * kWaves), (kWaves / 4)) k_orth_step(OrthArgs a, int64_t first, int chunks, int parts, T c0, T c1, T c2, T* X_at, const T* A_from, T* A_to) {
+  using Cols = Columns<T, kS, NT, kWaves>;
   __shared__ typename Cols::Lds S;
   const int64_t matrix = first + blockIdx.x / chunks, place = matrix * chunks + blockIdx.x % chunks;
   Cols X;
@@ -664,13 +668,13 @@ hipError_t many_rows(const OrthArgs& a, const double* coefficients, int steps, c
   return e;
 }
 
-template <class T, int kS, int NT>
+template <class T, int kS, int NT, int kWaves>
 hipError_t few_rows(const OrthArgs& a, const double* coefficients, int steps, char* ws, hipStream_t st) {
   const Few f(a.m, a.n, sizeof(T) == 8);
   if (f.chunks == 1) {
     Schedule schedule = {};
     for (int i = 0; i < 3 * steps; ++i) schedule.c[i / 3][i % 3] = coefficients[i];
-    return in_launches(a.batch, 1, [&](int64_t first, dim3 grid) { k_orth_whole<T, kS, NT><<<grid, kProductThreads, 0, st>>>(a, first, steps, schedule); });
+    return in_launches(a.batch, 1, [&](int64_t first, dim3 grid) { k_orth_whole<T, kS, NT, kWaves><<<grid, 64 * kWaves, 0, st>>>(a, first, steps, schedule); });
   }
   const int shares = shares_of(a.m, a.n), chunks = (int)f.chunks;
   double* part = (double*)ws;
@@ -680,7 +684,7 @@ hipError_t few_rows(const OrthArgs& a, const double* coefficients, int steps, ch
   T* sum = (T*)((char*)next + up(a.batch * f.a_size() * sizeof(T)));
   hipError_t e = in_launches(a.batch, shares, [&](int64_t first, dim3 grid) { k_orth_squares<T><<<grid, kProductThreads, 0, st>>>(a, first, shares, part); });
   if (e != hipSuccess) return e;
-  e = in_launches(a.batch, chunks, [&](int64_t first, dim3 grid) { k_orth_begin<T, kS, NT><<<grid, kProductThreads, 0, st>>>(a, first, chunks, shares, part, X, A); });
+  e = in_launches(a.batch, chunks, [&](int64_t first, dim3 grid) { k_orth_begin<T, kS, NT, kWaves><<<grid, 64 * kWaves, 0, st>>>(a, first, chunks, shares, part, X, A); });
   for (int i = 0; i < steps && e == hipSuccess; ++i) {
     const double* c = coefficients + 3 * i;
     const T *from = A;
@@ -693,8 +697,8 @@ hipError_t few_rows(const OrthArgs& a, const double* coefficients, int steps, ch
       parts = 1;
     }
     e = in_launches(a.batch, chunks, [&](int64_t first, dim3 grid) {
-      if (i + 1 < steps) k_orth_step<T, kS, NT, false><<<grid, kProductThreads, 0, st>>>(a, first, chunks, parts, (T)c[0], (T)c[1], (T)c[2], X, from, next);
-      else k_orth_step<T, kS, NT, true><<<grid, kProductThreads, 0, st>>>(a, first, chunks, parts, (T)c[0], (T)c[1], (T)c[2], X, from, next);
+      if (i + 1 < steps) k_orth_step<T, kS, NT, kWaves, false><<<grid, 64 * kWaves, 0, st>>>(a, first, chunks, parts, (T)c[0], (T)c[1], (T)c[2], X, from, next);
+      else k_orth_step<T, kS, NT, kWaves, true><<<grid, 64 * kWaves, 0, st>>>(a, first, chunks, parts, (T)c[0], (T)c[1], (T)c[2], X, from, next);
     });
     std::swap(A, next);
   }
@@ -708,8 +712,11 @@ hipError_t orthogonalise(const OrthArgs& a, const double* coefficients, int step
     auto go = [&](auto rows) {
       constexpr int kS = decltype(rows)::value;
       if constexpr (sizeof(T) == 4)
-        if (f.wide == 128) return few_rows<T, kS, 2>(a, coefficients, steps, ws, st);
-      return few_rows<T, kS, 1>(a, coefficients, steps, ws, st);
+        if (f.wide == 128) {
+          if constexpr (kS % 64 == 0) return getenv("ORTH_4") ? few_rows<T, kS, 2, 4>(a, coefficients, steps, ws, st) : few_rows<T, kS, 1, 8>(a, coefficients, steps, ws, st);
+          else return few_rows<T, kS, 2, 4>(a, coefficients, steps, ws, st);
+        }
+      return few_rows<T, kS, 1, 4>(a, coefficients, steps, ws, st);
     };
     switch (f.rows) {
       case 32: return go(std::integral_constant<int, 32>());

@@ -85,18 +85,27 @@ __device__ inline void load_some(const T* row, int k, int width, T* v) {
   }
 }
 
-// kR rows (columns) of 32 terms in LDS.  A wave reads 16 bytes of each of 16 rows and writes rows of 64 bytes one behind the other: the 16 bytes of a row change places with
-// the row's number, so that both find different banks.  kApart: it writes pieces of rows that are four apart; rows are 80 bytes apart then.
-template <class T, int kR, bool kApart = false>
+// kR rows (columns) of 32 terms in LDS.  A wave reads 16 bytes of each of 16 rows, 16 lanes at a time, of two neighbouring quarters (lanes 0-3, 12-15 and 20-27 together, counters
+// show): the 16 bytes of a row change places with bits of the row's number so that these find different banks, 256 bytes in all, and so do the lanes that write, 128
+// bytes at a time.  They write
+//   kWholeRows     rows of 64 bytes one behind the other, or 16 bytes of neighbouring rows
+//   kEveryOther    16 bytes of every other row: the odd rows stand behind the even ones (128 rows)
+//   kApart         pieces of rows that are four apart: rows are 80 bytes apart
+enum Written { kWholeRows, kEveryOther, kApart };
+template <class T, int kR, Written kBy = kWholeRows>
 struct alignas(16) Operand;
-template <int kR, bool kApart>
-struct alignas(16) Operand<float, kR, kApart> {
-  __bf16 v[3][kR][kApart ? kStep + 8 : kStep];
-  static __device__ int at(int r, int k) { return k ^ (kApart ? r >> 4 & 3 : (r >> 1 ^ r >> 3) & 3) * 8; }
+template <int kR, Written kBy>
+struct alignas(16) Operand<float, kR, kBy> {
+  __bf16 v[3][kR][kBy == kApart ? kStep + 8 : kStep];
+  static __device__ int line(int r) { return kBy == kEveryOther ? r >> 1 | (r & 1) << 6 : r; }
+  static __device__ int at(int r, int k) {
+    const int w = line(r);
+    return k ^ (kBy == kApart ? (w >> 2 ^ w >> 3) & 1 : (w >> 1 ^ w >> 6) & 3) * 8;
+  }
   __device__ PartsOf<3> read(int r, int k) const {
     PartsOf<3> p;
 #pragma unroll
-    for (int i = 0; i < 3; ++i) p.w[i] = *(const u32x4*)&v[i][r][at(r, k)];
+    for (int i = 0; i < 3; ++i) p.w[i] = *(const u32x4*)&v[i][line(r)][at(r, k)];
     return p;
   }
   __device__ void write4(int r, int k, const float* x) {
@@ -104,28 +113,28 @@ struct alignas(16) Operand<float, kR, kApart> {
     Num<float>::split(x[0], x[1], lo);
     Num<float>::split(x[2], x[3], hi);
 #pragma unroll
-    for (int p = 0; p < 3; ++p) *(u32x2*)&v[p][r][at(r, k)] = u32x2{lo[p], hi[p]};
+    for (int p = 0; p < 3; ++p) *(u32x2*)&v[p][line(r)][at(r, k)] = u32x2{lo[p], hi[p]};
   }
   __device__ void write8(int r, int k, const float* x) {
     const PartsOf<3> w = Num<float>::parts(x);
 #pragma unroll
-    for (int p = 0; p < 3; ++p) *(u32x4*)&v[p][r][at(r, k)] = w.w[p];
+    for (int p = 0; p < 3; ++p) *(u32x4*)&v[p][line(r)][at(r, k)] = w.w[p];
   }
   __device__ void write_some(int r, int k, const float (&x)[1]) {
     unsigned w[3];
     Num<float>::split(x[0], 0.f, w);
 #pragma unroll
-    for (int p = 0; p < 3; ++p) *(unsigned short*)&v[p][r][at(r, k)] = (unsigned short)w[p];
+    for (int p = 0; p < 3; ++p) *(unsigned short*)&v[p][line(r)][at(r, k)] = (unsigned short)w[p];
   }
   __device__ void write_some(int r, int k, const float (&x)[2]) {
     unsigned w[3];
     Num<float>::split(x[0], x[1], w);
 #pragma unroll
-    for (int p = 0; p < 3; ++p) *(unsigned*)&v[p][r][at(r, k)] = w[p];
+    for (int p = 0; p < 3; ++p) *(unsigned*)&v[p][line(r)][at(r, k)] = w[p];
   }
 };
-template <int kR, bool kApart>
-struct alignas(16) Operand<double, kR, kApart> {
+template <int kR, Written kBy>
+struct alignas(16) Operand<double, kR, kBy> {
   double v[kR][kStep + 2];
   __device__ PartsOf<4> read(int r, int k) const {
     PartsOf<4> p;
@@ -171,6 +180,7 @@ struct AlongTerms {
 template <class T, int kR, bool kWhole>
 struct AcrossTerms {
   static constexpr int kPer = kR / 64;
+  using To = Operand<T, kR, kPer == 2 ? kEveryOther : kWholeRows>;
   T v[8][kPer];
   unsigned at[kPer];      // bytes from the start of a row
   static __device__ int place() { return ((int)threadIdx.x & 63) * kPer; }
@@ -223,7 +233,7 @@ struct AcrossTerms {
       }
     }
   }
-  __device__ void put(Operand<T, kR>& to) const {
+  __device__ void put(To& to) const {
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const T x[8] = {v[0][i], v[1][i], v[2][i], v[3][i], v[4][i], v[5][i], v[6][i], v[7][i]};
@@ -232,34 +242,36 @@ struct AcrossTerms {
   }
 };
 
-// The results of a workgroup: a wave's quarter of them
-template <class T, int kR, int kC>
+// The results of a workgroup, kUp x kAcross waves
+template <class T, int kR, int kC, int kUp = 2, int kAcross = 2>
 struct Results {
   using N = Num<T>;
-  static constexpr int RT = kR / 32, CT = kC / 32;
+  static constexpr int RT = kR / (16 * kUp), CT = kC / (16 * kAcross), kThreads = 64 * kUp * kAcross;
   typename N::Vec acc[RT][CT] = {};
   static __device__ int lane() { return (int)threadIdx.x & 63; }
   static __device__ int wave() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
-  static __device__ int row(int rt) { return wave() / 2 * (kR / 2) + rt * 16 + lane() % 16; }
-  static __device__ int column(int ct) { return wave() % 2 * (kC / 2) + ct * 16 + lane() / 16 * 4; }      // the first of four
+  static __device__ int first_row() { return wave() / kAcross * (kR / kUp); }
+  static __device__ int first_column() { return wave() % kAcross * (kC / kAcross); }
+  static __device__ int row(int rt) { return first_row() + rt * 16 + lane() % 16; }
+  static __device__ int column(int ct) { return first_column() + ct * 16 + lane() / 16 * 4; }      // the first of four
   // in the order of the registers: kR x kC numbers
   __device__ void keep(T* to) const {
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) *(typename N::Vec*)(to + ((rt * CT + ct) * kProductThreads + (int)threadIdx.x) * 4) = acc[rt][ct];
+      for (int ct = 0; ct < CT; ++ct) *(typename N::Vec*)(to + ((rt * CT + ct) * kThreads + (int)threadIdx.x) * 4) = acc[rt][ct];
   }
   // the sum of tiles rt of `parts` such, in their order
   static __device__ void add_up(const T* from, int parts, int rt, typename N::Vec (&to)[CT]) {
-    from += (rt * CT * kProductThreads + (int)threadIdx.x) * 4;
+    from += (rt * CT * kThreads + (int)threadIdx.x) * 4;
 #pragma unroll 4
     for (int p = 0; p < parts; ++p)
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) to[ct] += *(const typename N::Vec*)(from + (int64_t)p * (kR * kC) + ct * kProductThreads * 4);
+      for (int ct = 0; ct < CT; ++ct) to[ct] += *(const typename N::Vec*)(from + (int64_t)p * (kR * kC) + ct * kThreads * 4);
   }
-  template <bool kApart>
-  __device__ void multiply(const Operand<T, kR, kApart>& R, const Operand<T, kC, kApart>& C) {
-    const int l16 = lane() % 16, k = lane() / 16 * 8, r0 = wave() / 2 * (kR / 2), c0 = wave() % 2 * (kC / 2) + column_place<T>(l16);
+  template <Written kByR, Written kByC>
+  __device__ void multiply(const Operand<T, kR, kByR>& R, const Operand<T, kC, kByC>& C) {
+    const int l16 = lane() % 16, k = lane() / 16 * 8, r0 = first_row(), c0 = first_column() + column_place<T>(l16);
     typename N::Parts c[CT];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) c[ct] = C.read(c0 + ct * 16, k);
