@@ -75,20 +75,18 @@ struct Stored<float> {
   int ld;             // blocks a row of blocks
   __device__ Stored(void* at, int64_t rows, int64_t terms) : p((unsigned short*)at), plane(rows * terms), ld((int)(terms / kStep)) {}
   __device__ int64_t at(int r, int k) const { return ((int64_t)(r / kBlock) * ld + k / kStep) * (kBlock * kStep) + r % kBlock * kStep + k % kStep; }
-  __device__ void write4(int r, int k, const float* x) const {
-    unsigned lo[3], hi[3];
-    Num<float>::split(x[0], x[1], lo);
-    Num<float>::split(x[2], x[3], hi);
+  __device__ void write8(int r, int k, const float* x) const {
+    const PartsOf<3> w = Num<float>::parts(x);
 #pragma unroll
-    for (int i = 0; i < 3; ++i) *(u32x2*)(p + i * plane + at(r, k)) = u32x2{lo[i], hi[i]};
+    for (int i = 0; i < 3; ++i) *(u32x4*)(p + i * plane + at(r, k)) = w.w[i];
   }
   // the parts' sum is the number itself
-  __device__ void read4(int r, int k, float* x) const {
-    u32x2 w[3];
+  __device__ void read8(int r, int k, float* x) const {
+    u32x4 w[3];
 #pragma unroll
-    for (int i = 0; i < 3; ++i) w[i] = *(const u32x2*)(p + i * plane + at(r, k));
+    for (int i = 0; i < 3; ++i) w[i] = *(const u32x4*)(p + i * plane + at(r, k));
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
+    for (int j = 0; j < 8; ++j) {
       float v[3];
 #pragma unroll
       for (int i = 0; i < 3; ++i) v[i] = __builtin_bit_cast(float, j & 1 ? w[i][j / 2] & 0xffff0000u : w[i][j / 2] << 16);
@@ -103,11 +101,17 @@ struct Stored<double> {
   int ld;
   __device__ Stored(void* at, int64_t, int64_t terms) : p((double*)at), ld((int)(terms / kStep)) {}
   __device__ int64_t at(int r, int k) const { return ((int64_t)(r / kBlock) * ld + k / kStep) * (kBlock * kStep) + r % kBlock * kStep + k % kStep; }
-  __device__ void write4(int r, int k, const double* x) const { *(f64x4*)(p + at(r, k)) = f64x4{x[0], x[1], x[2], x[3]}; }
-  __device__ void read4(int r, int k, double* x) const {
-    const f64x4 w = *(const f64x4*)(p + at(r, k));
+  __device__ void write8(int r, int k, const double* x) const {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) x[j] = w[j];
+    for (int h = 0; h < 8; h += 2) *(f64x2*)(p + at(r, k) + h) = f64x2{x[h], x[h + 1]};
+  }
+  __device__ void read8(int r, int k, double* x) const {
+#pragma unroll
+    for (int h = 0; h < 8; h += 2) {
+      const f64x2 w = *(const f64x2*)(p + at(r, k) + h);
+      x[h] = w[0];
+      x[h + 1] = w[1];
+    }
   }
 };
 
@@ -164,11 +168,16 @@ __global__ void __launch_bounds__(kProductThreads) k_orth_start(OrthArgs a, int6
     else tile[y][x] = v;
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < kBlock * kBlock / 4; i += kProductThreads) {
-    const int y = i / 16, k = i % 16 * 4;
-    const T v[4] = {tile[y][k], tile[y][k + 1], tile[y][k + 2], tile[y][k + 3]}, u[4] = {tile[k][y], tile[k + 1][y], tile[k + 2][y], tile[k + 3][y]};
-    to.write4(r0 + y, c0 + k, v);
-    to_t.write4(c0 + y, r0 + k, u);
+  for (int i = threadIdx.x; i < kBlock * kBlock / 8; i += kProductThreads) {      // whole blocks one behind the other
+    const int y = i / 4 % kBlock, k = i / (4 * kBlock) * kStep + i % 4 * 8;
+    T v[8], u[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      v[j] = tile[y][k + j];
+      u[j] = tile[k + j][y];
+    }
+    to.write8(r0 + y, c0 + k, v);
+    to_t.write8(c0 + y, r0 + k, u);
   }
 }
 
@@ -189,119 +198,142 @@ struct Product {
   bool symmetric, last;
 };
 
-constexpr int kStrip = 32;      // rows of a tile that are turned at a time: 16 of each half
-
-template <class T, int kTile>
+template <class T, int kR, int kC>
 union ProductLds {
   struct {
-    Operand<T, kTile> R, C;
+    Operand<T, kR> R;
+    Operand<T, kC> C;
   } in;
-  T out[kStrip][kTile + 1];
+  T out[64][kC + 1];      // rows of a tile that pass through LDS at a time: 32 of each half
   __device__ ProductLds() {}
 };
 
-template <class T, int kTile>
+template <int kC>
 __device__ inline void tile_of(const Product& p, int t, int& tr, int& tc) {
   if (p.symmetric) {
     upper_tile(t, tr, tc);
   } else {
-    tr = t / (p.columns / kTile);
-    tc = t % (p.columns / kTile);
+    tr = t / (p.columns / kC);
+    tc = t % (p.columns / kC);
   }
 }
 
-// the rows of tiles rt of the four waves
-template <class T, int kTile, class Vec>
-__device__ inline void finish(const OrthArgs& a, const Product& p, int64_t matrix, int tr, int tc, int rt, const Vec (&acc)[kTile / 32], T (&tile)[kStrip][kTile + 1]) {
-  using Out = Results<T, kTile, kTile>;
+// kRows rows of a tile, whose products (times beta) stand in LDS: the rows from r0 on, and with 64 those that are half a tile behind them
+template <class T, int kR, int kC, int kRows>
+__device__ inline void finish(const OrthArgs& a, const Product& p, int64_t matrix, int r0, int c0, T (&tile)[kRows][kC + 1]) {
   const int64_t size = (int64_t)p.rows * p.columns * Stored<T>::kBytes;
-  const int r0 = tr * kTile, c0 = tc * kTile;
-  const T alpha = (T)p.alpha, beta = (T)p.beta;
-  auto row = [&](int y) { return r0 + y / 16 * (kTile / 2) + rt * 16 + y % 16; };
-#pragma unroll
-  for (int ct = 0; ct < Out::CT; ++ct) {
-    const int r = Out::row(rt), c = Out::column(ct), y16 = Out::wave() / 2 * 16 + Out::lane() % 16;
-    T v[4], y[4] = {};
-    if (p.alpha != 0) Stored<T>(p.y + matrix * size, p.rows, p.columns).read4(r0 + r, c0 + c, y);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[i] = beta * acc[ct][i] + alpha * y[i];
-      tile[y16][c + i] = v[i];
-    }
-    if (!p.last) Stored<T>(p.to + matrix * size, p.rows, p.columns).write4(r0 + r, c0 + c, v);
-  }
-  if (p.symmetric && tr == tc) return;
+  const T alpha = (T)p.alpha;
+  auto row = [&](int y) { return r0 + y / 32 * (kR / 2) + y % 32; };
   __syncthreads();
+  const bool add = p.alpha != 0, mirror = !p.symmetric || r0 / kR != c0 / kC;
+  if (add || !p.last) {
+    const Stored<T> y(p.y + matrix * size, p.rows, p.columns), to(p.to + matrix * size, p.rows, p.columns);
+    for (int i = threadIdx.x; i < kRows * kC / 8; i += kProductThreads) {      // rows of 64 bytes one behind the other
+      const int r = i / 4 % kRows, k = i / (4 * kRows) * kStep + i % 4 * 8;
+      T v[8], u[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = tile[r][k + j];
+      if (add) {
+        y.read8(row(r), c0 + k, u);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          v[j] += alpha * u[j];
+          tile[r][k + j] = v[j];
+        }
+      }
+      if (!p.last) to.write8(row(r), c0 + k, v);
+    }
+    __syncthreads();
+  }
   if (p.last) {
     T* to = (T*)a.out + matrix * a.stride_out;
     if (a.m > a.n) {
-      for (int i = threadIdx.x; i < kTile * kStrip; i += kProductThreads) {
-        const int y = i % kStrip, x = i / kStrip;
+      for (int i = threadIdx.x; i < kC * kRows; i += kProductThreads) {
+        const int y = i % kRows, x = i / kRows;
         if (c0 + x < a.m && row(y) < a.n) to[(int64_t)(c0 + x) * a.ld_out + row(y)] = tile[y][x];
       }
     } else {
-      for (int i = threadIdx.x; i < kTile * kStrip; i += kProductThreads) {
-        const int y = i / kTile, x = i % kTile;
+      for (int i = threadIdx.x; i < kC * kRows; i += kProductThreads) {
+        const int y = i / kC, x = i % kC;
         if (row(y) < a.m && c0 + x < a.n) to[(int64_t)row(y) * a.ld_out + c0 + x] = tile[y][x];
       }
     }
-    return;
-  }
-  const Stored<T> to((p.symmetric ? p.to : p.to_t) + matrix * size, p.columns, p.rows);
-  for (int i = threadIdx.x; i < kTile * kStrip / 4; i += kProductThreads) {
-    const int c = i % kTile, k = i / kTile * 4;      // neighbours of a row of the tile side by side
-    const T v[4] = {tile[k][c], tile[k + 1][c], tile[k + 2][c], tile[k + 3][c]};
-    to.write4(c0 + c, row(k), v);
+  } else if (mirror) {
+    const Stored<T> to((p.symmetric ? p.to : p.to_t) + matrix * size, p.columns, p.rows);
+    for (int i = threadIdx.x; i < kRows * kC / 8; i += kProductThreads) {
+      const int c = i / 4 % kC, k = i / (4 * kC) * 32 + i % 4 * 8;
+      T v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = tile[k + j][c];
+      to.write8(c0 + c, row(k), v);
+    }
   }
 }
 
-template <class T, int kTile>
+template <class T, int kR, int kC>
 __global__ void __launch_bounds__(kProductThreads, 2) k_orth_product(OrthArgs a, Product p, int64_t first, T* part) {
-  __shared__ ProductLds<T, kTile> S;
+  __shared__ ProductLds<T, kR, kC> S;
   const unsigned block = on_one_die(blockIdx.x, gridDim.x);
   const int t = block % p.tiles, split = block / p.tiles % p.splits;
   const int64_t matrix = first + block / p.tiles / p.splits;
   int tr, tc;
-  tile_of<T, kTile>(p, t, tr, tc);
+  tile_of<kC>(p, t, tr, tc);
   const Stored<T> left(p.rows_at + matrix * p.rows * p.terms * Stored<T>::kBytes, p.rows, p.terms), right(p.columns_at + matrix * p.columns * p.terms * Stored<T>::kBytes, p.columns, p.terms);
   const int steps = p.terms / kStep, from = steps * split / p.splits, end = steps * (split + 1) / p.splits;
-  Copy<T, kTile> rows, columns;
-  Results<T, kTile, kTile> out;
-  rows.fetch(left, tr * kTile, from * kStep);
-  columns.fetch(right, tc * kTile, from * kStep);
+  Copy<T, kR> rows;
+  Copy<T, kC> columns;
+  Results<T, kR, kC> out;
+  rows.fetch(left, tr * kR, from * kStep);
+  columns.fetch(right, tc * kC, from * kStep);
   for (int k = from; k < end; ++k) {
     __syncthreads();
     rows.put(S.in.R);
     columns.put(S.in.C);
     __syncthreads();
     if (k + 1 < end) {
-      rows.fetch(left, tr * kTile, (k + 1) * kStep);
-      columns.fetch(right, tc * kTile, (k + 1) * kStep);
+      rows.fetch(left, tr * kR, (k + 1) * kStep);
+      columns.fetch(right, tc * kC, (k + 1) * kStep);
     }
     out.multiply(S.in.R, S.in.C);
   }
   if (p.splits > 1) {
-    out.keep(part + ((matrix * p.tiles + t) * p.splits + split) * (kTile * kTile));
+    out.keep(part + ((matrix * p.tiles + t) * p.splits + split) * (kR * kC));
     return;
   }
+  const T beta = (T)p.beta;
 #pragma unroll
-  for (int rt = 0; rt < out.RT; ++rt) {
+  for (int h = 0; h < out.RT / 2; ++h) {
     __syncthreads();
-    finish<T, kTile>(a, p, matrix, tr, tc, rt, out.acc[rt], S.out);
+#pragma unroll
+    for (int rt = 0; rt < 2; ++rt)
+#pragma unroll
+      for (int ct = 0; ct < out.CT; ++ct)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) S.out[out.wave() / 2 * 32 + rt * 16 + out.lane() % 16][out.column(ct) + i] = beta * out.acc[2 * h + rt][ct][i];
+    finish<T, kR, kC, 64>(a, p, matrix, tr * kR + h * 32, tc * kC, S.out);
   }
 }
 
-template <class T, int kTile>
+// 32 rows of a tile a workgroup
+template <class T, int kR, int kC>
 __global__ void __launch_bounds__(kProductThreads) k_orth_finish(OrthArgs a, Product p, int64_t first, const T* part) {
-  using Out = Results<T, kTile, kTile>;
-  __shared__ T tile[kStrip][kTile + 1];
-  const int rt = blockIdx.x % Out::RT, t = blockIdx.x / Out::RT % p.tiles;
-  const int64_t matrix = first + blockIdx.x / Out::RT / p.tiles;
+  using Out = Results<T, kR, kC>;
+  constexpr int kStrips = kR / 32;
+  __shared__ T tile[32][kC + 1];
+  const int strip = blockIdx.x % kStrips, t = blockIdx.x / kStrips % p.tiles;
+  const int64_t matrix = first + blockIdx.x / kStrips / p.tiles;
   int tr, tc;
-  tile_of<T, kTile>(p, t, tr, tc);
+  tile_of<kC>(p, t, tr, tc);
+  // of the product's waves the two that have these rows; a thread takes one of two tiles of 16 of them
+  const int half = strip / (kStrips / 2), h = strip % (kStrips / 2), rt = threadIdx.x / 128, thread = half * 128 + threadIdx.x % 128, lane = threadIdx.x % 64;
   typename Out::N::Vec acc[Out::CT] = {};
-  Out::add_up(part + (matrix * p.tiles + t) * p.splits * (kTile * kTile), p.splits, rt, acc);
-  finish<T, kTile>(a, p, matrix, tr, tc, rt, acc, tile);
+  Out::add_up(part + (matrix * p.tiles + t) * p.splits * (kR * kC) + ((2 * h + rt) * Out::CT * Out::kThreads + thread) * 4, p.splits, acc);
+  const T beta = (T)p.beta;
+#pragma unroll
+  for (int ct = 0; ct < Out::CT; ++ct)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) tile[rt * 16 + lane % 16][thread / 64 % 2 * (kC / 2) + ct * 16 + lane / 16 * 4 + i] = beta * acc[ct][i];
+  finish<T, kR, kC, 32>(a, p, matrix, tr * kR + half * (kR / 2) + h * 32, tc * kC, tile);
 }
 
 // ---- up to 128 rows of X --------------------------------------------------------------------------------------------------------
@@ -530,8 +562,7 @@ __global__ void __launch_bounds__((64 * kWaves), (kWaves / 4)) k_orth_step(OrthA
   Cols X;
   X.take(X_at + place * (kS * Cols::kWide));
   typename Cols::Gram A;
-#pragma unroll
-  for (int rt = 0; rt < Cols::Gram::RT; ++rt) Cols::Gram::add_up(A_from + matrix * parts * (kS * kS), parts, rt, A.acc[rt]);
+  A.add_all(A_from + matrix * parts * (kS * kS), parts);
   Cols::put(S, A);
   X.step(S, c0, c1, c2);
   if constexpr (kLast) {
@@ -601,7 +632,8 @@ struct Few {
 // The products of a step where X has many rows
 template <class T>
 struct Many {
-  bool large;                        // tiles of 128 x 128
+  bool large;                        // the least tiles are 128 rows of X high
+  int square_tile, tall, across;     // tiles of A and B, and of X
   int64_t s, l, square, wide;        // padded sizes, tiles of A (on and above the diagonal) and of X
   int a_splits, b_splits, x_splits;
   Many(int64_t batch, int64_t m, int64_t n) {
@@ -610,15 +642,22 @@ struct Many {
     const int64_t tile = large ? 128 : 64;
     s = (s0 + tile - 1) / tile * tile;
     l = (l0 + tile - 1) / tile * tile;
-    square = s / tile * (s / tile + 1) / 2;
-    wide = s / tile * (l / tile);
-    static const int per = getenv("ORTH_WANT") ? atoi(getenv("ORTH_WANT")) : 512;
-    auto splits = [&](int64_t tiles, int64_t terms) { return (int)std::max<int64_t>(1, std::min(terms / kStep / 4, per / (batch * tiles))); };
-    a_splits = splits(square, l);
-    b_splits = splits(square, s);
-    x_splits = splits(wide, s);
+    static const int sq = getenv("ORTH_SQ") ? atoi(getenv("ORTH_SQ")) : 128, xr = getenv("ORTH_XR") ? atoi(getenv("ORTH_XR")) : 128, xc = getenv("ORTH_XC") ? atoi(getenv("ORTH_XC")) : 128;
+    static const int per = getenv("ORTH_WANT") ? atoi(getenv("ORTH_WANT")) : 512, perx = getenv("ORTH_XWANT") ? atoi(getenv("ORTH_XWANT")) : 512;
+    square_tile = large ? sq : 64;
+    tall = large ? xr : 64;
+    across = large ? xc : 64;
+    square = s / square_tile * (s / square_tile + 1) / 2;
+    wide = s / tall * (l / across);
+    auto splits = [&](int64_t tiles, int64_t terms, int per) { return (int)std::max<int64_t>(1, std::min(terms / kStep / 4, per / (batch * tiles))); };
+    a_splits = splits(square, l, per);
+    b_splits = splits(square, s, per);
+    x_splits = splits(wide, s, perx);
   }
-  int64_t results() const { return (large ? 128 * 128 : 64 * 64) * std::max({square * (a_splits > 1 ? a_splits : 0), square * (b_splits > 1 ? b_splits : 0), wide * (x_splits > 1 ? x_splits : 0)}); }
+  int64_t results() const {
+    const int64_t a = (int64_t)square_tile * square_tile * square;
+    return std::max({a * (a_splits > 1 ? a_splits : 0), a * (b_splits > 1 ? b_splits : 0), (int64_t)tall * across * wide * (x_splits > 1 ? x_splits : 0)});
+  }
   size_t x_size() const { return s * l * Stored<T>::kBytes; }
   size_t a_size() const { return s * s * Stored<T>::kBytes; }
 };
@@ -634,14 +673,23 @@ size_t workspace_bytes(int64_t batch, int64_t m, int64_t n) {
   return up(batch * shares_of(m, n) * sizeof(double)) + 4 * up(batch * f.x_size()) + 2 * up(batch * f.a_size()) + up(batch * f.results() * sizeof(T));
 }
 
-template <class T, int kTile>
-hipError_t product(const OrthArgs& a, const Product& p, T* part, hipStream_t st) {
-  hipError_t e = in_launches(a.batch, (int64_t)p.tiles * p.splits, [&](int64_t first, dim3 grid) { k_orth_product<T, kTile><<<grid, kProductThreads, 0, st>>>(a, p, first, part); });
+template <class T, int kR, int kC>
+hipError_t product_of(const OrthArgs& a, const Product& p, T* part, hipStream_t st) {
+  hipError_t e = in_launches(a.batch, (int64_t)p.tiles * p.splits, [&](int64_t first, dim3 grid) { k_orth_product<T, kR, kC><<<grid, kProductThreads, 0, st>>>(a, p, first, part); });
   if (e != hipSuccess || p.splits == 1) return e;
-  return in_launches(a.batch, (int64_t)p.tiles * (kTile / 32), [&](int64_t first, dim3 grid) { k_orth_finish<T, kTile><<<grid, kProductThreads, 0, st>>>(a, p, first, part); });
+  return in_launches(a.batch, (int64_t)p.tiles * (kR / 32), [&](int64_t first, dim3 grid) { k_orth_finish<T, kR, kC><<<grid, kProductThreads, 0, st>>>(a, p, first, part); });
 }
 
-template <class T, int kTile>
+template <class T>
+hipError_t product(const OrthArgs& a, const Product& p, int rows, int columns, T* part, hipStream_t st) {
+  if constexpr (sizeof(T) == 4) {
+    if (rows == 128 && columns == 128) return product_of<T, 128, 128>(a, p, part, st);
+    if (rows == 128) return product_of<T, 128, 64>(a, p, part, st);
+  }
+  return product_of<T, 64, 64>(a, p, part, st);
+}
+
+template <class T>
 hipError_t many_rows(const OrthArgs& a, const double* coefficients, int steps, char* ws, hipStream_t st) {
   const Many<T> f(a.batch, a.m, a.n);
   const int shares = shares_of(a.m, a.n), s = (int)f.s, l = (int)f.l;
@@ -659,9 +707,9 @@ hipError_t many_rows(const OrthArgs& a, const double* coefficients, int steps, c
   e = in_launches(a.batch, blocks, [&](int64_t first, dim3 grid) { k_orth_start<T><<<grid, kProductThreads, 0, st>>>(a, first, (int)blocks, s, l, shares, part, X, XT); });
   for (int i = 0; i < steps && e == hipSuccess; ++i) {
     const double* c = coefficients + 3 * i;
-    e = product<T, kTile>(a, {X, X, nullptr, A, nullptr, s, s, l, (int)f.square, f.a_splits, 0, 1, true, false}, sums, st);
-    if (e == hipSuccess) e = product<T, kTile>(a, {A, A, A, B, nullptr, s, s, s, (int)f.square, f.b_splits, c[1], c[2], true, false}, sums, st);
-    if (e == hipSuccess) e = product<T, kTile>(a, {B, XT, X, other, other_t, s, l, s, (int)f.wide, f.x_splits, c[0], 1, false, i + 1 == steps}, sums, st);
+    e = product<T>(a, {X, X, nullptr, A, nullptr, s, s, l, (int)f.square, f.a_splits, 0, 1, true, false}, f.square_tile, f.square_tile, sums, st);
+    if (e == hipSuccess) e = product<T>(a, {A, A, A, B, nullptr, s, s, s, (int)f.square, f.b_splits, c[1], c[2], true, false}, f.square_tile, f.square_tile, sums, st);
+    if (e == hipSuccess) e = product<T>(a, {B, XT, X, other, other_t, s, l, s, (int)f.wide, f.x_splits, c[0], 1, false, i + 1 == steps}, f.tall, f.across, sums, st);
     std::swap(X, other);
     std::swap(XT, other_t);
   }
@@ -725,9 +773,7 @@ hipError_t orthogonalise(const OrthArgs& a, const double* coefficients, int step
       default: return go(std::integral_constant<int, 128>());
     }
   }
-  if constexpr (sizeof(T) == 4)
-    if (Many<T>(a.batch, a.m, a.n).large) return many_rows<T, 128>(a, coefficients, steps, ws, st);
-  return many_rows<T, 64>(a, coefficients, steps, ws, st);
+  return many_rows<T>(a, coefficients, steps, ws, st);
 }
 
 }  // namespace

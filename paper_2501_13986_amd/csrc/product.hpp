@@ -259,11 +259,36 @@ struct Results {
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) *(typename N::Vec*)(to + ((rt * CT + ct) * kThreads + (int)threadIdx.x) * 4) = acc[rt][ct];
+      for (int ct = 0; ct < CT; ++ct) __builtin_nontemporal_store(acc[rt][ct], (typename N::Vec*)(to + ((rt * CT + ct) * kThreads + (int)threadIdx.x) * 4));
   }
-  // the sum of tiles rt of `parts` such, in their order
-  static __device__ void add_up(const T* from, int parts, int rt, typename N::Vec (&to)[CT]) {
-    from += (rt * CT * kThreads + (int)threadIdx.x) * 4;
+  // the sum of `parts` such, in their order; sixteen loads on their way
+  __device__ void add_all(const T* from, int parts) {
+    constexpr int kAtOnce = RT * CT >= 16 ? 1 : 16 / (RT * CT);
+    from += (int)threadIdx.x * 4;
+    int p = 0;
+    for (; p + kAtOnce <= parts; p += kAtOnce) {
+      typename N::Vec v[kAtOnce][RT][CT];
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) v[j][rt][ct] = *(const typename N::Vec*)(from + (int64_t)(p + j) * (kR * kC) + (rt * CT + ct) * kThreads * 4);
+#pragma unroll
+      for (int j = 0; j < kAtOnce; ++j)
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) acc[rt][ct] += v[j][rt][ct];
+    }
+    for (; p < parts; ++p)
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) acc[rt][ct] += *(const typename N::Vec*)(from + (int64_t)p * (kR * kC) + (rt * CT + ct) * kThreads * 4);
+  }
+  // the same of one tile of rows, from a thread's own first number on
+  static __device__ void add_up(const T* from, int parts, typename N::Vec (&to)[CT]) {
 #pragma unroll 4
     for (int p = 0; p < parts; ++p)
 #pragma unroll
