@@ -5,7 +5,6 @@
 #pragma once
 
 #include <algorithm>
-#include <cstdlib>
 #include <type_traits>
 
 #include "orth.hpp"
@@ -198,37 +197,36 @@ struct Product {
   bool symmetric, last;
 };
 
-template <class T, int kR, int kC>
+template <class T, int kTile>
 union ProductLds {
   struct {
-    Operand<T, kR> R;
-    Operand<T, kC> C;
+    Operand<T, kTile> R, C;
   } in;
-  T out[64][kC + 1];      // rows of a tile that pass through LDS at a time: 32 of each half
+  T out[64][kTile + 1];      // rows of a tile that pass through LDS at a time: 32 of each half
   __device__ ProductLds() {}
 };
 
-template <int kC>
+template <int kTile>
 __device__ inline void tile_of(const Product& p, int t, int& tr, int& tc) {
   if (p.symmetric) {
     upper_tile(t, tr, tc);
   } else {
-    tr = t / (p.columns / kC);
-    tc = t % (p.columns / kC);
+    tr = t / (p.columns / kTile);
+    tc = t % (p.columns / kTile);
   }
 }
 
 // kRows rows of a tile, whose products (times beta) stand in LDS: the rows from r0 on, and with 64 those that are half a tile behind them
-template <class T, int kR, int kC, int kRows>
-__device__ inline void finish(const OrthArgs& a, const Product& p, int64_t matrix, int r0, int c0, T (&tile)[kRows][kC + 1]) {
+template <class T, int kTile, int kRows>
+__device__ inline void finish(const OrthArgs& a, const Product& p, int64_t matrix, int r0, int c0, T (&tile)[kRows][kTile + 1]) {
   const int64_t size = (int64_t)p.rows * p.columns * Stored<T>::kBytes;
   const T alpha = (T)p.alpha;
-  auto row = [&](int y) { return r0 + y / 32 * (kR / 2) + y % 32; };
+  auto row = [&](int y) { return r0 + y / 32 * (kTile / 2) + y % 32; };
   __syncthreads();
-  const bool add = p.alpha != 0, mirror = !p.symmetric || r0 / kR != c0 / kC;
+  const bool add = p.alpha != 0, mirror = !p.symmetric || r0 / kTile != c0 / kTile;
   if (add || !p.last) {
     const Stored<T> y(p.y + matrix * size, p.rows, p.columns), to(p.to + matrix * size, p.rows, p.columns);
-    for (int i = threadIdx.x; i < kRows * kC / 8; i += kProductThreads) {      // rows of 64 bytes one behind the other
+    for (int i = threadIdx.x; i < kRows * kTile / 8; i += kProductThreads) {      // rows of 64 bytes one behind the other
       const int r = i / 4 % kRows, k = i / (4 * kRows) * kStep + i % 4 * 8;
       T v[8], u[8];
 #pragma unroll
@@ -248,20 +246,20 @@ __device__ inline void finish(const OrthArgs& a, const Product& p, int64_t matri
   if (p.last) {
     T* to = (T*)a.out + matrix * a.stride_out;
     if (a.m > a.n) {
-      for (int i = threadIdx.x; i < kC * kRows; i += kProductThreads) {
+      for (int i = threadIdx.x; i < kTile * kRows; i += kProductThreads) {
         const int y = i % kRows, x = i / kRows;
         if (c0 + x < a.m && row(y) < a.n) to[(int64_t)(c0 + x) * a.ld_out + row(y)] = tile[y][x];
       }
     } else {
-      for (int i = threadIdx.x; i < kC * kRows; i += kProductThreads) {
-        const int y = i / kC, x = i % kC;
+      for (int i = threadIdx.x; i < kTile * kRows; i += kProductThreads) {
+        const int y = i / kTile, x = i % kTile;
         if (row(y) < a.m && c0 + x < a.n) to[(int64_t)row(y) * a.ld_out + c0 + x] = tile[y][x];
       }
     }
   } else if (mirror) {
     const Stored<T> to((p.symmetric ? p.to : p.to_t) + matrix * size, p.columns, p.rows);
-    for (int i = threadIdx.x; i < kRows * kC / 8; i += kProductThreads) {
-      const int c = i / 4 % kC, k = i / (4 * kC) * 32 + i % 4 * 8;
+    for (int i = threadIdx.x; i < kRows * kTile / 8; i += kProductThreads) {
+      const int c = i / 4 % kTile, k = i / (4 * kTile) * 32 + i % 4 * 8;
       T v[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] = tile[k + j][c];
@@ -270,34 +268,33 @@ __device__ inline void finish(const OrthArgs& a, const Product& p, int64_t matri
   }
 }
 
-template <class T, int kR, int kC>
+template <class T, int kTile>
 __global__ void __launch_bounds__(kProductThreads, 2) k_orth_product(OrthArgs a, Product p, int64_t first, T* part) {
-  __shared__ ProductLds<T, kR, kC> S;
+  __shared__ ProductLds<T, kTile> S;
   const unsigned block = on_one_die(blockIdx.x, gridDim.x);
   const int t = block % p.tiles, split = block / p.tiles % p.splits;
   const int64_t matrix = first + block / p.tiles / p.splits;
   int tr, tc;
-  tile_of<kC>(p, t, tr, tc);
+  tile_of<kTile>(p, t, tr, tc);
   const Stored<T> left(p.rows_at + matrix * p.rows * p.terms * Stored<T>::kBytes, p.rows, p.terms), right(p.columns_at + matrix * p.columns * p.terms * Stored<T>::kBytes, p.columns, p.terms);
   const int steps = p.terms / kStep, from = steps * split / p.splits, end = steps * (split + 1) / p.splits;
-  Copy<T, kR> rows;
-  Copy<T, kC> columns;
-  Results<T, kR, kC> out;
-  rows.fetch(left, tr * kR, from * kStep);
-  columns.fetch(right, tc * kC, from * kStep);
+  Copy<T, kTile> rows, columns;
+  Results<T, kTile, kTile> out;
+  rows.fetch(left, tr * kTile, from * kStep);
+  columns.fetch(right, tc * kTile, from * kStep);
   for (int k = from; k < end; ++k) {
     __syncthreads();
     rows.put(S.in.R);
     columns.put(S.in.C);
     __syncthreads();
     if (k + 1 < end) {
-      rows.fetch(left, tr * kR, (k + 1) * kStep);
-      columns.fetch(right, tc * kC, (k + 1) * kStep);
+      rows.fetch(left, tr * kTile, (k + 1) * kStep);
+      columns.fetch(right, tc * kTile, (k + 1) * kStep);
     }
     out.multiply(S.in.R, S.in.C);
   }
   if (p.splits > 1) {
-    out.keep(part + ((matrix * p.tiles + t) * p.splits + split) * (kR * kC));
+    out.keep(part + ((matrix * p.tiles + t) * p.splits + split) * (kTile * kTile));
     return;
   }
   const T beta = (T)p.beta;
@@ -310,30 +307,30 @@ __global__ void __launch_bounds__(kProductThreads, 2) k_orth_product(OrthArgs a,
       for (int ct = 0; ct < out.CT; ++ct)
 #pragma unroll
         for (int i = 0; i < 4; ++i) S.out[out.wave() / 2 * 32 + rt * 16 + out.lane() % 16][out.column(ct) + i] = beta * out.acc[2 * h + rt][ct][i];
-    finish<T, kR, kC, 64>(a, p, matrix, tr * kR + h * 32, tc * kC, S.out);
+    finish<T, kTile, 64>(a, p, matrix, tr * kTile + h * 32, tc * kTile, S.out);
   }
 }
 
 // 32 rows of a tile a workgroup
-template <class T, int kR, int kC>
+template <class T, int kTile>
 __global__ void __launch_bounds__(kProductThreads) k_orth_finish(OrthArgs a, Product p, int64_t first, const T* part) {
-  using Out = Results<T, kR, kC>;
-  constexpr int kStrips = kR / 32;
-  __shared__ T tile[32][kC + 1];
+  using Out = Results<T, kTile, kTile>;
+  constexpr int kStrips = kTile / 32;
+  __shared__ T tile[32][kTile + 1];
   const int strip = blockIdx.x % kStrips, t = blockIdx.x / kStrips % p.tiles;
   const int64_t matrix = first + blockIdx.x / kStrips / p.tiles;
   int tr, tc;
-  tile_of<kC>(p, t, tr, tc);
+  tile_of<kTile>(p, t, tr, tc);
   // of the product's waves the two that have these rows; a thread takes one of two tiles of 16 of them
   const int half = strip / (kStrips / 2), h = strip % (kStrips / 2), rt = threadIdx.x / 128, thread = half * 128 + threadIdx.x % 128, lane = threadIdx.x % 64;
   typename Out::N::Vec acc[Out::CT] = {};
-  Out::add_up(part + (matrix * p.tiles + t) * p.splits * (kR * kC) + ((2 * h + rt) * Out::CT * Out::kThreads + thread) * 4, p.splits, acc);
+  Out::add_up(part + (matrix * p.tiles + t) * p.splits * (kTile * kTile) + ((2 * h + rt) * Out::CT * Out::kThreads + thread) * 4, p.splits, acc);
   const T beta = (T)p.beta;
 #pragma unroll
   for (int ct = 0; ct < Out::CT; ++ct)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) tile[rt * 16 + lane % 16][thread / 64 % 2 * (kC / 2) + ct * 16 + lane / 16 * 4 + i] = beta * acc[ct][i];
-  finish<T, kR, kC, 32>(a, p, matrix, tr * kR + half * (kR / 2) + h * 32, tc * kC, tile);
+    for (int i = 0; i < 4; ++i) tile[rt * 16 + lane % 16][thread / 64 % 2 * (kTile / 2) + ct * 16 + lane / 16 * 4 + i] = beta * acc[ct][i];
+  finish<T, kTile, 32>(a, p, matrix, tr * kTile + half * (kTile / 2) + h * 32, tc * kTile, tile);
 }
 
 // ---- up to 128 rows of X --------------------------------------------------------------------------------------------------------
@@ -629,34 +626,33 @@ struct Few {
   size_t sum_size() const { return chunks > kMostShares ? rows * rows : 0; }
 };
 
-// The products of a step where X has many rows
+// The products of a step where X has many rows.  Tiles of 128 x 128 read half as much for a product, tiles of 64 x 64 leave less unfilled: X of 1152 x 2048 fp32 49 us a
+// product with the former (splits added up), 54 with the latter, 800 x 800 25 and 22; A and its square of 1600 rows 42 and 44 us, of 1152 33 and 27, of 500 (three of
+// them) 19 and 13.
 template <class T>
 struct Many {
-  bool large;                        // the least tiles are 128 rows of X high
-  int square_tile, tall, across;     // tiles of A and B, and of X
+  int square_tile, x_tile;           // of A and B, of X
   int64_t s, l, square, wide;        // padded sizes, tiles of A (on and above the diagonal) and of X
   int a_splits, b_splits, x_splits;
   Many(int64_t batch, int64_t m, int64_t n) {
     const int64_t s0 = std::min(m, n), l0 = std::max(m, n);
-    large = sizeof(T) == 4 && s0 > 384;
-    const int64_t tile = large ? 128 : 64;
-    s = (s0 + tile - 1) / tile * tile;
-    l = (l0 + tile - 1) / tile * tile;
-    static const int sq = getenv("ORTH_SQ") ? atoi(getenv("ORTH_SQ")) : 128, xr = getenv("ORTH_XR") ? atoi(getenv("ORTH_XR")) : 128, xc = getenv("ORTH_XC") ? atoi(getenv("ORTH_XC")) : 128;
-    static const int per = getenv("ORTH_WANT") ? atoi(getenv("ORTH_WANT")) : 512, perx = getenv("ORTH_XWANT") ? atoi(getenv("ORTH_XWANT")) : 512;
-    square_tile = large ? sq : 64;
-    tall = large ? xr : 64;
-    across = large ? xc : 64;
+    square_tile = sizeof(T) == 4 && s0 >= 1536 ? 128 : 64;
+    x_tile = sizeof(T) == 4 && s0 >= 1024 ? 128 : 64;
+    s = (s0 + x_tile - 1) / x_tile * x_tile;
+    l = (l0 + x_tile - 1) / x_tile * x_tile;
     square = s / square_tile * (s / square_tile + 1) / 2;
-    wide = s / tall * (l / across);
-    auto splits = [&](int64_t tiles, int64_t terms, int per) { return (int)std::max<int64_t>(1, std::min(terms / kStep / 4, per / (batch * tiles))); };
-    a_splits = splits(square, l, per);
-    b_splits = splits(square, s, per);
-    x_splits = splits(wide, s, perx);
+    wide = s / x_tile * (l / x_tile);
+    // splits of the terms, four steps of 32 or more each, up to three workgroups of small tiles a compute unit (1152 rows: 27 us a product of A; with two 31) or two of large ones
+    auto splits = [&](int tile, int64_t tiles, int64_t terms) {
+      return (int)std::max<int64_t>(1, std::min(terms / kStep / 4, (tile == 64 && sizeof(T) == 4 ? 768 : 512) / (batch * tiles)));
+    };
+    a_splits = splits(square_tile, square, l);
+    b_splits = splits(square_tile, square, s);
+    x_splits = splits(x_tile, wide, s);
   }
   int64_t results() const {
-    const int64_t a = (int64_t)square_tile * square_tile * square;
-    return std::max({a * (a_splits > 1 ? a_splits : 0), a * (b_splits > 1 ? b_splits : 0), (int64_t)tall * across * wide * (x_splits > 1 ? x_splits : 0)});
+    const int64_t a = (int64_t)square_tile * square_tile * square, x = (int64_t)x_tile * x_tile * wide;
+    return std::max({a * (a_splits > 1 ? a_splits : 0), a * (b_splits > 1 ? b_splits : 0), x * (x_splits > 1 ? x_splits : 0)});
   }
   size_t x_size() const { return s * l * Stored<T>::kBytes; }
   size_t a_size() const { return s * s * Stored<T>::kBytes; }
@@ -673,20 +669,18 @@ size_t workspace_bytes(int64_t batch, int64_t m, int64_t n) {
   return up(batch * shares_of(m, n) * sizeof(double)) + 4 * up(batch * f.x_size()) + 2 * up(batch * f.a_size()) + up(batch * f.results() * sizeof(T));
 }
 
-template <class T, int kR, int kC>
+template <class T, int kTile>
 hipError_t product_of(const OrthArgs& a, const Product& p, T* part, hipStream_t st) {
-  hipError_t e = in_launches(a.batch, (int64_t)p.tiles * p.splits, [&](int64_t first, dim3 grid) { k_orth_product<T, kR, kC><<<grid, kProductThreads, 0, st>>>(a, p, first, part); });
+  hipError_t e = in_launches(a.batch, (int64_t)p.tiles * p.splits, [&](int64_t first, dim3 grid) { k_orth_product<T, kTile><<<grid, kProductThreads, 0, st>>>(a, p, first, part); });
   if (e != hipSuccess || p.splits == 1) return e;
-  return in_launches(a.batch, (int64_t)p.tiles * (kR / 32), [&](int64_t first, dim3 grid) { k_orth_finish<T, kR, kC><<<grid, kProductThreads, 0, st>>>(a, p, first, part); });
+  return in_launches(a.batch, (int64_t)p.tiles * (kTile / 32), [&](int64_t first, dim3 grid) { k_orth_finish<T, kTile><<<grid, kProductThreads, 0, st>>>(a, p, first, part); });
 }
 
 template <class T>
-hipError_t product(const OrthArgs& a, const Product& p, int rows, int columns, T* part, hipStream_t st) {
-  if constexpr (sizeof(T) == 4) {
-    if (rows == 128 && columns == 128) return product_of<T, 128, 128>(a, p, part, st);
-    if (rows == 128) return product_of<T, 128, 64>(a, p, part, st);
-  }
-  return product_of<T, 64, 64>(a, p, part, st);
+hipError_t product(const OrthArgs& a, const Product& p, int tile, T* part, hipStream_t st) {
+  if constexpr (sizeof(T) == 4)
+    if (tile == 128) return product_of<T, 128>(a, p, part, st);
+  return product_of<T, 64>(a, p, part, st);
 }
 
 template <class T>
@@ -707,9 +701,9 @@ hipError_t many_rows(const OrthArgs& a, const double* coefficients, int steps, c
   e = in_launches(a.batch, blocks, [&](int64_t first, dim3 grid) { k_orth_start<T><<<grid, kProductThreads, 0, st>>>(a, first, (int)blocks, s, l, shares, part, X, XT); });
   for (int i = 0; i < steps && e == hipSuccess; ++i) {
     const double* c = coefficients + 3 * i;
-    e = product<T>(a, {X, X, nullptr, A, nullptr, s, s, l, (int)f.square, f.a_splits, 0, 1, true, false}, f.square_tile, f.square_tile, sums, st);
-    if (e == hipSuccess) e = product<T>(a, {A, A, A, B, nullptr, s, s, s, (int)f.square, f.b_splits, c[1], c[2], true, false}, f.square_tile, f.square_tile, sums, st);
-    if (e == hipSuccess) e = product<T>(a, {B, XT, X, other, other_t, s, l, s, (int)f.wide, f.x_splits, c[0], 1, false, i + 1 == steps}, f.tall, f.across, sums, st);
+    e = product<T>(a, {X, X, nullptr, A, nullptr, s, s, l, (int)f.square, f.a_splits, 0, 1, true, false}, f.square_tile, sums, st);
+    if (e == hipSuccess) e = product<T>(a, {A, A, A, B, nullptr, s, s, s, (int)f.square, f.b_splits, c[1], c[2], true, false}, f.square_tile, sums, st);
+    if (e == hipSuccess) e = product<T>(a, {B, XT, X, other, other_t, s, l, s, (int)f.wide, f.x_splits, c[0], 1, false, i + 1 == steps}, f.x_tile, sums, st);
     std::swap(X, other);
     std::swap(XT, other_t);
   }
@@ -761,7 +755,7 @@ hipError_t orthogonalise(const OrthArgs& a, const double* coefficients, int step
       constexpr int kS = decltype(rows)::value;
       if constexpr (sizeof(T) == 4)
         if (f.wide == 128) {
-          if constexpr (kS % 64 == 0) return getenv("ORTH_4") ? few_rows<T, kS, 2, 4>(a, coefficients, steps, ws, st) : few_rows<T, kS, 1, 8>(a, coefficients, steps, ws, st);
+          if constexpr (kS % 64 == 0) return few_rows<T, kS, 1, 8>(a, coefficients, steps, ws, st);
           else return few_rows<T, kS, 2, 4>(a, coefficients, steps, ws, st);
         }
       return few_rows<T, kS, 1, 4>(a, coefficients, steps, ws, st);
