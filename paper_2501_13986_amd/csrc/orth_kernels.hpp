@@ -533,33 +533,66 @@ __global__ void __launch_bounds__((64 * kWaves), (kWaves / 4)) k_orth_whole(Orth
   X.store((T*)a.out + matrix * a.stride_out, a.ld_out, s, l, 0, turned);
 }
 
+// The start leaves each chunk of X multiplied by the power of two that brings its size near one, so that no product of it overflows or is lost, with the sum of its squares: the
+// size of all of X is known when the first step begins, which multiplies X once (as if G were) and the shares of A by the squares.
+struct Chunk {
+  double squares, power;
+};
+
+// 1 / (|G| + eps), by all lanes of a wave
+__device__ inline double scale_of(const Chunk* chunk, int chunks, double eps) {
+  double v = 0;
+  for (int i = (int)threadIdx.x & 63; i < (chunks + 63) / 64 * 64; i += 64) v += i < chunks ? chunk[i < chunks ? i : 0].squares : 0;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+  return 1.0 / (sqrt(v) + eps);
+}
+
 // The first share of A [matrix][chunk][kS * kS] and X [matrix][chunk][kS * columns], in the order of the registers
 template <class T, int kS, int NT, int kWaves>
-__global__ void __launch_bounds__((64 * kWaves), (kWaves / 4)) k_orth_begin(OrthArgs a, int64_t first, int chunks, int shares, const double* part, T* X_to, T* A_to) {
+__global__ void __launch_bounds__((64 * kWaves), (kWaves / 4)) k_orth_begin(OrthArgs a, int64_t first, int chunks, Chunk* chunk, T* X_to, T* A_to) {
   using Cols = Columns<T, kS, NT, kWaves>;
   __shared__ typename Cols::Lds S;
+  __shared__ double sums[kWaves];
   const int64_t matrix = first + blockIdx.x / chunks, place = matrix * chunks + blockIdx.x % chunks;
   const bool turned = a.m > a.n;
   const int s = (int)(turned ? a.n : a.m), l = (int)(turned ? a.m : a.n);
   Cols X;
   X.load((const T*)a.g + matrix * a.stride_g, a.ld_g, s, l, blockIdx.x % chunks * Cols::kWide, turned);
-  X.scale(scale_of(part + matrix * shares, shares, a.eps));
+  const double squares = sum_of_all<kWaves>(X.squares(), sums);
+  const double power = squares > 0 && squares < __builtin_inf() ? ldexp(1.0, -ilogb(sqrt(squares))) : 1.0;
+  X.scale(power);
   X.keep(X_to + place * (kS * Cols::kWide));
   typename Cols::Gram A;
   X.gram(S, A);
   A.keep(A_to + place * (kS * kS));
+  if (threadIdx.x == 0) chunk[place] = {squares, power};
 }
 
-// A step.  parts: how many shares of A there are a matrix
+// A step.  parts: how many shares of A there are a matrix; chunk: of the first step
 template <class T, int kS, int NT, int kWaves, bool kLast>
-__global__ void __launch_bounds__((64 * kWaves), (kWaves / 4)) k_orth_step(OrthArgs a, int64_t first, int chunks, int parts, T c0, T c1, T c2, T* X_at, const T* A_from, T* A_to) {
+__global__ void __launch_bounds__((64 * kWaves), (kWaves / 4)) k_orth_step(OrthArgs a, int64_t first, int chunks, int parts, T c0, T c1, T c2, const Chunk* chunk, T* X_at, const T* A_from, T* A_to) {
   using Cols = Columns<T, kS, NT, kWaves>;
   __shared__ typename Cols::Lds S;
   const int64_t matrix = first + blockIdx.x / chunks, place = matrix * chunks + blockIdx.x % chunks;
   Cols X;
   X.take(X_at + place * (kS * Cols::kWide));
   typename Cols::Gram A;
-  A.add_all(A_from + matrix * parts * (kS * kS), parts);
+  A_from += matrix * parts * (kS * kS);
+  if (chunk) {
+    const double scale = scale_of(chunk + matrix * chunks, chunks, a.eps);
+    X.scale(scale / chunk[place].power);
+    if (parts == chunks) {
+      A.add_all(A_from, parts, [&](int p) {
+        const double f = scale / chunk[matrix * chunks + p].power;
+        return (T)(f * f);
+      });
+    } else {
+      A.add_all(A_from, parts, [](int) { return T(1); });
+    }
+  } else {
+    A.add_all(A_from, parts, [](int) { return T(1); });
+  }
   Cols::put(S, A);
   X.step(S, c0, c1, c2);
   if constexpr (kLast) {
@@ -574,19 +607,24 @@ __global__ void __launch_bounds__((64 * kWaves), (kWaves / 4)) k_orth_step(OrthA
   }
 }
 
-// to [matrix][size] = sums of from [matrix][parts][size], in their order
+// to [matrix][size] = sums of from [matrix][parts][size], in their order; chunk: of the first step
 template <class T>
-__global__ void __launch_bounds__(kProductThreads) k_orth_join(int64_t first, int blocks, int parts, int size, const T* from, T* to) {
+__global__ void __launch_bounds__(kProductThreads) k_orth_join(OrthArgs a, int64_t first, int blocks, int parts, int size, const Chunk* chunk, const T* from, T* to) {
   const int64_t matrix = first + blockIdx.x / blocks;
   const int i = blockIdx.x % blocks * kProductThreads + threadIdx.x;
-  if (i >= size) return;
   from += matrix * parts * size + i;
+  const double scale = chunk ? scale_of(chunk + matrix * parts, parts, a.eps) : 0;
+  auto factor = [&](int p) {
+    const double f = chunk ? scale / chunk[matrix * parts + p].power : 1;
+    return (T)(f * f);
+  };
+  if (i >= size) return;
   T v[8] = {};
   int p = 0;
   for (; p + 8 <= parts; p += 8)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] += from[(int64_t)(p + j) * size];
-  for (; p < parts; ++p) v[0] += from[(int64_t)p * size];
+    for (int j = 0; j < 8; ++j) v[j] += factor(p + j) * from[(int64_t)(p + j) * size];
+  for (; p < parts; ++p) v[0] += factor(p) * from[(int64_t)p * size];
   to[matrix * size + i] = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
 }
 
@@ -663,7 +701,7 @@ size_t workspace_bytes(int64_t batch, int64_t m, int64_t n) {
   if (std::min(m, n) <= kMostRows) {
     const Few f(m, n, sizeof(T) == 8);
     if (f.chunks == 1) return 0;
-    return up(batch * shares_of(m, n) * sizeof(double)) + up(batch * f.x_size() * sizeof(T)) + 2 * up(batch * f.a_size() * sizeof(T)) + up(batch * f.sum_size() * sizeof(T));
+    return up(batch * f.chunks * sizeof(Chunk)) + up(batch * f.x_size() * sizeof(T)) + 2 * up(batch * f.a_size() * sizeof(T)) + up(batch * f.sum_size() * sizeof(T));
   }
   const Many<T> f(batch, m, n);
   return up(batch * shares_of(m, n) * sizeof(double)) + 4 * up(batch * f.x_size()) + 2 * up(batch * f.a_size()) + up(batch * f.results() * sizeof(T));
@@ -718,29 +756,28 @@ hipError_t few_rows(const OrthArgs& a, const double* coefficients, int steps, ch
     for (int i = 0; i < 3 * steps; ++i) schedule.c[i / 3][i % 3] = coefficients[i];
     return in_launches(a.batch, 1, [&](int64_t first, dim3 grid) { k_orth_whole<T, kS, NT, kWaves><<<grid, 64 * kWaves, 0, st>>>(a, first, steps, schedule); });
   }
-  const int shares = shares_of(a.m, a.n), chunks = (int)f.chunks;
-  double* part = (double*)ws;
-  T* X = (T*)(ws + up(a.batch * shares * sizeof(double)));
+  const int chunks = (int)f.chunks;
+  Chunk* chunk = (Chunk*)ws;
+  T* X = (T*)(ws + up(a.batch * chunks * sizeof(Chunk)));
   T* A = (T*)((char*)X + up(a.batch * f.x_size() * sizeof(T)));
   T* next = (T*)((char*)A + up(a.batch * f.a_size() * sizeof(T)));
   T* sum = (T*)((char*)next + up(a.batch * f.a_size() * sizeof(T)));
-  hipError_t e = in_launches(a.batch, shares, [&](int64_t first, dim3 grid) { k_orth_squares<T><<<grid, kProductThreads, 0, st>>>(a, first, shares, part); });
-  if (e != hipSuccess) return e;
-  e = in_launches(a.batch, chunks, [&](int64_t first, dim3 grid) { k_orth_begin<T, kS, NT, kWaves><<<grid, 64 * kWaves, 0, st>>>(a, first, chunks, shares, part, X, A); });
+  hipError_t e = in_launches(a.batch, chunks, [&](int64_t first, dim3 grid) { k_orth_begin<T, kS, NT, kWaves><<<grid, 64 * kWaves, 0, st>>>(a, first, chunks, chunk, X, A); });
   for (int i = 0; i < steps && e == hipSuccess; ++i) {
     const double* c = coefficients + 3 * i;
-    const T *from = A;
+    const T* from = A;
+    const Chunk* start = i ? nullptr : chunk;
     int parts = chunks;
     if (chunks > kMostShares) {
       constexpr int kBlocks = kS * kS / kProductThreads;
-      e = in_launches(a.batch, kBlocks, [&](int64_t first, dim3 grid) { k_orth_join<T><<<grid, kProductThreads, 0, st>>>(first, kBlocks, chunks, kS * kS, A, sum); });
+      e = in_launches(a.batch, kBlocks, [&](int64_t first, dim3 grid) { k_orth_join<T><<<grid, kProductThreads, 0, st>>>(a, first, kBlocks, chunks, kS * kS, start, A, sum); });
       if (e != hipSuccess) break;
       from = sum;
       parts = 1;
     }
     e = in_launches(a.batch, chunks, [&](int64_t first, dim3 grid) {
-      if (i + 1 < steps) k_orth_step<T, kS, NT, kWaves, false><<<grid, 64 * kWaves, 0, st>>>(a, first, chunks, parts, (T)c[0], (T)c[1], (T)c[2], X, from, next);
-      else k_orth_step<T, kS, NT, kWaves, true><<<grid, 64 * kWaves, 0, st>>>(a, first, chunks, parts, (T)c[0], (T)c[1], (T)c[2], X, from, next);
+      if (i + 1 < steps) k_orth_step<T, kS, NT, kWaves, false><<<grid, 64 * kWaves, 0, st>>>(a, first, chunks, parts, (T)c[0], (T)c[1], (T)c[2], start, X, from, next);
+      else k_orth_step<T, kS, NT, kWaves, true><<<grid, 64 * kWaves, 0, st>>>(a, first, chunks, parts, (T)c[0], (T)c[1], (T)c[2], start, X, from, next);
     });
     std::swap(A, next);
   }

@@ -261,8 +261,9 @@ struct Results {
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) __builtin_nontemporal_store(acc[rt][ct], (typename N::Vec*)(to + ((rt * CT + ct) * kThreads + (int)threadIdx.x) * 4));
   }
-  // the sum of `parts` such, in their order; sixteen loads on their way
-  __device__ void add_all(const T* from, int parts) {
+  // the sum of `parts` such times factor(part), in their order; sixteen loads on their way
+  template <class F>
+  __device__ void add_all(const T* from, int parts, F factor) {
     constexpr int kAtOnce = RT * CT >= 16 ? 1 : 16 / (RT * CT);
     from += (int)threadIdx.x * 4;
     int p = 0;
@@ -275,17 +276,21 @@ struct Results {
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) v[j][rt][ct] = *(const typename N::Vec*)(from + (int64_t)(p + j) * (kR * kC) + (rt * CT + ct) * kThreads * 4);
 #pragma unroll
-      for (int j = 0; j < kAtOnce; ++j)
+      for (int j = 0; j < kAtOnce; ++j) {
+        const T f = factor(p + j);
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-          for (int ct = 0; ct < CT; ++ct) acc[rt][ct] += v[j][rt][ct];
+          for (int ct = 0; ct < CT; ++ct) acc[rt][ct] += f * v[j][rt][ct];
+      }
     }
-    for (; p < parts; ++p)
+    for (; p < parts; ++p) {
+      const T f = factor(p);
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) acc[rt][ct] += *(const typename N::Vec*)(from + (int64_t)p * (kR * kC) + (rt * CT + ct) * kThreads * 4);
+        for (int ct = 0; ct < CT; ++ct) acc[rt][ct] += f * *(const typename N::Vec*)(from + (int64_t)p * (kR * kC) + (rt * CT + ct) * kThreads * 4);
+    }
   }
   // the same of one tile of rows, from a thread's own first number on
   static __device__ void add_up(const T* from, int parts, typename N::Vec (&to)[CT]) {
