@@ -41,8 +41,8 @@ cgtp_status check_numbers(std::initializer_list<const void*> data, int32_t dtype
 cgtp_status check_orth(int64_t batch, int64_t m, int64_t n, int32_t dtype) {
   if (dtype != CGTP_F32 && dtype != CGTP_F64) return fail(CGTP_EINVAL, "dtype must be CGTP_F32 or CGTP_F64");
   if (batch < 0 || m <= 0 || n <= 0) return fail(CGTP_EINVAL, "batch must not be negative, m and n must be positive");
-  if (batch > INT32_MAX || m > INT32_MAX / n || batch > ((int64_t)1 << 40) / (m * n))
-    return fail(CGTP_EUNSUPPORTED, "batch and m n must be below 2^31, batch m n at most 2^40");
+  if (batch > INT32_MAX || m >= 1 << 22 || n >= 1 << 22 || m > INT32_MAX / n || batch > ((int64_t)1 << 40) / (m * n))
+    return fail(CGTP_EUNSUPPORTED, "m and n must be below 2^22, batch and m n below 2^31, batch m n at most 2^40");
   return CGTP_OK;
 }
 
@@ -116,9 +116,9 @@ cgtp_status orthogonalise(const void* g, void* out, int64_t batch, int64_t m, in
   if (s != CGTP_OK) return s;
   if (ld_g < n || ld_out < n) return fail(CGTP_EINVAL, "a row stride is smaller than its row");
   if (stride_g < 0 || stride_out < 0) return fail(CGTP_EINVAL, "strides of matrices must not be negative");
-  if (ld_g > ((int64_t)1 << 40) / m || ld_out > ((int64_t)1 << 40) / m || stride_g > ((int64_t)1 << 60) / std::max<int64_t>(batch, 1) ||
+  if (ld_g >= 1 << 22 || ld_out >= 1 << 22 || stride_g > ((int64_t)1 << 60) / std::max<int64_t>(batch, 1) ||
       stride_out > ((int64_t)1 << 60) / std::max<int64_t>(batch, 1))
-    return fail(CGTP_EUNSUPPORTED, "strides too large");
+    return fail(CGTP_EUNSUPPORTED, "row strides must be below 2^22, strides of matrices times batch below 2^60");
   // one behind the other, or side by side in wide rows
   if (batch > 1 && stride_out < (m - 1) * ld_out + n && (stride_out < n || ld_out < (batch - 1) * stride_out + n)) return fail(CGTP_EINVAL, "matrices of out overlap");
   if (steps < 1 || steps > 64) return fail(CGTP_EINVAL, "steps must be from 1 to 64");

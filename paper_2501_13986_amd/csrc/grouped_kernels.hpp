@@ -501,6 +501,7 @@ hipError_t in_launches(int64_t ids, int64_t tiles, F f) {
   return hipSuccess;
 }
 
+// columns of a tile of gW, which is 64 rows high: fp32 with 128 rows, two workgroups a compute unit instead of three, 20 000 x 7 x 128 x 128 49 us for 46, 30 000 x 300 x 300 72 for 60
 template <class T>
 constexpr int kTile = sizeof(T) == 4 ? 128 : 64;
 
@@ -540,23 +541,20 @@ hipError_t launch_rows(const GroupedArgs& a, hipStream_t st) {
   if ((kBack ? a.d_out : a.d_in) <= kMostTerms && in_reach(rows, std::max(kBack ? a.ld_gout : a.ld_x, kBack ? a.ld_gx : a.ld_out), sizeof(T))) return launch_few_terms<T, kBack>(a, st);
   const int64_t n = kBack ? a.d_in : a.d_out, lines = a.rows * a.comps;
   const bool whole = a.d_in % 4 == 0 && a.d_out % 4 == 0, near = in_reach(rows, kBack ? a.ld_gout : a.ld_x, sizeof(T)) && in_reach(a.d_in, a.d_out, sizeof(T));
-  auto go = [&](auto tall, auto wide, auto whole_, auto far) {
-    constexpr int kR = decltype(tall)::value, kC = decltype(wide)::value;
-    const int64_t tiles = (n + kC - 1) / kC;
+  const int64_t tiles = (n + 63) / 64;
+  auto go = [&](auto tall, auto whole_, auto far) {
+    constexpr int kR = decltype(tall)::value;
     return in_launches(lines / kR + a.groups, tiles, [&](int64_t first, dim3 grid) {
-      k_grouped_rows<T, kR, kC, decltype(whole_)::value, kBack, decltype(far)::value><<<grid, kProductThreads, 0, st>>>(a, first, (int)tiles);
+      k_grouped_rows<T, kR, 64, decltype(whole_)::value, kBack, decltype(far)::value><<<grid, kProductThreads, 0, st>>>(a, first, (int)tiles);
     });
   };
+  // tiles of half the lines where that fills compute units (fp64, 2503 x 301 -> 96: 17 us for 32; many lines, fp32 160 710 x 2176 -> 64: 343 us, with half 366, with 128
+  // columns of twice the registers no faster: 30 000 x 300 -> 300 47 us and 56)
   auto size = [&](auto whole_, auto far) {
-    constexpr int kAll = kTile<T>;
-    using Tall = std::integral_constant<int, kAll>;
-    using Half = std::integral_constant<int, kAll / 2>;
-    using Narrow = std::integral_constant<int, 64>;
-    // tiles of half the lines where there are fewer than two workgroups a compute unit
-    const bool half = !decltype(far)::value && lines / kAll * ((n + kAll - 1) / kAll) < 512;
+    constexpr int kR = sizeof(T) == 4 ? 128 : 64;
     if constexpr (!decltype(far)::value)
-      if (half) return go(Half(), Narrow(), whole_, far);
-    return n > 64 ? go(Tall(), Tall(), whole_, far) : go(Tall(), Narrow(), whole_, far);
+      if (lines / kR * tiles < 512) return go(std::integral_constant<int, kR / 2>(), whole_, far);
+    return go(std::integral_constant<int, kR>(), whole_, far);
   };
   if (!near) return size(std::false_type(), std::true_type());
   return whole ? size(std::true_type(), std::false_type()) : size(std::false_type(), std::false_type());
@@ -569,10 +567,8 @@ template <class T>
 struct Chunks {
   int64_t row_tiles, column_tiles, count, slots;      // chunks, partial sums
   int shift = 20;                                     // positions of a chunk
-  bool narrow;                                        // 64 rows of gW a workgroup
   Chunks(int64_t rows, int64_t K, int64_t n, int64_t comps) {
-    narrow = sizeof(T) == 8 || K <= 64;
-    row_tiles = (K + (narrow ? 63 : 127)) / (narrow ? 64 : 128);
+    row_tiles = (K + 63) / 64;
     column_tiles = (n + kTile<T> - 1) / kTile<T>;
     // 256 lines a chunk are few enough for partial sums to cost little (20 000 x 7 x 128 x 128: 60 us with 256 lines, 68 with 128); fewer where compute units are without work
     auto workgroups = [&]() { return (rows >> shift) * row_tiles * column_tiles; };
@@ -608,7 +604,7 @@ hipError_t backward(const GroupedArgs& a, char* ws, hipStream_t st) {
   if (e != hipSuccess) return e;
   const Chunks<T> c(a.rows, K, n, a.comps);
   T *part = (T*)ws, *part_b = (T*)(ws + up(c.slots * K * n * sizeof(T)));
-  e = c.narrow ? launch_weights<T, 64, kTile<T>>(a, c, part, part_b, st) : launch_weights<T, kTile<T>, kTile<T>>(a, c, part, part_b, st);
+  e = launch_weights<T, 64, kTile<T>>(a, c, part, part_b, st);
   if (e != hipSuccess || c.slots == 0) return e;
   // most chunks have nothing to add up, so that they get few workgroups
   const bool of_groups = a.groups <= c.count - 1, wide = n % 4 == 0 && aligned16(a.gW) && aligned16(a.gb);

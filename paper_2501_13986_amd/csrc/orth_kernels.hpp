@@ -346,31 +346,58 @@ constexpr int kMostRows = 128;
 // the place of row r among 32 terms of results
 __device__ inline int place(int r) { return r % 16 / 4 * 8 + r / 16 * 4 + r % 4; }
 
+// waves a SIMD whose registers are left: two where half of the registers are enough, so that none of their values are moved about
+template <class T, int kS, int kWaves>
+constexpr int kOrthWaves = kWaves == 8 || sizeof(T) == 4 || kS <= 64 ? 2 : 1;
+
 template <class T, int kS, int NT, int kWaves>
 struct Columns {
   using N = Num<T>;
   static constexpr int kTiles = kS / 16, kWide = 16 * NT * kWaves, kSlices = (kS > kWide ? kS : kWide) / 32, kThreads = 64 * kWaves;
   using Lds = Operand<T, kS, kApart>[kSlices];
-  using Gram = Results<T, kS, kS, 2, kWaves / 2>;
+  // A: 2 x (3 or kWaves / 2) of the waves
+  static constexpr int kGramAcross = kS % (kWaves * 8) == 0 ? kWaves / 2 : 3;
+  using Gram = Results<T, kS, kS, 2, kGramAcross>;
+  static __device__ bool forms_gram() { return kGramAcross * 2 == kWaves || Gram::wave() < kGramAcross * 2; }
   typename N::Vec x[kTiles][NT];
 
   static __device__ int lane() { return (int)threadIdx.x & 63; }
   static __device__ int column(int j) { return (int)(threadIdx.x / 64) * (16 * NT) + lane() % 16 * NT + j; }
   static __device__ int row(int t) { return t * 16 + lane() / 16 * 4; }      // the first of four
 
-  // columns c0 .. of the matrix at g (transposed: it has them as rows), as they are; zero outside
+  // columns c0 .. of the matrix at g (transposed: it has them as rows), as they are; zero outside.  Through descriptors of 16 of its rows (strides are below 2^22), so that no
+  // lane is masked off.
   __device__ void load(const T* g, int64_t ld, int s, int l, int c0, bool turned) {
-#pragma unroll
-    for (int j = 0; j < NT; ++j) {
-      const int c = c0 + column(j), cc = c < l ? c : 0;
+    constexpr int e = sizeof(T);
+    auto get = [](Buffer B, unsigned at) {
+      if constexpr (e == 4) return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b32(B, at, 0, 0));
+      else return __builtin_bit_cast(T, __builtin_amdgcn_raw_buffer_load_b64(B, at, 0, 0));
+    };
+    if (turned) {
+      const int first = c0 + Gram::wave() * (16 * NT), have = l - first < 16 * NT ? l - first : 16 * NT;
+      const Buffer B = buffer_of(g + (have > 0 ? first : 0) * ld, have > 0 ? ((have - 1) * ld + s) * e : 0);
 #pragma unroll
       for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = row(t) + i, rr = r < s ? r : 0;
-          const T v = turned ? g[cc * ld + rr] : g[rr * ld + cc];
-          x[t][j][i] = c < l && r < s ? v : T(0);
-        }
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int r = row(t) + i, c = lane() % 16 * NT + j;
+            x[t][j][i] = get(B, r < s && c < have ? ((unsigned)c * (unsigned)ld + (unsigned)r) * e : kNowhere);
+          }
+    } else {
+#pragma unroll
+      for (int t = 0; t < kTiles; ++t) {
+        const int have = s - t * 16 < 16 ? s - t * 16 : 16;
+        const Buffer B = buffer_of(g + (have > 0 ? t * 16 * ld : 0) + c0, have > 0 ? ((have - 1) * ld + l - c0) * e : 0);
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int r = lane() / 16 * 4 + i;
+            x[t][j][i] = get(B, r < have && c0 + column(j) < l ? ((unsigned)r * (unsigned)ld + (unsigned)column(j)) * e : kNowhere);
+          }
+      }
     }
   }
   __device__ void store(T* to, int64_t ld, int s, int l, int c0, bool turned) const {
@@ -421,33 +448,47 @@ struct Columns {
   // (the share of) A, through LDS
   __device__ void gram(Lds& S, Gram& A) const {
     __syncthreads();
+    if constexpr (NT == 1 && sizeof(T) == 4) {
+      // neighbouring lanes change two of their four rows, for pairs of columns in one word
+      const bool odd = threadIdx.x & 1;
+      const int c = column(0) & ~1;
 #pragma unroll
-    for (int t = 0; t < kTiles; ++t)
+      for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        T v[NT];
+        for (int i = 0; i < 2; ++i) {
+          const float lo = x[t][0][i], hi = x[t][0][i + 2], got = __builtin_bit_cast(float, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, odd ? lo : hi), 0xb1, 0xf, 0xf, true));
+          S[c / 32].write_some(row(t) + i + (odd ? 2 : 0), c % 32, {odd ? got : lo, odd ? hi : got});
+        }
+    } else {
 #pragma unroll
-        for (int j = 0; j < NT; ++j) v[j] = x[t][j][i];
-        S[column(0) / 32].write_some(row(t) + i, column(0) % 32, v);
-      }
+      for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          T v[NT];
+#pragma unroll
+          for (int j = 0; j < NT; ++j) v[j] = x[t][j][i];
+          S[column(0) / 32].write_some(row(t) + i, column(0) % 32, v);
+        }
+    }
     __syncthreads();
 #pragma unroll
     for (int k = 0; k < kWide / 32; ++k) {
-      A.multiply(S[k], S[k]);
+      if (forms_gram()) A.multiply(S[k], S[k]);
       __builtin_amdgcn_sched_barrier(0);
     }
     __syncthreads();
   }
   // A as the left operand of the step's products
   static __device__ void put(Lds& S, const Gram& A) {
+    if (forms_gram())
 #pragma unroll
-    for (int rt = 0; rt < Gram::RT; ++rt)
+      for (int rt = 0; rt < Gram::RT; ++rt)
 #pragma unroll
-      for (int ct = 0; ct < Gram::CT; ++ct) {
-        const int c = A.column(ct);
-        const T v[4] = {A.acc[rt][ct][0], A.acc[rt][ct][1], A.acc[rt][ct][2], A.acc[rt][ct][3]};
-        S[c / 32].write4(A.row(rt), place(c % 32), v);
-      }
+        for (int ct = 0; ct < Gram::CT; ++ct) {
+          const int c = A.column(ct);
+          const T v[4] = {A.acc[rt][ct][0], A.acc[rt][ct][1], A.acc[rt][ct][2], A.acc[rt][ct][3]};
+          S[c / 32].write4(A.row(rt), place(c % 32), v);
+        }
     __syncthreads();
   }
   // y += A v
@@ -514,7 +555,7 @@ struct Schedule {
 
 // all steps of a matrix of at most 16 NT kWaves columns
 template <class T, int kS, int NT, int kWaves>
-__global__ void __launch_bounds__((64 * kWaves), (kWaves / 4)) k_orth_whole(OrthArgs a, int64_t first, int steps, Schedule schedule) {
+__global__ void __launch_bounds__((64 * kWaves), (kOrthWaves<T, kS, kWaves>)) k_orth_whole(OrthArgs a, int64_t first, int steps, Schedule schedule) {
   using Cols = Columns<T, kS, NT, kWaves>;
   __shared__ typename Cols::Lds S;
   __shared__ double sums[kWaves];
@@ -542,7 +583,10 @@ struct Chunk {
 // 1 / (|G| + eps), by all lanes of a wave
 __device__ inline double scale_of(const Chunk* chunk, int chunks, double eps) {
   double v = 0;
-  for (int i = (int)threadIdx.x & 63; i < (chunks + 63) / 64 * 64; i += 64) v += i < chunks ? chunk[i < chunks ? i : 0].squares : 0;
+  for (int i = 0; i < chunks; i += 64) {      // no lane is masked off: those behind the end have the last one, times zero
+    const int at = i + ((int)threadIdx.x & 63);
+    v += chunk[at < chunks ? at : chunks - 1].squares * (at < chunks ? 1.0 : 0.0);
+  }
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
   return 1.0 / (sqrt(v) + eps);
@@ -550,7 +594,7 @@ __device__ inline double scale_of(const Chunk* chunk, int chunks, double eps) {
 
 // The first share of A [matrix][chunk][kS * kS] and X [matrix][chunk][kS * columns], in the order of the registers
 template <class T, int kS, int NT, int kWaves>
-__global__ void __launch_bounds__((64 * kWaves), (kWaves / 4)) k_orth_begin(OrthArgs a, int64_t first, int chunks, Chunk* chunk, T* X_to, T* A_to) {
+__global__ void __launch_bounds__((64 * kWaves), (kOrthWaves<T, kS, kWaves>)) k_orth_begin(OrthArgs a, int64_t first, int chunks, Chunk* chunk, T* X_to, T* A_to) {
   using Cols = Columns<T, kS, NT, kWaves>;
   __shared__ typename Cols::Lds S;
   __shared__ double sums[kWaves];
@@ -565,13 +609,13 @@ __global__ void __launch_bounds__((64 * kWaves), (kWaves / 4)) k_orth_begin(Orth
   X.keep(X_to + place * (kS * Cols::kWide));
   typename Cols::Gram A;
   X.gram(S, A);
-  A.keep(A_to + place * (kS * kS));
+  if (Cols::forms_gram()) A.keep(A_to + place * (kS * kS));
   if (threadIdx.x == 0) chunk[place] = {squares, power};
 }
 
 // A step.  parts: how many shares of A there are a matrix; chunk: of the first step
 template <class T, int kS, int NT, int kWaves, bool kLast>
-__global__ void __launch_bounds__((64 * kWaves), (kWaves / 4)) k_orth_step(OrthArgs a, int64_t first, int chunks, int parts, T c0, T c1, T c2, const Chunk* chunk, T* X_at, const T* A_from, T* A_to) {
+__global__ void __launch_bounds__((64 * kWaves), (kOrthWaves<T, kS, kWaves>)) k_orth_step(OrthArgs a, int64_t first, int chunks, int parts, T c0, T c1, T c2, const Chunk* chunk, T* X_at, const T* A_from, T* A_to) {
   using Cols = Columns<T, kS, NT, kWaves>;
   __shared__ typename Cols::Lds S;
   const int64_t matrix = first + blockIdx.x / chunks, place = matrix * chunks + blockIdx.x % chunks;
@@ -579,10 +623,10 @@ __global__ void __launch_bounds__((64 * kWaves), (kWaves / 4)) k_orth_step(OrthA
   X.take(X_at + place * (kS * Cols::kWide));
   typename Cols::Gram A;
   A_from += matrix * parts * (kS * kS);
-  if (chunk) {
-    const double scale = scale_of(chunk + matrix * chunks, chunks, a.eps);
-    X.scale(scale / chunk[place].power);
-    if (parts == chunks) {
+  const double scale = chunk ? scale_of(chunk + matrix * chunks, chunks, a.eps) : 1;
+  if (chunk) X.scale(scale / chunk[place].power);
+  if (Cols::forms_gram()) {
+    if (chunk && parts == chunks) {
       A.add_all(A_from, parts, [&](int p) {
         const double f = scale / chunk[matrix * chunks + p].power;
         return (T)(f * f);
@@ -590,8 +634,6 @@ __global__ void __launch_bounds__((64 * kWaves), (kWaves / 4)) k_orth_step(OrthA
     } else {
       A.add_all(A_from, parts, [](int) { return T(1); });
     }
-  } else {
-    A.add_all(A_from, parts, [](int) { return T(1); });
   }
   Cols::put(S, A);
   X.step(S, c0, c1, c2);
@@ -603,29 +645,32 @@ __global__ void __launch_bounds__((64 * kWaves), (kWaves / 4)) k_orth_step(OrthA
     X.keep(X_at + place * (kS * Cols::kWide));
     typename Cols::Gram next;
     X.gram(S, next);
-    next.keep(A_to + place * (kS * kS));
+    if (Cols::forms_gram()) next.keep(A_to + place * (kS * kS));
   }
 }
 
-// to [matrix][size] = sums of from [matrix][parts][size], in their order; chunk: of the first step
+// to [matrix][size] = sums of from [matrix][parts][size]; chunk: of the first step.  32 numbers a workgroup (size is a multiple of them), eighths of the parts one after
+// another: 157 shares of 32 x 32 numbers 7 us.
 template <class T>
 __global__ void __launch_bounds__(kProductThreads) k_orth_join(OrthArgs a, int64_t first, int blocks, int parts, int size, const Chunk* chunk, const T* from, T* to) {
+  __shared__ T sums[8][32];
   const int64_t matrix = first + blockIdx.x / blocks;
-  const int i = blockIdx.x % blocks * kProductThreads + threadIdx.x;
-  from += matrix * parts * size + i;
+  const int i = threadIdx.x % 32, group = threadIdx.x / 32, at = blockIdx.x % blocks * 32 + i;
   const double scale = chunk ? scale_of(chunk + matrix * parts, parts, a.eps) : 0;
-  auto factor = [&](int p) {
+  from += matrix * parts * size + at;
+  T v = 0;
+#pragma unroll 8
+  for (int p = parts * group / 8; p < parts * (group + 1) / 8; ++p) {
     const double f = chunk ? scale / chunk[matrix * parts + p].power : 1;
-    return (T)(f * f);
-  };
-  if (i >= size) return;
-  T v[8] = {};
-  int p = 0;
-  for (; p + 8 <= parts; p += 8)
+    v += (T)(f * f) * from[(int64_t)p * size];
+  }
+  sums[group][i] = v;
+  __syncthreads();
+  if (group > 0) return;
+  v = 0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] += factor(p + j) * from[(int64_t)(p + j) * size];
-  for (; p < parts; ++p) v[0] += factor(p) * from[(int64_t)p * size];
-  to[matrix * size + i] = ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+  for (int g = 0; g < 8; ++g) v += sums[g][i];
+  to[matrix * size + at] = v;
 }
 
 // ---- launches -------------------------------------------------------------------------------------------------------------------
@@ -648,20 +693,23 @@ hipError_t in_launches(int64_t batch, int64_t tiles, F f) {
 
 int shares_of(int64_t m, int64_t n) { return (int)std::min<int64_t>({kShares, m, std::max<int64_t>(1, m * n / 4096)}); }
 
-// What the columns of X are cut into where it has few rows.  Shares of A are added up by every workgroup of a matrix up to kMostShares of them, by a launch of its own beyond.
-constexpr int64_t kMostShares = 32;
+// What the columns of X are cut into where it has few rows.  Shares of A are added up by every workgroup of a matrix, beyond kMostShares bytes of them by a launch of its own
+// (128 rows, a step: 9 shares, of 64 KiB, 20 us, 24 of them 29, added up before 17 and 6).
+constexpr int64_t kMostShares = 640 << 10;
 
 struct Few {
   int64_t rows, wide, chunks;      // padded rows, columns of a chunk, chunks
+  bool join;
   Few(int64_t m, int64_t n, bool f64) {
     const int64_t s = std::min(m, n), l = std::max(m, n);
     rows = (s + 31) / 32 * 32;
     wide = f64 || l <= 64 ? 64 : 128;
     chunks = (l + wide - 1) / wide;
+    join = chunks * rows * rows * (f64 ? 8 : 4) > kMostShares;
   }
   size_t x_size() const { return rows * wide * chunks; }      // numbers a matrix
   size_t a_size() const { return rows * rows * chunks; }
-  size_t sum_size() const { return chunks > kMostShares ? rows * rows : 0; }
+  size_t sum_size() const { return join ? rows * rows : 0; }
 };
 
 // The products of a step where X has many rows.  Tiles of 128 x 128 read half as much for a product, tiles of 64 x 64 leave less unfilled: X of 1152 x 2048 fp32 49 us a
@@ -751,11 +799,15 @@ hipError_t many_rows(const OrthArgs& a, const double* coefficients, int steps, c
 template <class T, int kS, int NT, int kWaves>
 hipError_t few_rows(const OrthArgs& a, const double* coefficients, int steps, char* ws, hipStream_t st) {
   const Few f(a.m, a.n, sizeof(T) == 8);
-  if (f.chunks == 1) {
-    Schedule schedule = {};
-    for (int i = 0; i < 3 * steps; ++i) schedule.c[i / 3][i % 3] = coefficients[i];
-    return in_launches(a.batch, 1, [&](int64_t first, dim3 grid) { k_orth_whole<T, kS, NT, kWaves><<<grid, 64 * kWaves, 0, st>>>(a, first, steps, schedule); });
-  }
+  constexpr int kWide = 16 * NT * kWaves;
+  if constexpr (kS <= kWide)      // else there is more than one chunk
+    if (f.chunks == 1) {
+      Schedule schedule = {};
+      for (int i = 0; i < 3 * steps; ++i) schedule.c[i / 3][i % 3] = coefficients[i];
+      return in_launches(a.batch, 1, [&](int64_t first, dim3 grid) { k_orth_whole<T, kS, NT, kWaves><<<grid, 64 * kWaves, 0, st>>>(a, first, steps, schedule); });
+    }
+  if constexpr (sizeof(T) == 4 && kWide == 64) return hipErrorInvalidValue;      // more than 64 columns go by 128
+  else {
   const int chunks = (int)f.chunks;
   Chunk* chunk = (Chunk*)ws;
   T* X = (T*)(ws + up(a.batch * chunks * sizeof(Chunk)));
@@ -768,8 +820,8 @@ hipError_t few_rows(const OrthArgs& a, const double* coefficients, int steps, ch
     const T* from = A;
     const Chunk* start = i ? nullptr : chunk;
     int parts = chunks;
-    if (chunks > kMostShares) {
-      constexpr int kBlocks = kS * kS / kProductThreads;
+    if (f.join) {
+      constexpr int kBlocks = kS * kS / 32;
       e = in_launches(a.batch, kBlocks, [&](int64_t first, dim3 grid) { k_orth_join<T><<<grid, kProductThreads, 0, st>>>(a, first, kBlocks, chunks, kS * kS, start, A, sum); });
       if (e != hipSuccess) break;
       from = sum;
@@ -782,6 +834,7 @@ hipError_t few_rows(const OrthArgs& a, const double* coefficients, int steps, ch
     std::swap(A, next);
   }
   return e;
+  }
 }
 
 template <class T>
@@ -790,12 +843,11 @@ hipError_t orthogonalise(const OrthArgs& a, const double* coefficients, int step
     const Few f(a.m, a.n, sizeof(T) == 8);
     auto go = [&](auto rows) {
       constexpr int kS = decltype(rows)::value;
-      if constexpr (sizeof(T) == 4)
-        if (f.wide == 128) {
-          if constexpr (kS % 64 == 0) return few_rows<T, kS, 1, 8>(a, coefficients, steps, ws, st);
-          else return few_rows<T, kS, 2, 4>(a, coefficients, steps, ws, st);
-        }
-      return few_rows<T, kS, 1, 4>(a, coefficients, steps, ws, st);
+      if constexpr (sizeof(T) == 8) return few_rows<T, kS, 1, 4>(a, coefficients, steps, ws, st);
+      // 128 columns: eight waves of 16 each (89 of 128 x 128 74 us, four of 32 each 86), of 32 rows four of 32; there are no more rows than columns
+      else if constexpr (kS == 32) return f.wide == 128 ? few_rows<T, kS, 2, 4>(a, coefficients, steps, ws, st) : few_rows<T, kS, 1, 4>(a, coefficients, steps, ws, st);
+      else if constexpr (kS == 64) return f.wide == 128 ? few_rows<T, kS, 1, 8>(a, coefficients, steps, ws, st) : few_rows<T, kS, 1, 4>(a, coefficients, steps, ws, st);
+      else return few_rows<T, kS, 1, 8>(a, coefficients, steps, ws, st);
     };
     switch (f.rows) {
       case 32: return go(std::integral_constant<int, 32>());

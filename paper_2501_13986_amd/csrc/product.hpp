@@ -120,12 +120,6 @@ struct alignas(16) Operand<float, kR, kBy> {
 #pragma unroll
     for (int p = 0; p < 3; ++p) *(u32x4*)&v[p][line(r)][at(r, k)] = w.w[p];
   }
-  __device__ void write_some(int r, int k, const float (&x)[1]) {
-    unsigned w[3];
-    Num<float>::split(x[0], 0.f, w);
-#pragma unroll
-    for (int p = 0; p < 3; ++p) *(unsigned short*)&v[p][line(r)][at(r, k)] = (unsigned short)w[p];
-  }
   __device__ void write_some(int r, int k, const float (&x)[2]) {
     unsigned w[3];
     Num<float>::split(x[0], x[1], w);
