@@ -570,9 +570,11 @@ struct Chunks {
   Chunks(int64_t rows, int64_t K, int64_t n, int64_t comps) {
     row_tiles = (K + 63) / 64;
     column_tiles = (n + kTile<T> - 1) / kTile<T>;
-    // 256 lines a chunk are few enough for partial sums to cost little (20 000 x 7 x 128 x 128: 60 us with 256 lines, 68 with 128); fewer where compute units are without work
+    // Partial sums are 2 K n numbers of traffic a chunk, its lines K + n each: half as much with `least` lines (20 000 x 7 x 128 x 128, 256 lines: 60 us, with 128 68).
+    // Fewer lines where compute units are without work (2503 x 96 x 301: 17 us with 64, 29 with 256).
     auto workgroups = [&]() { return (rows >> shift) * row_tiles * column_tiles; };
-    while (shift > 4 && ((workgroups() < 1600 && comps << (shift - 1) >= 256) || (workgroups() < 320 && comps << (shift - 1) >= 64))) --shift;
+    const int64_t least = std::max<int64_t>(256, 4 * K * n / (K + n));
+    while (shift > 4 && ((workgroups() < 1600 && comps << (shift - 1) >= least) || (workgroups() < 320 && comps << (shift - 1) >= 64))) --shift;
     count = (rows + ((int64_t)1 << shift) - 1) >> shift;
     slots = count > 1 ? 2 * count : 0;
   }

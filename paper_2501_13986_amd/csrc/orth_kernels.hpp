@@ -610,7 +610,7 @@ __global__ void __launch_bounds__((64 * kWaves), (kOrthWaves<T, kS, kWaves>)) k_
   typename Cols::Gram A;
   X.gram(S, A);
   if (Cols::forms_gram()) A.keep(A_to + place * (kS * kS));
-  if (threadIdx.x == 0) chunk[place] = {squares, power};
+  if (threadIdx.x == 0) chunk[place] = {squares, squares == 0 ? __builtin_inf() : power};      // a chunk of zeros stays one, however small all of X is
 }
 
 // A step.  parts: how many shares of A there are a matrix; chunk: of the first step
@@ -675,7 +675,7 @@ __global__ void __launch_bounds__(kProductThreads) k_orth_join(OrthArgs a, int64
 
 // ---- launches -------------------------------------------------------------------------------------------------------------------
 
-constexpr int64_t kMostBlocks = (int64_t)1 << 23;   // workgroups of a launch: 2^32 threads are too many
+constexpr int64_t kMostBlocks = (int64_t)1 << 22;   // workgroups of a launch, of up to 512 threads: 2^32 of them are too many
 
 size_t up(size_t v) { return (v + 255) / 256 * 256; }
 
@@ -694,8 +694,8 @@ hipError_t in_launches(int64_t batch, int64_t tiles, F f) {
 int shares_of(int64_t m, int64_t n) { return (int)std::min<int64_t>({kShares, m, std::max<int64_t>(1, m * n / 4096)}); }
 
 // What the columns of X are cut into where it has few rows.  Shares of A are added up by every workgroup of a matrix, beyond kMostShares bytes of them by a launch of its own
-// (128 rows, a step: 9 shares, of 64 KiB, 20 us, 24 of them 29, added up before 17 and 6).
-constexpr int64_t kMostShares = 640 << 10;
+// (128 rows, a step: 9 shares, of 64 KiB, 20 us, 24 of them 29, added up before 16 and 5) or many of them (32 rows, 157 shares 17 us, added up before 5 and 7).
+constexpr int64_t kMostShares = 640 << 10, kManyShares = 64;
 
 struct Few {
   int64_t rows, wide, chunks;      // padded rows, columns of a chunk, chunks
@@ -705,7 +705,7 @@ struct Few {
     rows = (s + 31) / 32 * 32;
     wide = f64 || l <= 64 ? 64 : 128;
     chunks = (l + wide - 1) / wide;
-    join = chunks * rows * rows * (f64 ? 8 : 4) > kMostShares;
+    join = chunks * rows * rows * (f64 ? 8 : 4) > kMostShares || chunks > kManyShares;
   }
   size_t x_size() const { return rows * wide * chunks; }      // numbers a matrix
   size_t a_size() const { return rows * rows * chunks; }

@@ -246,6 +246,21 @@ def test_another_stream():
     assert torch.equal(outs[0], ref) and torch.equal(outs[1], ref) and torch.equal(gW[0], gW[1])
 
 
+def test_gradients_of_rows_beyond_32_bits():
+    """Rows of x and gx lie up to 2^33 bytes apart, several chunks of a group."""
+    from paper_2501_13986_amd import binding as b
+    rows, ld = 1100, 1 << 21
+    big = torch.empty(rows * ld, dtype=torch.float32, device="cuda")
+    x, gx = big.as_strided((rows, 60), (ld, 1)), big.as_strided((rows, 60), (ld, 1), 1 << 20)
+    p = inputs(rows, 20, 33, [500, 590], "f32", comps=3, perm=True, seed=1)
+    x.copy_(torch.from_numpy(p["x"]))
+    gx.fill_(float("nan"))
+    gW = torch.empty(2, 20, 33, device="cuda")
+    b.grouped_backward(x, dev(p["W"]), dev(p["gout"]), gx, gW, dev(p["ptr"]), perm=dev(p["perm"]), comps=3)
+    torch.cuda.synchronize()
+    compare(dict(out=None, gx=gx, gW=gW, gb=None), p, "far")
+
+
 def test_rows_beyond_32_bits():
     """Rows of x and out lie up to 2^33 bytes apart."""
     from paper_2501_13986_amd import binding as b

@@ -28,7 +28,7 @@ def run(G, **k):
 
 
 SIZES = [(1, 1, 1), (3, 1, 9), (2, 9, 1), (4, 5, 5), (1, 16, 16), (2, 31, 33), (2, 33, 31), (1, 64, 64), (3, 63, 65), (2, 64, 300), (2, 300, 64), (1, 65, 129), (2, 100, 97), (3, 128, 128),
-         (1, 127, 500), (1, 129, 130), (1, 200, 136), (2, 96, 301), (1, 8, 2176), (1, 257, 300), (40, 20, 24), (150, 3, 2), (1, 130, 520), (5, 48, 40)]
+         (1, 127, 500), (1, 129, 130), (1, 200, 136), (2, 96, 301), (1, 8, 2176), (1, 257, 300), (40, 20, 24), (150, 3, 2), (1, 130, 520), (5, 48, 40), (1, 90, 100), (2, 70, 400), (1, 20, 9000), (1, 9000, 20), (1, 128, 1700), (1, 65, 700)]
 
 
 @pytest.mark.parametrize("prec", PRECS)
@@ -38,6 +38,13 @@ def test_against_the_oracle(batch, m, n, prec):
         batch = 1
     G = gradients(batch, m, n, prec, seed=m + n)
     orth_check(run(G), G, prec, (batch, m, n))
+
+
+@pytest.mark.parametrize("m,n", [(1030, 1100), (1540, 1560), (1200, 1031)])
+def test_large_tiles(m, n):
+    G = gradients(1, m, n, "f32", seed=m)
+    c = [(3.4445, -4.7750, 2.0315)] * 2
+    orth_check(run(G, coefficients=c), G, "f32", (m, n), coefficients=c)
 
 
 @pytest.mark.parametrize("prec", PRECS)
@@ -79,6 +86,17 @@ def test_few_singular_values(prec):
 def test_sizes_of_numbers(scale, prec):
     G = (gradients(2, 24, 30, "f64", seed=8) * scale).astype(NP[prec])
     orth_check(run(G, eps=1e-40), G, prec, scale, eps=1e-40)
+
+
+@pytest.mark.parametrize("prec", PRECS)
+@pytest.mark.parametrize("m,n", [(40, 500), (500, 40), (128, 128), (100, 300), (150, 700)])
+def test_zeros_beside_small_numbers(m, n, prec):
+    """Whole chunks of columns are zero, the others small, and eps smaller still: nothing overflows on the way."""
+    G = (gradients(3, m, n, "f64", seed=12) * 1e-22).astype(NP[prec])
+    G[0, m // 2:], G[1, :, n // 2:], G[2] = 0, 0, 0
+    got = run(G, eps=1e-150)
+    orth_check(got, G, prec, (m, n), eps=1e-150)
+    assert not got[2].any() and not got[0, m // 2:].any() and not got[1, :, n // 2:].any()
 
 
 @pytest.mark.parametrize("prec", PRECS)

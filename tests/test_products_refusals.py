@@ -56,6 +56,7 @@ def test_grouped_workspace():
 
 
 COEFFICIENTS = (C.c_double * 6)(3, -4, 2, 3, -4, 2)
+WIDE, TALL = dict(m=8, n=300, ldg=300, ldo=300, sg=2400, so=2400), dict(m=300, n=200, ldg=200, ldo=200, sg=60000, so=60000)      # sizes that need a workspace
 
 
 def orth(g=P, out=P, batch=2, m=8, n=16, ldg=16, ldo=16, sg=128, so=128, c=COEFFICIENTS, steps=2, eps=1e-7, dtype=0, ws=P, nws=1 << 50):
@@ -66,8 +67,8 @@ def orth(g=P, out=P, batch=2, m=8, n=16, ldg=16, ldo=16, sg=128, so=128, c=COEFF
     (dict(g=0), 1), (dict(out=0), 1), (dict(g=P + 2), 1), (dict(out=P + 4, dtype=1), 1), (dict(batch=-1), 1), (dict(m=0), 1), (dict(n=-1), 1),
     (dict(ldg=15), 1), (dict(ldo=15), 1), (dict(sg=-1), 1), (dict(so=-128), 1), (dict(so=127), 1), (dict(so=0), 1), (dict(so=8, ldo=20), 1), (dict(c=None), 1),
     (dict(c=(C.c_double * 6)(1, 2, 3, 4, float("nan"), 1)), 1), (dict(c=(C.c_double * 6)(1, 2, 3, 4, 1e39, 1)), 1), (dict(steps=0), 1), (dict(steps=65), 1), (dict(eps=0.0), 1),
-    (dict(eps=-1.0), 1), (dict(eps=float("nan")), 1), (dict(eps=float("inf")), 1), (dict(eps=5e-324), 1), (dict(dtype=2), 1), (dict(ws=0), 1), (dict(ws=P + 128), 1), (dict(nws=1), 1),
-    (dict(batch=1 << 31), 2), (dict(m=1 << 16, n=1 << 16, ldg=1 << 16, ldo=1 << 16), 2), (dict(batch=1 << 30, m=1 << 10, n=1 << 10, ldg=1 << 10, ldo=1 << 10), 2), (dict(ldg=1 << 50), 2)])
+    (dict(eps=-1.0), 1), (dict(eps=float("nan")), 1), (dict(eps=float("inf")), 1), (dict(eps=5e-324), 1), (dict(dtype=2), 1), (dict(WIDE, ws=0), 1), (dict(WIDE, ws=P + 128), 1), (dict(WIDE, nws=1), 1), (dict(TALL, ws=0), 1), (dict(TALL, nws=255), 1),
+    (dict(batch=1 << 31), 2), (dict(m=1 << 16, n=1 << 16, ldg=1 << 16, ldo=1 << 16), 2), (dict(batch=1 << 30, m=1 << 10, n=1 << 10, ldg=1 << 10, ldo=1 << 10), 2), (dict(ldg=1 << 22), 2), (dict(ldo=1 << 50, so=1 << 59), 2), (dict(n=1 << 22, ldg=1 << 22, ldo=1 << 22), 2)])
 def test_orthogonalise_refuses(change, want):
     assert orth(**change) == want
     assert b.lib().cgtp_last_error()
