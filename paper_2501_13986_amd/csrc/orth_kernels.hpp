@@ -519,20 +519,23 @@ struct Columns {
       __builtin_amdgcn_sched_barrier(0);      // else all of A is on its way to registers at once
     }
   }
-  // X <- a X + A (b X + c A X), A in LDS
+  // X <- a X + A (b X + c A X), A in LDS.  The sum of A V starts from zero: from a X, every term's rounding would be one of the whole.
   __device__ void step(const Lds& S, T a, T b, T c) {
-    typename N::Vec y[kTiles][NT] = {};
+    typename N::Vec y[kTiles][NT] = {}, z[kTiles][NT] = {};
     times(S, x, y);
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
       for (int j = 0; j < NT; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          y[t][j][i] = b * x[t][j][i] + c * y[t][j][i];
-          x[t][j][i] *= a;
-        }
-    times(S, y, x);
+        for (int i = 0; i < 4; ++i) y[t][j][i] = b * x[t][j][i] + c * y[t][j][i];
+    times(S, y, z);
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[t][j][i] = a * x[t][j][i] + z[t][j][i];
   }
 };
 
