@@ -60,7 +60,7 @@ __device__ inline double scale_of(const double* part, int shares, double eps) {
 // X, its transpose, A and B stand in memory as operands: in parts, cut once by the kernel that writes them, in blocks of 64 rows x 32 terms, padded with
 // zeros.  A product is tiles of kTile x kTile results with the terms in splits, so that there is work for all compute units; sums of splits are left in
 // the order of the registers and added up, in their order, by k_orth_finish, which turns the results into operands both ways.  With one split the product does that itself.
-// 1152 x 2048 fp32, a step: A 21 us and 6 to finish, B the same, X 37 and 13 (its product 0.9 PFLOP/s of bf16 products, library 1.09, in 432 workgroups on 256 units); operands in fp32, cut by
+// 1152 x 2048 fp32, a step: A 19 us and 6 to finish, B the same, X 31 and 13 (its product 1.05 PFLOP/s of bf16 products, library 1.09, in 432 workgroups on 256 units); operands in fp32, cut by
 // each reader, took twice that.  More terms in LDS at a time were no faster, 128 x 64 tiles slower.
 
 constexpr int kBlock = 64;
@@ -280,20 +280,29 @@ __global__ void __launch_bounds__(kProductThreads, 2) k_orth_product(OrthArgs a,
   tile_of<kTile>(p, t, tr, tc);
   const Stored<T> left(p.rows_at + matrix * p.rows * p.terms * Stored<T>::kBytes, p.rows, p.terms), right(p.columns_at + matrix * p.columns * p.terms * Stored<T>::kBytes, p.columns, p.terms);
   const int steps = p.terms / kStep, from = steps * split / p.splits, end = steps * (split + 1) / p.splits;
-  Copy<T, kTile> rows, columns;
   Results<T, kTile, kTile> out;
-  rows.fetch(left, tr * kTile, from * kStep);
-  columns.fetch(right, tc * kTile, from * kStep);
-  for (int k = from; k < end; ++k) {
-    __syncthreads();
-    rows.put(S.in.R);
-    columns.put(S.in.C);
-    __syncthreads();
-    if (k + 1 < end) {
-      rows.fetch(left, tr * kTile, (k + 1) * kStep);
-      columns.fetch(right, tc * kTile, (k + 1) * kStep);
+  // fp64 fetches two steps ahead, for few waves share a unit (1000 x 1100 736 us, with one 792; fp32 tiles of 64 gain nothing).  What is fetched behind the end is the last step
+  // once more: without the condition tiles of 128 need 148 registers, three workgroups a unit, for 191 (2000 x 2000 1078 us for 1171); those of 64 lose (300 x 2000 209 for 201).
+  constexpr int kAhead = sizeof(T) == 8 ? 2 : 1;
+  Copy<T, kTile> rows[kAhead], columns[kAhead];
+  auto fetch = [&](int slot, int k) {
+    const int at = (k < end ? k : end - 1) * kStep;
+    rows[slot].fetch(left, tr * kTile, at);
+    columns[slot].fetch(right, tc * kTile, at);
+  };
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) fetch(i, from + i);
+  for (int k = from; k < end; k += kAhead) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (i > 0 && k + i >= end) break;
+      __syncthreads();
+      rows[i].put(S.in.R);
+      columns[i].put(S.in.C);
+      __syncthreads();
+      if (sizeof(T) == 8 || kTile == 128 || k + 1 < end) fetch(i, k + i + kAhead);
+      out.multiply(S.in.R, S.in.C);
     }
-    out.multiply(S.in.R, S.in.C);
   }
   if (p.splits > 1) {
     out.keep(part + ((matrix * p.tiles + t) * p.splits + split) * (kTile * kTile));
@@ -736,9 +745,23 @@ struct Many {
     l = (l0 + x_tile - 1) / x_tile * x_tile;
     square = s / square_tile * (s / square_tile + 1) / 2;
     wide = s / x_tile * (l / x_tile);
-    // splits of the terms, four steps of 32 or more each, up to three workgroups of small tiles a compute unit (1152 rows: 27 us a product of A; with two 31) or two of large ones
+    // Splits of the terms, four steps of 32 or more each.  fp32: up to three workgroups of small tiles a compute unit (1152 rows: 27 us a product of A; with two 31) or two of
+    // large ones (1152 x 2048 460 us; with three 488).  fp64: by the time of a unit that has the most of them (33 ns a term of a tile, one workgroup alone has two thirds of
+    // the rate) and, with several, that of another launch and of the sums at 4.5 TB/s: 1152 x 2048 1134 us, with two workgroups a unit 1219.
     auto splits = [&](int tile, int64_t tiles, int64_t terms) {
-      return (int)std::max<int64_t>(1, std::min(terms / kStep / 4, (tile == 64 && sizeof(T) == 4 ? 768 : 512) / (batch * tiles)));
+      const int64_t all = batch * tiles, most = std::max<int64_t>(1, terms / kStep / 4);
+      if constexpr (sizeof(T) == 4) return (int)std::max<int64_t>(1, std::min(most, (tile == 64 ? 768 : 512) / all));
+      int best = 1;
+      double least = 0;
+      for (int n = 1; n <= std::min<int64_t>(most, 32); ++n) {
+        const double rounds = std::max(1.5, (double)((all * n + 255) / 256));
+        const double time = rounds / n * terms * 0.033 + (n > 1 ? 6 + 2.0 * all * n * tile * tile * sizeof(T) / 4.5e6 : 0);
+        if (n == 1 || time < least) {
+          least = time;
+          best = n;
+        }
+      }
+      return best;
     };
     a_splits = splits(square_tile, square, l);
     b_splits = splits(square_tile, square, s);
