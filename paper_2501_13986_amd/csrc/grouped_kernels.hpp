@@ -249,52 +249,60 @@ __global__ void __launch_bounds__(kProductThreads, 2) k_grouped_rows(GroupedArgs
     at_x[i] = r < 0 ? kNowhere : (unsigned)(from * e);
     if (threadIdx.x % 8 == 0) place[line] = r < 0 || line >= have ? -1 : r * ld_to + m * (int64_t)n;
   }
-  Rows rows;
-  AcrossTerms<T, kC, kWhole> across(c0, n);
-  Along along;
+  // tiles of half the lines, taken where there are few, fetch two steps ahead (fp64 2503 x 96 x 301 both gradients 37.3 -> 33.7 us); the others have enough waves a unit
+  constexpr int kAhead = !kFar && kR < (sizeof(T) == 4 ? 128 : 64) ? 2 : 1;
+  Rows rows[2];
+  using Across = AcrossTerms<T, kC, kWhole>;
+  Across across[2] = {Across(c0, n), Across(c0, n)};
+  Along along[2];
   if constexpr (kBack)
 #pragma unroll
     for (int i = 0; i < Along::kPer; ++i) {
-      const int c = c0 + along.row(i);
+      const int c = c0 + Along::row(i);
       pw[i] = W + (int64_t)(c < n ? c : 0) * K;
       at_w[i] = c < n ? (unsigned)c * (unsigned)K * e : kNowhere;
     }
-  auto fetch = [&](int k0) {
-    if constexpr (kFar) rows.fetch(p, k0, K);
-    else rows.fetch(bx, at_x, k0, K);
+  auto fetch = [&](int slot, int k0) {
+    if constexpr (kFar) rows[slot].fetch(p, k0, K);
+    else rows[slot].fetch(bx, at_x, k0, K);
     if constexpr (kBack) {
-      if constexpr (kFar) along.fetch(pw, k0, K);
-      else along.fetch(bw, at_w, k0, K);
+      if constexpr (kFar) along[slot].fetch(pw, k0, K);
+      else along[slot].fetch(bw, at_w, k0, K);
     } else if constexpr (kFar) {
       const T* q[8];
       bool ok[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const int k = k0 + across.term() + j;
+        const int k = k0 + Across::term() + j;
         ok[j] = k < K;
         q[j] = W + (int64_t)(ok[j] ? k : 0) * n;
       }
-      across.fetch(q, ok);
+      across[slot].fetch(q, ok);
     } else {
       unsigned q[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const int k = k0 + across.term() + j;
+        const int k = k0 + Across::term() + j;
         q[j] = k < K ? (unsigned)k * (unsigned)n * e : kNowhere;
       }
-      across.fetch(bw, q);
+      across[slot].fetch(bw, q);
     }
   };
   Results<T, kR, kC> out;
-  fetch(0);
-  for (int k0 = 0; k0 < K; k0 += kStep) {
-    __syncthreads();
-    rows.put(R);
-    if constexpr (kBack) along.put(C);
-    else across.put(C);
-    __syncthreads();
-    if (k0 + kStep < K) fetch(k0 + kStep);
-    out.multiply(R, C);
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) fetch(i, i * kStep);
+  for (int k0 = 0; k0 < K; k0 += kAhead * kStep) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (i > 0 && k0 + i * kStep >= K) break;
+      __syncthreads();
+      rows[i].put(R);
+      if constexpr (kBack) along[i].put(C);
+      else across[i].put(C);
+      __syncthreads();
+      if (kAhead > 1 || k0 + kStep < K) fetch(i, k0 + (i + kAhead) * kStep);
+      out.multiply(R, C);
+    }
   }
   const T* bias = kBack || !a.b ? nullptr : (const T*)a.b + g * n;
   T* to = (T*)(kBack ? a.gx : a.out);

@@ -729,9 +729,9 @@ struct Few {
   size_t sum_size() const { return join ? rows * rows : 0; }
 };
 
-// The products of a step where X has many rows.  Tiles of 128 x 128 read half as much for a product, tiles of 64 x 64 leave less unfilled: X of 1152 x 2048 fp32 49 us a
-// product with the former (splits added up), 54 with the latter, 800 x 800 25 and 22; A and its square of 1600 rows 42 and 44 us, of 1152 33 and 27, of 500 (three of
-// them) 19 and 13.
+// The products of a step where X has many rows.  Tiles of 128 x 128 read half as much for a product, tiles of 64 x 64 leave less unfilled.  fp32, all steps, X in large tiles and
+// in small ones: 700 x 900 275 us and 234, 768 x 2048 310 and 297; A and its square in large and in small ones: 1500 x 1500 581 and 622, 1300 x 1400 515
+// and 486.
 template <class T>
 struct Many {
   int square_tile, x_tile;           // of A and B, of X
@@ -739,7 +739,7 @@ struct Many {
   int a_splits, b_splits, x_splits;
   Many(int64_t batch, int64_t m, int64_t n) {
     const int64_t s0 = std::min(m, n), l0 = std::max(m, n);
-    square_tile = sizeof(T) == 4 && s0 >= 1536 ? 128 : 64;
+    square_tile = sizeof(T) == 4 && s0 >= 1408 ? 128 : 64;
     x_tile = sizeof(T) == 4 && s0 >= 1024 ? 128 : 64;
     s = (s0 + x_tile - 1) / x_tile * x_tile;
     l = (l0 + x_tile - 1) / x_tile * x_tile;
