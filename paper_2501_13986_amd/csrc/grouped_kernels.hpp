@@ -627,7 +627,7 @@ hipError_t launch_rows(const GroupedArgs& a, hipStream_t st) {
       k_grouped_rows<T, kR, 64, decltype(whole_)::value, kBack, decltype(far)::value><<<grid, kProductThreads, 0, st>>>(a, first, (int)tiles);
     });
   };
-  // tiles of half the lines where that fills compute units (fp64, 2503 x 301 -> 96: 17 us for 32; many lines, fp32 160 710 x 2176 -> 64: 343 us, with half 366, with 128
+  // tiles of half the lines where that fills compute units (fp64, 2503 x 301 -> 96, both one step ahead: 17 us for 32; many lines, fp32 160 710 x 2176 -> 64: 343 us, with half 366, with 128
   // columns of twice the registers no faster: 30 000 x 300 -> 300 47 us and 56)
   auto size = [&](auto whole_, auto far) {
     constexpr int kR = sizeof(T) == 4 ? 128 : 64;
