@@ -299,17 +299,17 @@ struct Results {
     typename N::Parts c[CT];
 #pragma unroll
     for (int ct = 0; ct < CT; ++ct) c[ct] = C.read(c0 + ct * 16, k);
-    constexpr int kSide = CT >= 4 || RT < 2 ? 1 : 2;      // rows of tiles side by side: chains of sums in turn
+    constexpr int kSide = CT >= 4 || RT < 2 ? 1 : 2;      // rows of tiles side by side: chains of sums in turn; the last of an odd number stands alone
 #pragma unroll
     for (int rt = 0; rt < RT; rt += kSide) {
       typename N::Parts r[kSide];
 #pragma unroll
-      for (int s = 0; s < kSide; ++s) r[s] = R.read(r0 + (rt + s) * 16 + l16, k);
+      for (int s = 0; s < kSide && rt + s < RT; ++s) r[s] = R.read(r0 + (rt + s) * 16 + l16, k);
       constexpr int kUnits = sizeof(T) == 4 ? 6 : 8;
 #pragma unroll
       for (int m = 0; m < kUnits; ++m)
 #pragma unroll
-        for (int s = 0; s < kSide; ++s)
+        for (int s = 0; s < kSide && rt + s < RT; ++s)
 #pragma unroll
           for (int ct = 0; ct < CT; ++ct) {
             auto& a = acc[rt + s][ct];
