@@ -17,42 +17,88 @@ constexpr int kShares = 256;      // partial sums of squares of a matrix, at mos
 
 // ---- the start ------------------------------------------------------------------------------------------------------------------
 
-// part [batch][shares]: sums of squares of shares of the rows
+// Part of a matrix: the sum of squares of its numbers times `power`, a power of two.
+struct Size {
+  double squares, power;
+};
+
+// The power of two that brings the largest number near one, so that no square overflows or is lost (the squares of fp32 numbers do neither in fp64).  Of zeros the
+// greatest, so that they decide nothing beside others; of infinities and NaN any, for their squares tell.
+__device__ inline double power_for(double largest) {
+  const int e = largest == 0 ? -1000 : __builtin_amdgcn_frexp_exp(largest);
+  return __builtin_amdgcn_ldexp(1.0, e < -1000 ? 1000 : e > 1000 ? -1000 : -e);
+}
+
+// 1 / (|G| + eps) is power * inverse: numbers are multiplied by one after the other
+struct Scale {
+  double power, inverse;
+  // for numbers that have been multiplied by p
+  __device__ double of(double p) const { return power / p * inverse; }
+};
+
+// of the parts of a matrix, by all lanes of a wave; none is masked off: those behind the end have the last part again
+__device__ inline Scale scale_of(const Size* part, int parts, double eps) {
+  const int lane = (int)threadIdx.x & 63;
+  auto get = [&](int i) { return part[i + lane < parts ? i + lane : parts - 1]; };
+  const Size first = get(0);
+  double power = first.power, v = 0;
+  for (int i = 64; i < parts; i += 64) power = fmin(power, get(i).power);
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) power = fmin(power, __shfl_xor(power, d));
+  auto add = [&](int i, const Size& s) {
+    const double f = power / s.power, w = s.squares * (f * f);
+    v += i + lane < parts ? w : 0.0;
+  };
+  add(0, first);
+  for (int i = 64; i < parts; i += 64) add(i, get(i));
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
+  return {power, 1.0 / (sqrt(v) + eps * power)};
+}
+
+// part [batch][shares]: of shares of the rows
 template <class T>
-__global__ void __launch_bounds__(kProductThreads) k_orth_squares(OrthArgs a, int64_t first, int shares, double* part) {
-  __shared__ double sums[kProductThreads / 64];
+__global__ void __launch_bounds__(kProductThreads) k_orth_squares(OrthArgs a, int64_t first, int shares, Size* part) {
+  __shared__ double sums[2][kProductThreads / 64];
   const int64_t matrix = first + blockIdx.x / shares, share = blockIdx.x % shares;
   const T* g = (const T*)a.g + matrix * a.stride_g;
   const int64_t from = a.m * share / shares, end = a.m * (share + 1) / shares;
   // as many lanes side by side as a row has numbers, eight numbers on their way to a thread
   const int wide = a.n >= kProductThreads ? kProductThreads : a.n > 64 ? 128 : a.n > 16 ? 64 : 16, x = threadIdx.x % wide, y = threadIdx.x / wide, high = kProductThreads / wide;
-  double v = 0;
-  for (int64_t r = from + y; r < end; r += high) {
-    const T* p = g + r * a.ld_g;
-    int64_t c = x;
-    for (; c + 7 * wide < a.n; c += 8 * wide) {
-      double w[8];
+  auto each = [&](auto f) {
+    for (int64_t r = from + y; r < end; r += high) {
+      const T* p = g + r * a.ld_g;
+      int64_t c = x;
+      for (; c + 7 * wide < a.n; c += 8 * wide) {
+        double w[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) w[i] = (double)p[c + i * wide];
+        for (int i = 0; i < 8; ++i) w[i] = (double)p[c + i * wide];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v += w[i] * w[i];
+        for (int i = 0; i < 8; ++i) f(w[i]);
+      }
+      for (; c < a.n; c += wide) f((double)p[c]);
     }
-    for (; c < a.n; c += wide) v += (double)p[c] * (double)p[c];
+  };
+  double power = 1;
+  if constexpr (sizeof(T) == 8) {      // the second reading is from the caches
+    double most = 0;
+    each([&](double w) { most = fmax(most, fabs(w)); });
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) most = fmax(most, __shfl_xor(most, d));
+    if (threadIdx.x % 64 == 0) sums[0][threadIdx.x / 64] = most;
+    __syncthreads();
+    power = power_for(fmax(fmax(sums[0][0], sums[0][1]), fmax(sums[0][2], sums[0][3])));
   }
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-  if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = v;
-  __syncthreads();
-  if (threadIdx.x == 0) part[matrix * shares + share] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
-}
-
-// 1 / (|G| + eps), by all lanes of a wave
-__device__ inline double scale_of(const double* part, int shares, double eps) {
   double v = 0;
-  for (int i = (int)threadIdx.x & 63; i < (shares + 63) / 64 * 64; i += 64) v += i < shares ? part[i < shares ? i : 0] : 0;
+  each([&](double w) {
+    w *= power;
+    v += w * w;
+  });
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-  return 1.0 / (sqrt(v) + eps);
+  if (threadIdx.x % 64 == 0) sums[1][threadIdx.x / 64] = v;
+  __syncthreads();
+  if (threadIdx.x == 0) part[matrix * shares + share] = {(sums[1][0] + sums[1][1]) + (sums[1][2] + sums[1][3]), power};
 }
 
 // ---- more rows --------------------------------------------------------------------------------------------------------------------
@@ -153,18 +199,18 @@ struct Copy<double, kR> {
 
 // X and its transpose, 64 x 64 numbers of G a workgroup; rounded once.  s, l: padded
 template <class T>
-__global__ void __launch_bounds__(kProductThreads) k_orth_start(OrthArgs a, int64_t first, int tiles, int s, int l, int shares, const double* part, char* X, char* XT) {
+__global__ void __launch_bounds__(kProductThreads) k_orth_start(OrthArgs a, int64_t first, int tiles, int s, int l, int shares, const Size* part, char* X, char* XT) {
   __shared__ T tile[kBlock][kBlock + 1];
   const int64_t matrix = first + blockIdx.x / tiles, size = (int64_t)s * l * Stored<T>::kBytes;
   const bool turned = a.m > a.n;
   const int across = l / kBlock, r0 = blockIdx.x % tiles / across * kBlock, c0 = blockIdx.x % tiles % across * kBlock;      // of X
-  const double scale = scale_of(part + matrix * shares, shares, a.eps);
+  const Scale scale = scale_of(part + matrix * shares, shares, a.eps);
   const T* g = (const T*)a.g + matrix * a.stride_g;
   const Stored<T> to(X + matrix * size, s, l), to_t(XT + matrix * size, l, s);
   const int x = threadIdx.x % kBlock;
   for (int y = threadIdx.x / kBlock; y < kBlock; y += kProductThreads / kBlock) {      // neighbours of G side by side
     const int64_t r = (turned ? c0 : r0) + y, c = (turned ? r0 : c0) + x;
-    const T v = r < a.m && c < a.n ? (T)((double)g[r * a.ld_g + c] * scale) : T(0);
+    const T v = r < a.m && c < a.n ? (T)((double)g[r * a.ld_g + c] * scale.power * scale.inverse) : T(0);
     if (turned) tile[x][y] = v;
     else tile[y][x] = v;
   }
@@ -440,6 +486,17 @@ struct Columns {
 #pragma unroll
       for (int j = 0; j < NT; ++j) x[t][j] = *(const typename N::Vec*)(from + ((t * NT + j) * kThreads + (int)threadIdx.x) * 4);
   }
+  // the thread's largest number
+  __device__ double largest() const {
+    double v = 0;
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int j = 0; j < NT; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v = fmax(v, fabs((double)x[t][j][i]));
+    return v;
+  }
   // the thread's share of the sum of squares
   __device__ double squares() const {
     double v = 0;
@@ -555,7 +612,7 @@ struct Columns {
 
 // sum over the workgroup, to all its threads
 template <int kWaves>
-__device__ inline double sum_of_all(double v, double* sums) {
+__device__ inline double sum_of_all(double v, double (&sums)[kWaves]) {
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
   sums[threadIdx.x / 64] = v;      // all lanes the same
@@ -564,6 +621,32 @@ __device__ inline double sum_of_all(double v, double* sums) {
 #pragma unroll
   for (int i = 0; i < kWaves; ++i) v += sums[i];
   return v;
+}
+
+template <int kWaves>
+__device__ inline double largest_of_all(double v, double (&most)[kWaves]) {
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) v = fmax(v, __shfl_xor(v, d));
+  most[threadIdx.x / 64] = v;      // all lanes the same
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) v = fmax(v, most[i]);
+  return v;
+}
+
+// X, which is as it was read, is multiplied by a power of two that brings it near one: its size.  fp32: the squares are numbers of fp64 and name the power, so that only `near` asks
+// for it; fp64: the largest number does.
+template <bool near, int kWaves, class Cols>
+__device__ inline Size size_of(Cols& X, double (&sums)[2][kWaves]) {
+  if constexpr (sizeof(X.x[0][0][0]) == 8) {
+    const double power = power_for(largest_of_all<kWaves>(X.largest(), sums[0]));
+    X.scale(power);
+    return {sum_of_all<kWaves>(X.squares(), sums[1]), power};
+  } else {
+    const double squares = sum_of_all<kWaves>(X.squares(), sums[1]), power = near ? power_for(sqrt(squares)) : 1;
+    if (near) X.scale(power);
+    return {squares * power * power, power};
+  }
 }
 
 struct Schedule {
@@ -575,13 +658,14 @@ template <class T, int kS, int NT, int kWaves>
 __global__ void __launch_bounds__((64 * kWaves), (kOrthWaves<T, kS, kWaves>)) k_orth_whole(OrthArgs a, int64_t first, int steps, Schedule schedule) {
   using Cols = Columns<T, kS, NT, kWaves>;
   __shared__ typename Cols::Lds S;
-  __shared__ double sums[kWaves];
+  __shared__ double sums[2][kWaves];
   const int64_t matrix = first + blockIdx.x;
   const bool turned = a.m > a.n;
   const int s = (int)(turned ? a.n : a.m), l = (int)(turned ? a.m : a.n);
   Cols X;
   X.load((const T*)a.g + matrix * a.stride_g, a.ld_g, s, l, 0, turned);
-  X.scale(1.0 / (sqrt(sum_of_all<kWaves>(X.squares(), sums)) + a.eps));
+  const Size size = size_of<false>(X, sums);
+  X.scale(1.0 / (sqrt(size.squares) + a.eps * size.power));
   for (int i = 0; i < steps; ++i) {
     typename Cols::Gram A;
     X.gram(S, A);
@@ -591,48 +675,30 @@ __global__ void __launch_bounds__((64 * kWaves), (kOrthWaves<T, kS, kWaves>)) k_
   X.store((T*)a.out + matrix * a.stride_out, a.ld_out, s, l, 0, turned);
 }
 
-// The start leaves each chunk of X multiplied by the power of two that brings its size near one, so that no product of it overflows or is lost, with the sum of its squares: the
-// size of all of X is known when the first step begins, which multiplies X once (as if G were) and the shares of A by the squares.
-struct Chunk {
-  double squares, power;
-};
-
-// 1 / (|G| + eps), by all lanes of a wave
-__device__ inline double scale_of(const Chunk* chunk, int chunks, double eps) {
-  double v = 0;
-  for (int i = 0; i < chunks; i += 64) {      // no lane is masked off: those behind the end have the last one, times zero
-    const int at = i + ((int)threadIdx.x & 63);
-    v += chunk[at < chunks ? at : chunks - 1].squares * (at < chunks ? 1.0 : 0.0);
-  }
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-  return 1.0 / (sqrt(v) + eps);
-}
-
+// The start leaves each chunk of X multiplied by the power of two that brings its size near one, so that no product of it overflows or is lost, with its size: that of all of X is known
+// when the first step begins, which multiplies X once (as if G were) and the shares of A by the squares.
 // The first share of A [matrix][chunk][kS * kS] and X [matrix][chunk][kS * columns], in the order of the registers
 template <class T, int kS, int NT, int kWaves>
-__global__ void __launch_bounds__((64 * kWaves), (kOrthWaves<T, kS, kWaves>)) k_orth_begin(OrthArgs a, int64_t first, int chunks, Chunk* chunk, T* X_to, T* A_to) {
+__global__ void __launch_bounds__((64 * kWaves), (kOrthWaves<T, kS, kWaves>)) k_orth_begin(OrthArgs a, int64_t first, int chunks, Size* chunk, T* X_to, T* A_to) {
   using Cols = Columns<T, kS, NT, kWaves>;
   __shared__ typename Cols::Lds S;
-  __shared__ double sums[kWaves];
+  __shared__ double sums[2][kWaves];
   const int64_t matrix = first + blockIdx.x / chunks, place = matrix * chunks + blockIdx.x % chunks;
   const bool turned = a.m > a.n;
   const int s = (int)(turned ? a.n : a.m), l = (int)(turned ? a.m : a.n);
   Cols X;
   X.load((const T*)a.g + matrix * a.stride_g, a.ld_g, s, l, blockIdx.x % chunks * Cols::kWide, turned);
-  const double squares = sum_of_all<kWaves>(X.squares(), sums);
-  const double power = squares > 0 && squares < __builtin_inf() ? ldexp(1.0, -ilogb(sqrt(squares))) : 1.0;
-  X.scale(power);
+  const Size size = size_of<true>(X, sums);
   X.keep(X_to + place * (kS * Cols::kWide));
   typename Cols::Gram A;
   X.gram(S, A);
   if (Cols::forms_gram()) A.keep(A_to + place * (kS * kS));
-  if (threadIdx.x == 0) chunk[place] = {squares, squares == 0 ? __builtin_inf() : power};      // a chunk of zeros stays one, however small all of X is
+  if (threadIdx.x == 0) chunk[place] = size;
 }
 
 // A step.  parts: how many shares of A there are a matrix; chunk: of the first step
 template <class T, int kS, int NT, int kWaves, bool kLast>
-__global__ void __launch_bounds__((64 * kWaves), (kOrthWaves<T, kS, kWaves>)) k_orth_step(OrthArgs a, int64_t first, int chunks, int parts, T c0, T c1, T c2, const Chunk* chunk, T* X_at, const T* A_from, T* A_to) {
+__global__ void __launch_bounds__((64 * kWaves), (kOrthWaves<T, kS, kWaves>)) k_orth_step(OrthArgs a, int64_t first, int chunks, int parts, T c0, T c1, T c2, const Size* chunk, T* X_at, const T* A_from, T* A_to) {
   using Cols = Columns<T, kS, NT, kWaves>;
   __shared__ typename Cols::Lds S;
   const int64_t matrix = first + blockIdx.x / chunks, place = matrix * chunks + blockIdx.x % chunks;
@@ -640,12 +706,12 @@ __global__ void __launch_bounds__((64 * kWaves), (kOrthWaves<T, kS, kWaves>)) k_
   X.take(X_at + place * (kS * Cols::kWide));
   typename Cols::Gram A;
   A_from += matrix * parts * (kS * kS);
-  const double scale = chunk ? scale_of(chunk + matrix * chunks, chunks, a.eps) : 1;
-  if (chunk) X.scale(scale / chunk[place].power);
+  const Scale scale = chunk ? scale_of(chunk + matrix * chunks, chunks, a.eps) : Scale{1, 1};
+  if (chunk) X.scale(scale.of(chunk[place].power));
   if (Cols::forms_gram()) {
     if (chunk && parts == chunks) {
       A.add_all(A_from, parts, [&](int p) {
-        const double f = scale / chunk[matrix * chunks + p].power;
+        const double f = scale.of(chunk[matrix * chunks + p].power);
         return (T)(f * f);
       });
     } else {
@@ -669,16 +735,16 @@ __global__ void __launch_bounds__((64 * kWaves), (kOrthWaves<T, kS, kWaves>)) k_
 // to [matrix][size] = sums of from [matrix][parts][size]; chunk: of the first step.  32 numbers a workgroup (size is a multiple of them), eighths of the parts one after
 // another: 157 shares of 32 x 32 numbers 7 us.
 template <class T>
-__global__ void __launch_bounds__(kProductThreads) k_orth_join(OrthArgs a, int64_t first, int blocks, int parts, int size, const Chunk* chunk, const T* from, T* to) {
+__global__ void __launch_bounds__(kProductThreads) k_orth_join(OrthArgs a, int64_t first, int blocks, int parts, int size, const Size* chunk, const T* from, T* to) {
   __shared__ T sums[8][32];
   const int64_t matrix = first + blockIdx.x / blocks;
   const int i = threadIdx.x % 32, group = threadIdx.x / 32, at = blockIdx.x % blocks * 32 + i;
-  const double scale = chunk ? scale_of(chunk + matrix * parts, parts, a.eps) : 0;
+  const Scale scale = chunk ? scale_of(chunk + matrix * parts, parts, a.eps) : Scale{1, 1};
   from += matrix * parts * size + at;
   T v = 0;
 #pragma unroll 8
   for (int p = parts * group / 8; p < parts * (group + 1) / 8; ++p) {
-    const double f = chunk ? scale / chunk[matrix * parts + p].power : 1;
+    const double f = chunk ? scale.of(chunk[matrix * parts + p].power) : 1;
     v += (T)(f * f) * from[(int64_t)p * size];
   }
   sums[group][i] = v;
@@ -780,10 +846,10 @@ size_t workspace_bytes(int64_t batch, int64_t m, int64_t n) {
   if (std::min(m, n) <= kMostRows) {
     const Few f(m, n, sizeof(T) == 8);
     if (f.chunks == 1) return 0;
-    return up(batch * f.chunks * sizeof(Chunk)) + up(batch * f.x_size() * sizeof(T)) + 2 * up(batch * f.a_size() * sizeof(T)) + up(batch * f.sum_size() * sizeof(T));
+    return up(batch * f.chunks * sizeof(Size)) + up(batch * f.x_size() * sizeof(T)) + 2 * up(batch * f.a_size() * sizeof(T)) + up(batch * f.sum_size() * sizeof(T));
   }
   const Many<T> f(batch, m, n);
-  return up(batch * shares_of(m, n) * sizeof(double)) + 4 * up(batch * f.x_size()) + 2 * up(batch * f.a_size()) + up(batch * f.results() * sizeof(T));
+  return up(batch * shares_of(m, n) * sizeof(Size)) + 4 * up(batch * f.x_size()) + 2 * up(batch * f.a_size()) + up(batch * f.results() * sizeof(T));
 }
 
 template <class T, int kTile>
@@ -804,8 +870,8 @@ template <class T>
 hipError_t many_rows(const OrthArgs& a, const double* coefficients, int steps, char* ws, hipStream_t st) {
   const Many<T> f(a.batch, a.m, a.n);
   const int shares = shares_of(a.m, a.n), s = (int)f.s, l = (int)f.l;
-  double* part = (double*)ws;
-  auto next = [&, at = ws + up(a.batch * shares * sizeof(double))](size_t bytes) mutable {
+  Size* part = (Size*)ws;
+  auto next = [&, at = ws + up(a.batch * shares * sizeof(Size))](size_t bytes) mutable {
     char* p = at;
     at += up(a.batch * bytes);
     return p;
@@ -840,8 +906,8 @@ hipError_t few_rows(const OrthArgs& a, const double* coefficients, int steps, ch
   if constexpr (sizeof(T) == 4 && kWide == 64) return hipErrorInvalidValue;      // more than 64 columns go by 128
   else {
   const int chunks = (int)f.chunks;
-  Chunk* chunk = (Chunk*)ws;
-  T* X = (T*)(ws + up(a.batch * chunks * sizeof(Chunk)));
+  Size* chunk = (Size*)ws;
+  T* X = (T*)(ws + up(a.batch * chunks * sizeof(Size)));
   T* A = (T*)((char*)X + up(a.batch * f.x_size() * sizeof(T)));
   T* next = (T*)((char*)A + up(a.batch * f.a_size() * sizeof(T)));
   T* sum = (T*)((char*)next + up(a.batch * f.a_size() * sizeof(T)));
@@ -849,7 +915,7 @@ hipError_t few_rows(const OrthArgs& a, const double* coefficients, int steps, ch
   for (int i = 0; i < steps && e == hipSuccess; ++i) {
     const double* c = coefficients + 3 * i;
     const T* from = A;
-    const Chunk* start = i ? nullptr : chunk;
+    const Size* start = i ? nullptr : chunk;
     int parts = chunks;
     if (f.join) {
       constexpr int kBlocks = kS * kS / 32;
