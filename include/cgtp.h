@@ -407,8 +407,8 @@ cgtp_status grouped_forward(const void* x, const void* W, const void* b, void* o
                             int32_t dtype, void* hip_stream);
 
 /* Gradients of grouped_forward given gout = dE/dout [rows, comps, d_out]: gx [rows, comps, d_in] (rows of no group keep what it holds), gW [groups, d_in,
- * d_out] and, where gb is not NULL (comps = 1), gb [groups, d_out]; zero for groups without rows.  Sums over rows are held in the type
- * and formed in a fixed order (bit-identical from run to run) through `workspace`: caller-owned device memory of at least
+ * d_out] and, where gb is not NULL (comps = 1), gb [groups, d_out]; zero for groups without rows.  Sums over rows are held in the type,
+ * those of gb in fp64 and rounded once, and formed in a fixed order (bit-identical from run to run) through `workspace`: caller-owned device memory of at least
  * cgtp_grouped_workspace_bytes(rows, d_in, d_out, comps, groups, dtype) bytes, 256-byte aligned (CGTP_EINVAL if it is smaller), free again
  * for other work on hip_stream after the call.  The product is linear in x and in W, so that gradients of these gradients are the same
  * calls with other arguments.  No output may overlap an input or another output. */

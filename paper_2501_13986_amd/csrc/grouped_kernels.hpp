@@ -342,7 +342,7 @@ struct WeightsLds {
 };
 
 template <class T, int kR, int kC, bool kWhole, bool kFar>
-__device__ __forceinline__ void sum_weights(const GroupedArgs& a, int64_t first_id, unsigned block, int shift, int row_tiles, int column_tiles, T* part, T* part_b, WeightsLds<T, kR, kC, kFar>& S) {
+__device__ __forceinline__ void sum_weights(const GroupedArgs& a, int64_t first_id, unsigned block, int shift, int row_tiles, int column_tiles, T* part, double* part_b, WeightsLds<T, kR, kC, kFar>& S) {
   auto& R = S.R;
   auto& C = S.C;
   auto& table = S.table;
@@ -355,7 +355,10 @@ __device__ __forceinline__ void sum_weights(const GroupedArgs& a, int64_t first_
   AcrossTerms<T, kR, kWhole> x(k0, K);
   AcrossTerms<T, kC, kWhole> t(c0, n);
   Results<T, kR, kC> out;
-  T sum[kC / 64] = {};
+  // gb is summed in fp64 and rounded once: in fp32 each row would round the sum of those before it (root mean square error of 160 710 normal
+  // rows 4.5e-7, so 2.5e-8), for 1 % of the time of the kernel
+  const bool add_b = a.gb && k0 == 0;
+  double sum[kC / 64] = {};
   // the position and component of the wave's first term; all of it is the wave's own
   unsigned position = (unsigned)lo + x.term() / comps;      // below 2^31 but for steps behind the end
   int component = x.term() % comps;
@@ -396,11 +399,11 @@ __device__ __forceinline__ void sum_weights(const GroupedArgs& a, int64_t first_
     x.put(R);
     t.put(C);
     __syncthreads();
-    if (a.gb)
+    if (add_b)
 #pragma unroll
       for (int i = 0; i < kC / 64; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) sum[i] += t.v[j][i];
+        for (int j = 0; j < 8; ++j) sum[i] += (double)t.v[j][i];
     if (more) fetch_next();
     out.multiply(R, C);
   };
@@ -454,24 +457,24 @@ __device__ __forceinline__ void sum_weights(const GroupedArgs& a, int64_t first_
       for (int i = 0; i < 4; ++i) v[i] = out.acc[rt][ct][i];
       if (k < K && c < n) store_some(to + (int64_t)k * n + c, v, n - c);
     }
-  if (!a.gb || k0 > 0) return;
+  if (!add_b) return;
   // the waves' terms, one after another
   __syncthreads();
-  T* sums = (T*)&C;      // [4][kC]
+  double* sums = (double*)&C;      // [4][kC]
 #pragma unroll
   for (int i = 0; i < kC / 64; ++i) sums[x.term() / 8 * kC + t.place() + i] = sum[i];
   __syncthreads();
-  T* to_b = whole ? (T*)a.gb + g * a.d_out : part_b + slot * a.d_out;
   for (int c = threadIdx.x; c < kC && c0 + c < n; c += kProductThreads) {
-    T v = 0;
+    double v = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) v += sums[j * kC + c];
-    to_b[c0 + c] = v;
+    if (whole) ((T*)a.gb)[g * a.d_out + c0 + c] = (T)v;
+    else part_b[slot * a.d_out + c0 + c] = v;
   }
 }
 
 template <class T, int kR, int kC, bool kWhole, bool kFar>
-__global__ void __launch_bounds__(kProductThreads, 2) k_grouped_weights(GroupedArgs a, int64_t first_id, int shift, int row_tiles, int column_tiles, T* part, T* part_b) {
+__global__ void __launch_bounds__(kProductThreads, 2) k_grouped_weights(GroupedArgs a, int64_t first_id, int shift, int row_tiles, int column_tiles, T* part, double* part_b) {
   __shared__ WeightsLds<T, kR, kC, kFar> S;
   sum_weights<T, kR, kC, kWhole, kFar>(a, first_id, on_one_die(blockIdx.x, gridDim.x), shift, row_tiles, column_tiles, part, part_b, S);      // neighbours read the same rows
 }
@@ -485,18 +488,17 @@ union BackLds {
 };
 
 template <class T, int kC, int kIn, bool kWhole>
-__global__ void __launch_bounds__(kProductThreads, 2) k_grouped_back(GroupedArgs a, int split, int chunk_shift, int row_tiles, int column_tiles, T* part, T* part_b, int x_tiles, int shift) {
+__global__ void __launch_bounds__(kProductThreads, 2) k_grouped_back(GroupedArgs a, int split, int chunk_shift, int row_tiles, int column_tiles, T* part, double* part_b, int x_tiles, int shift) {
   __shared__ BackLds<T, kC, kIn> S;
   if ((int)blockIdx.x < split) sum_weights<T, 64, kC, kWhole, false>(a, 0, blockIdx.x, chunk_shift, row_tiles, column_tiles, part, part_b, S.weights);
   else stream_lines<T, kIn, 1, kWhole, true>(a, 0, blockIdx.x - split, x_tiles, shift, S.lines);
 }
 
 // Adds up, in a fixed order, the chunks of the groups that have several: of group `at` (of_groups), or of the one that begins in chunk `at` and goes on behind it, whichever are
-// fewer.  V numbers a thread; kParts: so many shares of the chunks are added up by threads of their own, where a matrix has too few numbers for the latency of its
+// fewer.  V numbers of gW a thread (of gb one, its sums are held in fp64); kParts: so many shares of the chunks are added up by threads of their own, where a matrix has too few numbers for the latency of its
 // chunks (10 000 x 32 x 64 fp32, 157 chunks: 4.1 us in eight shares, 7.0 in one; 160 710 x 64 x 2176 32 and 20).
 template <class T, int V, int kParts>
-__global__ void __launch_bounds__(kProductThreads) k_grouped_sums(GroupedArgs a, int64_t first, int shift, int blocks, bool of_groups, const T* part, const T* part_b) {
-  typedef T Words __attribute__((ext_vector_type(V)));
+__global__ void __launch_bounds__(kProductThreads) k_grouped_sums(GroupedArgs a, int64_t first, int shift, int blocks, bool of_groups, const T* part, const double* part_b) {
   const int64_t at = first + blockIdx.x / blocks;
   int64_t lo = at;
   if (!of_groups) {
@@ -517,31 +519,37 @@ __global__ void __launch_bounds__(kProductThreads) k_grouped_sums(GroupedArgs a,
   const int64_t from = cut(a, lo), end = cut(a, lo + 1), chunk = from >> shift, last = (end - 1) >> shift;
   if (end <= from || last <= chunk || (!of_groups && chunk != at)) return;
   constexpr int kSide = kProductThreads / kParts;
-  __shared__ Words sums[kParts][kSide];
-  const int64_t size = a.d_in * a.d_out, all = (size + (a.gb ? a.d_out : 0)) / V, many = last - chunk + 1;
+  __shared__ alignas(32) char lds[kProductThreads * std::max(V * sizeof(T), sizeof(double))];
+  const int64_t size = a.d_in * a.d_out, many = last - chunk + 1;
   const int lane = threadIdx.x % kSide, share = threadIdx.x / kSide;
   const int64_t from_c = many * share / kParts, end_c = many * (share + 1) / kParts;
-  for (int64_t w0 = (int64_t)(blockIdx.x % blocks) * kSide; w0 < all; w0 += (int64_t)blocks * kSide) {
-    const int64_t i = (w0 + lane < all ? w0 + lane : all - 1) * V;
-    const bool b = i >= size;
-    const T* p = b ? part_b + (i - size) : part + i;
-    const int64_t of = b ? a.d_out : size;
+  // words of kN numbers from w0 on, of `count` numbers a slot, whose sums are held in S
+  auto add_up = [&](auto numbers, const auto* from, int64_t count, int64_t w0, T* to) {
+    using S = std::remove_const_t<std::remove_pointer_t<decltype(from)>>;
+    constexpr int kN = decltype(numbers)::value;
+    typedef S Words __attribute__((ext_vector_type(kN)));
+    Words(&sums)[kParts][kSide] = *(Words(*)[kParts][kSide])lds;
+    const int64_t words = count / kN, i = (w0 + lane < words ? w0 + lane : words - 1) * kN;
     Words v = {};
+    const S* p = from + i + 2 * (chunk + from_c) * count;
 #pragma unroll 8
-    for (int64_t c = from_c; c < end_c; ++c) v += *(const Words*)(p + (2 * (chunk + c) + (c == 0)) * of);
+    for (int64_t c = from_c; c < end_c; ++c, p += 2 * count) v += *(const Words*)(p + (c == 0 ? count : 0));
     if constexpr (kParts > 1) {
       __syncthreads();
       sums[share][lane] = v;
       __syncthreads();
-      if (share > 0) continue;
+      if (share > 0) return;
 #pragma unroll
       for (int j = 1; j < kParts; ++j) v += sums[j][lane];
     }
-    if (w0 + lane >= all) continue;
-    T* to = b ? (T*)a.gb + lo * a.d_out + (i - size) : (T*)a.gW + lo * size + i;
+    if (w0 + lane >= words) return;
 #pragma unroll
-    for (int j = 0; j < V; ++j) to[j] = v[j];
-  }
+    for (int j = 0; j < kN; ++j) to[i + j] = (T)v[j];
+  };
+  const int64_t of_w = (size / V + kSide - 1) / kSide, of_b = a.gb ? (a.d_out + kSide - 1) / kSide : 0;
+  int64_t w = blockIdx.x % blocks;
+  for (; w < of_w; w += blocks) add_up(std::integral_constant<int, V>(), part, size, w * kSide, (T*)a.gW + lo * size);
+  for (; w < of_w + of_b; w += blocks) add_up(std::integral_constant<int, 1>(), part_b, a.d_out, (w - of_w) * kSide, (T*)a.gb + lo * a.d_out);
 }
 
 // ---- launches -------------------------------------------------------------------------------------------------------------------
@@ -662,7 +670,7 @@ struct Chunks {
 template <class T>
 size_t workspace_bytes(int64_t rows, int64_t K, int64_t n, int64_t comps) {
   const Chunks<T> c(rows, K, n, comps);
-  return up(c.slots * K * n * sizeof(T)) + up(c.slots * n * sizeof(T));
+  return up(c.slots * K * n * sizeof(T)) + up(c.slots * n * sizeof(double));
 }
 
 template <class T>
@@ -671,7 +679,7 @@ bool weights_near(const GroupedArgs& a, const Chunks<T>& c) {
 }
 
 template <class T, int kR, int kC>
-hipError_t launch_weights(const GroupedArgs& a, const Chunks<T>& c, T* part, T* part_b, hipStream_t st) {
+hipError_t launch_weights(const GroupedArgs& a, const Chunks<T>& c, T* part, double* part_b, hipStream_t st) {
   const bool whole = a.d_in % 4 == 0 && a.d_out % 4 == 0;
   auto go = [&](auto whole, auto far) {
     return in_launches((a.rows >> c.shift) + a.groups, c.row_tiles * c.column_tiles, [&](int64_t first, dim3 grid) {
@@ -689,7 +697,8 @@ template <class T>
 hipError_t backward(const GroupedArgs& a, char* ws, hipStream_t st) {
   const int64_t K = a.d_in, n = a.d_out;
   const Chunks<T> c(a.rows, K, n, a.comps);
-  T *part = (T*)ws, *part_b = (T*)(ws + up(c.slots * K * n * sizeof(T)));
+  T* part = (T*)ws;
+  double* part_b = (double*)(ws + up(c.slots * K * n * sizeof(T)));
   const int64_t x_tiles = (K + 63) / 64;
   const int shift = stream_shift(a.rows * a.comps, x_tiles);
   const int64_t for_weights = ((a.rows >> c.shift) + a.groups) * c.row_tiles * c.column_tiles, for_x = ((a.rows * a.comps >> shift) + a.groups) * x_tiles;
@@ -710,11 +719,11 @@ hipError_t backward(const GroupedArgs& a, char* ws, hipStream_t st) {
   }
   if (e != hipSuccess || c.slots == 0) return e;
   // most chunks have nothing to add up, so that they get few workgroups
-  const bool of_groups = a.groups <= c.count - 1, wide = n % 4 == 0 && aligned16(a.gW) && aligned16(a.gb);
-  const int64_t pieces = of_groups ? a.groups : c.count - 1, numbers = (K * n + n) / (wide ? 4 : 1);
+  const bool of_groups = a.groups <= c.count - 1, wide = n % 4 == 0 && aligned16(a.gW);
+  const int64_t pieces = of_groups ? a.groups : c.count - 1, numbers = K * n / (wide ? 4 : 1), numbers_b = a.gb ? n : 0;
   auto go = [&](auto wide_, auto parts) {
     constexpr int V = decltype(wide_)::value, kParts = decltype(parts)::value, kSide = kProductThreads / kParts;
-    const int64_t blocks = std::max<int64_t>(1, std::min((numbers + kSide - 1) / kSide, std::max<int64_t>(16, 16384 / pieces)));
+    const int64_t blocks = std::max<int64_t>(1, std::min((numbers + kSide - 1) / kSide + (numbers_b + kSide - 1) / kSide, std::max<int64_t>(16, 16384 / pieces)));
     return in_launches(pieces, blocks, [&](int64_t first, dim3 grid) {
       k_grouped_sums<T, V, kParts><<<grid, kProductThreads, 0, st>>>(a, first, c.shift, (int)blocks, of_groups, part, part_b);
     });
