@@ -397,8 +397,9 @@ cgtp_status norm_backward(const cgtp_norm* norm, const void* x, const void* weig
  * lies between them is not touched.  ptr (int64 device array [groups+1], not decreasing) and perm (int64 device array [rows], no
  * row twice) are what cgtp_csr_from_coo makes of the kinds as receivers (row_ptr and perm).  Rows of positions in front of ptr[0] and from ptr[groups]
  * on belong to no group and keep what out holds there.  Numbers of ptr outside [0, rows] are taken for the nearest one
- * inside; where ptr decreases the results are unspecified, within the arrays.  Positions whose perm is outside [0, rows) are left out; of a row that perm has twice out
- * holds one of the results.
+ * inside; where ptr decreases the results are unspecified, within the arrays.  Positions whose perm is outside [0, rows) are left out.  Where perm
+ * has a row twice, each number of the row in out (and gx) is that of one of its positions, which one may differ from number to number and from run to
+ * run; gW and gb count all its positions.
  * Pointers have to be aligned to their type alone.  Sums over d_in are held in the type; fp32 products as in gated_forward, with its limits at
  * infinite and smallest numbers.  Allocates nothing; no workspace; deterministic.  rows * comps < 2^31; comps up to 1024, groups up
  * to 2^24, d_in and d_out from 1 to 2^20, their product below 2^31; strides below 2^31.  out must not overlap an input. */
