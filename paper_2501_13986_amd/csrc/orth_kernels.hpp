@@ -56,15 +56,15 @@ __device__ inline Scale scale_of(const Size* part, int parts, double eps) {
   return {power, 1.0 / (sqrt(v) + eps * power)};
 }
 
-// part [batch][shares]: of shares of the rows
+// part [batch][shares]: of shares of the rows, for matrices of more than 128 rows and columns
 template <class T>
 __global__ void __launch_bounds__(kProductThreads) k_orth_squares(OrthArgs a, int64_t first, int shares, Size* part) {
   __shared__ double sums[2][kProductThreads / 64];
   const int64_t matrix = first + blockIdx.x / shares, share = blockIdx.x % shares;
   const T* g = (const T*)a.g + matrix * a.stride_g;
   const int64_t from = a.m * share / shares, end = a.m * (share + 1) / shares;
-  // as many lanes side by side as a row has numbers, eight numbers on their way to a thread
-  const int wide = a.n >= kProductThreads ? kProductThreads : a.n > 64 ? 128 : a.n > 16 ? 64 : 16, x = threadIdx.x % wide, y = threadIdx.x / wide, high = kProductThreads / wide;
+  // rows have more than 128 numbers; eight numbers on their way to a thread
+  const int wide = a.n >= kProductThreads ? kProductThreads : 128, x = threadIdx.x % wide, y = threadIdx.x / wide, high = kProductThreads / wide;
   auto each = [&](auto f) {
     for (int64_t r = from + y; r < end; r += high) {
       const T* p = g + r * a.ld_g;
