@@ -216,8 +216,10 @@ __global__ void __launch_bounds__(kProductThreads, 2) k_grouped_stream(GroupedAr
 
 // ---- rows times a matrix ------------------------------------------------------------------------------------------------------
 
-// kR lines x kC columns of out = x W + b (forward) or of gx = gout W^T (kBack), the terms 32 at a time: for more than 128 terms, and where lines lie far apart.  160 710 x 2176 -> 64 fp32
-// 340 us (4.2 TB/s; pipe busy 38 % of the cycles, vector instructions, half of them cuts into parts, issue in 41 %), 60 710 x 200 -> 800 151 us (129 TFLOP/s), fp64 30 000 x 200 -> 200 76 us (32 TFLOP/s, library 73).  kFar: rows lie 2^31 bytes apart or more, or the matrix is as large.
+// kR lines x kC columns of out = x W + b (forward) or of gx = gout W^T (kBack), the terms 32 at a time: for more than 128 terms, and where
+// lines lie far apart.  160 710 x 2176 -> 64 fp32 340 us (4.2 TB/s; pipe busy 38 % of the cycles, vector instructions, half of them cuts into
+// parts, issue in 41 %), 60 710 x 200 -> 800 151 us (129 TFLOP/s), fp64 30 000 x 200 -> 200 76 us (32 TFLOP/s, library 73; LDS conflicts in
+// 40 % of its cycles).  kFar: rows lie 2^31 bytes apart or more, or the matrix is as large.
 template <class T, int kR, int kC, bool kWhole, bool kBack, bool kFar>
 __global__ void __launch_bounds__(kProductThreads, 2) k_grouped_rows(GroupedArgs a, int64_t first_id, int column_tiles) {
   using Rows = AlongTerms<T, kR, kWhole>;
@@ -329,8 +331,9 @@ __global__ void __launch_bounds__(kProductThreads, 2) k_grouped_rows(GroupedArgs
 // kR x kC numbers of gW[g] (and kC of gb[g]) over the positions of group g in one chunk: chunks are the same for all groups, so that those of a group that has several
 // leave their sums at slot 2 chunk + (0: the group began before the chunk, 1: in it).  A group with one chunk, or without rows, is
 // written at once.
-// The lines' offsets stand in LDS, formed once for all waves (160 710 x 64 x 2176 fp32: 710 us with addresses formed by each thread, 420 to 430 so and in chunks of 1024; pipe busy
-// 31 % of the cycles, vector instructions 38, LDS 26; the library's rate for its products is 246).  20 000 x 7 x 128 x 128: 46 us, 3.1 TB/s of its two inputs, in 330 x 2 workgroups, fewer than three a unit.
+// The lines' offsets stand in LDS, formed once for all waves (160 710 x 64 x 2176 fp32: 710 us with addresses formed by each thread, 420 to 430
+// so and in chunks of 1024; pipe busy 31 % of the cycles, vector instructions 38, LDS 26; the library's rate for its products is 246).
+// 20 000 x 7 x 128 x 128: 46 us, 3.1 TB/s of its two inputs, in 330 x 2 workgroups, fewer than three a unit.
 constexpr int kTable = 512;      // lines whose offsets stand in LDS at a time
 
 // kFar: rows of x or gout lie 2^31 bytes apart or more, addresses are formed for each.
@@ -342,7 +345,8 @@ struct WeightsLds {
 };
 
 template <class T, int kR, int kC, bool kWhole, bool kFar>
-__device__ __forceinline__ void sum_weights(const GroupedArgs& a, int64_t first_id, unsigned block, int shift, int row_tiles, int column_tiles, T* part, double* part_b, WeightsLds<T, kR, kC, kFar>& S) {
+__device__ __forceinline__ void sum_weights(const GroupedArgs& a, int64_t first_id, unsigned block, int shift, int row_tiles, int column_tiles,
+                                            T* part, double* part_b, WeightsLds<T, kR, kC, kFar>& S) {
   auto& R = S.R;
   auto& C = S.C;
   auto& table = S.table;
@@ -494,9 +498,11 @@ __global__ void __launch_bounds__(kProductThreads, 2) k_grouped_back(GroupedArgs
   else stream_lines<T, kIn, 1, kWhole, true>(a, 0, blockIdx.x - split, x_tiles, shift, S.lines);
 }
 
-// Adds up, in a fixed order, the chunks of the groups that have several: of group `at` (of_groups), or of the one that begins in chunk `at` and goes on behind it, whichever are
-// fewer.  V numbers of gW a thread (of gb one, its sums are held in fp64); kParts: so many shares of the chunks are added up by threads of their own, where a matrix has too few numbers for the latency of its
-// chunks (10 000 x 32 x 64 fp32, 157 chunks: 4.1 us in eight shares, 7.0 in one; 160 710 x 64 x 2176 32 and 20).
+// Adds up, in a fixed order, the chunks of the groups that have several: of group `at` (of_groups), or of the one that begins in chunk `at` and
+// goes on behind it, whichever are fewer.  V numbers of gW a thread (of gb one, its sums are held in fp64); kParts: so many shares of the chunks
+// are added up by threads of their own, where a matrix has too few numbers for the latency of its chunks (10 000 x 32 x 64 fp32, 157 chunks:
+// 4.1 us in eight shares, 7.0 in one; 160 710 x 64 x 2176 32 and 20).  Addresses are stepped by sums: multiplied out for all eight loads on
+// their way they cost 1.4 of 6.4 us (20 000 x 7 x 128 x 128).
 template <class T, int V, int kParts>
 __global__ void __launch_bounds__(kProductThreads) k_grouped_sums(GroupedArgs a, int64_t first, int shift, int blocks, bool of_groups, const T* part, const double* part_b) {
   const int64_t at = first + blockIdx.x / blocks;

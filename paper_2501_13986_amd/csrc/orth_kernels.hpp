@@ -17,7 +17,9 @@ constexpr int kShares = 256;      // partial sums of squares of a matrix, at mos
 
 // ---- the start ------------------------------------------------------------------------------------------------------------------
 
-// Part of a matrix: the sum of squares of its numbers times `power`, a power of two.
+// Part of a matrix: the sum of squares of its numbers times `power`, a power of two.  With the power, fp64 numbers of any size serve: unscaled, squares
+// of those below 1e-154 are lost and of those above 1e154 overflow.  It costs 0.5 us of a launch for all steps (32 x 32 12.0), 3 of the start of tiles
+// (4 of 400 x 400 365); fp32 nothing.
 struct Size {
   double squares, power;
 };
@@ -698,7 +700,8 @@ __global__ void __launch_bounds__((64 * kWaves), (kOrthWaves<T, kS, kWaves>)) k_
 
 // A step.  parts: how many shares of A there are a matrix; chunk: of the first step
 template <class T, int kS, int NT, int kWaves, bool kLast>
-__global__ void __launch_bounds__((64 * kWaves), (kOrthWaves<T, kS, kWaves>)) k_orth_step(OrthArgs a, int64_t first, int chunks, int parts, T c0, T c1, T c2, const Size* chunk, T* X_at, const T* A_from, T* A_to) {
+__global__ void __launch_bounds__((64 * kWaves), (kOrthWaves<T, kS, kWaves>)) k_orth_step(OrthArgs a, int64_t first, int chunks, int parts, T c0, T c1, T c2, const Size* chunk,
+                                                                                             T* X_at, const T* A_from, T* A_to) {
   using Cols = Columns<T, kS, NT, kWaves>;
   __shared__ typename Cols::Lds S;
   const int64_t matrix = first + blockIdx.x / chunks, place = matrix * chunks + blockIdx.x % chunks;
