@@ -68,7 +68,7 @@ def filled(head, rows, piece):
 
 
 # remainders of 64 and of 16 lines, of a workgroup's lines, empty and tiny groups
-HEAD = [64 * 5 + 1, 64 * 7 + 16, 64 * 3 + 17, 0, 1, 1024 * 2, 1024 * 3 + 1, 1024 + 63, 15, 17, 64 * 2 + 48, 0, 64 * 9 + 49]
+HEAD = [64 * 5 + 1, 64 * 7 + 16, 64 * 3 + 17, 0, 1, 1024 * 2, 1024 * 5 + 1, 1024 + 63, 15, 17, 64 * 2 + 48, 0, 64 * 9 + 49]
 # rows, K, n, comps: workgroups of 1024 lines forward, for each number of parts of the matrix that a wave may keep
 STREAM = [(1_050_003, 8, 12, 1), (150_003, 9, 13, 7), (530_003, 40, 65, 1), (1_050_003, 70, 3, 1), (1_050_003, 128, 5, 1)]
 # full tiles: more than 128 terms, forward or backward
