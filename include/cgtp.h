@@ -422,11 +422,12 @@ cgtp_status grouped_backward(const void* x, const void* W, const void* gout, voi
  *     X = G / (|G| + eps), |G| the root of the sum of squares;  then for each of `steps` triples a, b, c of `coefficients`
  *     X <- a X + (b A + c A A) X,  A = X X^T,
  * and out = X.  coefficients: host array [steps, 3], read before the call returns; steps from 1 to 64.  ld_g and ld_out are the elements
- * from one row of a matrix to the next, stride_g and stride_out from one matrix to the next; matrices of out must not overlap.  A matrix of zeros gives zeros;
- * one with a number that is not finite gives NaN in it alone.  The sum of squares is held in fp64, that of fp64 numbers
- * under a power of two, so that numbers of any size serve; all other sums are held in the type; fp32 products as in gated_forward.  The gradients that
- * grouped_backward and gated_backward write are such batches.  `workspace` as above, of cgtp_orthogonalise_workspace_bytes(batch, m, n, dtype) bytes.  Allocates nothing; deterministic: the same call
- * gives the same bits, and a matrix of at most 128 rows or columns those that it gives alone (with more, how sums are split depends on batch).
+ * from one row of a matrix to the next, stride_g and stride_out from one matrix to the next; matrices of out must not overlap.  A matrix of zeros
+ * gives zeros; one with a number that is not finite gives NaN in it alone.  The sum of squares is held in fp64, that of fp64 numbers under a power
+ * of two, so that numbers of any size serve; all other sums are held in the type; fp32 products as in gated_forward.  The gradients that
+ * grouped_backward and gated_backward write are such batches.  `workspace` as above, of cgtp_orthogonalise_workspace_bytes(batch, m, n, dtype)
+ * bytes.  Allocates nothing; deterministic: the same call gives the same bits, and a matrix of at most 128 rows or columns those that it gives
+ * alone (with more, how sums are split depends on batch).
  * m, n and row strides below 2^22, m n and batch below 2^31, batch m n at most 2^40.  out must not overlap g. */
 size_t cgtp_orthogonalise_workspace_bytes(int64_t batch, int64_t m, int64_t n, int32_t dtype);
 cgtp_status orthogonalise(const void* g, void* out, int64_t batch, int64_t m, int64_t n, int64_t ld_g, int64_t ld_out, int64_t stride_g,
